@@ -344,6 +344,83 @@ qp_status qp_decode_attn_layers_ex(int n_layers, const void* const* q, const qp_
                                    size_t workspace_bytes, void* stream);
 
 /*
+ * Keeping a cache at a fixed budget by accumulated attention weight.  (The paper names H2O among its pruning methods, Sec. 4
+ * and Table 1, and defines none of them; the rules here are these.)  W[b,k,t] is the attention weight token t has received so
+ * far from the queries of KV head k's G query heads, fp32, one array per layer beside the cache:
+ *   prompt      qp_prompt_weights  (once, or chunk by chunk)  ->  qp_heavy_select  ->  qp_gather_quantize(_ex)
+ *   each step   qp_evict_kv (the new token's row takes a place in the full cache)  ->  qp_decode_attn_weights
+ * A single token can only be replaced where no group spans several tokens: these calls take 16-bit caches and caches with
+ * per-token keys (qp_strategy.k_axis = 1, no filtering), not the main path's per-channel keys.
+ */
+
+/*
+ * Attention weight the keys of a prompt have received from n_q query rows.  Query row i stands at position p = q_start + i and
+ * sees the keys j <= p:   S = q[h,i].k[j] / sqrt(D);   Pr = softmax_j(S);   W[b,k,j] = sum_{h of k} sum_i Pr_{h,i}[j].
+ * Q bf16 [Bt,Hq,n_q,D], K bf16 [Bt,Hkv,L,D], weights fp32 [Bt,Hkv,L] (device), 0 <= q_start, 1 <= n_q, q_start + n_q <= L.
+ * A whole prompt is q_start = 0, n_q = L; a prompt taken in by chunks is one call per chunk.  accumulate = 0: weights of
+ * positions below q_start + n_q are set, those behind are set to 0.  accumulate != 0: they are added to, and the positions
+ * behind are left as they are.  Keys at and behind q_start + n_q are not looked at and may hold anything.
+ * The error word of the bounded waits (see qp_window_scores) is at byte offset qp_prompt_weights_workspace_bytes(...) - 256.
+ */
+size_t qp_prompt_weights_workspace_bytes(int batch, int n_q_heads, int n_kv_heads, int head_dim, int L, int q_start, int n_q);
+qp_status qp_prompt_weights(const void* Q, const void* K, int batch, int n_q_heads, int n_kv_heads, int head_dim, int L,
+                            int q_start, int n_q, int accumulate, float* weights, void* workspace, size_t workspace_bytes,
+                            void* stream);
+
+/*
+ * Prompt form of the eviction: of the L - w positions before the last w the n_keep - w with the largest weight are kept (equal
+ * weights: the lower position), the last w always are.  weights fp32 [Bt,Hkv,L] (device, no NaN) ->
+ * kept_idx int32 [Bt,Hkv,n_keep] ascending; and, unless NULL, the state of a cache filled with these tokens in this order:
+ * kept_weights fp32 [Bt,Hkv,n_cap], kept_pos int32 [Bt,Hkv,n_cap] (slots n_keep .. n_cap-1 are set to 0).  n_cap >= n_keep.
+ */
+qp_status qp_heavy_select(const float* weights, int batch, int n_kv_heads, int L, int w, int n_keep, int n_cap,
+                          int32_t* kept_idx, float* kept_weights, int32_t* kept_pos, void* stream);
+
+/*
+ * qp_decode_attn for a cache whose tokens' weights are accumulated: the same output, and
+ *   weights[b,k,t] += sum over the G query heads of k of their softmax weight of token t,   t < n_keep
+ * (fp32 [Bt,Hkv,n_cap], device, in place; slots behind n_keep are left as they are).  strategy: NULL for a 16-bit cache, else
+ * k_axis = 1 and no filtering (QP_ERR_UNSUPPORTED otherwise).  Queries enter the tensor cores unscaled: |q| <= 65504 and, for
+ * B < 16, max|V| <= 4096.  Runs in plain stream order.
+ */
+size_t qp_decode_weights_workspace_bytes(const qp_cache* cache /* host */);
+qp_status qp_decode_attn_weights(const void* q, const qp_cache* cache /* host */, const qp_strategy* strategy /* host */,
+                                 float* weights, void* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Single-token form of the eviction: the key/value rows of the new token, k_new, v_new bf16 [Bt,Hkv,D], take a slot of the
+ * cache, each KV head its own.  A 16-bit cache with room (n_keep < n_cap) gives slot n_keep, and n_keep grows by 1; otherwise
+ * the slot is that of the token with the smallest weight among those with pos <= new_pos - recent (equal weights: the lower
+ * slot); if there is none, that of the token with the smallest pos (equal: the lower slot).  Per-token caches never grow here.
+ * The row is stored as qp_gather_quantize_ex would store it, but that the quotient (m - z)/(2^B - 1) is taken as the 32-bit
+ * product with the rounded reciprocal before it is rounded up to fp16 (the stored scale may differ in its last place);
+ * weights[slot] = 0, pos[slot] = new_pos, and, unless NULL,
+ * slots int32 [Bt,Hkv] = slot.  weights fp32, pos int32 [Bt,Hkv,n_cap] (device, in place; weights without NaN).
+ * new_pos >= 0, recent >= 0.  strategy as for qp_decode_attn_weights.  new_pos and n_keep are host values: a captured call
+ * stands for the step it was captured at.
+ */
+qp_status qp_evict_kv(const void* k_new, const void* v_new, qp_cache* cache /* host, in/out */,
+                      const qp_strategy* strategy /* host */, float* weights, int32_t* pos, int new_pos, int recent,
+                      int32_t* slots, void* stream);
+
+/*
+ * Attention of a tree of T drafted tokens over the cache (speculative decoding: all drafts are verified with one pass over the
+ * packed bytes).  Draft i sees every cached token, every token of the tail, and the drafts j whose bit j is set in mask[b,i]
+ * (its ancestors and itself; any set of bits is allowed, none included):
+ *   out[b,i,h] = softmax over those tokens of (q[b,i,h].k / sqrt(D)), times their values
+ * q, out bf16 [Bt,T,Hq,D]; k_draft, v_draft bf16 [Bt,T,Hkv,D]; mask uint64 [Bt,T]; 1 <= T <= QP_MAX_DRAFTS.  The drafts' rows
+ * need not be in the cache; accepted ones are appended with qp_append_kv.  tail: NULL or as for qp_decode_attn_tail.
+ * strategy: NULL (per-channel keys, or 16 bit) or k_axis 0 / 1 without filtering.  Any bits.  For B < 16 keys and values,
+ * drafts and tail included, are multiplied in fp16 (|x| <= 65504).  Plain stream order.  The error word of the bounded waits
+ * (see qp_window_scores) is at byte offset qp_decode_tree_workspace_bytes(...) - 256.
+ */
+#define QP_MAX_DRAFTS 64
+size_t qp_decode_tree_workspace_bytes(const qp_cache* cache /* host */, int T);
+qp_status qp_decode_attn_tree(const void* q, int T, const qp_cache* cache /* host */, const qp_strategy* strategy /* host */,
+                              const qp_tail* tail /* host */, const void* k_draft, const void* v_draft, const uint64_t* mask,
+                              void* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Debug build only (libqp_checked.so, compiled with -DQP_CHECKED; no counterpart in the paper).  In that build
  * every index a kernel reads from DEVICE memory and then uses as an address (the kept positions given to the
  * gather / quantize kernels, the side lists' tile pointers and entries), and every output position the top-k kernels

@@ -648,4 +648,158 @@ qp_status qp_decode_attn(const void* q, const qp_cache* cache, void* out, void* 
   return qp_decode_attn_layers(1, qs, cache, os, workspace, workspace_bytes, stream);
 }
 
+// ---- accumulated attention weights, eviction by them, drafted trees ------------------------------
+
+// strategy of a call on a cache whose tokens can be replaced one by one
+static qp_status check_token_strategy(const qp_strategy* s, const qp_cache* c) {
+  if (c->bits == 16) return s && (s->k_axis != 0 && s->k_axis != 1) ? QP_ERR_INVALID_ARG : QP_OK;   // nothing to choose
+  bool filter = false;
+  if (!s) return QP_ERR_UNSUPPORTED;                          // per-channel key groups span tokens
+  const qp_status r = check_strategy(s, c, &filter);
+  if (r != QP_OK) return r;
+  return filter || s->k_axis != 1 ? QP_ERR_UNSUPPORTED : QP_OK;
+}
+
+static qp_status check_prompt(int batch, int Hq, int Hkv, int D, int L, int q_start, int n_q) {
+  const qp_status s = check_shape(batch, Hq, Hkv, D);
+  if (s != QP_OK) return s;
+  if (L < 1 || q_start < 0 || n_q < 1 || n_q > L || q_start > L - n_q) return QP_ERR_INVALID_ARG;
+  // row coordinates of the tensor maps are 32-bit
+  if ((long long)batch * Hkv * L > 0x7fffffffLL - 1024 || (long long)batch * Hq * n_q > 0x7fffffffLL - 1024 ||
+      (long long)batch * Hkv > 65535 || (long long)batch * Hq > 65535)
+    return QP_ERR_UNSUPPORTED;
+  return QP_OK;
+}
+
+size_t qp_prompt_weights_workspace_bytes(int batch, int n_q_heads, int n_kv_heads, int head_dim, int L, int q_start, int n_q) {
+  if (check_prompt(batch, n_q_heads, n_kv_heads, head_dim, L, q_start, n_q) != QP_OK) return 0;
+  return prompt_workspace(PromptDims{batch, n_q_heads, n_kv_heads, head_dim, L, q_start, n_q});
+}
+
+qp_status qp_prompt_weights(const void* Q, const void* K, int batch, int n_q_heads, int n_kv_heads, int head_dim, int L,
+                            int q_start, int n_q, int accumulate, float* weights, void* workspace, size_t workspace_bytes,
+                            void* stream) {
+  if (!Q || !K || !weights || !workspace) return QP_ERR_INVALID_ARG;
+  const qp_status s = check_prompt(batch, n_q_heads, n_kv_heads, head_dim, L, q_start, n_q);
+  if (s != QP_OK) return s;
+  if (!aligned16(Q) || !aligned16(K) || !aligned16(weights) || !aligned16(workspace)) return QP_ERR_ALIGNMENT;
+  const PromptDims d{batch, n_q_heads, n_kv_heads, head_dim, L, q_start, n_q};
+  if (workspace_bytes < prompt_workspace(d)) return QP_ERR_WORKSPACE;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cache_written(st);                                          // plain order for the stream's next decode call
+  return launch_prompt_weights(Q, K, d, accumulate, weights, workspace, st) == cudaSuccess ? QP_OK : QP_ERR_CUDA;
+}
+
+qp_status qp_heavy_select(const float* weights, int batch, int n_kv_heads, int L, int w, int n_keep, int n_cap,
+                          int32_t* kept_idx, float* kept_weights, int32_t* kept_pos, void* stream) {
+  if (!weights || !kept_idx || batch < 1 || n_kv_heads < 1 || w < 1 || w >= L) return QP_ERR_INVALID_ARG;
+  if (n_keep <= w || n_keep > L || n_cap < n_keep) return QP_ERR_BUDGET;
+  if ((long long)batch * n_kv_heads > 65535) return QP_ERR_UNSUPPORTED;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cache_written(st);
+  const int BH = batch * n_kv_heads;
+  if (launch_heavy_topk(weights, BH, L, w, n_keep, kept_idx, st) != cudaSuccess) return QP_ERR_CUDA;
+  if (!kept_weights && !kept_pos) return QP_OK;
+  return launch_kept_state(weights, kept_idx, BH, L, n_keep, n_cap, kept_weights, kept_pos, st) == cudaSuccess ? QP_OK
+                                                                                                              : QP_ERR_CUDA;
+}
+
+size_t qp_decode_weights_workspace_bytes(const qp_cache* cache) {
+  if (check_cache(cache, false) != QP_OK) return 0;
+  const DecDims d{cache->batch, cache->n_q_heads, cache->n_kv_heads, cache->head_dim, cache->bits, cache->group};
+  return decode_weights_workspace(d, cache_capacity(*cache));
+}
+
+qp_status qp_decode_attn_weights(const void* q, const qp_cache* cache, const qp_strategy* strategy, float* weights, void* out,
+                                 void* workspace, size_t workspace_bytes, void* stream) {
+  if (!q || !cache || !weights || !out || !workspace) return QP_ERR_INVALID_ARG;
+  qp_status s = check_cache(cache, true);
+  if (s != QP_OK) return s;
+  s = check_token_strategy(strategy, cache);
+  if (s != QP_OK) return s;
+  if (!aligned16(q) || !aligned16(weights) || !aligned16(out) || !aligned16(workspace)) return QP_ERR_ALIGNMENT;
+  const qp_cache& c = *cache;
+  if ((long long)c.batch * c.n_kv_heads > 65535) return QP_ERR_UNSUPPORTED;
+  const DecDims d{c.batch, c.n_q_heads, c.n_kv_heads, c.head_dim, c.bits, c.group};
+  if (workspace_bytes < decode_weights_workspace(d, cache_capacity(c))) return QP_ERR_WORKSPACE;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cache_written(st);                                          // plain stream order here and for the next decode call
+  const DecLayer ly{c.k_codes, c.v_codes, static_cast<const __half*>(c.k_scale), static_cast<const __half*>(c.k_zero),
+                    static_cast<const __half*>(c.v_scale), static_cast<const __half*>(c.v_zero), q, out, c.n_keep, 0, 0,
+                    cache_capacity(c)};
+  return launch_decode_weights(ly, d, weights, workspace, st) == cudaSuccess ? QP_OK : QP_ERR_CUDA;
+}
+
+qp_status qp_evict_kv(const void* k_new, const void* v_new, qp_cache* cache, const qp_strategy* strategy, float* weights,
+                      int32_t* pos, int new_pos, int recent, int32_t* slots, void* stream) {
+  if (!k_new || !v_new || !cache || !weights || !pos || new_pos < 0 || recent < 0) return QP_ERR_INVALID_ARG;
+  qp_status s = check_cache(cache, true);
+  if (s != QP_OK) return s;
+  s = check_token_strategy(strategy, cache);
+  if (s != QP_OK) return s;
+  if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(weights) || !aligned16(pos)) return QP_ERR_ALIGNMENT;
+  const qp_cache& c = *cache;
+  const int ns = cache_capacity(c);
+  const bool grow = c.bits == 16 && c.n_keep < ns;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cache_written(st);                                          // arrays the next decode call reads are written
+  const EvictArgs a{static_cast<const uint16_t*>(k_new), static_cast<const uint16_t*>(v_new), c.k_codes, c.v_codes,
+                    static_cast<__half*>(c.k_scale), static_cast<__half*>(c.k_zero), static_cast<__half*>(c.v_scale),
+                    static_cast<__half*>(c.v_zero), weights, pos, slots, (long long)new_pos - recent, c.n_keep, ns,
+                    grow ? c.n_keep : -1, c.head_dim, c.group, c.bits, new_pos};
+  if (launch_evict(a, c.batch * c.n_kv_heads, st) != cudaSuccess) return QP_ERR_CUDA;
+  if (grow) cache->n_keep += 1;
+  return QP_OK;
+}
+
+static TreeArgs tree_args(const qp_cache& c, int T) {
+  TreeArgs a{};
+  a.kc = c.k_codes; a.vc = c.v_codes;
+  a.ks = static_cast<const __half*>(c.k_scale); a.kz = static_cast<const __half*>(c.k_zero);
+  a.vs = static_cast<const __half*>(c.v_scale); a.vz = static_cast<const __half*>(c.v_zero);
+  a.Bt = c.batch; a.Hq = c.n_q_heads; a.Hkv = c.n_kv_heads; a.D = c.head_dim; a.bits = c.bits; a.group = c.group;
+  a.n = c.n_keep; a.ns = cache_capacity(c); a.T = T;
+  return a;
+}
+
+size_t qp_decode_tree_workspace_bytes(const qp_cache* cache, int T) {
+  if (check_cache(cache, false) != QP_OK || T < 1 || T > QP_MAX_DRAFTS) return 0;
+  return tree_workspace(tree_args(*cache, T));
+}
+
+qp_status qp_decode_attn_tree(const void* q, int T, const qp_cache* cache, const qp_strategy* strategy, const qp_tail* tail,
+                              const void* k_draft, const void* v_draft, const uint64_t* mask, void* out, void* workspace,
+                              size_t workspace_bytes, void* stream) {
+  if (!q || !cache || !k_draft || !v_draft || !mask || !out || !workspace || T < 1) return QP_ERR_INVALID_ARG;
+  if (T > QP_MAX_DRAFTS) return QP_ERR_UNSUPPORTED;
+  qp_status s = check_cache(cache, true);
+  if (s != QP_OK) return s;
+  const qp_cache& c = *cache;
+  TreeArgs a = tree_args(c, T);
+  if (strategy && c.bits < 16) {
+    bool filter = false;
+    s = check_strategy(strategy, cache, &filter);
+    if (s != QP_OK) return s;
+    if (filter) return QP_ERR_UNSUPPORTED;
+    a.k_axis = strategy->k_axis;
+  }
+  if (tail && c.bits < 16) {
+    if (tail->n_tail < 0 || tail->n_tail >= c.group) return QP_ERR_INVALID_ARG;
+    if (tail->n_tail > 0) {
+      if (!tail->k_tail || !tail->v_tail) return QP_ERR_INVALID_ARG;
+      if (!aligned16(tail->k_tail) || !aligned16(tail->v_tail)) return QP_ERR_ALIGNMENT;
+      a.n_tail = tail->n_tail; a.k_tail = tail->k_tail; a.v_tail = tail->v_tail;
+    }
+  }
+  if (!aligned16(q) || !aligned16(k_draft) || !aligned16(v_draft) || !aligned16(mask) || !aligned16(out) || !aligned16(workspace))
+    return QP_ERR_ALIGNMENT;
+  if ((long long)c.batch * c.n_kv_heads > 65535) return QP_ERR_UNSUPPORTED;
+  if (workspace_bytes < tree_workspace(a)) return QP_ERR_WORKSPACE;
+  a.k_draft = k_draft; a.v_draft = v_draft; a.q = q; a.out = out;
+  a.mask = reinterpret_cast<const unsigned long long*>(mask);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cache_written(st);                                          // plain stream order here and for the next decode call
+  return launch_tree(a, workspace, st) == cudaSuccess ? QP_OK : QP_ERR_CUDA;
+}
+
 }  // extern "C"

@@ -229,4 +229,42 @@ int decode_mma_wide_workers_per_sm(const DecDims& d, int* min_tiles);
 cudaError_t launch_decode_mma(const DecTable& tab, const DecDims& d, float* partials, cudaStream_t st,
                               bool overlap_prev, const TailTable* tails = nullptr);
 
+// ---- accumulated attention weights and the eviction that goes by them (qp_prompt.cu, qp_weights.cu)
+struct PromptDims {
+  int Bt, Hq, Hkv, D, L, q_start, nq;
+};
+size_t prompt_workspace(const PromptDims& d);   // the last 256 bytes hold the error word
+cudaError_t launch_prompt_weights(const void* Q, const void* K, const PromptDims& d, int accumulate, float* weights, void* ws,
+                                  cudaStream_t st);
+// one layer; ly.ns: slots per (batch, KV head) of the cache and of weights
+size_t decode_weights_workspace(const DecDims& d, int n_cap);
+cudaError_t launch_decode_weights(const DecLayer& ly, const DecDims& d, float* weights, void* ws, cudaStream_t st);
+// selection over the first L - w of every head's L weights, see launch_select_topk
+cudaError_t launch_heavy_topk(const float* weights, int BH, int L, int w, int n_keep, int32_t* kept, cudaStream_t st);
+cudaError_t launch_kept_state(const float* weights, const int32_t* kept, int BH, int L, int n, int cap, float* kw, int32_t* kp,
+                              cudaStream_t st);
+struct EvictArgs {
+  const uint16_t *k_new, *v_new;
+  void *kc, *vc;
+  __half *ks, *kz, *vs, *vz;
+  float* weights;
+  int32_t *pos, *slots;
+  long long limit;          // tokens with pos <= limit may go
+  int n, ns, slot;          // slot: the one to take, or -1 = search
+  int D, g, bits, new_pos;
+};
+cudaError_t launch_evict(const EvictArgs& a, int BH, cudaStream_t st);
+
+// ---- attention of drafted tokens over a cache (qp_tree.cu)
+struct TreeArgs {
+  const void *kc, *vc;
+  const __half *ks, *kz, *vs, *vz;
+  const void *k_tail, *v_tail, *k_draft, *v_draft, *q;
+  const unsigned long long* mask;
+  void* out;
+  int Bt, Hq, Hkv, D, bits, group, k_axis, n, ns, n_tail, T;
+};
+size_t tree_workspace(const TreeArgs& a);       // the last 256 bytes hold the error word
+cudaError_t launch_tree(const TreeArgs& a, void* ws, cudaStream_t st);
+
 }  // namespace qp

@@ -18,12 +18,13 @@ constexpr int TK_THREADS = 1024;
 constexpr int TK_UNROLL = 8;
 constexpr int TKR_BINS = 4096;     // histogram bins of the register kernel's 12-bit digits
 
-// Outputs of the layers of one launch: block (layer, bh) reads scores[(layer * BH + bh) * P ..] and writes
+// Outputs of the layers of one launch: block (layer, bh) reads scores[(layer * BH + bh) * ld ..] and writes
 // kept[layer][bh * n_keep[layer] ..].
 template <int NL>
 struct TopkOut {
   int32_t* kept[NL];
   int n_keep[NL];
+  int ld;                   // floats from one head's scores to the next (P where they are packed)
 };
 
 // monotone map float -> uint32 (larger float = larger integer); -0 is treated as +0
@@ -39,7 +40,7 @@ topk_kernel(const float* __restrict__ scores, int L, int w, int BH, const __grid
   const int layer = blockIdx.x / BH, n_keep = o.n_keep[layer];
   const int P = L - w, k = n_keep - w;
   const int bh = blockIdx.x % BH, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const float* s = scores + (size_t)blockIdx.x * P;
+  const float* s = scores + (size_t)blockIdx.x * o.ld;
   int32_t* out = o.kept[layer] + (size_t)bh * n_keep;
 
   for (int i = tid; i < w; i += TK_THREADS) out[k + i] = P + i;   // window tokens are always kept
@@ -161,7 +162,7 @@ topk_reg_kernel(const float* __restrict__ scores, int L, int w, int BH, const __
   const int layer = blockIdx.x / BH, n_keep = o.n_keep[layer];
   const int P = L - w, k = n_keep - w;
   const int bh = blockIdx.x % BH, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const float* s = scores + (size_t)blockIdx.x * P;
+  const float* s = scores + (size_t)blockIdx.x * o.ld;
   int32_t* out = o.kept[layer] + (size_t)bh * n_keep;
 
   for (int i = tid; i < w; i += TK_THREADS) out[k + i] = P + i;   // window tokens are always kept
@@ -306,7 +307,7 @@ topk_cluster_kernel(const float* __restrict__ scores, int L, int w, int BH, cons
   const int layer = head / BH, n_keep = o.n_keep[layer];
   const int P = L - w, k = n_keep - w;
   const int bh = head % BH, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const float* s = scores + (size_t)head * P;
+  const float* s = scores + (size_t)head * o.ld;
   int32_t* out = o.kept[layer] + (size_t)bh * n_keep;
 
   if (crank == 0)
@@ -508,7 +509,16 @@ cudaError_t launch_select_topk(const float* scores, int BH, int L, int w, int n_
   TopkOut<1> o;
   o.kept[0] = kept;
   o.n_keep[0] = n_keep;
+  o.ld = L - w;
   return launch_topk<1>(scores, BH, BH, L, w, o, st);
+}
+
+cudaError_t launch_heavy_topk(const float* weights, int BH, int L, int w, int n_keep, int32_t* kept, cudaStream_t st) {
+  TopkOut<1> o;
+  o.kept[0] = kept;
+  o.n_keep[0] = n_keep;
+  o.ld = L;
+  return launch_topk<1>(weights, BH, BH, L, w, o, st);
 }
 
 cudaError_t launch_select_topk_layers(int n_layers, const float* scores, int BH, int L, int w, const int* n_keep,
@@ -519,6 +529,7 @@ cudaError_t launch_select_topk_layers(int n_layers, const float* scores, int BH,
     o.kept[l] = kept[l];
     o.n_keep[l] = n_keep[l];
   }
+  o.ld = L - w;
   return launch_topk<QP_MAX_LAYERS>(scores, n_layers * BH, BH, L, w, o, st);
 }
 

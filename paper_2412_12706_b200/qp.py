@@ -19,6 +19,7 @@ LIB_PATH = os.environ.get("QP_LIBRARY") or os.path.join(_HERE, "libqp.so")
 
 QP_OK = 0
 QP_MAX_LAYERS = 128
+QP_MAX_DRAFTS = 64
 STATUS_NAMES = {0: "QP_OK", 1: "QP_ERR_INVALID_ARG", 2: "QP_ERR_UNSUPPORTED", 3: "QP_ERR_BUDGET",
                 4: "QP_ERR_WORKSPACE", 5: "QP_ERR_ALIGNMENT", 6: "QP_ERR_CUDA"}
 
@@ -27,7 +28,9 @@ EXPORTS = ["qp_status_string", "qp_n_keep", "qp_cache_layout", "qp_compress_work
            "qp_compress_layer", "qp_decode_attn", "qp_decode_attn_layers", "qp_decode_attn_static",
            "qp_cache_layout_cap", "qp_append_kv", "qp_append_kv_layers", "qp_decode_attn_tail",
            "qp_decode_attn_tail_layers", "qp_compress_layers", "qp_decode_overlap", "qp_gather_quantize_ex",
-           "qp_decode_attn_ex", "qp_decode_attn_layers_ex", "qp_head_budgets", "qp_head_budgets_workspace_bytes", "qp_debug_check"]
+           "qp_decode_attn_ex", "qp_decode_attn_layers_ex", "qp_head_budgets", "qp_head_budgets_workspace_bytes", "qp_debug_check",
+           "qp_prompt_weights", "qp_prompt_weights_workspace_bytes", "qp_heavy_select", "qp_decode_attn_weights",
+           "qp_decode_weights_workspace_bytes", "qp_evict_kv", "qp_decode_attn_tree", "qp_decode_tree_workspace_bytes"]
 
 
 class QpError(RuntimeError):
@@ -128,6 +131,22 @@ def lib() -> ctypes.CDLL:
         L.qp_debug_check.argtypes = [ctypes.POINTER(ctypes.c_uint32)]
         L.qp_decode_overlap.restype = i
         L.qp_decode_overlap.argtypes = [p, i]
+        L.qp_prompt_weights_workspace_bytes.restype = sz
+        L.qp_prompt_weights_workspace_bytes.argtypes = [i] * 7
+        L.qp_prompt_weights.restype = i
+        L.qp_prompt_weights.argtypes = [p, p] + [i] * 8 + [p, p, sz, p]
+        L.qp_heavy_select.restype = i
+        L.qp_heavy_select.argtypes = [p] + [i] * 6 + [p, p, p, p]
+        L.qp_decode_weights_workspace_bytes.restype = sz
+        L.qp_decode_weights_workspace_bytes.argtypes = [cp]
+        L.qp_decode_attn_weights.restype = i
+        L.qp_decode_attn_weights.argtypes = [p, cp, sp, p, p, p, sz, p]
+        L.qp_evict_kv.restype = i
+        L.qp_evict_kv.argtypes = [p, p, cp, sp, p, p, i, i, p, p]
+        L.qp_decode_tree_workspace_bytes.restype = sz
+        L.qp_decode_tree_workspace_bytes.argtypes = [cp, i]
+        L.qp_decode_attn_tree.restype = i
+        L.qp_decode_attn_tree.argtypes = [p, i, cp, sp, tp, p, p, p, p, p, sz, p]
         _lib = L
     return _lib
 
@@ -584,6 +603,171 @@ def decode_attn_heads(q: torch.Tensor, hc: HeadCaches, out: torch.Tensor | None 
     return out
 
 
+def prompt_weights_workspace_bytes(batch, n_q_heads, n_kv_heads, head_dim, L, q_start, n_q) -> int:
+    return int(lib().qp_prompt_weights_workspace_bytes(batch, n_q_heads, n_kv_heads, head_dim, L, q_start, n_q))
+
+
+def decode_weights_workspace_bytes(cache: "Cache | qp_cache") -> int:
+    return int(lib().qp_decode_weights_workspace_bytes(ctypes.byref(cache.desc if isinstance(cache, Cache) else cache)))
+
+
+def decode_tree_workspace_bytes(cache: "Cache | qp_cache", T: int) -> int:
+    return int(lib().qp_decode_tree_workspace_bytes(ctypes.byref(cache.desc if isinstance(cache, Cache) else cache), T))
+
+
+def _dev(t: torch.Tensor, dtype: torch.dtype, shape: tuple) -> None:
+    assert t.is_cuda and t.dtype == dtype and t.is_contiguous() and tuple(t.shape) == tuple(shape), (t.dtype, t.shape, shape)
+
+
+def _ref(strategy: "Strategy | None"):
+    return None if strategy is None else ctypes.byref(strategy.desc)
+
+
+def _state_shape(cache: Cache) -> tuple:
+    d = cache.desc
+    return d.batch, d.n_kv_heads, d.n_cap or d.n_keep
+
+
+def prompt_weights(Q: torch.Tensor, K: torch.Tensor, q_start: int = 0, weights: torch.Tensor | None = None,
+                   workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """qp_prompt_weights: the attention weight each key of K [Bt,Hkv,L,D] has received from the query rows Q [Bt,Hq,n_q,D] at
+    positions q_start .. q_start+n_q-1, fp32 [Bt,Hkv,L].  Given ``weights`` they are added to (a prompt in chunks)."""
+    _dev_bf16(Q); _dev_bf16(K)
+    Bt, Hkv, L, D = K.shape
+    _, Hq, nq, _ = Q.shape
+    assert Q.shape == (Bt, Hq, nq, D)
+    accumulate = weights is not None
+    if weights is None:
+        weights = torch.empty((Bt, Hkv, L), dtype=torch.float32, device=K.device)
+    _dev(weights, torch.float32, (Bt, Hkv, L))
+    if workspace is None:
+        workspace = torch.empty(max(16, prompt_weights_workspace_bytes(Bt, Hq, Hkv, D, L, q_start, nq)), dtype=torch.uint8,
+                                device=K.device)
+    _check(lib().qp_prompt_weights(_ptr(Q), _ptr(K), Bt, Hq, Hkv, D, L, q_start, nq, 1 if accumulate else 0, _ptr(weights),
+                                   _ptr(workspace), workspace.numel(), _stream()), "qp_prompt_weights")
+    return weights
+
+
+def heavy_select(weights: torch.Tensor, w: int, n_keep_: int, n_cap: int = 0):
+    """qp_heavy_select: weights fp32 [Bt,Hkv,L] -> (kept_idx int32 [Bt,Hkv,n_keep], weights fp32 and positions int32
+    [Bt,Hkv,n_cap] of a cache that holds these tokens)."""
+    Bt, Hkv, L = weights.shape
+    _dev(weights, torch.float32, (Bt, Hkv, L))
+    cap = n_cap or n_keep_
+    kept = torch.empty((Bt, Hkv, n_keep_), dtype=torch.int32, device=weights.device)
+    kw = torch.empty((Bt, Hkv, cap), dtype=torch.float32, device=weights.device)
+    kp = torch.empty((Bt, Hkv, cap), dtype=torch.int32, device=weights.device)
+    _check(lib().qp_heavy_select(_ptr(weights), Bt, Hkv, L, w, n_keep_, cap, _ptr(kept), _ptr(kw), _ptr(kp), _stream()),
+           "qp_heavy_select")
+    return kept, kw, kp
+
+
+def decode_attn_weights(q: torch.Tensor, cache: Cache, weights: torch.Tensor, strategy: "Strategy | None" = None,
+                        out: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """qp_decode_attn_weights: decode attention that adds its softmax weights, summed over a KV head's query heads, to
+    ``weights`` fp32 [Bt,Hkv,n_cap] in place."""
+    d = cache.desc
+    _dev(q, torch.bfloat16, (d.batch, d.n_q_heads, d.head_dim))
+    _dev(weights, torch.float32, _state_shape(cache))
+    if out is None:
+        out = torch.empty_like(q)
+    if workspace is None:
+        workspace = new_decode_workspace(decode_weights_workspace_bytes(cache), q.device)
+    _check(lib().qp_decode_attn_weights(_ptr(q), ctypes.byref(d), _ref(strategy), _ptr(weights), _ptr(out), _ptr(workspace),
+                                        workspace.numel(), _stream()), "qp_decode_attn_weights")
+    return out
+
+
+def evict_kv(k_new: torch.Tensor, v_new: torch.Tensor, cache: Cache, weights: torch.Tensor, pos: torch.Tensor, new_pos: int,
+             recent: int, strategy: "Strategy | None" = None, slots: torch.Tensor | None = None) -> torch.Tensor:
+    """qp_evict_kv: the new token's rows [Bt,Hkv,D] take the slot of the lightest token that is not among the ``recent`` last
+    positions (a 16-bit cache with room grows first); returns the slots int32 [Bt,Hkv].  cache, weights and pos are updated."""
+    d = cache.desc
+    row = (d.batch, d.n_kv_heads, d.head_dim)
+    _dev(k_new, torch.bfloat16, row); _dev(v_new, torch.bfloat16, row)
+    _dev(weights, torch.float32, _state_shape(cache)); _dev(pos, torch.int32, _state_shape(cache))
+    if slots is None:
+        slots = torch.empty(row[:2], dtype=torch.int32, device=k_new.device)
+    _dev(slots, torch.int32, row[:2])
+    _check(lib().qp_evict_kv(_ptr(k_new), _ptr(v_new), ctypes.byref(d), _ref(strategy), _ptr(weights), _ptr(pos), new_pos, recent,
+                             _ptr(slots), _stream()), "qp_evict_kv")
+    return slots
+
+
+@dataclass
+class HeavyCache:
+    """A cache kept at a fixed budget by accumulated attention weight, with its tokens' weights and positions."""
+    cache: Cache
+    strategy: "Strategy | None"
+    weights: torch.Tensor    # fp32 [Bt,Hkv,n_cap]
+    pos: torch.Tensor        # int32 [Bt,Hkv,n_cap]
+    next_pos: int            # position of the next token
+
+
+def compress_layer_heavy(K: torch.Tensor, V: torch.Tensor, Q: torch.Tensor, budget_bits: int, bits: int, group: int = 32,
+                         recent: int = 32, n_cap: int = 0) -> HeavyCache:
+    """The prefill-side path with accumulated weights in place of the observation window: qp_prompt_weights over all queries
+    Q [Bt,Hq,L,D] -> qp_heavy_select -> qp_gather_quantize (16 bit) or qp_gather_quantize_ex with per-token keys."""
+    _dev_bf16(K); _dev_bf16(V); _dev_bf16(Q)
+    Bt, Hkv, L, D = K.shape
+    n = n_keep(budget_bits, bits, group, L, recent)
+    received = prompt_weights(Q, K)
+    kept, weights, pos = heavy_select(received, recent, n, n_cap)
+    cache = alloc_cache(Bt, Q.shape[1], Hkv, D, bits, group, n, K.device, n_cap)
+    strategy = None
+    if bits == 16:
+        gather_quantize(K, V, kept, cache)
+    else:
+        strategy = make_strategy(cache, 1, None)
+        gather_quantize_ex(K, V, kept, cache, strategy)
+    return HeavyCache(cache, strategy, weights, pos, L)
+
+
+def decode_step_heavy(q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, hc: HeavyCache, recent: int = 32,
+                      out: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """One generation step over a HeavyCache: qp_evict_kv, then qp_decode_attn_weights (the new token sees itself)."""
+    evict_kv(k_new, v_new, hc.cache, hc.weights, hc.pos, hc.next_pos, recent, hc.strategy)
+    hc.next_pos += 1
+    return decode_attn_weights(q, hc.cache, hc.weights, hc.strategy, out, workspace)
+
+
+def tree_mask(parents: torch.Tensor) -> torch.Tensor:
+    """Masks of a drafted tree for decode_attn_tree: parents int [Bt,T], parents[b,i] < i the node draft i hangs on, or -1 for
+    the context -> int64 [Bt,T], bit j of mask[b,i] set for i itself and its ancestors."""
+    Bt, T = parents.shape
+    assert 1 <= T <= QP_MAX_DRAFTS
+    i = torch.arange(T, device=parents.device)
+    if not bool(((parents >= -1) & (parents < i)).all()):
+        raise ValueError("every node hangs on an earlier one, or on the context (-1)")
+    own, up = (torch.ones_like(i) << i).expand(Bt, T), parents.long()
+    mask = own.clone()
+    for _ in range(6):                                # after r rounds a mask spans 2^r levels; 2^6 = QP_MAX_DRAFTS
+        above = torch.gather(mask, 1, up.clamp(min=0))
+        mask = torch.where(up >= 0, mask | above, mask)
+        up = torch.where(up >= 0, torch.gather(up, 1, up.clamp(min=0)), up)
+    return mask
+
+
+def decode_attn_tree(q: torch.Tensor, cache: Cache, k_draft: torch.Tensor, v_draft: torch.Tensor, mask: torch.Tensor,
+                     tail: "Tail | None" = None, strategy: "Strategy | None" = None, out: torch.Tensor | None = None,
+                     workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """qp_decode_attn_tree: q [Bt,T,Hq,D], drafts [Bt,T,Hkv,D], mask int64 [Bt,T] (see tree_mask) -> out [Bt,T,Hq,D]."""
+    d = cache.desc
+    T = q.shape[1]
+    _dev(q, torch.bfloat16, (d.batch, T, d.n_q_heads, d.head_dim))
+    for t in (k_draft, v_draft):
+        _dev(t, torch.bfloat16, (d.batch, T, d.n_kv_heads, d.head_dim))
+    _dev(mask, torch.int64, (d.batch, T))
+    if out is None:
+        out = torch.empty_like(q)
+    if workspace is None:
+        workspace = new_decode_workspace(decode_tree_workspace_bytes(cache, T), q.device)
+    _check(lib().qp_decode_attn_tree(_ptr(q), T, ctypes.byref(d), _ref(strategy), None if tail is None else ctypes.byref(tail.desc),
+                                     _ptr(k_draft), _ptr(v_draft), _ptr(mask), _ptr(out), _ptr(workspace), workspace.numel(),
+                                     _stream()), "qp_decode_attn_tree")
+    return out
+
+
 def debug_check() -> tuple[int, list[int]]:
     """qp_debug_check: (status, [1 + site of the first violation or 0, index, limit, violations]); status is
     QP_ERR_UNSUPPORTED (2) unless the loaded library is the range-checked build."""
@@ -618,3 +802,11 @@ qp_append_kv = append_kv
 qp_append_kv_layers = append_kv_layers
 qp_decode_attn_tail = decode_attn_tail
 qp_decode_attn_tail_layers = decode_attn_tail_layers
+qp_prompt_weights = prompt_weights
+qp_prompt_weights_workspace_bytes = prompt_weights_workspace_bytes
+qp_heavy_select = heavy_select
+qp_decode_attn_weights = decode_attn_weights
+qp_decode_weights_workspace_bytes = decode_weights_workspace_bytes
+qp_evict_kv = evict_kv
+qp_decode_attn_tree = decode_attn_tree
+qp_decode_tree_workspace_bytes = decode_tree_workspace_bytes
