@@ -687,7 +687,7 @@ qp_status qp_prompt_weights(const void* Q, const void* K, int batch, int n_q_hea
   if (workspace_bytes < prompt_workspace(d)) return QP_ERR_WORKSPACE;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   cache_written(st);                                          // plain order for the stream's next decode call
-  return launch_prompt_weights(Q, K, d, accumulate, weights, workspace, st) == cudaSuccess ? QP_OK : QP_ERR_CUDA;
+  return launch_prompt_weights(Q, K, d, accumulate, weights, workspace, workspace_bytes, st) == cudaSuccess ? QP_OK : QP_ERR_CUDA;
 }
 
 qp_status qp_heavy_select(const float* weights, int batch, int n_kv_heads, int L, int w, int n_keep, int n_cap,

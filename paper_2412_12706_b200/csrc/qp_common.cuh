@@ -235,7 +235,7 @@ struct PromptDims {
 };
 size_t prompt_workspace(const PromptDims& d);   // the last 256 bytes hold the error word
 cudaError_t launch_prompt_weights(const void* Q, const void* K, const PromptDims& d, int accumulate, float* weights, void* ws,
-                                  cudaStream_t st);
+                                  size_t ws_bytes, cudaStream_t st);
 // one layer; ly.ns: slots per (batch, KV head) of the cache and of weights
 size_t decode_weights_workspace(const DecDims& d, int n_cap);
 cudaError_t launch_decode_weights(const DecLayer& ly, const DecDims& d, float* weights, void* ws, cudaStream_t st);

@@ -1,86 +1,581 @@
-// Attention weight the keys of a prompt have received from its queries.
+// Attention weight the keys of a prompt have received from its queries (qp_prompt_weights).
 //
-// First form: a warp per query row for the normalisers, then a thread per key for the column sums.
-#include "qp_common.cuh"
+//   W[j] = sum over the G query heads h and the rows i with q_start + i >= j of 2^(t[h,i,j] - lse[h,i]),
+//   t = q[h,i].k[j] log2(e) / sqrt(D),   lse[h,i] = log2 sum_{j <= q_start+i} 2^t[h,i,j].
+//
+// A row's normaliser needs all of the row before any column can be summed and the L^2 logits are never stored, so the product
+// Q K^T is formed twice (sweep 1: lse, sweep 2: column sums), each time on the 5th-generation tensor cores.  The bound of a
+// sweep is per 128 x 128 tile of logits: 16384 exponentials, 1024 clocks of the SM's 16-per-clock unit, against 512 clocks of
+// the tensor cores (D = 128) and 32 KB of operand.  From that follow
+//   - one block per SM with FOUR operand tiles resident in shared memory (sweep 1: query tiles; sweep 2: key tiles) and the
+//     other operand streamed past them by TMA, so a streamed tile of 32 KB feeds four tiles of logits: one tile per block of
+//     logits would ask the L2 cache for 15 TB/s;
+//   - four reading groups of four warps, one per resident tile and 128-column tensor-memory buffer.  A thread owns one row of
+//     its resident tile (a query in sweep 1, a key in sweep 2: the operands are swapped), so running sums are thread-local:
+//     no shuffles, no atomics, a fixed order.  While one group waits for its next product the other three compute;
+//   - part of the exponentials evaluated on the FMA pipe (ex2_poly2), two at a time with packed 32-bit arithmetic;
+//   - sweep 1 without a running maximum: a row's reference is renewed only when a chunk's sum leaves the range in which
+//     nothing can overflow, which the sum itself shows.
+// Tiles above the diagonal are skipped, for each group on its own.  The work (a quad of resident tiles x a run of streamed
+// tiles, see Plan) is cut into pieces of nearly equal length; pieces leave partial results that two small kernels add in a
+// fixed order.
+#include <algorithm>
+
+#include "qp_mma.cuh"
+#include "qp_tc.cuh"
 
 namespace qp {
 
 namespace {
 
-__device__ __forceinline__ float dot_bf16(const uint16_t* a, const uint16_t* b, int D) {
-  float s = 0.f;
-  for (int d = 0; d < D; d += 2) {
-    const uint32_t x = *reinterpret_cast<const uint32_t*>(a + d), y = *reinterpret_cast<const uint32_t*>(b + d);
-    s = fmaf(bf16lo(x), bf16lo(y), s);
-    s = fmaf(bf16hi(x), bf16hi(y), s);
+constexpr int PW_GROUPS = 4, PW_STAGES = 3;
+constexpr int PW_READ_WARPS = 4 * PW_GROUPS;
+constexpr int PW_THREADS = (PW_READ_WARPS + 2) * 32;   // + the copy warp and the MMA warp
+constexpr uint32_t PW_TMEM_COLS = 512;
+
+// One sweep's work.  Resident tiles come in quads: sweep 1, tile r of a KV head = query tile r / G of its query head r % G;
+// sweep 2, tile r = keys 128 r ..  A quad's streamed tiles are numbered 0 .. quad_steps - 1 (sweep 1: key tiles from the
+// start; sweep 2: for each query head, the query tiles from the first that sees the quad) and cut into pieces of `chunk`.
+struct Plan {
+  int Hq, Hkv, G, L, nq, q_start, n;   // n = q_start + nq
+  int nqt, nquads, chunk, max_chunks, n_items;   // n_items: per (batch, KV head)
+};
+
+__host__ __device__ inline int quad_steps(int pass, const Plan& p, int quad) {
+  if (pass == 1) {
+    const int t = min(p.nqt - 1, (4 * quad + 3) / p.G);
+    return (p.q_start + min(p.nq, (t + 1) * 128) - 1) / 128 + 1;
   }
-  return s;
+  return p.G * (p.nqt - max(0, 512 * quad - p.q_start) / 128);
 }
 
-// lse[b, h, i] = log2 of the row's sum of 2^(logit), logits in the log2 domain
-__global__ void __launch_bounds__(128)
-prompt_lse_kernel(const PromptDims d, const uint16_t* __restrict__ Q, const uint16_t* __restrict__ K, float scale_log2,
-                  float* __restrict__ lse) {
-  const int lane = threadIdx.x & 31;
-  const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
-  if (row >= (long long)d.Bt * d.Hq * d.nq) return;
-  const int i = (int)(row % d.nq), bq = (int)(row / d.nq), b = bq / d.Hq, h = bq % d.Hq;
-  const uint16_t* q = Q + (size_t)row * d.D;
-  const uint16_t* k = K + ((size_t)b * d.Hkv + h / (d.Hq / d.Hkv)) * d.L * d.D;
-  float m = -INFINITY, s = 0.f;
-  for (int j = lane; j <= d.q_start + i; j += 32) {
-    const float x = dot_bf16(q, k + (size_t)j * d.D, d.D) * scale_log2, mn = fmaxf(m, x);
-    s = s * exp2f(m - mn) + exp2f(x - mn);
-    m = mn;
+enum : int { PB_A_FULL = 0, PB_S_FULL = 1, PB_S_EMPTY = PB_S_FULL + PW_STAGES, PB_T_FULL = PB_S_EMPTY + PW_STAGES,
+             PB_T_EMPTY = PB_T_FULL + PW_GROUPS, PB_COUNT = PB_T_EMPTY + PW_GROUPS };
+
+// ---- packed pairs of 32-bit floats
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};\n" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;\n" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;\n" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;\n" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// 2^a, 2^b on the FMA and integer pipes: ex2p (qp_tc.cuh) on two values at once.  TOP: arguments above 126 are clamped, too.
+template <bool TOP>
+__device__ __forceinline__ uint64_t ex2_poly2(uint64_t x) {
+  const uint64_t magic = pack2(12582912.f, 12582912.f), nmagic = pack2(-12582912.f, -12582912.f), neg = pack2(-1.f, -1.f);
+  float a, b;
+  unpack2(x, a, b);
+  a = fmaxf(a, -126.f);
+  b = fmaxf(b, -126.f);
+  if (TOP) {
+    a = fminf(a, 126.f);
+    b = fminf(b, 126.f);
   }
-  for (int o = 16; o > 0; o >>= 1) {
-    const float mo = __shfl_xor_sync(0xffffffffu, m, o), so = __shfl_xor_sync(0xffffffffu, s, o), mn = fmaxf(m, mo);
-    if (mn != -INFINITY) {
-      s = s * exp2f(m - mn) + so * exp2f(mo - mn);
-      m = mn;
-    }
-  }
-  if (lane == 0) lse[row] = m + log2f(s);
+  x = pack2(a, b);
+  const uint64_t t = add2(x, magic), f = fma2(add2(t, nmagic), neg, x);
+  uint64_t p = fma2(pack2(0x1.5c08e6p-10f, 0x1.5c08e6p-10f), f, pack2(0x1.3d0c52p-7f, 0x1.3d0c52p-7f));
+  p = fma2(p, f, pack2(0x1.c6b6e4p-5f, 0x1.c6b6e4p-5f));
+  p = fma2(p, f, pack2(0x1.ebf918p-3f, 0x1.ebf918p-3f));
+  p = fma2(p, f, pack2(0x1.62e428p-1f, 0x1.62e428p-1f));
+  p = fma2(p, f, pack2(0x1.000002p+0f, 0x1.000002p+0f));
+  float ta, tb;
+  unpack2(t, ta, tb);
+  unpack2(p, a, b);
+  return pack2(__uint_as_float(__float_as_uint(a) + (__float_as_uint(ta) << 23)),
+               __uint_as_float(__float_as_uint(b) + (__float_as_uint(tb) << 23)));
+}
+#ifndef QP_PW_POLY_NUM
+#define QP_PW_POLY_NUM 3
+#define QP_PW_POLY_DEN 8
+#endif
+// pair `i` of a chunk: PW_POLY_NUM of every PW_POLY_DEN pairs through ex2_poly2, the others through the hardware unit
+template <bool TOP>
+__device__ __forceinline__ uint64_t ex2_pair(uint64_t x, int i) {
+  if ((i * QP_PW_POLY_NUM) % QP_PW_POLY_DEN < QP_PW_POLY_NUM) return ex2_poly2<TOP>(x);
+  float a, b;
+  unpack2(x, a, b);
+  return pack2(ex2a(a), ex2a(b));
 }
 
-__global__ void __launch_bounds__(128)
-prompt_columns_kernel(const PromptDims d, const uint16_t* __restrict__ Q, const uint16_t* __restrict__ K, float scale_log2,
-                      const float* __restrict__ lse, int accumulate, float* __restrict__ weights) {
-  const int bh = blockIdx.y, b = bh / d.Hkv, hk = bh % d.Hkv, G = d.Hq / d.Hkv, j = blockIdx.x * 128 + threadIdx.x;
-  if (j >= d.L) return;
+// sweep 1, 32 logits of a row that sees them all: s += sum 2^(t - m).  The reference m is one of the row's own logits, so the
+// true sum is at least 1 and terms that vanish do not matter; a sum above 2^40 renews it (a term is clamped at or reaches at
+// least 2^126 before anything can overflow unnoticed).
+__device__ __forceinline__ void fold_row_all(const uint32_t (&r)[32], float scale_log2, float& m, float& s) {
+  const uint64_t sc = pack2(scale_log2, scale_log2);
+  const uint64_t nm = pack2(-m, -m);
+  uint64_t acc0 = pack2(0.f, 0.f), acc1 = acc0;
+#pragma unroll
+  for (int i = 0; i < 16; i += 2) {
+    acc0 = add2(acc0, ex2_pair<true>(fma2(pack2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])), sc, nm), i));
+    acc1 = add2(acc1, ex2_pair<true>(fma2(pack2(__uint_as_float(r[2 * i + 2]), __uint_as_float(r[2 * i + 3])), sc, nm), i + 1));
+  }
+  float a, b;
+  unpack2(add2(acc0, acc1), a, b);
+  const float sum = a + b;
+  if (sum <= 1.0995116e12f) {                                   // 2^40; false for the first chunk (m = -inf), inf and NaN
+    s += sum;
+    return;
+  }
+  float cm = __uint_as_float(r[0]);
+#pragma unroll
+  for (int i = 1; i < 32; ++i) cm = fmaxf(cm, __uint_as_float(r[i]));
+  const float mn = fmaxf(m, cm * scale_log2);                   // scale > 0: max commutes with it
   float acc = 0.f;
-  if (j < d.q_start + d.nq) {
-    const uint16_t* k = K + ((size_t)bh * d.L + j) * d.D;
-    for (int g = 0; g < G; ++g) {
-      const size_t row0 = ((size_t)b * d.Hq + hk * G + g) * d.nq;
-      float part = 0.f;
-      for (int i = max(0, j - d.q_start); i < d.nq; ++i)
-        part += exp2f(dot_bf16(Q + (row0 + i) * d.D, k, d.D) * scale_log2 - lse[row0 + i]);
-      acc += part;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) acc += ex2a(fmaf(__uint_as_float(r[i]), scale_log2, -mn));
+  s = fmaf(s, ex2a(m - mn), acc);
+  m = mn;
+}
+// the same where only the columns up to lim are seen (col0: this chunk's first)
+__device__ __forceinline__ void fold_row_masked(const uint32_t (&r)[32], int col0, int lim, float scale_log2, float& m, float& s) {
+  float cm = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) cm = fmaxf(cm, col0 + i <= lim ? __uint_as_float(r[i]) : -INFINITY);
+  if (cm == -INFINITY) return;
+  const float mn = fmaxf(m, cm * scale_log2);
+  float acc = 0.f;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) acc += col0 + i <= lim ? ex2a(fmaf(__uint_as_float(r[i]), scale_log2, -mn)) : 0.f;
+  s = fmaf(s, ex2a(m - mn), acc);
+  m = mn;
+}
+// sweep 2: the sum of 32 rows' probabilities for this thread's key; lse: the rows' normalisers, negated (-inf: no such row)
+__device__ __forceinline__ float fold_column(const uint32_t (&r)[32], const float* lse, float scale_log2) {
+  const uint64_t sc = pack2(scale_log2, scale_log2);
+  uint64_t acc0 = pack2(0.f, 0.f), acc1 = acc0;
+#pragma unroll
+  for (int i = 0; i < 16; i += 2) {
+    const ulonglong2 l = *reinterpret_cast<const ulonglong2*>(lse + 2 * i);      // two pairs
+    acc0 = add2(acc0, ex2_pair<false>(fma2(pack2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])), sc, l.x), i));
+    acc1 = add2(acc1, ex2_pair<false>(fma2(pack2(__uint_as_float(r[2 * i + 2]), __uint_as_float(r[2 * i + 3])), sc, l.y), i + 1));
+  }
+  float a, b;
+  unpack2(add2(acc0, acc1), a, b);
+  return a + b;
+}
+__device__ __forceinline__ float fold_column_masked(const uint32_t (&r)[32], const float* lse, int c0, int first, float scale_log2) {
+  float acc = 0.f;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) acc += c0 + i >= first ? ex2a(fmaf(__uint_as_float(r[i]), scale_log2, lse[i])) : 0.f;
+  return acc;
+}
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n" ::"r"(dst), "l"(src),
+               "r"(bytes), "r"(bar)
+               : "memory");
+}
+
+// out: sweep 1, float2 (reference, sum) [bh][quad][piece][512 rows]; sweep 2, float [piece][bh][512 * quads] column sums
+// neg_lse: -lse, [Bt * Hq][128 * nqt], -inf behind the last row
+template <int PASS, int D>
+__global__ void __launch_bounds__(PW_THREADS, 1)
+prompt_sweep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const Plan p, int BH,
+                    float scale_log2, const float* __restrict__ neg_lse, void* __restrict__ out, int* __restrict__ error_word) {
+  constexpr uint32_t OPER = 128 * D * 2;                // one operand tile: D/64 swizzled blocks of 16 KB
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ uint64_t bars[PB_COUNT];
+  __shared__ __align__(16) float s_lse[PW_STAGES][128];
+  __shared__ uint32_t tmem_base_slot;
+  __shared__ int give_up, s_quad, s_chunk;
+
+  const int tid = threadIdx.x, lane = tid & 31;
+  const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+  const int bh = blockIdx.x % BH, b = bh / p.Hkv, hk = bh % p.Hkv;
+  const uint32_t sA = (smem_u32(smem_raw) + 1023u) & ~1023u, sS = sA + PW_GROUPS * OPER;
+  const uint32_t bar0 = smem_u32(&bars[0]);
+  auto bar = [&](int which, int i) { return bar0 + (uint32_t)(which + i) * 8u; };
+  const volatile int* gu = &give_up;
+
+  if (tid == 0) {
+    mbar_init(bar(PB_A_FULL, 0), 1);
+    for (int i = 0; i < PW_STAGES; ++i) {
+      mbar_init(bar(PB_S_FULL, i), 1);
+      mbar_init(bar(PB_S_EMPTY, i), PASS == 1 ? 1 : 1 + PW_READ_WARPS);   // the commit (and the readers of the stage's lse)
+    }
+    for (int i = 0; i < PW_GROUPS; ++i) {
+      mbar_init(bar(PB_T_FULL, i), 1);
+      mbar_init(bar(PB_T_EMPTY, i), 128);
+    }
+    give_up = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+  }
+  if (warp == PW_READ_WARPS + 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(&tmem_base_slot)),
+                 "r"(PW_TMEM_COLS)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
+  }
+  if (warp == 0) {
+    // piece number -> (quad, piece of the quad): the longest quads first, 32 quads at a time
+    int left = blockIdx.x / BH, quad = -1, chunk = 0;
+    for (int q0 = 0; q0 < p.nquads && quad < 0; q0 += 32) {
+      const int qi = q0 + lane, q = PASS == 1 ? p.nquads - 1 - qi : qi;
+      const int c = qi < p.nquads ? (quad_steps(PASS, p, q) + p.chunk - 1) / p.chunk : 0;
+      int inc = c;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += v;
+      }
+      const unsigned past = __ballot_sync(0xffffffffu, inc > left);
+      if (past) {
+        const int src = __ffs(past) - 1;
+        quad = __shfl_sync(0xffffffffu, q, src);
+        chunk = left - __shfl_sync(0xffffffffu, inc - c, src);
+      } else {
+        left -= __shfl_sync(0xffffffffu, inc, 31);
+      }
+    }
+    if (lane == 0) { s_quad = quad; s_chunk = chunk; }
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+  const uint32_t tmem_base = tmem_base_slot;
+  const int quad = s_quad, chunk = s_chunk;
+  const int step0 = chunk * p.chunk, n_loc = min(p.chunk, quad_steps(PASS, p, quad) - step0);
+  const int t0 = PASS == 2 ? max(0, 512 * quad - p.q_start) / 128 : 0;     // sweep 2: first query tile of a head
+  // the resident tile of group g: does it exist, and the first and one-past-last streamed tile it needs (per head)
+  auto group_valid = [&](int g) { return PASS == 1 ? (4 * quad + g) / p.G < p.nqt : 128 * (4 * quad + g) < p.n; };
+  auto active = [&](int g, int step) {
+    if (!group_valid(g)) return false;
+    if (PASS == 1) {
+      const int t = (4 * quad + g) / p.G;
+      return 128 * step <= p.q_start + min(p.nq, (t + 1) * 128) - 1;
+    }
+    const int t = t0 + step % (p.nqt - t0);
+    return p.q_start + min(p.nq, (t + 1) * 128) - 1 >= 128 * (4 * quad + g);
+  };
+  chain_enter();                                        // the launch's set-up overlaps the previous kernel's end
+
+  float m_run = -INFINITY, s_run = 0.f;                 // sweep 1: this thread's row; sweep 2: s_run = its key's sum
+
+  if (warp == PW_READ_WARPS) {
+    // ---- copy warp
+    int issued = 0;
+    bool ok = true;
+    if (lane == 0) {
+      int valid = 0;
+      for (int g = 0; g < PW_GROUPS; ++g) valid += group_valid(g) ? 1 : 0;
+      mbar_expect_tx(bar(PB_A_FULL, 0), valid * OPER);
+      for (int g = 0; g < valid; ++g) {                 // the valid groups come first
+        const int r = 4 * quad + g;
+        const int y = PASS == 1 ? (b * p.Hq + hk * p.G + r % p.G) * p.nq + r / p.G * 128 : bh * p.L + 128 * r;
+#pragma unroll
+        for (int kb = 0; kb < D / 64; ++kb)
+          tma_load_2d(sA + g * OPER + kb * 16384, PASS == 1 ? &map_q : &map_k, kb * 64, y, bar(PB_A_FULL, 0));
+      }
+    }
+    __syncwarp();
+    for (int j = 0; j < n_loc; ++j) {
+      const int st = j % PW_STAGES;
+      if (j >= PW_STAGES) ok = mbar_wait(bar(PB_S_EMPTY, st), (uint32_t)((j / PW_STAGES - 1) & 1), gu);
+      if (!ok) break;
+      if (lane == 0) {
+        mbar_expect_tx(bar(PB_S_FULL, st), OPER + (PASS == 2 ? 512 : 0));
+        int y;
+        if (PASS == 1) {
+          y = bh * p.L + (step0 + j) * 128;
+        } else {
+          const int per = p.nqt - t0, h = (step0 + j) / per, t = t0 + (step0 + j) % per, bq = b * p.Hq + hk * p.G + h;
+          y = bq * p.nq + t * 128;
+          bulk_load(smem_u32(&s_lse[st][0]), neg_lse + ((size_t)bq * p.nqt + t) * 128, 512, bar(PB_S_FULL, st));
+        }
+#pragma unroll
+        for (int kb = 0; kb < D / 64; ++kb)
+          tma_load_2d(sS + st * OPER + kb * 16384, PASS == 1 ? &map_k : &map_q, kb * 64, y, bar(PB_S_FULL, st));
+      }
+      issued = j + 1;
+      __syncwarp();
+    }
+    if (!ok) {
+      give_up = 1;
+      // the copies still on their way land in this block's shared memory: wait for them before it is given up
+      auto landed = [&](uint32_t full, uint32_t parity) {
+        for (uint32_t i = 0; i < TC_SPIN_LIMIT; ++i)
+          if (mbar_try_wait(full, parity)) return;
+      };
+      landed(bar(PB_A_FULL, 0), 0u);
+      for (int j = max(0, issued - PW_STAGES); j < issued; ++j)
+        landed(bar(PB_S_FULL, j % PW_STAGES), (uint32_t)((j / PW_STAGES) & 1));
+    }
+  } else if (warp == PW_READ_WARPS + 1) {
+    // ---- MMA warp: streamed tile j against the resident tiles that need it
+    constexpr uint32_t IDESC = instr_desc(128, 128);
+    int uses[PW_GROUPS] = {};
+    bool ok = mbar_wait(bar(PB_A_FULL, 0), 0u, gu);
+    for (int j = 0; j < n_loc && ok; ++j) {
+      const int st = j % PW_STAGES;
+      ok = mbar_wait(bar(PB_S_FULL, st), (uint32_t)((j / PW_STAGES) & 1), gu);
+#pragma unroll
+      for (int g = 0; g < PW_GROUPS; ++g) {
+        if (!ok || !active(g, step0 + j)) continue;
+        if (uses[g] > 0) ok = mbar_wait(bar(PB_T_EMPTY, g), (uint32_t)((uses[g] - 1) & 1), gu);
+        if (!ok) continue;
+        ++uses[g];
+        asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+        if (lane == 0) {
+          const uint32_t a = sA + g * OPER, s = sS + st * OPER, tm = tmem_base + g * 128;
+#pragma unroll
+          for (int kb = 0; kb < D / 64; ++kb)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              umma_bf16(tm, smem_desc(a + kb * 16384 + k * 32), smem_desc(s + kb * 16384 + k * 32), IDESC, (kb | k) ? 1u : 0u);
+          umma_commit(bar(PB_T_FULL, g));
+        }
+        __syncwarp();
+      }
+      if (ok && lane == 0) umma_commit(bar(PB_S_EMPTY, st));
+      __syncwarp();
+    }
+    if (!ok) give_up = 1;
+  } else {
+    // ---- reading groups
+    const int g = warp >> 2, rloc = (warp & 3) * 32 + lane;
+    const uint32_t taddr = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + g * 128;
+    int uses = 0;
+    bool ok = true;
+    for (int j = 0; j < n_loc; ++j) {
+      const int st = j % PW_STAGES, step = step0 + j;
+      // sweep 2 hands the stage back below whether it needed it or not, and only once it has been filled: a group that
+      // skips tiles must not run ahead of the ring
+      if (PASS == 2) ok = mbar_wait(bar(PB_S_FULL, st), (uint32_t)((j / PW_STAGES) & 1), gu);
+      if (!ok) break;
+      if (active(g, step)) {
+        ok = mbar_wait(bar(PB_T_FULL, g), (uint32_t)(uses & 1), gu);
+        if (!ok) break;
+        ++uses;
+        asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+        bool all;                                       // every row of the tile sees every key of it
+        int lim;                                        // sweep 1: last column this row sees; sweep 2: first row that sees this key
+        if (PASS == 1) {
+          const int t = (4 * quad + g) / p.G;
+          all = 128 * step + 127 <= p.q_start + 128 * t;
+          lim = min(p.q_start + 128 * t + rloc, p.n - 1) - 128 * step;
+        } else {
+          const int t = t0 + step % (p.nqt - t0), key0 = 128 * (4 * quad + g);
+          all = key0 + 127 <= p.q_start + 128 * t;
+          lim = key0 + rloc - p.q_start - 128 * t;
+        }
+        auto fold = [&](const uint32_t (&r)[32], int c0) {
+          if constexpr (PASS == 1) {
+            if (all) fold_row_all(r, scale_log2, m_run, s_run);
+            else fold_row_masked(r, c0, lim, scale_log2, m_run, s_run);
+          } else {
+            const float* l = &s_lse[st][c0];
+            s_run += all ? fold_column(r, l, scale_log2) : fold_column_masked(r, l, c0, lim, scale_log2);
+          }
+          __syncwarp();                                 // the tensor-memory instructions want the whole warp
+        };
+        uint32_t va[32], vb[32];
+        tmem_ld32_issue(taddr, va);
+        tmem_wait(va);
+        tmem_ld32_issue(taddr + 32, vb);
+        fold(va, 0);
+        tmem_wait(vb);
+        tmem_ld32_issue(taddr + 64, va);
+        fold(vb, 32);
+        tmem_wait(va);
+        tmem_ld32_issue(taddr + 96, vb);
+        fold(va, 64);
+        tmem_wait(vb);
+        asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+        mbar_arrive(bar(PB_T_EMPTY, g));
+        fold(vb, 96);
+      }
+      if (PASS == 2) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(PB_S_EMPTY, st));
+      }
+    }
+    if (!ok) give_up = 1;
+    if (group_valid(g)) {
+      if (PASS == 1)
+        static_cast<float2*>(out)[(((size_t)bh * p.nquads + quad) * p.max_chunks + chunk) * 512 + g * 128 + rloc] = make_float2(m_run, s_run);
+      else
+        static_cast<float*>(out)[((size_t)chunk * BH + bh) * (512 * (size_t)p.nquads) + 512 * (size_t)quad + g * 128 + rloc] = s_run;
     }
   }
-  float* w = weights + (size_t)bh * d.L + j;
-  if (!accumulate) *w = acc;
-  else if (j < d.q_start + d.nq) *w += acc;
+
+  asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+  __syncthreads();                                      // every part is done with shared and tensor memory
+  if (give_up && tid == 0) atomicExch(error_word, 1);
+  if (warp == PW_READ_WARPS + 1) {
+    asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem_base), "r"(PW_TMEM_COLS) : "memory");
+  }
+}
+
+// -lse of every row from the pieces' (reference, sum) pairs, -inf for the padding rows of a head's last tile
+__global__ void __launch_bounds__(256)
+prompt_lse_kernel(const Plan p, const float2* __restrict__ stats, float* __restrict__ neg_lse) {
+  chain_enter();
+  const int i = blockIdx.x * 256 + threadIdx.x, bq = blockIdx.y, b = bq / p.Hq, hq = bq % p.Hq, h = hq % p.G;
+  if (i >= p.nqt * 128) return;
+  const int bh = b * p.Hkv + hq / p.G, r = (i / 128) * p.G + h, quad = r / 4;
+  const int pieces = (quad_steps(1, p, quad) + p.chunk - 1) / p.chunk;
+  const float2* s = stats + (((size_t)bh * p.nquads + quad) * p.max_chunks) * 512 + (r % 4) * 128 + (i & 127);
+  float m = -INFINITY, z = 0.f;
+  for (int c0 = 0; c0 < pieces; c0 += 4) {
+    float2 v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = s[(size_t)min(c0 + k, pieces - 1) * 512];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (c0 + k < pieces && v[k].x != -INFINITY) {
+        const float mn = fmaxf(m, v[k].x);
+        z = z * exp2f(m - mn) + v[k].y * exp2f(v[k].x - mn);
+        m = mn;
+      }
+  }
+  neg_lse[(size_t)bq * (p.nqt * 128) + i] = i < p.nq ? -(m + log2f(z)) : -INFINITY;
+}
+
+// weights from the pieces' column sums, in the pieces' order
+__global__ void __launch_bounds__(256)
+prompt_add_kernel(const Plan p, int BH, const float* __restrict__ part, int accumulate, float* __restrict__ weights) {
+  chain_enter();
+  const int j = blockIdx.x * 256 + threadIdx.x, bh = blockIdx.y;
+  if (j >= p.L) return;
+  float* w = weights + (size_t)bh * p.L + j;
+  if (j >= p.n) {
+    if (!accumulate) *w = 0.f;
+    return;
+  }
+  const int pieces = (quad_steps(2, p, j / 512) + p.chunk - 1) / p.chunk;
+  const size_t stride = (size_t)BH * (512 * (size_t)p.nquads);
+  const float* s = part + (size_t)bh * (512 * (size_t)p.nquads) + j;
+  float acc = 0.f;
+  for (int c0 = 0; c0 < pieces; c0 += 4) {
+    float v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = s[(size_t)min(c0 + k, pieces - 1) * stride];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) acc += c0 + k < pieces ? v[k] : 0.f;
+  }
+  *w = accumulate ? *w + acc : acc;
+}
+
+// rows of D bf16 values as a matrix fetched in boxes of [128 rows x 64 columns] with the 128-byte swizzle; boxes past the end
+// are filled with zeros
+cudaError_t row_map(CUtensorMap* map, const void* base, long long rows, int D) {
+  EncodeTiledFn enc = encode_tiled();
+  if (!enc) return cudaErrorNotSupported;
+  const cuuint64_t dims[2] = {(cuuint64_t)D, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)D * 2};
+  const cuuint32_t box[2] = {64, 128}, elem[2] = {1, 1};
+  const CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, elem,
+                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+Plan make_plan(int pass, const PromptDims& d) {
+  Plan p{};
+  p.Hq = d.Hq; p.Hkv = d.Hkv; p.G = d.Hq / d.Hkv; p.L = d.L; p.nq = d.nq; p.q_start = d.q_start; p.n = d.q_start + d.nq;
+  p.nqt = (d.nq + 127) / 128;
+  p.nquads = pass == 1 ? (p.nqt * p.G + 3) / 4 : (p.n + 511) / 512;
+  // Length of a piece: a piece costs its steps and about 2.5 more (loading the resident tiles, set-up); the launch lasts whole
+  // rounds of pieces when there are few of them, and about the average load and a part of a last piece when there are many.
+  const int sms = sm_count(), BH = d.Bt * d.Hkv;
+  int longest = 0;
+  long long total = 0;
+  for (int q = 0; q < p.nquads; ++q) {
+    const int s = quad_steps(pass, p, q);
+    longest = std::max(longest, s);
+    total += s;
+  }
+  double best = 1e300;
+  for (int c : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256}) {
+    if (c > 1 && c / 2 >= longest) break;
+    if ((double)total * BH / sms > 200.0 * c) continue;          // far too many pieces
+    long long items = 0;
+    for (int q = 0; q < p.nquads; ++q) items += (quad_steps(pass, p, q) + c - 1) / c;
+    const double len = std::min(c, longest) + 2.5, all = (double)items * BH;
+    const double rounds = (double)((items * BH + sms - 1) / sms) * len;
+    const double flow = ((double)total * BH + 2.5 * all) / sms + 0.75 * len;
+    const double cost = std::min(rounds, std::max(flow, len)) + 0.002 * all / sms;
+    if (cost < best) {
+      best = cost;
+      p.chunk = c;
+      p.n_items = (int)items;
+    }
+  }
+  if (p.chunk == 0) {                                            // (longer than any candidate)
+    p.chunk = longest;
+    p.n_items = p.nquads;
+  }
+  p.max_chunks = (longest + p.chunk - 1) / p.chunk;
+  return p;
+}
+
+struct PromptWorkspace {
+  size_t stats, lse, part, error, total;
+};
+PromptWorkspace carve(const PromptDims& d, const Plan& p1, const Plan& p2) {
+  auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
+  const size_t BH = (size_t)d.Bt * d.Hkv;
+  PromptWorkspace w{};
+  w.stats = 0;
+  w.lse = w.stats + up(BH * p1.nquads * p1.max_chunks * 512 * sizeof(float2));
+  w.part = w.lse + up((size_t)d.Bt * d.Hq * p1.nqt * 128 * sizeof(float));
+  w.error = w.part + up(BH * p2.max_chunks * p2.nquads * 512 * sizeof(float));
+  w.total = w.error + 256;
+  return w;
+}
+
+template <int PASS, int D>
+cudaError_t launch_sweep(const CUtensorMap& q, const CUtensorMap& k, const Plan& p, int BH, float scale_log2, const float* lse,
+                         void* out, int* err, cudaStream_t st) {
+  constexpr size_t smem = (PW_GROUPS + PW_STAGES) * (size_t)128 * D * 2 + 1024;
+  static unsigned char done[64] = {};
+  const cudaError_t e = allow_smem(prompt_sweep_kernel<PASS, D>, smem, done);
+  if (e != cudaSuccess) return e;
+  return launch_chained(prompt_sweep_kernel<PASS, D>, dim3(p.n_items * BH), dim3(PW_THREADS), smem, st, q, k, p, BH, scale_log2,
+                        lse, out, err);
 }
 
 }  // namespace
 
-size_t prompt_workspace(const PromptDims& d) { return (((size_t)d.Bt * d.Hq * d.nq * sizeof(float) + 255) & ~(size_t)255) + 256; }
+size_t prompt_workspace(const PromptDims& d) { return carve(d, make_plan(1, d), make_plan(2, d)).total; }
 
 cudaError_t launch_prompt_weights(const void* Q, const void* K, const PromptDims& d, int accumulate, float* weights, void* ws,
-                                  cudaStream_t st) {
-  float* lse = static_cast<float*>(ws);
-  const uint16_t *q = static_cast<const uint16_t*>(Q), *k = static_cast<const uint16_t*>(K);
+                                  size_t ws_bytes, cudaStream_t st) {
+  const Plan p1 = make_plan(1, d), p2 = make_plan(2, d);
+  const PromptWorkspace w = carve(d, p1, p2);
+  if (ws_bytes < w.total) return cudaErrorInvalidValue;
+  char* base = static_cast<char*>(ws);
+  float2* stats = reinterpret_cast<float2*>(base + w.stats);
+  float *lse = reinterpret_cast<float*>(base + w.lse), *part = reinterpret_cast<float*>(base + w.part);
+  int* err = reinterpret_cast<int*>(base + w.error);
+  const int BH = d.Bt * d.Hkv;
   const float scale_log2 = (float)(1.4426950408889634 / sqrt((double)d.D));
-  cudaError_t e = cudaMemsetAsync(static_cast<char*>(ws) + prompt_workspace(d) - 256, 0, 4, st);
+  CUtensorMap mq, mk;
+  cudaError_t e = row_map(&mq, Q, (long long)d.Bt * d.Hq * d.nq, d.D);
   if (e != cudaSuccess) return e;
-  const long long rows = (long long)d.Bt * d.Hq * d.nq;
-  prompt_lse_kernel<<<(unsigned)((rows + 3) / 4), 128, 0, st>>>(d, q, k, scale_log2, lse);
-  e = cudaGetLastError();
+  e = row_map(&mk, K, (long long)BH * d.L, d.D);
   if (e != cudaSuccess) return e;
-  prompt_columns_kernel<<<dim3((d.L + 127) / 128, d.Bt * d.Hkv), 128, 0, st>>>(d, q, k, scale_log2, lse, accumulate, weights);
-  return cudaGetLastError();
+  e = cudaMemsetAsync(err, 0, sizeof(int), st);
+  if (e != cudaSuccess) return e;
+  e = d.D == 128 ? launch_sweep<1, 128>(mq, mk, p1, BH, scale_log2, lse, stats, err, st)
+                 : launch_sweep<1, 64>(mq, mk, p1, BH, scale_log2, lse, stats, err, st);
+  if (e != cudaSuccess) return e;
+  e = launch_chained(prompt_lse_kernel, dim3((p1.nqt * 128 + 255) / 256, d.Bt * d.Hq), dim3(256), 0, st, p1, (const float2*)stats, lse);
+  if (e != cudaSuccess) return e;
+  e = d.D == 128 ? launch_sweep<2, 128>(mq, mk, p2, BH, scale_log2, lse, part, err, st)
+                 : launch_sweep<2, 64>(mq, mk, p2, BH, scale_log2, lse, part, err, st);
+  if (e != cudaSuccess) return e;
+  return launch_chained(prompt_add_kernel, dim3((d.L + 255) / 256, BH), dim3(256), 0, st, p2, BH, (const float*)part, accumulate, weights);
 }
 
 }  // namespace qp
