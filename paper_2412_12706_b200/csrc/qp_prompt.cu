@@ -205,7 +205,7 @@ prompt_sweep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     }
     for (int i = 0; i < PW_GROUPS; ++i) {
       mbar_init(bar(PB_T_FULL, i), 1);
-      mbar_init(bar(PB_T_EMPTY, i), 128);
+      mbar_init(bar(PB_T_EMPTY, i), 4);                                    // its warps
     }
     give_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
@@ -246,16 +246,12 @@ prompt_sweep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
   const int quad = s_quad, chunk = s_chunk;
   const int step0 = chunk * p.chunk, n_loc = min(p.chunk, quad_steps(PASS, p, quad) - step0);
   const int t0 = PASS == 2 ? max(0, 512 * quad - p.q_start) / 128 : 0;     // sweep 2: first query tile of a head
-  // the resident tile of group g: does it exist, and the first and one-past-last streamed tile it needs (per head)
+  // the resident tile of group g: does it exist
   auto group_valid = [&](int g) { return PASS == 1 ? (4 * quad + g) / p.G < p.nqt : 128 * (4 * quad + g) < p.n; };
-  auto active = [&](int g, int step) {
-    if (!group_valid(g)) return false;
-    if (PASS == 1) {
-      const int t = (4 * quad + g) / p.G;
-      return 128 * step <= p.q_start + min(p.nq, (t + 1) * 128) - 1;
-    }
-    const int t = t0 + step % (p.nqt - t0);
-    return p.q_start + min(p.nq, (t + 1) * 128) - 1 >= 128 * (4 * quad + g);
+  // sweep 1: the last streamed tile it needs; sweep 2: the first query tile of a head it needs (both never, if it does not exist)
+  auto group_bound = [&](int g) {
+    if (PASS == 1) return group_valid(g) ? (p.q_start + min(p.nq, ((4 * quad + g) / p.G + 1) * 128) - 1) / 128 : -1;
+    return group_valid(g) ? max(0, 128 * (4 * quad + g) - p.q_start) / 128 : 0x7fffffff;
   };
   chain_enter();                                        // the launch's set-up overlaps the previous kernel's end
 
@@ -313,14 +309,17 @@ prompt_sweep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
   } else if (warp == PW_READ_WARPS + 1) {
     // ---- MMA warp: streamed tile j against the resident tiles that need it
     constexpr uint32_t IDESC = instr_desc(128, 128);
-    int uses[PW_GROUPS] = {};
+    int uses[PW_GROUPS] = {}, bound[PW_GROUPS];
+#pragma unroll
+    for (int g = 0; g < PW_GROUPS; ++g) bound[g] = group_bound(g);
+    int t = PASS == 2 ? t0 + step0 % (p.nqt - t0) : 0;  // sweep 2: query tile of the step
     bool ok = mbar_wait(bar(PB_A_FULL, 0), 0u, gu);
     for (int j = 0; j < n_loc && ok; ++j) {
       const int st = j % PW_STAGES;
       ok = mbar_wait(bar(PB_S_FULL, st), (uint32_t)((j / PW_STAGES) & 1), gu);
 #pragma unroll
       for (int g = 0; g < PW_GROUPS; ++g) {
-        if (!ok || !active(g, step0 + j)) continue;
+        if (!ok || !(PASS == 1 ? step0 + j <= bound[g] : t >= bound[g])) continue;
         if (uses[g] > 0) ok = mbar_wait(bar(PB_T_EMPTY, g), (uint32_t)((uses[g] - 1) & 1), gu);
         if (!ok) continue;
         ++uses[g];
@@ -338,13 +337,15 @@ prompt_sweep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
       }
       if (ok && lane == 0) umma_commit(bar(PB_S_EMPTY, st));
       __syncwarp();
+      if (PASS == 2 && ++t == p.nqt) t = t0;
     }
     if (!ok) give_up = 1;
   } else {
     // ---- reading groups
     const int g = warp >> 2, rloc = (warp & 3) * 32 + lane;
     const uint32_t taddr = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + g * 128;
-    int uses = 0;
+    const int bound = group_bound(g), tq = PASS == 1 ? (4 * quad + g) / p.G : 0;
+    int uses = 0, t = PASS == 2 ? t0 + step0 % (p.nqt - t0) : 0;
     bool ok = true;
     for (int j = 0; j < n_loc; ++j) {
       const int st = j % PW_STAGES, step = step0 + j;
@@ -352,7 +353,7 @@ prompt_sweep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
       // skips tiles must not run ahead of the ring
       if (PASS == 2) ok = mbar_wait(bar(PB_S_FULL, st), (uint32_t)((j / PW_STAGES) & 1), gu);
       if (!ok) break;
-      if (active(g, step)) {
+      if (PASS == 1 ? step <= bound : t >= bound) {
         ok = mbar_wait(bar(PB_T_FULL, g), (uint32_t)(uses & 1), gu);
         if (!ok) break;
         ++uses;
@@ -360,11 +361,10 @@ prompt_sweep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
         bool all;                                       // every row of the tile sees every key of it
         int lim;                                        // sweep 1: last column this row sees; sweep 2: first row that sees this key
         if (PASS == 1) {
-          const int t = (4 * quad + g) / p.G;
-          all = 128 * step + 127 <= p.q_start + 128 * t;
-          lim = min(p.q_start + 128 * t + rloc, p.n - 1) - 128 * step;
+          all = 128 * step + 127 <= p.q_start + 128 * tq;
+          lim = min(p.q_start + 128 * tq + rloc, p.n - 1) - 128 * step;
         } else {
-          const int t = t0 + step % (p.nqt - t0), key0 = 128 * (4 * quad + g);
+          const int key0 = 128 * (4 * quad + g);
           all = key0 + 127 <= p.q_start + 128 * t;
           lim = key0 + rloc - p.q_start - 128 * t;
         }
@@ -386,17 +386,19 @@ prompt_sweep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
         tmem_wait(vb);
         tmem_ld32_issue(taddr + 64, va);
         fold(vb, 32);
-        tmem_wait(va);
         tmem_ld32_issue(taddr + 96, vb);
-        fold(va, 64);
+        tmem_wait(va);
         tmem_wait(vb);
         asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
-        mbar_arrive(bar(PB_T_EMPTY, g));
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(PB_T_EMPTY, g));   // half of the arithmetic hides the next product
+        fold(va, 64);
         fold(vb, 96);
       }
       if (PASS == 2) {
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(PB_S_EMPTY, st));
+        if (++t == p.nqt) t = t0;
       }
     }
     if (!ok) give_up = 1;
