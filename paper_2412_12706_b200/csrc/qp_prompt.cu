@@ -95,8 +95,8 @@ __device__ __forceinline__ uint64_t ex2_poly2(uint64_t x) {
                __uint_as_float(__float_as_uint(b) + (__float_as_uint(tb) << 23)));
 }
 #ifndef QP_PW_POLY_NUM
-#define QP_PW_POLY_NUM 3
-#define QP_PW_POLY_DEN 8
+#define QP_PW_POLY_NUM 1
+#define QP_PW_POLY_DEN 4
 #endif
 // pair `i` of a chunk: PW_POLY_NUM of every PW_POLY_DEN pairs through ex2_poly2, the others through the hardware unit
 template <bool TOP>
@@ -110,7 +110,7 @@ __device__ __forceinline__ uint64_t ex2_pair(uint64_t x, int i) {
 // sweep 1, 32 logits of a row that sees them all: s += sum 2^(t - m).  The reference m is one of the row's own logits, so the
 // true sum is at least 1 and terms that vanish do not matter; a sum above 2^40 renews it (a term is clamped at or reaches at
 // least 2^126 before anything can overflow unnoticed).
-__device__ __forceinline__ void fold_row_all(const uint32_t (&r)[32], float scale_log2, float& m, float& s) {
+__device__ __forceinline__ bool fold_row_all(const uint32_t (&r)[32], float scale_log2, float m, float& s) {
   const uint64_t sc = pack2(scale_log2, scale_log2);
   const uint64_t nm = pack2(-m, -m);
   uint64_t acc0 = pack2(0.f, 0.f), acc1 = acc0;
@@ -122,27 +122,17 @@ __device__ __forceinline__ void fold_row_all(const uint32_t (&r)[32], float scal
   float a, b;
   unpack2(add2(acc0, acc1), a, b);
   const float sum = a + b;
-  if (sum <= 1.0995116e12f) {                                   // 2^40; false for the first chunk (m = -inf), inf and NaN
-    s += sum;
-    return;
-  }
-  float cm = __uint_as_float(r[0]);
-#pragma unroll
-  for (int i = 1; i < 32; ++i) cm = fmaxf(cm, __uint_as_float(r[i]));
-  const float mn = fmaxf(m, cm * scale_log2);                   // scale > 0: max commutes with it
-  float acc = 0.f;
-#pragma unroll
-  for (int i = 0; i < 32; ++i) acc += ex2a(fmaf(__uint_as_float(r[i]), scale_log2, -mn));
-  s = fmaf(s, ex2a(m - mn), acc);
-  m = mn;
+  if (!(sum <= 1.0995116e12f)) return false;                    // 2^40; so for the first chunk (m = -inf), for inf and NaN
+  s += sum;
+  return true;
 }
-// the same where only the columns up to lim are seen (col0: this chunk's first)
-__device__ __forceinline__ void fold_row_masked(const uint32_t (&r)[32], int col0, int lim, float scale_log2, float& m, float& s) {
+// the same with a renewed reference, for the columns up to lim only (col0: this chunk's first)
+__device__ __forceinline__ void fold_row_any(const uint32_t (&r)[32], int col0, int lim, float scale_log2, float& m, float& s) {
   float cm = -INFINITY;
 #pragma unroll
   for (int i = 0; i < 32; ++i) cm = fmaxf(cm, col0 + i <= lim ? __uint_as_float(r[i]) : -INFINITY);
   if (cm == -INFINITY) return;
-  const float mn = fmaxf(m, cm * scale_log2);
+  const float mn = fmaxf(m, cm * scale_log2);                   // scale > 0: max commutes with it
   float acc = 0.f;
 #pragma unroll
   for (int i = 0; i < 32; ++i) acc += col0 + i <= lim ? ex2a(fmaf(__uint_as_float(r[i]), scale_log2, -mn)) : 0.f;
@@ -370,30 +360,29 @@ prompt_sweep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
         }
         auto fold = [&](const uint32_t (&r)[32], int c0) {
           if constexpr (PASS == 1) {
-            if (all) fold_row_all(r, scale_log2, m_run, s_run);
-            else fold_row_masked(r, c0, lim, scale_log2, m_run, s_run);
+            if (!all || !fold_row_all(r, scale_log2, m_run, s_run)) fold_row_any(r, c0, lim, scale_log2, m_run, s_run);
           } else {
             const float* l = &s_lse[st][c0];
             s_run += all ? fold_column(r, l, scale_log2) : fold_column_masked(r, l, c0, lim, scale_log2);
           }
           __syncwarp();                                 // the tensor-memory instructions want the whole warp
         };
-        uint32_t va[32], vb[32];
-        tmem_ld32_issue(taddr, va);
-        tmem_wait(va);
-        tmem_ld32_issue(taddr + 32, vb);
-        fold(va, 0);
-        tmem_wait(vb);
-        tmem_ld32_issue(taddr + 64, va);
-        fold(vb, 32);
-        tmem_ld32_issue(taddr + 96, vb);
-        tmem_wait(va);
-        tmem_wait(vb);
-        asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(PB_T_EMPTY, g));   // half of the arithmetic hides the next product
-        fold(va, 64);
-        fold(vb, 96);
+        // two halves of 64 columns; a loop, not unrolled: the folds are long, and their code has to stay in the instruction cache
+#pragma unroll 1
+        for (int c0 = 0; c0 < 128; c0 += 64) {
+          uint32_t va[32], vb[32];
+          tmem_ld32_issue(taddr + c0, va);
+          tmem_ld32_issue(taddr + c0 + 32, vb);
+          tmem_wait(va);
+          tmem_wait(vb);
+          if (c0) {                                     // half of the arithmetic hides the next product
+            asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(PB_T_EMPTY, g));
+          }
+          fold(va, c0);
+          fold(vb, c0 + 32);
+        }
       }
       if (PASS == 2) {
         __syncwarp();
