@@ -229,7 +229,8 @@ int decode_mma_wide_workers_per_sm(const DecDims& d, int* min_tiles);
 cudaError_t launch_decode_mma(const DecTable& tab, const DecDims& d, float* partials, cudaStream_t st,
                               bool overlap_prev, const TailTable* tails = nullptr);
 
-// ---- accumulated attention weights and the eviction that goes by them (qp_prompt.cu, qp_weights.cu)
+// ---- accumulated attention weights and the eviction that goes by them (qp_prompt.cu, qp_decode_weights.cu,
+// qp_weights.cu)
 struct PromptDims {
   int Bt, Hq, Hkv, D, L, q_start, nq;
 };

@@ -1,0 +1,645 @@
+// Decode attention that accumulates its softmax weights (qp_decode_attn_weights).
+//
+//   out[h] = sum_t p[h,t] V'[t],   W[t] += sum_h p[h,t],   p[h,t] = 2^(x[h,t] - M[h]) / Z[h],   x = q.K' log2(e) / sqrt(D)
+//
+// A token's weight needs the normaliser over all tokens, the output does not: the logits are kept (G floats per token, against
+// 2 D B / 8 bytes of cache) until the head's statistics are known.  One thread-block cluster per (batch, KV head) makes this one
+// launch: CTA r streams a contiguous run of 32-token tiles with one pass over keys and values, leaves (max, sum, accumulators)
+// in its shared memory, the cluster exchanges them through distributed shared memory, and every CTA then turns its own logits
+// into weights and writes its slice of the output.  Bound: the packed bytes from HBM; the logits stay in shared memory, or for
+// very long runs in the caller's workspace (L2).
+//
+// The weights are results of their own, so logits, maxima and sums are 32-bit exact: queries enter the tensor cores unscaled
+// (a bf16 value is an f16 value in the range the interface allows, and codes are integers), scales, zero points and
+// log2(e)/sqrt(D) are applied to 32-bit accumulators.  Only the second product, whose result is rounded to bf16, uses
+// weights rounded to 16 bits.
+//
+// Per-token caches (B = 2, 4, 8; both matrices [token][D] with groups of g channels): a 16-bit lane holding a small integer c
+// is the f16 number c * 2^-24, so masked words are MMA operands; see decode_weights_packed_kernel.
+#include <cooperative_groups.h>
+
+#include <algorithm>
+
+#include "qp_mma.cuh"
+
+namespace qp {
+
+namespace {
+
+namespace cg = cooperative_groups;
+
+constexpr int DW_WARPS = 4, DW_THREADS = DW_WARPS * 32, DW_MAX_CLUSTER = 16;
+constexpr int DW_LOGIT_BYTES = 16384;    // of shared memory; runs with more logits keep them in the workspace
+
+struct DwArgs {
+  DecLayer ly;
+  int Bt, Hq, Hkv, group, cluster;
+  float* weights;
+  float* logits;                         // workspace [BH, G, n32], null: shared memory holds them
+  int n32;                               // tokens rounded up to whole tiles
+};
+
+// ---- what both kernels do around their streams
+
+// this CTA's run of tiles
+__device__ __forceinline__ void dw_run(const DwArgs& a, int rank, int& lo, int& hi) {
+  const int tiles = a.n32 / 32;
+  lo = (int)((long long)tiles * rank / a.cluster);
+  hi = (int)((long long)tiles * (rank + 1) / a.cluster);
+}
+
+// After a __syncthreads: warps' partial results s_acc [warp][8][D], s_m, s_l [warp][8] -> this CTA's (in s_out [8][D], s_ml [8][2]),
+// -> across the cluster -> weights of this CTA's tokens and a slice of the output.  lg: logits of this CTA's run, head h at
+// lg + h * stride, first token at index 0.
+template <int D>
+__device__ __forceinline__ void dw_finish(const DwArgs& a, int bh, int G, int tok_lo, int tok_hi, const float* s_acc, const float* s_m,
+                                          const float* s_l, float* s_out, float2* s_ml, const float* lg, size_t stride) {
+  cg::cluster_group cluster = cg::this_cluster();
+  const int tid = threadIdx.x, rank = (int)cluster.block_rank(), C = a.cluster;
+  for (int idx = tid; idx < G * D; idx += DW_THREADS) {
+    const int h = idx / D, d = idx % D;
+    float M = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < DW_WARPS; ++w) M = fmaxf(M, s_m[w * 8 + h]);
+    float Z = 0.f, A = 0.f;
+#pragma unroll
+    for (int w = 0; w < DW_WARPS; ++w) {
+      const float mw = s_m[w * 8 + h];
+      if (mw != -INFINITY) {
+        const float f = ex2(mw - M);
+        Z = fmaf(s_l[w * 8 + h], f, Z);
+        A = fmaf(s_acc[(w * 8 + h) * D + d], f, A);
+      }
+    }
+    s_out[idx] = A;
+    if (d == 0) s_ml[h] = make_float2(M, Z);
+  }
+  cluster.sync();
+  // head statistics of the whole cluster: thread h of every warp's first eight lanes
+  __shared__ float2 s_head[8];           // (M, 1 / Z)
+  __shared__ float s_f[DW_MAX_CLUSTER][8];
+  if (tid < G) {
+    float2 v[DW_MAX_CLUSTER];
+    float M = -INFINITY, Z = 0.f;
+#pragma unroll
+    for (int r = 0; r < DW_MAX_CLUSTER; ++r) {
+      if (r < C) v[r] = cluster.map_shared_rank(s_ml, r)[tid];
+      if (r < C) M = fmaxf(M, v[r].x);
+    }
+#pragma unroll
+    for (int r = 0; r < DW_MAX_CLUSTER; ++r)
+      if (r < C) {
+        const float f = v[r].x == -INFINITY ? 0.f : ex2(v[r].x - M);
+        Z = fmaf(v[r].y, f, Z);
+        s_f[r][tid] = f;
+      }
+    s_head[tid] = make_float2(M, __fdiv_rn(1.0f, Z));
+  }
+  __syncthreads();
+  // the output's slice of this CTA, ranks in order
+  const int per = (G * D + C - 1) / C, o_hi = min(G * D, (rank + 1) * per);
+  for (int idx = rank * per + tid; idx < o_hi; idx += DW_THREADS) {
+    const int h = idx / D;
+    float A = 0.f;
+    for (int r = 0; r < C; ++r) A = fmaf(cluster.map_shared_rank(s_out, r)[idx], s_f[r][h], A);
+    static_cast<bf16*>(a.ly.out)[(size_t)bh * G * D + idx] = __float2bfloat16_rn(A * s_head[h].y);
+  }
+  float* w = a.weights + (size_t)bh * a.ly.ns;
+  for (int t = tok_lo + tid; t < tok_hi; t += DW_THREADS) {
+    float s = 0.f;
+    for (int h = 0; h < G; ++h) s = fmaf(ex2(lg[h * stride + (t - tok_lo)] - s_head[h].x), s_head[h].y, s);
+    w[t] += s;
+  }
+  cluster.sync();                        // nobody leaves while another may still read its shared memory
+}
+
+__device__ __forceinline__ void dw_cp16_zf(uint32_t saddr, const void* gptr, bool valid) {
+  const int n = valid ? 16 : 0;
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(saddr), "l"(gptr), "r"(n));
+}
+__device__ __forceinline__ uint32_t dw_bf16x2(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// ---- 16-bit caches: query heads as MMA rows, so the weights leave the first product in the layout the second wants
+constexpr int DW16_STAGES = 3;
+
+template <int D>
+constexpr size_t dw16_smem() { return (size_t)DW_WARPS * DW16_STAGES * 128 * D + DW_LOGIT_BYTES; }
+
+template <int D>
+__global__ void __launch_bounds__(DW_THREADS, 1)
+decode_weights16_kernel(const __grid_constant__ DwArgs a) {
+  constexpr int CPR = D / 8, KST = D / 16, NJ = D / 8, TILE = 128 * D;   // bytes of a 32-token tile: keys, then values
+  extern __shared__ __align__(128) unsigned char smem[];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+  const int G = a.Hq / a.Hkv, C = a.cluster, bh = blockIdx.x / C, n = a.ly.n;
+  int lo, hi;
+  dw_run(a, blockIdx.x % C, lo, hi);
+  const int tok_lo = lo * 32, tok_hi = min(n, hi * 32);
+  float* lg = a.logits ? a.logits + (size_t)bh * G * a.n32 + tok_lo : reinterpret_cast<float*>(smem + DW_WARPS * DW16_STAGES * TILE);
+  const size_t lstride = a.logits ? (size_t)a.n32 : (size_t)((a.n32 / 32 + C - 1) / C * 32);
+  chain_enter();
+
+  const uint32_t wsm = smem_u32(smem + warp * (DW16_STAGES * TILE));
+  const unsigned char* gK = static_cast<const unsigned char*>(a.ly.kc) + (size_t)bh * a.ly.ns * D * 2;
+  const unsigned char* gV = static_cast<const unsigned char*>(a.ly.vc) + (size_t)bh * a.ly.ns * D * 2;
+  auto issue = [&](int tile, int stage) {
+    const uint32_t sb = wsm + stage * TILE;
+#pragma unroll
+    for (int i = 0; i < CPR; ++i) {                             // a row's 16-byte pieces, XOR-swizzled by the token
+      const int idx = lane + 32 * i, tau = idx / CPR, ch = idx % CPR;
+      const bool ok = tile * 32 + tau < n;
+      const size_t off = ok ? (size_t)(tile * 32 + tau) * (D * 2) + ch * 16 : 0;
+      const uint32_t dst = tau * (2 * D) + ((ch ^ (tau & 7)) << 4);
+      dw_cp16_zf(sb + dst, gK + off, ok);
+      dw_cp16_zf(sb + 64 * D + dst, gV + off, ok);
+    }
+  };
+  const int n_my = max(0, (hi - lo - warp + DW_WARPS - 1) / DW_WARPS);
+#pragma unroll
+  for (int s = 0; s < DW16_STAGES - 1; ++s) {
+    if (s < n_my) issue(lo + warp + DW_WARPS * s, s);
+    cp_async_commit();
+  }
+  uint32_t qa[KST][2];
+  {
+    const uint16_t* q = static_cast<const uint16_t*>(a.ly.q) + ((size_t)bh * G + g) * D;
+#pragma unroll
+    for (int c = 0; c < KST; ++c) {
+      qa[c][0] = g < G ? *reinterpret_cast<const uint32_t*>(q + 16 * c + 2 * t) : 0u;
+      qa[c][1] = g < G ? *reinterpret_cast<const uint32_t*>(q + 16 * c + 8 + 2 * t) : 0u;
+    }
+  }
+  const float scale_log2 = 1.4426950408889634f * rsqrtf((float)D);
+  const int lrow = lane & 7, lsel = lane >> 3;
+  float m_run = -INFINITY, l_run = 0.f, acc[NJ][4];             // head g (m replicated over t)
+#pragma unroll
+  for (int j = 0; j < NJ; ++j)
+#pragma unroll
+    for (int x = 0; x < 4; ++x) acc[j][x] = 0.f;
+
+  for (int it = 0; it < n_my; ++it) {
+    __syncwarp();
+    if (it + DW16_STAGES - 1 < n_my) issue(lo + warp + DW_WARPS * (it + DW16_STAGES - 1), (it + DW16_STAGES - 1) % DW16_STAGES);
+    cp_async_commit();
+    cp_async_wait<DW16_STAGES - 1>();
+    __syncwarp();
+    const uint32_t sb = wsm + (it % DW16_STAGES) * TILE;
+    const int tok0 = (lo + warp + DW_WARPS * it) * 32;
+    float sc[4][4];
+#pragma unroll
+    for (int nt = 0; nt < 4; ++nt) {
+      sc[nt][0] = sc[nt][1] = sc[nt][2] = sc[nt][3] = 0.f;
+      const int tau = 8 * nt + lrow;
+#pragma unroll
+      for (int c = 0; c < KST; c += 2) {
+        uint32_t b0, b1, b2, b3;
+        ldmatrix_x4(b0, b1, b2, b3, sb + tau * (2 * D) + (((2 * c + lsel) ^ (tau & 7)) << 4));
+        mma_bf16_m16n8k16(sc[nt], {qa[c][0], 0u, qa[c][1], 0u}, b0, b1);
+        mma_bf16_m16n8k16(sc[nt], {qa[c + 1][0], 0u, qa[c + 1][1], 0u}, b2, b3);
+      }
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int nt = 0; nt < 4; ++nt) {
+      const int tk = tok0 + 8 * nt + 2 * t;
+      sc[nt][0] = tk < n ? sc[nt][0] * scale_log2 : -INFINITY;
+      sc[nt][1] = tk + 1 < n ? sc[nt][1] * scale_log2 : -INFINITY;
+      mx = fmaxf(mx, fmaxf(sc[nt][0], sc[nt][1]));
+      if (g < G) *reinterpret_cast<float2*>(lg + g * lstride + (tk - tok_lo)) = make_float2(sc[nt][0], sc[nt][1]);
+    }
+    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+    const float mnew = fmaxf(m_run, mx), corr = ex2(m_run - mnew);       // finite: a tile's first token is < n
+    m_run = mnew;
+    float sum = 0.f;
+    uint32_t pa[4];
+#pragma unroll
+    for (int nt = 0; nt < 4; ++nt) {
+      const float p0 = ex2(sc[nt][0] - mnew), p1 = ex2(sc[nt][1] - mnew);
+      sum += p0 + p1;
+      pa[nt] = dw_bf16x2(p0, p1);
+    }
+    l_run = fmaf(l_run, corr, sum);
+    if (__any_sync(0xffffffffu, corr != 1.f)) {
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) { acc[j][0] *= corr; acc[j][1] *= corr; }
+    }
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const int tau = 8 * lsel + lrow;
+      uint32_t v0, v1, v2, v3;
+      ldmatrix_x4_trans(v0, v1, v2, v3, sb + 64 * D + tau * (2 * D) + ((j ^ (tau & 7)) << 4));
+      mma_bf16_m16n8k16(acc[j], {pa[0], 0u, pa[1], 0u}, v0, v1);
+      mma_bf16_m16n8k16(acc[j], {pa[2], 0u, pa[3], 0u}, v2, v3);
+    }
+  }
+  l_run += __shfl_xor_sync(0xffffffffu, l_run, 1);
+  l_run += __shfl_xor_sync(0xffffffffu, l_run, 2);
+  __syncthreads();                                              // the stages are idle
+  float* s_acc = reinterpret_cast<float*>(smem);                // [warp][8][D]
+  float *s_m = s_acc + DW_WARPS * 8 * D, *s_l = s_m + DW_WARPS * 8, *s_out = s_l + DW_WARPS * 8;
+  float2* s_ml = reinterpret_cast<float2*>(s_out + 8 * D);
+#pragma unroll
+  for (int j = 0; j < NJ; ++j)
+    *reinterpret_cast<float2*>(s_acc + (warp * 8 + g) * D + 8 * j + 2 * t) = make_float2(acc[j][0], acc[j][1]);
+  if (t == 0) { s_m[warp * 8 + g] = m_run; s_l[warp * 8 + g] = l_run; }
+  __syncthreads();
+  dw_finish<D>(a, bh, G, tok_lo, tok_hi, s_acc, s_m, s_l, s_out, s_ml, lg, lstride);
+}
+
+// ---- per-token caches
+// Keys, first product (rows = 16 tokens, columns = heads): ldmatrix hands lane (g, t) the 32-bit word t of a 16-byte piece of
+// token g: CHW = 32/B channels.  The word's pair f is (field f, field f + CHW/2), 16 bits apart: `word & mask` is an f16 operand
+// pair of integers times 2^-24 times 2^(position), pairs beyond the first byte after a shift by 8.  The contraction index is a
+// permutation of the channels that the query operand follows; it also carries the factors 2^-(position).
+// Values, second product (rows = channels, columns = heads): the transposing ldmatrix hands lane (g, t) the 16-bit unit g of
+// tokens 2t and 2t+1: U = 16/B channels, field f of both tokens again by masking.  The scale goes into the weights (per group),
+// the zero points are one small product of their own.
+// At 2 bits a 16-byte piece is 64 channels: with groups of 32 it holds two, and the operand lanes of the other group are zeroed.
+template <int BITS, int D, int GROUP>
+struct Pk {
+  static constexpr int RB = D * BITS / 8;              // bytes of a token's codes
+  static constexpr int NP = RB / 16;                   // 16-byte pieces of them
+  static constexpr int NG = D / GROUP;                 // groups per token
+  static constexpr int CH = 128 / BITS, CHW = 32 / BITS, U = 16 / BITS;
+  static constexpr int SETS = CH > GROUP ? CH / GROUP : 1;      // groups that share a piece
+  static constexpr int PPG = CH > GROUP ? 1 : GROUP / CH;       // pieces of a group
+  // a 32-token tile in shared memory
+  static constexpr int KC = 0, VC = 32 * RB, KS = 64 * RB, MB = 64 * NG, KZ = KS + MB, VS = KZ + MB, VZ = VS + MB, BYTES = VZ + MB;
+  static constexpr int STAGES = 4;
+  static constexpr int P_STRIDE = 80, P_BYTES = 8 * P_STRIDE;   // weights of a tile, [head][32 tokens] f16 and a pad
+  static constexpr int WARP_BYTES = STAGES * BYTES + P_BYTES;
+  static constexpr size_t SMEM = (size_t)DW_WARPS * WARP_BYTES + DW_LOGIT_BYTES;
+  // the epilogue's arrays overlay the stages
+  static constexpr int EPI = (DW_WARPS * 8 * D + 2 * DW_WARPS * 8 + 8 * D + 16) * 4;
+  static constexpr size_t SMEM_ALL = SMEM > (size_t)EPI + DW_LOGIT_BYTES ? SMEM : (size_t)EPI + DW_LOGIT_BYTES;
+  static __host__ __device__ constexpr int piece(int tau, int v) {      // conflict-free for both ldmatrix forms
+    const int sw = RB == 128 ? tau & 7 : RB == 64 ? (tau >> 1) & 3 : RB == 32 ? (tau >> 2) & 1 : 0;
+    return tau * RB + ((v ^ sw) << 4);
+  }
+};
+
+template <int BITS, int D, int GROUP>
+__global__ void __launch_bounds__(DW_THREADS, 2)
+decode_weights_packed_kernel(const __grid_constant__ DwArgs a) {
+  using L = Pk<BITS, D, GROUP>;
+  constexpr int NP = L::NP, NG = L::NG, NF = L::CHW / 2;        // NF: operand pairs of a word
+  constexpr float C24 = 16777216.0f;
+  extern __shared__ __align__(128) unsigned char smem[];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+  const int G = a.Hq / a.Hkv, C = a.cluster, bh = blockIdx.x / C;
+  int lo, hi;
+  dw_run(a, blockIdx.x % C, lo, hi);
+  const int tok_lo = lo * 32, tok_hi = hi * 32;                 // n is a multiple of 32
+  float* lg_out = a.logits ? a.logits + (size_t)bh * G * a.n32 + tok_lo : reinterpret_cast<float*>(smem + L::SMEM_ALL - DW_LOGIT_BYTES);
+  const size_t lstride = a.logits ? (size_t)a.n32 : (size_t)((a.n32 / 32 + C - 1) / C * 32);
+  chain_enter();
+
+  const uint32_t wsm = smem_u32(smem + warp * L::WARP_BYTES), sP = wsm + L::STAGES * L::BYTES;
+  // copies of a tile: this lane's pieces of both code blocks, and of the four scale / zero arrays
+  constexpr int MP = L::MB / 16;                                // 16-byte pieces of one such array
+  const size_t row0 = (size_t)bh * a.ly.ns;
+  auto issue = [&](int tile, uint32_t sb) {
+    const size_t row = row0 + (size_t)tile * 32;
+    const unsigned char* k = static_cast<const unsigned char*>(a.ly.kc) + row * L::RB;
+    const unsigned char* v = static_cast<const unsigned char*>(a.ly.vc) + row * L::RB;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int c = lane + 32 * i;
+      const uint32_t dst = L::piece(c / NP, c % NP);
+      cp_async16(sb + L::KC + dst, k + c * 16);
+      cp_async16(sb + L::VC + dst, v + c * 16);
+    }
+    const size_t m = row * NG * 2;
+    for (int c = lane; c < 4 * MP; c += 32) {
+      const int arr = c / MP, o = (c % MP) * 16;
+      const __half* src = arr == 0 ? a.ly.ks : arr == 1 ? a.ly.kz : arr == 2 ? a.ly.vs : a.ly.vz;
+      cp_async16(sb + L::KS + arr * L::MB + o, reinterpret_cast<const unsigned char*>(src) + m + o);
+    }
+  };
+  const int n_my = max(0, (hi - lo - warp + DW_WARPS - 1) / DW_WARPS);
+#pragma unroll
+  for (int s = 0; s < L::STAGES - 1; ++s) {
+    if (s < n_my) issue(lo + warp + DW_WARPS * s, wsm + s * L::BYTES);
+    cp_async_commit();
+  }
+
+  // query operands: pair f of word t of piece v, channels v CH + t CHW + f (+ CHW/2), times 2^-(position); head g
+  const float scale_log2 = 1.4426950408889634f * rsqrtf((float)D);
+  uint32_t qb[NP][NF];
+  float qsum[NG][2];                                            // sum of a group's query channels, heads 2t and 2t+1, scaled
+  {
+    const uint16_t* q = static_cast<const uint16_t*>(a.ly.q) + ((size_t)bh * G + (g < G ? g : 0)) * D;
+    float part[NG];
+#pragma unroll
+    for (int i = 0; i < NG; ++i) part[i] = 0.f;
+#pragma unroll
+    for (int v = 0; v < NP; ++v)
+#pragma unroll
+      for (int f = 0; f < NF; ++f) {
+        const int d0 = v * L::CH + t * L::CHW + f, d1 = d0 + L::CHW / 2;
+        const float x = g < G ? bf16_bits_to_f32(q[d0]) : 0.f, y = g < G ? bf16_bits_to_f32(q[d1]) : 0.f;
+        const float down = 1.0f / (float)(1 << ((f * BITS) & 7));
+        qb[v][f] = pack_half2(x * down, y * down);
+#pragma unroll
+        for (int i = 0; i < NG; ++i) part[i] += d0 / GROUP == i ? x + y : 0.f;      // (a word lies in one group)
+      }
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
+      float s = part[i];
+      s += __shfl_xor_sync(0xffffffffu, s, 1);
+      s += __shfl_xor_sync(0xffffffffu, s, 2);                  // lanes (g, *): head g
+      qsum[i][0] = __shfl_sync(0xffffffffu, s, 8 * t) * scale_log2;
+      qsum[i][1] = __shfl_sync(0xffffffffu, s, 8 * t + 4) * scale_log2;
+    }
+  }
+  const float kscale = C24 * scale_log2;
+  const int tau_ld = 8 * (lane >> 3) + (lane & 7);              // ldmatrix row of this lane
+
+  float m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};       // heads 2t, 2t+1 (l: this lane's tokens)
+  constexpr int MT = L::U / 2;                                  // products per piece of the value side: two fields each
+  float acc[NP][MT][4], acc_z[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int v = 0; v < NP; ++v)
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[v][mt][e] = 0.f;
+
+  uint32_t sb = wsm, sb_copy = wsm + (L::STAGES - 1) * L::BYTES;
+  for (int it = 0; it < n_my; ++it) {
+    __syncwarp();
+    if (it + L::STAGES - 1 < n_my) issue(lo + warp + DW_WARPS * (it + L::STAGES - 1), sb_copy);
+    cp_async_commit();
+    cp_async_wait<L::STAGES - 1>();
+    __syncwarp();
+    const int tok0 = (lo + warp + DW_WARPS * it) * 32;
+
+    // ---- keys: lane (g, t) ends up with tokens g + 8j and heads 2t + e
+    float lg[4][2] = {{0.f, 0.f}, {0.f, 0.f}, {0.f, 0.f}, {0.f, 0.f}};
+#pragma unroll
+    for (int gi = 0; gi < NG; ++gi) {
+      float a0[4] = {0.f, 0.f, 0.f, 0.f}, a1[4] = {0.f, 0.f, 0.f, 0.f};         // tokens 0..15, 16..31
+#pragma unroll
+      for (int pp = 0; pp < L::PPG; ++pp) {
+        const int v = L::SETS > 1 ? gi / L::SETS : gi * L::PPG + pp;
+        uint32_t r[4];
+        ldmatrix_x4(r[0], r[1], r[2], r[3], sb + L::KC + L::piece(tau_ld, v));
+        const bool mine = L::SETS == 1 || t / (4 / L::SETS) == gi % L::SETS;    // this lane's word belongs to group gi
+#pragma unroll
+        for (int f = 0; f < NF; f += 2) {
+          uint32_t x[4], y[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            constexpr uint32_t ones = (1u << BITS) - 1u;
+            const int p0 = f * BITS, p1 = (f + 1) * BITS;
+            x[i] = (p0 < 8 ? r[i] : r[i] >> 8) & ((ones | ones << 16) << (p0 & 7));
+            y[i] = (p1 < 8 ? r[i] : r[i] >> 8) & ((ones | ones << 16) << (p1 & 7));
+          }
+          const uint32_t b0 = mine ? qb[v][f] : 0u, b1 = mine ? qb[v][f + 1] : 0u;
+          mma_f16_m16n8k16(a0, x[0], x[1], y[0], y[1], b0, b1);
+          mma_f16_m16n8k16(a1, x[2], x[3], y[2], y[3], b0, b1);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        unsigned short s16, z16;
+        asm volatile("ld.shared.u16 %0, [%1];\n" : "=h"(s16) : "r"(sb + L::KS + ((g + 8 * j) * NG + gi) * 2));
+        asm volatile("ld.shared.u16 %0, [%1];\n" : "=h"(z16) : "r"(sb + L::KZ + ((g + 8 * j) * NG + gi) * 2));
+        const float s = __half2float(*reinterpret_cast<const __half*>(&s16)) * kscale, z = __half2float(*reinterpret_cast<const __half*>(&z16));
+        lg[j][0] = fmaf(s, (j < 2 ? a0 : a1)[2 * (j & 1)], fmaf(z, qsum[gi][0], lg[j][0]));
+        lg[j][1] = fmaf(s, (j < 2 ? a0 : a1)[2 * (j & 1) + 1], fmaf(z, qsum[gi][1], lg[j][1]));
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      if (2 * t + e < G)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) lg_out[(2 * t + e) * lstride + (tok0 - tok_lo + g + 8 * j)] = lg[j][e];
+
+    // ---- running softmax; the reference is renewed only when a logit exceeds it by more than 4 (weights up to 2^4 in f16)
+    float over = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) over = fmaxf(over, fmaxf(lg[j][0] - m_run[0], lg[j][1] - m_run[1]));
+    if (__any_sync(0xffffffffu, over > 4.f)) {
+      float corr[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float mx = fmaxf(fmaxf(lg[0][e], lg[1][e]), fmaxf(lg[2][e], lg[3][e]));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+        const float mnew = fmaxf(m_run[e], mx);
+        corr[e] = ex2(m_run[e] - mnew);
+        m_run[e] = mnew;
+        l_run[e] *= corr[e];
+      }
+#pragma unroll
+      for (int v = 0; v < NP; ++v)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+          acc[v][mt][0] *= corr[0]; acc[v][mt][1] *= corr[1];
+          acc[v][mt][2] *= corr[0]; acc[v][mt][3] *= corr[1];
+        }
+      acc_z[0] *= corr[0]; acc_z[1] *= corr[1];
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float p = ex2(lg[j][e] - m_run[e]);
+        l_run[e] += p;
+        const __half hv = __float2half_rn(p);
+        asm volatile("st.shared.u16 [%0], %1;\n" ::"r"(sP + (2 * t + e) * L::P_STRIDE + (g + 8 * j) * 2),
+                     "h"(*reinterpret_cast<const unsigned short*>(&hv)));
+      }
+    __syncwarp();
+    uint32_t p2[4];                                             // tokens (2t, 2t+1) + 8 pr of head g
+#pragma unroll
+    for (int pr = 0; pr < 4; ++pr) p2[pr] = lds32(sP + g * L::P_STRIDE + 4 * t + 16 * pr);
+
+    // ---- values
+    uint32_t zp[4];
+#pragma unroll
+    for (int pr = 0; pr < 4; ++pr) {                            // row g < NG: the zero points of group g
+      const int tau = 8 * pr + 2 * t;
+      zp[pr] = 0u;
+      if (g < NG) {
+        unsigned short z0, z1;
+        asm volatile("ld.shared.u16 %0, [%1];\n" : "=h"(z0) : "r"(sb + L::VZ + (tau * NG + g) * 2));
+        asm volatile("ld.shared.u16 %0, [%1];\n" : "=h"(z1) : "r"(sb + L::VZ + ((tau + 1) * NG + g) * 2));
+        zp[pr] = (uint32_t)z0 | (uint32_t)z1 << 16;
+      }
+    }
+    mma_f16_m16n8k16(acc_z, zp[0], 0u, zp[1], 0u, p2[0], p2[1]);
+    mma_f16_m16n8k16(acc_z, zp[2], 0u, zp[3], 0u, p2[2], p2[3]);
+#pragma unroll
+    for (int gi = 0; gi < NG; ++gi) {
+      uint32_t ps[4];
+#pragma unroll
+      for (int pr = 0; pr < 4; ++pr) {
+        const int tau = 8 * pr + 2 * t;
+        unsigned short s0, s1;
+        asm volatile("ld.shared.u16 %0, [%1];\n" : "=h"(s0) : "r"(sb + L::VS + (tau * NG + gi) * 2));
+        asm volatile("ld.shared.u16 %0, [%1];\n" : "=h"(s1) : "r"(sb + L::VS + ((tau + 1) * NG + gi) * 2));
+        ps[pr] = hmul2_u32(p2[pr], (uint32_t)s0 | (uint32_t)s1 << 16);
+      }
+#pragma unroll
+      for (int pp = 0; pp < L::PPG; ++pp) {
+        const int v = L::SETS > 1 ? gi / L::SETS : gi * L::PPG + pp;
+        uint32_t r[4];
+        ldmatrix_x4_trans(r[0], r[1], r[2], r[3], sb + L::VC + L::piece(tau_ld, v));
+        if (L::SETS > 1 && g / (8 / L::SETS) != gi % L::SETS) r[0] = r[1] = r[2] = r[3] = 0u;   // this lane's unit is the other group's
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+          uint32_t x[4], y[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            constexpr uint32_t ones = (1u << BITS) - 1u;
+            const int p0 = 2 * mt * BITS, p1 = (2 * mt + 1) * BITS;
+            x[i] = (p0 < 8 ? r[i] : r[i] >> 8) & ((ones | ones << 16) << (p0 & 7));
+            y[i] = (p1 < 8 ? r[i] : r[i] >> 8) & ((ones | ones << 16) << (p1 & 7));
+          }
+          mma_f16_m16n8k16(acc[v][mt], x[0], y[0], x[1], y[1], ps[0], ps[1]);
+          mma_f16_m16n8k16(acc[v][mt], x[2], y[2], x[3], y[3], ps[2], ps[3]);
+        }
+      }
+    }
+    sb_copy = sb;
+    sb = sb + L::BYTES == sP ? wsm : sb + L::BYTES;
+  }
+
+  // ---- this warp's result: head 2t + e, channel of (piece v, unit g, field)
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], 4);
+    l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], 8);
+    l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], 16);
+  }
+  __syncthreads();                                              // the stages are idle
+  float* s_acc = reinterpret_cast<float*>(smem);                // [warp][8][D]
+  float *s_m = s_acc + DW_WARPS * 8 * D, *s_l = s_m + DW_WARPS * 8, *s_out = s_l + DW_WARPS * 8;
+  float2* s_ml = reinterpret_cast<float2*>(s_out + 8 * D);
+#pragma unroll
+  for (int v = 0; v < NP; ++v) {
+    const int grp = (v * L::CH + g * L::U) / GROUP;             // group of this lane's channels: its zero term is with lane (grp, t)
+    const float z0 = __shfl_sync(0xffffffffu, acc_z[0], grp * 4 + t), z1 = __shfl_sync(0xffffffffu, acc_z[1], grp * 4 + t);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int f = 2 * mt + half, d = v * L::CH + g * L::U + f;
+        const float up = C24 / (float)(1 << ((f * BITS) & 7));
+        s_acc[(warp * 8 + 2 * t) * D + d] = fmaf(acc[v][mt][2 * half], up, z0);
+        s_acc[(warp * 8 + 2 * t + 1) * D + d] = fmaf(acc[v][mt][2 * half + 1], up, z1);
+      }
+  }
+  if (g == 0)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) { s_m[warp * 8 + 2 * t + e] = m_run[e]; s_l[warp * 8 + 2 * t + e] = l_run[e]; }
+  __syncthreads();
+  dw_finish<D>(a, bh, G, tok_lo, tok_hi, s_acc, s_m, s_l, s_out, s_ml, lg_out, lstride);
+}
+
+// CTAs per (batch, KV head): the cluster size with the shortest schedule.  All CTAs of a launch stream the same number of tiles
+// (+-1), `active` clusters of a size fit on the GPU at once, so the launch lasts ceil(heads / active) rounds of (tiles per warp
+// + a fixed cost of about two tiles for set-up and exchange).
+template <typename K>
+cudaError_t launch_dw(K kernel, size_t smem, DwArgs a, int BH, float* ws, unsigned char (&done)[64],
+                      int (&active)[64][DW_MAX_CLUSTER + 1], cudaStream_t st) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  e = allow_smem(kernel, smem, done);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.blockDim = dim3(DW_THREADS);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  if (active[dev][0] == 0) {                                    // once per device: what fits
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return e;
+    for (int c = 1; c <= DW_MAX_CLUSTER; ++c) {
+      int n = 0;
+      cfg.gridDim = dim3(c);
+      attr[0].val.clusterDim.x = c;
+      cfg.numAttrs = 1;
+      e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
+      if (e != cudaSuccess) return e;
+      active[dev][c] = n;
+    }
+    active[dev][0] = 1;
+  }
+  const int tiles = a.n32 / 32;
+  double best = 1e300;
+  a.cluster = 1;
+  for (int c = 1; c <= DW_MAX_CLUSTER && c <= tiles; ++c) {
+    if (active[dev][c] < 1) continue;
+    const int per_warp = ((tiles + c - 1) / c + DW_WARPS - 1) / DW_WARPS;
+    const double cost = (double)((BH + active[dev][c] - 1) / active[dev][c]) * (per_warp + 2);
+    if (cost < best) { best = cost; a.cluster = c; }
+  }
+  const size_t run = (size_t)((tiles + a.cluster - 1) / a.cluster) * 32;
+  a.logits = run * (a.Hq / a.Hkv) * sizeof(float) <= DW_LOGIT_BYTES ? nullptr : ws;
+  cfg.gridDim = dim3((unsigned)BH * a.cluster);
+  attr[0].val.clusterDim.x = a.cluster;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+
+template <int BITS, int D, int GROUP>
+cudaError_t launch_packed(const DwArgs& a, int BH, float* ws, cudaStream_t st) {
+  static unsigned char done[64] = {};
+  static int active[64][DW_MAX_CLUSTER + 1] = {};
+  return launch_dw(decode_weights_packed_kernel<BITS, D, GROUP>, Pk<BITS, D, GROUP>::SMEM_ALL, a, BH, ws, done, active, st);
+}
+template <int D>
+cudaError_t launch_16(const DwArgs& a, int BH, float* ws, cudaStream_t st) {
+  static unsigned char done[64] = {};
+  static int active[64][DW_MAX_CLUSTER + 1] = {};
+  return launch_dw(decode_weights16_kernel<D>, dw16_smem<D>(), a, BH, ws, done, active, st);
+}
+template <int BITS>
+cudaError_t launch_bits(const DwArgs& a, int D, int BH, float* ws, cudaStream_t st) {
+  if (D == 128) {
+    if (a.group == 32) return launch_packed<BITS, 128, 32>(a, BH, ws, st);
+    if (a.group == 64) return launch_packed<BITS, 128, 64>(a, BH, ws, st);
+    return launch_packed<BITS, 128, 128>(a, BH, ws, st);
+  }
+  if (a.group == 32) return launch_packed<BITS, 64, 32>(a, BH, ws, st);
+  return launch_packed<BITS, 64, 64>(a, BH, ws, st);
+}
+
+}  // namespace
+
+size_t decode_weights_workspace(const DecDims& d, int n_cap) {
+  return ((size_t)d.Bt * d.Hq * ((n_cap + 31) / 32 * 32) * sizeof(float) + 255) & ~(size_t)255;
+}
+
+cudaError_t launch_decode_weights(const DecLayer& ly, const DecDims& d, float* weights, void* ws, cudaStream_t st) {
+  DwArgs a{};
+  a.ly = ly;
+  a.Bt = d.Bt; a.Hq = d.Hq; a.Hkv = d.Hkv; a.group = d.group;
+  a.weights = weights;
+  a.n32 = (ly.n + 31) / 32 * 32;
+  const int BH = d.Bt * d.Hkv;
+  float* w = static_cast<float*>(ws);
+  switch (d.bits) {
+    case 2: return launch_bits<2>(a, d.D, BH, w, st);
+    case 4: return launch_bits<4>(a, d.D, BH, w, st);
+    case 8: return launch_bits<8>(a, d.D, BH, w, st);
+    case 16: return d.D == 128 ? launch_16<128>(a, BH, w, st) : launch_16<64>(a, BH, w, st);
+    default: return cudaErrorInvalidValue;
+  }
+}
+
+}  // namespace qp

@@ -1,76 +1,10 @@
-// Accumulated attention weights: decode attention that adds its softmax weights to the tokens' accumulators, and the two forms
-// of the eviction that goes by them (selection after a prompt, replacement of one token per step).
-//
-// First form: one thread per token and SIMT arithmetic throughout, element by element from the packed arrays.
+// The two forms of the eviction by accumulated attention weight: the state of a cache after a prompt's selection, and the
+// replacement of one token per step.
 #include "qp_common.cuh"
 
 namespace qp {
 
 namespace {
-
-// one element of a 16-bit cache or of a cache with per-token groups
-__device__ __forceinline__ float cache_element(const void* codes, const __half* scale, const __half* zero, size_t row, int d,
-                                               int D, int g, int bits) {
-  if (bits == 16) return bf16_bits_to_f32(static_cast<const uint16_t*>(codes)[row * D + d]);
-  const size_t grp = row * (D / g) + d / g;
-  const int e = d % g, per = 32 / bits;
-  const uint32_t word = static_cast<const uint32_t*>(codes)[grp * (g * bits / 32) + e / per];
-  const float c = (float)((word >> ((e % per) * bits)) & ((1u << bits) - 1u));
-  return fmaf(c, __half2float(scale[grp]), __half2float(zero[grp]));
-}
-
-// logits [BH, G, n] in the log2 domain
-__global__ void __launch_bounds__(128)
-weights_logits_kernel(const DecLayer ly, const DecDims dm, float* __restrict__ logits) {
-  const int bh = blockIdx.y, t = blockIdx.x * 128 + threadIdx.x, D = dm.D, G = dm.Hq / dm.Hkv;
-  if (t >= ly.n) return;
-  const uint16_t* q = static_cast<const uint16_t*>(ly.q) + (size_t)bh * G * D;
-  float acc[8] = {};
-  for (int d = 0; d < D; ++d) {
-    const float k = cache_element(ly.kc, ly.ks, ly.kz, (size_t)bh * ly.ns + t, d, D, dm.group, dm.bits);
-    for (int h = 0; h < G; ++h) acc[h] = fmaf(bf16_bits_to_f32(q[h * D + d]), k, acc[h]);
-  }
-  const float scale_log2 = 1.4426950408889634f * rsqrtf((float)D);
-  for (int h = 0; h < G; ++h) logits[((size_t)bh * G + h) * ly.n + t] = acc[h] * scale_log2;
-}
-
-__device__ __forceinline__ float block_reduce(float v, bool sum, float* s) {
-  for (int o = 16; o > 0; o >>= 1) {
-    const float x = __shfl_xor_sync(0xffffffffu, v, o);
-    v = sum ? v + x : fmaxf(v, x);
-  }
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
-  __syncthreads();
-  v = s[0];
-  for (int i = 1; i < 4; ++i) v = sum ? v + s[i] : fmaxf(v, s[i]);
-  return v;
-}
-
-// one block per (batch, KV head): statistics, weights and output
-__global__ void __launch_bounds__(128)
-weights_apply_kernel(const DecLayer ly, const DecDims dm, const float* __restrict__ logits, float* __restrict__ weights) {
-  __shared__ float s_red[4];
-  const int bh = blockIdx.x, D = dm.D, G = dm.Hq / dm.Hkv, n = ly.n, tid = threadIdx.x;
-  float* w = weights + (size_t)bh * ly.ns;
-  for (int h = 0; h < G; ++h) {
-    const float* lg = logits + ((size_t)bh * G + h) * n;
-    float m = -INFINITY;
-    for (int t = tid; t < n; t += 128) m = fmaxf(m, lg[t]);
-    m = block_reduce(m, false, s_red);
-    float l = 0.f;
-    for (int t = tid; t < n; t += 128) l += exp2f(lg[t] - m);
-    l = block_reduce(l, true, s_red);
-    const float inv = 1.f / l;
-    for (int t = tid; t < n; t += 128) w[t] += exp2f(lg[t] - m) * inv;
-    if (tid < D) {
-      float o = 0.f;
-      for (int t = 0; t < n; ++t)
-        o = fmaf(exp2f(lg[t] - m), cache_element(ly.vc, ly.vs, ly.vz, (size_t)bh * ly.ns + t, tid, D, dm.group, dm.bits), o);
-      static_cast<bf16*>(ly.out)[((size_t)bh * G + h) * D + tid] = __float2bfloat16_rn(o * inv);
-    }
-  }
-}
 
 // state of a cache filled with the kept tokens: their weights and positions, zero behind them
 __global__ void __launch_bounds__(256)
@@ -168,20 +102,6 @@ evict_kernel(const EvictArgs a) {
 }
 
 }  // namespace
-
-size_t decode_weights_workspace(const DecDims& d, int n_cap) {
-  return ((size_t)d.Bt * d.Hq * n_cap * sizeof(float) + 255) & ~(size_t)255;
-}
-
-cudaError_t launch_decode_weights(const DecLayer& ly, const DecDims& d, float* weights, void* ws, cudaStream_t st) {
-  const int BH = d.Bt * d.Hkv;
-  float* logits = static_cast<float*>(ws);
-  weights_logits_kernel<<<dim3((ly.n + 127) / 128, BH), 128, 0, st>>>(ly, d, logits);
-  cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess) return e;
-  weights_apply_kernel<<<BH, 128, 0, st>>>(ly, d, logits, weights);
-  return cudaGetLastError();
-}
 
 cudaError_t launch_kept_state(const float* weights, const int32_t* kept, int BH, int L, int n, int cap, float* kw, int32_t* kp,
                               cudaStream_t st) {
