@@ -22,6 +22,13 @@
 
 #include "qp_mma.cuh"
 
+#ifndef DWS
+#define DWS 2
+#define DWB 3
+#endif
+#ifndef DWL
+#define DWL 24576
+#endif
 namespace qp {
 
 namespace {
@@ -29,7 +36,7 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int DW_WARPS = 4, DW_THREADS = DW_WARPS * 32, DW_MAX_CLUSTER = 16;
-constexpr int DW_LOGIT_BYTES = 16384;    // of shared memory; runs with more logits keep them in the workspace
+constexpr int DW_LOGIT_BYTES = DWL;    // of shared memory; runs with more logits keep them in the workspace
 
 struct DwArgs {
   DecLayer ly;
@@ -51,19 +58,19 @@ __device__ __forceinline__ void dw_run(const DwArgs& a, int rank, int& lo, int& 
 // After a __syncthreads: warps' partial results s_acc [warp][8][D], s_m, s_l [warp][8] -> this CTA's (in s_out [8][D], s_ml [8][2]),
 // -> across the cluster -> weights of this CTA's tokens and a slice of the output.  lg: logits of this CTA's run, head h at
 // lg + h * stride, first token at index 0.
-template <int D>
+template <int D, int WARPS>
 __device__ __forceinline__ void dw_finish(const DwArgs& a, int bh, int G, int tok_lo, int tok_hi, const float* s_acc, const float* s_m,
                                           const float* s_l, float* s_out, float2* s_ml, const float* lg, size_t stride) {
   cg::cluster_group cluster = cg::this_cluster();
   const int tid = threadIdx.x, rank = (int)cluster.block_rank(), C = a.cluster;
-  for (int idx = tid; idx < G * D; idx += DW_THREADS) {
+  for (int idx = tid; idx < G * D; idx += WARPS * 32) {
     const int h = idx / D, d = idx % D;
     float M = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < DW_WARPS; ++w) M = fmaxf(M, s_m[w * 8 + h]);
+    for (int w = 0; w < WARPS; ++w) M = fmaxf(M, s_m[w * 8 + h]);
     float Z = 0.f, A = 0.f;
 #pragma unroll
-    for (int w = 0; w < DW_WARPS; ++w) {
+    for (int w = 0; w < WARPS; ++w) {
       const float mw = s_m[w * 8 + h];
       if (mw != -INFINITY) {
         const float f = ex2(mw - M);
@@ -98,17 +105,35 @@ __device__ __forceinline__ void dw_finish(const DwArgs& a, int bh, int G, int to
   __syncthreads();
   // the output's slice of this CTA, ranks in order
   const int per = (G * D + C - 1) / C, o_hi = min(G * D, (rank + 1) * per);
-  for (int idx = rank * per + tid; idx < o_hi; idx += DW_THREADS) {
+  for (int idx = rank * per + tid; idx < o_hi; idx += WARPS * 32) {
     const int h = idx / D;
     float A = 0.f;
-    for (int r = 0; r < C; ++r) A = fmaf(cluster.map_shared_rank(s_out, r)[idx], s_f[r][h], A);
+    float v[DW_MAX_CLUSTER];
+#pragma unroll
+    for (int r = 0; r < DW_MAX_CLUSTER; ++r) v[r] = r < C ? cluster.map_shared_rank(s_out, r)[idx] : 0.f;
+#pragma unroll
+    for (int r = 0; r < DW_MAX_CLUSTER; ++r) A = r < C ? fmaf(v[r], s_f[r][h], A) : A;
     static_cast<bf16*>(a.ly.out)[(size_t)bh * G * D + idx] = __float2bfloat16_rn(A * s_head[h].y);
   }
   float* w = a.weights + (size_t)bh * a.ly.ns;
-  for (int t = tok_lo + tid; t < tok_hi; t += DW_THREADS) {
-    float s = 0.f;
-    for (int h = 0; h < G; ++h) s = fmaf(ex2(lg[h * stride + (t - tok_lo)] - s_head[h].x), s_head[h].y, s);
-    w[t] += s;
+  for (int t = tok_lo + 4 * tid; t < tok_hi; t += 4 * WARPS * 32) {      // all heads' logits of four tokens in flight
+    float4 x[8];
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int h = 0; h < 8; ++h)
+      if (h < G) x[h] = *reinterpret_cast<const float4*>(lg + h * stride + (t - tok_lo));
+#pragma unroll
+    for (int h = 0; h < 8; ++h)
+      if (h < G) {
+        const float M = s_head[h].x, inv = s_head[h].y;
+        s[0] = fmaf(ex2(x[h].x - M), inv, s[0]);
+        s[1] = fmaf(ex2(x[h].y - M), inv, s[1]);
+        s[2] = fmaf(ex2(x[h].z - M), inv, s[2]);
+        s[3] = fmaf(ex2(x[h].w - M), inv, s[3]);
+      }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (t + i < tok_hi) atomicAdd(&w[t + i], s[i]);           // one addition per token: no order to depend on, nothing to wait for
   }
   cluster.sync();                        // nobody leaves while another may still read its shared memory
 }
@@ -122,45 +147,63 @@ __device__ __forceinline__ uint32_t dw_bf16x2(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// ---- 16-bit caches: query heads as MMA rows, so the weights leave the first product in the layout the second wants
-constexpr int DW16_STAGES = 3;
+// ---- 16-bit caches: query heads as MMA rows, so the weights leave the first product in the layout the second wants.  Eight
+// warps that walk over 16 tokens each: the stream is bound by how many warps wait for their own copies and products, not by
+// bytes in flight.
+constexpr int DW16_STAGES = 3, DW16_WARPS = 8, DW16_THREADS = DW16_WARPS * 32;
 
 template <int D>
-constexpr size_t dw16_smem() { return (size_t)DW_WARPS * DW16_STAGES * 128 * D + DW_LOGIT_BYTES; }
+constexpr size_t dw16_smem() { return (size_t)DW16_WARPS * DW16_STAGES * 64 * D + DW_LOGIT_BYTES; }
 
 template <int D>
-__global__ void __launch_bounds__(DW_THREADS, 1)
+__global__ void __launch_bounds__(DW16_THREADS, 1)
 decode_weights16_kernel(const __grid_constant__ DwArgs a) {
-  constexpr int CPR = D / 8, KST = D / 16, NJ = D / 8, TILE = 128 * D;   // bytes of a 32-token tile: keys, then values
+  constexpr int CPR = D / 8, KST = D / 16, NJ = D / 8, TILE = 64 * D, VOFF = 32 * D;   // bytes of 16 tokens: keys, then values
   extern __shared__ __align__(128) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
   const int G = a.Hq / a.Hkv, C = a.cluster, bh = blockIdx.x / C, n = a.ly.n;
   int lo, hi;
   dw_run(a, blockIdx.x % C, lo, hi);
   const int tok_lo = lo * 32, tok_hi = min(n, hi * 32);
-  float* lg = a.logits ? a.logits + (size_t)bh * G * a.n32 + tok_lo : reinterpret_cast<float*>(smem + DW_WARPS * DW16_STAGES * TILE);
+  float* lg = a.logits ? a.logits + (size_t)bh * G * a.n32 + tok_lo : reinterpret_cast<float*>(smem + DW16_WARPS * DW16_STAGES * TILE);
   const size_t lstride = a.logits ? (size_t)a.n32 : (size_t)((a.n32 / 32 + C - 1) / C * 32);
   chain_enter();
 
   const uint32_t wsm = smem_u32(smem + warp * (DW16_STAGES * TILE));
-  const unsigned char* gK = static_cast<const unsigned char*>(a.ly.kc) + (size_t)bh * a.ly.ns * D * 2;
-  const unsigned char* gV = static_cast<const unsigned char*>(a.ly.vc) + (size_t)bh * a.ly.ns * D * 2;
-  auto issue = [&](int tile, int stage) {
-    const uint32_t sb = wsm + stage * TILE;
+  // this lane's pieces of a tile: rows tau0 + i * TSTEP (of 16), one 16-byte column
+  constexpr int TSTEP = 32 / CPR, NP = 16 / TSTEP;
+  const int tau0 = lane / CPR, ch = lane % CPR;
+  uint32_t dst[NP];
 #pragma unroll
-    for (int i = 0; i < CPR; ++i) {                             // a row's 16-byte pieces, XOR-swizzled by the token
-      const int idx = lane + 32 * i, tau = idx / CPR, ch = idx % CPR;
-      const bool ok = tile * 32 + tau < n;
-      const size_t off = ok ? (size_t)(tile * 32 + tau) * (D * 2) + ch * 16 : 0;
-      const uint32_t dst = tau * (2 * D) + ((ch ^ (tau & 7)) << 4);
-      dw_cp16_zf(sb + dst, gK + off, ok);
-      dw_cp16_zf(sb + 64 * D + dst, gV + off, ok);
+  for (int i = 0; i < NP; ++i) dst[i] = (tau0 + i * TSTEP) * (2 * D) + ((ch ^ ((tau0 + i * TSTEP) & 7)) << 4);
+  int tok = tok_lo + warp * 16;                                 // first token of the next tile to fetch
+  const size_t row0 = ((size_t)bh * a.ly.ns + tok + tau0) * (D * 2) + ch * 16;
+  const unsigned char* gk = static_cast<const unsigned char*>(a.ly.kc) + row0;
+  const unsigned char* gv = static_cast<const unsigned char*>(a.ly.vc) + row0;
+  auto issue = [&](uint32_t sb) {
+    if (tok + 16 <= n) {
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        cp_async16(sb + dst[i], gk + i * TSTEP * (D * 2));
+        cp_async16(sb + VOFF + dst[i], gv + i * TSTEP * (D * 2));
+      }
+    } else {                                                    // rows behind the last token are zeros, whatever the array holds
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        const bool ok = tok + tau0 + i * TSTEP < n;
+        dw_cp16_zf(sb + dst[i], ok ? gk + i * TSTEP * (D * 2) : static_cast<const unsigned char*>(a.ly.kc), ok);
+        dw_cp16_zf(sb + VOFF + dst[i], ok ? gv + i * TSTEP * (D * 2) : static_cast<const unsigned char*>(a.ly.vc), ok);
+      }
     }
+    tok += DW16_WARPS * 16;
+    gk += DW16_WARPS * 16 * (D * 2);
+    gv += DW16_WARPS * 16 * (D * 2);
   };
-  const int n_my = max(0, (hi - lo - warp + DW_WARPS - 1) / DW_WARPS);
+  // tiles of 16 tokens with at least one token: every one of them has a finite maximum
+  const int n_tiles = (tok_hi - tok_lo + 15) / 16, n_my = max(0, (n_tiles - warp + DW16_WARPS - 1) / DW16_WARPS);
 #pragma unroll
   for (int s = 0; s < DW16_STAGES - 1; ++s) {
-    if (s < n_my) issue(lo + warp + DW_WARPS * s, s);
+    if (s < n_my) issue(wsm + s * TILE);
     cp_async_commit();
   }
   uint32_t qa[KST][2];
@@ -180,17 +223,17 @@ decode_weights16_kernel(const __grid_constant__ DwArgs a) {
 #pragma unroll
     for (int x = 0; x < 4; ++x) acc[j][x] = 0.f;
 
+  uint32_t sb = wsm, sb_copy = wsm + (DW16_STAGES - 1) * TILE;
   for (int it = 0; it < n_my; ++it) {
     __syncwarp();
-    if (it + DW16_STAGES - 1 < n_my) issue(lo + warp + DW_WARPS * (it + DW16_STAGES - 1), (it + DW16_STAGES - 1) % DW16_STAGES);
+    if (it + DW16_STAGES - 1 < n_my) issue(sb_copy);
     cp_async_commit();
     cp_async_wait<DW16_STAGES - 1>();
     __syncwarp();
-    const uint32_t sb = wsm + (it % DW16_STAGES) * TILE;
-    const int tok0 = (lo + warp + DW_WARPS * it) * 32;
-    float sc[4][4];
+    const int tok0 = tok_lo + (warp + DW16_WARPS * it) * 16;
+    float sc[2][4];
 #pragma unroll
-    for (int nt = 0; nt < 4; ++nt) {
+    for (int nt = 0; nt < 2; ++nt) {
       sc[nt][0] = sc[nt][1] = sc[nt][2] = sc[nt][3] = 0.f;
       const int tau = 8 * nt + lrow;
 #pragma unroll
@@ -203,7 +246,7 @@ decode_weights16_kernel(const __grid_constant__ DwArgs a) {
     }
     float mx = -INFINITY;
 #pragma unroll
-    for (int nt = 0; nt < 4; ++nt) {
+    for (int nt = 0; nt < 2; ++nt) {
       const int tk = tok0 + 8 * nt + 2 * t;
       sc[nt][0] = tk < n ? sc[nt][0] * scale_log2 : -INFINITY;
       sc[nt][1] = tk + 1 < n ? sc[nt][1] * scale_log2 : -INFINITY;
@@ -212,12 +255,12 @@ decode_weights16_kernel(const __grid_constant__ DwArgs a) {
     }
     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-    const float mnew = fmaxf(m_run, mx), corr = ex2(m_run - mnew);       // finite: a tile's first token is < n
+    const float mnew = fmaxf(m_run, mx), corr = ex2(m_run - mnew);
     m_run = mnew;
+    uint32_t pa[2];
     float sum = 0.f;
-    uint32_t pa[4];
 #pragma unroll
-    for (int nt = 0; nt < 4; ++nt) {
+    for (int nt = 0; nt < 2; ++nt) {
       const float p0 = ex2(sc[nt][0] - mnew), p1 = ex2(sc[nt][1] - mnew);
       sum += p0 + p1;
       pa[nt] = dw_bf16x2(p0, p1);
@@ -228,26 +271,29 @@ decode_weights16_kernel(const __grid_constant__ DwArgs a) {
       for (int j = 0; j < NJ; ++j) { acc[j][0] *= corr; acc[j][1] *= corr; }
     }
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      const int tau = 8 * lsel + lrow;
+    for (int j = 0; j < NJ; j += 2) {
+      const int tau = 8 * (lsel & 1) + lrow;                    // matrices: tokens 0-7, 8-15 of column block j, then of j + 1
       uint32_t v0, v1, v2, v3;
-      ldmatrix_x4_trans(v0, v1, v2, v3, sb + 64 * D + tau * (2 * D) + ((j ^ (tau & 7)) << 4));
+      ldmatrix_x4_trans(v0, v1, v2, v3, sb + VOFF + tau * (2 * D) + (((j + (lsel >> 1)) ^ (tau & 7)) << 4));
       mma_bf16_m16n8k16(acc[j], {pa[0], 0u, pa[1], 0u}, v0, v1);
-      mma_bf16_m16n8k16(acc[j], {pa[2], 0u, pa[3], 0u}, v2, v3);
+      mma_bf16_m16n8k16(acc[j + 1], {pa[0], 0u, pa[1], 0u}, v2, v3);
     }
+    sb_copy = sb;
+    sb = sb + TILE == wsm + DW16_STAGES * TILE ? wsm : sb + TILE;
   }
   l_run += __shfl_xor_sync(0xffffffffu, l_run, 1);
   l_run += __shfl_xor_sync(0xffffffffu, l_run, 2);
+  cp_async_wait<0>();
   __syncthreads();                                              // the stages are idle
   float* s_acc = reinterpret_cast<float*>(smem);                // [warp][8][D]
-  float *s_m = s_acc + DW_WARPS * 8 * D, *s_l = s_m + DW_WARPS * 8, *s_out = s_l + DW_WARPS * 8;
+  float *s_m = s_acc + DW16_WARPS * 8 * D, *s_l = s_m + DW16_WARPS * 8, *s_out = s_l + DW16_WARPS * 8;
   float2* s_ml = reinterpret_cast<float2*>(s_out + 8 * D);
 #pragma unroll
   for (int j = 0; j < NJ; ++j)
     *reinterpret_cast<float2*>(s_acc + (warp * 8 + g) * D + 8 * j + 2 * t) = make_float2(acc[j][0], acc[j][1]);
   if (t == 0) { s_m[warp * 8 + g] = m_run; s_l[warp * 8 + g] = l_run; }
   __syncthreads();
-  dw_finish<D>(a, bh, G, tok_lo, tok_hi, s_acc, s_m, s_l, s_out, s_ml, lg, lstride);
+  dw_finish<D, DW16_WARPS>(a, bh, G, tok_lo, tok_hi, s_acc, s_m, s_l, s_out, s_ml, lg, lstride);
 }
 
 // ---- per-token caches
@@ -269,7 +315,7 @@ struct Pk {
   static constexpr int PPG = CH > GROUP ? 1 : GROUP / CH;       // pieces of a group
   // a 32-token tile in shared memory
   static constexpr int KC = 0, VC = 32 * RB, KS = 64 * RB, MB = 64 * NG, KZ = KS + MB, VS = KZ + MB, VZ = VS + MB, BYTES = VZ + MB;
-  static constexpr int STAGES = 4;
+  static constexpr int STAGES = DWS;
   static constexpr int P_STRIDE = 80, P_BYTES = 8 * P_STRIDE;   // weights of a tile, [head][32 tokens] f16 and a pad
   static constexpr int WARP_BYTES = STAGES * BYTES + P_BYTES;
   static constexpr size_t SMEM = (size_t)DW_WARPS * WARP_BYTES + DW_LOGIT_BYTES;
@@ -282,8 +328,24 @@ struct Pk {
   }
 };
 
+// N halves from shared memory, aligned to their size, in the widest loads
+template <int N>
+__device__ __forceinline__ void lds_halves(__half (&h)[N], uint32_t addr) {
+  if constexpr (N == 8) {
+    *reinterpret_cast<uint4*>(h) = lds128(addr);
+  } else if constexpr (N == 4) {
+    *reinterpret_cast<uint2*>(h) = lds64(addr);
+  } else if constexpr (N == 2) {
+    *reinterpret_cast<uint32_t*>(h) = lds32(addr);
+  } else {
+    unsigned short v;
+    asm volatile("ld.shared.u16 %0, [%1];\n" : "=h"(v) : "r"(addr));
+    h[0] = *reinterpret_cast<const __half*>(&v);
+  }
+}
+
 template <int BITS, int D, int GROUP>
-__global__ void __launch_bounds__(DW_THREADS, 2)
+__global__ void __launch_bounds__(DW_THREADS, DWB)
 decode_weights_packed_kernel(const __grid_constant__ DwArgs a) {
   using L = Pk<BITS, D, GROUP>;
   constexpr int NP = L::NP, NG = L::NG, NF = L::CHW / 2;        // NF: operand pairs of a word
@@ -299,31 +361,40 @@ decode_weights_packed_kernel(const __grid_constant__ DwArgs a) {
   chain_enter();
 
   const uint32_t wsm = smem_u32(smem + warp * L::WARP_BYTES), sP = wsm + L::STAGES * L::BYTES;
-  // copies of a tile: this lane's pieces of both code blocks, and of the four scale / zero arrays
-  constexpr int MP = L::MB / 16;                                // 16-byte pieces of one such array
-  const size_t row0 = (size_t)bh * a.ly.ns;
-  auto issue = [&](int tile, uint32_t sb) {
-    const size_t row = row0 + (size_t)tile * 32;
-    const unsigned char* k = static_cast<const unsigned char*>(a.ly.kc) + row * L::RB;
-    const unsigned char* v = static_cast<const unsigned char*>(a.ly.vc) + row * L::RB;
+  // copies of a tile: this lane's pieces of both code blocks, and of the four scale / zero arrays; the pointers walk from
+  // one tile of this warp to its next, DW_WARPS tiles on
+  constexpr int MP = L::MB / 16, MPL = (4 * MP + 31) / 32;      // 16-byte pieces of one such array; pieces of all four per lane
+  const size_t row0 = (size_t)bh * a.ly.ns + (size_t)(lo + warp) * 32;
+  const unsigned char* gk = static_cast<const unsigned char*>(a.ly.kc) + row0 * L::RB + lane * 16;
+  const unsigned char* gv = static_cast<const unsigned char*>(a.ly.vc) + row0 * L::RB + lane * 16;
+  const unsigned char* gm[MPL];
+  uint32_t cdst[NP];
+#pragma unroll
+  for (int i = 0; i < NP; ++i) cdst[i] = L::piece((lane + 32 * i) / NP, (lane + 32 * i) % NP);
+#pragma unroll
+  for (int i = 0; i < MPL; ++i) {
+    const int c = lane + 32 * i, arr = c / MP;
+    const __half* src = arr == 0 ? a.ly.ks : arr == 1 ? a.ly.kz : arr == 2 ? a.ly.vs : a.ly.vz;
+    gm[i] = reinterpret_cast<const unsigned char*>(src) + row0 * NG * 2 + (c % MP) * 16;
+  }
+  auto issue = [&](uint32_t sb) {
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      const int c = lane + 32 * i;
-      const uint32_t dst = L::piece(c / NP, c % NP);
-      cp_async16(sb + L::KC + dst, k + c * 16);
-      cp_async16(sb + L::VC + dst, v + c * 16);
+      cp_async16(sb + L::KC + cdst[i], gk + i * 512);
+      cp_async16(sb + L::VC + cdst[i], gv + i * 512);
     }
-    const size_t m = row * NG * 2;
-    for (int c = lane; c < 4 * MP; c += 32) {
-      const int arr = c / MP, o = (c % MP) * 16;
-      const __half* src = arr == 0 ? a.ly.ks : arr == 1 ? a.ly.kz : arr == 2 ? a.ly.vs : a.ly.vz;
-      cp_async16(sb + L::KS + arr * L::MB + o, reinterpret_cast<const unsigned char*>(src) + m + o);
+#pragma unroll
+    for (int i = 0; i < MPL; ++i) {
+      if (lane + 32 * i < 4 * MP) cp_async16(sb + L::KS + (lane + 32 * i) * 16, gm[i]);   // the arrays lie one behind the other
+      gm[i] += DW_WARPS * 64 * NG;
     }
+    gk += DW_WARPS * 32 * L::RB;
+    gv += DW_WARPS * 32 * L::RB;
   };
   const int n_my = max(0, (hi - lo - warp + DW_WARPS - 1) / DW_WARPS);
 #pragma unroll
   for (int s = 0; s < L::STAGES - 1; ++s) {
-    if (s < n_my) issue(lo + warp + DW_WARPS * s, wsm + s * L::BYTES);
+    if (s < n_my) issue(wsm + s * L::BYTES);
     cp_async_commit();
   }
 
@@ -372,7 +443,7 @@ decode_weights_packed_kernel(const __grid_constant__ DwArgs a) {
   uint32_t sb = wsm, sb_copy = wsm + (L::STAGES - 1) * L::BYTES;
   for (int it = 0; it < n_my; ++it) {
     __syncwarp();
-    if (it + L::STAGES - 1 < n_my) issue(lo + warp + DW_WARPS * (it + L::STAGES - 1), sb_copy);
+    if (it + L::STAGES - 1 < n_my) issue(sb_copy);
     cp_async_commit();
     cp_async_wait<L::STAGES - 1>();
     __syncwarp();
@@ -380,6 +451,12 @@ decode_weights_packed_kernel(const __grid_constant__ DwArgs a) {
 
     // ---- keys: lane (g, t) ends up with tokens g + 8j and heads 2t + e
     float lg[4][2] = {{0.f, 0.f}, {0.f, 0.f}, {0.f, 0.f}, {0.f, 0.f}};
+    __half ksh[4][NG], kzh[4][NG];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      lds_halves(ksh[j], sb + L::KS + (g + 8 * j) * NG * 2);
+      lds_halves(kzh[j], sb + L::KZ + (g + 8 * j) * NG * 2);
+    }
 #pragma unroll
     for (int gi = 0; gi < NG; ++gi) {
       float a0[4] = {0.f, 0.f, 0.f, 0.f}, a1[4] = {0.f, 0.f, 0.f, 0.f};         // tokens 0..15, 16..31
@@ -406,10 +483,7 @@ decode_weights_packed_kernel(const __grid_constant__ DwArgs a) {
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        unsigned short s16, z16;
-        asm volatile("ld.shared.u16 %0, [%1];\n" : "=h"(s16) : "r"(sb + L::KS + ((g + 8 * j) * NG + gi) * 2));
-        asm volatile("ld.shared.u16 %0, [%1];\n" : "=h"(z16) : "r"(sb + L::KZ + ((g + 8 * j) * NG + gi) * 2));
-        const float s = __half2float(*reinterpret_cast<const __half*>(&s16)) * kscale, z = __half2float(*reinterpret_cast<const __half*>(&z16));
+        const float s = __half2float(ksh[j][gi]) * kscale, z = __half2float(kzh[j][gi]);
         lg[j][0] = fmaf(s, (j < 2 ? a0 : a1)[2 * (j & 1)], fmaf(z, qsum[gi][0], lg[j][0]));
         lg[j][1] = fmaf(s, (j < 2 ? a0 : a1)[2 * (j & 1) + 1], fmaf(z, qsum[gi][1], lg[j][1]));
       }
@@ -462,11 +536,18 @@ decode_weights_packed_kernel(const __grid_constant__ DwArgs a) {
     for (int pr = 0; pr < 4; ++pr) p2[pr] = lds32(sP + g * L::P_STRIDE + 4 * t + 16 * pr);
 
     // ---- values
-    uint32_t zp[4];
+    uint32_t zp[4], ps[4][NG];
 #pragma unroll
-    for (int pr = 0; pr < 4; ++pr) {                            // row g < NG: the zero points of group g
+    for (int pr = 0; pr < 4; ++pr) {
       const int tau = 8 * pr + 2 * t;
-      zp[pr] = 0u;
+      __half s0[2 * NG];                                        // groups of token tau, then of tau + 1
+      lds_halves(s0, sb + L::VS + tau * NG * 2);
+#pragma unroll
+      for (int gi = 0; gi < NG; ++gi) {
+        const __half2 pair = __halves2half2(s0[gi], s0[NG + gi]);
+        ps[pr][gi] = hmul2_u32(p2[pr], *reinterpret_cast<const uint32_t*>(&pair));
+      }
+      zp[pr] = 0u;                                              // row g < NG: the zero points of group g
       if (g < NG) {
         unsigned short z0, z1;
         asm volatile("ld.shared.u16 %0, [%1];\n" : "=h"(z0) : "r"(sb + L::VZ + (tau * NG + g) * 2));
@@ -478,15 +559,6 @@ decode_weights_packed_kernel(const __grid_constant__ DwArgs a) {
     mma_f16_m16n8k16(acc_z, zp[2], 0u, zp[3], 0u, p2[2], p2[3]);
 #pragma unroll
     for (int gi = 0; gi < NG; ++gi) {
-      uint32_t ps[4];
-#pragma unroll
-      for (int pr = 0; pr < 4; ++pr) {
-        const int tau = 8 * pr + 2 * t;
-        unsigned short s0, s1;
-        asm volatile("ld.shared.u16 %0, [%1];\n" : "=h"(s0) : "r"(sb + L::VS + (tau * NG + gi) * 2));
-        asm volatile("ld.shared.u16 %0, [%1];\n" : "=h"(s1) : "r"(sb + L::VS + ((tau + 1) * NG + gi) * 2));
-        ps[pr] = hmul2_u32(p2[pr], (uint32_t)s0 | (uint32_t)s1 << 16);
-      }
 #pragma unroll
       for (int pp = 0; pp < L::PPG; ++pp) {
         const int v = L::SETS > 1 ? gi / L::SETS : gi * L::PPG + pp;
@@ -503,8 +575,8 @@ decode_weights_packed_kernel(const __grid_constant__ DwArgs a) {
             x[i] = (p0 < 8 ? r[i] : r[i] >> 8) & ((ones | ones << 16) << (p0 & 7));
             y[i] = (p1 < 8 ? r[i] : r[i] >> 8) & ((ones | ones << 16) << (p1 & 7));
           }
-          mma_f16_m16n8k16(acc[v][mt], x[0], y[0], x[1], y[1], ps[0], ps[1]);
-          mma_f16_m16n8k16(acc[v][mt], x[2], y[2], x[3], y[3], ps[2], ps[3]);
+          mma_f16_m16n8k16(acc[v][mt], x[0], y[0], x[1], y[1], ps[0][gi], ps[1][gi]);
+          mma_f16_m16n8k16(acc[v][mt], x[2], y[2], x[3], y[3], ps[2][gi], ps[3][gi]);
         }
       }
     }
@@ -541,14 +613,14 @@ decode_weights_packed_kernel(const __grid_constant__ DwArgs a) {
 #pragma unroll
     for (int e = 0; e < 2; ++e) { s_m[warp * 8 + 2 * t + e] = m_run[e]; s_l[warp * 8 + 2 * t + e] = l_run[e]; }
   __syncthreads();
-  dw_finish<D>(a, bh, G, tok_lo, tok_hi, s_acc, s_m, s_l, s_out, s_ml, lg_out, lstride);
+  dw_finish<D, DW_WARPS>(a, bh, G, tok_lo, tok_hi, s_acc, s_m, s_l, s_out, s_ml, lg_out, lstride);
 }
 
 // CTAs per (batch, KV head): the cluster size with the shortest schedule.  All CTAs of a launch stream the same number of tiles
 // (+-1), `active` clusters of a size fit on the GPU at once, so the launch lasts ceil(heads / active) rounds of (tiles per warp
 // + a fixed cost of about two tiles for set-up and exchange).
 template <typename K>
-cudaError_t launch_dw(K kernel, size_t smem, DwArgs a, int BH, float* ws, unsigned char (&done)[64],
+cudaError_t launch_dw(K kernel, int warps, int warp_tokens, size_t smem, DwArgs a, int BH, float* ws, unsigned char (&done)[64],
                       int (&active)[64][DW_MAX_CLUSTER + 1], cudaStream_t st) {
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
@@ -556,7 +628,7 @@ cudaError_t launch_dw(K kernel, size_t smem, DwArgs a, int BH, float* ws, unsign
   e = allow_smem(kernel, smem, done);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.blockDim = dim3(DW_THREADS);
+  cfg.blockDim = dim3(warps * 32);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
@@ -584,7 +656,7 @@ cudaError_t launch_dw(K kernel, size_t smem, DwArgs a, int BH, float* ws, unsign
   a.cluster = 1;
   for (int c = 1; c <= DW_MAX_CLUSTER && c <= tiles; ++c) {
     if (active[dev][c] < 1) continue;
-    const int per_warp = ((tiles + c - 1) / c + DW_WARPS - 1) / DW_WARPS;
+    const int per_warp = ((tiles + c - 1) / c * (32 / warp_tokens) + warps - 1) / warps;
     const double cost = (double)((BH + active[dev][c] - 1) / active[dev][c]) * (per_warp + 2);
     if (cost < best) { best = cost; a.cluster = c; }
   }
@@ -600,13 +672,13 @@ template <int BITS, int D, int GROUP>
 cudaError_t launch_packed(const DwArgs& a, int BH, float* ws, cudaStream_t st) {
   static unsigned char done[64] = {};
   static int active[64][DW_MAX_CLUSTER + 1] = {};
-  return launch_dw(decode_weights_packed_kernel<BITS, D, GROUP>, Pk<BITS, D, GROUP>::SMEM_ALL, a, BH, ws, done, active, st);
+  return launch_dw(decode_weights_packed_kernel<BITS, D, GROUP>, DW_WARPS, 32, Pk<BITS, D, GROUP>::SMEM_ALL, a, BH, ws, done, active, st);
 }
 template <int D>
 cudaError_t launch_16(const DwArgs& a, int BH, float* ws, cudaStream_t st) {
   static unsigned char done[64] = {};
   static int active[64][DW_MAX_CLUSTER + 1] = {};
-  return launch_dw(decode_weights16_kernel<D>, dw16_smem<D>(), a, BH, ws, done, active, st);
+  return launch_dw(decode_weights16_kernel<D>, DW16_WARPS, 16, dw16_smem<D>(), a, BH, ws, done, active, st);
 }
 template <int BITS>
 cudaError_t launch_bits(const DwArgs& a, int D, int BH, float* ws, cudaStream_t st) {

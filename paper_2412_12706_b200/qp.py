@@ -156,8 +156,14 @@ def _check(status: int, where: str) -> None:
         raise QpError(status, where)
 
 
+# the handle of torch's current stream without building a Stream object (3 us, as much as a launch)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+    if _raw_stream is None:
+        return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(torch.cuda.current_device())
 
 
 def _ptr(t: torch.Tensor | None) -> int | None:
@@ -616,7 +622,7 @@ def decode_tree_workspace_bytes(cache: "Cache | qp_cache", T: int) -> int:
 
 
 def _dev(t: torch.Tensor, dtype: torch.dtype, shape: tuple) -> None:
-    assert t.is_cuda and t.dtype == dtype and t.is_contiguous() and tuple(t.shape) == tuple(shape), (t.dtype, t.shape, shape)
+    assert t.is_cuda and t.dtype is dtype and t.shape == shape and t.is_contiguous(), (t.dtype, t.shape, shape)
 
 
 def _ref(strategy: "Strategy | None"):
@@ -687,8 +693,9 @@ def evict_kv(k_new: torch.Tensor, v_new: torch.Tensor, cache: Cache, weights: to
     _dev(k_new, torch.bfloat16, row); _dev(v_new, torch.bfloat16, row)
     _dev(weights, torch.float32, _state_shape(cache)); _dev(pos, torch.int32, _state_shape(cache))
     if slots is None:
-        slots = torch.empty(row[:2], dtype=torch.int32, device=k_new.device)
-    _dev(slots, torch.int32, row[:2])
+        slots = pos.new_empty(row[:2])
+    else:
+        _dev(slots, torch.int32, row[:2])
     _check(lib().qp_evict_kv(_ptr(k_new), _ptr(v_new), ctypes.byref(d), _ref(strategy), _ptr(weights), _ptr(pos), new_pos, recent,
                              _ptr(slots), _stream()), "qp_evict_kv")
     return slots
