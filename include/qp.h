@@ -406,7 +406,7 @@ qp_status qp_evict_kv(const void* k_new, const void* v_new, qp_cache* cache /* h
 /*
  * Attention of a tree of T drafted tokens over the cache (speculative decoding: all drafts are verified with one pass over the
  * packed bytes).  Draft i sees every cached token, every token of the tail, and the drafts j whose bit j is set in mask[b,i]
- * (its ancestors and itself; any set of bits is allowed, none included):
+ * (its ancestors and itself; any set of bits is allowed, none included; bits T and above are ignored):
  *   out[b,i,h] = softmax over those tokens of (q[b,i,h].k / sqrt(D)), times their values
  * q, out bf16 [Bt,T,Hq,D]; k_draft, v_draft bf16 [Bt,T,Hkv,D]; mask uint64 [Bt,T]; 1 <= T <= QP_MAX_DRAFTS.  The drafts' rows
  * need not be in the cache; accepted ones are appended with qp_append_kv.  tail: NULL or as for qp_decode_attn_tail.

@@ -52,48 +52,6 @@ __host__ __device__ inline int quad_steps(int pass, const Plan& p, int quad) {
 enum : int { PB_A_FULL = 0, PB_S_FULL = 1, PB_S_EMPTY = PB_S_FULL + PW_STAGES, PB_T_FULL = PB_S_EMPTY + PW_STAGES,
              PB_T_EMPTY = PB_T_FULL + PW_GROUPS, PB_COUNT = PB_T_EMPTY + PW_GROUPS };
 
-// ---- packed pairs of 32-bit floats
-__device__ __forceinline__ uint64_t pack2(float a, float b) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};\n" : "=l"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ void unpack2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;\n" : "=f"(a), "=f"(b) : "l"(v)); }
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;\n" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;\n" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-// 2^a, 2^b on the FMA and integer pipes: ex2p (qp_tc.cuh) on two values at once.  TOP: arguments above 126 are clamped, too.
-template <bool TOP>
-__device__ __forceinline__ uint64_t ex2_poly2(uint64_t x) {
-  const uint64_t magic = pack2(12582912.f, 12582912.f), nmagic = pack2(-12582912.f, -12582912.f), neg = pack2(-1.f, -1.f);
-  float a, b;
-  unpack2(x, a, b);
-  a = fmaxf(a, -126.f);
-  b = fmaxf(b, -126.f);
-  if (TOP) {
-    a = fminf(a, 126.f);
-    b = fminf(b, 126.f);
-  }
-  x = pack2(a, b);
-  const uint64_t t = add2(x, magic), f = fma2(add2(t, nmagic), neg, x);
-  uint64_t p = fma2(pack2(0x1.5c08e6p-10f, 0x1.5c08e6p-10f), f, pack2(0x1.3d0c52p-7f, 0x1.3d0c52p-7f));
-  p = fma2(p, f, pack2(0x1.c6b6e4p-5f, 0x1.c6b6e4p-5f));
-  p = fma2(p, f, pack2(0x1.ebf918p-3f, 0x1.ebf918p-3f));
-  p = fma2(p, f, pack2(0x1.62e428p-1f, 0x1.62e428p-1f));
-  p = fma2(p, f, pack2(0x1.000002p+0f, 0x1.000002p+0f));
-  float ta, tb;
-  unpack2(t, ta, tb);
-  unpack2(p, a, b);
-  return pack2(__uint_as_float(__float_as_uint(a) + (__float_as_uint(ta) << 23)),
-               __uint_as_float(__float_as_uint(b) + (__float_as_uint(tb) << 23)));
-}
 #ifndef QP_PW_POLY_NUM
 #define QP_PW_POLY_NUM 1
 #define QP_PW_POLY_DEN 4

@@ -136,4 +136,91 @@ inline EncodeTiledFn encode_tiled() {
   }();
   return fn;
 }
+
+// ---- packed pairs of 32-bit floats
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};\n" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;\n" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;\n" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;\n" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// 2^a, 2^b on the FMA and integer pipes: ex2p (qp_tc.cuh) on two values at once.  TOP: arguments above 126 are clamped, too.
+template <bool TOP>
+__device__ __forceinline__ uint64_t ex2_poly2(uint64_t x) {
+  const uint64_t magic = pack2(12582912.f, 12582912.f), nmagic = pack2(-12582912.f, -12582912.f), neg = pack2(-1.f, -1.f);
+  float a, b;
+  unpack2(x, a, b);
+  a = fmaxf(a, -126.f);
+  b = fmaxf(b, -126.f);
+  if (TOP) {
+    a = fminf(a, 126.f);
+    b = fminf(b, 126.f);
+  }
+  x = pack2(a, b);
+  const uint64_t t = add2(x, magic), f = fma2(add2(t, nmagic), neg, x);
+  uint64_t p = fma2(pack2(0x1.5c08e6p-10f, 0x1.5c08e6p-10f), f, pack2(0x1.3d0c52p-7f, 0x1.3d0c52p-7f));
+  p = fma2(p, f, pack2(0x1.c6b6e4p-5f, 0x1.c6b6e4p-5f));
+  p = fma2(p, f, pack2(0x1.ebf918p-3f, 0x1.ebf918p-3f));
+  p = fma2(p, f, pack2(0x1.62e428p-1f, 0x1.62e428p-1f));
+  p = fma2(p, f, pack2(0x1.000002p+0f, 0x1.000002p+0f));
+  float ta, tb;
+  unpack2(t, ta, tb);
+  unpack2(p, a, b);
+  return pack2(__uint_as_float(__float_as_uint(a) + (__float_as_uint(ta) << 23)),
+               __uint_as_float(__float_as_uint(b) + (__float_as_uint(tb) << 23)));
+}
+
+// as umma_bf16 (the element types are in the instruction descriptor), operand A from tensor memory: two 16-bit elements a column
+__device__ __forceinline__ void umma_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t db, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}\n" ::"r"(tmem_d),
+      "r"(tmem_a), "l"(db), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// shared-memory matrix descriptor of the same tiles ([rows][64 columns] blocks of 128-byte rows, 128-byte swizzle) read with the
+// ROWS as the contraction: the contiguous direction is then the operand's outer one; blocks of 64 columns are `block` bytes apart,
+// groups of eight rows 1024 bytes
+__device__ __forceinline__ uint64_t smem_desc_mn(uint32_t saddr, uint32_t block) {
+  uint64_t d = 0;
+  d |= (uint64_t)((saddr & 0x3ffffu) >> 4);
+  d |= (uint64_t)(block >> 4) << 16;
+  d |= (uint64_t)(1024 >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+// 16 columns of this warp's 32 TMEM lanes
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};\n" ::"r"(r[0]),
+      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+      "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};\n" ::"r"(r[0]),
+      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+      "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]),
+      "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]),
+      "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory"); }
+
 }  // namespace qp
