@@ -224,7 +224,7 @@ prompt_sweep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     __syncwarp();
     for (int j = 0; j < n_loc; ++j) {
       const int st = j % PW_STAGES;
-      if (j >= PW_STAGES) ok = mbar_wait(bar(PB_S_EMPTY, st), (uint32_t)((j / PW_STAGES - 1) & 1), gu);
+      if (j >= PW_STAGES) ok = mbar_wait_warp(bar(PB_S_EMPTY, st), (uint32_t)((j / PW_STAGES - 1) & 1), gu);
       if (!ok) break;
       if (lane == 0) {
         mbar_expect_tx(bar(PB_S_FULL, st), OPER + (PASS == 2 ? 512 : 0));
@@ -261,14 +261,14 @@ prompt_sweep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
 #pragma unroll
     for (int g = 0; g < PW_GROUPS; ++g) bound[g] = group_bound(g);
     int t = PASS == 2 ? t0 + step0 % (p.nqt - t0) : 0;  // sweep 2: query tile of the step
-    bool ok = mbar_wait(bar(PB_A_FULL, 0), 0u, gu);
+    bool ok = mbar_wait_warp(bar(PB_A_FULL, 0), 0u, gu);
     for (int j = 0; j < n_loc && ok; ++j) {
       const int st = j % PW_STAGES;
-      ok = mbar_wait(bar(PB_S_FULL, st), (uint32_t)((j / PW_STAGES) & 1), gu);
+      ok = mbar_wait_warp(bar(PB_S_FULL, st), (uint32_t)((j / PW_STAGES) & 1), gu);
 #pragma unroll
       for (int g = 0; g < PW_GROUPS; ++g) {
         if (!ok || !(PASS == 1 ? step0 + j <= bound[g] : t >= bound[g])) continue;
-        if (uses[g] > 0) ok = mbar_wait(bar(PB_T_EMPTY, g), (uint32_t)((uses[g] - 1) & 1), gu);
+        if (uses[g] > 0) ok = mbar_wait_warp(bar(PB_T_EMPTY, g), (uint32_t)((uses[g] - 1) & 1), gu);
         if (!ok) continue;
         ++uses[g];
         asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
@@ -299,10 +299,10 @@ prompt_sweep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
       const int st = j % PW_STAGES, step = step0 + j;
       // sweep 2 hands the stage back below whether it needed it or not, and only once it has been filled: a group that
       // skips tiles must not run ahead of the ring
-      if (PASS == 2) ok = mbar_wait(bar(PB_S_FULL, st), (uint32_t)((j / PW_STAGES) & 1), gu);
+      if (PASS == 2) ok = mbar_wait_warp(bar(PB_S_FULL, st), (uint32_t)((j / PW_STAGES) & 1), gu);
       if (!ok) break;
       if (PASS == 1 ? step <= bound : t >= bound) {
-        ok = mbar_wait(bar(PB_T_FULL, g), (uint32_t)(uses & 1), gu);
+        ok = mbar_wait_warp(bar(PB_T_FULL, g), (uint32_t)(uses & 1), gu);
         if (!ok) break;
         ++uses;
         asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");

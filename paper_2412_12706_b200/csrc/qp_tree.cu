@@ -5,20 +5,21 @@
 // tcgen05, the codes are expanded to fp16 once per (KV head, tile) whatever R is, and all T drafts cost one pass over the cache.
 //
 // A block owns up to 256 rows of one KV head and walks over a run of 128-token tiles; its parts talk through mbarriers only:
-//   8 loader warps    tile j -> keys, then values, into a ring of 32 KB operand slots (128-byte swizzle).  Packed caches: words
-//                     from global memory, one operand ahead in registers, to fp16 and into the slot.  16-bit caches: TMA, with
-//                     the token count as the tensor's extent, so rows behind the last one arrive as zeros whatever the array
-//                     holds there.  Tail and drafts form the last one or two tiles.
+//   8 loader warps    tile j -> keys, then values, into a ring of 32 KB operand slots (128-byte swizzle).  Packed caches: words,
+//                     scales and zero points by asynchronous copies into raw stages, several operands ahead, then to fp16 and
+//                     into the slot.  16-bit caches: TMA, with the token count as the tensor's extent, so rows behind the last
+//                     one arrive as zeros whatever the array holds there.  Tail and drafts form the last one or two tiles.
 //   1 MMA warp        S[u] = Q[u] K_j^T into tensor memory; O[u] += P[u] V_j with P from tensor memory and V read with its rows
 //                     as the contraction, so neither operand is transposed
-//   2 softmax groups  u = 0, 1, four warps each, one row per thread: no shuffles.  S is read twice (maximum; exponentials); P
-//                     overwrites the columns of S already read.  O is rescaled only when the maximum grows by more than 2^8
+//   2 softmax groups  u = 0, 1, four warps each, one row per thread: no shuffles.  S is read once; P overwrites the columns
+//                     of S already read.  O is rescaled only when the maximum grows by more than 2^8
 //                     (the weights then stay below 2^8 in 16 bits, relative precision unchanged).
 // u is a tile of 128 rows when there are two, else (R <= 128) the parity of the token tile: two independent streams either
 // way, so one group's exponentials run beside the other's products.
 //
 // The runs of one (KV head, row group) form a cluster: partial (max, sum, O) stay in shared memory, every CTA adds up its slice
-// of the rows from all of them through distributed shared memory and writes it: one launch, no workspace but the error word.
+// of the rows from all of them through distributed shared memory and writes it.  Where clusters of the GPU's size would leave
+// SMs idle, several smaller ones share a (KV head, row group) and a small kernel merges what they leave in the workspace.
 // Order of additions fixed; every mbarrier wait bounded (see the score sweeps).
 //
 // Types: 16-bit caches multiply in bf16; packed ones in fp16 (2^-11 on a reconstructed value, against 2^-8 in bf16), tail,
@@ -38,10 +39,12 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int TR_SOFT = 8, TR_LOAD = 8;                          // warps
-constexpr int TR_LOADERS = TR_LOAD * 32;
-constexpr int TR_THREADS = (TR_SOFT + TR_LOAD + 1) * 32;
-constexpr int TR_MAX_SLOTS = 6, TR_MAX_CLUSTER = 16;
+constexpr int TR_SOFT = 8;                                       // softmax warps
+// Loader warps: eight expand codes (96 registers a thread, with 17 warps); copying by TMA takes one, and with four of them (the
+// other three help with the last tile) every thread may have 128 registers.
+__host__ __device__ constexpr int tr_load(int bits) { return bits == 16 ? 4 : 8; }
+__host__ __device__ constexpr int tr_threads(int bits) { return (TR_SOFT + tr_load(bits) + 1) * 32; }
+constexpr int TR_MAX_SLOTS = 6, TR_MAX_CLUSTER = 16, TR_MAX_SUBS = 16;
 
 enum : int { TB_FULL = 0, TB_EMPTY = TR_MAX_SLOTS, TB_S = 2 * TR_MAX_SLOTS, TB_P = TB_S + 2, TB_COUNT = TB_P + 2 };
 
@@ -50,7 +53,11 @@ struct TreeLaunch {
   int R, n_groups;           // rows per KV head, groups of up to 256 of them
   int two_rows;              // 1: stream u = row tile u of the group; 0: stream u = parity of the token tile
   int ctx_tiles, tiles;      // context tiles, and with the tail's and drafts'
-  int slots, cluster;
+  int slots, raw;            // operand slots, raw stages (packed caches)
+  int cluster, subs, max_subs;   // CTAs per cluster, clusters per (KV head, row group): more than one leave partial results
+  int lg;                    // log2 of the quantization group
+  float* part;               // [KV head, row group][sub][256][D], then
+  float2* part_ml;           // [KV head, row group][sub][256]
 };
 
 // byte offset of 16-byte chunk c of row r in an operand tile of 128 rows
@@ -64,6 +71,15 @@ __device__ __forceinline__ uint32_t half2_fma(uint32_t a, uint32_t b, uint32_t c
   uint32_t d;
   asm("fma.rn.f16x2 %0, %1, %2, %3;\n" : "=r"(d) : "r"(a), "r"(b), "r"(c));
   return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;\n" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+__device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
 }
 // two bf16 values to two fp16 values
 __device__ __forceinline__ uint32_t bf2_to_half2(uint32_t v) { return pack_half2(bf16lo(v), bf16hi(v)); }
@@ -80,116 +96,132 @@ __device__ __forceinline__ uint32_t code_pair(uint32_t x, int p, uint32_t s2, ui
   return half2_fma(half2_fma(h, down | down << 16, off | off << 16), s2, z2);
 }
 
-// ---- loaders of one packed operand tile: fetch (global -> registers) and put (registers -> slot)
+// ---- packed operands.  The words, scales and zero points of one operand (128 tokens of keys or of values) come into a raw stage
+// by asynchronous copies, several operands ahead; then the loaders expand them into an operand slot.  Raw stage: codes, scales,
+// zero points.  The codes of keys with groups along the tokens lie in rows of 8 channels (32 wpg bytes) with 16 bytes of pad, so
+// that eight lanes with eight such rows hit different banks.
+__device__ __forceinline__ uint32_t lds16(uint32_t a) {
+  unsigned short v;
+  asm volatile("ld.shared.u16 %0, [%1];\n" : "=h"(v) : "r"(a));
+  return v;
+}
+template <int BITS, int D>
+struct Raw {
+  static constexpr int CODES = 128 * D * BITS / 8 + (128 / 32) * (D / 8) * 16;  // most: groups of 32
+  static constexpr int META = 128 * (D / 32) * 2;                               // of scales, or of zero points
+  static constexpr int BYTES = CODES + 2 * META;
+};
+// copies of the operand's valid tokens (a multiple of 32, of the group if the groups run along the tokens); lg: log2 of the group
+template <int BITS, int D>
+__device__ __forceinline__ void raw_issue(const TreeArgs& a, int lg, bool cols, const void* codes, const __half* scale, const __half* zero,
+                                          int bh, int tok0, int lt, uint32_t raw) {
+  using R = Raw<BITS, D>;
+  constexpr int LB = BITS == 8 ? 3 : BITS == 4 ? 2 : 1, NT = tr_load(BITS) * 32;
+  const int nt = min(128, a.n - tok0);
+  const size_t row = (size_t)bh * a.ns + tok0;                  // first token row
+  const unsigned char* c = static_cast<const unsigned char*>(codes) + row * (D * BITS / 8) + lt * 16;
+  const int chunks = nt * (D * BITS / 8) / 16, lline = lg + LB - 4;             // 16-byte chunks; log2 of those in a row of 8 channels
+#pragma unroll
+  for (int k = 0; k < 128 * (D * BITS / 8) / 16 / NT + (128 * (D * BITS / 8) / 16 % NT ? 1 : 0); ++k) {
+    const int i = lt + k * NT;
+    if (i < chunks) cp_async16(raw + i * 16 + (cols ? (i >> lline) * 16 : 0), c + k * NT * 16);
+  }
+  // scales and zero points: D/g a token row, or D a row of g tokens, either way row * D / g from the start
+  const size_t m0 = (row * D >> lg) * 2;
+  const int meta = (nt * D >> lg) * 2 / 16;
+#pragma unroll
+  for (int k = 0; k < (2 * R::META / 16 + NT - 1) / NT; ++k) {
+    const int i = lt + k * NT, o = i < meta ? i : i - meta;
+    if (i < 2 * meta)
+      cp_async16(raw + R::CODES + (i < meta ? 0 : R::META) + o * 16, reinterpret_cast<const unsigned char*>(i < meta ? scale : zero) + m0 + o * 16);
+  }
+}
 // Groups along the tokens (keys of the main path): an item is 8 channels x PT tokens, a word per channel.
 template <int BITS, int D>
-struct ColLoader {
-  static constexpr int PER = 32 / BITS, PT = PER < 8 ? PER : 8, OCT = D / 8, ITEMS = (128 / PT) * OCT;
-  static constexpr int PT_ITEMS = (ITEMS + TR_LOADERS - 1) / TR_LOADERS;
-  uint32_t w[PT_ITEMS][8];
-  uint4 s[PT_ITEMS], z[PT_ITEMS];
-  __device__ __forceinline__ void fetch(const TreeArgs& a, int bh, int tok0, int lt) {
-    const int g = a.group, wpg = g * BITS / 32;
+__device__ __forceinline__ void put_cols(const TreeArgs& a, int lg, int tok0, int lt, uint32_t raw, uint32_t slot) {
+  using R = Raw<BITS, D>;
+  constexpr int TR_LOADERS = tr_load(BITS) * 32;
+  constexpr int PER = 32 / BITS, PT = PER < 8 ? PER : 8, OCT = D / 8, ITEMS = (128 / PT) * OCT;
+  const int g = 1 << lg, wpg = g * BITS / 32;
 #pragma unroll
-    for (int k = 0; k < PT_ITEMS; ++k) {
-      const int i = lt + k * TR_LOADERS, oct = i % OCT, tok = tok0 + i / OCT * PT;
-      if (i >= ITEMS || tok >= a.n) continue;
-      const size_t base = ((size_t)bh * (a.ns / g) + tok / g) * D + oct * 8;
-      const uint32_t* src = static_cast<const uint32_t*>(a.kc) + base * wpg + (tok % g) / PER;
+  for (int k = 0; k < (ITEMS + TR_LOADERS - 1) / TR_LOADERS; ++k) {
+    const int i = lt + k * TR_LOADERS, oct = i % OCT, row = i / OCT * PT;
+    if (i >= ITEMS) continue;
+    if (tok0 + row >= a.n) {                                    // (n is a multiple of 32: an item is inside or outside)
 #pragma unroll
-      for (int c = 0; c < 8; ++c) w[k][c] = __ldg(src + c * wpg);
-      s[k] = __ldg(reinterpret_cast<const uint4*>(a.ks + base));
-      z[k] = __ldg(reinterpret_cast<const uint4*>(a.kz + base));
+      for (int e = 0; e < PT; ++e) sts128(slot + tile_off(row + e, oct), make_uint4(0u, 0u, 0u, 0u));
+      continue;
     }
-  }
-  __device__ __forceinline__ void put(const TreeArgs& a, int tok0, int lt, uint32_t slot) {
+    const int u = row >> lg, e0 = row & (g - 1);
+    const uint32_t src = raw + (u * OCT + oct) * (32 * wpg + 16) + e0 / PER * 4, m = raw + R::CODES + (u * D + oct * 8) * 2;
+    uint32_t w[8];
 #pragma unroll
-    for (int k = 0; k < PT_ITEMS; ++k) {
-      const int i = lt + k * TR_LOADERS, oct = i % OCT, row = i / OCT * PT;
-      if (i >= ITEMS) continue;
-      if (tok0 + row >= a.n) {                                  // (n is a multiple of 32: an item is inside or outside)
+    for (int c = 0; c < 8; ++c) w[c] = lds32(src + c * wpg * 4);
+    const uint4 sv = lds128(m), zv = lds128(m + R::META);
+    const uint32_t s2[4] = {sv.x, sv.y, sv.z, sv.w}, z2[4] = {zv.x, zv.y, zv.z, zv.w};
+    const bool upper = BITS == 2 && (e0 & 8);                   // 16 tokens a word, 8 an item
 #pragma unroll
-        for (int e = 0; e < PT; ++e) sts128(slot + tile_off(row + e, oct), make_uint4(0u, 0u, 0u, 0u));
-        continue;
-      }
-      const uint32_t s2[4] = {s[k].x, s[k].y, s[k].z, s[k].w}, z2[4] = {z[k].x, z[k].y, z[k].z, z[k].w};
-      const bool upper = BITS == 2 && ((tok0 + row) & 8);       // 16 tokens a word, 8 an item
+    for (int half = 0; half < (PT * BITS > 16 ? 2 : 1); ++half) {
+      uint32_t x[4];
 #pragma unroll
-      for (int half = 0; half < (PT * BITS > 16 ? 2 : 1); ++half) {
-        uint32_t x[4];
+      for (int c = 0; c < 4; ++c) x[c] = __byte_perm(w[2 * c], w[2 * c + 1], half || upper ? 0x7632 : 0x5410);
+      constexpr int N = PT * BITS > 16 ? PT / 2 : PT;           // tokens in 16 bits
 #pragma unroll
-        for (int c = 0; c < 4; ++c) x[c] = __byte_perm(w[k][2 * c], w[k][2 * c + 1], half || upper ? 0x7632 : 0x5410);
-        constexpr int N = PT * BITS > 16 ? PT / 2 : PT;         // tokens in 16 bits
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-          uint4 v;
-          v.x = code_pair<BITS>(x[0], e * BITS, s2[0], z2[0]);
-          v.y = code_pair<BITS>(x[1], e * BITS, s2[1], z2[1]);
-          v.z = code_pair<BITS>(x[2], e * BITS, s2[2], z2[2]);
-          v.w = code_pair<BITS>(x[3], e * BITS, s2[3], z2[3]);
-          sts128(slot + tile_off(row + half * N + e, oct), v);
-        }
+      for (int e = 0; e < N; ++e) {
+        uint4 v;
+        v.x = code_pair<BITS>(x[0], e * BITS, s2[0], z2[0]);
+        v.y = code_pair<BITS>(x[1], e * BITS, s2[1], z2[1]);
+        v.z = code_pair<BITS>(x[2], e * BITS, s2[2], z2[2]);
+        v.w = code_pair<BITS>(x[3], e * BITS, s2[3], z2[3]);
+        sts128(slot + tile_off(row + half * N + e, oct), v);
       }
     }
   }
-};
+}
 // Groups along the channels (values; keys quantized token by token): an item is 16 channels of one token.
 template <int BITS, int D>
-struct RowLoader {
-  static constexpr int PIECES = D / 16, PT_ITEMS = 128 * PIECES / TR_LOADERS, W = BITS / 2;   // words of an item
-  uint32_t w[PT_ITEMS][W];
-  __half s[PT_ITEMS], z[PT_ITEMS];
-  __device__ __forceinline__ void fetch(const TreeArgs& a, const void* codes, const __half* scale, const __half* zero, int bh, int tok0,
-                                        int lt) {
+__device__ __forceinline__ void put_rows(const TreeArgs& a, int lg, int tok0, int lt, uint32_t raw, uint32_t slot) {
+  using R = Raw<BITS, D>;
+  constexpr int TR_LOADERS = tr_load(BITS) * 32;
+  constexpr int PIECES = D / 16, W = BITS / 2;                  // words of an item
 #pragma unroll
-    for (int k = 0; k < PT_ITEMS; ++k) {
-      const int i = lt + k * TR_LOADERS, piece = i % PIECES, tok = tok0 + i / PIECES;
-      if (tok >= a.n) continue;
-      const size_t row = (size_t)bh * a.ns + tok, grp = row * (D / a.group) + piece * 16 / a.group;
-      const uint32_t* src = static_cast<const uint32_t*>(codes) + (row * PIECES + piece) * W;
+  for (int k = 0; k < 128 * PIECES / TR_LOADERS; ++k) {
+    const int i = lt + k * TR_LOADERS, piece = i % PIECES, row = i / PIECES;
+    uint4 v[2] = {make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)};
+    if (tok0 + row < a.n) {
+      const uint32_t src = raw + (row * PIECES + piece) * (W * 4), m = raw + R::CODES + ((row * D + piece * 16) >> lg) * 2;
+      uint32_t w[W];
       if constexpr (W == 4) {
-        const uint4 v = __ldg(reinterpret_cast<const uint4*>(src));
-        w[k][0] = v.x; w[k][1] = v.y; w[k][2] = v.z; w[k][3] = v.w;
+        const uint4 x = lds128(src);
+        w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
       } else if constexpr (W == 2) {
-        const uint2 v = __ldg(reinterpret_cast<const uint2*>(src));
-        w[k][0] = v.x; w[k][1] = v.y;
+        const uint2 x = lds64(src);
+        w[0] = x.x; w[1] = x.y;
       } else {
-        w[k][0] = __ldg(src);
+        w[0] = lds32(src);
       }
-      s[k] = scale[grp];
-      z[k] = zero[grp];
-    }
-  }
-  __device__ __forceinline__ void put(const TreeArgs& a, int tok0, int lt, uint32_t slot) {
+      const uint32_t s2 = lds16(m) * 0x10001u, z2 = lds16(m + R::META) * 0x10001u;
+      // a word's pair f holds channels f and f + 16/BITS; pairs f, f + 1 make the channel pairs (f, f+1) and the upper ones
+      uint32_t c[8];                                            // channels (0,1) .. (14,15)
 #pragma unroll
-    for (int k = 0; k < PT_ITEMS; ++k) {
-      const int i = lt + k * TR_LOADERS, piece = i % PIECES, row = i / PIECES;
-      uint4 v[2] = {make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)};
-      if (tok0 + row < a.n) {
-        const __half2 sh = __half2half2(s[k]), zh = __half2half2(z[k]);
-        const uint32_t s2 = *reinterpret_cast<const uint32_t*>(&sh), z2 = *reinterpret_cast<const uint32_t*>(&zh);
-        // a word's pair f holds channels f and f + 16/BITS; pairs f, f + 1 make the channel pairs (f, f+1) and the upper ones
-        uint32_t c[8];                                          // channels (0,1) .. (14,15)
+      for (int j = 0; j < W; ++j) {
+        constexpr int U = 16 / BITS;
 #pragma unroll
-        for (int j = 0; j < W; ++j) {
-          constexpr int U = 16 / BITS;
-#pragma unroll
-          for (int f = 0; f < U; f += 2) {
-            const uint32_t p = code_pair<BITS>(w[k][j], f * BITS, s2, z2), q = code_pair<BITS>(w[k][j], (f + 1) * BITS, s2, z2);
-            c[j * U + f / 2] = __byte_perm(p, q, 0x5410);
-            c[j * U + U / 2 + f / 2] = __byte_perm(p, q, 0x7632);
-          }
+        for (int f = 0; f < U; f += 2) {
+          const uint32_t p = code_pair<BITS>(w[j], f * BITS, s2, z2), q = code_pair<BITS>(w[j], (f + 1) * BITS, s2, z2);
+          c[j * U + f / 2] = __byte_perm(p, q, 0x5410);
+          c[j * U + U / 2 + f / 2] = __byte_perm(p, q, 0x7632);
         }
-        v[0] = make_uint4(c[0], c[1], c[2], c[3]);
-        v[1] = make_uint4(c[4], c[5], c[6], c[7]);
       }
-      sts128(slot + tile_off(row, 2 * piece), v[0]);
-      sts128(slot + tile_off(row, 2 * piece + 1), v[1]);
+      v[0] = make_uint4(c[0], c[1], c[2], c[3]);
+      v[1] = make_uint4(c[4], c[5], c[6], c[7]);
     }
+    sts128(slot + tile_off(row, 2 * piece), v[0]);
+    sts128(slot + tile_off(row, 2 * piece + 1), v[1]);
   }
-};
+}
 // rows 128 x .. of the tail followed by the drafts, zeros behind them
-template <int D, bool HALF>
+template <int D, bool HALF, int TR_LOADERS>
 __device__ __forceinline__ void put_extra(const TreeArgs& a, bool keys, int b, int hk, int bh, int x, int lt, uint32_t slot) {
   constexpr int PIECES = D / 16;
   const uint16_t* tail = static_cast<const uint16_t*>(keys ? a.k_tail : a.v_tail);
@@ -224,10 +256,11 @@ template <int D>
 __device__ __forceinline__ uint32_t part_off(int r, int c) { return (uint32_t)(r * (D * 4) + ((c ^ (r & (D / 4 - 1))) << 4)); }
 
 template <int BITS, int D>
-__global__ void __launch_bounds__(TR_THREADS, 1)
+__global__ void __launch_bounds__(tr_threads(BITS), 1)
 tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-            int* __restrict__ error_word) {
+            int* __restrict__ error_words) {
   constexpr bool HALF = BITS < 16;
+  constexpr int TR_LOAD = tr_load(BITS), TR_THREADS = tr_threads(BITS);
   constexpr uint32_t SLOT = 128 * D * 2;
   constexpr uint32_t FMT = HALF ? 0u : (1u << 7) | (1u << 10);  // both operands fp16 / bf16
   constexpr uint32_t ID_S = (1u << 4) | FMT | ((128u >> 3) << 17) | ((128u >> 4) << 24);
@@ -241,10 +274,12 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
   const TreeArgs& a = p.a;
   const int tid = threadIdx.x, lane = tid & 31;
   const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
-  const int C = p.cluster, rank = blockIdx.x % C, item = blockIdx.x / C, rg = item % p.n_groups, bh = item / p.n_groups;
+  const int C = p.cluster, rank = blockIdx.x % C, sub = blockIdx.x / C % p.subs, item = blockIdx.x / C / p.subs;
+  const int rg = item % p.n_groups, bh = item / p.n_groups;
   const int b = bh / a.Hkv, hk = bh % a.Hkv, G = a.Hq / a.Hkv;
   const int row0 = rg * 256, rows = min(256, p.R - row0);       // of this group
-  const int j0 = (int)((long long)p.tiles * rank / C), n_loc = (int)((long long)p.tiles * (rank + 1) / C) - j0;
+  const int run = sub * C + rank, runs = p.subs * C;
+  const int j0 = (int)((long long)p.tiles * run / runs), n_loc = (int)((long long)p.tiles * (run + 1) / runs) - j0;
   const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t sQ = sbase, ring = sbase + (p.two_rows ? 2 : 1) * SLOT;
   const uint32_t bar0 = smem_u32(&bars[0]);
@@ -258,7 +293,7 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
     }
     for (int u = 0; u < 2; ++u) {
       mbar_init(bar(TB_S, u), 1);                               // a tcgen05.commit
-      mbar_init(bar(TB_P, u), 4);                               // the group's warps
+      mbar_init(bar(TB_P, u), max(1, min(4, (rows - (p.two_rows ? u * 128 : 0) + 31) / 32)));    // the group's warps with rows
     }
     give_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
@@ -268,15 +303,22 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
   }
   chain_enter();
-  // query rows t G + h of this group, zeros behind the last
-  for (int i = tid; i < (p.two_rows ? 256 : 128) * (D / 8); i += TR_THREADS) {
-    const int r = i / (D / 8), c = i % (D / 8), gr = row0 + r;
-    uint4 v = make_uint4(0u, 0u, 0u, 0u);
-    if (r < rows) {
-      v = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + (((size_t)b * a.T + gr / G) * a.Hq + hk * G + gr % G) * D + c * 8);
-      if (HALF) v = make_uint4(bf2_to_half2(v.x), bf2_to_half2(v.y), bf2_to_half2(v.z), bf2_to_half2(v.w));
+  // query rows t G + h of this group, zeros behind the last; four loads in flight
+  for (int i0 = tid; i0 < (p.two_rows ? 256 : 128) * (D / 8); i0 += 4 * TR_THREADS) {
+    uint4 v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int i = i0 + k * TR_THREADS, r = i / (D / 8), c = i % (D / 8), gr = row0 + r;
+      v[k] = make_uint4(0u, 0u, 0u, 0u);
+      if (r < rows)
+        v[k] = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + (((size_t)b * a.T + gr / G) * a.Hq + hk * G + gr % G) * D + c * 8));
     }
-    sts128(sQ + (r >> 7) * SLOT + tile_off(r & 127, c), v);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int i = i0 + k * TR_THREADS, r = i / (D / 8), c = i % (D / 8);
+      if (HALF) v[k] = make_uint4(bf2_to_half2(v[k].x), bf2_to_half2(v[k].y), bf2_to_half2(v[k].z), bf2_to_half2(v[k].w));
+      if (r < (p.two_rows ? 256 : 128)) sts128(sQ + (r >> 7) * SLOT + tile_off(r & 127, c), v[k]);
+    }
   }
   asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
   asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
@@ -297,11 +339,12 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const bool work = (p.two_rows ? u * 128 : 0) + (warp & 3) * 32 < rows;      // warp-uniform: has rows
     const unsigned long long mask = r < rows ? a.mask[(size_t)b * a.T + (row0 + r) / G] & (~0ull >> (64 - a.T)) : 0ull;
-    const int steps = stream_tiles(u);
+    // a warp without rows has nothing to do; a group without any sends its first warp to answer for it
+    const int steps = work || (warp & 3) == 0 ? stream_tiles(u) : 0;
     bool ok = true;
     for (int k = 0; k < steps; ++k) {
       const int j = j0 + (p.two_rows ? k : 2 * k + u);
-      ok = mbar_wait(bar(TB_S, u), (uint32_t)(k & 1), gu);
+      ok = mbar_wait_warp(bar(TB_S, u), (uint32_t)(k & 1), gu);
       if (!ok) break;
       if (work) {
         asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
@@ -317,76 +360,103 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
           return v;
         };
         const bool full = j < p.ctx_tiles && 128 * (j + 1) <= a.n;
-        float mx = -INFINITY;
+        if (k == 0) {                                           // the first reference: the first tile's maximum
+          float mx = -INFINITY;
 #pragma unroll 1
-        for (int c0 = 0; c0 < 128; c0 += 64) {
-          uint32_t x[32], y[32];
-          tmem_ld32_issue(ts + c0, x);
-          tmem_ld32_issue(ts + c0 + 32, y);
-          tmem_wait(x);
-          tmem_wait(y);
-          if (full) {
+          for (int c0 = 0; c0 < 128; c0 += 32) {
+            uint32_t x[32];
+            tmem_ld32_issue(ts + c0, x);
+            tmem_wait(x);
+            const uint32_t vis = visible(c0);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) mx = fmaxf(mx, fmaxf(__uint_as_float(x[i]), __uint_as_float(y[i])));
-          } else {
-            const uint32_t vx = visible(c0), vy = visible(c0 + 32);
-#pragma unroll
-            for (int i = 0; i < 32; ++i) {
-              mx = fmaxf(mx, (vx >> i) & 1u ? __uint_as_float(x[i]) : -INFINITY);
-              mx = fmaxf(mx, (vy >> i) & 1u ? __uint_as_float(y[i]) : -INFINITY);
-            }
+            for (int i = 0; i < 32; ++i) mx = fmaxf(mx, (vis >> i) & 1u ? __uint_as_float(x[i]) : -INFINITY);
+            __syncwarp();
           }
-          __syncwarp();
+          m_run = mx * scale_log2;                              // scale > 0; -inf stays
         }
-        mx *= scale_log2;                                       // scale > 0; -inf stays
-        // a new reference only where the old one is exceeded by more than 2^8 (or there is none yet)
-        const bool renew = mx > m_run + 8.f;
-        if (__any_sync(0xffffffffu, renew)) {
-          const float mn = renew ? mx : m_run, corr = renew ? ex2a(m_run - mn) : 1.f;
-          m_run = mn;
-          l_run *= corr;
-          if (k > 0) {
-#pragma unroll 1
-            for (int c0 = 0; c0 < D; c0 += 32) {
-              uint32_t o[32];
-              tmem_ld32_issue(tO(u) + lanes + c0, o);
-              tmem_wait(o);
-#pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * corr);
-              tmem_st32(tO(u) + lanes + c0, o);
-            }
-            tmem_wait_st();
-          }
-        }
-        const float ref = m_run == -INFINITY ? 0.f : m_run;
-        const uint64_t sc = pack2(scale_log2, scale_log2), nm = pack2(-ref, -ref);
+        const uint64_t sc = pack2(scale_log2, scale_log2);
         uint64_t sum2 = pack2(0.f, 0.f);
-#pragma unroll 1
-        for (int c0 = 0; c0 < 128; c0 += 32) {
-          uint32_t x[32], pk[16];
-          tmem_ld32_issue(ts + c0, x);
-          tmem_wait(x);
-          const uint32_t vis = full ? 0xffffffffu : visible(c0);
+        // 32 columns: P over columns of S that have been read.  Exceeds a logit the reference by more than 2^8 (or is there none
+        // yet), the row gets a new one, and what has been summed up to here is scaled down to it: O, the sum, this tile's P.
+        auto fold = [&](uint32_t (&x)[32], int c0) {
           if (!full) {
+            const uint32_t vis = visible(c0);
 #pragma unroll
             for (int i = 0; i < 32; ++i) x[i] = (vis >> i) & 1u ? x[i] : 0xff800000u;
           }
+          float mx0 = __uint_as_float(x[0]), mx1 = __uint_as_float(x[1]);
+#pragma unroll
+          for (int i = 2; i < 30; i += 4) {
+            mx0 = max3(mx0, __uint_as_float(x[i]), __uint_as_float(x[i + 1]));
+            mx1 = max3(mx1, __uint_as_float(x[i + 2]), __uint_as_float(x[i + 3]));
+          }
+          mx0 = max3(mx0, __uint_as_float(x[30]), __uint_as_float(x[31]));
+          const float mx = fmaxf(mx0, mx1) * scale_log2;
+          const bool renew = mx > m_run + 8.f;
+          if (__any_sync(0xffffffffu, renew)) {
+            const float mn = renew ? mx : m_run, corr = renew ? ex2a(m_run - mn) : 1.f;
+            m_run = mn;
+            l_run *= corr;
+            float s0, s1;
+            unpack2(sum2, s0, s1);
+            sum2 = pack2(s0 * corr, s1 * corr);
+#pragma unroll 1
+            for (int c = 0; c < c0 / 2; c += 16) {
+              uint32_t q[16];
+              tmem_ld16(ts + c, q);
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                const float lo = HALF ? __low2float(*reinterpret_cast<const __half2*>(&q[i])) : bf16lo(q[i]);
+                const float hi = HALF ? __high2float(*reinterpret_cast<const __half2*>(&q[i])) : bf16hi(q[i]);
+                q[i] = HALF ? pack_half2(lo * corr, hi * corr) : pack_bf16x2(lo * corr, hi * corr);
+              }
+              __syncwarp();
+              tmem_st16(ts + c, q);
+            }
+            if (k > 0) {
+#pragma unroll 1
+              for (int c = 0; c < D; c += 16) {
+                uint32_t o[16];
+                tmem_ld16(tO(u) + lanes + c, o);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * corr);
+                __syncwarp();
+                tmem_st16(tO(u) + lanes + c, o);
+              }
+            }
+            tmem_wait_st();
+          }
+          const float ref = m_run == -INFINITY ? 0.f : m_run;
+          const uint64_t nm = pack2(-ref, -ref);
+          uint32_t pk[16];
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
+            uint64_t e = fma2(pack2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), sc, nm);
             float e0, e1;
-            unpack2(fma2(pack2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), sc, nm), e0, e1);
-            e0 = ex2a(e0);
-            e1 = ex2a(e1);
-            sum2 = add2(sum2, pack2(e0, e1));
-            if (HALF) {
-              pk[i] = pack_half2(e0, e1);
+            if (i % 4 == 3) {                                   // a quarter of the exponentials on the FMA pipe
+              e = ex2_poly2<false>(e);
+              unpack2(e, e0, e1);
             } else {
-              const __nv_bfloat162 h = __floats2bfloat162_rn(e0, e1);
-              pk[i] = *reinterpret_cast<const uint32_t*>(&h);
+              unpack2(e, e0, e1);
+              e0 = ex2a(e0);
+              e1 = ex2a(e1);
+              e = pack2(e0, e1);
             }
+            sum2 = add2(sum2, e);
+            pk[i] = HALF ? pack_half2(e0, e1) : pack_bf16x2(e0, e1);
           }
           __syncwarp();
-          tmem_st16(ts + c0 / 2, pk);                           // over columns of S that have been read
+          tmem_st16(ts + c0 / 2, pk);
+        };
+#pragma unroll 1
+        for (int c0 = 0; c0 < 128; c0 += 64) {                  // not unrolled: the code has to stay in the instruction cache
+          uint32_t xa[32], xb[32];
+          tmem_ld32_issue(ts + c0, xa);
+          tmem_wait(xa);
+          tmem_ld32_issue(ts + c0 + 32, xb);
+          fold(xa, c0);
+          tmem_wait(xb);
+          fold(xb, c0 + 32);
         }
         float s0, s1;
         unpack2(sum2, s0, s1);
@@ -399,14 +469,14 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
     }
     // O is complete with one more commit
     if (ok && steps > 0) {
-      ok = mbar_wait(bar(TB_S, u), (uint32_t)(steps & 1), gu);
+      ok = mbar_wait_warp(bar(TB_S, u), (uint32_t)(steps & 1), gu);
       asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
     }
     if (!ok) give_up = 1;
   } else if (warp == TR_SOFT + TR_LOAD) {
     // ---- MMA warp.  Operand idx (keys of tile j: 2 j, values: 2 j + 1) sits in slot idx % slots.
     bool ok = true;
-    auto wait_full = [&](int idx) { ok = ok && mbar_wait(bar(TB_FULL, idx % p.slots), (uint32_t)((idx / p.slots) & 1), gu); };
+    auto wait_full = [&](int idx) { ok = ok && mbar_wait_warp(bar(TB_FULL, idx % p.slots), (uint32_t)((idx / p.slots) & 1), gu); };
     auto issue_s = [&](int jl, int u, bool last_reader) {
       asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
       if (lane == 0) {
@@ -441,7 +511,7 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
       for (int j = 0; j < n_loc && ok; ++j)
         for (int u = 0; u < 2 && ok; ++u) {
           if (u == 0) wait_full(2 * j + 1);
-          ok = ok && mbar_wait(bar(TB_P, u), (uint32_t)(j & 1), gu);
+          ok = ok && mbar_wait_warp(bar(TB_P, u), (uint32_t)(j & 1), gu);
           if (!ok) break;
           issue_o(j, u, j == 0, u == 1);
           if (j + 1 < n_loc) {
@@ -460,7 +530,7 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
       for (int j = 0; j < n_loc && ok; ++j) {
         const int u = j & 1;
         wait_full(2 * j + 1);
-        ok = ok && mbar_wait(bar(TB_P, u), (uint32_t)((j >> 1) & 1), gu);
+        ok = ok && mbar_wait_warp(bar(TB_P, u), (uint32_t)((j >> 1) & 1), gu);
         if (!ok) break;
         issue_o(j, u, j < 2, true);
         if (j + 2 < n_loc) {
@@ -478,7 +548,7 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
     const int lt = tid - TR_SOFT * 32;
     bool ok = true;
     auto wait_empty = [&](int idx) {
-      if (idx >= p.slots) ok = ok && mbar_wait(bar(TB_EMPTY, idx % p.slots), (uint32_t)((idx / p.slots - 1) & 1), gu);
+      if (idx >= p.slots) ok = ok && mbar_wait_warp(bar(TB_EMPTY, idx % p.slots), (uint32_t)((idx / p.slots - 1) & 1), gu);
     };
     auto slot_of = [&](int idx) { return ring + (idx % p.slots) * SLOT; };
     auto publish = [&](int idx) {                               // this warp's part of an operand is in place
@@ -512,33 +582,39 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
             if (mbar_try_wait(bar(TB_FULL, i % p.slots), (uint32_t)((i / p.slots) & 1))) break;
       }
     } else {
-      RowLoader<BITS, D> rk, rv;
-      ColLoader<BITS, D> ck;
+      // operand i: keys (even) or values (odd) of context tile i / 2, through raw stage i % p.raw
       const bool cols = a.k_axis == 0;
-      if (n_ctx > 0) {
-        if (cols) ck.fetch(a, bh, 128 * j0, lt); else rk.fetch(a, a.kc, a.ks, a.kz, bh, 128 * j0, lt);
+      const uint32_t raw0 = ring + p.slots * SLOT;
+      auto issue = [&](int i) {
+        const int tok0 = 128 * (j0 + i / 2);
+        const uint32_t raw = raw0 + (uint32_t)(i % p.raw) * Raw<BITS, D>::BYTES;
+        if (i & 1) raw_issue<BITS, D>(a, p.lg, false, a.vc, a.vs, a.vz, bh, tok0, lt, raw);
+        else raw_issue<BITS, D>(a, p.lg, cols, a.kc, a.ks, a.kz, bh, tok0, lt, raw);
+      };
+      for (int i = 0; i < p.raw - 1; ++i) {
+        if (i < 2 * n_ctx) issue(i);
+        cp_async_commit();
       }
-      for (int j = 0; j < n_ctx && ok; ++j) {
-        const int tok0 = 128 * (j0 + j);
-        rv.fetch(a, a.vc, a.vs, a.vz, bh, tok0, lt);
-        wait_empty(2 * j);
-        if (!ok) break;
-        if (cols) ck.put(a, tok0, lt, slot_of(2 * j)); else rk.put(a, tok0, lt, slot_of(2 * j));
-        publish(2 * j);
-        if (j + 1 < n_ctx) {
-          if (cols) ck.fetch(a, bh, tok0 + 128, lt); else rk.fetch(a, a.kc, a.ks, a.kz, bh, tok0 + 128, lt);
-        }
-        wait_empty(2 * j + 1);
-        if (!ok) break;
-        rv.put(a, tok0, lt, slot_of(2 * j + 1));
-        publish(2 * j + 1);
+      for (int i = 0; i < 2 * n_ctx; ++i) {
+        if (p.raw == 3) cp_async_wait<1>(); else cp_async_wait<2>();            // operand i has landed (this thread's part)
+        asm volatile("bar.sync 1, %0;\n" ::"n"(TR_LOAD * 32) : "memory");        // ... everybody's; and operand i - 1 is used up
+        if (i + p.raw - 1 < 2 * n_ctx) issue(i + p.raw - 1);
+        cp_async_commit();
+        if (ok) wait_empty(i);
+        if (!ok) continue;                                      // (keeps the loaders' barrier together)
+        const int tok0 = 128 * (j0 + i / 2);
+        const uint32_t raw = raw0 + (uint32_t)(i % p.raw) * Raw<BITS, D>::BYTES;
+        if (cols && !(i & 1)) put_cols<BITS, D>(a, p.lg, tok0, lt, raw, slot_of(i));
+        else put_rows<BITS, D>(a, p.lg, tok0, lt, raw, slot_of(i));
+        publish(i);
       }
+      cp_async_wait<0>();
     }
     for (int j = n_ctx; j < n_loc && ok; ++j)
       for (int kv = 0; kv < 2 && ok; ++kv) {
         wait_empty(2 * j + kv);
         if (!ok) break;
-        put_extra<D, HALF>(a, kv == 0, b, hk, bh, j0 + j - p.ctx_tiles, lt, slot_of(2 * j + kv));
+        put_extra<D, HALF, TR_LOAD * 32>(a, kv == 0, b, hk, bh, j0 + j - p.ctx_tiles, lt, slot_of(2 * j + kv));
         publish(2 * j + kv);
       }
     if (!ok) give_up = 1;
@@ -567,57 +643,102 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
       }
     }
   }
-  if (give_up && tid == 0) atomicExch(error_word, 1);
+  const int word = item * p.max_subs + sub;
+  if (tid == 0 && rank == 0) {                                  // (the cluster's barrier orders it before the next)
+    error_words[word] = 0;
+    for (int s = p.subs; sub == 0 && s < p.max_subs; ++s) error_words[item * p.max_subs + s] = 0;
+  }
   asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
   cluster.sync();
+  if (give_up && tid == 0) atomicExch(&error_words[word], 1);
   asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
   if (warp == TR_SOFT + TR_LOAD)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(512u) : "memory");
 
-  // ---- this CTA's slice of the rows: a warp per row, lane c the contribution c (CTA c / per, stream c % per) for the
-  // statistics, then the row's 16-byte chunk
+  // ---- this CTA's slice of the rows.  Contribution c of a row is with CTA c / per, stream c % per (two row tiles: the row's)
   const int per = p.two_rows ? 1 : 2, n_part = C * per;         // <= 32
-  const int r_lo = (int)((long long)rows * rank / C), r_hi = (int)((long long)rows * (rank + 1) / C);
-  for (int r = r_lo + warp; r < r_hi; r += TR_THREADS / 32) {
-    const int rl = r & 127, u_row = r >> 7;                     // two_rows: the stream that owns the row
-    float2 ml = make_float2(-INFINITY, 0.f);
-    if (lane < n_part) ml = cluster.map_shared_rank(s_ml, lane / per)[(p.two_rows ? u_row : lane % per) * 128 + rl];
-    float M = ml.x;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-    const float f = ml.x == -INFINITY ? 0.f : ex2a(ml.x - M);
-    float Z = ml.y * f;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) Z += __shfl_xor_sync(0xffffffffu, Z, o);
+  const int r_lo = (int)((long long)rows * rank / C), n_rows = (int)((long long)rows * (rank + 1) / C) - r_lo;
+  // their statistics, n_rows * n_part <= 256 + 32 pairs, behind this CTA's own
+  float2* s_all = s_ml + 256;
+  for (int i = tid; i < n_rows * n_part; i += TR_THREADS) {
+    const int r = r_lo + i / n_part, c = i % n_part;
+    s_all[i] = cluster.map_shared_rank(s_ml, c / per)[(p.two_rows ? r >> 7 : c % per) * 128 + (r & 127)];
+  }
+  __syncthreads();
+  for (int i = tid; i < n_rows * (D / 4); i += TR_THREADS) {    // a 16-byte chunk of a row's output
+    const int rr = i / (D / 4), ch = i % (D / 4), r = r_lo + rr, rl = r & 127;
+    const float2* ml = s_all + rr * n_part;
+    float M = -INFINITY, Z = 0.f;
+    for (int c = 0; c < n_part; ++c) M = fmaxf(M, ml[c].x);
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int c0 = 0; c0 < n_part; c0 += 8) {
       float4 v[8];
-      float fc[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        fc[i] = __shfl_sync(0xffffffffu, f, (c0 + i) & 31);
-        const int c = c0 + i;
-        v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (c < n_part && fc[i] != 0.f && lane < D / 4) {       // (a stream without tiles left nothing behind)
-          const unsigned char* base = cluster.map_shared_rank(part_base, c / per);
-          v[i] = *reinterpret_cast<const float4*>(base + (p.two_rows ? u_row : c % per) * PART + part_off<D>(rl, lane));
-        }
+      for (int k = 0; k < 8; ++k) {
+        const int c = c0 + k;
+        v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (c < n_part && ml[c].x != -INFINITY)                 // (a stream without tiles left nothing behind)
+          v[k] = *reinterpret_cast<const float4*>(cluster.map_shared_rank(part_base, c / per) + (p.two_rows ? r >> 7 : c % per) * PART +
+                                                  part_off<D>(rl, ch));
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        acc.x = fmaf(v[i].x, fc[i], acc.x); acc.y = fmaf(v[i].y, fc[i], acc.y);
-        acc.z = fmaf(v[i].z, fc[i], acc.z); acc.w = fmaf(v[i].w, fc[i], acc.w);
+      for (int k = 0; k < 8; ++k) {
+        const int c = c0 + k;
+        if (c >= n_part) break;
+        const float f = ml[c].x == -INFINITY ? 0.f : ex2a(ml[c].x - M);
+        Z = fmaf(ml[c].y, f, Z);
+        acc.x = fmaf(v[k].x, f, acc.x); acc.y = fmaf(v[k].y, f, acc.y);
+        acc.z = fmaf(v[k].z, f, acc.z); acc.w = fmaf(v[k].w, f, acc.w);
       }
     }
-    if (lane < D / 4) {
+    if (p.subs > 1) {                                           // for the merge: unnormalised, with its reference and sum
+      const size_t row = ((size_t)item * p.subs + sub) * 256 + r;
+      *reinterpret_cast<float4*>(p.part + row * D + 4 * ch) = acc;
+      if (ch == 0) p.part_ml[row] = make_float2(M, Z);
+    } else {
       const float inv = __fdiv_rn(1.0f, Z);
       const int gr = row0 + r;
-      const __nv_bfloat162 lo = __floats2bfloat162_rn(acc.x * inv, acc.y * inv), hi = __floats2bfloat162_rn(acc.z * inv, acc.w * inv);
-      *reinterpret_cast<uint2*>(static_cast<bf16*>(a.out) + (((size_t)b * a.T + gr / G) * a.Hq + hk * G + gr % G) * D + 4 * lane) =
-          make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+      *reinterpret_cast<uint2*>(static_cast<bf16*>(a.out) + (((size_t)b * a.T + gr / G) * a.Hq + hk * G + gr % G) * D + 4 * ch) =
+          make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
     }
   }
   cluster.sync();                                               // nobody leaves while another may still read its shared memory
+}
+
+// out from the partial results of several clusters per (KV head, row group), in their order: a 16-byte chunk of a row per thread
+template <int D>
+__global__ void __launch_bounds__(256)
+tree_merge_kernel(const __grid_constant__ TreeLaunch p) {
+  chain_enter();
+  const TreeArgs& a = p.a;
+  const int item = blockIdx.y, rg = item % p.n_groups, bh = item / p.n_groups, b = bh / a.Hkv, hk = bh % a.Hkv, G = a.Hq / a.Hkv;
+  const int i = blockIdx.x * 256 + threadIdx.x, r = i / (D / 4), ch = i % (D / 4), gr = rg * 256 + r;
+  if (gr >= p.R || r >= 256) return;
+  const size_t row = (size_t)item * p.subs * 256 + r;
+  float2 ml[TR_MAX_SUBS];
+  float4 v[TR_MAX_SUBS];
+  float M = -INFINITY, Z = 0.f;
+#pragma unroll
+  for (int s = 0; s < TR_MAX_SUBS; ++s)
+    if (s < p.subs) {
+      ml[s] = p.part_ml[row + s * 256];
+      v[s] = *reinterpret_cast<const float4*>(p.part + (row + s * 256) * D + 4 * ch);
+    }
+#pragma unroll
+  for (int s = 0; s < TR_MAX_SUBS; ++s)
+    if (s < p.subs) M = fmaxf(M, ml[s].x);
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int s = 0; s < TR_MAX_SUBS; ++s)
+    if (s < p.subs && ml[s].x != -INFINITY) {                   // (-inf: a run in which the row sees nothing)
+      const float f = ex2a(ml[s].x - M);
+      Z = fmaf(ml[s].y, f, Z);
+      acc.x = fmaf(v[s].x, f, acc.x); acc.y = fmaf(v[s].y, f, acc.y);
+      acc.z = fmaf(v[s].z, f, acc.z); acc.w = fmaf(v[s].w, f, acc.w);
+    }
+  const float inv = __fdiv_rn(1.0f, Z);
+  *reinterpret_cast<uint2*>(static_cast<bf16*>(a.out) + (((size_t)b * a.T + gr / G) * a.Hq + hk * G + gr % G) * D + 4 * ch) =
+      make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
 }
 
 // rows of one KV head as [n x D], zeros behind row n whatever the array holds there
@@ -633,6 +754,21 @@ cudaError_t token_map(CUtensorMap* map, const void* base, const TreeArgs& a) {
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
+// most clusters per (KV head, row group): as many as keep every SM busy with clusters of one
+int tree_max_subs(int items) { return std::max(1, std::min(TR_MAX_SUBS, 148 / items)); }
+struct TreeWorkspace {
+  size_t part, part_ml, total;   // the error words come first
+};
+TreeWorkspace tree_carve(const TreeArgs& a) {
+  const int items = a.Bt * a.Hkv * ((a.T * (a.Hq / a.Hkv) + 255) / 256), subs = tree_max_subs(items);
+  auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
+  TreeWorkspace w;
+  w.part = up((size_t)items * subs * sizeof(int));
+  w.part_ml = w.part + (subs > 1 ? (size_t)items * subs * 256 * a.D * sizeof(float) : 0);
+  w.total = w.part_ml + (subs > 1 ? (size_t)items * subs * 256 * sizeof(float2) : 0);
+  return w;
+}
+
 template <int BITS, int D>
 cudaError_t launch_tree_t(TreeLaunch p, const CUtensorMap& mk, const CUtensorMap& mv, int* err, cudaStream_t st) {
   static unsigned char done[64] = {};
@@ -646,7 +782,7 @@ cudaError_t launch_tree_t(TreeLaunch p, const CUtensorMap& mk, const CUtensorMap
   e = allow_smem(kernel, smem_max, done);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.blockDim = dim3(TR_THREADS);
+  cfg.blockDim = dim3(tr_threads(BITS));
   cfg.dynamicSmemBytes = smem_max;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
@@ -669,31 +805,48 @@ cudaError_t launch_tree_t(TreeLaunch p, const CUtensorMap& mk, const CUtensorMap
     }
     active[dev][0] = 1;
   }
-  p.slots = p.two_rows ? 5 : 6;
-  // CTAs per (KV head, row group): the shortest schedule, rounds of (tiles + about three tiles of set-up and exchange)
-  const int items = p.a.Bt * p.a.Hkv * p.n_groups;
+  if (BITS == 16) {
+    p.slots = p.two_rows ? 5 : 6;
+  } else {                                                      // the least the order of the products needs; raw stages from the rest
+    p.slots = p.two_rows ? 3 : 4;
+    p.raw = (2 * SLOT) / Raw<BITS == 16 ? 8 : BITS, D>::BYTES >= 4 ? 4 : 3;
+  }
+  // CTAs per cluster and clusters per (KV head, row group): the shortest schedule, rounds of (tiles + about three tiles of set-up
+  // and exchange), the merge of several clusters about another one and a half.  Large clusters need no merge, but leave SMs idle
+  // that do not fill one inside their GPC.
+  const int items = p.a.Bt * p.a.Hkv * p.n_groups, max_subs = tree_max_subs(items);
   double best = 1e300;
-  p.cluster = 1;
+  p.cluster = p.subs = 1;
+  p.max_subs = max_subs;
   for (int c = 1; c <= TR_MAX_CLUSTER && c <= p.tiles; ++c) {
     if (active[dev][c] < 1) continue;
-    const double cost = (double)((items + active[dev][c] - 1) / active[dev][c]) * ((p.tiles + c - 1) / c + 3);
-    if (cost < best) { best = cost; p.cluster = c; }
+    for (int s = 1; s <= max_subs && s * c <= p.tiles; ++s) {
+      const double cost = (double)(((long long)items * s + active[dev][c] - 1) / active[dev][c]) * ((p.tiles + s * c - 1) / (s * c) + 3) +
+                          (s > 1 ? 1.5 : 0.) + 0.01 * c;
+      if (cost < best) { best = cost; p.cluster = c; p.subs = s; }
+    }
   }
-  cfg.gridDim = dim3((unsigned)items * p.cluster);
+  cfg.gridDim = dim3((unsigned)items * p.subs * p.cluster);
   attr[0].val.clusterDim.x = p.cluster;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, kernel, p, mk, mv, err);
+  e = cudaLaunchKernelEx(&cfg, kernel, p, mk, mv, err);
+  if (e != cudaSuccess || p.subs == 1) return e;
+  const int chunks = std::min(256, p.R) * (D / 4);
+  return launch_chained(tree_merge_kernel<D>, dim3((chunks + 255) / 256, items), dim3(256), 0, st, p);
 }
 
 }  // namespace
 
-size_t tree_workspace(const TreeArgs&) { return 256; }
+size_t tree_workspace(const TreeArgs& a) { return tree_carve(a).total; }
 
 cudaError_t launch_tree(const TreeArgs& a, void* ws, cudaStream_t st) {
-  int* err = reinterpret_cast<int*>(static_cast<char*>(ws) + tree_workspace(a) - 256);
-  cudaError_t e = cudaMemsetAsync(err, 0, sizeof(int), st);
-  if (e != cudaSuccess) return e;
+  int* err = static_cast<int*>(ws);
+  cudaError_t e = cudaSuccess;
   TreeLaunch p{};
+  const TreeWorkspace w = tree_carve(a);
+  p.part = reinterpret_cast<float*>(static_cast<char*>(ws) + w.part);
+  p.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + w.part_ml);
+  p.lg = a.group == 32 ? 5 : a.group == 64 ? 6 : 7;
   p.a = a;
   p.R = a.T * (a.Hq / a.Hkv);
   p.n_groups = (p.R + 255) / 256;
