@@ -11,8 +11,8 @@
 //                     one arrive as zeros whatever the array holds there.  Tail and drafts form the last one or two tiles.
 //   1 MMA warp        S[u] = Q[u] K_j^T into tensor memory; O[u] += P[u] V_j with P from tensor memory and V read with its rows
 //                     as the contraction, so neither operand is transposed
-//   2 softmax groups  u = 0, 1, four warps each, one row per thread: no shuffles.  S is read once; P overwrites the columns
-//                     of S already read.  O is rescaled only when the maximum grows by more than 2^8
+//   2 softmax groups  u = 0, 1, four warps each, one row per thread: no shuffles.  S is read twice (maximum; exponentials); P
+//                     overwrites the columns of S already read.  O is rescaled only when the maximum grows by more than 2^8
 //                     (the weights then stay below 2^8 in 16 bits, relative precision unchanged).
 // u is a tile of 128 rows when there are two, else (R <= 128) the parity of the token tile: two independent streams either
 // way, so one group's exponentials run beside the other's products.
@@ -58,6 +58,16 @@ struct TreeLaunch {
   int lg;                    // log2 of the quantization group
   float* part;               // [KV head, row group][sub][256][D], then
   float2* part_ml;           // [KV head, row group][sub][256]
+};
+
+// a place in a ring of n, with the parity of the round; walks without divisions
+struct Ring {
+  int i = 0;
+  uint32_t round = 0;
+  __device__ __forceinline__ void next(int n, int step = 1) {
+    i += step;
+    if (i >= n) { i -= n; round ^= 1u; }
+  }
 };
 
 // byte offset of 16-byte chunk c of row r in an operand tile of 128 rows
@@ -360,104 +370,86 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
           return v;
         };
         const bool full = j < p.ctx_tiles && 128 * (j + 1) <= a.n;
-        if (k == 0) {                                           // the first reference: the first tile's maximum
-          float mx = -INFINITY;
-#pragma unroll 1
-          for (int c0 = 0; c0 < 128; c0 += 32) {
-            uint32_t x[32];
-            tmem_ld32_issue(ts + c0, x);
-            tmem_wait(x);
-            const uint32_t vis = visible(c0);
+        uint32_t xa[32], xb[32];
+        auto hide = [&](uint32_t (&x)[32], int c0) {            // what the row does not see
+          const uint32_t vis = visible(c0);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) mx = fmaxf(mx, (vis >> i) & 1u ? __uint_as_float(x[i]) : -INFINITY);
-            __syncwarp();
-          }
-          m_run = mx * scale_log2;                              // scale > 0; -inf stays
-        }
-        const uint64_t sc = pack2(scale_log2, scale_log2);
-        uint64_t sum2 = pack2(0.f, 0.f);
-        // 32 columns: P over columns of S that have been read.  Exceeds a logit the reference by more than 2^8 (or is there none
-        // yet), the row gets a new one, and what has been summed up to here is scaled down to it: O, the sum, this tile's P.
-        auto fold = [&](uint32_t (&x)[32], int c0) {
-          if (!full) {
-            const uint32_t vis = visible(c0);
+          for (int i = 0; i < 32; ++i) x[i] = (vis >> i) & 1u ? x[i] : 0xff800000u;
+        };
+        // the tile's maximum, columns 0..31 last: they stay in registers for the second pass
+        float mx0 = -INFINITY, mx1 = -INFINITY;
+        auto top = [&](uint32_t (&x)[32], int c0) {
+          if (!full) hide(x, c0);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) x[i] = (vis >> i) & 1u ? x[i] : 0xff800000u;
-          }
-          float mx0 = __uint_as_float(x[0]), mx1 = __uint_as_float(x[1]);
-#pragma unroll
-          for (int i = 2; i < 30; i += 4) {
+          for (int i = 0; i < 32; i += 4) {
             mx0 = max3(mx0, __uint_as_float(x[i]), __uint_as_float(x[i + 1]));
             mx1 = max3(mx1, __uint_as_float(x[i + 2]), __uint_as_float(x[i + 3]));
           }
-          mx0 = max3(mx0, __uint_as_float(x[30]), __uint_as_float(x[31]));
-          const float mx = fmaxf(mx0, mx1) * scale_log2;
-          const bool renew = mx > m_run + 8.f;
-          if (__any_sync(0xffffffffu, renew)) {
-            const float mn = renew ? mx : m_run, corr = renew ? ex2a(m_run - mn) : 1.f;
-            m_run = mn;
-            l_run *= corr;
-            float s0, s1;
-            unpack2(sum2, s0, s1);
-            sum2 = pack2(s0 * corr, s1 * corr);
+        };
+        tmem_ld32_issue(ts + 96, xa);
+        tmem_wait(xa);
+        tmem_ld32_issue(ts + 64, xb);
+        top(xa, 96);
+        tmem_wait(xb);
+        tmem_ld32_issue(ts + 32, xa);
+        top(xb, 64);
+        tmem_wait(xa);
+        tmem_ld32_issue(ts, xb);
+        top(xa, 32);
+        tmem_wait(xb);
+        top(xb, 0);
+        const float mx = fmaxf(mx0, mx1) * scale_log2;          // scale > 0; -inf stays
+        // a new reference only where the old one is exceeded by more than 2^8 (or there is none yet)
+        const bool renew = mx > m_run + 8.f;
+        if (__any_sync(0xffffffffu, renew)) {
+          const float mn = renew ? mx : m_run, corr = renew ? ex2a(m_run - mn) : 1.f;
+          m_run = mn;
+          l_run *= corr;
+          if (k > 0) {
 #pragma unroll 1
-            for (int c = 0; c < c0 / 2; c += 16) {
-              uint32_t q[16];
-              tmem_ld16(ts + c, q);
+            for (int c = 0; c < D; c += 16) {
+              uint32_t o[16];
+              tmem_ld16(tO(u) + lanes + c, o);
 #pragma unroll
-              for (int i = 0; i < 16; ++i) {
-                const float lo = HALF ? __low2float(*reinterpret_cast<const __half2*>(&q[i])) : bf16lo(q[i]);
-                const float hi = HALF ? __high2float(*reinterpret_cast<const __half2*>(&q[i])) : bf16hi(q[i]);
-                q[i] = HALF ? pack_half2(lo * corr, hi * corr) : pack_bf16x2(lo * corr, hi * corr);
-              }
+              for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * corr);
               __syncwarp();
-              tmem_st16(ts + c, q);
-            }
-            if (k > 0) {
-#pragma unroll 1
-              for (int c = 0; c < D; c += 16) {
-                uint32_t o[16];
-                tmem_ld16(tO(u) + lanes + c, o);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * corr);
-                __syncwarp();
-                tmem_st16(tO(u) + lanes + c, o);
-              }
+              tmem_st16(tO(u) + lanes + c, o);
             }
             tmem_wait_st();
           }
-          const float ref = m_run == -INFINITY ? 0.f : m_run;
-          const uint64_t nm = pack2(-ref, -ref);
+        }
+        const float ref = m_run == -INFINITY ? 0.f : m_run;
+        const uint64_t sc = pack2(scale_log2, scale_log2), nm = pack2(-ref, -ref);
+        uint64_t sum2 = pack2(0.f, 0.f), sum3 = sum2;
+        // 32 columns: P over columns of S that have been read
+        auto fold = [&](const uint32_t (&x)[32], int c0) {
           uint32_t pk[16];
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            uint64_t e = fma2(pack2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), sc, nm);
             float e0, e1;
-            if (i % 4 == 3) {                                   // a quarter of the exponentials on the FMA pipe
-              e = ex2_poly2<false>(e);
-              unpack2(e, e0, e1);
-            } else {
-              unpack2(e, e0, e1);
-              e0 = ex2a(e0);
-              e1 = ex2a(e1);
-              e = pack2(e0, e1);
-            }
-            sum2 = add2(sum2, e);
+            unpack2(fma2(pack2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), sc, nm), e0, e1);
+            e0 = ex2a(e0);
+            e1 = ex2a(e1);
+            if (i & 1) sum3 = add2(sum3, pack2(e0, e1)); else sum2 = add2(sum2, pack2(e0, e1));
             pk[i] = HALF ? pack_half2(e0, e1) : pack_bf16x2(e0, e1);
           }
           __syncwarp();
           tmem_st16(ts + c0 / 2, pk);
         };
-#pragma unroll 1
-        for (int c0 = 0; c0 < 128; c0 += 64) {                  // not unrolled: the code has to stay in the instruction cache
-          uint32_t xa[32], xb[32];
-          tmem_ld32_issue(ts + c0, xa);
-          tmem_wait(xa);
-          tmem_ld32_issue(ts + c0 + 32, xb);
-          fold(xa, c0);
-          tmem_wait(xb);
-          fold(xb, c0 + 32);
-        }
+        tmem_ld32_issue(ts + 32, xa);
+        fold(xb, 0);
+        tmem_wait(xa);
+        if (!full) hide(xa, 32);
+        tmem_ld32_issue(ts + 64, xb);
+        fold(xa, 32);
+        tmem_wait(xb);
+        if (!full) hide(xb, 64);
+        tmem_ld32_issue(ts + 96, xa);
+        fold(xb, 64);
+        tmem_wait(xa);
+        if (!full) hide(xa, 96);
+        fold(xa, 96);
+        sum2 = add2(sum2, sum3);
         float s0, s1;
         unpack2(sum2, s0, s1);
         l_run += s0 + s1;
@@ -474,71 +466,78 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
     }
     if (!ok) give_up = 1;
   } else if (warp == TR_SOFT + TR_LOAD) {
-    // ---- MMA warp.  Operand idx (keys of tile j: 2 j, values: 2 j + 1) sits in slot idx % slots.
+    // ---- MMA warp.  Operands in the ring: keys of tile 0, values of tile 0, keys of tile 1, ...
     bool ok = true;
-    auto wait_full = [&](int idx) { ok = ok && mbar_wait_warp(bar(TB_FULL, idx % p.slots), (uint32_t)((idx / p.slots) & 1), gu); };
-    auto issue_s = [&](int jl, int u, bool last_reader) {
+    Ring kr, vr;                                                // the next keys and values
+    vr.next(p.slots);
+    auto wait_full = [&](const Ring& r) { ok = ok && mbar_wait_warp(bar(TB_FULL, r.i), r.round, gu); };
+    auto issue_s = [&](int u, bool last_reader) {
       asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
       if (lane == 0) {
-        const uint32_t q = sQ + (p.two_rows ? u : 0) * SLOT, kk = ring + (2 * jl % p.slots) * SLOT;
+        const uint32_t q = sQ + (p.two_rows ? u : 0) * SLOT, kk = ring + kr.i * SLOT;
 #pragma unroll
         for (int kb = 0; kb < D / 64; ++kb)
 #pragma unroll
           for (int s = 0; s < 4; ++s)
             umma_bf16(tS(u), smem_desc(q + kb * 16384 + s * 32), smem_desc(kk + kb * 16384 + s * 32), ID_S, (kb | s) ? 1u : 0u);
-        if (last_reader) umma_commit(bar(TB_EMPTY, 2 * jl % p.slots));
         umma_commit(bar(TB_S, u));
+        if (last_reader) umma_commit(bar(TB_EMPTY, kr.i));
       }
       __syncwarp();
+      if (last_reader) kr.next(p.slots, 2);
     };
-    auto issue_o = [&](int jl, int u, bool first, bool last_reader) {
+    auto issue_o = [&](int u, bool first, bool last_reader) {
       asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
       if (lane == 0) {
-        const uint32_t vv = ring + ((2 * jl + 1) % p.slots) * SLOT;
+        const uint32_t vv = ring + vr.i * SLOT;
 #pragma unroll
         for (int s = 0; s < 8; ++s)
           umma_ts(tO(u), tS(u) + 8 * s, smem_desc_mn(vv + s * 2048, 16384), ID_O, (first && s == 0) ? 0u : 1u);
-        if (last_reader) umma_commit(bar(TB_EMPTY, (2 * jl + 1) % p.slots));
+        if (last_reader) umma_commit(bar(TB_EMPTY, vr.i));
       }
+      __syncwarp();
+      if (last_reader) vr.next(p.slots, 2);
+    };
+    // stream u's last product is followed by one more commit: O[u] is complete
+    auto finish = [&](int u) {
+      if (lane == 0) umma_commit(bar(TB_S, u));
       __syncwarp();
     };
     if (p.two_rows) {
       if (n_loc > 0) {
-        wait_full(0);
-        if (ok) issue_s(0, 0, false);
-        if (ok) issue_s(0, 1, true);
+        wait_full(kr);
+        if (ok) issue_s(0, false);
+        if (ok) issue_s(1, true);
       }
       for (int j = 0; j < n_loc && ok; ++j)
         for (int u = 0; u < 2 && ok; ++u) {
-          if (u == 0) wait_full(2 * j + 1);
+          if (u == 0) wait_full(vr);
           ok = ok && mbar_wait_warp(bar(TB_P, u), (uint32_t)(j & 1), gu);
           if (!ok) break;
-          issue_o(j, u, j == 0, u == 1);
+          issue_o(u, j == 0, u == 1);
           if (j + 1 < n_loc) {
-            if (u == 0) wait_full(2 * j + 2);
-            if (ok) issue_s(j + 1, u, u == 1);
+            if (u == 0) wait_full(kr);
+            if (ok) issue_s(u, u == 1);
           } else {
-            if (lane == 0) umma_commit(bar(TB_S, u));           // O[u] is complete
-            __syncwarp();
+            finish(u);
           }
         }
     } else {
       for (int j = 0; j < min(2, n_loc) && ok; ++j) {
-        wait_full(2 * j);
-        if (ok) issue_s(j, j, true);
+        wait_full(kr);
+        if (ok) issue_s(j, true);
       }
       for (int j = 0; j < n_loc && ok; ++j) {
         const int u = j & 1;
-        wait_full(2 * j + 1);
+        wait_full(vr);
         ok = ok && mbar_wait_warp(bar(TB_P, u), (uint32_t)((j >> 1) & 1), gu);
         if (!ok) break;
-        issue_o(j, u, j < 2, true);
+        issue_o(u, j < 2, true);
         if (j + 2 < n_loc) {
-          wait_full(2 * j + 4);
-          if (ok) issue_s(j + 2, u, true);
+          wait_full(kr);
+          if (ok) issue_s(u, true);
         } else {
-          if (lane == 0) umma_commit(bar(TB_S, u));
-          __syncwarp();
+          finish(u);
         }
       }
     }
@@ -546,34 +545,41 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
   } else {
     // ---- loader warps
     const int lt = tid - TR_SOFT * 32;
-    bool ok = true;
-    auto wait_empty = [&](int idx) {
-      if (idx >= p.slots) ok = ok && mbar_wait_warp(bar(TB_EMPTY, idx % p.slots), (uint32_t)((idx / p.slots - 1) & 1), gu);
+    bool ok = true, filled = false;                             // filled: the ring has been round once
+    Ring wr;                                                    // the next operand's slot
+    auto wait_empty = [&]() {
+      if (filled) ok = ok && mbar_wait_warp(bar(TB_EMPTY, wr.i), wr.round ^ 1u, gu);
     };
-    auto slot_of = [&](int idx) { return ring + (idx % p.slots) * SLOT; };
-    auto publish = [&](int idx) {                               // this warp's part of an operand is in place
+    auto slot = [&]() { return ring + wr.i * SLOT; };
+    auto advance = [&]() {
+      wr.next(p.slots);
+      filled = filled || wr.i == 0;
+    };
+    auto publish = [&]() {                                      // this warp's part of an operand is in place
       asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar(TB_FULL, idx % p.slots));
+      if (lane == 0) mbar_arrive(bar(TB_FULL, wr.i));
+      advance();
     };
     const int n_ctx = max(0, min(n_loc, p.ctx_tiles - j0));     // this block's context tiles
     if constexpr (BITS == 16) {
       int issued = 0;
       for (int i = 0; i < 2 * n_ctx; ++i) {
-        wait_empty(i);
+        wait_empty();
         if (!ok) break;
         if (lane == 0) {
           if (warp == TR_SOFT) {
-            mbar_expect_tx(bar(TB_FULL, i % p.slots), SLOT);
+            mbar_expect_tx(bar(TB_FULL, wr.i), SLOT);
 #pragma unroll
             for (int kb = 0; kb < D / 64; ++kb)
-              tma_load_3d(slot_of(i) + kb * 16384, i & 1 ? &map_v : &map_k, kb * 64, 128 * (j0 + i / 2), bh, bar(TB_FULL, i % p.slots));
+              tma_load_3d(slot() + kb * 16384, i & 1 ? &map_v : &map_k, kb * 64, 128 * (j0 + i / 2), bh, bar(TB_FULL, wr.i));
           } else {
-            mbar_arrive(bar(TB_FULL, i % p.slots));
+            mbar_arrive(bar(TB_FULL, wr.i));
           }
         }
         issued = i + 1;
         __syncwarp();
+        advance();
       }
       if (!ok && warp == TR_SOFT) {
         // the copies still on their way land in this block's shared memory: wait (bounded) for them before it is given up
@@ -582,40 +588,46 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
             if (mbar_try_wait(bar(TB_FULL, i % p.slots), (uint32_t)((i / p.slots) & 1))) break;
       }
     } else {
-      // operand i: keys (even) or values (odd) of context tile i / 2, through raw stage i % p.raw
+      // operand i: keys (even) or values (odd) of context tile i / 2, through the raw stages in turn
       const bool cols = a.k_axis == 0;
-      const uint32_t raw0 = ring + p.slots * SLOT;
+      const uint32_t raw0 = ring + p.slots * SLOT, raw_end = raw0 + p.raw * Raw<BITS, D>::BYTES;
+      uint32_t raw_in = raw0, raw_out = raw0;
       auto issue = [&](int i) {
         const int tok0 = 128 * (j0 + i / 2);
-        const uint32_t raw = raw0 + (uint32_t)(i % p.raw) * Raw<BITS, D>::BYTES;
-        if (i & 1) raw_issue<BITS, D>(a, p.lg, false, a.vc, a.vs, a.vz, bh, tok0, lt, raw);
-        else raw_issue<BITS, D>(a, p.lg, cols, a.kc, a.ks, a.kz, bh, tok0, lt, raw);
+        if (i & 1) raw_issue<BITS, D>(a, p.lg, false, a.vc, a.vs, a.vz, bh, tok0, lt, raw_in);
+        else raw_issue<BITS, D>(a, p.lg, cols, a.kc, a.ks, a.kz, bh, tok0, lt, raw_in);
+      };
+      auto turn = [&](uint32_t& raw) {
+        raw += Raw<BITS, D>::BYTES;
+        if (raw == raw_end) raw = raw0;
       };
       for (int i = 0; i < p.raw - 1; ++i) {
         if (i < 2 * n_ctx) issue(i);
+        turn(raw_in);
         cp_async_commit();
       }
       for (int i = 0; i < 2 * n_ctx; ++i) {
         if (p.raw == 3) cp_async_wait<1>(); else cp_async_wait<2>();            // operand i has landed (this thread's part)
-        asm volatile("bar.sync 1, %0;\n" ::"n"(TR_LOAD * 32) : "memory");        // ... everybody's; and operand i - 1 is used up
+        asm volatile("bar.sync 1, %0;\n" ::"n"(TR_LOAD * 32) : "memory");      // ... everybody's; and operand i - 1 is used up
         if (i + p.raw - 1 < 2 * n_ctx) issue(i + p.raw - 1);
+        turn(raw_in);
         cp_async_commit();
-        if (ok) wait_empty(i);
+        wait_empty();
         if (!ok) continue;                                      // (keeps the loaders' barrier together)
         const int tok0 = 128 * (j0 + i / 2);
-        const uint32_t raw = raw0 + (uint32_t)(i % p.raw) * Raw<BITS, D>::BYTES;
-        if (cols && !(i & 1)) put_cols<BITS, D>(a, p.lg, tok0, lt, raw, slot_of(i));
-        else put_rows<BITS, D>(a, p.lg, tok0, lt, raw, slot_of(i));
-        publish(i);
+        if (cols && !(i & 1)) put_cols<BITS, D>(a, p.lg, tok0, lt, raw_out, slot());
+        else put_rows<BITS, D>(a, p.lg, tok0, lt, raw_out, slot());
+        turn(raw_out);
+        publish();
       }
       cp_async_wait<0>();
     }
     for (int j = n_ctx; j < n_loc && ok; ++j)
       for (int kv = 0; kv < 2 && ok; ++kv) {
-        wait_empty(2 * j + kv);
+        wait_empty();
         if (!ok) break;
-        put_extra<D, HALF, TR_LOAD * 32>(a, kv == 0, b, hk, bh, j0 + j - p.ctx_tiles, lt, slot_of(2 * j + kv));
-        publish(2 * j + kv);
+        put_extra<D, HALF, TR_LOAD * 32>(a, kv == 0, b, hk, bh, j0 + j - p.ctx_tiles, lt, slot());
+        publish();
       }
     if (!ok) give_up = 1;
   }
