@@ -272,18 +272,18 @@ prompt_sweep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
         if (!ok) continue;
         ++uses[g];
         asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
-        if (lane == 0) {
-          const uint32_t a = sA + g * OPER, s = sS + st * OPER, tm = tmem_base + g * 128;
+        const uint32_t a = uniform(desc_lo(sA + g * OPER, 1)), s = uniform(desc_lo(sS + st * OPER, 1));
+        const uint32_t tm = uniform(tmem_base + g * 128), done = uniform(bar(PB_T_FULL, g));
+        if (elect_one()) {
+          umma_ss<false>(tm, a, s, IDESC);
 #pragma unroll
-          for (int kb = 0; kb < D / 64; ++kb)
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              umma_bf16(tm, smem_desc(a + kb * 16384 + k * 32), smem_desc(s + kb * 16384 + k * 32), IDESC, (kb | k) ? 1u : 0u);
-          umma_commit(bar(PB_T_FULL, g));
+          for (int k = 1; k < D / 16; ++k) umma_ss<true>(tm, a + (k / 4) * 1024 + (k % 4) * 2, s + (k / 4) * 1024 + (k % 4) * 2, IDESC);
+          umma_commit(done);
         }
         __syncwarp();
       }
-      if (ok && lane == 0) umma_commit(bar(PB_S_EMPTY, st));
+      const uint32_t empty = uniform(bar(PB_S_EMPTY, st));
+      if (ok && elect_one()) umma_commit(empty);
       __syncwarp();
       if (PASS == 2 && ++t == p.nqt) t = t0;
     }

@@ -184,27 +184,6 @@ __device__ __forceinline__ uint64_t ex2_poly2(uint64_t x) {
                __uint_as_float(__float_as_uint(b) + (__float_as_uint(tb) << 23)));
 }
 
-// as umma_bf16 (the element types are in the instruction descriptor), operand A from tensor memory: two 16-bit elements a column
-__device__ __forceinline__ void umma_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t db, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}\n" ::"r"(tmem_d),
-      "r"(tmem_a), "l"(db), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
-// shared-memory matrix descriptor of the same tiles ([rows][64 columns] blocks of 128-byte rows, 128-byte swizzle) read with the
-// ROWS as the contraction: the contiguous direction is then the operand's outer one; blocks of 64 columns are `block` bytes apart,
-// groups of eight rows 1024 bytes
-__device__ __forceinline__ uint64_t smem_desc_mn(uint32_t saddr, uint32_t block) {
-  uint64_t d = 0;
-  d |= (uint64_t)((saddr & 0x3ffffu) >> 4);
-  d |= (uint64_t)(block >> 4) << 16;
-  d |= (uint64_t)(1024 >> 4) << 32;
-  d |= (uint64_t)1 << 46;
-  d |= (uint64_t)2 << 61;
-  return d;
-}
 // 16 columns of this warp's 32 TMEM lanes
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
   asm volatile(
@@ -226,5 +205,37 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
       : "memory");
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory"); }
+
+// ---- products issued from uniform registers.  A tcgen05.mma takes its descriptors from the warp's uniform registers; computed
+// per thread they are moved there one by one, about 100 clocks for each product of 64.  So the callers broadcast the operands'
+// addresses once per tile (uniform()), one thread is elected in place (elect_one), and only the low word of a descriptor walks.
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __shfl_sync(0xffffffffu, v, 0); }
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}\n" : "=r"(p));
+  return p != 0;
+}
+constexpr uint32_t kDescHi = (1024 >> 4) | 1u << 14 | 2u << 29;   // 1024 bytes between groups of eight rows, version, 128-byte swizzle
+// low word of a descriptor: address in 16-byte units; leading offset `lead` in the same (K-major operands ignore it)
+__device__ __forceinline__ uint32_t desc_lo(uint32_t saddr, uint32_t lead) { return ((saddr & 0x3ffffu) >> 4) | lead << 16; }
+template <bool ACCUMULATE>
+__device__ __forceinline__ void umma_ss(uint32_t tmem_d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+      "mov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\t"
+      "setp.ne.b32 p, %5, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, p;\n\t}\n" ::"r"(tmem_d),
+      "r"(a_lo), "r"(b_lo), "n"(kDescHi), "r"(idesc), "n"(ACCUMULATE ? 1 : 0)
+      : "memory");
+}
+__device__ __forceinline__ void umma_ts(uint32_t tmem_d, uint32_t tmem_a, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\t"
+      "mov.b64 db, {%2, %3};\n\t"
+      "setp.ne.b32 p, %5, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n\t}\n" ::"r"(tmem_d),
+      "r"(tmem_a), "r"(b_lo), "n"(kDescHi), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
 
 }  // namespace qp

@@ -473,34 +473,36 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
     auto wait_full = [&](const Ring& r) { ok = ok && mbar_wait_warp(bar(TB_FULL, r.i), r.round, gu); };
     auto issue_s = [&](int u, bool last_reader) {
       asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
-      if (lane == 0) {
-        const uint32_t q = sQ + (p.two_rows ? u : 0) * SLOT, kk = ring + kr.i * SLOT;
+      const uint32_t q = uniform(desc_lo(sQ + (p.two_rows ? u : 0) * SLOT, 1)), kk = uniform(desc_lo(ring + kr.i * SLOT, 1));
+      const uint32_t d = uniform(tS(u)), done = uniform(bar(TB_S, u)), empty = uniform(bar(TB_EMPTY, kr.i));
+      if (elect_one()) {
+        umma_ss<false>(d, q, kk, ID_S);
 #pragma unroll
-        for (int kb = 0; kb < D / 64; ++kb)
-#pragma unroll
-          for (int s = 0; s < 4; ++s)
-            umma_bf16(tS(u), smem_desc(q + kb * 16384 + s * 32), smem_desc(kk + kb * 16384 + s * 32), ID_S, (kb | s) ? 1u : 0u);
-        umma_commit(bar(TB_S, u));
-        if (last_reader) umma_commit(bar(TB_EMPTY, kr.i));
+        for (int s = 1; s < D / 16; ++s) umma_ss<true>(d, q + (s / 4) * 1024 + (s % 4) * 2, kk + (s / 4) * 1024 + (s % 4) * 2, ID_S);
+        umma_commit(done);
+        if (last_reader) umma_commit(empty);
       }
       __syncwarp();
       if (last_reader) kr.next(p.slots, 2);
     };
     auto issue_o = [&](int u, bool first, bool last_reader) {
       asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
-      if (lane == 0) {
-        const uint32_t vv = ring + vr.i * SLOT;
+      // values with their rows as the contraction: blocks of 64 columns are 16 KB apart, 16 rows 2 KB
+      const uint32_t vv = uniform(desc_lo(ring + vr.i * SLOT, 1024)), d = uniform(tO(u)), pp = uniform(tS(u));
+      const uint32_t empty = uniform(bar(TB_EMPTY, vr.i));
+      if (elect_one()) {
+        umma_ts(d, pp, vv, ID_O, first ? 0u : 1u);
 #pragma unroll
-        for (int s = 0; s < 8; ++s)
-          umma_ts(tO(u), tS(u) + 8 * s, smem_desc_mn(vv + s * 2048, 16384), ID_O, (first && s == 0) ? 0u : 1u);
-        if (last_reader) umma_commit(bar(TB_EMPTY, vr.i));
+        for (int s = 1; s < 8; ++s) umma_ts(d, pp + 8 * s, vv + s * 128, ID_O, 1u);
+        if (last_reader) umma_commit(empty);
       }
       __syncwarp();
       if (last_reader) vr.next(p.slots, 2);
     };
     // stream u's last product is followed by one more commit: O[u] is complete
     auto finish = [&](int u) {
-      if (lane == 0) umma_commit(bar(TB_S, u));
+      const uint32_t done = uniform(bar(TB_S, u));
+      if (elect_one()) umma_commit(done);
       __syncwarp();
     };
     if (p.two_rows) {
