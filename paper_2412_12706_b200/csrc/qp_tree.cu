@@ -46,7 +46,7 @@ __host__ __device__ constexpr int tr_load(int bits) { return bits == 16 ? 4 : 8;
 __host__ __device__ constexpr int tr_threads(int bits) { return (TR_SOFT + tr_load(bits) + 1) * 32; }
 constexpr int TR_MAX_SLOTS = 6, TR_MAX_CLUSTER = 16, TR_MAX_SUBS = 16;
 
-enum : int { TB_FULL = 0, TB_EMPTY = TR_MAX_SLOTS, TB_S = 2 * TR_MAX_SLOTS, TB_P = TB_S + 2, TB_COUNT = TB_P + 2 };
+enum : int { TB_FULL = 0, TB_EMPTY = TR_MAX_SLOTS, TB_S = 2 * TR_MAX_SLOTS, TB_P = TB_S + 2, TB_Q = TB_P + 2, TB_COUNT = TB_Q + 1 };
 
 struct TreeLaunch {
   TreeArgs a;
@@ -56,6 +56,7 @@ struct TreeLaunch {
   int slots, raw;            // operand slots, raw stages (packed caches)
   int cluster, subs, max_subs;   // CTAs per cluster, clusters per (KV head, row group): more than one leave partial results
   int lg;                    // log2 of the quantization group
+  int inv_g;                 // ceil(2^16 / G): a row below 512 times this, shifted by 16, is the row's draft
   float* part;               // [KV head, row group][sub][256][D], then
   float2* part_ml;           // [KV head, row group][sub][256]
 };
@@ -290,6 +291,10 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
   const int row0 = rg * 256, rows = min(256, p.R - row0);       // of this group
   const int run = sub * C + rank, runs = p.subs * C;
   const int j0 = (int)((long long)p.tiles * run / runs), n_loc = (int)((long long)p.tiles * (run + 1) / runs) - j0;
+  // draft of row gr = t G + h of this KV head, and where its query or output row starts (t Hq + h = gr + t (Hq - G))
+  const size_t q0 = ((size_t)b * a.T * a.Hq + hk * G) * D;
+  auto draft_of = [&](int gr) { return (gr * p.inv_g) >> 16; };
+  auto row_off = [&](int gr) { return q0 + (size_t)(gr + draft_of(gr) * (a.Hq - G)) * D; };
   const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t sQ = sbase, ring = sbase + (p.two_rows ? 2 : 1) * SLOT;
   const uint32_t bar0 = smem_u32(&bars[0]);
@@ -305,6 +310,7 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
       mbar_init(bar(TB_S, u), 1);                               // a tcgen05.commit
       mbar_init(bar(TB_P, u), max(1, min(4, (rows - (p.two_rows ? u * 128 : 0) + 31) / 32)));    // the group's warps with rows
     }
+    mbar_init(bar(TB_Q, 0), TR_SOFT);                           // the softmax warps, which fetch the queries
     give_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
   }
@@ -312,29 +318,11 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(&tmem_base_slot)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
   }
-  chain_enter();
-  // query rows t G + h of this group, zeros behind the last; four loads in flight
-  for (int i0 = tid; i0 < (p.two_rows ? 256 : 128) * (D / 8); i0 += 4 * TR_THREADS) {
-    uint4 v[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int i = i0 + k * TR_THREADS, r = i / (D / 8), c = i % (D / 8), gr = row0 + r;
-      v[k] = make_uint4(0u, 0u, 0u, 0u);
-      if (r < rows)
-        v[k] = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + (((size_t)b * a.T + gr / G) * a.Hq + hk * G + gr % G) * D + c * 8));
-    }
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int i = i0 + k * TR_THREADS, r = i / (D / 8), c = i % (D / 8);
-      if (HALF) v[k] = make_uint4(bf2_to_half2(v[k].x), bf2_to_half2(v[k].y), bf2_to_half2(v[k].z), bf2_to_half2(v[k].w));
-      if (r < (p.two_rows ? 256 : 128)) sts128(sQ + (r >> 7) * SLOT + tile_off(r & 127, c), v[k]);
-    }
-  }
-  asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
   asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
   const uint32_t tmem = tmem_base_slot;
+  chain_enter();                                                // the launch's set-up overlaps the previous kernel's end
   auto tS = [&](int u) { return tmem + (uint32_t)u * 128u; };
   auto tO = [&](int u) { return tmem + 256u + (uint32_t)u * D; };
   // stream u's tiles: all of them, or every second one
@@ -344,11 +332,30 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
   const float scale_log2 = 1.4426950408889634f * rsqrtf((float)D);
 
   if (warp < TR_SOFT) {
-    // ---- softmax groups
+    // ---- softmax groups.  First the query rows t G + h of this group, zeros behind the last, eight loads in flight
+    for (int i0 = tid; i0 < (p.two_rows ? 256 : 128) * (D / 8); i0 += 8 * TR_SOFT * 32) {
+      uint4 v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int i = i0 + k * TR_SOFT * 32, r = i / (D / 8), c = i % (D / 8), gr = row0 + r;
+        v[k] = make_uint4(0u, 0u, 0u, 0u);
+        if (r < rows)
+          v[k] = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + row_off(gr) + c * 8));
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int i = i0 + k * TR_SOFT * 32, r = i / (D / 8), c = i % (D / 8);
+        if (HALF) v[k] = make_uint4(bf2_to_half2(v[k].x), bf2_to_half2(v[k].y), bf2_to_half2(v[k].z), bf2_to_half2(v[k].w));
+        if (r < (p.two_rows ? 256 : 128)) sts128(sQ + (r >> 7) * SLOT + tile_off(r & 127, c), v[k]);
+      }
+    }
+    asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar(TB_Q, 0));
     const int u = warp >> 2, rl = (warp & 3) * 32 + lane, r = (p.two_rows ? u * 128 : 0) + rl;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const bool work = (p.two_rows ? u * 128 : 0) + (warp & 3) * 32 < rows;      // warp-uniform: has rows
-    const unsigned long long mask = r < rows ? a.mask[(size_t)b * a.T + (row0 + r) / G] & (~0ull >> (64 - a.T)) : 0ull;
+    const unsigned long long mask = r < rows ? a.mask[(size_t)b * a.T + draft_of(row0 + r)] & (~0ull >> (64 - a.T)) : 0ull;
     // a warp without rows has nothing to do; a group without any sends its first warp to answer for it
     const int steps = work || (warp & 3) == 0 ? stream_tiles(u) : 0;
     bool ok = true;
@@ -505,6 +512,7 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
       if (elect_one()) umma_commit(done);
       __syncwarp();
     };
+    ok = mbar_wait_warp(bar(TB_Q, 0), 0u, gu);
     if (p.two_rows) {
       if (n_loc > 0) {
         wait_full(kr);
@@ -669,52 +677,97 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
   if (warp == TR_SOFT + TR_LOAD)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(512u) : "memory");
 
-  // ---- this CTA's slice of the rows.  Contribution c of a row is with CTA c / per, stream c % per (two row tiles: the row's)
-  const int per = p.two_rows ? 1 : 2, n_part = C * per;         // <= 32
+  // ---- this CTA's slice of the rows.  Contribution c of a row is with CTA c (two row tiles; the row's stream), or with CTA c / 2,
+  // stream c % 2
+  const int sh = p.two_rows ? 0 : 1, n_part = C << sh;          // <= 32
   const int r_lo = (int)((long long)rows * rank / C), n_rows = (int)((long long)rows * (rank + 1) / C) - r_lo;
   // their statistics, n_rows * n_part <= 256 + 32 pairs, behind this CTA's own
   float2* s_all = s_ml + 256;
   for (int i = tid; i < n_rows * n_part; i += TR_THREADS) {
     const int r = r_lo + i / n_part, c = i % n_part;
-    s_all[i] = cluster.map_shared_rank(s_ml, c / per)[(p.two_rows ? r >> 7 : c % per) * 128 + (r & 127)];
+    s_all[i] = cluster.map_shared_rank(s_ml, c >> sh)[(p.two_rows ? r >> 7 : c & 1) * 128 + (r & 127)];
   }
   __syncthreads();
-  for (int i = tid; i < n_rows * (D / 4); i += TR_THREADS) {    // a 16-byte chunk of a row's output
-    const int rr = i / (D / 4), ch = i % (D / 4), r = r_lo + rr, rl = r & 127;
-    const float2* ml = s_all + rr * n_part;
-    float M = -INFINITY, Z = 0.f;
-    for (int c = 0; c < n_part; ++c) M = fmaxf(M, ml[c].x);
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int c0 = 0; c0 < n_part; c0 += 8) {
-      float4 v[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int c = c0 + k;
-        v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (c < n_part && ml[c].x != -INFINITY)                 // (a stream without tiles left nothing behind)
-          v[k] = *reinterpret_cast<const float4*>(cluster.map_shared_rank(part_base, c / per) + (p.two_rows ? r >> 7 : c % per) * PART +
-                                                  part_off<D>(rl, ch));
-      }
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int c = c0 + k;
-        if (c >= n_part) break;
-        const float f = ml[c].x == -INFINITY ? 0.f : ex2a(ml[c].x - M);
-        Z = fmaf(ml[c].y, f, Z);
-        acc.x = fmaf(v[k].x, f, acc.x); acc.y = fmaf(v[k].y, f, acc.y);
-        acc.z = fmaf(v[k].z, f, acc.z); acc.w = fmaf(v[k].w, f, acc.w);
-      }
-    }
+  // a unit is a 16-byte chunk of a row's output; a remote read takes about a microsecond, so a thread has eight in flight: of
+  // four units from two CTAs each where it has several units, else of one unit from eight
+  auto emit = [&](int r, int ch, float M, float Z, float4 acc) {
     if (p.subs > 1) {                                           // for the merge: unnormalised, with its reference and sum
       const size_t row = ((size_t)item * p.subs + sub) * 256 + r;
       *reinterpret_cast<float4*>(p.part + row * D + 4 * ch) = acc;
       if (ch == 0) p.part_ml[row] = make_float2(M, Z);
     } else {
       const float inv = __fdiv_rn(1.0f, Z);
-      const int gr = row0 + r;
-      *reinterpret_cast<uint2*>(static_cast<bf16*>(a.out) + (((size_t)b * a.T + gr / G) * a.Hq + hk * G + gr % G) * D + 4 * ch) =
+      *reinterpret_cast<uint2*>(static_cast<bf16*>(a.out) + row_off(row0 + r) + 4 * ch) =
           make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
     }
+  };
+  auto fetch = [&](int r, int ch, int c, float2 ml) {
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (ml.x != -INFINITY)                                      // (a stream without tiles left nothing behind)
+      v = *reinterpret_cast<const float4*>(cluster.map_shared_rank(part_base, c >> sh) + (p.two_rows ? r >> 7 : c & 1) * PART +
+                                           part_off<D>(r & 127, ch));
+    return v;
+  };
+  auto fold_in = [&](float4& acc, float& Z, float M, float2 ml, float4 v) {
+    const float f = ml.x == -INFINITY ? 0.f : ex2a(ml.x - M);
+    Z = fmaf(ml.y, f, Z);
+    acc.x = fmaf(v.x, f, acc.x); acc.y = fmaf(v.y, f, acc.y);
+    acc.z = fmaf(v.z, f, acc.z); acc.w = fmaf(v.w, f, acc.w);
+  };
+  const int units = n_rows * (D / 4);
+  const float2 none = make_float2(-INFINITY, 0.f);
+  if (units > TR_THREADS) {
+    for (int i0 = tid; i0 < units; i0 += 4 * TR_THREADS) {
+      float4 acc[4];
+      float M[4], Z[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int i = i0 + k * TR_THREADS;
+        M[k] = -INFINITY;
+        Z[k] = 0.f;
+        acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (i < units)
+          for (int c = 0; c < n_part; ++c) M[k] = fmaxf(M[k], s_all[i / (D / 4) * n_part + c].x);
+      }
+      for (int c0 = 0; c0 < n_part; c0 += 2) {
+        float4 v[4][2];
+        float2 ml[4][2];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int i = i0 + k * TR_THREADS, rr = i / (D / 4);
+            ml[k][j] = i < units && c0 + j < n_part ? s_all[rr * n_part + c0 + j] : none;
+            v[k][j] = fetch(r_lo + rr, i % (D / 4), c0 + j, ml[k][j]);
+          }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) fold_in(acc[k], Z[k], M[k], ml[k][j], v[k][j]);
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int i = i0 + k * TR_THREADS;
+        if (i < units) emit(r_lo + i / (D / 4), i % (D / 4), M[k], Z[k], acc[k]);
+      }
+    }
+  } else if (tid < units) {
+    const int rr = tid / (D / 4), ch = tid % (D / 4), r = r_lo + rr;
+    float M = -INFINITY, Z = 0.f;
+    for (int c = 0; c < n_part; ++c) M = fmaxf(M, s_all[rr * n_part + c].x);
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int c0 = 0; c0 < n_part; c0 += 8) {
+      float4 v[8];
+      float2 ml[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        ml[k] = c0 + k < n_part ? s_all[rr * n_part + c0 + k] : none;
+        v[k] = fetch(r, ch, c0 + k, ml[k]);
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) fold_in(acc, Z, M, ml[k], v[k]);
+    }
+    emit(r, ch, M, Z, acc);
   }
   cluster.sync();                                               // nobody leaves while another may still read its shared memory
 }
@@ -860,6 +913,7 @@ cudaError_t launch_tree(const TreeArgs& a, void* ws, cudaStream_t st) {
   const TreeWorkspace w = tree_carve(a);
   p.part = reinterpret_cast<float*>(static_cast<char*>(ws) + w.part);
   p.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + w.part_ml);
+  p.inv_g = (65536 + a.Hq / a.Hkv - 1) / (a.Hq / a.Hkv);
   p.lg = a.group == 32 ? 5 : a.group == 64 ? 6 : 7;
   p.a = a;
   p.R = a.T * (a.Hq / a.Hkv);
