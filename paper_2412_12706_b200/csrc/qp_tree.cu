@@ -5,7 +5,7 @@
 // tcgen05, the codes are expanded to fp16 once per (KV head, tile) whatever R is, and all T drafts cost one pass over the cache.
 //
 // A block owns up to 256 rows of one KV head and walks over a run of 128-token tiles; its parts talk through mbarriers only:
-//   8 loader warps    tile j -> keys, then values, into a ring of 32 KB operand slots (128-byte swizzle).  Packed caches: words,
+//   loader warps      tile j -> keys, then values, into a ring of 32 KB operand slots (128-byte swizzle).  Packed caches: words,
 //                     scales and zero points by asynchronous copies into raw stages, several operands ahead, then to fp16 and
 //                     into the slot.  16-bit caches: TMA, with the token count as the tensor's extent, so rows behind the last
 //                     one arrive as zeros whatever the array holds there.  Tail and drafts form the last one or two tiles.
@@ -40,10 +40,13 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int TR_SOFT = 8;                                       // softmax warps
-// Loader warps: eight expand codes (96 registers a thread, with 17 warps); copying by TMA takes one, and with four of them (the
-// other three help with the last tile) every thread may have 128 registers.
-__host__ __device__ constexpr int tr_load(int bits) { return bits == 16 ? 4 : 8; }
-__host__ __device__ constexpr int tr_threads(int bits) { return (TR_SOFT + tr_load(bits) + 1) * 32; }
+// Loader warps: seven, so that with the MMA warp there are sixteen and every thread has 128 registers; with a seventeenth it is
+// 96 and the softmax spills (8 x 8192 tokens, 33 drafts: 78 -> 104 us).  Softmax warps that have no rows load, too.
+constexpr int TR_LOAD = 7;
+// Teams of loaders: one expands the keys, one the values, each at its own pace (an operand is a chain of waits and barriers that
+// one team after the other would walk).  At 8 bits there is no room for the raw stages of two.
+__host__ __device__ constexpr int tr_teams(int bits) { return bits == 8 ? 1 : 2; }
+constexpr int TR_THREADS = (TR_SOFT + TR_LOAD + 1) * 32;
 constexpr int TR_MAX_SLOTS = 6, TR_MAX_CLUSTER = 16, TR_MAX_SUBS = 16;
 
 enum : int { TB_FULL = 0, TB_EMPTY = TR_MAX_SLOTS, TB_S = 2 * TR_MAX_SLOTS, TB_P = TB_S + 2, TB_Q = TB_P + 2, TB_COUNT = TB_Q + 1 };
@@ -125,39 +128,32 @@ struct Raw {
 // copies of the operand's valid tokens (a multiple of 32, of the group if the groups run along the tokens); lg: log2 of the group
 template <int BITS, int D>
 __device__ __forceinline__ void raw_issue(const TreeArgs& a, int lg, bool cols, const void* codes, const __half* scale, const __half* zero,
-                                          int bh, int tok0, int lt, uint32_t raw) {
+                                          int bh, int tok0, int lt, int NT, uint32_t raw) {
   using R = Raw<BITS, D>;
-  constexpr int LB = BITS == 8 ? 3 : BITS == 4 ? 2 : 1, NT = tr_load(BITS) * 32;
+  constexpr int LB = BITS == 8 ? 3 : BITS == 4 ? 2 : 1;
   const int nt = min(128, a.n - tok0);
   const size_t row = (size_t)bh * a.ns + tok0;                  // first token row
-  const unsigned char* c = static_cast<const unsigned char*>(codes) + row * (D * BITS / 8) + lt * 16;
+  const unsigned char* c = static_cast<const unsigned char*>(codes) + row * (D * BITS / 8);
   const int chunks = nt * (D * BITS / 8) / 16, lline = lg + LB - 4;             // 16-byte chunks; log2 of those in a row of 8 channels
-#pragma unroll
-  for (int k = 0; k < 128 * (D * BITS / 8) / 16 / NT + (128 * (D * BITS / 8) / 16 % NT ? 1 : 0); ++k) {
-    const int i = lt + k * NT;
-    if (i < chunks) cp_async16(raw + i * 16 + (cols ? (i >> lline) * 16 : 0), c + k * NT * 16);
-  }
+#pragma unroll 2
+  for (int i = lt; i < chunks; i += NT) cp_async16(raw + i * 16 + (cols ? (i >> lline) * 16 : 0), c + i * 16);
   // scales and zero points: D/g a token row, or D a row of g tokens, either way row * D / g from the start
   const size_t m0 = (row * D >> lg) * 2;
   const int meta = (nt * D >> lg) * 2 / 16;
-#pragma unroll
-  for (int k = 0; k < (2 * R::META / 16 + NT - 1) / NT; ++k) {
-    const int i = lt + k * NT, o = i < meta ? i : i - meta;
-    if (i < 2 * meta)
-      cp_async16(raw + R::CODES + (i < meta ? 0 : R::META) + o * 16, reinterpret_cast<const unsigned char*>(i < meta ? scale : zero) + m0 + o * 16);
+  for (int i = lt; i < 2 * meta; i += NT) {
+    const int o = i < meta ? i : i - meta;
+    cp_async16(raw + R::CODES + (i < meta ? 0 : R::META) + o * 16, reinterpret_cast<const unsigned char*>(i < meta ? scale : zero) + m0 + o * 16);
   }
 }
 // Groups along the tokens (keys of the main path): an item is 8 channels x PT tokens, a word per channel.
 template <int BITS, int D>
-__device__ __forceinline__ void put_cols(const TreeArgs& a, int lg, int tok0, int lt, uint32_t raw, uint32_t slot) {
+__device__ __forceinline__ void put_cols(const TreeArgs& a, int lg, int tok0, int lt, int NT, uint32_t raw, uint32_t slot) {
   using R = Raw<BITS, D>;
-  constexpr int TR_LOADERS = tr_load(BITS) * 32;
   constexpr int PER = 32 / BITS, PT = PER < 8 ? PER : 8, OCT = D / 8, ITEMS = (128 / PT) * OCT;
   const int g = 1 << lg, wpg = g * BITS / 32;
-#pragma unroll
-  for (int k = 0; k < (ITEMS + TR_LOADERS - 1) / TR_LOADERS; ++k) {
-    const int i = lt + k * TR_LOADERS, oct = i % OCT, row = i / OCT * PT;
-    if (i >= ITEMS) continue;
+#pragma unroll 1
+  for (int i = lt; i < ITEMS; i += NT) {
+    const int oct = i % OCT, row = i / OCT * PT;
     if (tok0 + row >= a.n) {                                    // (n is a multiple of 32: an item is inside or outside)
 #pragma unroll
       for (int e = 0; e < PT; ++e) sts128(slot + tile_off(row + e, oct), make_uint4(0u, 0u, 0u, 0u));
@@ -191,13 +187,12 @@ __device__ __forceinline__ void put_cols(const TreeArgs& a, int lg, int tok0, in
 }
 // Groups along the channels (values; keys quantized token by token): an item is 16 channels of one token.
 template <int BITS, int D>
-__device__ __forceinline__ void put_rows(const TreeArgs& a, int lg, int tok0, int lt, uint32_t raw, uint32_t slot) {
+__device__ __forceinline__ void put_rows(const TreeArgs& a, int lg, int tok0, int lt, int NT, uint32_t raw, uint32_t slot) {
   using R = Raw<BITS, D>;
-  constexpr int TR_LOADERS = tr_load(BITS) * 32;
   constexpr int PIECES = D / 16, W = BITS / 2;                  // words of an item
-#pragma unroll
-  for (int k = 0; k < 128 * PIECES / TR_LOADERS; ++k) {
-    const int i = lt + k * TR_LOADERS, piece = i % PIECES, row = i / PIECES;
+#pragma unroll 1
+  for (int i = lt; i < 128 * PIECES; i += NT) {
+    const int piece = i % PIECES, row = i / PIECES;
     uint4 v[2] = {make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)};
     if (tok0 + row < a.n) {
       const uint32_t src = raw + (row * PIECES + piece) * (W * 4), m = raw + R::CODES + ((row * D + piece * 16) >> lg) * 2;
@@ -232,14 +227,14 @@ __device__ __forceinline__ void put_rows(const TreeArgs& a, int lg, int tok0, in
   }
 }
 // rows 128 x .. of the tail followed by the drafts, zeros behind them
-template <int D, bool HALF, int TR_LOADERS>
-__device__ __forceinline__ void put_extra(const TreeArgs& a, bool keys, int b, int hk, int bh, int x, int lt, uint32_t slot) {
+template <int D, bool HALF>
+__device__ __forceinline__ void put_extra(const TreeArgs& a, bool keys, int b, int hk, int bh, int x, int lt, int NT, uint32_t slot) {
   constexpr int PIECES = D / 16;
   const uint16_t* tail = static_cast<const uint16_t*>(keys ? a.k_tail : a.v_tail);
   const uint16_t* draft = static_cast<const uint16_t*>(keys ? a.k_draft : a.v_draft);
-#pragma unroll
-  for (int k = 0; k < 128 * PIECES / TR_LOADERS; ++k) {
-    const int i = lt + k * TR_LOADERS, piece = i % PIECES, row = i / PIECES, e = 128 * x + row;
+#pragma unroll 2
+  for (int i = lt; i < 128 * PIECES; i += NT) {
+    const int piece = i % PIECES, row = i / PIECES, e = 128 * x + row;
     uint4 v[2] = {make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)};
     if (e < a.n_tail + a.T) {
       const uint16_t* src = e < a.n_tail ? tail + ((size_t)bh * a.group + e) * D
@@ -267,11 +262,11 @@ template <int D>
 __device__ __forceinline__ uint32_t part_off(int r, int c) { return (uint32_t)(r * (D * 4) + ((c ^ (r & (D / 4 - 1))) << 4)); }
 
 template <int BITS, int D>
-__global__ void __launch_bounds__(tr_threads(BITS), 1)
+__global__ void __launch_bounds__(TR_THREADS, 1)
 tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
             int* __restrict__ error_words) {
   constexpr bool HALF = BITS < 16;
-  constexpr int TR_LOAD = tr_load(BITS), TR_THREADS = tr_threads(BITS);
+  constexpr int TEAMS = tr_teams(BITS);
   constexpr uint32_t SLOT = 128 * D * 2;
   constexpr uint32_t FMT = HALF ? 0u : (1u << 7) | (1u << 10);  // both operands fp16 / bf16
   constexpr uint32_t ID_S = (1u << 4) | FMT | ((128u >> 3) << 17) | ((128u >> 4) << 24);
@@ -301,14 +296,20 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
   auto bar = [&](int which, int i) { return bar0 + (uint32_t)(which + i) * 8u; };
   const volatile int* gu = &give_up;
 
+  // softmax warps at work: those with rows, and the first of each group; the others load.  Loaders are numbered from the
+  // dedicated ones on, so that loader 0 is always warp TR_SOFT.
+  auto warps_of = [&](int u) { return max(1, min(4, (rows - (p.two_rows ? u * 128 : 0) + 31) / 32)); };
+  const int w0 = warps_of(0), w1 = warps_of(1), n_load = TR_LOAD + 8 - w0 - w1;
+  const bool loads = warp < TR_SOFT ? (warp & 3) >= (warp < 4 ? w0 : w1) : warp < TR_SOFT + TR_LOAD;
+  const int lw = warp >= TR_SOFT ? warp - TR_SOFT : TR_LOAD + (warp < 4 ? warp - w0 : 4 - w0 + (warp - 4) - w1);
   if (tid == 0) {
     for (int i = 0; i < p.slots; ++i) {
-      mbar_init(bar(TB_FULL, i), TR_LOAD);                      // one arrival per loader warp
+      mbar_init(bar(TB_FULL, i), (n_load + TEAMS - 1) / TEAMS); // one arrival per warp of a team of loaders
       mbar_init(bar(TB_EMPTY, i), 1);                           // a tcgen05.commit
     }
     for (int u = 0; u < 2; ++u) {
       mbar_init(bar(TB_S, u), 1);                               // a tcgen05.commit
-      mbar_init(bar(TB_P, u), max(1, min(4, (rows - (p.two_rows ? u * 128 : 0) + 31) / 32)));    // the group's warps with rows
+      mbar_init(bar(TB_P, u), u ? w1 : w0);                     // the group's warps at work
     }
     mbar_init(bar(TB_Q, 0), TR_SOFT);                           // the softmax warps, which fetch the queries
     give_up = 0;
@@ -332,7 +333,7 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
   const float scale_log2 = 1.4426950408889634f * rsqrtf((float)D);
 
   if (warp < TR_SOFT) {
-    // ---- softmax groups.  First the query rows t G + h of this group, zeros behind the last, eight loads in flight
+    // the first eight warps fetch the query rows t G + h of this group, zeros behind the last, eight loads in flight
     for (int i0 = tid; i0 < (p.two_rows ? 256 : 128) * (D / 8); i0 += 8 * TR_SOFT * 32) {
       uint4 v[8];
 #pragma unroll
@@ -352,12 +353,15 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
     asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
     __syncwarp();
     if (lane == 0) mbar_arrive(bar(TB_Q, 0));
+  }
+
+  if (warp < TR_SOFT && !loads) {
+    // ---- softmax groups
     const int u = warp >> 2, rl = (warp & 3) * 32 + lane, r = (p.two_rows ? u * 128 : 0) + rl;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const bool work = (p.two_rows ? u * 128 : 0) + (warp & 3) * 32 < rows;      // warp-uniform: has rows
     const unsigned long long mask = r < rows ? a.mask[(size_t)b * a.T + draft_of(row0 + r)] & (~0ull >> (64 - a.T)) : 0ull;
-    // a warp without rows has nothing to do; a group without any sends its first warp to answer for it
-    const int steps = work || (warp & 3) == 0 ? stream_tiles(u) : 0;
+    const int steps = stream_tiles(u);                          // (a group without rows has its first warp here to answer for it)
     bool ok = true;
     for (int k = 0; k < steps; ++k) {
       const int j = j0 + (p.two_rows ? k : 2 * k + u);
@@ -416,11 +420,12 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
 #pragma unroll 1
             for (int c = 0; c < D; c += 16) {
               uint32_t o[16];
-              tmem_ld16(tO(u) + lanes + c, o);
+              tmem_ld16_issue(tO(u) + lanes + c, o);
+              tmem_wait16(o);
 #pragma unroll
               for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * corr);
               __syncwarp();
-              tmem_st16(tO(u) + lanes + c, o);
+              tmem_st(tO(u) + lanes + c, o);
             }
             tmem_wait_st();
           }
@@ -428,11 +433,12 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
         const float ref = m_run == -INFINITY ? 0.f : m_run;
         const uint64_t sc = pack2(scale_log2, scale_log2), nm = pack2(-ref, -ref);
         uint64_t sum2 = pack2(0.f, 0.f), sum3 = sum2;
-        // 32 columns: P over columns of S that have been read
-        auto fold = [&](const uint32_t (&x)[32], int c0) {
-          uint32_t pk[16];
+        // NC columns: P over columns of S that have been read
+        auto fold = [&](auto& x, int c0) {
+          constexpr int NC = sizeof(x) / 4;
+          uint32_t pk[NC / 2];
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
+          for (int i = 0; i < NC / 2; ++i) {
             float e0, e1;
             unpack2(fma2(pack2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), sc, nm), e0, e1);
             e0 = ex2a(e0);
@@ -441,21 +447,43 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
             pk[i] = HALF ? pack_half2(e0, e1) : pack_bf16x2(e0, e1);
           }
           __syncwarp();
-          tmem_st16(ts + c0 / 2, pk);
+          tmem_st(ts + c0 / 2, pk);
         };
-        tmem_ld32_issue(ts + 32, xa);
-        fold(xb, 0);
-        tmem_wait(xa);
-        if (!full) hide(xa, 32);
-        tmem_ld32_issue(ts + 64, xb);
-        fold(xa, 32);
-        tmem_wait(xb);
-        if (!full) hide(xb, 64);
-        tmem_ld32_issue(ts + 96, xa);
-        fold(xb, 64);
-        tmem_wait(xa);
-        if (!full) hide(xa, 96);
-        fold(xa, 96);
+        if constexpr (BITS == 16) {
+          tmem_ld32_issue(ts + 32, xa);
+          fold(xb, 0);
+          tmem_wait(xa);
+          if (!full) hide(xa, 32);
+          tmem_ld32_issue(ts + 64, xb);
+          fold(xa, 32);
+          tmem_wait(xb);
+          if (!full) hide(xb, 64);
+          tmem_ld32_issue(ts + 96, xa);
+          fold(xb, 64);
+          tmem_wait(xa);
+          if (!full) hide(xa, 96);
+          fold(xa, 96);
+        } else {                                                // 96 registers a thread: chunks of 16 columns
+          uint32_t ya[16], yb[16];
+          auto hide16 = [&](uint32_t (&x)[16], int c0) {
+            const uint32_t vis = visible(c0 & ~31) >> (c0 & 16);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = (vis >> i) & 1u ? x[i] : 0xff800000u;
+          };
+          tmem_ld16_issue(ts, ya);
+          tmem_wait16(ya);
+#pragma unroll
+          for (int c0 = 0; c0 < 128; c0 += 32) {
+            tmem_ld16_issue(ts + c0 + 16, yb);
+            if (!full) hide16(ya, c0);
+            fold(ya, c0);
+            tmem_wait16(yb);
+            if (c0 < 96) tmem_ld16_issue(ts + c0 + 32, ya);
+            if (!full) hide16(yb, c0 + 16);
+            fold(yb, c0 + 16);
+            if (c0 < 96) tmem_wait16(ya);
+          }
+        }
         sum2 = add2(sum2, sum3);
         float s0, s1;
         unpack2(sum2, s0, s1);
@@ -472,7 +500,7 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
       asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
     }
     if (!ok) give_up = 1;
-  } else if (warp == TR_SOFT + TR_LOAD) {
+  } else if (!loads) {
     // ---- MMA warp.  Operands in the ring: keys of tile 0, values of tile 0, keys of tile 1, ...
     bool ok = true;
     Ring kr, vr;                                                // the next keys and values
@@ -554,91 +582,86 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
     if (!ok) give_up = 1;
   } else {
     // ---- loader warps
-    const int lt = tid - TR_SOFT * 32;
-    bool ok = true, filled = false;                             // filled: the ring has been round once
-    Ring wr;                                                    // the next operand's slot
-    auto wait_empty = [&]() {
-      if (filled) ok = ok && mbar_wait_warp(bar(TB_EMPTY, wr.i), wr.round ^ 1u, gu);
+    const int team = lw % TEAMS, t_size = (n_load - team + TEAMS - 1) / TEAMS, NT = t_size * 32, lt = lw / TEAMS * 32 + lane;
+    const bool first = lw / TEAMS == 0;                         // the team's first warp also arrives for those that a smaller team lacks
+    const uint32_t arrivals = first ? 1 + (n_load + TEAMS - 1) / TEAMS - t_size : 1;
+    // operand i: keys (even) or values (odd) of this block's tile i / 2; this team's are team, team + TEAMS, ...
+    bool ok = true;
+    Ring wr;                                                    // the team's next operand's slot
+    if (team) wr.next(p.slots);
+    auto wait_empty = [&](int i) {
+      if (i >= p.slots) ok = ok && mbar_wait_warp(bar(TB_EMPTY, wr.i), wr.round ^ 1u, gu);
     };
     auto slot = [&]() { return ring + wr.i * SLOT; };
-    auto advance = [&]() {
-      wr.next(p.slots);
-      filled = filled || wr.i == 0;
-    };
     auto publish = [&]() {                                      // this warp's part of an operand is in place
       asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar(TB_FULL, wr.i));
-      advance();
+      if (lane == 0) mbar_arrive_n(bar(TB_FULL, wr.i), arrivals);
+      wr.next(p.slots, TEAMS);
     };
     const int n_ctx = max(0, min(n_loc, p.ctx_tiles - j0));     // this block's context tiles
+    int i = team;
     if constexpr (BITS == 16) {
-      int issued = 0;
-      for (int i = 0; i < 2 * n_ctx; ++i) {
-        wait_empty();
+      // one lane of the team copies; the others follow the ring, whose parity they could not tell after two rounds
+      Ring back = wr;                                           // the oldest copy that may still be on its way
+      int flying = 0;
+      for (; i < 2 * n_ctx; i += TEAMS) {
+        wait_empty(i);
         if (!ok) break;
-        if (lane == 0) {
-          if (warp == TR_SOFT) {
-            mbar_expect_tx(bar(TB_FULL, wr.i), SLOT);
+        if (first && lane == 0) {
+          mbar_expect_tx(bar(TB_FULL, wr.i), SLOT);
 #pragma unroll
-            for (int kb = 0; kb < D / 64; ++kb)
-              tma_load_3d(slot() + kb * 16384, i & 1 ? &map_v : &map_k, kb * 64, 128 * (j0 + i / 2), bh, bar(TB_FULL, wr.i));
-          } else {
-            mbar_arrive(bar(TB_FULL, wr.i));
-          }
+          for (int kb = 0; kb < D / 64; ++kb)
+            tma_load_3d(slot() + kb * 16384, team ? &map_v : &map_k, kb * 64, 128 * (j0 + i / 2), bh, bar(TB_FULL, wr.i));
+          mbar_arrive_n(bar(TB_FULL, wr.i), (n_load + TEAMS - 1) / TEAMS - 1);
         }
-        issued = i + 1;
         __syncwarp();
-        advance();
+        wr.next(p.slots, TEAMS);
+        if (flying == p.slots) back.next(p.slots, TEAMS); else ++flying;
       }
-      if (!ok && warp == TR_SOFT) {
+      if (!ok && first)
         // the copies still on their way land in this block's shared memory: wait (bounded) for them before it is given up
-        for (int i = max(0, issued - p.slots); i < issued; ++i)
+        for (; flying > 0; --flying, back.next(p.slots, TEAMS))
           for (uint32_t s = 0; s < TC_SPIN_LIMIT; ++s)
-            if (mbar_try_wait(bar(TB_FULL, i % p.slots), (uint32_t)((i / p.slots) & 1))) break;
-      }
+            if (mbar_try_wait(bar(TB_FULL, back.i), back.round)) break;
     } else {
-      // operand i: keys (even) or values (odd) of context tile i / 2, through the raw stages in turn
       const bool cols = a.k_axis == 0;
-      const uint32_t raw0 = ring + p.slots * SLOT, raw_end = raw0 + p.raw * Raw<BITS, D>::BYTES;
+      const int stages = p.raw / TEAMS;
+      const uint32_t raw0 = ring + p.slots * SLOT + team * stages * Raw<BITS, D>::BYTES, raw_end = raw0 + stages * Raw<BITS, D>::BYTES;
       uint32_t raw_in = raw0, raw_out = raw0;
-      auto issue = [&](int i) {
-        const int tok0 = 128 * (j0 + i / 2);
-        if (i & 1) raw_issue<BITS, D>(a, p.lg, false, a.vc, a.vs, a.vz, bh, tok0, lt, raw_in);
-        else raw_issue<BITS, D>(a, p.lg, cols, a.kc, a.ks, a.kz, bh, tok0, lt, raw_in);
-      };
-      auto turn = [&](uint32_t& raw) {
-        raw += Raw<BITS, D>::BYTES;
-        if (raw == raw_end) raw = raw0;
-      };
-      for (int i = 0; i < p.raw - 1; ++i) {
-        if (i < 2 * n_ctx) issue(i);
-        turn(raw_in);
+      auto issue = [&](int op) {
+        if (op < 2 * n_ctx) {
+          const int tok0 = 128 * (j0 + op / 2);
+          if (op & 1) raw_issue<BITS, D>(a, p.lg, false, a.vc, a.vs, a.vz, bh, tok0, lt, NT, raw_in);
+          else raw_issue<BITS, D>(a, p.lg, cols, a.kc, a.ks, a.kz, bh, tok0, lt, NT, raw_in);
+        }
         cp_async_commit();
-      }
-      for (int i = 0; i < 2 * n_ctx; ++i) {
-        if (p.raw == 3) cp_async_wait<1>(); else cp_async_wait<2>();            // operand i has landed (this thread's part)
-        asm volatile("bar.sync 1, %0;\n" ::"n"(TR_LOAD * 32) : "memory");      // ... everybody's; and operand i - 1 is used up
-        if (i + p.raw - 1 < 2 * n_ctx) issue(i + p.raw - 1);
-        turn(raw_in);
-        cp_async_commit();
-        wait_empty();
-        if (!ok) continue;                                      // (keeps the loaders' barrier together)
-        const int tok0 = 128 * (j0 + i / 2);
-        if (cols && !(i & 1)) put_cols<BITS, D>(a, p.lg, tok0, lt, raw_out, slot());
-        else put_rows<BITS, D>(a, p.lg, tok0, lt, raw_out, slot());
-        turn(raw_out);
-        publish();
+        raw_in += Raw<BITS, D>::BYTES;
+        if (raw_in == raw_end) raw_in = raw0;
+      };
+      for (int k = 0; k < stages - 1; ++k) issue(team + k * TEAMS);
+      for (; i < 2 * n_ctx; i += TEAMS) {
+        if (stages == 2) cp_async_wait<0>(); else if (stages == 3) cp_async_wait<1>(); else cp_async_wait<2>();   // this thread's part
+        asm volatile("bar.sync %0, %1;\n" ::"r"(1 + team), "r"(NT) : "memory");     // the team's; and the stage before is used up
+        issue(i + (stages - 1) * TEAMS);
+        wait_empty(i);
+        if (ok) {                                               // (otherwise keep the team's barrier together)
+          const int tok0 = 128 * (j0 + i / 2);
+          if (cols && !(i & 1)) put_cols<BITS, D>(a, p.lg, tok0, lt, NT, raw_out, slot());
+          else put_rows<BITS, D>(a, p.lg, tok0, lt, NT, raw_out, slot());
+          publish();
+        }
+        raw_out += Raw<BITS, D>::BYTES;
+        if (raw_out == raw_end) raw_out = raw0;
       }
       cp_async_wait<0>();
     }
-    for (int j = n_ctx; j < n_loc && ok; ++j)
-      for (int kv = 0; kv < 2 && ok; ++kv) {
-        wait_empty();
-        if (!ok) break;
-        put_extra<D, HALF, TR_LOAD * 32>(a, kv == 0, b, hk, bh, j0 + j - p.ctx_tiles, lt, slot());
-        publish();
-      }
+    for (; i < 2 * n_loc && ok; i += TEAMS) {
+      wait_empty(i);
+      if (!ok) break;
+      put_extra<D, HALF>(a, !(i & 1), b, hk, bh, j0 + i / 2 - p.ctx_tiles, lt, NT, slot());
+      publish();
+    }
     if (!ok) give_up = 1;
   }
 
@@ -849,7 +872,7 @@ cudaError_t launch_tree_t(TreeLaunch p, const CUtensorMap& mk, const CUtensorMap
   e = allow_smem(kernel, smem_max, done);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.blockDim = dim3(tr_threads(BITS));
+  cfg.blockDim = dim3(TR_THREADS);
   cfg.dynamicSmemBytes = smem_max;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
@@ -876,7 +899,7 @@ cudaError_t launch_tree_t(TreeLaunch p, const CUtensorMap& mk, const CUtensorMap
     p.slots = p.two_rows ? 5 : 6;
   } else {                                                      // the least the order of the products needs; raw stages from the rest
     p.slots = p.two_rows ? 3 : 4;
-    p.raw = (2 * SLOT) / Raw<BITS == 16 ? 8 : BITS, D>::BYTES >= 4 ? 4 : 3;
+    p.raw = std::min(8, (int)(2 * SLOT / Raw<BITS == 16 ? 8 : BITS, D>::BYTES)) / tr_teams(BITS) * tr_teams(BITS);   // 3, 4 or 8
   }
   // CTAs per cluster and clusters per (KV head, row group): the shortest schedule, rounds of (tiles + about three tiles of set-up
   // and exchange), the merge of several clusters about another one and a half.  Large clusters need no merge, but leave SMs idle
