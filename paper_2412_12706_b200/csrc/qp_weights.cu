@@ -10,11 +10,20 @@ namespace {
 __global__ void __launch_bounds__(256)
 kept_state_kernel(const float* __restrict__ weights, const int32_t* __restrict__ kept, int L, int n, int cap,
                   float* __restrict__ kw, int32_t* __restrict__ kp) {
-  const int bh = blockIdx.y, i = blockIdx.x * 256 + threadIdx.x;
-  if (i >= cap) return;
-  const int src = i < n ? kept[(size_t)bh * n + i] : 0;
-  if (kw) kw[(size_t)bh * cap + i] = i < n ? weights[(size_t)bh * L + src] : 0.f;
-  if (kp) kp[(size_t)bh * cap + i] = src;
+  chain_enter();
+  const int bh = blockIdx.y, i0 = blockIdx.x * 1024 + threadIdx.x;
+  int src[4];
+  float v[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) src[k] = i0 + 256 * k < n ? kept[(size_t)bh * n + i0 + 256 * k] : 0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = kw && i0 + 256 * k < n ? weights[(size_t)bh * L + src[k]] : 0.f;
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (i0 + 256 * k < cap) {
+      if (kw) kw[(size_t)bh * cap + i0 + 256 * k] = v[k];
+      if (kp) kp[(size_t)bh * cap + i0 + 256 * k] = src[k];
+    }
 }
 
 // monotone map float -> uint32 (larger float = larger integer); -0 as +0
@@ -23,78 +32,127 @@ __device__ __forceinline__ uint32_t order_image(float f) {
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-__device__ __forceinline__ void quantize_row_group(const uint16_t* x, int g, int bits, uint32_t* words, __half* scale, __half* zero) {
-  const int qmax = (1 << bits) - 1, per = 32 / bits;
-  float mn = INFINITY, mx = -INFINITY;
-  for (int e = 0; e < g; ++e) {
-    const float v = bf16_bits_to_f32(x[e]);
-    mn = fminf(mn, v);
-    mx = fmaxf(mx, v);
-  }
-  const __half z16 = __float2half_rd(mn);
-  const float z = __half2float(z16);
-  const __half s16 = __float2half_ru(__fmul_rn(__fsub_rn(mx, z), 1.0f / (float)qmax));   // product with the rounded reciprocal
-  const float s = __half2float(s16);
-  for (int w = 0; w < g / per; ++w) {
-    uint32_t word = 0;
-    for (int i = 0; i < per; ++i) {
-      const float c = s > 0.f ? rintf(__fdiv_rn(__fsub_rn(bf16_bits_to_f32(x[w * per + i]), z), s)) : 0.f;
-      word |= (uint32_t)fminf(fmaxf(c, 0.f), (float)qmax) << (i * bits);
-    }
-    words[w] = word;
-  }
-  *scale = s16;
-  *zero = z16;
+// One block per (batch, KV head).  The call is a chain of latencies (a few hundred KB in all): the row is fetched and quantized
+// while the search's loads are on their way, every thread has EV_PER weights and positions in flight, and the two minima the
+// rule may need (lightest of the old, oldest of all) are taken together as 64-bit keys (order image, slot), which makes equal
+// values go to the lower slot.
+constexpr int EV_THREADS = 1024, EV_PER = 8;
+
+// code of one element, RN((x - z) / s) clamped
+__device__ __forceinline__ uint32_t code_of(float x, float z, float s, int qmax) {
+  const float c = s > 0.f ? rintf(__fdiv_rn(__fsub_rn(x, z), s)) : 0.f;
+  return (uint32_t)fminf(fmaxf(c, 0.f), (float)qmax);
 }
 
-// one block per (batch, KV head): the slot, then the row
-__global__ void __launch_bounds__(256)
-evict_kernel(const EvictArgs a) {
-  __shared__ unsigned long long s_light[8], s_old[8];
-  const int bh = blockIdx.x, tid = threadIdx.x;
+__global__ void __launch_bounds__(EV_THREADS)
+evict_kernel(const __grid_constant__ EvictArgs a) {
+  __shared__ unsigned long long s_light[EV_THREADS / 32], s_old[EV_THREADS / 32];
+  __shared__ int s_slot;
+  const int bh = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int D = a.D, g = a.g, ngv = D / g;
+  chain_enter();
   float* w = a.weights + (size_t)bh * a.ns;
   int32_t* pos = a.pos + (size_t)bh * a.ns;
+
+  // the row: packed caches, a warp per group (keys, then values), up to four elements a lane; 16 bit, 16-byte pieces
+  const bool quant = a.bits < 16 && warp < 2 * ngv, key = warp < ngv;
+  const int grp = key ? warp : warp - ngv, per_lane = g / 32;
+  const uint16_t* src = (key ? a.k_new : a.v_new) + (size_t)bh * D + grp * g;
+  float x[4];
+  uint4 piece;
+  if (quant) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = k < per_lane ? bf16_bits_to_f32(src[lane * per_lane + k]) : 0.f;
+  } else if (a.bits == 16 && tid < D / 4) {
+    piece = *reinterpret_cast<const uint4*>((tid < D / 8 ? a.k_new : a.v_new) + (size_t)bh * D + (tid % (D / 8)) * 8);
+  }
+
   int slot = a.slot;
-  if (slot < 0) {
-    unsigned long long light = ~0ull, oldest = ~0ull;
-    for (int t = tid; t < a.n; t += 256) {
-      const int p = pos[t];
-      const unsigned long long o = ((unsigned long long)((uint32_t)p ^ 0x80000000u) << 32) | (unsigned)t;
-      oldest = o < oldest ? o : oldest;
-      if ((long long)p <= a.limit) {
-        const unsigned long long k = ((unsigned long long)order_image(w[t]) << 32) | (unsigned)t;
-        light = k < light ? k : light;
+  unsigned long long light = ~0ull, oldest = ~0ull;
+  if (slot < 0)
+    for (int t0 = tid; t0 < a.n; t0 += EV_PER * EV_THREADS) {
+      int32_t p[EV_PER];
+      float v[EV_PER];
+#pragma unroll
+      for (int k = 0; k < EV_PER; ++k) {
+        const int t = min(t0 + k * EV_THREADS, a.n - 1);        // past the end: the last one again
+        p[k] = pos[t];
+        v[k] = w[t];
+      }
+#pragma unroll
+      for (int k = 0; k < EV_PER; ++k) {
+        const unsigned t = (unsigned)min(t0 + k * EV_THREADS, a.n - 1);
+        const unsigned long long o = ((unsigned long long)((uint32_t)p[k] ^ 0x80000000u) << 32) | t;
+        const unsigned long long l = (long long)p[k] <= a.limit ? ((unsigned long long)order_image(v[k]) << 32) | t : ~0ull;
+        oldest = o < oldest ? o : oldest;
+        light = l < light ? l : light;
       }
     }
+
+  // quantization of this warp's group (its loads came first)
+  uint32_t word = 0;
+  __half s16, z16;
+  if (quant) {
+    const int qmax = (1 << a.bits) - 1, bits = a.bits;
+    float mn = x[0], mx = x[0];
+#pragma unroll
+    for (int k = 1; k < 4; ++k)
+      if (k < per_lane) { mn = fminf(mn, x[k]); mx = fmaxf(mx, x[k]); }
+#pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
-      const unsigned long long x = __shfl_xor_sync(0xffffffffu, light, o), y = __shfl_xor_sync(0xffffffffu, oldest, o);
-      light = x < light ? x : light;
+      mn = fminf(mn, __shfl_xor_sync(0xffffffffu, mn, o));
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    }
+    z16 = __float2half_rd(mn);
+    const float z = __half2float(z16);
+    s16 = __float2half_ru(__fmul_rn(__fsub_rn(mx, z), 1.0f / (float)qmax));      // product with the rounded reciprocal
+    const float s = __half2float(s16);
+    // this lane's elements fill per_lane * bits bits of a word; the lanes of a word put theirs together
+    const int lanes = 32 / (per_lane * bits), sub = lanes > 1 ? lane % lanes : 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (k < per_lane) word |= code_of(x[k], z, s, qmax) << (((sub * per_lane + k) * bits) & 31);
+    for (int o = 1; o < lanes; o <<= 1) word |= __shfl_xor_sync(0xffffffffu, word, o);
+  }
+
+  if (slot < 0) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      const unsigned long long l = __shfl_xor_sync(0xffffffffu, light, o), y = __shfl_xor_sync(0xffffffffu, oldest, o);
+      light = l < light ? l : light;
       oldest = y < oldest ? y : oldest;
     }
-    if ((tid & 31) == 0) { s_light[tid >> 5] = light; s_old[tid >> 5] = oldest; }
+    if (lane == 0) { s_light[warp] = light; s_old[warp] = oldest; }
     __syncthreads();
-    light = s_light[0]; oldest = s_old[0];
-    for (int i = 1; i < 8; ++i) {
-      light = s_light[i] < light ? s_light[i] : light;
-      oldest = s_old[i] < oldest ? s_old[i] : oldest;
+    if (warp == 0) {
+      light = s_light[lane];
+      oldest = s_old[lane];
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) {
+        const unsigned long long l = __shfl_xor_sync(0xffffffffu, light, o), y = __shfl_xor_sync(0xffffffffu, oldest, o);
+        light = l < light ? l : light;
+        oldest = y < oldest ? y : oldest;
+      }
+      if (lane == 0) s_slot = (int)(uint32_t)(light != ~0ull ? light : oldest);
     }
-    slot = (int)(uint32_t)(light != ~0ull ? light : oldest);
+    __syncthreads();
+    slot = s_slot;
   }
-  const int D = a.D, g = a.g;
+
   const size_t row = (size_t)bh * a.ns + slot;
-  const uint16_t *k = a.k_new + (size_t)bh * D, *v = a.v_new + (size_t)bh * D;
-  if (a.bits == 16) {
-    for (int d = tid; d < D; d += 256) {
-      static_cast<uint16_t*>(a.kc)[row * D + d] = k[d];
-      static_cast<uint16_t*>(a.vc)[row * D + d] = v[d];
+  if (quant) {
+    const size_t gi = row * ngv + grp;
+    const int lanes = 32 / (per_lane * a.bits);
+    uint32_t* words = static_cast<uint32_t*>(key ? a.kc : a.vc) + gi * (g * a.bits / 32);
+    if (lane % lanes == 0) words[lane / lanes] = word;
+    if (lane == 0) {
+      (key ? a.ks : a.vs)[gi] = s16;
+      (key ? a.kz : a.vz)[gi] = z16;
     }
-  } else if (tid < 2 * (D / g)) {
-    const int grp = tid >> 1, wpg = g * a.bits / 32;
-    const size_t gi = row * (D / g) + grp;
-    if (tid & 1) quantize_row_group(v + grp * g, g, a.bits, static_cast<uint32_t*>(a.vc) + gi * wpg, a.vs + gi, a.vz + gi);
-    else quantize_row_group(k + grp * g, g, a.bits, static_cast<uint32_t*>(a.kc) + gi * wpg, a.ks + gi, a.kz + gi);
+  } else if (a.bits == 16 && tid < D / 4) {
+    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(tid < D / 8 ? a.kc : a.vc) + row * D + (tid % (D / 8)) * 8) = piece;
   }
-  if (tid == 0) {
+  if (tid == EV_THREADS - 1) {
     w[slot] = 0.f;
     pos[slot] = a.new_pos;
     if (a.slots) a.slots[bh] = slot;
@@ -105,13 +163,11 @@ evict_kernel(const EvictArgs a) {
 
 cudaError_t launch_kept_state(const float* weights, const int32_t* kept, int BH, int L, int n, int cap, float* kw, int32_t* kp,
                               cudaStream_t st) {
-  kept_state_kernel<<<dim3((cap + 255) / 256, BH), 256, 0, st>>>(weights, kept, L, n, cap, kw, kp);
-  return cudaGetLastError();
+  return launch_chained(kept_state_kernel, dim3((cap + 1023) / 1024, BH), dim3(256), 0, st, weights, kept, L, n, cap, kw, kp);
 }
 
 cudaError_t launch_evict(const EvictArgs& a, int BH, cudaStream_t st) {
-  evict_kernel<<<BH, 256, 0, st>>>(a);
-  return cudaGetLastError();
+  return launch_chained(evict_kernel, dim3(BH), dim3(EV_THREADS), 0, st, a);
 }
 
 }  // namespace qp

@@ -689,15 +689,18 @@ def evict_kv(k_new: torch.Tensor, v_new: torch.Tensor, cache: Cache, weights: to
     """qp_evict_kv: the new token's rows [Bt,Hkv,D] take the slot of the lightest token that is not among the ``recent`` last
     positions (a 16-bit cache with room grows first); returns the slots int32 [Bt,Hkv].  cache, weights and pos are updated."""
     d = cache.desc
-    row = (d.batch, d.n_kv_heads, d.head_dim)
+    Bt, Hkv = d.batch, d.n_kv_heads
+    row, state = (Bt, Hkv, d.head_dim), (Bt, Hkv, d.n_cap or d.n_keep)
     _dev(k_new, torch.bfloat16, row); _dev(v_new, torch.bfloat16, row)
-    _dev(weights, torch.float32, _state_shape(cache)); _dev(pos, torch.int32, _state_shape(cache))
+    _dev(weights, torch.float32, state); _dev(pos, torch.int32, state)
     if slots is None:
-        slots = pos.new_empty(row[:2])
+        slots = pos.new_empty((Bt, Hkv))
     else:
-        _dev(slots, torch.int32, row[:2])
-    _check(lib().qp_evict_kv(_ptr(k_new), _ptr(v_new), ctypes.byref(d), _ref(strategy), _ptr(weights), _ptr(pos), new_pos, recent,
-                             _ptr(slots), _stream()), "qp_evict_kv")
+        _dev(slots, torch.int32, (Bt, Hkv))
+    status = lib().qp_evict_kv(k_new.data_ptr(), v_new.data_ptr(), ctypes.byref(d), _ref(strategy), weights.data_ptr(),
+                               pos.data_ptr(), new_pos, recent, slots.data_ptr(), _stream())
+    if status:
+        _check(status, "qp_evict_kv")
     return slots
 
 
