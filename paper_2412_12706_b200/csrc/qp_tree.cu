@@ -381,34 +381,35 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
           return v;
         };
         const bool full = j < p.ctx_tiles && 128 * (j + 1) <= a.n;
-        uint32_t xa[32], xb[32];
-        auto hide = [&](uint32_t (&x)[32], int c0) {            // what the row does not see
-          const uint32_t vis = visible(c0);
+        if (!full) {                                            // what the row does not see leaves S
+#pragma unroll 1
+          for (int c0 = 0; c0 < 128; c0 += 16) {
+            const uint32_t vis = visible(c0 & ~31) >> (c0 & 16);
+            uint32_t x[16];
+            tmem_ld16_issue(ts + c0, x);
+            tmem_wait16(x);
 #pragma unroll
-          for (int i = 0; i < 32; ++i) x[i] = (vis >> i) & 1u ? x[i] : 0xff800000u;
-        };
-        // the tile's maximum, columns 0..31 last: they stay in registers for the second pass
-        float mx0 = -INFINITY, mx1 = -INFINITY;
-        auto top = [&](uint32_t (&x)[32], int c0) {
-          if (!full) hide(x, c0);
-#pragma unroll
-          for (int i = 0; i < 32; i += 4) {
-            mx0 = max3(mx0, __uint_as_float(x[i]), __uint_as_float(x[i + 1]));
-            mx1 = max3(mx1, __uint_as_float(x[i + 2]), __uint_as_float(x[i + 3]));
+            for (int i = 0; i < 16; ++i) x[i] = (vis >> i) & 1u ? x[i] : 0xff800000u;
+            __syncwarp();
+            tmem_st(ts + c0, x);
           }
-        };
-        tmem_ld32_issue(ts + 96, xa);
-        tmem_wait(xa);
-        tmem_ld32_issue(ts + 64, xb);
-        top(xa, 96);
-        tmem_wait(xb);
-        tmem_ld32_issue(ts + 32, xa);
-        top(xb, 64);
-        tmem_wait(xa);
-        tmem_ld32_issue(ts, xb);
-        top(xa, 32);
-        tmem_wait(xb);
-        top(xb, 0);
+          tmem_wait_st();
+        }
+        // (loops, not unrolled: the kernel waits for instructions otherwise; the loaders' unrolled by two cost 20 %)
+        uint32_t xa[32], xb[32];
+        float mx0 = -INFINITY, mx1 = -INFINITY;
+#pragma unroll 1
+        for (int c0 = 0; c0 < 128; c0 += 64) {
+          tmem_ld32_issue(ts + c0, xa);
+          tmem_ld32_issue(ts + c0 + 32, xb);
+          tmem_wait(xa);
+          tmem_wait(xb);
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) {
+            mx0 = max3(mx0, __uint_as_float(xa[i]), __uint_as_float(xa[i + 1]));
+            mx1 = max3(mx1, __uint_as_float(xb[i]), __uint_as_float(xb[i + 1]));
+          }
+        }
         const float mx = fmaxf(mx0, mx1) * scale_log2;          // scale > 0; -inf stays
         // a new reference only where the old one is exceeded by more than 2^8 (or there is none yet)
         const bool renew = mx > m_run + 8.f;
@@ -433,12 +434,11 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
         const float ref = m_run == -INFINITY ? 0.f : m_run;
         const uint64_t sc = pack2(scale_log2, scale_log2), nm = pack2(-ref, -ref);
         uint64_t sum2 = pack2(0.f, 0.f), sum3 = sum2;
-        // NC columns: P over columns of S that have been read
-        auto fold = [&](auto& x, int c0) {
-          constexpr int NC = sizeof(x) / 4;
-          uint32_t pk[NC / 2];
+        // 32 columns: P over columns of S that have been read
+        auto fold = [&](const uint32_t (&x)[32], int c0) {
+          uint32_t pk[16];
 #pragma unroll
-          for (int i = 0; i < NC / 2; ++i) {
+          for (int i = 0; i < 16; ++i) {
             float e0, e1;
             unpack2(fma2(pack2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), sc, nm), e0, e1);
             e0 = ex2a(e0);
@@ -449,40 +449,15 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
           __syncwarp();
           tmem_st(ts + c0 / 2, pk);
         };
-        if constexpr (BITS == 16) {
-          tmem_ld32_issue(ts + 32, xa);
-          fold(xb, 0);
+        tmem_ld32_issue(ts, xa);
+#pragma unroll 1
+        for (int c0 = 0; c0 < 128; c0 += 64) {
           tmem_wait(xa);
-          if (!full) hide(xa, 32);
-          tmem_ld32_issue(ts + 64, xb);
-          fold(xa, 32);
+          tmem_ld32_issue(ts + c0 + 32, xb);
+          fold(xa, c0);
           tmem_wait(xb);
-          if (!full) hide(xb, 64);
-          tmem_ld32_issue(ts + 96, xa);
-          fold(xb, 64);
-          tmem_wait(xa);
-          if (!full) hide(xa, 96);
-          fold(xa, 96);
-        } else {                                                // 96 registers a thread: chunks of 16 columns
-          uint32_t ya[16], yb[16];
-          auto hide16 = [&](uint32_t (&x)[16], int c0) {
-            const uint32_t vis = visible(c0 & ~31) >> (c0 & 16);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = (vis >> i) & 1u ? x[i] : 0xff800000u;
-          };
-          tmem_ld16_issue(ts, ya);
-          tmem_wait16(ya);
-#pragma unroll
-          for (int c0 = 0; c0 < 128; c0 += 32) {
-            tmem_ld16_issue(ts + c0 + 16, yb);
-            if (!full) hide16(ya, c0);
-            fold(ya, c0);
-            tmem_wait16(yb);
-            if (c0 < 96) tmem_ld16_issue(ts + c0 + 32, ya);
-            if (!full) hide16(yb, c0 + 16);
-            fold(yb, c0 + 16);
-            if (c0 < 96) tmem_wait16(ya);
-          }
+          if (c0 == 0) tmem_ld32_issue(ts + 64, xa);
+          fold(xb, c0 + 32);
         }
         sum2 = add2(sum2, sum3);
         float s0, s1;
@@ -712,7 +687,7 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
   }
   __syncthreads();
   // a unit is a 16-byte chunk of a row's output; a remote read takes about a microsecond, so a thread has eight in flight: of
-  // four units from two CTAs each where it has several units, else of one unit from eight
+  // four units from two CTAs each where it has several units, sixteen of one unit else
   auto emit = [&](int r, int ch, float M, float Z, float4 acc) {
     if (p.subs > 1) {                                           // for the merge: unnormalised, with its reference and sum
       const size_t row = ((size_t)item * p.subs + sub) * 256 + r;
@@ -779,16 +754,16 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
     float M = -INFINITY, Z = 0.f;
     for (int c = 0; c < n_part; ++c) M = fmaxf(M, s_all[rr * n_part + c].x);
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int c0 = 0; c0 < n_part; c0 += 8) {
-      float4 v[8];
-      float2 ml[8];
+    for (int c0 = 0; c0 < n_part; c0 += 16) {
+      float4 v[16];
+      float2 ml[16];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
+      for (int k = 0; k < 16; ++k) {
         ml[k] = c0 + k < n_part ? s_all[rr * n_part + c0 + k] : none;
         v[k] = fetch(r, ch, c0 + k, ml[k]);
       }
 #pragma unroll
-      for (int k = 0; k < 8; ++k) fold_in(acc, Z, M, ml[k], v[k]);
+      for (int k = 0; k < 16; ++k) fold_in(acc, Z, M, ml[k], v[k]);
     }
     emit(r, ch, M, Z, acc);
   }
