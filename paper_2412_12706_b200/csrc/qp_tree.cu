@@ -125,26 +125,34 @@ struct Raw {
   static constexpr int META = 128 * (D / 32) * 2;                               // of scales, or of zero points
   static constexpr int BYTES = CODES + 2 * META;
 };
-// copies of the operand's valid tokens (a multiple of 32, of the group if the groups run along the tokens); lg: log2 of the group
+// Copies of one operand's valid tokens (a multiple of 32, of the group if the groups run along the tokens), tile after tile: the
+// pointers walk.  lg: log2 of the group.
 template <int BITS, int D>
-__device__ __forceinline__ void raw_issue(const TreeArgs& a, int lg, bool cols, const void* codes, const __half* scale, const __half* zero,
-                                          int bh, int tok0, int lt, int NT, uint32_t raw) {
-  using R = Raw<BITS, D>;
-  constexpr int LB = BITS == 8 ? 3 : BITS == 4 ? 2 : 1;
-  const int nt = min(128, a.n - tok0);
-  const size_t row = (size_t)bh * a.ns + tok0;                  // first token row
-  const unsigned char* c = static_cast<const unsigned char*>(codes) + row * (D * BITS / 8);
-  const int chunks = nt * (D * BITS / 8) / 16, lline = lg + LB - 4;             // 16-byte chunks; log2 of those in a row of 8 channels
-#pragma unroll 2
-  for (int i = lt; i < chunks; i += NT) cp_async16(raw + i * 16 + (cols ? (i >> lline) * 16 : 0), c + i * 16);
-  // scales and zero points: D/g a token row, or D a row of g tokens, either way row * D / g from the start
-  const size_t m0 = (row * D >> lg) * 2;
-  const int meta = (nt * D >> lg) * 2 / 16;
-  for (int i = lt; i < 2 * meta; i += NT) {
-    const int o = i < meta ? i : i - meta;
-    cp_async16(raw + R::CODES + (i < meta ? 0 : R::META) + o * 16, reinterpret_cast<const unsigned char*>(i < meta ? scale : zero) + m0 + o * 16);
+struct RawCopy {
+  const unsigned char *codes, *scale, *zero;                    // of the next tile, at this thread's first piece
+  int lline;                                                    // log2 of the 16-byte pieces in a row of 8 channels; 31: no rows
+  __device__ __forceinline__ void start(const void* c, const __half* s, const __half* z, size_t row, int lg, bool cols, int lt) {
+    constexpr int LB = BITS == 8 ? 3 : BITS == 4 ? 2 : 1;
+    codes = static_cast<const unsigned char*>(c) + row * (D * BITS / 8) + lt * 16;
+    // scales and zero points: D/g a token row, or D a row of g tokens, either way row * D / g from the start
+    scale = reinterpret_cast<const unsigned char*>(s) + (row * D >> lg) * 2 + lt * 16;
+    zero = reinterpret_cast<const unsigned char*>(z) + (row * D >> lg) * 2 + lt * 16;
+    lline = cols ? lg + LB - 4 : 31;
   }
-}
+  __device__ __forceinline__ void issue(int nt, int lg, int lt, int NT, uint32_t raw) {
+    using R = Raw<BITS, D>;
+    const int pieces = nt * (D * BITS / 8) / 16, meta = (nt * D >> lg) * 2 / 16;
+    const unsigned char* c = codes;
+    for (int i = lt; i < pieces; i += NT, c += NT * 16) cp_async16(raw + i * 16 + (i >> lline) * 16, c);
+    for (int i = lt; i < meta; i += NT) {
+      cp_async16(raw + R::CODES + i * 16, scale + (i - lt) * 16);
+      cp_async16(raw + R::CODES + R::META + i * 16, zero + (i - lt) * 16);
+    }
+    codes += 128 * (D * BITS / 8);
+    scale += (128 * D >> lg) * 2;
+    zero += (128 * D >> lg) * 2;
+  }
+};
 // Groups along the tokens (keys of the main path): an item is 8 channels x PT tokens, a word per channel.
 template <int BITS, int D>
 __device__ __forceinline__ void put_cols(const TreeArgs& a, int lg, int tok0, int lt, int NT, uint32_t raw, uint32_t slot) {
@@ -185,45 +193,49 @@ __device__ __forceinline__ void put_cols(const TreeArgs& a, int lg, int tok0, in
     }
   }
 }
-// Groups along the channels (values; keys quantized token by token): an item is 16 channels of one token.
+// Groups along the channels (values; keys quantized token by token): an item is 32 channels of one token.
 template <int BITS, int D>
 __device__ __forceinline__ void put_rows(const TreeArgs& a, int lg, int tok0, int lt, int NT, uint32_t raw, uint32_t slot) {
   using R = Raw<BITS, D>;
-  constexpr int PIECES = D / 16, W = BITS / 2;                  // words of an item
+  constexpr int PIECES = D / 32, W = BITS;                      // words of an item
 #pragma unroll 1
   for (int i = lt; i < 128 * PIECES; i += NT) {
     const int piece = i % PIECES, row = i / PIECES;
-    uint4 v[2] = {make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)};
-    if (tok0 + row < a.n) {
-      const uint32_t src = raw + (row * PIECES + piece) * (W * 4), m = raw + R::CODES + ((row * D + piece * 16) >> lg) * 2;
-      uint32_t w[W];
-      if constexpr (W == 4) {
-        const uint4 x = lds128(src);
-        w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
-      } else if constexpr (W == 2) {
-        const uint2 x = lds64(src);
-        w[0] = x.x; w[1] = x.y;
-      } else {
-        w[0] = lds32(src);
-      }
-      const uint32_t s2 = lds16(m) * 0x10001u, z2 = lds16(m + R::META) * 0x10001u;
-      // a word's pair f holds channels f and f + 16/BITS; pairs f, f + 1 make the channel pairs (f, f+1) and the upper ones
-      uint32_t c[8];                                            // channels (0,1) .. (14,15)
+    // chunks 4 piece .. 4 piece + 3 of the row
+    const uint32_t at = slot + (piece >> 1) * 16384 + (row >> 3) * 1024 + (row & 7) * 128;
+    const uint32_t c0 = (piece & 1) * 4, sw = row & 7;
+    if (tok0 + row >= a.n) {
 #pragma unroll
-      for (int j = 0; j < W; ++j) {
-        constexpr int U = 16 / BITS;
-#pragma unroll
-        for (int f = 0; f < U; f += 2) {
-          const uint32_t p = code_pair<BITS>(w[j], f * BITS, s2, z2), q = code_pair<BITS>(w[j], (f + 1) * BITS, s2, z2);
-          c[j * U + f / 2] = __byte_perm(p, q, 0x5410);
-          c[j * U + U / 2 + f / 2] = __byte_perm(p, q, 0x7632);
-        }
-      }
-      v[0] = make_uint4(c[0], c[1], c[2], c[3]);
-      v[1] = make_uint4(c[4], c[5], c[6], c[7]);
+      for (int q = 0; q < 4; ++q) sts128(at + (((c0 + q) ^ sw) << 4), make_uint4(0u, 0u, 0u, 0u));
+      continue;
     }
-    sts128(slot + tile_off(row, 2 * piece), v[0]);
-    sts128(slot + tile_off(row, 2 * piece + 1), v[1]);
+    const uint32_t src = raw + (row * PIECES + piece) * (W * 4), m = raw + R::CODES + ((row * D + piece * 32) >> lg) * 2;
+    const uint32_t s2 = lds16(m) * 0x10001u, z2 = lds16(m + R::META) * 0x10001u;
+    uint32_t w[W];
+    if constexpr (W == 2) {
+      const uint2 x = lds64(src);
+      w[0] = x.x; w[1] = x.y;
+    } else {
+#pragma unroll
+      for (int j = 0; j < W; j += 4) {
+        const uint4 x = lds128(src + j * 4);
+        w[j] = x.x; w[j + 1] = x.y; w[j + 2] = x.z; w[j + 3] = x.w;
+      }
+    }
+    // a word's pair f holds channels f and f + 16/BITS; pairs f, f + 1 make the channel pairs (f, f+1) and the upper ones
+    constexpr int U = 16 / BITS;
+    uint32_t c[16];                                             // channels (0,1) .. (30,31)
+#pragma unroll
+    for (int j = 0; j < W; ++j)
+#pragma unroll
+      for (int f = 0; f < U; f += 2) {
+        const uint32_t p = code_pair<BITS>(w[j], f * BITS, s2, z2), q = code_pair<BITS>(w[j], (f + 1) * BITS, s2, z2);
+        c[j * U + f / 2] = __byte_perm(p, q, 0x5410);
+        c[j * U + U / 2 + f / 2] = __byte_perm(p, q, 0x7632);
+      }
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      sts128(at + (((c0 + q) ^ sw) << 4), make_uint4(c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]));
   }
 }
 // rows 128 x .. of the tail followed by the drafts, zeros behind them
@@ -300,11 +312,13 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
   // dedicated ones on, so that loader 0 is always warp TR_SOFT.
   auto warps_of = [&](int u) { return max(1, min(4, (rows - (p.two_rows ? u * 128 : 0) + 31) / 32)); };
   const int w0 = warps_of(0), w1 = warps_of(1), n_load = TR_LOAD + 8 - w0 - w1;
+  // the keys' team: two fifths (their words come apart with less work); arrivals that fill an operand: the larger team
+  const int k_load = TEAMS == 1 ? n_load : (2 * n_load + 2) / 5, full_load = max(k_load, n_load - k_load);
   const bool loads = warp < TR_SOFT ? (warp & 3) >= (warp < 4 ? w0 : w1) : warp < TR_SOFT + TR_LOAD;
   const int lw = warp >= TR_SOFT ? warp - TR_SOFT : TR_LOAD + (warp < 4 ? warp - w0 : 4 - w0 + (warp - 4) - w1);
   if (tid == 0) {
     for (int i = 0; i < p.slots; ++i) {
-      mbar_init(bar(TB_FULL, i), (n_load + TEAMS - 1) / TEAMS); // one arrival per warp of a team of loaders
+      mbar_init(bar(TB_FULL, i), full_load);                    // one arrival per warp of the larger team
       mbar_init(bar(TB_EMPTY, i), 1);                           // a tcgen05.commit
     }
     for (int u = 0; u < 2; ++u) {
@@ -557,9 +571,10 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
     if (!ok) give_up = 1;
   } else {
     // ---- loader warps
-    const int team = lw % TEAMS, t_size = (n_load - team + TEAMS - 1) / TEAMS, NT = t_size * 32, lt = lw / TEAMS * 32 + lane;
-    const bool first = lw / TEAMS == 0;                         // the team's first warp also arrives for those that a smaller team lacks
-    const uint32_t arrivals = first ? 1 + (n_load + TEAMS - 1) / TEAMS - t_size : 1;
+    const int team = TEAMS == 2 && lw >= k_load ? 1 : 0, t_size = TEAMS == 1 ? n_load : team ? n_load - k_load : k_load;
+    const int tw = lw - (team ? k_load : 0), NT = t_size * 32, lt = tw * 32 + lane;
+    const bool first = tw == 0;                                 // the team's first warp also arrives for those that a smaller team lacks
+    const uint32_t arrivals = first ? 1 + full_load - t_size : 1;
     // operand i: keys (even) or values (odd) of this block's tile i / 2; this team's are team, team + TEAMS, ...
     bool ok = true;
     Ring wr;                                                    // the team's next operand's slot
@@ -588,7 +603,7 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
 #pragma unroll
           for (int kb = 0; kb < D / 64; ++kb)
             tma_load_3d(slot() + kb * 16384, team ? &map_v : &map_k, kb * 64, 128 * (j0 + i / 2), bh, bar(TB_FULL, wr.i));
-          mbar_arrive_n(bar(TB_FULL, wr.i), (n_load + TEAMS - 1) / TEAMS - 1);
+          mbar_arrive_n(bar(TB_FULL, wr.i), full_load - 1);
         }
         __syncwarp();
         wr.next(p.slots, TEAMS);
@@ -604,11 +619,16 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
       const int stages = p.raw / TEAMS;
       const uint32_t raw0 = ring + p.slots * SLOT + team * stages * Raw<BITS, D>::BYTES, raw_end = raw0 + stages * Raw<BITS, D>::BYTES;
       uint32_t raw_in = raw0, raw_out = raw0;
+      RawCopy<BITS, D> ck, cv;                                  // a team of two uses one of them
+      const size_t row0_ctx = (size_t)bh * a.ns + 128 * j0;
+      if (TEAMS == 1 || team == 0) ck.start(a.kc, a.ks, a.kz, row0_ctx, p.lg, cols, lt);
+      if (TEAMS == 1) cv.start(a.vc, a.vs, a.vz, row0_ctx, p.lg, false, lt);
+      else if (team == 1) ck.start(a.vc, a.vs, a.vz, row0_ctx, p.lg, false, lt);
       auto issue = [&](int op) {
         if (op < 2 * n_ctx) {
-          const int tok0 = 128 * (j0 + op / 2);
-          if (op & 1) raw_issue<BITS, D>(a, p.lg, false, a.vc, a.vs, a.vz, bh, tok0, lt, NT, raw_in);
-          else raw_issue<BITS, D>(a, p.lg, cols, a.kc, a.ks, a.kz, bh, tok0, lt, NT, raw_in);
+          const int nt = min(128, a.n - 128 * (j0 + op / 2));
+          if (TEAMS == 1 && (op & 1)) cv.issue(nt, p.lg, lt, NT, raw_in);
+          else ck.issue(nt, p.lg, lt, NT, raw_in);
         }
         cp_async_commit();
         raw_in += Raw<BITS, D>::BYTES;
