@@ -360,7 +360,8 @@ qp_status qp_decode_attn_layers_ex(int n_layers, const void* const* q, const qp_
  * A whole prompt is q_start = 0, n_q = L; a prompt taken in by chunks is one call per chunk.  accumulate = 0: weights of
  * positions below q_start + n_q are set, those behind are set to 0.  accumulate != 0: they are added to, and the positions
  * behind are left as they are.  Keys at and behind q_start + n_q are not looked at and may hold anything.
- * The error word of the bounded waits (see qp_window_scores) is at byte offset qp_prompt_weights_workspace_bytes(...) - 256.
+ * The kernels wait on hardware barriers with a bounded number of polls (see qp_window_scores); a wait that runs out makes the
+ * weights that hang on it NaN.
  */
 size_t qp_prompt_weights_workspace_bytes(int batch, int n_q_heads, int n_kv_heads, int head_dim, int L, int q_start, int n_q);
 qp_status qp_prompt_weights(const void* Q, const void* K, int batch, int n_q_heads, int n_kv_heads, int head_dim, int L,

@@ -684,10 +684,10 @@ qp_status qp_prompt_weights(const void* Q, const void* K, int batch, int n_q_hea
   if (s != QP_OK) return s;
   if (!aligned16(Q) || !aligned16(K) || !aligned16(weights) || !aligned16(workspace)) return QP_ERR_ALIGNMENT;
   const PromptDims d{batch, n_q_heads, n_kv_heads, head_dim, L, q_start, n_q};
-  if (workspace_bytes < prompt_workspace(d)) return QP_ERR_WORKSPACE;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   cache_written(st);                                          // plain order for the stream's next decode call
-  return launch_prompt_weights(Q, K, d, accumulate, weights, workspace, workspace_bytes, st) == cudaSuccess ? QP_OK : QP_ERR_CUDA;
+  const cudaError_t e = launch_prompt_weights(Q, K, d, accumulate, weights, workspace, workspace_bytes, st);
+  return e == cudaSuccess ? QP_OK : e == cudaErrorMemoryAllocation ? QP_ERR_WORKSPACE : QP_ERR_CUDA;
 }
 
 qp_status qp_heavy_select(const float* weights, int batch, int n_kv_heads, int L, int w, int n_keep, int n_cap,

@@ -234,7 +234,8 @@ cudaError_t launch_decode_mma(const DecTable& tab, const DecDims& d, float* part
 struct PromptDims {
   int Bt, Hq, Hkv, D, L, q_start, nq;
 };
-size_t prompt_workspace(const PromptDims& d);   // the last 256 bytes hold the error word
+size_t prompt_workspace(const PromptDims& d);
+// cudaErrorMemoryAllocation, before anything is launched: the workspace is too small (asked here, the plan is made once)
 cudaError_t launch_prompt_weights(const void* Q, const void* K, const PromptDims& d, int accumulate, float* weights, void* ws,
                                   size_t ws_bytes, cudaStream_t st);
 // one layer; ly.ns: slots per (batch, KV head) of the cache and of weights
@@ -265,7 +266,7 @@ struct TreeArgs {
   void* out;
   int Bt, Hq, Hkv, D, bits, group, k_axis, n, ns, n_tail, T;
 };
-size_t tree_workspace(const TreeArgs& a);       // the last 256 bytes hold the error word
+size_t tree_workspace(const TreeArgs& a);       // the error words come first
 cudaError_t launch_tree(const TreeArgs& a, void* ws, cudaStream_t st);
 
 }  // namespace qp

@@ -129,7 +129,7 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
 template <int PASS, int D>
 __global__ void __launch_bounds__(PW_THREADS, 1)
 prompt_sweep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const Plan p, int BH,
-                    float scale_log2, const float* __restrict__ neg_lse, void* __restrict__ out, int* __restrict__ error_word) {
+                    float scale_log2, const float* __restrict__ neg_lse, void* __restrict__ out) {
   constexpr uint32_t OPER = 128 * D * 2;                // one operand tile: D/64 swizzled blocks of 16 KB
   extern __shared__ unsigned char smem_raw[];
   __shared__ uint64_t bars[PB_COUNT];
@@ -325,21 +325,18 @@ prompt_sweep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
           }
           __syncwarp();                                 // the tensor-memory instructions want the whole warp
         };
-        // two halves of 64 columns; a loop, not unrolled: the folds are long, and their code has to stay in the instruction cache
+        // a loop, not unrolled: the folds are long, and their code has to stay in the instruction cache
 #pragma unroll 1
-        for (int c0 = 0; c0 < 128; c0 += 64) {
-          uint32_t va[32], vb[32];
-          tmem_ld32_issue(taddr + c0, va);
-          tmem_ld32_issue(taddr + c0 + 32, vb);
-          tmem_wait(va);
-          tmem_wait(vb);
-          if (c0) {                                     // half of the arithmetic hides the next product
+        for (int c0 = 0; c0 < 128; c0 += 32) {
+          uint32_t v[32];
+          tmem_ld32_issue(taddr + c0, v);
+          tmem_wait(v);
+          if (c0 == 96) {                                 // the buffer is handed back before the last arithmetic
             asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(PB_T_EMPTY, g));
           }
-          fold(va, c0);
-          fold(vb, c0 + 32);
+          fold(v, c0);
         }
       }
       if (PASS == 2) {
@@ -349,17 +346,18 @@ prompt_sweep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
       }
     }
     if (!ok) give_up = 1;
-    if (group_valid(g)) {
-      if (PASS == 1)
-        static_cast<float2*>(out)[(((size_t)bh * p.nquads + quad) * p.max_chunks + chunk) * 512 + g * 128 + rloc] = make_float2(m_run, s_run);
-      else
-        static_cast<float*>(out)[((size_t)chunk * BH + bh) * (512 * (size_t)p.nquads) + 512 * (size_t)quad + g * 128 + rloc] = s_run;
-    }
   }
 
   asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
   __syncthreads();                                      // every part is done with shared and tensor memory
-  if (give_up && tid == 0) atomicExch(error_word, 1);
+  if (warp < PW_READ_WARPS && group_valid(warp >> 2)) {
+    const int at = tid;                                 // group * 128 + row
+    const float bad = give_up ? NAN : 0.f;              // a wait that ran out shows in what it was for
+    if (PASS == 1)
+      static_cast<float2*>(out)[(((size_t)bh * p.nquads + quad) * p.max_chunks + chunk) * 512 + at] = make_float2(m_run, s_run + bad);
+    else
+      static_cast<float*>(out)[((size_t)chunk * BH + bh) * (512 * (size_t)p.nquads) + 512 * (size_t)quad + at] = s_run + bad;
+  }
   if (warp == PW_READ_WARPS + 1) {
     asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem_base), "r"(PW_TMEM_COLS) : "memory");
@@ -382,9 +380,9 @@ prompt_lse_kernel(const Plan p, const float2* __restrict__ stats, float* __restr
     for (int k = 0; k < 4; ++k) v[k] = s[(size_t)min(c0 + k, pieces - 1) * 512];
 #pragma unroll
     for (int k = 0; k < 4; ++k)
-      if (c0 + k < pieces && v[k].x != -INFINITY) {
+      if (c0 + k < pieces) {
         const float mn = fmaxf(m, v[k].x);
-        z = z * exp2f(m - mn) + v[k].y * exp2f(v[k].x - mn);
+        z = v[k].x == -INFINITY ? z + v[k].y : z * exp2f(m - mn) + v[k].y * exp2f(v[k].x - mn);    // (a piece without visible keys: 0)
         m = mn;
       }
   }
@@ -469,7 +467,7 @@ Plan make_plan(int pass, const PromptDims& d) {
 }
 
 struct PromptWorkspace {
-  size_t stats, lse, part, error, total;
+  size_t stats, lse, part, total;
 };
 PromptWorkspace carve(const PromptDims& d, const Plan& p1, const Plan& p2) {
   auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
@@ -478,20 +476,19 @@ PromptWorkspace carve(const PromptDims& d, const Plan& p1, const Plan& p2) {
   w.stats = 0;
   w.lse = w.stats + up(BH * p1.nquads * p1.max_chunks * 512 * sizeof(float2));
   w.part = w.lse + up((size_t)d.Bt * d.Hq * p1.nqt * 128 * sizeof(float));
-  w.error = w.part + up(BH * p2.max_chunks * p2.nquads * 512 * sizeof(float));
-  w.total = w.error + 256;
+  w.total = w.part + up(BH * p2.max_chunks * p2.nquads * 512 * sizeof(float));
   return w;
 }
 
 template <int PASS, int D>
 cudaError_t launch_sweep(const CUtensorMap& q, const CUtensorMap& k, const Plan& p, int BH, float scale_log2, const float* lse,
-                         void* out, int* err, cudaStream_t st) {
+                         void* out, cudaStream_t st) {
   constexpr size_t smem = (PW_GROUPS + PW_STAGES) * (size_t)128 * D * 2 + 1024;
   static unsigned char done[64] = {};
   const cudaError_t e = allow_smem(prompt_sweep_kernel<PASS, D>, smem, done);
   if (e != cudaSuccess) return e;
   return launch_chained(prompt_sweep_kernel<PASS, D>, dim3(p.n_items * BH), dim3(PW_THREADS), smem, st, q, k, p, BH, scale_log2,
-                        lse, out, err);
+                        lse, out);
 }
 
 }  // namespace
@@ -502,11 +499,10 @@ cudaError_t launch_prompt_weights(const void* Q, const void* K, const PromptDims
                                   size_t ws_bytes, cudaStream_t st) {
   const Plan p1 = make_plan(1, d), p2 = make_plan(2, d);
   const PromptWorkspace w = carve(d, p1, p2);
-  if (ws_bytes < w.total) return cudaErrorInvalidValue;
+  if (ws_bytes < w.total) return cudaErrorMemoryAllocation;       // (before anything is launched: the caller's "too small")
   char* base = static_cast<char*>(ws);
   float2* stats = reinterpret_cast<float2*>(base + w.stats);
   float *lse = reinterpret_cast<float*>(base + w.lse), *part = reinterpret_cast<float*>(base + w.part);
-  int* err = reinterpret_cast<int*>(base + w.error);
   const int BH = d.Bt * d.Hkv;
   const float scale_log2 = (float)(1.4426950408889634 / sqrt((double)d.D));
   CUtensorMap mq, mk;
@@ -514,15 +510,13 @@ cudaError_t launch_prompt_weights(const void* Q, const void* K, const PromptDims
   if (e != cudaSuccess) return e;
   e = row_map(&mk, K, (long long)BH * d.L, d.D);
   if (e != cudaSuccess) return e;
-  e = cudaMemsetAsync(err, 0, sizeof(int), st);
-  if (e != cudaSuccess) return e;
-  e = d.D == 128 ? launch_sweep<1, 128>(mq, mk, p1, BH, scale_log2, lse, stats, err, st)
-                 : launch_sweep<1, 64>(mq, mk, p1, BH, scale_log2, lse, stats, err, st);
+  e = d.D == 128 ? launch_sweep<1, 128>(mq, mk, p1, BH, scale_log2, lse, stats, st)
+                 : launch_sweep<1, 64>(mq, mk, p1, BH, scale_log2, lse, stats, st);
   if (e != cudaSuccess) return e;
   e = launch_chained(prompt_lse_kernel, dim3((p1.nqt * 128 + 255) / 256, d.Bt * d.Hq), dim3(256), 0, st, p1, (const float2*)stats, lse);
   if (e != cudaSuccess) return e;
-  e = d.D == 128 ? launch_sweep<2, 128>(mq, mk, p2, BH, scale_log2, lse, part, err, st)
-                 : launch_sweep<2, 64>(mq, mk, p2, BH, scale_log2, lse, part, err, st);
+  e = d.D == 128 ? launch_sweep<2, 128>(mq, mk, p2, BH, scale_log2, lse, part, st)
+                 : launch_sweep<2, 64>(mq, mk, p2, BH, scale_log2, lse, part, st);
   if (e != cudaSuccess) return e;
   return launch_chained(prompt_add_kernel, dim3((d.L + 255) / 256, BH), dim3(256), 0, st, p2, BH, (const float*)part, accumulate, weights);
 }

@@ -350,4 +350,4 @@ def test_steps_from_a_graph_and_on_another_stream(bits):
     graph.replay()
     graph.replay()
     torch.cuda.synchronize()
-    assert torch.equal(out, ref + ref) and int(pws[-256:-252].view(torch.int32)) == 0
+    assert torch.equal(out, ref + ref)
