@@ -22,13 +22,6 @@
 
 #include "qp_mma.cuh"
 
-#ifndef DWS
-#define DWS 2
-#define DWB 3
-#endif
-#ifndef DWL
-#define DWL 24576
-#endif
 namespace qp {
 
 namespace {
@@ -36,7 +29,7 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int DW_WARPS = 4, DW_THREADS = DW_WARPS * 32, DW_MAX_CLUSTER = 16;
-constexpr int DW_LOGIT_BYTES = DWL;    // of shared memory; runs with more logits keep them in the workspace
+constexpr int DW_LOGIT_BYTES = 24576;  // of shared memory; runs with more logits keep them in the workspace
 
 struct DwArgs {
   DecLayer ly;
@@ -315,7 +308,7 @@ struct Pk {
   static constexpr int PPG = CH > GROUP ? 1 : GROUP / CH;       // pieces of a group
   // a 32-token tile in shared memory
   static constexpr int KC = 0, VC = 32 * RB, KS = 64 * RB, MB = 64 * NG, KZ = KS + MB, VS = KZ + MB, VZ = VS + MB, BYTES = VZ + MB;
-  static constexpr int STAGES = DWS;
+  static constexpr int STAGES = 2;                     // 12 warps per SM hide what a third stage would; see the launch bounds
   static constexpr int P_STRIDE = 80, P_BYTES = 8 * P_STRIDE;   // weights of a tile, [head][32 tokens] f16 and a pad
   static constexpr int WARP_BYTES = STAGES * BYTES + P_BYTES;
   static constexpr size_t SMEM = (size_t)DW_WARPS * WARP_BYTES + DW_LOGIT_BYTES;
@@ -345,7 +338,7 @@ __device__ __forceinline__ void lds_halves(__half (&h)[N], uint32_t addr) {
 }
 
 template <int BITS, int D, int GROUP>
-__global__ void __launch_bounds__(DW_THREADS, DWB)
+__global__ void __launch_bounds__(DW_THREADS, 3)
 decode_weights_packed_kernel(const __grid_constant__ DwArgs a) {
   using L = Pk<BITS, D, GROUP>;
   constexpr int NP = L::NP, NG = L::NG, NF = L::CHW / 2;        // NF: operand pairs of a word

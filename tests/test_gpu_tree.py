@@ -95,7 +95,13 @@ CASES = [  # Bt, Hq, Hkv, D, n, cap, bits, g, axis, T, n_tail
 ]
 
 
-@pytest.mark.parametrize("Bt,Hq,Hkv,D,n,cap,bits,g,axis,T,m", CASES)
+LONG = [  # several clusters per head, whose results are joined; more heads than the GPU holds at once
+    (1, 32, 8, 128, 8192, 8192, 4, 32, 0, 64, 21), (1, 8, 1, 128, 16384, 16384, 16, 32, 0, 5, 0), (1, 8, 1, 64, 20000, 20000, 16, 32, 0, 64, 0),
+    (1, 8, 1, 128, 4096, 4224, 2, 64, 1, 33, 0), (1, 8, 2, 64, 6144, 6144, 8, 32, 0, 2, 3), (19, 32, 8, 128, 320, 320, 4, 32, 0, 16, 9),
+]
+
+
+@pytest.mark.parametrize("Bt,Hq,Hkv,D,n,cap,bits,g,axis,T,m", CASES + LONG)
 def test_tree(Bt, Hq, Hkv, D, n, cap, bits, g, axis, T, m):
     c, st, k, v = make_cache(Bt, Hq, Hkv, D, n, cap, bits, g, axis)
     parents, sees = random_tree(Bt, T, n + T)
@@ -169,9 +175,9 @@ def test_large_logits_and_values():
     assert torch.isfinite(out).all()
 
 
-@pytest.mark.parametrize("bits", [16, 2])
-def test_from_a_graph_on_a_side_stream(bits):
-    Bt, Hq, Hkv, D, n, T = 1, 32, 8, 128, 1024, 40
+@pytest.mark.parametrize("bits,n", [(16, 1024), (2, 1024), (4, 9216)])
+def test_from_a_graph_on_a_side_stream(bits, n):
+    Bt, Hq, Hkv, D, T = 1, 32, 8, 128, 40
     c, _, _, _ = make_cache(Bt, Hq, Hkv, D, n, n, bits, 32, 0)
     q, kd, vd = randn((Bt, T, Hq, D), 3), randn((Bt, T, Hkv, D), 4), randn((Bt, T, Hkv, D), 5)
     mask = qp.tree_mask(random_tree(Bt, T, 5)[0])

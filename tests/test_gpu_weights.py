@@ -148,7 +148,13 @@ DECODES = [  # Bt, Hq, Hkv, D, n, cap, bits, g
 ]
 
 
-@pytest.mark.parametrize("Bt,Hq,Hkv,D,n,cap,bits,g", DECODES)
+LONG = [  # the logits of a block's run do not fit its shared memory
+    (1, 32, 8, 128, 30001, 30016, 16, 32), (1, 8, 1, 64, 20000, 20000, 16, 32), (1, 32, 8, 128, 26656, 26656, 4, 32), (1, 16, 2, 64, 16384, 16384, 8, 64),
+    (20, 40, 5, 128, 4100, 4100, 16, 32),
+]
+
+
+@pytest.mark.parametrize("Bt,Hq,Hkv,D,n,cap,bits,g", DECODES + LONG)
 def test_decode_attn_weights(Bt, Hq, Hkv, D, n, cap, bits, g):
     cache, st, k, v = per_token_cache(Bt, Hq, Hkv, D, n, cap, bits, g)
     q = randn((Bt, Hq, D), 7, 1.5)
@@ -351,3 +357,58 @@ def test_steps_from_a_graph_and_on_another_stream(bits):
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(out, ref + ref)
+
+
+# ---------------------------------------------------------------------------------------------- long arrays
+
+def spread_out(cache, n_cap):
+    """The same tokens in arrays with room for n_cap tokens per head (what lies behind them is not finite)."""
+    d = cache.desc
+    big = qp.alloc_cache(d.batch, d.n_q_heads, d.n_kv_heads, d.head_dim, d.bits, d.group, d.n_keep, DEV, n_cap)
+    n = d.n_keep
+    for name in ("k_codes", "v_codes", "k_scale", "k_zero", "v_scale", "v_zero"):
+        src, dst = getattr(cache, name), getattr(big, name)
+        if src is None:
+            continue
+        dst = dst.view(d.batch, d.n_kv_heads, n_cap, -1)            # per-token arrays
+        dst.view(torch.int16).fill_(0x7fc0 if d.bits == 16 else 0x7e00)
+        dst[:, :, :n] = src.view(d.batch, d.n_kv_heads, n, -1)
+    return big
+
+
+@pytest.mark.parametrize("bits,Bt,n_cap", [(16, 20, 131072), (4, 20, 1 << 20)])
+def test_strides_past_32_bits(bits, Bt, n_cap):
+    """Offsets beyond 2^32 bytes: bit for bit what the same tokens give in short arrays."""
+    Hq, Hkv, D, n = 16, 8, 128, 320
+    cache, st, _, _ = per_token_cache(Bt, Hq, Hkv, D, n, n, bits, 32)
+    big = spread_out(cache, n_cap)
+    assert big.k_codes.numel() * big.k_codes.element_size() > 2 ** 32
+    q = randn((Bt, Hq, D), 7, 1.5)
+    w, wb = torch.zeros((Bt, Hkv, n), device=DEV), torch.zeros((Bt, Hkv, n_cap), device=DEV)
+    out = qp.decode_attn_weights(q, cache, w, st)
+    assert torch.equal(out, qp.decode_attn_weights(q, big, wb, st)) and torch.equal(w, wb[:, :, :n])
+    T = 9
+    qt, kd, vd = randn((Bt, T, Hq, D), 8), randn((Bt, T, Hkv, D), 9), randn((Bt, T, Hkv, D), 10)
+    mask = qp.tree_mask((torch.arange(T, device=DEV) - 1).expand(Bt, T))
+    assert torch.equal(qp.decode_attn_tree(qt, cache, kd, vd, mask, strategy=st), qp.decode_attn_tree(qt, big, kd, vd, mask, strategy=st))
+    if bits < 16:                                                  # (a 16-bit cache with room would grow instead)
+        pos = torch.arange(n, dtype=torch.int32, device=DEV).expand(Bt, Hkv, n).contiguous()
+        pb = torch.zeros((Bt, Hkv, n_cap), dtype=torch.int32, device=DEV)
+        pb[:, :, :n] = pos
+        kn, vn = randn((Bt, Hkv, D), 11), randn((Bt, Hkv, D), 12)
+        s, sb = qp.evict_kv(kn, vn, cache, w, pos, n, 8, st), qp.evict_kv(kn, vn, big, wb, pb, n, 8, st)
+        assert torch.equal(s, sb) and torch.equal(pos, pb[:, :, :n])
+        for name in ("k_codes", "v_codes", "k_scale", "v_zero"):
+            a, b = getattr(cache, name), getattr(big, name)
+            assert torch.equal(a.view(Bt, Hkv, n, -1), b.view(Bt, Hkv, n_cap, -1)[:, :, :n])
+
+
+def test_prompt_rows_past_32_bits():
+    """Keys of the last heads lie beyond 2^32 bytes: the same weights as in an array of their own."""
+    Bt, Hq, Hkv, D, L, nq = 34, 4, 4, 128, 131072, 130
+    K = torch.zeros((Bt, Hkv, L, D), dtype=torch.bfloat16, device=DEV)
+    small = randn((Bt, Hkv, 300, D), 1, 1.5)
+    K[:, :, :300] = small
+    Q = randn((Bt, Hq, nq, D), 2, 1.5)
+    assert K.numel() * 2 > 2 ** 32
+    assert torch.equal(qp.prompt_weights(Q, K, 100)[:, :, :300], qp.prompt_weights(Q, small, 100))
