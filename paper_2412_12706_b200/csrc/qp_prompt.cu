@@ -16,9 +16,9 @@
 //   - part of the exponentials evaluated on the FMA pipe (ex2_poly2), two at a time with packed 32-bit arithmetic;
 //   - sweep 1 without a running maximum: a row's reference is renewed only when a chunk's sum leaves the range in which
 //     nothing can overflow, which the sum itself shows.
-// Tiles above the diagonal are skipped, for each group on its own.  The work (a quad of resident tiles x a run of streamed
-// tiles, see Plan) is cut into pieces of nearly equal length; pieces leave partial results that two small kernels add in a
-// fixed order.
+// Tiles above the diagonal are skipped, for each group on its own.  The work of all quads of resident tiles, end to end, is cut
+// into one run per SM (see Plan); a quad that several runs share leaves partial results, which two small kernels add in a fixed
+// order.
 #include <algorithm>
 
 #include "qp_mma.cuh"
@@ -35,10 +35,19 @@ constexpr uint32_t PW_TMEM_COLS = 512;
 
 // One sweep's work.  Resident tiles come in quads: sweep 1, tile r of a KV head = query tile r / G of its query head r % G;
 // sweep 2, tile r = keys 128 r ..  A quad's streamed tiles are numbered 0 .. quad_steps - 1 (sweep 1: key tiles from the
-// start; sweep 2: for each query head, the query tiles from the first that sees the quad) and cut into pieces of `chunk`.
+// start; sweep 2: for each query head, the query tiles from the first that sees the quad).  The quads of all (batch, KV head)
+// lie on one line, each as PW_SWITCH places that stand for fetching its resident tiles and then its steps; block i of `runs` does
+// the steps in one of `runs` equal shares of it, so every block is done at the same time whatever the shape.
+// (Pieces of one length, one to a block, dealt out by the hardware: 593 us for 8192 tokens of 32 heads over 8, 1080 us for the
+// last 1999 of 16k of 64 over 8; the line: 562 and 1070, at 1.73 GHz and the GPU's power limit.  1, 2 or 3 places for a fetch
+// differ by less than 2 %.)
+constexpr int PW_SWITCH = 1;
 struct Plan {
   int Hq, Hkv, G, L, nq, q_start, n;   // n = q_start + nq
-  int nqt, nquads, chunk, max_chunks, n_items;   // n_items: per (batch, KV head)
+  int nqt, nquads, runs, max_parts;    // max_parts: runs that can share a quad
+  long long head_len, length;          // places of a (batch, KV head), of all
+  long long run_len;                   // of a run; the first `longer` runs have one more
+  int longer;
 };
 
 __host__ __device__ inline int quad_steps(int pass, const Plan& p, int quad) {
@@ -48,18 +57,46 @@ __host__ __device__ inline int quad_steps(int pass, const Plan& p, int quad) {
   }
   return p.G * (p.nqt - max(0, 512 * quad - p.q_start) / 128);
 }
+__device__ __forceinline__ long long run_start(const Plan& p, int i) { return p.run_len * i + min(i, p.longer); }
+// places divided by a length: 32 bits for all but the very longest
+__device__ __forceinline__ int place_div(const Plan& p, long long x, long long len) {
+  return p.length <= 0x7fffffff ? (int)((unsigned)x / (unsigned)len) : (int)(x / len);
+}
+__device__ __forceinline__ int run_of(const Plan& p, long long place) {
+  const long long split = (p.run_len + 1) * p.longer;
+  return place < split ? place_div(p, place, p.run_len + 1) : p.longer + place_div(p, place - split, p.run_len);
+}
+// the quad that holds place `at` of a head, or with at < 0 quad `want`; its first place.  Called by whole warps.
+__device__ __forceinline__ int find_quad(int pass, const Plan& p, long long at, int want, long long& first) {
+  const int lane = threadIdx.x & 31;
+  long long base = 0;
+  for (int q0 = 0;; q0 += 32) {
+    const int q = q0 + lane, len = q < p.nquads ? quad_steps(pass, p, q) + PW_SWITCH : 0;
+    int inc = len;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += v;
+    }
+    const unsigned past = __ballot_sync(0xffffffffu, at < 0 ? q >= want : base + inc > at);
+    if (past || q0 + 32 >= p.nquads) {
+      const int src = past ? __ffs(past) - 1 : 31;
+      first = base + __shfl_sync(0xffffffffu, inc - len, src);
+      return q0 + src;
+    }
+    base += __shfl_sync(0xffffffffu, inc, 31);
+  }
+}
 
-enum : int { PB_A_FULL = 0, PB_S_FULL = 1, PB_S_EMPTY = PB_S_FULL + PW_STAGES, PB_T_FULL = PB_S_EMPTY + PW_STAGES,
+enum : int { PB_A_FULL = 0, PB_A_EMPTY = PW_GROUPS, PB_S_FULL = 2 * PW_GROUPS, PB_S_EMPTY = PB_S_FULL + PW_STAGES, PB_T_FULL = PB_S_EMPTY + PW_STAGES,
              PB_T_EMPTY = PB_T_FULL + PW_GROUPS, PB_COUNT = PB_T_EMPTY + PW_GROUPS };
 
-#ifndef QP_PW_POLY_NUM
-#define QP_PW_POLY_NUM 1
-#define QP_PW_POLY_DEN 4
-#endif
-// pair `i` of a chunk: PW_POLY_NUM of every PW_POLY_DEN pairs through ex2_poly2, the others through the hardware unit
+// pair `i` of a chunk: one of every PW_POLY through ex2_poly2, the others through the hardware unit (8192 tokens of 32 heads
+// over 8, none / 1 of 8 / 1 of 4 / 3 of 8: 668 / 624 / 614 / 630 us)
+constexpr int PW_POLY = 4;
 template <bool TOP>
 __device__ __forceinline__ uint64_t ex2_pair(uint64_t x, int i) {
-  if ((i * QP_PW_POLY_NUM) % QP_PW_POLY_DEN < QP_PW_POLY_NUM) return ex2_poly2<TOP>(x);
+  if (i % PW_POLY == 0) return ex2_poly2<TOP>(x);
   float a, b;
   unpack2(x, a, b);
   return pack2(ex2a(a), ex2a(b));
@@ -111,10 +148,10 @@ __device__ __forceinline__ float fold_column(const uint32_t (&r)[32], const floa
   unpack2(add2(acc0, acc1), a, b);
   return a + b;
 }
-__device__ __forceinline__ float fold_column_masked(const uint32_t (&r)[32], const float* lse, int c0, int first, float scale_log2) {
+__device__ __forceinline__ float fold_column_masked(const uint32_t (&r)[32], const float* lse, int first, int rows, float scale_log2) {
   float acc = 0.f;
 #pragma unroll
-  for (int i = 0; i < 32; ++i) acc += c0 + i >= first ? ex2a(fmaf(__uint_as_float(r[i]), scale_log2, lse[i])) : 0.f;
+  for (int i = 0; i < 32; ++i) acc += i >= first && i < rows ? ex2a(fmaf(__uint_as_float(r[i]), scale_log2, lse[i])) : 0.f;
   return acc;
 }
 
@@ -124,34 +161,35 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
                : "memory");
 }
 
-// out: sweep 1, float2 (reference, sum) [bh][quad][piece][512 rows]; sweep 2, float [piece][bh][512 * quads] column sums
+// out: sweep 1, float2 (reference, sum) [bh][quad][part][512 rows]; sweep 2, float [part][bh][512 * quads] column sums
 // neg_lse: -lse, [Bt * Hq][128 * nqt], -inf behind the last row
 template <int PASS, int D>
 __global__ void __launch_bounds__(PW_THREADS, 1)
-prompt_sweep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const Plan p, int BH,
+prompt_sweep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ Plan p, int BH,
                     float scale_log2, const float* __restrict__ neg_lse, void* __restrict__ out) {
   constexpr uint32_t OPER = 128 * D * 2;                // one operand tile: D/64 swizzled blocks of 16 KB
   extern __shared__ unsigned char smem_raw[];
   __shared__ uint64_t bars[PB_COUNT];
   __shared__ __align__(16) float s_lse[PW_STAGES][128];
   __shared__ uint32_t tmem_base_slot;
-  __shared__ int give_up, s_quad, s_chunk;
+  __shared__ int give_up, s_quad;
+  __shared__ long long s_first;
 
   const int tid = threadIdx.x, lane = tid & 31;
   const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
-  const int bh = blockIdx.x % BH, b = bh / p.Hkv, hk = bh % p.Hkv;
   const uint32_t sA = (smem_u32(smem_raw) + 1023u) & ~1023u, sS = sA + PW_GROUPS * OPER;
   const uint32_t bar0 = smem_u32(&bars[0]);
   auto bar = [&](int which, int i) { return bar0 + (uint32_t)(which + i) * 8u; };
   const volatile int* gu = &give_up;
 
   if (tid == 0) {
-    mbar_init(bar(PB_A_FULL, 0), 1);
     for (int i = 0; i < PW_STAGES; ++i) {
       mbar_init(bar(PB_S_FULL, i), 1);
       mbar_init(bar(PB_S_EMPTY, i), PASS == 1 ? 1 : 1 + PW_READ_WARPS);   // the commit (and the readers of the stage's lse)
     }
     for (int i = 0; i < PW_GROUPS; ++i) {
+      mbar_init(bar(PB_A_FULL, i), 1);
+      mbar_init(bar(PB_A_EMPTY, i), 1);
       mbar_init(bar(PB_T_FULL, i), 1);
       mbar_init(bar(PB_T_EMPTY, i), 4);                                    // its warps
     }
@@ -164,84 +202,99 @@ prompt_sweep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
   }
+  const long long run0 = run_start(p, blockIdx.x), run1 = run_start(p, blockIdx.x + 1);
+  const int bh0 = place_div(p, run0, p.head_len);
   if (warp == 0) {
-    // piece number -> (quad, piece of the quad): the longest quads first, 32 quads at a time
-    int left = blockIdx.x / BH, quad = -1, chunk = 0;
-    for (int q0 = 0; q0 < p.nquads && quad < 0; q0 += 32) {
-      const int qi = q0 + lane, q = PASS == 1 ? p.nquads - 1 - qi : qi;
-      const int c = qi < p.nquads ? (quad_steps(PASS, p, q) + p.chunk - 1) / p.chunk : 0;
-      int inc = c;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += v;
-      }
-      const unsigned past = __ballot_sync(0xffffffffu, inc > left);
-      if (past) {
-        const int src = __ffs(past) - 1;
-        quad = __shfl_sync(0xffffffffu, q, src);
-        chunk = left - __shfl_sync(0xffffffffu, inc - c, src);
-      } else {
-        left -= __shfl_sync(0xffffffffu, inc, 31);
-      }
-    }
-    if (lane == 0) { s_quad = quad; s_chunk = chunk; }
+    long long first;
+    const int q = find_quad(PASS, p, run0 - bh0 * p.head_len, 0, first);
+    if (lane == 0) { s_quad = q; s_first = bh0 * p.head_len + first; }
   }
   asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
   const uint32_t tmem_base = tmem_base_slot;
-  const int quad = s_quad, chunk = s_chunk;
-  const int step0 = chunk * p.chunk, n_loc = min(p.chunk, quad_steps(PASS, p, quad) - step0);
-  const int t0 = PASS == 2 ? max(0, 512 * quad - p.q_start) / 128 : 0;     // sweep 2: first query tile of a head
+  // This block's part of a quad, and the walk over them: every warp does it for itself.
+  struct Part {
+    int bh, quad, b, hk, step0, n_loc, t0;                // n_loc 0: none of the quad's steps;  t0: sweep 2, first query tile of a head
+    long long first;                                      // the quad's place
+  };
+  Part part{bh0, s_quad - 1, 0, 0, 0, 0, 0, s_first};
+  auto next_part = [&]() {                                // false: the run is done
+    do {
+      if (part.quad >= 0 && part.quad + 1 == p.nquads) {
+        part.quad = -1;
+        ++part.bh;
+      }
+      ++part.quad;
+      const int steps = quad_steps(PASS, p, part.quad);
+      if (part.first >= run1) return false;
+      const long long s0 = part.first + PW_SWITCH;
+      part.step0 = (int)(max(run0, s0) - s0);
+      part.n_loc = (int)(min(run1, s0 + steps) - s0) - part.step0;
+      part.first = s0 + steps;
+    } while (part.n_loc <= 0);
+    part.b = part.bh / p.Hkv;
+    part.hk = part.bh % p.Hkv;
+    part.t0 = PASS == 2 ? max(0, 512 * part.quad - p.q_start) / 128 : 0;
+    return true;
+  };
   // the resident tile of group g: does it exist
-  auto group_valid = [&](int g) { return PASS == 1 ? (4 * quad + g) / p.G < p.nqt : 128 * (4 * quad + g) < p.n; };
+  auto group_valid = [&](int g) { return PASS == 1 ? (4 * part.quad + g) / p.G < p.nqt : 128 * (4 * part.quad + g) < p.n; };
   // sweep 1: the last streamed tile it needs; sweep 2: the first query tile of a head it needs (both never, if it does not exist)
   auto group_bound = [&](int g) {
-    if (PASS == 1) return group_valid(g) ? (p.q_start + min(p.nq, ((4 * quad + g) / p.G + 1) * 128) - 1) / 128 : -1;
-    return group_valid(g) ? max(0, 128 * (4 * quad + g) - p.q_start) / 128 : 0x7fffffff;
+    if (PASS == 1) return group_valid(g) ? (p.q_start + min(p.nq, ((4 * part.quad + g) / p.G + 1) * 128) - 1) / 128 : -1;
+    return group_valid(g) ? max(0, 128 * (4 * part.quad + g) - p.q_start) / 128 : 0x7fffffff;
   };
+  bool more = next_part();
   chain_enter();                                        // the launch's set-up overlaps the previous kernel's end
 
-  float m_run = -INFINITY, s_run = 0.f;                 // sweep 1: this thread's row; sweep 2: s_run = its key's sum
-
+  int done = 0;                                         // streamed tiles of the parts before this one
   if (warp == PW_READ_WARPS) {
     // ---- copy warp
-    int issued = 0;
+    int issued = 0, resident = 0;                       // resident: fetches of resident tiles so far, PW_GROUPS a part
     bool ok = true;
-    if (lane == 0) {
-      int valid = 0;
-      for (int g = 0; g < PW_GROUPS; ++g) valid += group_valid(g) ? 1 : 0;
-      mbar_expect_tx(bar(PB_A_FULL, 0), valid * OPER);
-      for (int g = 0; g < valid; ++g) {                 // the valid groups come first
-        const int r = 4 * quad + g;
-        const int y = PASS == 1 ? (b * p.Hq + hk * p.G + r % p.G) * p.nq + r / p.G * 128 : bh * p.L + 128 * r;
+    for (int n = 0; ok && more; ++n, more = next_part()) {
+      for (int j = 0; j < part.n_loc; ++j) {
+        const int at = done + j, st = at % PW_STAGES;
+        if (at >= PW_STAGES) ok = mbar_wait_warp(bar(PB_S_EMPTY, st), (uint32_t)((at / PW_STAGES - 1) & 1), gu);
+        if (!ok) break;
+        if (lane == 0) {
+          mbar_expect_tx(bar(PB_S_FULL, st), OPER + (PASS == 2 ? 512 : 0));
+          int y;
+          if (PASS == 1) {
+            y = part.bh * p.L + (part.step0 + j) * 128;
+          } else {
+            const int per = p.nqt - part.t0, s = part.step0 + j, bq = part.b * p.Hq + part.hk * p.G + s / per, t = part.t0 + s % per;
+            y = bq * p.nq + t * 128;
+            bulk_load(smem_u32(&s_lse[st][0]), neg_lse + ((size_t)bq * p.nqt + t) * 128, 512, bar(PB_S_FULL, st));
+          }
 #pragma unroll
-        for (int kb = 0; kb < D / 64; ++kb)
-          tma_load_2d(sA + g * OPER + kb * 16384, PASS == 1 ? &map_q : &map_k, kb * 64, y, bar(PB_A_FULL, 0));
-      }
-    }
-    __syncwarp();
-    for (int j = 0; j < n_loc; ++j) {
-      const int st = j % PW_STAGES;
-      if (j >= PW_STAGES) ok = mbar_wait_warp(bar(PB_S_EMPTY, st), (uint32_t)((j / PW_STAGES - 1) & 1), gu);
-      if (!ok) break;
-      if (lane == 0) {
-        mbar_expect_tx(bar(PB_S_FULL, st), OPER + (PASS == 2 ? 512 : 0));
-        int y;
-        if (PASS == 1) {
-          y = bh * p.L + (step0 + j) * 128;
-        } else {
-          const int per = p.nqt - t0, h = (step0 + j) / per, t = t0 + (step0 + j) % per, bq = b * p.Hq + hk * p.G + h;
-          y = bq * p.nq + t * 128;
-          bulk_load(smem_u32(&s_lse[st][0]), neg_lse + ((size_t)bq * p.nqt + t) * 128, 512, bar(PB_S_FULL, st));
+          for (int kb = 0; kb < D / 64; ++kb)
+            tma_load_2d(sS + st * OPER + kb * 16384, PASS == 1 ? &map_k : &map_q, kb * 64, y, bar(PB_S_FULL, st));
         }
+        issued = at + 1;
+        __syncwarp();
+        for (int g = 0; j == 0 && g < PW_GROUPS; ++g) { // behind the first streamed tile: the resident ones
+          if (n > 0) ok = mbar_wait_warp(bar(PB_A_EMPTY, g), (uint32_t)((n - 1) & 1), gu);
+          if (!ok) break;
+          if (lane == 0) {
+            if (group_valid(g)) {
+              const int r = 4 * part.quad + g;
+              const int y = PASS == 1 ? (part.b * p.Hq + part.hk * p.G + r % p.G) * p.nq + r / p.G * 128 : part.bh * p.L + 128 * r;
+              mbar_expect_tx(bar(PB_A_FULL, g), OPER);
 #pragma unroll
-        for (int kb = 0; kb < D / 64; ++kb)
-          tma_load_2d(sS + st * OPER + kb * 16384, PASS == 1 ? &map_k : &map_q, kb * 64, y, bar(PB_S_FULL, st));
+              for (int kb = 0; kb < D / 64; ++kb)
+                tma_load_2d(sA + g * OPER + kb * 16384, PASS == 1 ? &map_q : &map_k, kb * 64, y, bar(PB_A_FULL, g));
+            } else {
+              mbar_arrive(bar(PB_A_FULL, g));           // (one phase a part for every group)
+            }
+          }
+          ++resident;
+          __syncwarp();
+        }
+        if (!ok) break;
       }
-      issued = j + 1;
-      __syncwarp();
+      done += part.n_loc;
     }
     if (!ok) {
       give_up = 1;
@@ -250,7 +303,8 @@ prompt_sweep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
         for (uint32_t i = 0; i < TC_SPIN_LIMIT; ++i)
           if (mbar_try_wait(full, parity)) return;
       };
-      landed(bar(PB_A_FULL, 0), 0u);
+      for (int i = max(0, resident - PW_GROUPS); i < resident; ++i)
+        landed(bar(PB_A_FULL, i % PW_GROUPS), (uint32_t)((i / PW_GROUPS) & 1));
       for (int j = max(0, issued - PW_STAGES); j < issued; ++j)
         landed(bar(PB_S_FULL, j % PW_STAGES), (uint32_t)((j / PW_STAGES) & 1));
     }
@@ -258,129 +312,156 @@ prompt_sweep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     // ---- MMA warp: streamed tile j against the resident tiles that need it
     constexpr uint32_t IDESC = instr_desc(128, 128);
     int uses[PW_GROUPS] = {}, bound[PW_GROUPS];
+    bool ok = true;
+    for (int n = 0; ok && more; ++n, more = next_part()) {
 #pragma unroll
-    for (int g = 0; g < PW_GROUPS; ++g) bound[g] = group_bound(g);
-    int t = PASS == 2 ? t0 + step0 % (p.nqt - t0) : 0;  // sweep 2: query tile of the step
-    bool ok = mbar_wait_warp(bar(PB_A_FULL, 0), 0u, gu);
-    for (int j = 0; j < n_loc && ok; ++j) {
-      const int st = j % PW_STAGES;
-      ok = mbar_wait_warp(bar(PB_S_FULL, st), (uint32_t)((j / PW_STAGES) & 1), gu);
+      for (int g = 0; g < PW_GROUPS; ++g) bound[g] = group_bound(g);
+      int t = PASS == 2 ? part.t0 + part.step0 % (p.nqt - part.t0) : 0;   // sweep 2: query tile of the step
+      for (int j = 0; j < part.n_loc && ok; ++j) {
+        const int st = (done + j) % PW_STAGES;
+        ok = mbar_wait_warp(bar(PB_S_FULL, st), (uint32_t)(((done + j) / PW_STAGES) & 1), gu);
 #pragma unroll
-      for (int g = 0; g < PW_GROUPS; ++g) {
-        if (!ok || !(PASS == 1 ? step0 + j <= bound[g] : t >= bound[g])) continue;
-        if (uses[g] > 0) ok = mbar_wait_warp(bar(PB_T_EMPTY, g), (uint32_t)((uses[g] - 1) & 1), gu);
-        if (!ok) continue;
-        ++uses[g];
-        asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
-        const uint32_t a = uniform(desc_lo(sA + g * OPER, 1)), s = uniform(desc_lo(sS + st * OPER, 1));
-        const uint32_t tm = uniform(tmem_base + g * 128), done = uniform(bar(PB_T_FULL, g));
-        if (elect_one()) {
-          umma_ss<false>(tm, a, s, IDESC);
+        for (int g = 0; g < PW_GROUPS; ++g) {
+          // (needed or not: a tile whose fetch may be under way is not handed back)
+          if (ok && j == 0) ok = mbar_wait_warp(bar(PB_A_FULL, g), (uint32_t)(n & 1), gu);
+          if (ok && (PASS == 1 ? part.step0 + j <= bound[g] : t >= bound[g])) {
+            if (uses[g] > 0) ok = mbar_wait_warp(bar(PB_T_EMPTY, g), (uint32_t)((uses[g] - 1) & 1), gu);
+            if (ok) {
+              ++uses[g];
+              asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+              const uint32_t a = uniform(desc_lo(sA + g * OPER, 1)), s = uniform(desc_lo(sS + st * OPER, 1));
+              const uint32_t tm = uniform(tmem_base + g * 128), full = uniform(bar(PB_T_FULL, g));
+              if (elect_one()) {
+                umma_ss<false>(tm, a, s, IDESC);
 #pragma unroll
-          for (int k = 1; k < D / 16; ++k) umma_ss<true>(tm, a + (k / 4) * 1024 + (k % 4) * 2, s + (k / 4) * 1024 + (k % 4) * 2, IDESC);
-          umma_commit(done);
+                for (int k = 1; k < D / 16; ++k)
+                  umma_ss<true>(tm, a + (k / 4) * 1024 + (k % 4) * 2, s + (k / 4) * 1024 + (k % 4) * 2, IDESC);
+                umma_commit(full);
+              }
+              __syncwarp();
+            }
+          }
+          const uint32_t idle = uniform(bar(PB_A_EMPTY, g));
+          if (ok && j + 1 == part.n_loc && elect_one()) umma_commit(idle);
+          __syncwarp();
         }
+        const uint32_t empty = uniform(bar(PB_S_EMPTY, st));
+        if (ok && elect_one()) umma_commit(empty);
         __syncwarp();
+        if (PASS == 2 && ++t == p.nqt) t = part.t0;
       }
-      const uint32_t empty = uniform(bar(PB_S_EMPTY, st));
-      if (ok && elect_one()) umma_commit(empty);
-      __syncwarp();
-      if (PASS == 2 && ++t == p.nqt) t = t0;
+      done += part.n_loc;
     }
+    // the last hand-back, which nobody waits for, has arrived before the block ends
+    if (ok && done > 0) ok = mbar_wait_warp(bar(PB_S_EMPTY, (done - 1) % PW_STAGES), (uint32_t)(((done - 1) / PW_STAGES) & 1), gu);
     if (!ok) give_up = 1;
   } else {
     // ---- reading groups
     const int g = warp >> 2, rloc = (warp & 3) * 32 + lane;
     const uint32_t taddr = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + g * 128;
-    const int bound = group_bound(g), tq = PASS == 1 ? (4 * quad + g) / p.G : 0;
-    int uses = 0, t = PASS == 2 ? t0 + step0 % (p.nqt - t0) : 0;
+    int uses = 0;
     bool ok = true;
-    for (int j = 0; j < n_loc; ++j) {
-      const int st = j % PW_STAGES, step = step0 + j;
-      // sweep 2 hands the stage back below whether it needed it or not, and only once it has been filled: a group that
-      // skips tiles must not run ahead of the ring
-      if (PASS == 2) ok = mbar_wait_warp(bar(PB_S_FULL, st), (uint32_t)((j / PW_STAGES) & 1), gu);
-      if (!ok) break;
-      if (PASS == 1 ? step <= bound : t >= bound) {
-        ok = mbar_wait_warp(bar(PB_T_FULL, g), (uint32_t)(uses & 1), gu);
+    for (; more; more = next_part()) {
+      const int bound = group_bound(g), tq = PASS == 1 ? (4 * part.quad + g) / p.G : 0;
+      float m_run = -INFINITY, s_run = 0.f;             // sweep 1: this thread's row; sweep 2: s_run = its key's sum
+      int t = PASS == 2 ? part.t0 + part.step0 % (p.nqt - part.t0) : 0;
+      for (int j = 0; j < part.n_loc && ok; ++j) {
+        const int st = (done + j) % PW_STAGES, step = part.step0 + j;
+        // sweep 2 hands the stage back below whether it needed it or not, and only once it has been filled: a group that
+        // skips tiles must not run ahead of the ring
+        if (PASS == 2) ok = mbar_wait_warp(bar(PB_S_FULL, st), (uint32_t)(((done + j) / PW_STAGES) & 1), gu);
         if (!ok) break;
-        ++uses;
-        asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
-        bool all;                                       // every row of the tile sees every key of it
-        int lim;                                        // sweep 1: last column this row sees; sweep 2: first row that sees this key
-        if (PASS == 1) {
-          all = 128 * step + 127 <= p.q_start + 128 * tq;
-          lim = min(p.q_start + 128 * tq + rloc, p.n - 1) - 128 * step;
-        } else {
-          const int key0 = 128 * (4 * quad + g);
-          all = key0 + 127 <= p.q_start + 128 * t;
-          lim = key0 + rloc - p.q_start - 128 * t;
-        }
-        auto fold = [&](const uint32_t (&r)[32], int c0) {
-          if constexpr (PASS == 1) {
-            if (!all || !fold_row_all(r, scale_log2, m_run, s_run)) fold_row_any(r, c0, lim, scale_log2, m_run, s_run);
+        if (PASS == 1 ? step <= bound : t >= bound) {
+          ok = mbar_wait_warp(bar(PB_T_FULL, g), (uint32_t)(uses & 1), gu);
+          if (!ok) break;
+          ++uses;
+          asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+          bool all;                                     // every row of the tile sees every key of it
+          int lim, rows = 128;                          // sweep 1: last column this row sees; sweep 2: first row that sees this key
+          if (PASS == 1) {
+            all = 128 * step + 127 <= p.q_start + 128 * tq;
+            lim = min(p.q_start + 128 * tq + rloc, p.n - 1) - 128 * step;
           } else {
-            const float* l = &s_lse[st][c0];
-            s_run += all ? fold_column(r, l, scale_log2) : fold_column_masked(r, l, c0, lim, scale_log2);
+            const int key0 = 128 * (4 * part.quad + g);
+            rows = p.nq - 128 * t;                      // (what lies behind a head's last row is the next head's, and may hold anything)
+            all = key0 + 127 <= p.q_start + 128 * t && rows >= 128;
+            lim = key0 + rloc - p.q_start - 128 * t;
           }
-          __syncwarp();                                 // the tensor-memory instructions want the whole warp
-        };
-        // a loop, not unrolled: the folds are long, and their code has to stay in the instruction cache
+          auto fold = [&](const uint32_t (&r)[32], int c0) {
+            if constexpr (PASS == 1) {
+              if (!all || !fold_row_all(r, scale_log2, m_run, s_run)) fold_row_any(r, c0, lim, scale_log2, m_run, s_run);
+            } else {
+              const float* l = &s_lse[st][c0];
+              s_run += all ? fold_column(r, l, scale_log2) : fold_column_masked(r, l, lim - c0, rows - c0, scale_log2);
+            }
+            __syncwarp();                               // the tensor-memory instructions want the whole warp
+          };
+          // a loop, not unrolled: the folds are long, and their code has to stay in the instruction cache
 #pragma unroll 1
-        for (int c0 = 0; c0 < 128; c0 += 32) {
-          uint32_t v[32];
-          tmem_ld32_issue(taddr + c0, v);
-          tmem_wait(v);
-          if (c0 == 96) {                                 // the buffer is handed back before the last arithmetic
-            asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(PB_T_EMPTY, g));
+          for (int c0 = 0; c0 < 128; c0 += 32) {
+            uint32_t v[32];
+            tmem_ld32_issue(taddr + c0, v);
+            tmem_wait(v);
+            if (c0 == 96) {                               // the buffer is handed back before the last arithmetic
+              asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+              __syncwarp();
+              if (lane == 0) mbar_arrive(bar(PB_T_EMPTY, g));
+            }
+            fold(v, c0);
           }
-          fold(v, c0);
+        }
+        if (PASS == 2) {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(PB_S_EMPTY, st));
+          if (++t == p.nqt) t = part.t0;
         }
       }
-      if (PASS == 2) {
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(PB_S_EMPTY, st));
-        if (++t == p.nqt) t = t0;
+      done += part.n_loc;
+      if (!ok) { give_up = 1; s_run = NAN; }            // a wait that ran out shows in what it was for
+      if (group_valid(g)) {
+        // the quad's first place is behind us by its steps: which of the runs that share it this one is
+        const int nth = blockIdx.x - run_of(p, part.first - quad_steps(PASS, p, part.quad));
+        if (PASS == 1)
+          static_cast<float2*>(out)[(((size_t)part.bh * p.nquads + part.quad) * p.max_parts + nth) * 512 + tid] = make_float2(m_run, s_run);
+        else
+          static_cast<float*>(out)[((size_t)nth * BH + part.bh) * (512 * (size_t)p.nquads) + 512 * (size_t)part.quad + tid] = s_run;
       }
     }
-    if (!ok) give_up = 1;
   }
 
   asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
   __syncthreads();                                      // every part is done with shared and tensor memory
-  if (warp < PW_READ_WARPS && group_valid(warp >> 2)) {
-    const int at = tid;                                 // group * 128 + row
-    const float bad = give_up ? NAN : 0.f;              // a wait that ran out shows in what it was for
-    if (PASS == 1)
-      static_cast<float2*>(out)[(((size_t)bh * p.nquads + quad) * p.max_chunks + chunk) * 512 + at] = make_float2(m_run, s_run + bad);
-    else
-      static_cast<float*>(out)[((size_t)chunk * BH + bh) * (512 * (size_t)p.nquads) + 512 * (size_t)quad + at] = s_run + bad;
-  }
   if (warp == PW_READ_WARPS + 1) {
     asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem_base), "r"(PW_TMEM_COLS) : "memory");
   }
 }
 
-// -lse of every row from the pieces' (reference, sum) pairs, -inf for the padding rows of a head's last tile
+// runs that share a quad.  Called by whole warps.
+__device__ __forceinline__ int quad_parts(int pass, const Plan& p, int bh, int quad) {
+  long long first;
+  find_quad(pass, p, -1, quad, first);
+  first += bh * p.head_len + PW_SWITCH;
+  return run_of(p, first + quad_steps(pass, p, quad) - 1) - run_of(p, first) + 1;
+}
+
+// -lse of every row from the parts' (reference, sum) pairs, -inf for the padding rows of a head's last tile
 __global__ void __launch_bounds__(256)
 prompt_lse_kernel(const Plan p, const float2* __restrict__ stats, float* __restrict__ neg_lse) {
-  chain_enter();
   const int i = blockIdx.x * 256 + threadIdx.x, bq = blockIdx.y, b = bq / p.Hq, hq = bq % p.Hq, h = hq % p.G;
-  if (i >= p.nqt * 128) return;
+  if (i >= p.nqt * 128) return;                         // (whole warps)
   const int bh = b * p.Hkv + hq / p.G, r = (i / 128) * p.G + h, quad = r / 4;
-  const int pieces = (quad_steps(1, p, quad) + p.chunk - 1) / p.chunk;
-  const float2* s = stats + (((size_t)bh * p.nquads + quad) * p.max_chunks) * 512 + (r % 4) * 128 + (i & 127);
+  const int parts = quad_parts(1, p, bh, quad);
+  chain_enter();
+  const float2* s = stats + (((size_t)bh * p.nquads + quad) * p.max_parts) * 512 + (r % 4) * 128 + (i & 127);
   float m = -INFINITY, z = 0.f;
-  for (int c0 = 0; c0 < pieces; c0 += 4) {
+  for (int c0 = 0; c0 < parts; c0 += 4) {
     float2 v[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = s[(size_t)min(c0 + k, pieces - 1) * 512];
+    for (int k = 0; k < 4; ++k) v[k] = s[(size_t)min(c0 + k, parts - 1) * 512];
 #pragma unroll
     for (int k = 0; k < 4; ++k)
-      if (c0 + k < pieces) {
+      if (c0 + k < parts) {
         const float mn = fmaxf(m, v[k].x);
         z = v[k].x == -INFINITY ? z + v[k].y : z * exp2f(m - mn) + v[k].y * exp2f(v[k].x - mn);    // (a piece without visible keys: 0)
         m = mn;
@@ -389,27 +470,27 @@ prompt_lse_kernel(const Plan p, const float2* __restrict__ stats, float* __restr
   neg_lse[(size_t)bq * (p.nqt * 128) + i] = i < p.nq ? -(m + log2f(z)) : -INFINITY;
 }
 
-// weights from the pieces' column sums, in the pieces' order
+// weights from the parts' column sums, in the parts' order
 __global__ void __launch_bounds__(256)
 prompt_add_kernel(const Plan p, int BH, const float* __restrict__ part, int accumulate, float* __restrict__ weights) {
-  chain_enter();
   const int j = blockIdx.x * 256 + threadIdx.x, bh = blockIdx.y;
+  const int parts = j / 512 < p.nquads ? quad_parts(2, p, bh, j / 512) : 0;      // (the same for a whole block)
+  chain_enter();
   if (j >= p.L) return;
   float* w = weights + (size_t)bh * p.L + j;
   if (j >= p.n) {
     if (!accumulate) *w = 0.f;
     return;
   }
-  const int pieces = (quad_steps(2, p, j / 512) + p.chunk - 1) / p.chunk;
   const size_t stride = (size_t)BH * (512 * (size_t)p.nquads);
   const float* s = part + (size_t)bh * (512 * (size_t)p.nquads) + j;
   float acc = 0.f;
-  for (int c0 = 0; c0 < pieces; c0 += 4) {
+  for (int c0 = 0; c0 < parts; c0 += 4) {
     float v[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = s[(size_t)min(c0 + k, pieces - 1) * stride];
+    for (int k = 0; k < 4; ++k) v[k] = s[(size_t)min(c0 + k, parts - 1) * stride];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) acc += c0 + k < pieces ? v[k] : 0.f;
+    for (int k = 0; k < 4; ++k) acc += c0 + k < parts ? v[k] : 0.f;
   }
   *w = accumulate ? *w + acc : acc;
 }
@@ -432,37 +513,17 @@ Plan make_plan(int pass, const PromptDims& d) {
   p.Hq = d.Hq; p.Hkv = d.Hkv; p.G = d.Hq / d.Hkv; p.L = d.L; p.nq = d.nq; p.q_start = d.q_start; p.n = d.q_start + d.nq;
   p.nqt = (d.nq + 127) / 128;
   p.nquads = pass == 1 ? (p.nqt * p.G + 3) / 4 : (p.n + 511) / 512;
-  // Length of a piece: a piece costs its steps and about 2.5 more (loading the resident tiles, set-up); the launch lasts whole
-  // rounds of pieces when there are few of them, and about the average load and a part of a last piece when there are many.
-  const int sms = sm_count(), BH = d.Bt * d.Hkv;
   int longest = 0;
-  long long total = 0;
   for (int q = 0; q < p.nquads; ++q) {
-    const int s = quad_steps(pass, p, q);
-    longest = std::max(longest, s);
-    total += s;
+    const int n = quad_steps(pass, p, q);
+    longest = std::max(longest, n);
+    p.head_len += n + PW_SWITCH;
   }
-  double best = 1e300;
-  for (int c : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256}) {
-    if (c > 1 && c / 2 >= longest) break;
-    if ((double)total * BH / sms > 200.0 * c) continue;          // far too many pieces
-    long long items = 0;
-    for (int q = 0; q < p.nquads; ++q) items += (quad_steps(pass, p, q) + c - 1) / c;
-    const double len = std::min(c, longest) + 2.5, all = (double)items * BH;
-    const double rounds = (double)((items * BH + sms - 1) / sms) * len;
-    const double flow = ((double)total * BH + 2.5 * all) / sms + 0.75 * len;
-    const double cost = std::min(rounds, std::max(flow, len)) + 0.002 * all / sms;
-    if (cost < best) {
-      best = cost;
-      p.chunk = c;
-      p.n_items = (int)items;
-    }
-  }
-  if (p.chunk == 0) {                                            // (longer than any candidate)
-    p.chunk = longest;
-    p.n_items = p.nquads;
-  }
-  p.max_chunks = (longest + p.chunk - 1) / p.chunk;
+  p.length = p.head_len * (d.Bt * d.Hkv);
+  p.runs = (int)std::min<long long>(p.length, sm_count());
+  p.run_len = p.length / p.runs;
+  p.longer = (int)(p.length % p.runs);
+  p.max_parts = (int)std::min<long long>(longest, longest / p.run_len + 2);
   return p;
 }
 
@@ -474,9 +535,9 @@ PromptWorkspace carve(const PromptDims& d, const Plan& p1, const Plan& p2) {
   const size_t BH = (size_t)d.Bt * d.Hkv;
   PromptWorkspace w{};
   w.stats = 0;
-  w.lse = w.stats + up(BH * p1.nquads * p1.max_chunks * 512 * sizeof(float2));
+  w.lse = w.stats + up(BH * p1.nquads * p1.max_parts * 512 * sizeof(float2));
   w.part = w.lse + up((size_t)d.Bt * d.Hq * p1.nqt * 128 * sizeof(float));
-  w.total = w.part + up(BH * p2.max_chunks * p2.nquads * 512 * sizeof(float));
+  w.total = w.part + up(BH * p2.max_parts * p2.nquads * 512 * sizeof(float));
   return w;
 }
 
@@ -487,7 +548,7 @@ cudaError_t launch_sweep(const CUtensorMap& q, const CUtensorMap& k, const Plan&
   static unsigned char done[64] = {};
   const cudaError_t e = allow_smem(prompt_sweep_kernel<PASS, D>, smem, done);
   if (e != cudaSuccess) return e;
-  return launch_chained(prompt_sweep_kernel<PASS, D>, dim3(p.n_items * BH), dim3(PW_THREADS), smem, st, q, k, p, BH, scale_log2,
+  return launch_chained(prompt_sweep_kernel<PASS, D>, dim3(p.runs), dim3(PW_THREADS), smem, st, q, k, p, BH, scale_log2,
                         lse, out);
 }
 

@@ -412,3 +412,18 @@ def test_prompt_rows_past_32_bits():
     Q = randn((Bt, Hq, nq, D), 2, 1.5)
     assert K.numel() * 2 > 2 ** 32
     assert torch.equal(qp.prompt_weights(Q, K, 100)[:, :, :300], qp.prompt_weights(Q, small, 100))
+
+
+def test_prompt_rows_of_other_heads_do_not_matter():
+    """A head's last tile of queries reaches into the next head's rows, its last keys into the next head's keys: NaN there stays there."""
+    Bt, Hq, Hkv, D, L, q0, nq = 2, 8, 2, 128, 300, 70, 200
+    Q, K = randn((Bt, Hq, nq, D), 1, 1.5), randn((Bt, Hkv, L, D), 2, 1.5)
+    ref = qp.prompt_weights(Q, K, q0)
+    for poison in (float("nan"), float("inf")):
+        Q2, K2 = Q.clone(), K.clone()
+        Q2[1], K2[1] = poison, poison
+        K2[:, :, q0 + nq:] = poison                                     # keys that no query sees
+        assert torch.equal(qp.prompt_weights(Q2, K2, q0)[0], ref[0])
+        Q2, K2 = Q.clone(), K.clone()
+        Q2[0], K2[0] = poison, poison
+        assert torch.equal(qp.prompt_weights(Q2, K2, q0)[1], ref[1])
