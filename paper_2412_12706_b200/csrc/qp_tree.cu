@@ -597,6 +597,7 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
       int flying = 0;
       for (; i < 2 * n_ctx; i += TEAMS) {
         wait_empty(i);
+        if (i == team + TEAMS) ok = ok && mbar_wait_warp(bar(TB_Q, 0), 0u, gu);   // the queries overtake all but the first tile
         if (!ok) break;
         if (first && lane == 0) {
           mbar_expect_tx(bar(TB_FULL, wr.i), SLOT);
