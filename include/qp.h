@@ -412,9 +412,11 @@ qp_status qp_evict_kv(const void* k_new, const void* v_new, qp_cache* cache /* h
  * q, out bf16 [Bt,T,Hq,D]; k_draft, v_draft bf16 [Bt,T,Hkv,D]; mask uint64 [Bt,T]; 1 <= T <= QP_MAX_DRAFTS.  The drafts' rows
  * need not be in the cache; accepted ones are appended with qp_append_kv.  tail: NULL or as for qp_decode_attn_tail.
  * strategy: NULL (per-channel keys, or 16 bit) or k_axis 0 / 1 without filtering.  Any bits.  For B < 16 keys and values,
- * drafts and tail included, are multiplied in fp16 (|x| <= 65504).  Plain stream order.  The workspace begins with W * max(1, min(16, 148 / W)) 32-bit
- * error words, W = batch * n_kv_heads * ceil(T G / 256), set by every call: one that is not 0 says that a bounded wait ran out
- * (see qp_window_scores) and the output is invalid.  They are 0 in every correct run.
+ * drafts and tail included, are multiplied in fp16 (|x| <= 65504).  What a draft holds, numbers or not, reaches only the rows
+ * that see it (the drafts behind the last of a smaller tree of the batch may hold anything).  Plain stream order.  The workspace
+ * begins with W * max(1, min(16, 148 / W)) 32-bit error words, W = batch * n_kv_heads * ceil(T G / 256), set by every call: one
+ * that is not 0 says that a bounded wait ran out (see qp_window_scores) and the output is invalid.  They are 0 in every correct
+ * run.
  */
 #define QP_MAX_DRAFTS 64
 size_t qp_decode_tree_workspace_bytes(const qp_cache* cache /* host */, int T);

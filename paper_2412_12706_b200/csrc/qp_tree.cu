@@ -238,9 +238,16 @@ __device__ __forceinline__ void put_rows(const TreeArgs& a, int lg, int tok0, in
       sts128(at + (((c0 + q) ^ sw) << 4), make_uint4(c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]));
   }
 }
-// rows 128 x .. of the tail followed by the drafts, zeros behind them
+// halves of w that are not finite (of fp16, or of bf16)
+template <bool HALF>
+__device__ __forceinline__ uint32_t not_finite2(uint32_t w) { return __vcmpgeu2(w & 0x7fff7fffu, HALF ? 0x7c007c00u : 0x7f807f80u); }
+
+// rows 128 x .. of the tail followed by the drafts, zeros behind them.  A draft's value that is not finite must not reach the
+// rows that do not see the draft (their weight 0 times it is NaN, and a padded tree may hold anything there): it becomes 0 and
+// the draft's bit is set in `bad`; the rows that do see it get it at the end, see add_bad.
 template <int D, bool HALF>
-__device__ __forceinline__ void put_extra(const TreeArgs& a, bool keys, int b, int hk, int bh, int x, int lt, int NT, uint32_t slot) {
+__device__ __forceinline__ void put_extra(const TreeArgs& a, bool keys, int b, int hk, int bh, int x, int lt, int NT, uint32_t slot,
+                                          unsigned long long* bad) {
   constexpr int PIECES = D / 16;
   const uint16_t* tail = static_cast<const uint16_t*>(keys ? a.k_tail : a.v_tail);
   const uint16_t* draft = static_cast<const uint16_t*>(keys ? a.k_draft : a.v_draft);
@@ -256,6 +263,17 @@ __device__ __forceinline__ void put_extra(const TreeArgs& a, bool keys, int b, i
       for (int j = 0; j < 2; ++j) {
         v[j] = __ldg(p + j);
         if (HALF) v[j] = make_uint4(bf2_to_half2(v[j].x), bf2_to_half2(v[j].y), bf2_to_half2(v[j].z), bf2_to_half2(v[j].w));
+      }
+      if (!keys && e >= a.n_tail) {
+        uint32_t any = 0u;
+        auto clear = [&](uint32_t& w) {
+          const uint32_t m = not_finite2<HALF>(w);
+          w &= ~m;
+          any |= m;
+        };
+#pragma unroll
+        for (int j = 0; j < 2; ++j) { clear(v[j].x); clear(v[j].y); clear(v[j].z); clear(v[j].w); }
+        if (any) atomicOr(bad, 1ull << (e - a.n_tail));
       }
     }
     sts128(slot + tile_off(row, 2 * piece), v[0]);
@@ -273,6 +291,23 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
 template <int D>
 __device__ __forceinline__ uint32_t part_off(int r, int c) { return (uint32_t)(r * (D * 4) + ((c ^ (r & (D / 4 - 1))) << 4)); }
 
+// the values that put_extra left out, for row r of the partial O, which sees the drafts `hit` of them
+template <int D, bool HALF>
+__device__ __forceinline__ void add_bad(unsigned char* part, int r, unsigned long long hit, const uint16_t* draft, int stride) {
+#pragma unroll 1
+  for (; hit; hit &= hit - 1) {
+    const uint16_t* v = draft + (size_t)(__ffsll((long long)hit) - 1) * stride;
+#pragma unroll 1
+    for (int d = 0; d < D; ++d) {
+      const uint32_t w = HALF ? bf2_to_half2(v[d]) : v[d];
+      if (not_finite2<HALF>(w) & 0xffffu) {
+        float* o = reinterpret_cast<float*>(part + part_off<D>(r, d / 4)) + d % 4;
+        *o += HALF ? __half2float(__ushort_as_half((unsigned short)w)) : __uint_as_float(w << 16);
+      }
+    }
+  }
+}
+
 template <int BITS, int D>
 __global__ void __launch_bounds__(TR_THREADS, 1)
 tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
@@ -287,6 +322,7 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
   __shared__ uint64_t bars[TB_COUNT];
   __shared__ uint32_t tmem_base_slot;
   __shared__ int give_up;
+  __shared__ unsigned long long bad_drafts;                     // of this block's tiles: values that are not finite, see put_extra
   cg::cluster_group cluster = cg::this_cluster();
 
   const TreeArgs& a = p.a;
@@ -327,6 +363,7 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
     }
     mbar_init(bar(TB_Q, 0), TR_SOFT);                           // the softmax warps, which fetch the queries
     give_up = 0;
+    bad_drafts = 0ull;
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
   }
   if (warp == TR_SOFT + TR_LOAD) {
@@ -655,7 +692,7 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
     for (; i < 2 * n_loc && ok; i += TEAMS) {
       wait_empty(i);
       if (!ok) break;
-      put_extra<D, HALF>(a, !(i & 1), b, hk, bh, j0 + i / 2 - p.ctx_tiles, lt, NT, slot());
+      put_extra<D, HALF>(a, !(i & 1), b, hk, bh, j0 + i / 2 - p.ctx_tiles, lt, NT, slot(), &bad_drafts);
       publish();
     }
     if (!ok) give_up = 1;
@@ -681,6 +718,16 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
 #pragma unroll
         for (int i = 0; i < 8; ++i)
           sts128(sbase + u * PART + part_off<D>(rl, c0 / 4 + i), make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]));
+      }
+      const int r = (p.two_rows ? u * 128 : 0) + rl;
+      if (bad_drafts && r < rows) {
+        unsigned long long hit = bad_drafts & a.mask[(size_t)b * a.T + draft_of(row0 + r)];
+        if (!p.two_rows) {                                      // this stream's part of a row: the drafts of every second tile
+          const unsigned long long first = a.n_tail + a.T <= 128 ? ~0ull : (1ull << (128 - a.n_tail)) - 1;   // of the first extra tile
+          hit &= ((p.ctx_tiles - j0) & 1) == u ? first : ~first;
+        }
+        add_bad<D, HALF>(part_base + u * PART, rl, hit, static_cast<const uint16_t*>(a.v_draft) + ((size_t)b * a.T * a.Hkv + hk) * D,
+                         a.Hkv * D);
       }
     }
   }

@@ -196,3 +196,39 @@ def test_from_a_graph_on_a_side_stream(bits, n):
     side.synchronize()
     assert torch.equal(o[0], ref) and torch.equal(o[1], ref)
     assert torch.all(ws[:4 * Bt * Hkv].view(torch.int32) == 0)     # no wait ran out
+
+
+@pytest.mark.parametrize("bits,n,T,m", [(16, 300, 64, 0), (16, 5000, 20, 0), (4, 2048, 64, 63), (4, 96, 9, 0), (8, 512, 33, 31), (2, 4096, 64, 100), (2, 256, 40, 100)])
+def test_drafts_that_are_not_finite(bits, n, T, m):
+    """A padded tree: what a draft holds reaches only the rows that see it, channel by channel."""
+    Bt, Hq, Hkv, D = 2, 8, 2, 128
+    g = 128 if m > 63 else 64 if m > 31 else 32
+    n = n // g * g if bits < 16 else n
+    c, _, k, v = make_cache(Bt, Hq, Hkv, D, n, n, bits, g, 0)
+    tail = qp.alloc_tail(c)
+    kt = vt = torch.zeros((Bt, Hkv, 0, D), dtype=torch.bfloat16, device=DEV)
+    if m:
+        tail.k_tail.copy_(randn(tail.k_tail.shape, 6, 1.5)); tail.v_tail.copy_(randn(tail.v_tail.shape, 7))
+        tail.desc.n_tail = m
+        kt, vt = tail.k_tail[:, :, :m], tail.v_tail[:, :, :m]
+    q, kd, vd = randn((Bt, T, Hq, D), 3, 1.5), randn((Bt, T, Hkv, D), 4, 1.5), randn((Bt, T, Hkv, D), 5)
+    sees = random_tree(Bt, T, 7)[1]
+    last = T - 3                                                   # the first tree has padding behind its drafts
+    sees[0, last:] = False
+    sees[0, :, last:] = False
+    sees[0, range(last, T), range(last, T)] = True
+    ref, tol = reference(q, k, v, kt, vt, kd, vd, sees.to(DEV), bits)
+    kd[0, last:], vd[0, last] = float("nan"), float("nan")
+    vd[0, last + 1] = float("inf")
+    vd[0, last + 2] = -1e30 if bits < 16 else float("-inf")        # beyond fp16
+    vd[1, 2, 0, 5] = float("inf"); vd[1, T - 1, 1, 77] = float("-inf")
+    out = qp.decode_attn_tree(q, c, kd, vd, mask_of(sees), tail)
+    want = ref.clone()
+    s = sees.to(DEV)
+    want[1, :, :Hq // 2, 5] = torch.where(s[1, :, 2, None], math.inf, want[1, :, :Hq // 2, 5])
+    want[1, :, Hq // 2:, 77] = torch.where(s[1, :, T - 1, None], -math.inf, want[1, :, Hq // 2:, 77])
+    assert torch.isnan(out[0, last:]).all()                        # their keys are not numbers
+    out, want, tol = torch.cat([out[0, :last], out[1]]).double(), torch.cat([want[0, :last], want[1]]), torch.cat([tol[0, :last], tol[1]])
+    inf = torch.isinf(want)
+    assert inf.any() and torch.equal(out[inf], want[inf])
+    assert torch.all((out - want).abs()[~inf] <= tol[~inf])
