@@ -622,7 +622,13 @@ def decode_tree_workspace_bytes(cache: "Cache | qp_cache", T: int) -> int:
 
 
 def _dev(t: torch.Tensor, dtype: torch.dtype, shape: tuple) -> None:
+    """Contiguous, of this type and shape, and on the device the kernels are launched on."""
     assert t.is_cuda and t.dtype is dtype and t.shape == shape and t.is_contiguous(), (t.dtype, t.shape, shape)
+    assert t.get_device() == torch._C._cuda_getDevice(), "not on the current device"
+
+
+def _dev_cache(cache: Cache) -> None:
+    assert cache.k_codes.get_device() == torch._C._cuda_getDevice(), "cache not on the current device"
 
 
 def _ref(strategy: "Strategy | None"):
@@ -638,10 +644,9 @@ def prompt_weights(Q: torch.Tensor, K: torch.Tensor, q_start: int = 0, weights: 
                    workspace: torch.Tensor | None = None) -> torch.Tensor:
     """qp_prompt_weights: the attention weight each key of K [Bt,Hkv,L,D] has received from the query rows Q [Bt,Hq,n_q,D] at
     positions q_start .. q_start+n_q-1, fp32 [Bt,Hkv,L].  Given ``weights`` they are added to (a prompt in chunks)."""
-    _dev_bf16(Q); _dev_bf16(K)
     Bt, Hkv, L, D = K.shape
     _, Hq, nq, _ = Q.shape
-    assert Q.shape == (Bt, Hq, nq, D)
+    _dev(Q, torch.bfloat16, (Bt, Hq, nq, D)); _dev(K, torch.bfloat16, (Bt, Hkv, L, D))
     accumulate = weights is not None
     if weights is None:
         weights = torch.empty((Bt, Hkv, L), dtype=torch.float32, device=K.device)
@@ -675,8 +680,11 @@ def decode_attn_weights(q: torch.Tensor, cache: Cache, weights: torch.Tensor, st
     d = cache.desc
     _dev(q, torch.bfloat16, (d.batch, d.n_q_heads, d.head_dim))
     _dev(weights, torch.float32, _state_shape(cache))
+    _dev_cache(cache)
     if out is None:
         out = torch.empty_like(q)
+    else:
+        _dev(out, torch.bfloat16, q.shape)
     if workspace is None:
         workspace = new_decode_workspace(decode_weights_workspace_bytes(cache), q.device)
     _check(lib().qp_decode_attn_weights(_ptr(q), ctypes.byref(d), _ref(strategy), _ptr(weights), _ptr(out), _ptr(workspace),
@@ -693,6 +701,7 @@ def evict_kv(k_new: torch.Tensor, v_new: torch.Tensor, cache: Cache, weights: to
     row, state = (Bt, Hkv, d.head_dim), (Bt, Hkv, d.n_cap or d.n_keep)
     _dev(k_new, torch.bfloat16, row); _dev(v_new, torch.bfloat16, row)
     _dev(weights, torch.float32, state); _dev(pos, torch.int32, state)
+    _dev_cache(cache)
     if slots is None:
         slots = pos.new_empty((Bt, Hkv))
     else:
@@ -768,8 +777,11 @@ def decode_attn_tree(q: torch.Tensor, cache: Cache, k_draft: torch.Tensor, v_dra
     for t in (k_draft, v_draft):
         _dev(t, torch.bfloat16, (d.batch, T, d.n_kv_heads, d.head_dim))
     _dev(mask, torch.int64, (d.batch, T))
+    _dev_cache(cache)
     if out is None:
         out = torch.empty_like(q)
+    else:
+        _dev(out, torch.bfloat16, q.shape)
     if workspace is None:
         workspace = new_decode_workspace(decode_tree_workspace_bytes(cache, T), q.device)
     _check(lib().qp_decode_attn_tree(_ptr(q), T, ctypes.byref(d), _ref(strategy), None if tail is None else ctypes.byref(tail.desc),

@@ -5,6 +5,9 @@ it is off by at most (D + 8) 2^-23 sum|q k| / sqrt(D), the 8 for the scaling and
 A softmax weight is off by the factor e^(2 e) of the largest such e (numerator and normaliser), and by 2^-20 for the
 exponential and the additions of positive terms.  Weights are sums of such terms, so the same relative bound holds for them."""
 import math
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -427,3 +430,50 @@ def test_prompt_rows_of_other_heads_do_not_matter():
         Q2, K2 = Q.clone(), K.clone()
         Q2[0], K2[0] = poison, poison
         assert torch.equal(qp.prompt_weights(Q2, K2, q0)[1], ref[1])
+
+
+FIRST_CALLS = """
+import torch
+from paper_2412_12706_b200 import qp
+torch.manual_seed(1)
+r = lambda *s: torch.randn(s, device="cuda").bfloat16()
+Bt, Hq, Hkv, D, L, n, T = 1, 8, 2, 64, 700, 128, 9
+c = qp.alloc_cache(Bt, Hq, Hkv, D, 8, 32, n, "cuda")
+c16 = qp.alloc_cache(Bt, Hq, Hkv, D, 16, 32, n, "cuda")
+for t in (c.k_codes, c.v_codes, c16.k_codes, c16.v_codes, c.k_scale, c.k_zero, c.v_scale, c.v_zero):
+    t.zero_()
+st = qp.make_strategy(c, 1)
+Q, K, q, kd, vd, kn = r(Bt, Hq, L, D), r(Bt, Hkv, L, D), r(Bt, T, Hq, D), r(Bt, T, Hkv, D), r(Bt, T, Hkv, D), r(Bt, Hkv, D)
+mask = torch.full((Bt, T), -1, dtype=torch.int64, device="cuda")
+q1 = q[:, 0].contiguous()
+w = [torch.zeros((Bt, Hkv, n), device="cuda") for _ in range(2)]
+pos = torch.arange(n, dtype=torch.int32, device="cuda").expand(Bt, Hkv, n).contiguous()
+def calls():
+    a = qp.prompt_weights(Q, K)
+    s = qp.heavy_select(a, 8, n)
+    outs = [a, *s]
+    for x, y in ((c, st), (c16, None)):
+        outs += [qp.decode_attn_weights(q1, x, w[0], y), qp.decode_attn_tree(q, x, kd, vd, mask, strategy=y)]
+    outs.append(qp.evict_kv(kn, kn, c, w[1], pos, n, 4, st))
+    return outs
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    got = calls()
+g.replay()
+torch.cuda.synchronize()
+got = [t.clone() for t in got]
+for t in (c.k_codes, c.v_codes, c.k_scale, c.k_zero, c.v_scale, c.v_zero, *w):
+    t.zero_()
+pos.copy_(torch.arange(n, dtype=torch.int32, device="cuda").expand(Bt, Hkv, n))
+for a, b in zip(got, calls()):
+    assert torch.equal(a, b)
+print("same")
+"""
+
+
+def test_first_calls_of_a_process_are_captured():
+    """Every operator's first call, with what it sets up once, under capture; the replay gives what eager calls give."""
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS], capture_output=True, text=True, timeout=300,
+                       cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert r.returncode == 0 and r.stdout.strip() == "same", r.stderr[-2000:]
