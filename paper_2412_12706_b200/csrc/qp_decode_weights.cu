@@ -74,8 +74,14 @@ __device__ __forceinline__ void dw_finish(const DwArgs& a, int bh, int G, int to
     s_out[idx] = A;
     if (d == 0) s_ml[h] = make_float2(M, Z);
   }
+  __syncthreads();
+  // the statistics are handed to every CTA before the barrier (a read after it would be a round trip of a thousand clocks);
+  // the wait is for the arrival at the kernel's start: all CTAs of the cluster are running
+  __shared__ float2 s_all[DW_MAX_CLUSTER][8];
+  cluster.barrier_wait();
+  if (tid < 8 * C && (tid & 7) < G) cluster.map_shared_rank(&s_all[0][0], tid >> 3)[rank * 8 + (tid & 7)] = s_ml[tid & 7];
   cluster.sync();
-  // head statistics of the whole cluster: thread h of every warp's first eight lanes
+  // head statistics of the whole cluster
   __shared__ float2 s_head[8];           // (M, 1 / Z)
   __shared__ float s_f[DW_MAX_CLUSTER][8];
   if (tid < G) {
@@ -83,7 +89,7 @@ __device__ __forceinline__ void dw_finish(const DwArgs& a, int bh, int G, int to
     float M = -INFINITY, Z = 0.f;
 #pragma unroll
     for (int r = 0; r < DW_MAX_CLUSTER; ++r) {
-      if (r < C) v[r] = cluster.map_shared_rank(s_ml, r)[tid];
+      if (r < C) v[r] = s_all[r][tid];
       if (r < C) M = fmaxf(M, v[r].x);
     }
 #pragma unroll
@@ -108,7 +114,10 @@ __device__ __forceinline__ void dw_finish(const DwArgs& a, int bh, int G, int to
     for (int r = 0; r < DW_MAX_CLUSTER; ++r) A = r < C ? fmaf(v[r], s_f[r][h], A) : A;
     static_cast<bf16*>(a.ly.out)[(size_t)bh * G * D + idx] = __float2bfloat16_rn(A * s_head[h].y);
   }
+  __syncwarp();
+  cluster.barrier_arrive();              // done with the others' shared memory
   float* w = a.weights + (size_t)bh * a.ly.ns;
+  const bool quads = (a.ly.ns & 3) == 0; // rows of weights begin on 16 bytes
   for (int t = tok_lo + 4 * tid; t < tok_hi; t += 4 * WARPS * 32) {      // all heads' logits of four tokens in flight
     float4 x[8];
     float s[4] = {0.f, 0.f, 0.f, 0.f};
@@ -124,11 +133,17 @@ __device__ __forceinline__ void dw_finish(const DwArgs& a, int bh, int G, int to
         s[2] = fmaf(ex2(x[h].z - M), inv, s[2]);
         s[3] = fmaf(ex2(x[h].w - M), inv, s[3]);
       }
+    // one addition per token: no order to depend on, nothing to wait for
+    if (quads && t + 4 <= tok_hi) {
+      asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};\n" ::"l"(w + t), "f"(s[0]), "f"(s[1]), "f"(s[2]), "f"(s[3]) : "memory");
+    } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (t + i < tok_hi) atomicAdd(&w[t + i], s[i]);           // one addition per token: no order to depend on, nothing to wait for
+      for (int i = 0; i < 4; ++i)
+        if (t + i < tok_hi) atomicAdd(&w[t + i], s[i]);
+    }
   }
-  cluster.sync();                        // nobody leaves while another may still read its shared memory
+  __syncwarp();
+  cluster.barrier_wait();                // nobody leaves while another may still read its shared memory
 }
 
 __device__ __forceinline__ void dw_cp16_zf(uint32_t saddr, const void* gptr, bool valid) {
@@ -160,6 +175,7 @@ decode_weights16_kernel(const __grid_constant__ DwArgs a) {
   const int tok_lo = lo * 32, tok_hi = min(n, hi * 32);
   float* lg = a.logits ? a.logits + (size_t)bh * G * a.n32 + tok_lo : reinterpret_cast<float*>(smem + DW16_WARPS * DW16_STAGES * TILE);
   const size_t lstride = a.logits ? (size_t)a.n32 : (size_t)((a.n32 / 32 + C - 1) / C * 32);
+  cg::this_cluster().barrier_arrive();   // waited for before the first access to another CTA's shared memory
   chain_enter();
 
   const uint32_t wsm = smem_u32(smem + warp * (DW16_STAGES * TILE));
@@ -351,6 +367,7 @@ decode_weights_packed_kernel(const __grid_constant__ DwArgs a) {
   const int tok_lo = lo * 32, tok_hi = hi * 32;                 // n is a multiple of 32
   float* lg_out = a.logits ? a.logits + (size_t)bh * G * a.n32 + tok_lo : reinterpret_cast<float*>(smem + L::SMEM_ALL - DW_LOGIT_BYTES);
   const size_t lstride = a.logits ? (size_t)a.n32 : (size_t)((a.n32 / 32 + C - 1) / C * 32);
+  cg::this_cluster().barrier_arrive();   // waited for before the first access to another CTA's shared memory
   chain_enter();
 
   const uint32_t wsm = smem_u32(smem + warp * L::WARP_BYTES), sP = wsm + L::STAGES * L::BYTES;
