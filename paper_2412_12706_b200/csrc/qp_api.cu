@@ -698,10 +698,8 @@ qp_status qp_heavy_select(const float* weights, int batch, int n_kv_heads, int L
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   cache_written(st);
   const int BH = batch * n_kv_heads;
-  if (launch_heavy_topk(weights, BH, L, w, n_keep, kept_idx, st) != cudaSuccess) return QP_ERR_CUDA;
-  if (!kept_weights && !kept_pos) return QP_OK;
-  return launch_kept_state(weights, kept_idx, BH, L, n_keep, n_cap, kept_weights, kept_pos, st) == cudaSuccess ? QP_OK
-                                                                                                              : QP_ERR_CUDA;
+  return launch_heavy_topk(weights, BH, L, w, n_keep, n_cap, kept_idx, kept_weights, kept_pos, st) == cudaSuccess ? QP_OK
+                                                                                                                  : QP_ERR_CUDA;
 }
 
 size_t qp_decode_weights_workspace_bytes(const qp_cache* cache) {

@@ -242,9 +242,8 @@ cudaError_t launch_prompt_weights(const void* Q, const void* K, const PromptDims
 size_t decode_weights_workspace(const DecDims& d, int n_cap);
 cudaError_t launch_decode_weights(const DecLayer& ly, const DecDims& d, float* weights, void* ws, cudaStream_t st);
 // selection over the first L - w of every head's L weights, see launch_select_topk
-cudaError_t launch_heavy_topk(const float* weights, int BH, int L, int w, int n_keep, int32_t* kept, cudaStream_t st);
-cudaError_t launch_kept_state(const float* weights, const int32_t* kept, int BH, int L, int n, int cap, float* kw, int32_t* kp,
-                              cudaStream_t st);
+cudaError_t launch_heavy_topk(const float* weights, int BH, int L, int w, int n_keep, int cap, int32_t* kept, float* kept_weights,
+                              int32_t* kept_pos, cudaStream_t st);
 struct EvictArgs {
   const uint16_t *k_new, *v_new;
   void *kc, *vc;

@@ -1,30 +1,9 @@
-// The two forms of the eviction by accumulated attention weight: the state of a cache after a prompt's selection, and the
-// replacement of one token per step.
+// Eviction by accumulated attention weight, one token per step (the prompt's form is a selection: qp_topk.cu).
 #include "qp_common.cuh"
 
 namespace qp {
 
 namespace {
-
-// state of a cache filled with the kept tokens: their weights and positions, zero behind them
-__global__ void __launch_bounds__(256)
-kept_state_kernel(const float* __restrict__ weights, const int32_t* __restrict__ kept, int L, int n, int cap,
-                  float* __restrict__ kw, int32_t* __restrict__ kp) {
-  chain_enter();
-  const int bh = blockIdx.y, i0 = blockIdx.x * 1024 + threadIdx.x;
-  int src[4];
-  float v[4];
-#pragma unroll
-  for (int k = 0; k < 4; ++k) src[k] = i0 + 256 * k < n ? kept[(size_t)bh * n + i0 + 256 * k] : 0;
-#pragma unroll
-  for (int k = 0; k < 4; ++k) v[k] = kw && i0 + 256 * k < n ? weights[(size_t)bh * L + src[k]] : 0.f;
-#pragma unroll
-  for (int k = 0; k < 4; ++k)
-    if (i0 + 256 * k < cap) {
-      if (kw) kw[(size_t)bh * cap + i0 + 256 * k] = v[k];
-      if (kp) kp[(size_t)bh * cap + i0 + 256 * k] = src[k];
-    }
-}
 
 // monotone map float -> uint32 (larger float = larger integer); -0 as +0
 __device__ __forceinline__ uint32_t order_image(float f) {
@@ -160,11 +139,6 @@ evict_kernel(const __grid_constant__ EvictArgs a) {
 }
 
 }  // namespace
-
-cudaError_t launch_kept_state(const float* weights, const int32_t* kept, int BH, int L, int n, int cap, float* kw, int32_t* kp,
-                              cudaStream_t st) {
-  return launch_chained(kept_state_kernel, dim3((cap + 1023) / 1024, BH), dim3(256), 0, st, weights, kept, L, n, cap, kw, kp);
-}
 
 cudaError_t launch_evict(const EvictArgs& a, int BH, cudaStream_t st) {
   return launch_chained(evict_kernel, dim3(BH), dim3(EV_THREADS), 0, st, a);

@@ -666,8 +666,7 @@ def heavy_select(weights: torch.Tensor, w: int, n_keep_: int, n_cap: int = 0):
     _dev(weights, torch.float32, (Bt, Hkv, L))
     cap = n_cap or n_keep_
     kept = torch.empty((Bt, Hkv, n_keep_), dtype=torch.int32, device=weights.device)
-    kw = torch.empty((Bt, Hkv, cap), dtype=torch.float32, device=weights.device)
-    kp = torch.empty((Bt, Hkv, cap), dtype=torch.int32, device=weights.device)
+    kw, kp = weights.new_empty((Bt, Hkv, cap)), kept.new_empty((Bt, Hkv, cap))
     _check(lib().qp_heavy_select(_ptr(weights), Bt, Hkv, L, w, n_keep_, cap, _ptr(kept), _ptr(kw), _ptr(kp), _stream()),
            "qp_heavy_select")
     return kept, kw, kp
