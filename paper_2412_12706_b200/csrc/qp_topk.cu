@@ -73,11 +73,12 @@ topk_kernel(const float* __restrict__ scores, int L, int w, int BH, const __grid
   const int bh = blockIdx.x % BH, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const float* s = scores + (size_t)blockIdx.x * o.ld;
   int32_t* out = o.kept[layer] + (size_t)bh * n_keep;
+  auto put = [&](unsigned i, int j) { topk_put(o, out, s, bh, i, j); };
 
   topk_pad(o, bh);
-  for (int i = tid; i < w; i += TK_THREADS) topk_put(o, out, s, bh, k + i, P + i);   // window tokens are always kept
+  for (int i = tid; i < w; i += TK_THREADS) put(k + i, P + i);   // window tokens are always kept
   if (k >= P) {                                                    // keep everything
-    for (int j = tid; j < P; j += TK_THREADS) topk_put(o, out, s, bh, j, j);
+    for (int j = tid; j < P; j += TK_THREADS) put(j, j);
     return;
   }
 
@@ -175,8 +176,7 @@ topk_kernel(const float* __restrict__ scores, int L, int w, int BH, const __grid
       const unsigned tot_g = __shfl_sync(0xffffffffu, sg, 31), tot_e = __shfl_sync(0xffffffffu, se, 31);
       const unsigned pre_g = __shfl_sync(0xffffffffu, sg - wg, warp), pre_e = __shfl_sync(0xffffffffu, se - we, warp);
       const unsigned pg = run_g + pre_g + __popc(bg & lt_mask), pe = run_e + pre_e + __popc(be & lt_mask);
-      if ((gt || (eq && pe < need)) && QP_IN_RANGE(pg + min(pe, need), k, QP_SITE_TOPK_OUT))
-        topk_put(o, out, s, bh, pg + min(pe, need), j);
+      if ((gt || (eq && pe < need)) && QP_IN_RANGE(pg + min(pe, need), k, QP_SITE_TOPK_OUT)) put(pg + min(pe, need), j);
       run_g += tot_g;
       run_e += tot_e;
       __syncthreads();                                      // warp_gt / warp_eq are rewritten by the next chunk
@@ -197,11 +197,12 @@ topk_reg_kernel(const float* __restrict__ scores, int L, int w, int BH, const __
   const int bh = blockIdx.x % BH, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const float* s = scores + (size_t)blockIdx.x * o.ld;
   int32_t* out = o.kept[layer] + (size_t)bh * n_keep;
+  auto put = [&](unsigned i, int j) { topk_put(o, out, s, bh, i, j); };
 
   topk_pad(o, bh);
-  for (int i = tid; i < w; i += TK_THREADS) topk_put(o, out, s, bh, k + i, P + i);   // window tokens are always kept
+  for (int i = tid; i < w; i += TK_THREADS) put(k + i, P + i);   // window tokens are always kept
   if (k >= P) {                                                    // keep everything
-    for (int j = tid; j < P; j += TK_THREADS) topk_put(o, out, s, bh, j, j);
+    for (int j = tid; j < P; j += TK_THREADS) put(j, j);
     return;
   }
 
@@ -319,8 +320,7 @@ topk_reg_kernel(const float* __restrict__ scores, int L, int w, int BH, const __
     const unsigned bg = __ballot_sync(0xffffffffu, gt), be = __ballot_sync(0xffffffffu, eq);
     const unsigned pg = row_g[q] + cnt_g[q][warp] + __popc(bg & lt_mask);
     const unsigned pe = row_e[q] + cnt_e[q][warp] + __popc(be & lt_mask);
-    if ((gt || (eq && pe < need)) && QP_IN_RANGE(pg + min(pe, need), k, QP_SITE_TOPK_OUT))
-        topk_put(o, out, s, bh, pg + min(pe, need), j);
+    if ((gt || (eq && pe < need)) && QP_IN_RANGE(pg + min(pe, need), k, QP_SITE_TOPK_OUT)) put(pg + min(pe, need), j);
   }
 }
 
@@ -344,12 +344,13 @@ topk_cluster_kernel(const float* __restrict__ scores, int L, int w, int BH, cons
   const int bh = head % BH, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const float* s = scores + (size_t)head * o.ld;
   int32_t* out = o.kept[layer] + (size_t)bh * n_keep;
+  auto put = [&](unsigned i, int j) { topk_put(o, out, s, bh, i, j); };
 
   if (crank == 0) topk_pad(o, bh);
   if (crank == 0)
-    for (int i = tid; i < w; i += TK_THREADS) topk_put(o, out, s, bh, k + i, P + i);  // window tokens are always kept
+    for (int i = tid; i < w; i += TK_THREADS) put(k + i, P + i);  // window tokens are always kept
   if (k >= P) {                                                    // keep everything (the whole cluster leaves)
-    for (int j = crank * TK_THREADS + tid; j < P; j += CTAS * TK_THREADS) topk_put(o, out, s, bh, j, j);
+    for (int j = crank * TK_THREADS + tid; j < P; j += CTAS * TK_THREADS) put(j, j);
     return;
   }
 
@@ -510,8 +511,7 @@ topk_cluster_kernel(const float* __restrict__ scores, int L, int w, int BH, cons
     const unsigned bg = __ballot_sync(0xffffffffu, gt), be = __ballot_sync(0xffffffffu, eq);
     const unsigned pg = base_g + row_g[q] + cnt_g[q][warp] + __popc(bg & lt_mask);
     const unsigned pe = base_e + row_e[q] + cnt_e[q][warp] + __popc(be & lt_mask);
-    if ((gt || (eq && pe < need)) && QP_IN_RANGE(pg + min(pe, need), k, QP_SITE_TOPK_OUT))
-      topk_put(o, out, s, bh, pg + min(pe, need), seg0 + i);
+    if ((gt || (eq && pe < need)) && QP_IN_RANGE(pg + min(pe, need), k, QP_SITE_TOPK_OUT)) put(pg + min(pe, need), seg0 + i);
   }
   cluster.sync();                                                // no CTA leaves while another may still read its totals
 }
