@@ -19,6 +19,10 @@
 // Tiles above the diagonal are skipped, for each group on its own.  The work of all quads of resident tiles, end to end, is cut
 // into one run per SM (see Plan); a quad that several runs share leaves partial results, which two small kernels add in a fixed
 // order.
+//
+// Measured in a replayed graph: 8192 tokens of 32 heads over 8 (D = 128) 0.56 ms = 0.98 PFLOP/s of products, the exponential unit
+// 73 to 76 % busy, the tensor pipe 53 to 56 %, at the GPU's power limit; 1999 queries behind 14301 keys, 64 heads over 8, 1.07 ms;
+// 1024 tokens of 8 heads over 2 (D = 64) 19 us, four launches one after another.
 #include <algorithm>
 
 #include "qp_mma.cuh"
@@ -215,10 +219,11 @@ prompt_sweep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
   const uint32_t tmem_base = tmem_base_slot;
   // This block's part of a quad, and the walk over them: every warp does it for itself.
   struct Part {
-    int bh, quad, b, hk, step0, n_loc, t0;                // n_loc 0: none of the quad's steps;  t0: sweep 2, first query tile of a head
+    int bh, quad, b, hk, step0, n_loc;
+    int t0;                                               // sweep 2: first query tile of a head
     long long first;                                      // the quad's place
   };
-  Part part{bh0, s_quad - 1, 0, 0, 0, 0, 0, s_first};
+  Part part{bh0, s_quad - 1, 0, 0, 0, 0, 0, s_first};     // (before the first)
   auto next_part = [&]() {                                // false: the run is done
     do {
       if (part.quad >= 0 && part.quad + 1 == p.nquads) {

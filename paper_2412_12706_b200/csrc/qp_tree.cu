@@ -22,6 +22,11 @@
 // SMs idle, several smaller ones share a (KV head, row group) and a small kernel merges what they leave in the workspace.
 // Order of additions fixed; every mbarrier wait bounded (see the score sweeps).
 //
+// Measured in a replayed graph (32 heads over 8): 8 drafts on 2048 tokens at 4 bit 12.0 us, mostly latencies one after another; 64
+// on 8192 at 16 bit 26.9 us, of which the exchange of 128 KB per block (14 bytes a clock through distributed shared memory) is
+// 4; 33 on 8 x 8192 at 2 bit 86 us = 0.41 PFLOP/s: a tile of two row tiles reads and writes 256 KB of shared memory at 128 bytes
+// a clock, and the second row tile holds four rows.
+//
 // Types: 16-bit caches multiply in bf16; packed ones in fp16 (2^-11 on a reconstructed value, against 2^-8 in bf16), tail,
 // drafts and queries converted (exact but for |x| below 2^-14, off by at most 2^-25, or above 65504).  Logits, maxima, sums
 // and O in 32 bits; the softmax weights enter the second product in 16 bits like its values.
