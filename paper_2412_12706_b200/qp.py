@@ -158,12 +158,13 @@ def _check(status: int, where: str) -> None:
 
 # the handle of torch's current stream without building a Stream object (3 us, as much as a launch)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream() -> int:
     if _raw_stream is None:
         return torch.cuda.current_stream().cuda_stream
-    return _raw_stream(torch.cuda.current_device())
+    return _raw_stream(_current_device())
 
 
 def _ptr(t: torch.Tensor | None) -> int | None:
@@ -623,12 +624,12 @@ def decode_tree_workspace_bytes(cache: "Cache | qp_cache", T: int) -> int:
 
 def _dev(t: torch.Tensor, dtype: torch.dtype, shape: tuple) -> None:
     """Contiguous, of this type and shape, and on the device the kernels are launched on."""
-    assert t.is_cuda and t.dtype is dtype and t.shape == shape and t.is_contiguous(), (t.dtype, t.shape, shape)
-    assert t.get_device() == torch._C._cuda_getDevice(), "not on the current device"
+    assert (t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.is_cuda
+            and t.get_device() == _current_device()), (t.device, t.dtype, t.shape, shape)
 
 
 def _dev_cache(cache: Cache) -> None:
-    assert cache.k_codes.get_device() == torch._C._cuda_getDevice(), "cache not on the current device"
+    assert cache.k_codes.get_device() == _current_device(), "cache not on the current device"
 
 
 def _ref(strategy: "Strategy | None"):
