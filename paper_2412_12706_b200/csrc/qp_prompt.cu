@@ -451,6 +451,8 @@ __device__ __forceinline__ int quad_parts(int pass, const Plan& p, int bh, int q
 }
 
 // -lse of every row from the parts' (reference, sum) pairs, -inf for the padding rows of a head's last tile
+// A launch of its own: a warp of sweep 2 that forms them for every streamed tile saves it, but is a chain of two reads and a loop
+// per step (1024 tokens of 8 heads over 2: 19.4 -> 22.0 us, 8192 of 32 over 8: 565 -> 645 us).
 __global__ void __launch_bounds__(256)
 prompt_lse_kernel(const Plan p, const float2* __restrict__ stats, float* __restrict__ neg_lse) {
   const int i = blockIdx.x * 256 + threadIdx.x, bq = blockIdx.y, b = bq / p.Hq, hq = bq % p.Hq, h = hq % p.G;
