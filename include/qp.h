@@ -415,8 +415,8 @@ qp_status qp_evict_kv(const void* k_new, const void* v_new, qp_cache* cache /* h
  * drafts and tail included, are multiplied in fp16 (|x| <= 65504).  What a draft holds, numbers or not, reaches only the rows
  * that see it (the drafts behind the last of a smaller tree of the batch may hold anything).  Plain stream order.  The workspace
  * begins with W * max(1, min(16, 148 / W)) 32-bit error words, W = batch * n_kv_heads * ceil(T G / 256), set by every call: one
- * that is not 0 says that a bounded wait ran out (see qp_window_scores) and the output is invalid.  They are 0 in every correct
- * run.
+ * that is not 0 says that a bounded wait ran out (see qp_window_scores); the outputs that hang on it, up to 256 rows of one KV
+ * head, are NaN.  They are 0 in every correct run.
  */
 #define QP_MAX_DRAFTS 64
 size_t qp_decode_tree_workspace_bytes(const qp_cache* cache /* host */, int T);
@@ -436,6 +436,13 @@ qp_status qp_decode_attn_tree(const void* q, int T, const qp_cache* cache /* hos
  * both builds.  The normal build returns QP_ERR_UNSUPPORTED and zeros.
  */
 qp_status qp_debug_check(uint32_t* words4 /* host, out */);
+
+/*
+ * Debug build only: from now on thread block `block` of every qp_decode_attn_tree launch on the current device reports, after its
+ * work is done and all its waits have returned, that a bounded wait ran out; -1: none does.  For tests of what is made of such a
+ * block.  Synchronises like a cudaMemcpy.  The normal build returns QP_ERR_UNSUPPORTED.
+ */
+qp_status qp_debug_give_up(int block);
 
 /*
  * Decode attention without any caller-supplied scratch.  (The paper has no counterpart to this

@@ -555,6 +555,7 @@ namespace qp {
 cudaError_t quant_check_read(unsigned int (&out)[4]);
 cudaError_t decode_check_read(unsigned int (&out)[4]);
 cudaError_t topk_check_read(unsigned int (&out)[4]);
+cudaError_t tree_give_up(int block);
 }
 extern "C" {
 #endif
@@ -571,6 +572,15 @@ qp_status qp_debug_check(uint32_t* words4) {
   return QP_OK;
 #else
   words4[0] = words4[1] = words4[2] = words4[3] = 0u;
+  return QP_ERR_UNSUPPORTED;
+#endif
+}
+
+qp_status qp_debug_give_up(int block) {
+  if (block < -1) return QP_ERR_INVALID_ARG;
+#ifdef QP_CHECKED
+  return qp::tree_give_up(block) == cudaSuccess ? QP_OK : QP_ERR_CUDA;
+#else
   return QP_ERR_UNSUPPORTED;
 #endif
 }

@@ -313,6 +313,10 @@ __device__ __forceinline__ void add_bad(unsigned char* part, int r, unsigned lon
   }
 }
 
+#ifdef QP_CHECKED
+__device__ int g_give_up = -1;                                  // see qp_debug_give_up
+#endif
+
 template <int BITS, int D>
 __global__ void __launch_bounds__(TR_THREADS, 1)
 tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
@@ -706,6 +710,10 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
   asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
   __syncthreads();                                              // every product is done: ring and queries are idle
   asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+#ifdef QP_CHECKED
+  if (tid == 0 && (int)blockIdx.x == g_give_up) give_up = 1;    // (every wait of the block has returned)
+  __syncthreads();
+#endif
   constexpr uint32_t PART = 128 * D * 4;                        // one stream's O; the statistics [2][128] follow the two
   unsigned char* part_base = smem_raw + (sbase - smem_u32(smem_raw));
   float2* s_ml = reinterpret_cast<float2*>(part_base + 2 * PART);
@@ -713,7 +721,9 @@ tree_kernel(const __grid_constant__ TreeLaunch p, const __grid_constant__ CUtens
     const int u = warp >> 2, rl = (warp & 3) * 32 + lane;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const bool any = !give_up && stream_tiles(u) > 0 && (p.two_rows ? u * 128 : 0) + (warp & 3) * 32 < rows;
-    s_ml[u * 128 + rl] = make_float2(any ? m_run : -INFINITY, l_run);
+    // What the block lost, because a wait ran out, must not look like a run in which nothing was seen: with a reference that counts
+    // and a sum that is no number the row's output is NaN, whatever the partial O holds.
+    s_ml[u * 128 + rl] = give_up ? make_float2(0.f, NAN) : make_float2(any ? m_run : -INFINITY, l_run);
     if (any) {
 #pragma unroll 1
       for (int c0 = 0; c0 < D; c0 += 32) {
@@ -976,6 +986,10 @@ cudaError_t launch_tree_t(TreeLaunch p, const CUtensorMap& mk, const CUtensorMap
 }  // namespace
 
 size_t tree_workspace(const TreeArgs& a) { return tree_carve(a).total; }
+
+#ifdef QP_CHECKED
+cudaError_t tree_give_up(int block) { return cudaMemcpyToSymbol(g_give_up, &block, sizeof(block)); }
+#endif
 
 cudaError_t launch_tree(const TreeArgs& a, void* ws, cudaStream_t st) {
   int* err = static_cast<int*>(ws);

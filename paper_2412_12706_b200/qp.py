@@ -30,7 +30,7 @@ EXPORTS = ["qp_status_string", "qp_n_keep", "qp_cache_layout", "qp_compress_work
            "qp_decode_attn_tail_layers", "qp_compress_layers", "qp_decode_overlap", "qp_gather_quantize_ex",
            "qp_decode_attn_ex", "qp_decode_attn_layers_ex", "qp_head_budgets", "qp_head_budgets_workspace_bytes", "qp_debug_check",
            "qp_prompt_weights", "qp_prompt_weights_workspace_bytes", "qp_heavy_select", "qp_decode_attn_weights",
-           "qp_decode_weights_workspace_bytes", "qp_evict_kv", "qp_decode_attn_tree", "qp_decode_tree_workspace_bytes"]
+           "qp_decode_weights_workspace_bytes", "qp_evict_kv", "qp_decode_attn_tree", "qp_decode_tree_workspace_bytes", "qp_debug_give_up"]
 
 
 class QpError(RuntimeError):
@@ -129,6 +129,8 @@ def lib() -> ctypes.CDLL:
         L.qp_head_budgets.argtypes = [p, i, i, i, i, i, i, p, p, sz, p]
         L.qp_debug_check.restype = i
         L.qp_debug_check.argtypes = [ctypes.POINTER(ctypes.c_uint32)]
+        L.qp_debug_give_up.restype = i
+        L.qp_debug_give_up.argtypes = [i]
         L.qp_decode_overlap.restype = i
         L.qp_decode_overlap.argtypes = [p, i]
         L.qp_prompt_weights_workspace_bytes.restype = sz
@@ -798,6 +800,11 @@ def debug_check() -> tuple[int, list[int]]:
     return st, list(w)
 
 
+def debug_give_up(block: int) -> int:
+    """qp_debug_give_up: the status; QP_ERR_UNSUPPORTED (2) unless the loaded library is the range-checked build."""
+    return lib().qp_debug_give_up(block)
+
+
 # the C entry points under their own names
 qp_status_string = status_string
 qp_n_keep = n_keep
@@ -816,6 +823,7 @@ qp_decode_overlap = decode_overlap
 qp_gather_quantize_ex = gather_quantize_ex
 qp_decode_attn_ex = decode_attn_ex
 qp_debug_check = debug_check
+qp_debug_give_up = debug_give_up
 qp_decode_attn_layers_ex = decode_attn_layers_ex
 qp_head_budgets = head_budgets
 qp_head_budgets_workspace_bytes = lambda *a: int(lib().qp_head_budgets_workspace_bytes(*a))
