@@ -390,6 +390,9 @@ prompt_sweep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
             const int key0 = 128 * (4 * part.quad + g);
             rows = p.nq - 128 * t;                      // (what lies behind a head's last row is the next head's, and may hold anything)
             all = key0 + 127 <= p.q_start + 128 * t && rows >= 128;
+            // a query that is not finite has no normaliser: its tile takes the other path, because the polynomial clamps NaN away
+            const float4 l = *reinterpret_cast<const float4*>(&s_lse[st][4 * lane]);
+            all = all && __all_sync(0xffffffffu, fabsf(l.x + l.y + l.z + l.w) < INFINITY);
             lim = key0 + rloc - p.q_start - 128 * t;
           }
           auto fold = [&](const uint32_t (&r)[32], int c0) {

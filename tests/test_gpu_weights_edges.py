@@ -102,3 +102,22 @@ def test_output_is_the_mean_of_the_values_under_the_weights_it_adds(bits, g, D, 
     tol = 2.0 ** -8 * ref.abs() + (2.0 ** -10 * (1 + 2.0 ** -10) + 2.0 ** -19) * terms + 2 * n * 2.0 ** -35 * top_scale * largest + 1e-30
     worst = float(((out - ref).abs() / tol).max())
     assert worst <= 1, worst
+
+
+# ---------------------------------------------------------------------------------------------- queries that are not numbers
+
+@pytest.mark.parametrize("poison", [float("nan"), float("inf")])
+@pytest.mark.parametrize("rows", [(1, 130, 259, 388, 517, 646, 775, 896), (640,), (641,), (642,), (643,), (1022,), (1023,)])
+@pytest.mark.parametrize("Hq,Hkv,D", [(8, 2, 128), (3, 3, 64)])
+def test_a_query_that_is_not_finite_shows_in_every_key_it_sees(Hq, Hkv, D, rows, poison):
+    """Whatever its row number: its softmax has no value, so neither have the weights up to its position; those behind do not change."""
+    Bt, L = 2, 1024
+    Q, K = randn((Bt, Hq, L, D), 1, 1.5), randn((Bt, Hkv, L, D), 2, 1.5)
+    ref = qp.prompt_weights(Q, K)
+    h = Hq - 1                                             # one query head of the last KV head, second batch entry
+    Q[1, h, list(rows)] = poison
+    got = qp.prompt_weights(Q, K)
+    last = max(rows)
+    assert torch.isnan(got[1, Hkv - 1, :last + 1]).all()
+    assert torch.equal(got[1, Hkv - 1, last + 1:], ref[1, Hkv - 1, last + 1:])
+    assert torch.equal(got[0], ref[0]) and torch.equal(got[1, :Hkv - 1], ref[1, :Hkv - 1])
