@@ -113,6 +113,7 @@ void cache_written(cudaStream_t st) {
 }
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 inline bool pow2_bits(int b) { return b == 2 || b == 4 || b == 8 || b == 16; }
 inline bool ok_group(int g) { return g == 32 || g == 64 || g == 128; }
 
@@ -704,6 +705,7 @@ qp_status qp_heavy_select(const float* weights, int batch, int n_kv_heads, int L
                           int32_t* kept_idx, float* kept_weights, int32_t* kept_pos, void* stream) {
   if (!weights || !kept_idx || batch < 1 || n_kv_heads < 1 || w < 1 || w >= L) return QP_ERR_INVALID_ARG;
   if (n_keep <= w || n_keep > L || n_cap < n_keep) return QP_ERR_BUDGET;
+  if (!aligned4(weights) || !aligned4(kept_idx) || !aligned4(kept_weights) || !aligned4(kept_pos)) return QP_ERR_ALIGNMENT;
   if ((long long)batch * n_kv_heads > 65535) return QP_ERR_UNSUPPORTED;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   cache_written(st);
@@ -745,7 +747,7 @@ qp_status qp_evict_kv(const void* k_new, const void* v_new, qp_cache* cache, con
   if (s != QP_OK) return s;
   s = check_token_strategy(strategy, cache);
   if (s != QP_OK) return s;
-  if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(weights) || !aligned16(pos)) return QP_ERR_ALIGNMENT;
+  if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(weights) || !aligned16(pos) || !aligned4(slots)) return QP_ERR_ALIGNMENT;
   const qp_cache& c = *cache;
   const int ns = cache_capacity(c);
   const bool grow = c.bits == 16 && c.n_keep < ns;
