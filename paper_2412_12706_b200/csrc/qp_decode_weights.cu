@@ -681,20 +681,8 @@ cudaError_t launch_dw(K kernel, int warps, int warp_tokens, size_t smem, DwArgs 
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  if (active[dev][0] == 0) {                                    // once per device: what fits
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    if (e != cudaSuccess) return e;
-    for (int c = 1; c <= DW_MAX_CLUSTER; ++c) {
-      int n = 0;
-      cfg.gridDim = dim3(c);
-      attr[0].val.clusterDim.x = c;
-      cfg.numAttrs = 1;
-      e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
-      if (e != cudaSuccess) return e;
-      active[dev][c] = n;
-    }
-    active[dev][0] = 1;
-  }
+  e = clusters_that_fit(kernel, cfg, DW_MAX_CLUSTER, active[dev]);
+  if (e != cudaSuccess) return e;
   const int tiles = a.n32 / 32;
   double best = 1e300;
   a.cluster = 1;

@@ -939,20 +939,8 @@ cudaError_t launch_tree_t(TreeLaunch p, const CUtensorMap& mk, const CUtensorMap
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  if (active[dev][0] == 0) {                                    // once per device: how many clusters of a size fit at once
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    if (e != cudaSuccess) return e;
-    for (int c = 1; c <= TR_MAX_CLUSTER; ++c) {
-      int n = 0;
-      cfg.gridDim = dim3(c);
-      attr[0].val.clusterDim.x = c;
-      cfg.numAttrs = 1;
-      e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
-      if (e != cudaSuccess) return e;
-      active[dev][c] = n;
-    }
-    active[dev][0] = 1;
-  }
+  e = clusters_that_fit(kernel, cfg, TR_MAX_CLUSTER, active[dev]);
+  if (e != cudaSuccess) return e;
   if (BITS == 16) {
     p.slots = p.two_rows ? 5 : 6;
   } else {                                                      // the least the order of the products needs; raw stages from the rest

@@ -1,5 +1,8 @@
 """Accumulated attention weights at the edges of their ranges: small and large values, queries that are not numbers, host threads."""
 import math
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -121,3 +124,55 @@ def test_a_query_that_is_not_finite_shows_in_every_key_it_sees(Hq, Hkv, D, rows,
     assert torch.isnan(got[1, Hkv - 1, :last + 1]).all()
     assert torch.equal(got[1, Hkv - 1, last + 1:], ref[1, Hkv - 1, last + 1:])
     assert torch.equal(got[0], ref[0]) and torch.equal(got[1, :Hkv - 1], ref[1, :Hkv - 1])
+
+
+# ---------------------------------------------------------------------------------------------- host threads
+
+THREADS = """
+import threading
+import torch
+from paper_2412_12706_b200 import qp
+from tests.test_gpu_tree import make_cache, mask_of, random_tree
+from tests.test_gpu_weights import per_token_cache, randn
+Bt, Hq, Hkv, D, n, T, N = 1, 8, 2, 128, 2048, 12, 6
+caches = [per_token_cache(Bt, Hq, Hkv, D, n, n, bits, 32)[:2] for bits in (2, 4, 8, 16)]
+q, qt, kd, vd = randn((Bt, Hq, D), 1), randn((Bt, T, Hq, D), 2), randn((Bt, T, Hkv, D), 3), randn((Bt, T, Hkv, D), 4)
+mask = mask_of(random_tree(Bt, T, 5)[1])
+Q, K = randn((Bt, Hq, 900, D), 6), randn((Bt, Hkv, 900, D), 7)
+torch.cuda.synchronize()
+gate, got, failed = threading.Barrier(N), [None] * N, []
+
+def calls():
+    out = []
+    for c, st in caches:
+        w = torch.zeros((Bt, Hkv, n), device="cuda")
+        out += [qp.decode_attn_weights(q, c, w, st), w, qp.decode_attn_tree(qt, c, kd, vd, mask, strategy=st)]
+    a = qp.prompt_weights(Q, K)
+    return out + [a, *qp.heavy_select(a, 8, 128)]
+
+def work(i):
+    try:
+        with torch.cuda.stream(torch.cuda.Stream()):
+            gate.wait()
+            got[i] = calls()
+            torch.cuda.current_stream().synchronize()
+    except Exception as e:
+        failed.append(e)
+
+threads = [threading.Thread(target=work, args=(i,)) for i in range(N)]
+for t in threads: t.start()
+for t in threads: t.join()
+assert not failed, failed
+ref = calls()
+for g in got:
+    for a, b in zip(g, ref):
+        assert torch.equal(a, b)
+print("same")
+"""
+
+
+def test_first_calls_of_several_host_threads_at_once():
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    for _ in range(3):
+        r = subprocess.run([sys.executable, "-c", THREADS], capture_output=True, text=True, timeout=300, cwd=root)
+        assert r.returncode == 0 and r.stdout.strip() == "same", r.stderr[-2000:]
