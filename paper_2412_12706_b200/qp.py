@@ -630,6 +630,12 @@ def _dev(t: torch.Tensor, dtype: torch.dtype, shape: tuple) -> None:
             and t.get_device() == _current_device()), (t.device, t.dtype, t.shape, shape)
 
 
+def _scratch(t: torch.Tensor) -> tuple:
+    """Address and bytes of a workspace: contiguous, of any type, and on the device the kernels are launched on."""
+    assert t.get_device() == _current_device() and t.is_contiguous(), (t.device, t.shape)
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
 def _dev_cache(cache: Cache) -> None:
     assert cache.k_codes.get_device() == _current_device(), "cache not on the current device"
 
@@ -658,7 +664,7 @@ def prompt_weights(Q: torch.Tensor, K: torch.Tensor, q_start: int = 0, weights: 
         workspace = torch.empty(max(16, prompt_weights_workspace_bytes(Bt, Hq, Hkv, D, L, q_start, nq)), dtype=torch.uint8,
                                 device=K.device)
     _check(lib().qp_prompt_weights(_ptr(Q), _ptr(K), Bt, Hq, Hkv, D, L, q_start, nq, 1 if accumulate else 0, _ptr(weights),
-                                   _ptr(workspace), workspace.numel(), _stream()), "qp_prompt_weights")
+                                   *_scratch(workspace), _stream()), "qp_prompt_weights")
     return weights
 
 
@@ -689,8 +695,8 @@ def decode_attn_weights(q: torch.Tensor, cache: Cache, weights: torch.Tensor, st
         _dev(out, torch.bfloat16, q.shape)
     if workspace is None:
         workspace = new_decode_workspace(decode_weights_workspace_bytes(cache), q.device)
-    _check(lib().qp_decode_attn_weights(_ptr(q), ctypes.byref(d), _ref(strategy), _ptr(weights), _ptr(out), _ptr(workspace),
-                                        workspace.numel(), _stream()), "qp_decode_attn_weights")
+    _check(lib().qp_decode_attn_weights(_ptr(q), ctypes.byref(d), _ref(strategy), _ptr(weights), _ptr(out), *_scratch(workspace),
+                                        _stream()), "qp_decode_attn_weights")
     return out
 
 
@@ -787,8 +793,8 @@ def decode_attn_tree(q: torch.Tensor, cache: Cache, k_draft: torch.Tensor, v_dra
     if workspace is None:
         workspace = new_decode_workspace(decode_tree_workspace_bytes(cache, T), q.device)
     _check(lib().qp_decode_attn_tree(_ptr(q), T, ctypes.byref(d), _ref(strategy), None if tail is None else ctypes.byref(tail.desc),
-                                     _ptr(k_draft), _ptr(v_draft), _ptr(mask), _ptr(out), _ptr(workspace), workspace.numel(),
-                                     _stream()), "qp_decode_attn_tree")
+                                     _ptr(k_draft), _ptr(v_draft), _ptr(mask), _ptr(out), *_scratch(workspace), _stream()),
+           "qp_decode_attn_tree")
     return out
 
 

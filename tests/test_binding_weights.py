@@ -1,0 +1,93 @@
+"""What the binding of the weight, eviction and tree calls refuses before the library is called.  No GPU: the tensors are stand-ins
+that say where they live, and the library one that writes down what it was asked for."""
+import math
+
+import pytest
+import torch
+
+from paper_2412_12706_b200 import qp
+
+
+class Tensor:
+    def __init__(self, shape, dtype=torch.bfloat16, device=0, contiguous=True):
+        self.shape, self.dtype, self.on, self.contiguous = torch.Size(shape), dtype, device, contiguous
+        self.is_cuda, self.device = device is not None, "cpu" if device is None else f"cuda:{device}"
+
+    def is_contiguous(self): return self.contiguous
+    def get_device(self): return -1 if self.on is None else self.on
+    def data_ptr(self): return 0x1000
+    def numel(self): return math.prod(self.shape)
+    def element_size(self): return self.dtype.itemsize
+
+
+class Library:
+    def __init__(self, real):
+        self.real, self.calls = real, []
+
+    def __getattr__(self, name):
+        if name.endswith("_bytes") or name.startswith("qp_cache_layout") or name in ("qp_status_string", "qp_n_keep"):
+            return getattr(self.real, name)
+
+        def call(*args):
+            self.calls.append((name, args))
+            return 0
+        return call
+
+
+Bt, Hq, Hkv, D, n, T, L = 1, 8, 2, 128, 64, 4, 256
+
+
+@pytest.fixture
+def library(monkeypatch):
+    from paper_2412_12706_b200 import build as qp_build
+    qp_build.build()
+    fake = Library(qp.lib())
+    monkeypatch.setattr(qp, "lib", lambda: fake)
+    monkeypatch.setattr(qp, "_current_device", lambda: 0)
+    monkeypatch.setattr(qp, "_stream", lambda: 0)
+    return fake
+
+
+def cache(bits=16, n_cap=0, device=0):
+    d = qp.cache_layout_cap(Bt, Hq, Hkv, D, bits, 32, n, n_cap)
+    return qp.Cache(d, Tensor((Bt, Hkv, n_cap or n, D), device=device), None, None, None, None, None)
+
+
+def tail(device=0, group=32, heads=Hkv):
+    t = qp.qp_tail()
+    t.n_tail = 3
+    return qp.Tail(t, Tensor((Bt, heads, group, D), device=device), Tensor((Bt, heads, group, D), device=device))
+
+
+def calls(ws_device=0, ws_dtype=torch.uint8, ws_bytes=1 << 26, contiguous=True, tree_tail=None, bits=16):
+    ws = Tensor((ws_bytes // ws_dtype.itemsize,), ws_dtype, ws_device, contiguous)
+    st = None
+    if bits < 16:
+        s = qp.qp_strategy()
+        s.k_axis = 1
+        st = qp.Strategy(s, [])
+    f = torch.float32
+    return dict(
+        prompt=lambda: qp.prompt_weights(Tensor((Bt, Hq, L, D)), Tensor((Bt, Hkv, L, D)), 0, Tensor((Bt, Hkv, L), f), ws),
+        decode=lambda: qp.decode_attn_weights(Tensor((Bt, Hq, D)), cache(bits), Tensor((Bt, Hkv, n), f), st, Tensor((Bt, Hq, D)), ws),
+        tree=lambda: qp.decode_attn_tree(Tensor((Bt, T, Hq, D)), cache(bits), Tensor((Bt, T, Hkv, D)), Tensor((Bt, T, Hkv, D)),
+                                         Tensor((Bt, T), torch.int64), tree_tail, None, Tensor((Bt, T, Hq, D)), ws))
+
+
+NAMES = ("prompt", "decode", "tree")
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_a_workspace_of_the_gpu_in_use_is_taken_with_all_its_bytes(library, name):
+    for dtype in (torch.uint8, torch.float32):                     # its size is counted in bytes, whatever it holds
+        library.calls.clear()
+        calls(ws_dtype=dtype)[name]()
+        assert len(library.calls) == 1 and 1 << 26 in library.calls[0][1]
+
+
+@pytest.mark.parametrize("name", NAMES)
+@pytest.mark.parametrize("bad", [dict(ws_device=None), dict(ws_device=1), dict(contiguous=False)])
+def test_a_workspace_elsewhere_is_refused(library, name, bad):
+    with pytest.raises(AssertionError):
+        calls(**bad)[name]()
+    assert not library.calls
