@@ -786,6 +786,9 @@ def decode_attn_tree(q: torch.Tensor, cache: Cache, k_draft: torch.Tensor, v_dra
         _dev(t, torch.bfloat16, (d.batch, T, d.n_kv_heads, d.head_dim))
     _dev(mask, torch.int64, (d.batch, T))
     _dev_cache(cache)
+    if tail is not None and d.bits < 16:
+        for t in (tail.k_tail, tail.v_tail):
+            _dev(t, torch.bfloat16, (d.batch, d.n_kv_heads, d.group, d.head_dim))
     if out is None:
         out = torch.empty_like(q)
     else:

@@ -91,3 +91,12 @@ def test_a_workspace_elsewhere_is_refused(library, name, bad):
     with pytest.raises(AssertionError):
         calls(**bad)[name]()
     assert not library.calls
+
+
+@pytest.mark.parametrize("bad", [dict(device=None), dict(device=1), dict(heads=1), dict(group=64)])
+def test_a_tail_of_another_device_or_cache_is_refused(library, bad):
+    calls(bits=4, tree_tail=tail())["tree"]()
+    assert len(library.calls) == 1
+    with pytest.raises(AssertionError):
+        calls(bits=4, tree_tail=tail(**bad))["tree"]()
+    assert len(library.calls) == 1
