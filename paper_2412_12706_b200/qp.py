@@ -752,7 +752,24 @@ def compress_layer_heavy(K: torch.Tensor, V: torch.Tensor, Q: torch.Tensor, budg
 
 def decode_step_heavy(q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, hc: HeavyCache, recent: int = 32,
                       out: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
-    """One generation step over a HeavyCache: qp_evict_kv, then qp_decode_attn_weights (the new token sees itself)."""
+    """One generation step over a HeavyCache: qp_evict_kv, then qp_decode_attn_weights (the new token sees itself).  A step that
+    is refused has changed nothing: what the second call asks for is looked at before the first takes the token in."""
+    d = hc.cache.desc
+    _dev(q, torch.bfloat16, (d.batch, d.n_q_heads, d.head_dim))
+    if out is None:
+        out = torch.empty_like(q)
+    else:
+        _dev(out, torch.bfloat16, q.shape)
+    need = decode_weights_workspace_bytes(hc.cache)
+    if workspace is None:
+        workspace = new_decode_workspace(need, q.device)
+    address, size = _scratch(workspace)
+    if d.batch * d.n_kv_heads > 65535:
+        raise QpError(2, "decode_step_heavy")
+    if size < need:
+        raise QpError(4, "decode_step_heavy")
+    if (address | q.data_ptr() | out.data_ptr()) & 15:
+        raise QpError(5, "decode_step_heavy")
     evict_kv(k_new, v_new, hc.cache, hc.weights, hc.pos, hc.next_pos, recent, hc.strategy)
     hc.next_pos += 1
     return decode_attn_weights(q, hc.cache, hc.weights, hc.strategy, out, workspace)
@@ -786,7 +803,7 @@ def decode_attn_tree(q: torch.Tensor, cache: Cache, k_draft: torch.Tensor, v_dra
         _dev(t, torch.bfloat16, (d.batch, T, d.n_kv_heads, d.head_dim))
     _dev(mask, torch.int64, (d.batch, T))
     _dev_cache(cache)
-    if tail is not None and d.bits < 16:
+    if tail is not None and tail.desc.n_tail and d.bits < 16:      # (an empty one needs no arrays)
         for t in (tail.k_tail, tail.v_tail):
             _dev(t, torch.bfloat16, (d.batch, d.n_kv_heads, d.group, d.head_dim))
     if out is None:

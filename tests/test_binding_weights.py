@@ -9,13 +9,14 @@ from paper_2412_12706_b200 import qp
 
 
 class Tensor:
-    def __init__(self, shape, dtype=torch.bfloat16, device=0, contiguous=True):
+    def __init__(self, shape, dtype=torch.bfloat16, device=0, contiguous=True, address=0x1000):
+        self.address = address
         self.shape, self.dtype, self.on, self.contiguous = torch.Size(shape), dtype, device, contiguous
         self.is_cuda, self.device = device is not None, "cpu" if device is None else f"cuda:{device}"
 
     def is_contiguous(self): return self.contiguous
     def get_device(self): return -1 if self.on is None else self.on
-    def data_ptr(self): return 0x1000
+    def data_ptr(self): return self.address
     def numel(self): return math.prod(self.shape)
     def element_size(self): return self.dtype.itemsize
 
@@ -100,3 +101,40 @@ def test_a_tail_of_another_device_or_cache_is_refused(library, bad):
     with pytest.raises(AssertionError):
         calls(bits=4, tree_tail=tail(**bad))["tree"]()
     assert len(library.calls) == 1
+
+
+def test_an_empty_tail_needs_no_arrays(library):
+    calls(bits=4, tree_tail=qp.Tail(qp.qp_tail(), None, None))["tree"]()
+    assert len(library.calls) == 1
+
+
+# ---------------------------------------------------------------------------------------------- the runs of calls
+
+def held(bits=16, n_cap=0):
+    f = torch.float32
+    cap = n_cap or n
+    return qp.HeavyCache(cache(bits, n_cap), None, Tensor((Bt, Hkv, cap), f), Tensor((Bt, Hkv, cap), torch.int32), 300)
+
+
+def step(hc, q=None, out=None, ws=None, k=None):
+    kv = k or Tensor((Bt, Hkv, D))
+    pos = hc.pos
+    pos.new_empty = lambda shape: Tensor(shape, torch.int32)
+    return qp.decode_step_heavy(q or Tensor((Bt, Hq, D)), kv, kv, hc, 8, out or Tensor((Bt, Hq, D)), ws or Tensor((1 << 20,), torch.uint8))
+
+
+@pytest.mark.parametrize("bad", [dict(q=Tensor((Bt, Hq, D + 1))), dict(q=Tensor((Bt, Hq, D), torch.float16)), dict(q=Tensor((Bt, Hq, D), device=None)),
+                                 dict(out=Tensor((Bt, Hq + 1, D))), dict(out=Tensor((Bt, Hq, D), device=1)), dict(ws=Tensor((16,), torch.uint8)),
+                                 dict(ws=Tensor((1 << 20,), torch.uint8, None)), dict(k=Tensor((Bt, Hkv, D), torch.float32)),
+                                 dict(q=Tensor((Bt, Hq, D), address=0x1008)), dict(out=Tensor((Bt, Hq, D), address=0x1002)),
+                                 dict(ws=Tensor((1 << 20,), torch.uint8, address=0x1004))])
+@pytest.mark.parametrize("n_cap", [0, 96])
+def test_a_refused_step_leaves_the_cache_as_it_was(library, bad, n_cap):
+    """A step is two calls: what the second would refuse is refused before the first has taken the token in, so the step can be
+    taken again."""
+    hc = held(n_cap=n_cap)
+    step(hc)
+    assert [c[0] for c in library.calls] == ["qp_evict_kv", "qp_decode_attn_weights"] and hc.next_pos == 301
+    with pytest.raises((AssertionError, qp.QpError)):
+        step(hc, **bad)
+    assert len(library.calls) == 2 and hc.next_pos == 301
