@@ -735,8 +735,9 @@ def compress_layer_heavy(K: torch.Tensor, V: torch.Tensor, Q: torch.Tensor, budg
                          recent: int = 32, n_cap: int = 0) -> HeavyCache:
     """The prefill-side path with accumulated weights in place of the observation window: qp_prompt_weights over all queries
     Q [Bt,Hq,L,D] -> qp_heavy_select -> qp_gather_quantize (16 bit) or qp_gather_quantize_ex with per-token keys."""
-    _dev_bf16(K); _dev_bf16(V); _dev_bf16(Q)
     Bt, Hkv, L, D = K.shape
+    for t, heads in ((K, Hkv), (V, Hkv), (Q, Q.shape[1])):
+        _dev(t, torch.bfloat16, (Bt, heads, L, D))
     n = n_keep(budget_bits, bits, group, L, recent)
     received = prompt_weights(Q, K)
     kept, weights, pos = heavy_select(received, recent, n, n_cap)

@@ -138,3 +138,17 @@ def test_a_refused_step_leaves_the_cache_as_it_was(library, bad, n_cap):
     with pytest.raises((AssertionError, qp.QpError)):
         step(hc, **bad)
     assert len(library.calls) == 2 and hc.next_pos == 301
+
+
+@pytest.mark.parametrize("K,V,Q", [((Bt, Hkv, L, D), (Bt, Hkv, L - 1, D), (Bt, Hq, L, D)), ((Bt, Hkv, L, D), (Bt, Hkv, L, D), (Bt, Hq, 32, D)),
+                                   ((Bt, Hkv, L, D), (Bt, 1, L, D), (Bt, Hq, L, D)), ((Bt, Hkv, L, D), (Bt, Hkv, L, D), (Bt + 1, Hq, L, D)),
+                                   ((Bt, Hkv, L, D), (Bt, Hkv, L, 64), (Bt, Hq, L, D)), ((Bt, Hkv, L, D), (Bt, Hkv, L, D), (Bt, Hq, L, 64))])
+@pytest.mark.parametrize("bits", [16, 4])
+def test_a_prompt_whose_arrays_do_not_belong_together_is_refused(library, monkeypatch, K, V, Q, bits):
+    """All queries of the prompt are asked for: a window of them would leave every key without weight that only later rows see."""
+    monkeypatch.setattr(qp, "alloc_cache", lambda *a, **k: cache(bits))
+    monkeypatch.setattr(qp, "heavy_select", lambda *a: (Tensor((Bt, Hkv, n), torch.int32), None, None))
+    monkeypatch.setattr(qp, "prompt_weights", lambda *a: library.calls.append(("qp_prompt_weights", a)))
+    with pytest.raises(AssertionError):
+        qp.compress_layer_heavy(Tensor(K), Tensor(V), Tensor(Q), n * bits, bits, 32, 8)
+    assert not library.calls
