@@ -62,3 +62,50 @@ def test_what_a_block_lost_whose_wait_ran_out_is_nan():
     r = subprocess.run([sys.executable, "-c", GIVE_UP], env=env, cwd=ROOT, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and r.stdout.strip() == "poisoned", r.stdout[-1000:] + r.stderr[-3000:]
     assert qp.debug_give_up(-1) == 2 and qp.debug_give_up(-2) == 1         # the normal build has no such call
+
+
+def error_words(ws, Bt, Hq, Hkv, T):
+    W = Bt * Hkv * ((T * (Hq // Hkv) + 255) // 256)
+    return ws[:4 * W * max(1, min(16, 148 // W))].view(torch.int32)
+
+
+@pytest.mark.parametrize("Bt,Hq,Hkv,D,n,bits,T", [(1, 32, 8, 128, 1024, 16, 40), (1, 32, 8, 128, 9216, 4, 40), (1, 8, 1, 64, 20000, 16, 64),
+                                                  (2, 8, 1, 128, 512, 2, 64), (19, 32, 8, 128, 320, 4, 16), (1, 8, 1, 128, 128, 8, 1)])
+def test_every_error_word_is_cleared_by_the_call(Bt, Hq, Hkv, D, n, bits, T):
+    c, _, _, _ = make_cache(Bt, Hq, Hkv, D, n, n, bits, 32, 0)
+    q, kd, vd = randn((Bt, T, Hq, D), 3), randn((Bt, T, Hkv, D), 4), randn((Bt, T, Hkv, D), 5)
+    mask = mask_of(random_tree(Bt, T, 5)[1])
+    ws = qp.new_decode_workspace(qp.decode_tree_workspace_bytes(c, T), DEV)
+    ws.fill_(255)
+    out = qp.decode_attn_tree(q, c, kd, vd, mask, workspace=ws)
+    assert torch.isfinite(out).all() and torch.all(error_words(ws, Bt, Hq, Hkv, T) == 0)
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4, 2])
+def test_large_logits_and_values_against_64_bits(bits):
+    """Logits of several hundred, drafts' values of several hundred: one token takes nearly everything, in cache and drafts."""
+    Bt, Hq, Hkv, D, n, T = 1, 8, 2, 128, 512, 9
+    c, _, k, v = make_cache(Bt, Hq, Hkv, D, n, n, bits, 32, 0, scale=10.0)
+    q, kd, vd = randn((Bt, T, Hq, D), 3, 20.0), randn((Bt, T, Hkv, D), 4, 10.0), randn((Bt, T, Hkv, D), 5, 500.0)
+    sees = torch.ones((T, T), dtype=torch.bool, device=DEV).tril().expand(Bt, T, T)
+    out = qp.decode_attn_tree(q, c, kd, vd, mask_of(sees)).double()
+    if bits < 16:
+        # what fp16 makes of the keys and queries is part of the operator: compare with the same factors, so that a logit of
+        # several hundred is not moved by 2^-11 of its terms
+        half = lambda x: x.double().half().double()
+        k, kq, vq, qq = half(k), half(kd), half(vd), half(q)
+    else:
+        kq, vq, qq = kd, vd, q
+    none = torch.zeros((Bt, Hkv, 0, D), dtype=torch.float64, device=DEV)
+    ref, _ = reference(qq, k, v, none, none, kq, vq, sees, bits)
+    x = qq.double().view(Bt, T, Hkv, Hq // Hkv, D)
+    keys, vals = torch.cat([k, kq.double().transpose(1, 2)], 2), torch.cat([v, vq.double().transpose(1, 2)], 2)
+    s = torch.einsum("bthgd,bhnd->bthgn", x, keys) / math.sqrt(D)
+    hide = torch.cat([torch.zeros((Bt, T, n), dtype=torch.bool, device=DEV), ~sees], -1)[:, :, None, None]
+    p = torch.softmax(s.masked_fill(hide, -math.inf), -1)
+    assert float(p.max()) > 0.99
+    spread = torch.einsum("bthgn,bhnd->bthgd", p, vals.abs()).reshape(out.shape)
+    sum_abs = float(torch.einsum("bthgd,bhnd->bthgn", x.abs(), keys.abs()).max())
+    e = (D + 8) * 2.0 ** -23 * sum_abs / math.sqrt(D)
+    tol = 2.0 ** -8 * ref.abs() + ((2.0 ** -8 if bits == 16 else 2.0 ** -11) + 2.0 ** -11 + math.expm1(2 * e)) * spread + 1e-6
+    assert torch.all((out - ref).abs() <= tol), float(((out - ref).abs() / tol).max())

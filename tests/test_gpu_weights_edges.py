@@ -176,3 +176,153 @@ def test_first_calls_of_several_host_threads_at_once():
     for _ in range(3):
         r = subprocess.run([sys.executable, "-c", THREADS], capture_output=True, text=True, timeout=300, cwd=root)
         assert r.returncode == 0 and r.stdout.strip() == "same", r.stderr[-2000:]
+
+
+# ---------------------------------------------------------------------------------------------- runs of calls
+
+def overlapping_run(alone, steps=70):
+    """Every call of a generation loop reads what the call before it wrote, on a stream whose decode calls may overlap.  alone: the
+    GPU is waited for after every call.  (The setting itself stays: a decode call cuts its work by it, so its last bits differ.)"""
+    done = torch.cuda.synchronize if alone else lambda: None
+    Bt, H, D, n, g = 2, 4, 128, 512, 32
+    r = lambda *shape, seed: randn(shape, seed)
+    K, V = r(Bt, H, n, D, seed=1), r(Bt, H, n, D, seed=2)
+    kept = torch.arange(n, dtype=torch.int32, device=DEV).expand(Bt, H, n).contiguous()
+    X = qp.alloc_cache(Bt, H, H, D, 4, g, n, DEV, n + 3 * g)
+    for t in (X.k_codes, X.v_codes, X.k_scale, X.k_zero, X.v_scale, X.v_zero):
+        t.zero_()
+    qp.gather_quantize(K, V, kept, X)
+    tail = qp.alloc_tail(X)
+    held = []
+    for bits in (8, 16):
+        Y = qp.alloc_cache(Bt, H, H, D, bits, g, n, DEV, n + 40 if bits == 16 else 0)
+        st = None
+        if bits == 16:
+            Y.k_codes.zero_(); Y.v_codes.zero_()
+            qp.gather_quantize(K, V, kept, Y)
+        else:
+            st = qp.make_strategy(Y, 1)
+            qp.gather_quantize_ex(K, V, kept, Y, st)
+        cap = Y.desc.n_cap or n
+        pos = torch.arange(cap, dtype=torch.int32, device=DEV).expand(Bt, H, cap).contiguous()
+        held.append((Y, st, torch.rand((Bt, H, cap), generator=torch.Generator(device=DEV).manual_seed(3), device=DEV), pos))
+    size = max([qp.decode_workspace_bytes(X), qp.decode_tree_workspace_bytes(X, 1)] + [qp.decode_weights_workspace_bytes(Y[0]) for Y in held])
+    ws = qp.new_decode_workspace(size, DEV)
+    mask = torch.ones((Bt, 1), dtype=torch.int64, device=DEV)
+    outs = [torch.empty((Bt, H, D), dtype=torch.bfloat16, device=DEV) for _ in range(5 * steps)]
+    slots = torch.empty((Bt, H), dtype=torch.int32, device=DEV)
+    q = r(Bt, H, D, seed=4)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        qp.decode_overlap(True)
+        for s in range(steps):
+            a, b, c, d, e = outs[5 * s:5 * s + 5]
+            qp.decode_attn(q, X, a, ws); done()
+            for (Y, st, w, pos), kv, o in zip(held, (a, b), (b, c)):
+                qp.evict_kv(kv, kv, Y, w, pos, 3 * n + s, 16, st, slots); done()
+                qp.decode_attn_weights(kv, Y, w, st, o, ws); done()
+            qp.append_kv(c, b, X, tail); done()
+            qp.decode_attn_tree(c.view(Bt, 1, H, D), X, b.view(Bt, 1, H, D), a.view(Bt, 1, H, D), mask, tail, None, d.view(Bt, 1, H, D), ws)
+            done()
+            qp.decode_attn_tail(d, X, tail, e, ws); done()
+            q = e
+        qp.decode_overlap(False)
+    torch.cuda.synchronize()
+    state = [t for Y, _, w, pos in held for t in (Y.k_codes, Y.v_codes, w, pos)]
+    return outs + state + [X.k_codes, X.v_codes, tail.k_tail, tail.v_tail]
+
+
+def test_new_calls_among_decode_calls_that_may_overlap():
+    ref = overlapping_run(True)
+    assert all(torch.isfinite(t.float()).all() for t in ref)
+    for _ in range(5):
+        for i, (a, b) in enumerate(zip(ref, overlapping_run(False))):
+            assert torch.equal(a, b), i
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_steps_at_rising_positions_from_graphs(bits):
+    """A captured step stands for the position it was captured at: one graph per step, replayed in order, gives the eager steps'
+    bits, through growth (16 bit) and eviction."""
+    Bt, Hq, Hkv, D, L, n, recent, steps = 2, 8, 2, 128, 500, 64, 16, 40
+    K, V, Q = randn((Bt, Hkv, L, D), 1, 1.5), randn((Bt, Hkv, L, D), 2), randn((Bt, Hq, L, D), 3, 1.5)
+    cap = n + 10 if bits == 16 else 0
+    news = [(randn((Bt, Hq, D), 10 + s, 1.5), randn((Bt, Hkv, D), 100 + s), randn((Bt, Hkv, D), 200 + s)) for s in range(steps)]
+
+    def state():
+        hc = qp.compress_layer_heavy(K, V, Q, n * bits, bits, 32, recent, cap)
+        return hc, torch.zeros((steps, Bt, Hq, D), dtype=torch.bfloat16, device=DEV)
+
+    (e, eo), (c, co) = state(), state()
+    ws = qp.new_decode_workspace(qp.decode_weights_workspace_bytes(e.cache), DEV)
+    for s, (q, k, v) in enumerate(news):
+        qp.decode_step_heavy(q, k, v, e, recent, eo[s], ws)
+    torch.cuda.synchronize()
+    graphs = []
+    for s, (q, k, v) in enumerate(news):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            qp.decode_step_heavy(q, k, v, c, recent, co[s], ws)
+        graphs.append(g)
+    for g in graphs:
+        g.replay()
+    torch.cuda.synchronize()
+    used = e.cache.desc.n_keep
+    assert used == c.cache.desc.n_keep == (cap or n) and e.next_pos == c.next_pos == L + steps
+    assert torch.equal(eo, co) and torch.equal(e.weights, c.weights) and torch.equal(e.pos, c.pos)
+    assert torch.equal(e.cache.k_codes, c.cache.k_codes) and torch.equal(e.cache.v_codes, c.cache.v_codes)
+
+
+def test_decode_attn_weights_where_one_token_takes_everything():
+    """Logits of several hundred, against 64 bits: the token that wins, its weight and the output."""
+    for bits in (16, 8, 4, 2):
+        Bt, Hq, Hkv, D, n = 1, 8, 2, 128, 512
+        K, V = randn((Bt, Hkv, n, D), 3, 8.0), randn((Bt, Hkv, n, D), 4)
+        q = randn((Bt, Hq, D), 8, 16.0)
+        if bits == 16:
+            cache, st = qp.alloc_cache(Bt, Hq, Hkv, D, 16, 32, n, DEV), None
+            qp.gather_quantize(K, V, torch.arange(n, dtype=torch.int32, device=DEV).expand(Bt, Hkv, n).contiguous(), cache)
+            k, v, terms = K.double(), V.double(), V.double().abs()
+        else:
+            cache, st, k, cs, z = packed(K, V, Hq, bits, 32)
+            v, terms = cs + z, cs.abs() + z.abs()
+        w = torch.zeros((Bt, Hkv, n), device=DEV)
+        out = qp.decode_attn_weights(q, cache, w, st).double().view(Bt, Hkv, Hq // Hkv, D)
+        x = q.double().view(Bt, Hkv, Hq // Hkv, D)
+        p = torch.softmax(torch.einsum("bhgd,bhnd->bhgn", x, k) / math.sqrt(D), -1)
+        assert float(p.max()) > 0.99
+        rel = rel_bound(3 * float(torch.einsum("bhgd,bhnd->bhgn", x.abs(), k.abs()).max()), D)
+        assert torch.all((w.double() - p.sum(2)).abs() <= rel * p.sum(2) + 2.0 ** -100)      # (a weight below 2^-126 is 0)
+        ref, spread = torch.einsum("bhgn,bhnd->bhgd", p, v), torch.einsum("bhgn,bhnd->bhgd", p, terms)
+        tol = 2.0 ** -8 * ref.abs() + (2.0 ** -8 if bits == 16 else 2.0 ** -9) * spread + rel * spread + 1e-6
+        assert torch.all((out - ref).abs() <= tol), (bits, float(((out - ref).abs() / tol).max()))
+
+
+@pytest.mark.parametrize("bits,g,D", [(4, 32, 128), (4, 64, 64), (4, 128, 128), (8, 32, 128), (8, 64, 64), (2, 32, 128), (2, 64, 64)])
+def test_an_evicted_row_beside_the_same_row_of_the_quantizer(bits, g, D):
+    """The row that eviction stores and the row that qp_gather_quantize_ex stores of the same numbers.  The zero point is the same.
+    The scale is the range times RN(1 / (2^B - 1)), which lies above 1 / (2^B - 1) for B = 2, 4, 8, so never below the quotient's and
+    at most one fp16 step above it; codes are rounded against the stored scale, so every number comes back to half of it."""
+    Bt, H, n = 4, 8, 256
+    n = n // g * g
+    K, V = randn((Bt, H, n, D), 5, 3.0), randn((Bt, H, n, D), 6, 0.2)
+    kept = torch.arange(n, dtype=torch.int32, device=DEV).expand(Bt, H, n).contiguous()
+    ref, got = [qp.alloc_cache(Bt, H, H, D, bits, g, n, DEV) for _ in range(2)]
+    st = qp.make_strategy(ref, 1)
+    qp.gather_quantize_ex(K, V, kept, ref, st)
+    qp.gather_quantize_ex(V, K, kept, got, st)
+    w, pos = torch.zeros((Bt, H, n), device=DEV), torch.arange(n, dtype=torch.int32, device=DEV).expand(Bt, H, n).contiguous()
+    for t in range(n):                                             # every row gives its place to the other cache's
+        s = qp.evict_kv(K[:, :, t].contiguous(), V[:, :, t].contiguous(), got, w, pos, n + t, n, st)
+        assert torch.all(s == t)
+    for x, side in ((K, "k"), (V, "v")):
+        rows = lambda c, name: getattr(c, f"{side}_{name}").view(Bt, H, n, D // g, -1)
+        assert torch.equal(rows(got, "zero"), rows(ref, "zero"))
+        step = rows(got, "scale").view(torch.int16).int() - rows(ref, "scale").view(torch.int16).int()
+        assert int(step.min()) >= 0 and int(step.max()) <= 1
+        same = step[..., 0] == 0
+        assert torch.equal(rows(got, "codes")[same], rows(ref, "codes")[same])
+        back = unpack(getattr(got, f"{side}_codes"), getattr(got, f"{side}_scale"), getattr(got, f"{side}_zero"), bits).reshape(x.shape)
+        half = 0.5 * rows(got, "scale").double().expand(Bt, H, n, D // g, g).reshape(x.shape)
+        assert torch.all((back - x.double()).abs() <= half * (1 + 2.0 ** -10) + 2.0 ** -24 * x.double().abs())
