@@ -326,3 +326,21 @@ def test_an_evicted_row_beside_the_same_row_of_the_quantizer(bits, g, D):
         back = unpack(getattr(got, f"{side}_codes"), getattr(got, f"{side}_scale"), getattr(got, f"{side}_zero"), bits).reshape(x.shape)
         half = 0.5 * rows(got, "scale").double().expand(Bt, H, n, D // g, g).reshape(x.shape)
         assert torch.all((back - x.double()).abs() <= half * (1 + 2.0 ** -10) + 2.0 ** -24 * x.double().abs())
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,L,q0,nq", [(8, 1, 128, 65536, 0, 65536), (4, 2, 64, 131072, 0, 131072), (8, 2, 128, 300001, 299000, 1001)])
+def test_prompt_weights_of_long_prompts(Hq, Hkv, D, L, q0, nq):
+    """Every row gives 1 in all; the last keys, which only the last rows see, against 64 bits."""
+    Q, K = randn((1, Hq, nq, D), 1, 1.5), randn((1, Hkv, L, D), 2, 1.5)
+    got = qp.prompt_weights(Q, K, q0).double()
+    G, last = Hq // Hkv, 200
+    sum_abs, ref = 0.0, []
+    hide = torch.arange(L, device=DEV) > (L - last + torch.arange(last, device=DEV))[:, None]
+    for h in range(Hkv):
+        q, k = Q[0, h * G:(h + 1) * G, -last:].double(), K[0, h].double()
+        p = torch.softmax((q @ k.T / math.sqrt(D)).masked_fill(hide, -math.inf), -1)
+        ref.append(p.sum((0, 1))[-last:])
+        sum_abs = max(sum_abs, float(Q[0, h * G:(h + 1) * G].double().abs().amax((0, 1)) @ k.abs().amax(0)))
+    rel = rel_bound(sum_abs, D, G * nq)
+    assert torch.all(((got[0, :, -last:] - torch.stack(ref)).abs() / torch.stack(ref)) <= rel)
+    assert torch.all((got.sum(-1) - G * nq).abs() <= G * nq * rel)
