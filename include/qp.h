@@ -351,6 +351,9 @@ qp_status qp_decode_attn_layers_ex(int n_layers, const void* const* q, const qp_
  *   each step   qp_evict_kv (the new token's row takes a place in the full cache)  ->  qp_decode_attn_weights
  * A single token can only be replaced where no group spans several tokens: these calls take 16-bit caches and caches with
  * per-token keys (qp_strategy.k_axis = 1, no filtering), not the main path's per-channel keys.
+ * Alignment, of these calls and of qp_decode_attn_tree: every device pointer 16 bytes, arrays of 32- and 64-bit numbers (weights,
+ * pos, mask) included; the arrays of qp_heavy_select and slots, 4 bytes.  Calls that may run at the same time (on different
+ * streams, or from two graphs) must not share a workspace, nor weights, pos or a cache that one of them writes.
  */
 
 /*
@@ -361,7 +364,7 @@ qp_status qp_decode_attn_layers_ex(int n_layers, const void* const* q, const qp_
  * positions below q_start + n_q are set, those behind are set to 0.  accumulate != 0: they are added to, and the positions
  * behind are left as they are.  Keys at and behind q_start + n_q are not looked at and may hold anything.
  * The kernels wait on hardware barriers with a bounded number of polls (see qp_window_scores); a wait that runs out makes the
- * weights that hang on it NaN.
+ * weights that hang on it NaN.  So does a query that is not finite: every key that it sees is NaN then.
  */
 size_t qp_prompt_weights_workspace_bytes(int batch, int n_q_heads, int n_kv_heads, int head_dim, int L, int q_start, int n_q);
 qp_status qp_prompt_weights(const void* Q, const void* K, int batch, int n_q_heads, int n_kv_heads, int head_dim, int L,
@@ -382,7 +385,8 @@ qp_status qp_heavy_select(const float* weights, int batch, int n_kv_heads, int L
  *   weights[b,k,t] += sum over the G query heads of k of their softmax weight of token t,   t < n_keep
  * (fp32 [Bt,Hkv,n_cap], device, in place; slots behind n_keep are left as they are).  strategy: NULL for a 16-bit cache, else
  * k_axis = 1 and no filtering (QP_ERR_UNSUPPORTED otherwise).  Queries enter the tensor cores unscaled: |q| <= 65504 and, for
- * B < 16, max|V| <= 4096.  Runs in plain stream order.
+ * B < 16, max|V| <= 4096.  The product of a weight with a value's scale is off by 2^-11 of itself, or by 2^-35 of the heaviest
+ * weight where that is more (the older decode calls multiply the two in fp16 as they are: 2^-25).  Runs in plain stream order.
  */
 size_t qp_decode_weights_workspace_bytes(const qp_cache* cache /* host */);
 qp_status qp_decode_attn_weights(const void* q, const qp_cache* cache /* host */, const qp_strategy* strategy /* host */,
@@ -394,7 +398,9 @@ qp_status qp_decode_attn_weights(const void* q, const qp_cache* cache /* host */
  * the slot is that of the token with the smallest weight among those with pos <= new_pos - recent (equal weights: the lower
  * slot); if there is none, that of the token with the smallest pos (equal: the lower slot).  Per-token caches never grow here.
  * The row is stored as qp_gather_quantize_ex would store it, but that the quotient (m - z)/(2^B - 1) is taken as the 32-bit
- * product with the rounded reciprocal before it is rounded up to fp16 (the stored scale may differ in its last place);
+ * product with the rounded reciprocal before it is rounded up to fp16, as tensor code on the GPU does that divides by that number:
+ * the stored scale is the same or one fp16 step larger (4 bit: about one group in 23), never smaller, and the codes are rounded
+ * against it;
  * weights[slot] = 0, pos[slot] = new_pos, and, unless NULL,
  * slots int32 [Bt,Hkv] = slot.  weights fp32, pos int32 [Bt,Hkv,n_cap] (device, in place; weights without NaN).
  * new_pos >= 0, recent >= 0.  strategy as for qp_decode_attn_weights.  new_pos and n_keep are host values: a captured call
@@ -410,7 +416,9 @@ qp_status qp_evict_kv(const void* k_new, const void* v_new, qp_cache* cache /* h
  * (its ancestors and itself; any set of bits is allowed, none included; bits T and above are ignored):
  *   out[b,i,h] = softmax over those tokens of (q[b,i,h].k / sqrt(D)), times their values
  * q, out bf16 [Bt,T,Hq,D]; k_draft, v_draft bf16 [Bt,T,Hkv,D]; mask uint64 [Bt,T]; 1 <= T <= QP_MAX_DRAFTS.  The drafts' rows
- * need not be in the cache; accepted ones are appended with qp_append_kv.  tail: NULL or as for qp_decode_attn_tail.
+ * need not be in the cache; accepted ones are appended with qp_append_kv, which adds a token to every sequence: n_keep and n_tail
+ * are one number for the batch, so a batch can keep as many drafts as the sequence that accepted fewest (sequences that go their
+ * own way have caches of batch 1).  tail: NULL or as for qp_decode_attn_tail.
  * strategy: NULL (per-channel keys, or 16 bit) or k_axis 0 / 1 without filtering.  Any bits.  For B < 16 keys and values,
  * drafts and tail included, are multiplied in fp16 (|x| <= 65504).  What a draft holds, numbers or not, reaches only the rows
  * that see it (the drafts behind the last of a smaller tree of the batch may hold anything).  Plain stream order.  The workspace

@@ -9,10 +9,12 @@
 // into weights and writes its slice of the output.  Bound: the packed bytes from HBM; the logits stay in shared memory, or for
 // very long runs in the caller's workspace (L2).
 //
-// The weights are results of their own, so logits, maxima and sums are 32-bit exact: queries enter the tensor cores unscaled
-// (a bf16 value is an f16 value in the range the interface allows, and codes are integers), scales, zero points and
-// log2(e)/sqrt(D) are applied to 32-bit accumulators.  Only the second product, whose result is rounded to bf16, uses
-// weights rounded to 16 bits.
+// The weights are results of their own, so logits, maxima and sums are held in 32 bits: queries enter the tensor cores unscaled,
+// codes are integers, and scales, zero points and log2(e)/sqrt(D) (by the approximate reciprocal root, 2 ulp) are applied to
+// 32-bit accumulators.  At 16 bit every factor of a logit is exact; in packed caches a query channel is a bf16 value times 2^-p,
+// p <= 8 - B, in f16: exact from 2^(p-17) on, below that off by at most 2^(p-25), at 2 bit 2^-19.  Only the second product, whose
+// result is rounded to bf16, uses weights rounded to 16 bits: bf16 in 16-bit caches, like their values (2^-8 of a weight), f16 in
+// packed ones (2^-11, and 2^-11 for the product with the scale).
 //
 // Measured in a replayed graph: 8192 tokens x 64 KV heads at 4 bit 25.2 us = 3.5 TB/s (the stream 17 us of it, exchange and weights
 // 5), 5001 x 32 KV heads of eight query heads at 16 bit 20.8 us = 4.0 TB/s, 512 tokens x 8 KV heads at 16 bit 5.5 us.

@@ -20,8 +20,9 @@
 // into one run per SM (see Plan); a quad that several runs share leaves partial results, which two small kernels add in a fixed
 // order.
 //
-// Measured in a replayed graph: 8192 tokens of 32 heads over 8 (D = 128) 0.56 ms = 0.98 PFLOP/s of products, the exponential unit
-// 73 to 76 % busy, the tensor pipe 53 to 56 %, at the GPU's power limit; 1999 queries behind 14301 keys, 64 heads over 8, 1.07 ms;
+// Measured in a replayed graph: 8192 tokens of 32 heads over 8 (D = 128) 0.56 ms = 0.98 PFLOP/s of products (0.54 in short runs, before
+// the limit is reached), the exponential unit
+// 73 to 76 % busy, the tensor pipe 48 to 50 %, at the GPU's power limit; 1999 queries behind 14301 keys, 64 heads over 8, 1.07 ms;
 // 1024 tokens of 8 heads over 2 (D = 64) 19 us, four launches one after another.
 #include <algorithm>
 

@@ -902,7 +902,8 @@ cudaError_t token_map(CUtensorMap* map, const void* base, const TreeArgs& a) {
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-// most clusters per (KV head, row group): as many as keep every SM busy with clusters of one
+// most clusters per (KV head, row group): as many as keep every SM busy with clusters of one.  A B200's 148 and not the device's
+// count, because the layout of the workspace, which the interface gives, goes by it.
 int tree_max_subs(int items) { return std::max(1, std::min(TR_MAX_SUBS, 148 / items)); }
 struct TreeWorkspace {
   size_t part, part_ml, total;   // the error words come first

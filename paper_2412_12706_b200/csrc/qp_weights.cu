@@ -84,7 +84,10 @@ evict_kernel(const __grid_constant__ EvictArgs a) {
     }
     z16 = __float2half_rd(mn);
     const float z = __half2float(z16);
-    s16 = __float2half_ru(__fmul_rn(__fsub_rn(mx, z), 1.0f / (float)qmax));      // product with the rounded reciprocal
+    // The product with the rounded reciprocal, where the prompt's quantizer takes the rounded quotient: what tensor code stores that
+    // divides a row on the GPU by the number 2^B - 1, so that such code and this call agree bit for bit.  RN(1/3), RN(1/15) and
+    // RN(1/255) lie above the reciprocals: the scale is the quotient's or one fp16 step more, never less, and nothing clips.
+    s16 = __float2half_ru(__fmul_rn(__fsub_rn(mx, z), 1.0f / (float)qmax));
     const float s = __half2float(s16);
     // this lane's elements fill per_lane * bits bits of a word; the lanes of a word put theirs together
     const int lanes = 32 / (per_lane * bits), sub = lanes > 1 ? lane % lanes : 0;

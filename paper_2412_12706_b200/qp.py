@@ -778,7 +778,8 @@ def decode_step_heavy(q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor,
 
 def tree_mask(parents: torch.Tensor) -> torch.Tensor:
     """Masks of a drafted tree for decode_attn_tree: parents int [Bt,T], parents[b,i] < i the node draft i hangs on, or -1 for
-    the context -> int64 [Bt,T], bit j of mask[b,i] set for i itself and its ancestors."""
+    the context -> int64 [Bt,T], bit j of mask[b,i] set for i itself and its ancestors.  Tensor code that waits for the device to
+    look at the parents (not for a capture): a tree whose shape does not change from step to step needs it once."""
     Bt, T = parents.shape
     assert 1 <= T <= QP_MAX_DRAFTS
     i = torch.arange(T, device=parents.device)
