@@ -25,6 +25,7 @@
 
 #include <algorithm>
 
+#include "qp_cluster.cuh"
 #include "qp_mma.cuh"
 
 namespace qp {
@@ -151,15 +152,6 @@ __device__ __forceinline__ void dw_finish(const DwArgs& a, int bh, int G, int to
   cluster.barrier_wait();                // nobody leaves while another may still read its shared memory
 }
 
-__device__ __forceinline__ void dw_cp16_zf(uint32_t saddr, const void* gptr, bool valid) {
-  const int n = valid ? 16 : 0;
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(saddr), "l"(gptr), "r"(n));
-}
-__device__ __forceinline__ uint32_t dw_bf16x2(float lo, float hi) {
-  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-
 // ---- 16-bit caches: query heads as MMA rows, so the weights leave the first product in the layout the second wants.  Eight
 // warps that walk over 16 tokens each: the stream is bound by how many warps wait for their own copies and products, not by
 // bytes in flight.
@@ -205,8 +197,8 @@ decode_weights16_kernel(const __grid_constant__ DwArgs a) {
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
         const bool ok = tok + tau0 + i * TSTEP < n;
-        dw_cp16_zf(sb + dst[i], ok ? gk + i * TSTEP * (D * 2) : static_cast<const unsigned char*>(a.ly.kc), ok);
-        dw_cp16_zf(sb + VOFF + dst[i], ok ? gv + i * TSTEP * (D * 2) : static_cast<const unsigned char*>(a.ly.vc), ok);
+        cp_async16_zfill(sb + dst[i], ok ? gk + i * TSTEP * (D * 2) : static_cast<const unsigned char*>(a.ly.kc), ok);
+        cp_async16_zfill(sb + VOFF + dst[i], ok ? gv + i * TSTEP * (D * 2) : static_cast<const unsigned char*>(a.ly.vc), ok);
       }
     }
     tok += DW16_WARPS * 16;
@@ -277,7 +269,7 @@ decode_weights16_kernel(const __grid_constant__ DwArgs a) {
     for (int nt = 0; nt < 2; ++nt) {
       const float p0 = ex2(sc[nt][0] - mnew), p1 = ex2(sc[nt][1] - mnew);
       sum += p0 + p1;
-      pa[nt] = dw_bf16x2(p0, p1);
+      pa[nt] = pack_bf16x2(p0, p1);
     }
     l_run = fmaf(l_run, corr, sum);
     if (__any_sync(0xffffffffu, corr != 1.f)) {
@@ -666,13 +658,11 @@ decode_weights_packed_kernel(const __grid_constant__ DwArgs a) {
 // (+-1), `active` clusters of a size fit on the GPU at once, so the launch lasts ceil(heads / active) rounds of (tiles per warp
 // + a fixed cost of about two tiles for set-up and exchange).
 template <typename K>
-cudaError_t launch_dw(K kernel, int warps, int warp_tokens, size_t smem, DwArgs a, int BH, float* ws, unsigned char (&done)[64],
-                      int (&active)[64][DW_MAX_CLUSTER + 1], cudaStream_t st) {
+cudaError_t launch_dw(K kernel, int warps, int warp_tokens, size_t smem, DwArgs a, int BH, float* ws, int (&active)[64][DW_MAX_CLUSTER + 1],
+                      cudaStream_t st) {
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
-  e = allow_smem(kernel, smem, done);
-  if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.blockDim = dim3(warps * 32);
   cfg.dynamicSmemBytes = smem;
@@ -704,15 +694,13 @@ cudaError_t launch_dw(K kernel, int warps, int warp_tokens, size_t smem, DwArgs 
 
 template <int BITS, int D, int GROUP>
 cudaError_t launch_packed(const DwArgs& a, int BH, float* ws, cudaStream_t st) {
-  static unsigned char done[64] = {};
   static int active[64][DW_MAX_CLUSTER + 1] = {};
-  return launch_dw(decode_weights_packed_kernel<BITS, D, GROUP>, DW_WARPS, 32, Pk<BITS, D, GROUP>::SMEM_ALL, a, BH, ws, done, active, st);
+  return launch_dw(decode_weights_packed_kernel<BITS, D, GROUP>, DW_WARPS, 32, Pk<BITS, D, GROUP>::SMEM_ALL, a, BH, ws, active, st);
 }
 template <int D>
 cudaError_t launch_16(const DwArgs& a, int BH, float* ws, cudaStream_t st) {
-  static unsigned char done[64] = {};
   static int active[64][DW_MAX_CLUSTER + 1] = {};
-  return launch_dw(decode_weights16_kernel<D>, DW16_WARPS, 16, dw16_smem<D>(), a, BH, ws, done, active, st);
+  return launch_dw(decode_weights16_kernel<D>, DW16_WARPS, 16, dw16_smem<D>(), a, BH, ws, active, st);
 }
 template <int BITS>
 cudaError_t launch_bits(const DwArgs& a, int D, int BH, float* ws, cudaStream_t st) {

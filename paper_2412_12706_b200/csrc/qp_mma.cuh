@@ -1,8 +1,6 @@
 // Device helpers shared by the tensor-core decode kernels.
 #pragma once
 
-#include <mutex>
-
 #include "qp_common.cuh"
 
 namespace qp {
@@ -126,33 +124,9 @@ template <typename K>
 cudaError_t allow_smem(K kernel, size_t bytes, unsigned char (&done)[64]) {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
-  if (__atomic_load_n(&done[dev], __ATOMIC_ACQUIRE)) return cudaSuccess;         // (host threads may call at the same time)
+  if (done[dev]) return cudaSuccess;
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-  if (e == cudaSuccess) __atomic_store_n(&done[dev], (unsigned char)1, __ATOMIC_RELEASE);
-  return e;
-}
-
-// How many clusters of 1 .. max_cluster CTAs of a kernel fit on the current device at once: active[1 .. max_cluster], asked by the
-// first call only; active[0] != 0 once they are there, so a host thread that comes meanwhile waits and reads whole answers.
-// cfg: block, shared memory and stream of the launch.
-template <typename K>
-cudaError_t clusters_that_fit(K kernel, cudaLaunchConfig_t cfg, int max_cluster, int* active) {
-  if (__atomic_load_n(&active[0], __ATOMIC_ACQUIRE)) return cudaSuccess;
-  static std::mutex mu;
-  std::lock_guard<std::mutex> lock(mu);
-  if (__atomic_load_n(&active[0], __ATOMIC_RELAXED)) return cudaSuccess;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  for (int c = 1; c <= max_cluster && e == cudaSuccess; ++c) {
-    cfg.gridDim = dim3(c);
-    attr[0].val.clusterDim.x = c;
-    e = cudaOccupancyMaxActiveClusters(&active[c], kernel, &cfg);
-  }
-  if (e == cudaSuccess) __atomic_store_n(&active[0], 1, __ATOMIC_RELEASE);
+  if (e == cudaSuccess) done[dev] = 1;
   return e;
 }
 

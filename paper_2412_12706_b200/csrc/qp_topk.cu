@@ -58,12 +58,6 @@ __device__ __forceinline__ void topk_pad([[maybe_unused]] const TopkOut<NL>& o, 
     }
 }
 
-// monotone map float -> uint32 (larger float = larger integer); -0 is treated as +0
-__device__ __forceinline__ uint32_t order_key(float f) {
-  const uint32_t u = __float_as_uint(f + 0.0f);
-  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-}
-
 template <int NL>
 __global__ void __launch_bounds__(TK_THREADS)
 topk_kernel(const float* __restrict__ scores, int L, int w, int BH, const __grid_constant__ TopkOut<NL> o) {

@@ -35,6 +35,7 @@
 #include <algorithm>
 #include <cstring>
 
+#include "qp_cluster.cuh"
 #include "qp_mma.cuh"
 #include "qp_tc.cuh"
 
@@ -95,10 +96,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;\n" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
-}
-__device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
-  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&h);
 }
 // two bf16 values to two fp16 values
 __device__ __forceinline__ uint32_t bf2_to_half2(uint32_t v) { return pack_half2(bf16lo(v), bf16hi(v)); }
@@ -920,7 +917,6 @@ TreeWorkspace tree_carve(const TreeArgs& a) {
 
 template <int BITS, int D>
 cudaError_t launch_tree_t(TreeLaunch p, const CUtensorMap& mk, const CUtensorMap& mv, int* err, cudaStream_t st) {
-  static unsigned char done[64] = {};
   static int active[64][TR_MAX_CLUSTER + 1] = {};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
@@ -928,8 +924,6 @@ cudaError_t launch_tree_t(TreeLaunch p, const CUtensorMap& mk, const CUtensorMap
   constexpr size_t SLOT = 128 * (size_t)D * 2;
   constexpr size_t smem_max = 7 * SLOT + 1024;                  // queries and ring, or the partial results that overlay them
   auto kernel = tree_kernel<BITS, D>;
-  e = allow_smem(kernel, smem_max, done);
-  if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.blockDim = dim3(TR_THREADS);
   cfg.dynamicSmemBytes = smem_max;

@@ -5,12 +5,6 @@ namespace qp {
 
 namespace {
 
-// monotone map float -> uint32 (larger float = larger integer); -0 as +0
-__device__ __forceinline__ uint32_t order_image(float f) {
-  const uint32_t u = __float_as_uint(f + 0.0f);
-  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-}
-
 // One block per (batch, KV head).  The call is a chain of latencies (a few hundred KB in all): the row is fetched and quantized
 // while the search's loads are on their way, every thread has EV_PER weights and positions in flight, and the two minima the
 // rule may need (lightest of the old, oldest of all) are taken together as 64-bit keys (order image, slot), which makes equal
@@ -62,7 +56,7 @@ evict_kernel(const __grid_constant__ EvictArgs a) {
       for (int k = 0; k < EV_PER; ++k) {
         const unsigned t = (unsigned)min(t0 + k * EV_THREADS, a.n - 1);
         const unsigned long long o = ((unsigned long long)((uint32_t)p[k] ^ 0x80000000u) << 32) | t;
-        const unsigned long long l = (long long)p[k] <= a.limit ? ((unsigned long long)order_image(v[k]) << 32) | t : ~0ull;
+        const unsigned long long l = (long long)p[k] <= a.limit ? ((unsigned long long)order_key(v[k]) << 32) | t : ~0ull;
         oldest = o < oldest ? o : oldest;
         light = l < light ? l : light;
       }
