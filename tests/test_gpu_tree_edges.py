@@ -109,3 +109,38 @@ def test_large_logits_and_values_against_64_bits(bits):
     e = (D + 8) * 2.0 ** -23 * sum_abs / math.sqrt(D)
     tol = 2.0 ** -8 * ref.abs() + ((2.0 ** -8 if bits == 16 else 2.0 ** -11) + 2.0 ** -11 + math.expm1(2 * e)) * spread + 1e-6
     assert torch.all((out - ref).abs() <= tol), float(((out - ref).abs() / tol).max())
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("Bt,Hq,Hkv,T", [(18, 32, 8, 40), (1, 8, 8, 64)])
+def test_a_draft_that_takes_nearly_everything_gives_its_own_value(bits, Bt, Hq, Hkv, T):
+    """Two light tokens in the cache (32 for packed ones), and drafts that see themselves 4 to 5.4 nats above them: less than the 2^8
+    by which the reference may lag, so the heavy weight is not 1 and its 16 bits round it.  It is in the sum as it is in the product, so that
+    a weight's rounding (2^-8 in bf16, 2^-11 in fp16, of it and of the sum) moves the output by twice that of sum p |v - out| only."""
+    D, n = 128, 2 if bits == 16 else 32
+    c = qp.alloc_cache(Bt, Hq, Hkv, D, bits, 32, n, DEV)
+    K, V = torch.zeros((Bt, Hkv, n, D), dtype=torch.bfloat16, device=DEV), randn((Bt, Hkv, n, D), 2)
+    qp.gather_quantize(K, V, torch.arange(n, dtype=torch.int32, device=DEV).expand(Bt, Hkv, n).contiguous(), c)
+    v = V.double()
+    if bits < 16:
+        cv = ((c.v_codes.long()[..., None] >> (bits * torch.arange(32 // bits, device=DEV))) & (2 ** bits - 1)).flatten(-2).double()
+        v = (cv * c.v_scale.double()[..., None] + c.v_zero.double()[..., None]).reshape(Bt, Hkv, n, D)
+    one = randn((Bt, T, Hkv, 1, D), 3)
+    q = one.expand(Bt, T, Hkv, Hq // Hkv, D).reshape(Bt, T, Hq, D).contiguous()
+    g = torch.Generator(device=DEV).manual_seed(4)
+    above = 4.0 + 1.4 * torch.rand((Bt, T, Hkv, 1), generator=g, device=DEV, dtype=torch.float64) + math.log(n / 2)
+    above = above.clamp(max=5.4)
+    x = one[:, :, :, 0].double()
+    kd, vd = (x * above * math.sqrt(D) / x.square().sum(-1, keepdim=True)).to(torch.bfloat16), randn((Bt, T, Hkv, D), 5)
+    sees = torch.eye(T, dtype=torch.bool, device=DEV).expand(Bt, T, T)
+    out = qp.decode_attn_tree(q, c, kd, vd, mask_of(sees)).double().view(Bt, T, Hkv, -1, D)
+    s = (x * kd.double()).sum(-1) / math.sqrt(D)                       # [Bt,T,Hkv]; the cached tokens' logits are 0
+    p = torch.exp(s) / (torch.exp(s) + n)
+    ref = p[..., None] * vd.double() + ((1 - p)[..., None] / n) * v.sum(2)[:, None]
+    away = p[..., None] * (vd.double() - ref).abs() + ((1 - p)[..., None] / n) * (v[:, None] - ref[:, :, :, None]).abs().sum(3)
+    spread = p[..., None] * vd.double().abs() + ((1 - p)[..., None] / n) * v.abs().sum(2)[:, None]
+    e = ((D + 8) * 2.0 ** -23 + (0.0 if bits == 16 else 3 * 2.0 ** -11)) * float((x * kd.double()).abs().sum(-1).max()) / math.sqrt(D)
+    tol = 2.0 ** -8 * ref.abs() + 2 * (2.0 ** -8 if bits == 16 else 2.0 ** -11) * away + (2.0 ** -10 if bits < 16 else 2.0 ** -20) * spread \
+        + 2 * math.expm1(2 * e) * away + 1e-6
+    worst = float(((out - ref[:, :, :, None]).abs() / tol[:, :, :, None]).max())
+    assert worst <= 1, worst
