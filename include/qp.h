@@ -433,6 +433,117 @@ qp_status qp_decode_attn_tree(const void* q, int T, const qp_cache* cache /* hos
                               void* out, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Rotation of queries and keys by their positions.  (The paper's models rotate them before anything it speaks of; the calls above
+ * take them rotated.)  Channels pair up, (i, i + rot_dim/2) or, interleaved, (2i, 2i+1), i < rot_dim/2; at position p
+ *   u' = m (u cos a_i - v sin a_i),   v' = m (v cos a_i + u sin a_i),   a_i = p w_i
+ * and the channels from rot_dim on stay as they are.  A rotation is a host descriptor that kernels take by value; it may be copied
+ * freely.  w_i is held as turn[i] = w_i / 2 pi in units of 2^-64, so that p w_i keeps its fraction of a turn at any position.
+ */
+typedef struct qp_rope {
+  int32_t rot_dim;      /* even, 2 .. 128; at most the head dimension of the call */
+  int32_t interleaved;
+  float factor;         /* m */
+  int32_t reserved_;
+  uint64_t turn[64];
+} qp_rope;
+/* Frequencies beyond base^(-2i/rot_dim), for contexts `factor` times as long as the trained_len positions of training (L):
+ *   PLAIN   w_i = base^(-2i/rot_dim)
+ *   LINEAR  w_i / factor
+ *   NTK     base becomes base * factor^(rot_dim/(rot_dim-2)); rot_dim > 2
+ *   YARN    w_i (1 - r_i) + (w_i / factor) r_i,  r_i = (i - lo) / (hi - lo) held to [0, 1]  (hi - lo = 0.001 where they are equal),
+ *           lo = max(floor(d(32)), 0), hi = min(ceil(d(1)), rot_dim - 1), d(x) = rot_dim ln(L / (2 pi x)) / (2 ln base);
+ *           m = 0.1 ln(factor) + 1
+ *   BANDS   (w_i / factor) (1 - s_i) + w_i s_i,  s_i = (L w_i / 2 pi - 1) / 3 held to [0, 1]
+ * m = 1 but for YARN. */
+#define QP_ROPE_PLAIN 0
+#define QP_ROPE_LINEAR 1
+#define QP_ROPE_NTK 2
+#define QP_ROPE_YARN 3
+#define QP_ROPE_BANDS 4
+/* base > 1, factor >= 1 (ignored by PLAIN), trained_len >= 1 (YARN, BANDS).  Host only. */
+qp_status qp_rope_init(int rot_dim, int interleaved, double base, int kind, double factor, int trained_len, qp_rope* out /* host, out */);
+/* The same from frequencies of the caller's own: w [rot_dim/2] (host) in radians a position, finite, |w| <= 2 pi.  Host only. */
+qp_status qp_rope_freqs(int rot_dim, int interleaved, const double* w, float factor, qp_rope* out /* host, out */);
+
+/*
+ * out = x rotated; x, out bf16 [batch, n_heads, len, head_dim] (device), with strides in elements for batch, head and token
+ * (multiples of 8; the channels of a row are contiguous), so rows of a fused projection can be taken as they are.  out may be x, with
+ * the same strides; otherwise they do not overlap, and no two rows of out do.  pos int32 [batch, len] (device), rows pos_stride
+ * apart (0: one row for the batch); any value, negative ones included.  head_dim 64 or 128, rot_dim <= head_dim.
+ * transpose != 0: by -a_i, with the same m: the gradient of the call, and where m = 1 the way back.
+ * Products and sums in 32 bits, rounded to bf16 once.
+ */
+qp_status qp_rotary(const void* x, const int64_t* x_stride /* host, 3 */, void* out, const int64_t* out_stride /* host, 3 */, int batch,
+                    int n_heads, int len, int head_dim, const int32_t* pos, int64_t pos_stride, const qp_rope* rope /* host */,
+                    int transpose, void* stream);
+
+/*
+ * A cache in pages, for sequences that grow and end on their own.  (No counterpart in the paper: what a serving process keeps before,
+ * or instead of, pruning a prompt.)  A page holds `page` consecutive tokens of one sequence, for every KV head, in 8 bits:
+ *   k_codes, v_codes  8 bits [n_pages, Hkv, page, D]     QP_E4M3: fp8 e4m3 (no infinities);  QP_INT8: -127 .. 127
+ *   k_scale, v_scale  bf16   [n_pages, Hkv]              one scale for each page and head; a number is code * scale
+ *   k_tail,  v_tail   bf16   [n_seqs, Hkv, page, D]      tokens behind a sequence's last whole page, at slot position mod page
+ * Storing a page: scale = max|x| / T rounded up to bf16 (T = 448, 127; a page of zeros: 0), code = x times the 32-bit reciprocal of
+ * the stored scale, rounded to nearest even.  Pages are only ever whole, so what a page holds does not depend on how its tokens came
+ * in; a whole page is not written again and can be in several sequences' tables (a shared beginning of two prompts).
+ * A sequence keeps its row b of the tails and of the page table as long as it lives; a row whose sequence has ended serves the next.
+ * n_seqs <= QP_MAX_SEQS, head_dim 64 or 128, page 32, 64 or 128, n_pages * Hkv * page and n_seqs * Hkv * page < 2^31 - 1024,
+ * max_pages * page < 2^31 - 1024.
+ */
+#define QP_E4M3 0
+#define QP_INT8 1
+#define QP_MAX_SEQS 2048
+typedef struct qp_paged {
+  int32_t n_seqs, n_q_heads, n_kv_heads, head_dim, format, page;
+  int32_t n_pages;       /* in the pool */
+  int32_t max_pages;     /* entries in a row of the page table */
+  size_t codes_bytes, scale_bytes, tail_bytes; /* of the key arrays; the value arrays have the same */
+  void *k_codes, *v_codes, *k_scale, *v_scale, *k_tail, *v_tail; /* device */
+} qp_paged;
+/* Fills the shape fields and byte sizes of *out and sets the six pointers to NULL.  Host only. */
+qp_status qp_paged_layout(int n_seqs, int n_q_heads, int n_kv_heads, int head_dim, int format, int page, int n_pages, int max_pages,
+                          qp_paged* out /* host, out */);
+
+/*
+ * One step of a batch, the same for all layers: sequence b gets start[b+1] - start[b] new tokens (none, one, or a chunk of its
+ * prompt), which are rows start[b] .. start[b+1]-1 of the step's arrays and stand at positions len[b], len[b]+1, ...  The caller adds
+ * them to len when all layers are done.  The arrays are read on the device, so a captured step serves every later one with the same
+ * n_tokens and max_new (rows of the arrays that are no sequence's are not looked at, and left as they are in outputs).
+ * A sequence whose numbers do not belong together (rows outside 0 .. n_tokens-1, more than max_new new tokens, a negative len, more
+ * positions than its row of the page table) is left out, nothing of it is written; a page number outside the pool is not written to,
+ * and makes the attention rows that would read it NaN.  len[b] may be set back only to where b's last whole page ends or behind.
+ */
+typedef struct qp_step {
+  int32_t n_tokens;      /* rows of the step's arrays */
+  int32_t max_new;       /* no sequence has more new tokens */
+  const int32_t* start;  /* device [n_seqs + 1] */
+  const int32_t* len;    /* device [n_seqs] */
+  const int32_t* pages;  /* device [n_seqs, max_pages]: page i of b's tokens i*page .. (i+1)*page-1 */
+} qp_step;
+
+/*
+ * Takes the step's new tokens into one layer's cache: k_new, v_new bf16 rows [n_tokens, Hkv, D] (device), k_stride, v_stride elements
+ * from a token's row to the next (multiples of 8, at least Hkv*D).  Keys are rotated on the way unless rope is NULL, at the positions
+ * pos int32 [n_tokens] (device) or, if that is NULL, at those of the tokens in their sequences, and rounded to bf16 before anything
+ * else is made of them.  q (NULL: none; needs rope): the step's queries, bf16 rows [n_tokens, Hq, D], q_stride apart, rotated into q_out
+ * bf16 [n_tokens, Hq, D], contiguous; q_out may be q if that is contiguous, too.  One launch.
+ */
+qp_status qp_paged_append(const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, const qp_paged* cache /* host */,
+                          const qp_step* step /* host */, const qp_rope* rope /* host or NULL */, const int32_t* pos, const void* q,
+                          int64_t q_stride, void* q_out, void* stream);
+
+/*
+ * Attention of the step's tokens, after qp_paged_append has taken them in: the token at position p of its sequence sees the tokens at
+ * positions <= p,   out[r,h,:] = softmax_t(q[r,h].K[t] / sqrt(D)) V.   q bf16 rows [n_tokens, Hq, D] (device), q_stride elements apart;
+ * out bf16 [n_tokens, Hq, D], contiguous.  Magnitudes are free: queries and pages meet the tensor cores scaled by powers of two.
+ * workspace: its contents are irrelevant; calls that may run at the same time must not share it.
+ * Bounded waits as for qp_window_scores; one that runs out makes the rows that hang on it NaN.
+ */
+size_t qp_paged_attn_workspace_bytes(const qp_paged* cache /* host */, int n_tokens, int max_new);
+qp_status qp_paged_attn(const void* q, int64_t q_stride, const qp_paged* cache /* host */, const qp_step* step /* host */, void* out,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Debug build only (libqp_checked.so, compiled with -DQP_CHECKED; no counterpart in the paper).  In that build
  * every index a kernel reads from DEVICE memory and then uses as an address (the kept positions given to the
  * gather / quantize kernels, the side lists' tile pointers and entries), and every output position the top-k kernels

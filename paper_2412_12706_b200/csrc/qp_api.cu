@@ -10,6 +10,7 @@
 
 #include "qp_common.cuh"
 #include "qp_mma.cuh"
+#include "qp_paged.cuh"
 
 using namespace qp;
 
@@ -810,6 +811,191 @@ qp_status qp_decode_attn_tree(const void* q, int T, const qp_cache* cache, const
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   cache_written(st);                                          // plain stream order here and for the next decode call
   return launch_tree(a, workspace, st) == cudaSuccess ? QP_OK : QP_ERR_CUDA;
+}
+
+// ---- rotation by position, and the paged cache in 8 bits ------------------------------------------
+
+static qp_status check_rope(const qp_rope* r, int head_dim) {
+  if (!r || r->rot_dim < 2 || r->rot_dim % 2 != 0 || r->rot_dim > 128) return QP_ERR_INVALID_ARG;
+  return r->rot_dim > head_dim ? QP_ERR_INVALID_ARG : QP_OK;
+}
+
+qp_status qp_rope_freqs(int rot_dim, int interleaved, const double* w, float factor, qp_rope* out) {
+  if (!w || !out || rot_dim < 2 || rot_dim % 2 != 0 || rot_dim > 128 || !std::isfinite(factor)) return QP_ERR_INVALID_ARG;
+  const long double turn = 6.283185307179586476925286766559005768L;
+  qp_rope r;
+  memset(&r, 0, sizeof(r));
+  r.rot_dim = rot_dim;
+  r.interleaved = interleaved != 0;
+  r.factor = factor;
+  for (int i = 0; i < rot_dim / 2; ++i) {
+    if (!(std::fabs(w[i]) <= 6.2831853071795865)) return QP_ERR_INVALID_ARG;
+    const long double part = w[i] / turn;                       // |part| <= 1: whole turns count for nothing
+    const long double f = (part - std::floor(part)) * 18446744073709551616.0L;
+    r.turn[i] = f >= 18446744073709551615.5L ? 0 : (uint64_t)(f + 0.5L);
+  }
+  *out = r;
+  return QP_OK;
+}
+
+qp_status qp_rope_init(int rot_dim, int interleaved, double base, int kind, double factor, int trained_len, qp_rope* out) {
+  if (!out || rot_dim < 2 || rot_dim % 2 != 0 || rot_dim > 128 || !(base > 1.0) || !std::isfinite(base)) return QP_ERR_INVALID_ARG;
+  if (kind < QP_ROPE_PLAIN || kind > QP_ROPE_BANDS) return QP_ERR_INVALID_ARG;
+  if (kind != QP_ROPE_PLAIN && (!(factor >= 1.0) || !std::isfinite(factor))) return QP_ERR_INVALID_ARG;
+  if ((kind == QP_ROPE_YARN || kind == QP_ROPE_BANDS) && trained_len < 1) return QP_ERR_INVALID_ARG;
+  if (kind == QP_ROPE_NTK) {
+    if (rot_dim == 2) return QP_ERR_INVALID_ARG;
+    base *= std::pow(factor, (double)rot_dim / (rot_dim - 2));
+  }
+  const double pi2 = 6.283185307179586;
+  double lo = 0, hi = 0;
+  if (kind == QP_ROPE_YARN) {
+    auto pair = [&](double turns) { return rot_dim * std::log(trained_len / (turns * pi2)) / (2 * std::log(base)); };
+    lo = std::max(std::floor(pair(32)), 0.0);
+    hi = std::min(std::ceil(pair(1)), rot_dim - 1.0);
+    if (hi == lo) hi += 0.001;
+  }
+  double w[64];
+  for (int i = 0; i < rot_dim / 2; ++i) {
+    w[i] = std::pow(base, -2.0 * i / rot_dim);
+    if (kind == QP_ROPE_LINEAR) w[i] /= factor;
+    double keep = 1;                                            // share of the frequency that is not stretched
+    if (kind == QP_ROPE_YARN) keep = 1 - std::min(1.0, std::max(0.0, (i - lo) / (hi - lo)));
+    if (kind == QP_ROPE_BANDS) keep = std::min(1.0, std::max(0.0, (trained_len * w[i] / pi2 - 1) / 3));
+    if (keep != 1) w[i] = w[i] * keep + w[i] / factor * (1 - keep);
+  }
+  return qp_rope_freqs(rot_dim, interleaved, w, kind == QP_ROPE_YARN ? (float)(0.1 * std::log(factor) + 1) : 1.f, out);
+}
+
+qp_status qp_rotary(const void* x, const int64_t* x_stride, void* out, const int64_t* out_stride, int batch, int n_heads, int len,
+                    int head_dim, const int32_t* pos, int64_t pos_stride, const qp_rope* rope, int transpose, void* stream) {
+  if (!x || !x_stride || !out || !out_stride || !pos || batch < 1 || n_heads < 1 || len < 1 || head_dim < 1 || pos_stride < 0)
+    return QP_ERR_INVALID_ARG;
+  if (head_dim != 64 && head_dim != 128) return QP_ERR_UNSUPPORTED;
+  const qp_status s = check_rope(rope, head_dim);
+  if (s != QP_OK) return s;
+  RotaryArgs a{};
+  for (int i = 0; i < 3; ++i) {
+    if (x_stride[i] < 0 || out_stride[i] < 0) return QP_ERR_INVALID_ARG;
+    if (x_stride[i] % 8 != 0 || out_stride[i] % 8 != 0) return QP_ERR_ALIGNMENT;
+    if (x == out && x_stride[i] != out_stride[i]) return QP_ERR_INVALID_ARG;
+    a.xs[i] = x_stride[i];
+    a.os[i] = out_stride[i];
+  }
+  if (!aligned16(x) || !aligned16(out) || !aligned4(pos)) return QP_ERR_ALIGNMENT;
+  if (n_heads > 1 << 16) return QP_ERR_UNSUPPORTED;
+  a.x = static_cast<const uint16_t*>(x); a.out = static_cast<uint16_t*>(out);
+  a.pos = pos; a.ps = pos_stride;
+  a.Bt = batch; a.H = n_heads; a.L = len; a.D = head_dim; a.transpose = transpose != 0;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cache_written(st);                                          // the next decode call may read what is written here
+  return launch_rotary(a, *rope, st) == cudaSuccess ? QP_OK : QP_ERR_CUDA;
+}
+
+static qp_status check_paged(const qp_paged* c, bool need_ptrs) {
+  if (!c) return QP_ERR_INVALID_ARG;
+  qp_status s = check_shape(1, c->n_q_heads, c->n_kv_heads, c->head_dim);
+  if (s != QP_OK) return s;
+  if (c->n_seqs < 1 || c->n_pages < 1 || c->max_pages < 1) return QP_ERR_INVALID_ARG;
+  if ((c->format != QP_E4M3 && c->format != QP_INT8) || !ok_group(c->page) || c->n_seqs > QP_MAX_SEQS) return QP_ERR_UNSUPPORTED;
+  const long long most = 0x7fffffffLL - 1024, rows = (long long)c->n_kv_heads * c->page;
+  if (rows > most || c->n_pages > most / rows || c->n_seqs > most / rows || c->max_pages > most / c->page) return QP_ERR_UNSUPPORTED;
+  if (need_ptrs) {
+    void* const all[6] = {c->k_codes, c->v_codes, c->k_scale, c->v_scale, c->k_tail, c->v_tail};
+    for (void* p : all)
+      if (!p) return QP_ERR_INVALID_ARG;
+    for (void* p : all)
+      if (!aligned16(p)) return QP_ERR_ALIGNMENT;
+  }
+  return QP_OK;
+}
+
+qp_status qp_paged_layout(int n_seqs, int n_q_heads, int n_kv_heads, int head_dim, int format, int page, int n_pages, int max_pages,
+                          qp_paged* out) {
+  if (!out) return QP_ERR_INVALID_ARG;
+  qp_paged c;
+  memset(&c, 0, sizeof(c));
+  c.n_seqs = n_seqs; c.n_q_heads = n_q_heads; c.n_kv_heads = n_kv_heads; c.head_dim = head_dim;
+  c.format = format; c.page = page; c.n_pages = n_pages; c.max_pages = max_pages;
+  const qp_status s = check_paged(&c, false);
+  if (s != QP_OK) return s;
+  c.codes_bytes = (size_t)n_pages * n_kv_heads * page * head_dim;
+  c.scale_bytes = (size_t)n_pages * n_kv_heads * 2;
+  c.tail_bytes = (size_t)n_seqs * n_kv_heads * page * head_dim * 2;
+  *out = c;
+  return QP_OK;
+}
+
+static qp_status check_step(const qp_paged& c, const qp_step* t, StepView* v) {
+  if (!t || !t->start || !t->len || !t->pages || t->n_tokens < 1 || t->max_new < 1 || t->max_new > t->n_tokens) return QP_ERR_INVALID_ARG;
+  if (!aligned4(t->start) || !aligned4(t->len) || !aligned4(t->pages)) return QP_ERR_ALIGNMENT;
+  *v = StepView{t->start, t->len, t->pages, c.n_seqs, t->n_tokens, t->max_new, c.max_pages, c.page, c.n_pages};
+  return QP_OK;
+}
+
+qp_status qp_paged_append(const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, const qp_paged* cache,
+                          const qp_step* step, const qp_rope* rope, const int32_t* pos, const void* q, int64_t q_stride, void* q_out,
+                          void* stream) {
+  if (!k_new || !v_new || (q && (!q_out || !rope))) return QP_ERR_INVALID_ARG;
+  qp_status s = check_paged(cache, true);
+  if (s != QP_OK) return s;
+  const qp_paged& c = *cache;
+  AppendArgs a{};
+  s = check_step(c, step, &a.s);
+  if (s == QP_OK && rope) s = check_rope(rope, c.head_dim);
+  if (s != QP_OK) return s;
+  const int64_t kv = (int64_t)c.n_kv_heads * c.head_dim, qw = (int64_t)c.n_q_heads * c.head_dim;
+  if (k_stride < kv || v_stride < kv || (q && (q_stride < qw || (q == q_out && q_stride != qw)))) return QP_ERR_INVALID_ARG;
+  if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(q) || !aligned16(q_out) || !aligned4(pos) || k_stride % 8 || v_stride % 8 ||
+      (q && q_stride % 8))
+    return QP_ERR_ALIGNMENT;
+  a.k = static_cast<const uint16_t*>(k_new); a.v = static_cast<const uint16_t*>(v_new);
+  a.q = static_cast<const uint16_t*>(q); a.q_out = static_cast<uint16_t*>(q_out);
+  a.ks = k_stride; a.vs = v_stride; a.qs = q_stride;
+  a.pos = pos;
+  a.kc = static_cast<uint8_t*>(c.k_codes); a.vc = static_cast<uint8_t*>(c.v_codes);
+  a.k_scale = static_cast<uint16_t*>(c.k_scale); a.v_scale = static_cast<uint16_t*>(c.v_scale);
+  a.k_tail = static_cast<uint16_t*>(c.k_tail); a.v_tail = static_cast<uint16_t*>(c.v_tail);
+  a.Hq = c.n_q_heads; a.Hkv = c.n_kv_heads; a.D = c.head_dim; a.format = c.format;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cache_written(st);
+  return launch_paged_append(a, rope, st) == cudaSuccess ? QP_OK : QP_ERR_CUDA;
+}
+
+static qp_status check_attn(const qp_paged& c, int n_tokens, int max_new) {
+  if (n_tokens < 1 || max_new < 1 || max_new > n_tokens) return QP_ERR_INVALID_ARG;
+  return paged_attn_fits(c.n_seqs, n_tokens, max_new, c.n_q_heads, c.n_kv_heads, (long long)c.max_pages * c.page) ? QP_OK
+                                                                                                                  : QP_ERR_UNSUPPORTED;
+}
+
+size_t qp_paged_attn_workspace_bytes(const qp_paged* cache, int n_tokens, int max_new) {
+  if (check_paged(cache, false) != QP_OK || check_attn(*cache, n_tokens, max_new) != QP_OK) return 0;
+  return paged_attn_workspace(cache->n_seqs, n_tokens, max_new, cache->n_q_heads, cache->n_kv_heads, cache->head_dim);
+}
+
+qp_status qp_paged_attn(const void* q, int64_t q_stride, const qp_paged* cache, const qp_step* step, void* out, void* workspace,
+                        size_t workspace_bytes, void* stream) {
+  if (!q || !out || !workspace) return QP_ERR_INVALID_ARG;
+  qp_status s = check_paged(cache, true);
+  if (s != QP_OK) return s;
+  const qp_paged& c = *cache;
+  PagedAttnArgs a{};
+  s = check_step(c, step, &a.s);
+  if (s == QP_OK) s = check_attn(c, step->n_tokens, step->max_new);
+  if (s != QP_OK) return s;
+  if (q_stride < (int64_t)c.n_q_heads * c.head_dim) return QP_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(out) || !aligned16(workspace) || q_stride % 8) return QP_ERR_ALIGNMENT;
+  if (workspace_bytes < paged_attn_workspace(c.n_seqs, step->n_tokens, step->max_new, c.n_q_heads, c.n_kv_heads, c.head_dim))
+    return QP_ERR_WORKSPACE;
+  a.q = static_cast<const uint16_t*>(q); a.qs = q_stride;
+  a.out = static_cast<uint16_t*>(out);
+  a.kc = static_cast<const uint8_t*>(c.k_codes); a.vc = static_cast<const uint8_t*>(c.v_codes);
+  a.k_scale = static_cast<const uint16_t*>(c.k_scale); a.v_scale = static_cast<const uint16_t*>(c.v_scale);
+  a.k_tail = static_cast<const uint16_t*>(c.k_tail); a.v_tail = static_cast<const uint16_t*>(c.v_tail);
+  a.Hq = c.n_q_heads; a.Hkv = c.n_kv_heads; a.D = c.head_dim; a.format = c.format;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cache_written(st);                                          // plain stream order here and for the next decode call
+  return launch_paged_attn(a, workspace, st) == cudaSuccess ? QP_OK : QP_ERR_CUDA;
 }
 
 }  // extern "C"

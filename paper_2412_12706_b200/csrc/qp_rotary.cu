@@ -1,0 +1,353 @@
+// Rotation by position (qp_rotary) and the appends to a paged cache in 8 bits (qp_paged_append).
+//
+// A pair (u, v) of channels turns by the angle a = pos * w:  u' = m (u cos a - v sin a),  v' = m (v cos a + u sin a).  What counts of
+// pos * w is its fraction of a full turn, so w is held as w / 2 pi in units of 2^-64 and the product taken in 64-bit integers, whose
+// overflow drops the whole turns: exact to 2^-33 of a turn at any 31-bit position, where a 32-bit float angle is off by 0.06 at a
+// million.
+#include <algorithm>
+#include <cfloat>
+
+#include "qp_paged.cuh"
+
+namespace qp {
+
+namespace {
+
+constexpr int THREADS = 128;
+constexpr int ROT_UNITS = 4, ROT_TOKENS = 32;                   // rotation: units in flight a thread, most tokens a block
+
+// how the channels pair up: neighbours; i with i + rot/2 where rot/2 is a whole number of 16-byte vectors; the same where it is not
+enum : int { PAIR_NEXT = 0, PAIR_HALF = 1, PAIR_ODD = 2 };
+inline int pairing(const qp_rope& r) { return r.interleaved ? PAIR_NEXT : r.rot_dim % 16 == 0 ? PAIR_HALF : PAIR_ODD; }
+
+// cosine and sine, times m, of pair `turn` at position pos
+__device__ __forceinline__ float2 cos_sin(uint64_t turn, int pos, float m) {
+  const uint64_t part = turn * (uint64_t)(int64_t)pos;
+  float s, c;
+  sincospif((float)(int)(uint32_t)(part >> 32) * 0x1p-31f, &s, &c);
+  return make_float2(c * m, s * m);
+}
+
+// A unit is 16 channels of a row: two vectors of 8, numbers c0 and c1, such that pairs of PAIR_NEXT and PAIR_HALF lie inside it.
+__device__ __forceinline__ void unit_vectors(int mode, int rot, int u, int& c0, int& c1) {
+  const int half = rot >> 4;                                    // vectors in half of the rotated part
+  const bool across = mode == PAIR_HALF && u < half;
+  c0 = across ? u : 2 * u;
+  c1 = across ? u + half : 2 * u + 1;
+}
+// Rotates a unit whose vectors are a and b.  cs(i): cosine and sine of pair i.  row: the row itself, which PAIR_ODD reads again.
+template <int MODE, typename CS>
+__device__ __forceinline__ void rotate_unit(uint4& a, uint4& b, int u, int rot, const uint16_t* row, CS cs) {
+  uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  if (MODE == PAIR_NEXT) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int p = 8 * u + i;
+      if (2 * p < rot) {
+        const float2 t = cs(p);
+        const float x = bf16lo(w[i]), y = bf16hi(w[i]);
+        w[i] = pack_bf16x2(x * t.x - y * t.y, y * t.x + x * t.y);
+      }
+    }
+  } else if (MODE == PAIR_HALF) {
+    if (16 * u < rot) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float2 t0 = cs(8 * u + 2 * i), t1 = cs(8 * u + 2 * i + 1);
+        const float x0 = bf16lo(w[i]), x1 = bf16hi(w[i]), y0 = bf16lo(w[4 + i]), y1 = bf16hi(w[4 + i]);
+        w[i] = pack_bf16x2(x0 * t0.x - y0 * t0.y, x1 * t1.x - y1 * t1.y);
+        w[4 + i] = pack_bf16x2(y0 * t0.x + x0 * t0.y, y1 * t1.x + x1 * t1.y);
+      }
+    }
+  } else {
+    const int half = rot >> 1;
+#pragma unroll 1
+    for (int i = 0; i < 8; ++i) {
+      float o[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int d = 16 * u + 2 * i + j;
+        const float x = bf16_bits_to_f32(row[d]);
+        o[j] = x;
+        if (d < rot) {
+          const float2 t = cs(d < half ? d : d - half);
+          const float y = bf16_bits_to_f32(row[d < half ? d + half : d - half]);
+          o[j] = x * t.x + (d < half ? -y : y) * t.y;
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (k == i) w[k] = pack_bf16x2(o[0], o[1]);
+    }
+  }
+  a = make_uint4(w[0], w[1], w[2], w[3]);
+  b = make_uint4(w[4], w[5], w[6], w[7]);
+}
+
+// ---- rotation alone, and of a step's queries.  HBM-bound: 4 bytes a number.  A block takes up to 32 tokens of all heads, so that
+// the cosines and sines are computed once a token and read from shared memory by every head.
+template <int MODE, typename OK>
+__device__ __forceinline__ void rotate_tokens(const uint16_t* x, long long xh, long long xl, uint16_t* out, long long oh, long long ol,
+                                              int n, int H, int lgu, int rot, const float2* table, OK ok) {
+  const int units = (n * H) << lgu, half = rot >> 1;            // 2^lgu units a row
+  for (int base = 0; base < units; base += THREADS * ROT_UNITS) {
+    uint4 a[ROT_UNITS], b[ROT_UNITS];
+    const uint16_t* src[ROT_UNITS];
+    uint16_t* dst[ROT_UNITS];
+    int tok[ROT_UNITS], c0[ROT_UNITS], c1[ROT_UNITS], u[ROT_UNITS];
+    bool on[ROT_UNITS];
+#pragma unroll
+    for (int k = 0; k < ROT_UNITS; ++k) {
+      const int i = base + k * THREADS + threadIdx.x, r = i >> lgu, t = r / H, h = r - t * H;
+      u[k] = i & ((1 << lgu) - 1);
+      tok[k] = t;
+      unit_vectors(MODE, rot, u[k], c0[k], c1[k]);
+      src[k] = x + h * xh + t * xl;
+      dst[k] = out + h * oh + t * ol;
+      on[k] = i < units && ok(t);
+      if (on[k]) {
+        a[k] = *reinterpret_cast<const uint4*>(src[k] + 8 * c0[k]);
+        b[k] = *reinterpret_cast<const uint4*>(src[k] + 8 * c1[k]);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < ROT_UNITS; ++k)
+      if (on[k]) rotate_unit<MODE>(a[k], b[k], u[k], rot, src[k], [&](int p) { return table[tok[k] * half + p]; });
+    if (MODE == PAIR_ODD) __syncwarp();                         // in place: a row's units are one warp's, all read before one writes
+#pragma unroll
+    for (int k = 0; k < ROT_UNITS; ++k)
+      if (on[k]) {
+        *reinterpret_cast<uint4*>(dst[k] + 8 * c0[k]) = a[k];
+        *reinterpret_cast<uint4*>(dst[k] + 8 * c1[k]) = b[k];
+      }
+  }
+}
+// tokens a block takes: four units for every thread, so that short calls spread over the SMs, but no more than the table holds
+int tokens_a_block(int H, int D) { return std::max(1, std::min(ROT_TOKENS, THREADS * ROT_UNITS / (H * (D / 16)))); }
+
+template <int MODE>
+__global__ void __launch_bounds__(THREADS)
+rotary_kernel(const __grid_constant__ RotaryArgs a, const __grid_constant__ qp_rope rope, int tokens) {
+  __shared__ float2 table[ROT_TOKENS * 64];
+  chain_enter();
+  const int t0 = blockIdx.x * tokens, n = min(tokens, a.L - t0), half = rope.rot_dim >> 1;
+  for (int b = blockIdx.y; b < a.Bt; b += gridDim.y) {
+    for (int i = threadIdx.x; i < n * half; i += THREADS) {
+      const int t = i / half, p = i - t * half;
+      float2 cs = cos_sin(rope.turn[p], __ldg(a.pos + b * a.ps + t0 + t), rope.factor);
+      if (a.transpose) cs.y = -cs.y;
+      table[i] = cs;
+    }
+    __syncthreads();
+    rotate_tokens<MODE>(a.x + b * a.xs[0] + t0 * a.xs[2], a.xs[1], a.xs[2], a.out + b * a.os[0] + t0 * a.os[2], a.os[1], a.os[2], n,
+                        a.H, a.D == 128 ? 3 : 2, rope.rot_dim, table, [](int) { return true; });
+    __syncthreads();
+  }
+}
+
+// ---- appends
+
+// largest b < n for which f(start[b]) is not above x, 0 if there is none
+template <typename F>
+__device__ __forceinline__ int last_at_most(const int32_t* start, int n, int x, F f) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (f(__ldg(start + mid)) <= x) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+// codes of 8 numbers
+__device__ __forceinline__ uint2 codes8(const uint4& v, float inv, bool e4m3) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  uint32_t o[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const float x0 = __fmul_rn(bf16lo(w[2 * i]), inv), x1 = __fmul_rn(bf16hi(w[2 * i]), inv);
+    const float x2 = __fmul_rn(bf16lo(w[2 * i + 1]), inv), x3 = __fmul_rn(bf16hi(w[2 * i + 1]), inv);
+    if (e4m3) {
+      uint16_t lo, hi;
+      asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;\n" : "=h"(lo) : "f"(x1), "f"(x0));
+      asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;\n" : "=h"(hi) : "f"(x3), "f"(x2));
+      o[i] = lo | (uint32_t)hi << 16;
+    } else {
+      auto code = [](float x) { return (uint32_t)__float2int_rn(fminf(fmaxf(x, -127.f), 127.f)) & 0xffu; };
+      o[i] = code(x0) | code(x1) << 8 | code(x2) << 16 | code(x3) << 24;
+    }
+  }
+  return make_uint2(o[0], o[1]);
+}
+__device__ __forceinline__ uint32_t abs_max2(uint32_t m, const uint4& v) {
+  m = __vmaxu2(m, v.x & 0x7fff7fffu);
+  m = __vmaxu2(m, v.y & 0x7fff7fffu);
+  m = __vmaxu2(m, v.z & 0x7fff7fffu);
+  return __vmaxu2(m, v.w & 0x7fff7fffu);
+}
+
+// A block is one of three kinds:
+//   edge    (sequence, head, keys or values): the page that waiting rows and new ones complete together, then the new rows that wait
+//   whole   (whole page of new tokens, head, keys or values)
+//   query   some tokens' queries
+// The edge block reads the waiting rows it uses up before it writes new ones in their place.  A page's numbers stay in registers
+// between the search for the largest magnitude and the rounding to codes: page * D / 16 / 128 = UNITS units of 16 channels a thread.
+// The host does not know the sequences' lengths, so it launches a whole-page block for every `page` rows of the step: unit u belongs
+// to the last sequence b with start[b] / page <= u, which has at least as many of them as pages begin and end in its new tokens.
+template <int UNITS, int MODE>
+__global__ void __launch_bounds__(THREADS)
+append_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ qp_rope rope, int edge_blocks, int page_blocks, int tokens) {
+  __shared__ float2 table[ROT_TOKENS * 64];
+  __shared__ int s_pos[ROT_TOKENS];
+  __shared__ uint32_t s_max[THREADS / 32];
+  chain_enter();
+  const int bid = blockIdx.x, tid = threadIdx.x;
+  const StepView& s = a.s;
+  const int D = a.D, lgu = D == 128 ? 3 : 2, page = s.page, lgp = 31 - __clz(page), rot = rope.rot_dim;
+
+  if (bid >= page_blocks) {                                     // queries
+    const int t0 = (bid - page_blocks) * tokens, n = min(tokens, s.n_tokens - t0), half = rot >> 1;
+    bool in = false;
+    if (tid < n) {
+      const int r = t0 + tid, b = last_at_most(s.start, s.n_seqs, r, [](int x) { return x; });
+      const Seq q = seq_of(s, b);
+      in = r >= q.row0 && r < q.row0 + q.n;
+      s_pos[tid] = a.pos ? __ldg(a.pos + r) : q.len + r - q.row0;
+    }
+    __shared__ uint32_t s_in;                                   // tokens that are a sequence's
+    const uint32_t some = __ballot_sync(0xffffffffu, in);
+    if (tid == 0) s_in = some;
+    __syncthreads();
+    for (int i = tid; i < n * half; i += THREADS) {
+      const int t = i / half, p = i - t * half;
+      table[i] = cos_sin(rope.turn[p], s_pos[t], rope.factor);
+    }
+    __syncthreads();
+    const uint32_t mine = s_in;
+    rotate_tokens<MODE>(a.q + t0 * a.qs, D, a.qs, a.q_out + (size_t)t0 * a.Hq * D, D, (long long)a.Hq * D, n, a.Hq, lgu, rot, table,
+                        [&](int t) { return (mine >> t & 1u) != 0; });
+    return;
+  }
+
+  const bool edge = bid < edge_blocks;
+  const int i = edge ? bid : bid - edge_blocks;
+  const bool keys = (i & 1) == 0;
+  const int which = (i >> 1) / a.Hkv, h = (i >> 1) - which * a.Hkv;
+  int b = which, pg;                                            // sequence, and the page to write (-1: none)
+  Seq q;
+  if (edge) {
+    q = seq_of(s, b);
+    pg = q.len >> lgp;
+    if (q.len == pg << lgp || q.len + q.n < (pg + 1) << lgp) pg = -1;
+  } else {
+    b = last_at_most(s.start, s.n_seqs, which, [&](int x) { return x >> lgp; });
+    q = seq_of(s, b);
+    pg = ((q.len + page - 1) >> lgp) + which - (q.row0 >> lgp);
+    if (which < q.row0 >> lgp || (pg + 1) << lgp > q.len + q.n) return;
+  }
+  if (q.n == 0) return;
+  const uint16_t* rows = (keys ? a.k : a.v) + (size_t)h * D;
+  const long long stride = keys ? a.ks : a.vs;
+  uint16_t* tail = (keys ? a.k_tail : a.v_tail) + (((size_t)b * a.Hkv + h) << lgp) * D;
+  // unit u of the row at position p of the sequence; new rows of keys are rotated
+  auto load = [&](int p, int u, uint4& x, uint4& y, int& c0, int& c1) {
+    const bool fresh = p >= q.len;
+    const int r = q.row0 + p - q.len;
+    const uint16_t* row = fresh ? rows + r * stride : tail + (p & (page - 1)) * D;
+    unit_vectors(MODE, rot, u, c0, c1);
+    x = *reinterpret_cast<const uint4*>(row + 8 * c0);
+    y = *reinterpret_cast<const uint4*>(row + 8 * c1);
+    if (fresh && keys && rot) {
+      const int at = a.pos ? __ldg(a.pos + r) : p;
+      rotate_unit<MODE>(x, y, u, rot, row, [&](int j) { return cos_sin(rope.turn[j], at, rope.factor); });
+    }
+  };
+  if (pg >= 0) {
+    const int id = page_of(s, b, pg);
+    uint4 x[UNITS], y[UNITS];
+    uint32_t m = 0u;
+#pragma unroll
+    for (int k = 0; k < UNITS; ++k) {
+      const int j = tid + k * THREADS;
+      int c0, c1;
+      load((pg << lgp) + (j >> lgu), j & ((1 << lgu) - 1), x[k], y[k], c0, c1);
+      m = abs_max2(abs_max2(m, x[k]), y[k]);
+    }
+    m = max(m & 0xffffu, m >> 16);
+    m = __reduce_max_sync(0xffffffffu, m);
+    if ((tid & 31) == 0) s_max[tid >> 5] = m;
+    __syncthreads();
+    m = max(max(s_max[0], s_max[1]), max(s_max[2], s_max[3]));
+    // the scale is rounded up to bf16, so that no code is cut off; a number that is none makes the whole page so
+    const bool e4m3 = a.format == QP_E4M3;
+    const float top = __uint_as_float(m << 16);
+    const uint32_t sb = m > 0x7f80u ? 0x7fc0u : (__float_as_uint(__fdiv_rn(top, e4m3 ? 448.f : 127.f)) + 0xffffu) >> 16;
+    const float sc = __uint_as_float(sb << 16), inv = sc == 0.f ? 0.f : fminf(__fdiv_rn(1.f, sc), FLT_MAX);
+    if (id >= 0) {
+      const size_t ph = (size_t)id * a.Hkv + h;
+      uint8_t* codes = (keys ? a.kc : a.vc) + (ph << lgp) * D;
+      if (tid == 0) (keys ? a.k_scale : a.v_scale)[ph] = (uint16_t)sb;
+#pragma unroll
+      for (int k = 0; k < UNITS; ++k) {
+        const int j = tid + k * THREADS;
+        int c0, c1;
+        unit_vectors(MODE, rot, j & ((1 << lgu) - 1), c0, c1);
+        uint8_t* row = codes + (j >> lgu) * D;
+        *reinterpret_cast<uint2*>(row + 8 * c0) = codes8(x[k], inv, e4m3);
+        *reinterpret_cast<uint2*>(row + 8 * c1) = codes8(y[k], inv, e4m3);
+      }
+    }
+  }
+  if (edge) {                                                   // (the barrier above: every waiting row of the page has been read)
+    const int end = q.len + q.n, lo = max(q.len, end >> lgp << lgp);
+    for (int j = tid; j < (end - lo) << lgu; j += THREADS) {
+      const int p = lo + (j >> lgu);
+      uint4 x, y;
+      int c0, c1;
+      load(p, j & ((1 << lgu) - 1), x, y, c0, c1);
+      uint16_t* row = tail + (p & (page - 1)) * D;
+      *reinterpret_cast<uint4*>(row + 8 * c0) = x;
+      *reinterpret_cast<uint4*>(row + 8 * c1) = y;
+    }
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_rotary(const RotaryArgs& a, const qp_rope& rope, cudaStream_t st) {
+  const int tokens = tokens_a_block(a.H, a.D);
+  const dim3 grid((a.L + tokens - 1) / tokens, std::min(a.Bt, 65535));
+  switch (pairing(rope)) {
+    case PAIR_NEXT: return launch_chained(rotary_kernel<PAIR_NEXT>, grid, dim3(THREADS), 0, st, a, rope, tokens);
+    case PAIR_HALF: return launch_chained(rotary_kernel<PAIR_HALF>, grid, dim3(THREADS), 0, st, a, rope, tokens);
+    default: return launch_chained(rotary_kernel<PAIR_ODD>, grid, dim3(THREADS), 0, st, a, rope, tokens);
+  }
+}
+
+cudaError_t launch_paged_append(const AppendArgs& a, const qp_rope* rope_or_null, cudaStream_t st) {
+  qp_rope rope{};                                               // none: nothing is rotated
+  if (rope_or_null) rope = *rope_or_null;
+  const int units = a.s.page * a.D / 16 / THREADS, tokens = tokens_a_block(a.Hq, a.D);
+  const long long edge = 2LL * a.s.n_seqs * a.Hkv, whole = 2LL * (a.s.n_tokens / a.s.page) * a.Hkv;
+  const long long queries = a.q ? (a.s.n_tokens + tokens - 1) / tokens : 0;
+  if (edge + whole + queries > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
+  const dim3 grid((unsigned)(edge + whole + queries));
+#define QP_APPEND(U, M) \
+  return launch_chained(append_kernel<U, M>, grid, dim3(THREADS), 0, st, a, rope, (int)edge, (int)(edge + whole), tokens)
+#define QP_APPEND_M(U)            \
+  switch (pairing(rope)) {        \
+    case PAIR_NEXT: QP_APPEND(U, PAIR_NEXT); \
+    case PAIR_HALF: QP_APPEND(U, PAIR_HALF); \
+    default: QP_APPEND(U, PAIR_ODD);         \
+  }
+  switch (units) {
+    case 1: QP_APPEND_M(1)
+    case 2: QP_APPEND_M(2)
+    case 4: QP_APPEND_M(4)
+    case 8: QP_APPEND_M(8)
+    default: return cudaErrorInvalidValue;
+  }
+#undef QP_APPEND_M
+#undef QP_APPEND
+}
+
+}  // namespace qp

@@ -20,6 +20,7 @@ LIB_PATH = os.environ.get("QP_LIBRARY") or os.path.join(_HERE, "libqp.so")
 QP_OK = 0
 QP_MAX_LAYERS = 128
 QP_MAX_DRAFTS = 64
+QP_MAX_SEQS = 2048
 STATUS_NAMES = {0: "QP_OK", 1: "QP_ERR_INVALID_ARG", 2: "QP_ERR_UNSUPPORTED", 3: "QP_ERR_BUDGET",
                 4: "QP_ERR_WORKSPACE", 5: "QP_ERR_ALIGNMENT", 6: "QP_ERR_CUDA"}
 
@@ -30,7 +31,9 @@ EXPORTS = ["qp_status_string", "qp_n_keep", "qp_cache_layout", "qp_compress_work
            "qp_decode_attn_tail_layers", "qp_compress_layers", "qp_decode_overlap", "qp_gather_quantize_ex",
            "qp_decode_attn_ex", "qp_decode_attn_layers_ex", "qp_head_budgets", "qp_head_budgets_workspace_bytes", "qp_debug_check",
            "qp_prompt_weights", "qp_prompt_weights_workspace_bytes", "qp_heavy_select", "qp_decode_attn_weights",
-           "qp_decode_weights_workspace_bytes", "qp_evict_kv", "qp_decode_attn_tree", "qp_decode_tree_workspace_bytes", "qp_debug_give_up"]
+           "qp_decode_weights_workspace_bytes", "qp_evict_kv", "qp_decode_attn_tree", "qp_decode_tree_workspace_bytes", "qp_debug_give_up",
+           "qp_rope_init", "qp_rope_freqs", "qp_rotary", "qp_paged_layout", "qp_paged_append", "qp_paged_attn",
+           "qp_paged_attn_workspace_bytes"]
 
 
 class QpError(RuntimeError):
@@ -63,6 +66,25 @@ class qp_strategy(ctypes.Structure):
 class qp_tail(ctypes.Structure):
     _fields_ = [("n_tail", ctypes.c_int32), ("reserved_", ctypes.c_int32),
                 ("k_tail", ctypes.c_void_p), ("v_tail", ctypes.c_void_p)]
+
+
+class qp_rope(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("factor", ctypes.c_float),
+                ("reserved_", ctypes.c_int32), ("turn", ctypes.c_uint64 * 64)]
+
+
+class qp_paged(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("format", ctypes.c_int32), ("page", ctypes.c_int32),
+                ("n_pages", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("codes_bytes", ctypes.c_size_t), ("scale_bytes", ctypes.c_size_t), ("tail_bytes", ctypes.c_size_t),
+                ("k_codes", ctypes.c_void_p), ("v_codes", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("k_tail", ctypes.c_void_p), ("v_tail", ctypes.c_void_p)]
+
+
+class qp_step(ctypes.Structure):
+    _fields_ = [("n_tokens", ctypes.c_int32), ("max_new", ctypes.c_int32), ("start", ctypes.c_void_p),
+                ("len", ctypes.c_void_p), ("pages", ctypes.c_void_p)]
 
 
 _lib = None
@@ -149,6 +171,21 @@ def lib() -> ctypes.CDLL:
         L.qp_decode_tree_workspace_bytes.argtypes = [cp, i]
         L.qp_decode_attn_tree.restype = i
         L.qp_decode_attn_tree.argtypes = [p, i, cp, sp, tp, p, p, p, p, p, sz, p]
+        rp, pp, st, dp = ctypes.POINTER(qp_rope), ctypes.POINTER(qp_paged), ctypes.POINTER(qp_step), ctypes.c_double
+        L.qp_rope_init.restype = i
+        L.qp_rope_init.argtypes = [i, i, dp, i, dp, i, rp]
+        L.qp_rope_freqs.restype = i
+        L.qp_rope_freqs.argtypes = [i, i, ctypes.POINTER(dp), ctypes.c_float, rp]
+        L.qp_rotary.restype = i
+        L.qp_rotary.argtypes = [p, ctypes.POINTER(i64), p, ctypes.POINTER(i64), i, i, i, i, p, i64, rp, i, p]
+        L.qp_paged_layout.restype = i
+        L.qp_paged_layout.argtypes = [i] * 8 + [pp]
+        L.qp_paged_append.restype = i
+        L.qp_paged_append.argtypes = [p, i64, p, i64, pp, st, rp, p, p, i64, p, p]
+        L.qp_paged_attn_workspace_bytes.restype = sz
+        L.qp_paged_attn_workspace_bytes.argtypes = [pp, i, i]
+        L.qp_paged_attn.restype = i
+        L.qp_paged_attn.argtypes = [p, i64, pp, st, p, p, sz, p]
         _lib = L
     return _lib
 
@@ -820,6 +857,211 @@ def decode_attn_tree(q: torch.Tensor, cache: Cache, k_draft: torch.Tensor, v_dra
     return out
 
 
+ROPE_KINDS = {"plain": 0, "linear": 1, "ntk": 2, "yarn": 3, "bands": 4}
+PAGED_FORMATS = {torch.float8_e4m3fn: 0, torch.int8: 1}
+
+
+def rope(rot_dim: int, base: float = 10000.0, interleaved: bool = False, scaling: str = "plain", factor: float = 1.0,
+         trained_len: int = 8192, freqs=None) -> qp_rope:
+    """qp_rope_init: the rotation of ``rot_dim`` channels by position, plain or scaled for long contexts ("linear", "ntk", "yarn",
+    "bands"); with ``freqs`` (rot_dim/2 numbers, radians a position) qp_rope_freqs, ``factor`` being what the rotated channels are
+    multiplied by."""
+    r = qp_rope()
+    if freqs is not None:
+        if len(freqs) != rot_dim // 2:
+            raise ValueError("one frequency for each pair of channels")
+        w = (ctypes.c_double * max(1, len(freqs)))(*[float(x) for x in freqs])
+        _check(lib().qp_rope_freqs(rot_dim, int(interleaved), w, factor, ctypes.byref(r)), "qp_rope_freqs")
+    else:
+        _check(lib().qp_rope_init(rot_dim, int(interleaved), base, ROPE_KINDS[scaling], factor, trained_len, ctypes.byref(r)),
+               "qp_rope_init")
+    return r
+
+
+def _strides(t: torch.Tensor):
+    """Strides of batch, head and token as qp_rotary takes them (0 where there is one only)."""
+    (b, h, n, d), (sb, sh, sn, sd) = t.shape, t.stride()
+    assert t.dtype is torch.bfloat16 and t.get_device() == _current_device() and (sd == 1 or d == 1), (t.device, t.dtype, t.stride())
+    return (ctypes.c_int64 * 3)(sb if b > 1 else 0, sh if h > 1 else 0, sn if n > 1 else 0)
+
+
+def rotary(x: torch.Tensor, pos: torch.Tensor, rope_: qp_rope, out: torch.Tensor | None = None, transpose: bool = False) -> torch.Tensor:
+    """qp_rotary: x [Bt,H,L,D] (any strides that keep a row's channels together: rows of a fused projection, seen head by head, do)
+    rotated by pos int32 [L] or [Bt,L]; ``out`` may be x.  transpose: by the negative angles (the gradient; the way back where the
+    rotation has no factor)."""
+    Bt, H, L, D = x.shape
+    if out is None:
+        out = x.new_empty((Bt, H, L, D))
+    assert out.shape == x.shape
+    if pos.dim() == 1:
+        _dev(pos, torch.int32, (L,))
+        ps = 0
+    else:
+        _dev(pos, torch.int32, (Bt, L))
+        ps = L
+    to = _strides(out)
+    assert (to[0] or Bt == 1) and (to[1] or H == 1) and (to[2] or L == 1), "rows of out overlap"
+    status = lib().qp_rotary(x.data_ptr(), _strides(x), out.data_ptr(), to, Bt, H, L, D, pos.data_ptr(), ps, ctypes.byref(rope_),
+                             int(transpose), _stream())
+    if status:
+        _check(status, "qp_rotary")
+    return out
+
+
+def compress_layer_rotary(K: torch.Tensor, V: torch.Tensor, Q_win: torch.Tensor, rope_: qp_rope, budget_bits: int, bits: int,
+                          group: int = 32, pool: int = 7, first_pos: int = 0, **kw):
+    """compress_layer for a prompt as it leaves the projections: K [Bt,Hkv,L,D] and Q_win [Bt,Hq,w,D] (any strides, see rotary) are
+    rotated first, at positions first_pos .. first_pos+L-1, the window's at the last w of them."""
+    L, w = K.shape[2], Q_win.shape[2]
+    pos = torch.arange(first_pos, first_pos + L, dtype=torch.int32, device=K.device)
+    return compress_layer(rotary(K, pos, rope_), V, rotary(Q_win, pos[L - w:], rope_), budget_bits, bits, group, pool, **kw)
+
+
+@dataclass
+class PagedCache:
+    """Device buffers of one layer's paged 8-bit cache plus the C descriptor that points at them."""
+    desc: qp_paged
+    k_codes: torch.Tensor    # float8_e4m3fn or int8 [n_pages,Hkv,page,D]
+    v_codes: torch.Tensor
+    k_scale: torch.Tensor    # bf16 [n_pages,Hkv]
+    v_scale: torch.Tensor
+    k_tail: torch.Tensor     # bf16 [n_seqs,Hkv,page,D]
+    v_tail: torch.Tensor
+
+
+def paged_layout(n_seqs: int, n_q_heads: int, n_kv_heads: int, head_dim: int, format: int, page: int, n_pages: int,
+                 max_pages: int) -> qp_paged:
+    c = qp_paged()
+    _check(lib().qp_paged_layout(n_seqs, n_q_heads, n_kv_heads, head_dim, format, page, n_pages, max_pages, ctypes.byref(c)),
+           "qp_paged_layout")
+    return c
+
+
+def paged_cache(n_q_heads: int, k_codes: torch.Tensor, v_codes: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor,
+                k_tail: torch.Tensor, v_tail: torch.Tensor, max_pages: int) -> PagedCache:
+    """The cache that these arrays are (shapes as in PagedCache)."""
+    n_pages, Hkv, page, D = k_codes.shape
+    n_seqs = k_tail.shape[0]
+    c = paged_layout(n_seqs, n_q_heads, Hkv, D, PAGED_FORMATS[k_codes.dtype], page, n_pages, max_pages)
+    both = ((k_codes, v_codes, k_codes.dtype, (n_pages, Hkv, page, D)), (k_scale, v_scale, torch.bfloat16, (n_pages, Hkv)),
+            (k_tail, v_tail, torch.bfloat16, (n_seqs, Hkv, page, D)))
+    for k, v, dtype, shape in both:
+        _dev(k, dtype, shape); _dev(v, dtype, shape)
+    c.k_codes, c.v_codes, c.k_scale, c.v_scale, c.k_tail, c.v_tail = map(_ptr, (k_codes, v_codes, k_scale, v_scale, k_tail, v_tail))
+    return PagedCache(c, k_codes, v_codes, k_scale, v_scale, k_tail, v_tail)
+
+
+def alloc_paged(n_seqs: int, n_q_heads: int, n_kv_heads: int, head_dim: int, n_pages: int, max_pages: int, page: int = 64,
+                dtype: torch.dtype = torch.float8_e4m3fn, device="cuda") -> PagedCache:
+    """Allocates the buffers of ``qp_paged_layout`` with torch: a pool of n_pages pages for up to n_seqs sequences of up to
+    max_pages pages each.  dtype: torch.float8_e4m3fn or torch.int8."""
+    codes = lambda: torch.empty((n_pages, n_kv_heads, page, head_dim), dtype=dtype, device=device)
+    wide = lambda *shape: torch.empty(shape, dtype=torch.bfloat16, device=device)
+    tail = (n_seqs, n_kv_heads, page, head_dim)
+    return paged_cache(n_q_heads, codes(), codes(), wide(n_pages, n_kv_heads), wide(n_pages, n_kv_heads), wide(*tail), wide(*tail),
+                       max_pages)
+
+
+class PagedStep:
+    """One step of a batch (qp_step), the same for all layers: sequence b's new tokens are rows start[b] .. start[b+1]-1 and stand
+    behind the len[b] tokens it has; pages [n_seqs, max_pages] is the page table (int32 all, on the device).  The caller adds the
+    new tokens to len after the last layer."""
+
+    def __init__(self, start: torch.Tensor, len: torch.Tensor, pages: torch.Tensor, n_tokens: int, max_new: int):
+        n_seqs, max_pages = pages.shape
+        _dev(start, torch.int32, (n_seqs + 1,)); _dev(len, torch.int32, (n_seqs,)); _dev(pages, torch.int32, (n_seqs, max_pages))
+        self.start, self.len, self.pages, self.n_tokens, self.max_new = start, len, pages, n_tokens, max_new
+        self.shape, self.device = (n_seqs, max_pages), start.get_device()
+        self.desc = qp_step(n_tokens, max_new, start.data_ptr(), len.data_ptr(), pages.data_ptr())
+
+
+def _token_rows(t: torch.Tensor, n: int, heads: int, D: int) -> int:
+    """bf16 rows [n, heads, D] whose heads lie one behind the other, on the current device: elements from a row to the next."""
+    assert (t.dtype is torch.bfloat16 and t.shape == (n, heads, D) and t.get_device() == _current_device() and t.stride(2) == 1
+            and (heads == 1 or t.stride(1) == D)), (t.device, t.dtype, t.shape, t.stride())
+    return t.stride(0) if n > 1 else heads * D
+
+
+def _fits(cache: PagedCache, step: PagedStep) -> None:
+    d = cache.desc
+    assert step.shape == (d.n_seqs, d.max_pages) and step.device == _current_device() == cache.k_codes.get_device(), \
+        "step and cache do not belong together, or are not on the current device"
+
+
+def paged_append(k_new: torch.Tensor, v_new: torch.Tensor, cache: PagedCache, step: PagedStep, rope_: "qp_rope | None" = None,
+                 pos: torch.Tensor | None = None, q: torch.Tensor | None = None, q_out: torch.Tensor | None = None):
+    """qp_paged_append: the step's keys and values [n_tokens,Hkv,D] go into the cache, keys rotated unless rope_ is None, at the
+    tokens' positions in their sequences or at ``pos`` int32 [n_tokens]; returns the step's queries q [n_tokens,Hq,D] rotated, if
+    they are given.  Rows may be parts of a fused projection's."""
+    d, n = cache.desc, step.n_tokens
+    _fits(cache, step)
+    ks, vs = _token_rows(k_new, n, d.n_kv_heads, d.head_dim), _token_rows(v_new, n, d.n_kv_heads, d.head_dim)
+    qs = 0
+    if q is not None:
+        qs = _token_rows(q, n, d.n_q_heads, d.head_dim)
+        if q_out is None:
+            q_out = q.new_empty((n, d.n_q_heads, d.head_dim))
+        else:
+            _dev(q_out, torch.bfloat16, (n, d.n_q_heads, d.head_dim))
+    if pos is not None:
+        _dev(pos, torch.int32, (n,))
+    status = lib().qp_paged_append(k_new.data_ptr(), ks, v_new.data_ptr(), vs, ctypes.byref(d), ctypes.byref(step.desc),
+                                   None if rope_ is None else ctypes.byref(rope_), _ptr(pos), _ptr(q), qs, None if q is None else _ptr(q_out),
+                                   _stream())
+    if status:
+        _check(status, "qp_paged_append")
+    return None if q is None else q_out
+
+
+def paged_attn_workspace_bytes(cache: "PagedCache | qp_paged", n_tokens: int, max_new: int) -> int:
+    return int(lib().qp_paged_attn_workspace_bytes(ctypes.byref(cache.desc if isinstance(cache, PagedCache) else cache), n_tokens, max_new))
+
+
+def paged_attn(q: torch.Tensor, cache: PagedCache, step: PagedStep, out: torch.Tensor | None = None,
+               workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """qp_paged_attn: attention of the step's tokens, which paged_append has taken in, over their sequences: q [n_tokens,Hq,D] ->
+    out [n_tokens,Hq,D] (rows that are no sequence's are left as they are)."""
+    d, n = cache.desc, step.n_tokens
+    _fits(cache, step)
+    qs = _token_rows(q, n, d.n_q_heads, d.head_dim)
+    if out is None:
+        out = q.new_empty((n, d.n_q_heads, d.head_dim))
+    else:
+        _dev(out, torch.bfloat16, (n, d.n_q_heads, d.head_dim))
+    if workspace is None:
+        workspace = new_decode_workspace(paged_attn_workspace_bytes(cache, n, step.max_new), q.device)
+    status = lib().qp_paged_attn(q.data_ptr(), qs, ctypes.byref(d), ctypes.byref(step.desc), out.data_ptr(), *_scratch(workspace), _stream())
+    if status:
+        _check(status, "qp_paged_attn")
+    return out
+
+
+def paged_layer_step(q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, cache: PagedCache, step: PagedStep,
+                     rope_: "qp_rope | None" = None, pos: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                     workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """One layer of a step: qp_paged_append (with the queries, if there is a rotation), then qp_paged_attn.  A step that is refused
+    has changed nothing: what the second call asks for is looked at before the first takes the tokens in."""
+    d, n = cache.desc, step.n_tokens
+    _fits(cache, step)
+    stride = _token_rows(q, n, d.n_q_heads, d.head_dim)
+    if out is None:
+        out = q.new_empty((n, d.n_q_heads, d.head_dim))
+    else:
+        _dev(out, torch.bfloat16, (n, d.n_q_heads, d.head_dim))
+    need = paged_attn_workspace_bytes(cache, n, step.max_new)
+    if workspace is None:
+        workspace = new_decode_workspace(need, q.device)
+    address, size = _scratch(workspace)
+    if need == 0:
+        raise QpError(2, "paged_layer_step")
+    if size < need:
+        raise QpError(4, "paged_layer_step")
+    if (address | q.data_ptr() | out.data_ptr()) & 15 or stride & 7:
+        raise QpError(5, "paged_layer_step")
+    turned = paged_append(k_new, v_new, cache, step, rope_, pos, None if rope_ is None else q)
+    return paged_attn(q if rope_ is None else turned, cache, step, out, workspace)
+
+
 def debug_check() -> tuple[int, list[int]]:
     """qp_debug_check: (status, [1 + site of the first violation or 0, index, limit, violations]); status is
     QP_ERR_UNSUPPORTED (2) unless the loaded library is the range-checked build."""
@@ -868,3 +1110,10 @@ qp_decode_weights_workspace_bytes = decode_weights_workspace_bytes
 qp_evict_kv = evict_kv
 qp_decode_attn_tree = decode_attn_tree
 qp_decode_tree_workspace_bytes = decode_tree_workspace_bytes
+qp_rope_init = rope
+qp_rope_freqs = lambda rot_dim, interleaved, w, factor=1.0: rope(rot_dim, interleaved=interleaved, factor=factor, freqs=w)
+qp_rotary = rotary
+qp_paged_layout = paged_layout
+qp_paged_append = paged_append
+qp_paged_attn = paged_attn
+qp_paged_attn_workspace_bytes = paged_attn_workspace_bytes
