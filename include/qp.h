@@ -511,7 +511,7 @@ qp_status qp_paged_layout(int n_seqs, int n_q_heads, int n_kv_heads, int head_di
  * n_tokens and max_new (rows of the arrays that are no sequence's are not looked at, and left as they are in outputs).
  * A sequence whose numbers do not belong together (rows outside 0 .. n_tokens-1, more than max_new new tokens, a negative len, more
  * positions than its row of the page table) is left out, nothing of it is written; a page number outside the pool is not written to,
- * and makes the attention rows that would read it NaN.  len[b] may be set back only to where b's last whole page ends or behind.
+ * and makes attention rows of its sequence NaN: those that read it, and possibly others of the step.  len[b] may be set back only to where b's last whole page ends or behind.
  */
 typedef struct qp_step {
   int32_t n_tokens;      /* rows of the step's arrays */
@@ -535,7 +535,8 @@ qp_status qp_paged_append(const void* k_new, int64_t k_stride, const void* v_new
 /*
  * Attention of the step's tokens, after qp_paged_append has taken them in: the token at position p of its sequence sees the tokens at
  * positions <= p,   out[r,h,:] = softmax_t(q[r,h].K[t] / sqrt(D)) V.   q bf16 rows [n_tokens, Hq, D] (device), q_stride elements apart;
- * out bf16 [n_tokens, Hq, D], contiguous.  Magnitudes are free: queries and pages meet the tensor cores scaled by powers of two.
+ * out bf16 [n_tokens, Hq, D], contiguous.  Magnitudes are free (queries and waiting rows meet the tensor cores scaled by powers of
+ * two), but that with more than 16 query rows per KV head the value scales of a head's pages have to be within 2^90 of one another.
  * workspace: its contents are irrelevant; calls that may run at the same time must not share it.
  * Bounded waits as for qp_window_scores; one that runs out makes the rows that hang on it NaN.
  */

@@ -1,6 +1,8 @@
 // Position rotation and the paged cache in 8 bits: what their kernels share, and their launchers.
 #pragma once
 
+#include <cuda.h>
+
 #include "qp_common.cuh"
 
 namespace qp {
@@ -64,5 +66,9 @@ struct PagedAttnArgs {
 bool paged_attn_fits(int n_seqs, int n_tokens, int max_new, int Hq, int Hkv, long long most_len);
 size_t paged_attn_workspace(int n_seqs, int n_tokens, int max_new, int Hq, int Hkv, int D);
 cudaError_t launch_paged_attn(const PagedAttnArgs& a, void* ws, cudaStream_t st);
+// the form for many query rows per KV head; mk, mv: the codes as rows of D bytes, boxes of 32 of them
+bool paged_chunk_fits(int n_seqs, int n_tokens, int Hq, int Hkv, long long most_len);
+size_t paged_chunk_workspace(int n_seqs, int n_tokens, int Hq, int Hkv, int D);
+cudaError_t launch_paged_chunk(const PagedAttnArgs& a, void* ws, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t st);
 
 }  // namespace qp

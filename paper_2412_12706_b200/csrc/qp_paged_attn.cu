@@ -619,6 +619,8 @@ paged_merge_kernel(const __grid_constant__ PagedLaunch p) {
   a.out[((size_t)(q.row0 + tok) * a.Hq + head) * D + d] = *reinterpret_cast<const uint16_t*>(&v);
 }
 
+// more query rows per KV head than the products here are made for
+bool many_rows(int max_new, int G) { return (long long)max_new * G > 16; }
 int rows_of(int max_new, int G) { return max_new * G <= 8 ? 8 : 16; }
 
 struct Carve {
@@ -666,14 +668,22 @@ cudaError_t launch_decode_t(const PagedLaunch& p, const CUtensorMap (&m)[4], cud
 }  // namespace
 
 bool paged_attn_fits(int n_seqs, int n_tokens, int max_new, int Hq, int Hkv, long long most_len) {
+  if (many_rows(max_new, Hq / Hkv)) return paged_chunk_fits(n_seqs, n_tokens, Hq, Hkv, most_len);
   const long long G = Hq / Hkv, items = Hkv * (n_tokens * G / rows_of(max_new, (int)G) + n_seqs);
   return items * (most_len / 32 + 8) < 0x7fffffffLL;
 }
 size_t paged_attn_workspace(int n_seqs, int n_tokens, int max_new, int Hq, int Hkv, int D) {
+  if (many_rows(max_new, Hq / Hkv)) return paged_chunk_workspace(n_seqs, n_tokens, Hq, Hkv, D);
   return carve(n_seqs, n_tokens, max_new, Hq, Hkv, D).total;
 }
 
 cudaError_t launch_paged_attn(const PagedAttnArgs& a, void* ws, cudaStream_t st) {
+  CUtensorMap m[4];
+  const size_t rows = (size_t)a.s.n_pages * a.Hkv * a.s.page, tail_rows = (size_t)a.s.n_seqs * a.Hkv * a.s.page;
+  cudaError_t e = byte_map(&m[0], a.kc, rows, a.D, 32, a.D);
+  if (e == cudaSuccess) e = byte_map(&m[1], a.vc, rows, a.D, 32, a.D);
+  if (e != cudaSuccess) return e;
+  if (many_rows(a.s.max_new, a.Hq / a.Hkv)) return launch_paged_chunk(a, ws, m[0], m[1], st);
   PagedLaunch p{};
   p.a = a;
   p.G = a.Hq / a.Hkv;
@@ -686,11 +696,7 @@ cudaError_t launch_paged_attn(const PagedAttnArgs& a, void* ws, cudaStream_t st)
   p.base = reinterpret_cast<SeqBase*>(w + c.base);
   p.rec_ml = reinterpret_cast<float2*>(w + c.ml);
   p.rec = reinterpret_cast<float*>(w + c.rec);
-  CUtensorMap m[4];
-  const size_t rows = (size_t)a.s.n_pages * a.Hkv * a.s.page, tail_rows = (size_t)a.s.n_seqs * a.Hkv * a.s.page;
-  cudaError_t e = byte_map(&m[0], a.kc, rows, a.D, 32, a.D);
-  if (e == cudaSuccess) e = byte_map(&m[1], a.vc, rows, a.D, 32, a.D);
-  if (e == cudaSuccess) e = byte_map(&m[2], a.k_tail, tail_rows, 2 * a.D, 16, 128);
+  e = byte_map(&m[2], a.k_tail, tail_rows, 2 * a.D, 16, 128);
   if (e == cudaSuccess) e = byte_map(&m[3], a.v_tail, tail_rows, 2 * a.D, 16, 128);
   if (e != cudaSuccess) return e;
 #define QP_PAGED(F, DD)                                                                                         \

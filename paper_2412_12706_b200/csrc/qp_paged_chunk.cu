@@ -1,0 +1,870 @@
+// Attention of a step's new tokens over a paged cache in 8 bits (qp_paged_attn): many rows per KV head, as a prompt's chunk has.
+//
+// The G n query rows of a KV head are one attention problem of 4 G n D flop a token, far above what the cache's bytes cost, so both
+// products run on tcgen05: S = Q K^T from shared memory, O += P V with P from tensor memory.  The codes are turned into fp16
+// operands in shared memory once for 256 rows.
+//   e4m3   by the hardware's conversion; int8: with the codes as low bits of 1024 + 128 + c.  Neighbouring int8 codes of a word come
+//          out as channels (0, 2) and (1, 3), so operands hold the channels of every four in the order 0, 2, 1, 3: the queries are
+//          stored in the same order, and the output's columns are put right when they leave.
+// The scale of a page's keys multiplies 32 columns of S at a time; that of its values enters the exponent of their weights:
+// P = 2^(x + log2(scale) - M) with M the running maximum of that sum, and the row's sum takes P s0 / scale, in 32 bits, s0 being the
+// scale at the beginning of what the block does of the item: good for pages whose scales are within 2^90 of one another.
+//
+// Work: an item is (sequence, 256 rows, KV head); its tiles are the 128-token pieces of what its last row sees.  All items' tiles form
+// one sequence (a small kernel numbers them, from the lengths on the device), cut into one equal run for each of 148 blocks.  A block
+// walks through its run item by item; an item that is whole inside it is written out, the pieces of one that a cut goes through
+// leave records that a third kernel adds up.
+//
+// A block's sixteen warps talk through mbarriers only:
+//   copies (1)    TMA boxes of 32 tokens of keys and of values into raw stages, and their pages' scales
+//   expansion (6) two teams, keys and values: raw stages into operand slots; waiting rows (bf16) times the power of two that brings
+//                 their largest magnitude near 1, a box a warp
+//   products (1)  S[u] = Q[u] K_j^T, O[u] += P[u] V_j
+//   softmax (8)   two groups u, a row a thread, which also fetch the queries and write the output
+// u is a tile of 128 rows when there are two, else the parity of the token tile, so that one group's exponentials always run beside
+// the other's products.  Every wait is bounded; a block that gives up leaves NaN.
+#include <algorithm>
+
+#include "qp_mma.cuh"
+#include "qp_paged.cuh"
+#include "qp_tc.cuh"
+
+namespace qp {
+
+namespace {
+
+constexpr int PC_SOFT = 8, PC_TEAM = 3;                         // softmax warps; warps that expand the keys, and the values
+constexpr int PC_MMA = PC_SOFT + 2 * PC_TEAM, PC_COPY = PC_MMA + 1;   // the warp that issues the products, the one that copies
+constexpr int PC_THREADS = (PC_COPY + 1) * 32;
+constexpr int PC_SLOTS = 4, PC_RAW = 4;                         // operand slots, keys and values in turn; raw stages of a team (32 tokens each)
+constexpr int PC_SOFT_REGS = 184;
+constexpr int PC_BLOCKS = 148;                                  // of a B200, one a SM; the layout of the workspace goes by it
+constexpr int PC_SCALES = 8;                                    // tiles whose scales are kept: more than copies can be ahead of the softmax
+#ifndef QP_PC_POLY
+#define QP_PC_POLY 99
+#endif
+constexpr int PC_POLY = QP_PC_POLY;                             // every so many pairs of exponentials is a polynomial
+constexpr float PC_HEAD = 11.f, PC_SLACK = 4.f;                 // see PA_HEAD, PA_SLACK
+
+struct ChunkEntry {                                             // 256 rows of a sequence
+  int tile, tiles, b, rg;                                       // first of its Hkv * tiles tiles
+};
+struct ChunkLaunch {
+  PagedAttnArgs a;
+  int G, max_entries;
+  int* head;                                                    // {entries, tiles}
+  ChunkEntry* entry;
+  float* rec;                                                   // [2 * PC_BLOCKS][256][D]
+  float2* rec_ml;                                               // [2 * PC_BLOCKS][256]
+};
+
+__device__ __forceinline__ int c_start(int c, int T) { return (int)((long long)T * c / PC_BLOCKS); }
+__device__ __forceinline__ int c_owner(int x, int T) { return (int)((((long long)x + 1) * PC_BLOCKS - 1) / T); }
+
+// numbers the items' tiles: one thread for a sequence, then one for 256 rows of one
+__global__ void __launch_bounds__(1024)
+chunk_plan_kernel(const __grid_constant__ ChunkLaunch p) {
+  __shared__ int s_sum[32], s_first[QP_MAX_SEQS + 1];           // first entry of every sequence
+  chain_enter();
+  const StepView& s = p.a.s;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  auto scan = [&](int v, int& all) {                            // exclusive sum over the block
+    int in = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, in, o);
+      if (lane >= o) in += x;
+    }
+    __syncthreads();
+    if (lane == 31) s_sum[warp] = in;
+    __syncthreads();
+    int before = 0;
+    all = 0;
+    for (int w = 0; w < 32; ++w) {
+      if (w < warp) before += s_sum[w];
+      all += s_sum[w];
+    }
+    return before + in - v;
+  };
+  int entries = 0, all;
+  for (int b0 = 0; b0 < s.n_seqs; b0 += 1024) {
+    const int b = b0 + tid, n = b < s.n_seqs ? (seq_of(s, b).n * p.G + 255) / 256 : 0, e = scan(n, all);
+    if (b < s.n_seqs) s_first[b] = entries + e;
+    entries += all;
+  }
+  // (rows that several sequences claim could make more entries than there is room for: the call is left out then)
+  if (entries > p.max_entries) entries = 0;
+  int tiles = 0;
+  __syncthreads();
+  for (int e0 = 0; e0 < entries; e0 += 1024) {
+    const int e = e0 + tid;
+    ChunkEntry en{0, 0, 0, 0};
+    if (e < entries) {
+      int lo = 0, hi = s.n_seqs;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (s_first[mid] <= e) lo = mid; else hi = mid;
+      }
+      const Seq q = seq_of(s, lo);
+      en.b = lo;
+      en.rg = e - s_first[lo];
+      en.tiles = (q.len + (min(q.n * p.G, (en.rg + 1) * 256) - 1) / p.G + 1 + 127) / 128;
+    }
+    en.tile = tiles + scan(en.tiles * p.a.Hkv, all);
+    if (e < entries) p.entry[e] = en;
+    tiles += all;
+  }
+  if (tid == 0) {
+    p.head[0] = entries;
+    p.head[1] = tiles;
+  }
+}
+
+// a tile of the flat sequence
+struct Place {
+  int e, b, h, rg, tiles, j;
+};
+__device__ __forceinline__ Place place_of(const ChunkLaunch& p, int entries, int x) {
+  int lo = 0, hi = entries;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (p.entry[mid].tile <= x) lo = mid; else hi = mid;
+  }
+  const ChunkEntry en = p.entry[lo];
+  const int in = x - en.tile, h = in / en.tiles;
+  return Place{lo, en.b, h, en.rg, en.tiles, in - h * en.tiles};
+}
+
+// byte offset of 16-byte chunk c of row r in an operand tile of 128 rows
+__device__ __forceinline__ uint32_t op_off(int r, int c) {
+  return (uint32_t)((c >> 3) * 16384 + (r >> 3) * 1024 + (r & 7) * 128 + (((c & 7) ^ (r & 7)) << 4));
+}
+__device__ __forceinline__ void sts128(uint32_t addr, uint4 v) {
+  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};\n" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;\n" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+__device__ __forceinline__ uint32_t hadd2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("add.rn.f16x2 %0, %1, %2;\n" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+// four codes as fp16 operands.  e4m3: the hardware's conversion (exact), in order; int8: as they are (1024 + 128 + c, less 1152), in
+// the order 0, 2, 1, 3
+template <int FORMAT>
+__device__ __forceinline__ uint2 four_codes(uint32_t w) {
+  if (FORMAT == QP_E4M3) {
+    uint2 d;
+    asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\tcvt.rn.f16x2.e4m3x2 %1, hi;\n\t}\n" : "=r"(d.x), "=r"(d.y) : "r"(w));
+    return d;
+  }
+  return make_uint2(hadd2((w & 0x00ff00ffu) ^ 0x64806480u, 0xe480e480u), hadd2(((w >> 8) & 0x00ff00ffu) ^ 0x64806480u, 0xe480e480u));
+}
+// 16-byte chunk c of row r of a raw box, as the copy's swizzle leaves it
+template <int D>
+__device__ __forceinline__ uint32_t raw_off(int r, int c) {
+  return D == 128 ? (uint32_t)(r * 128 + ((c ^ (r & 7)) << 4)) : (uint32_t)(r * 64 + ((c ^ ((r >> 1) & 3)) << 4));
+}
+// channels 0 .. 3 of two bf16 words times f, in the operands' order
+template <int FORMAT>
+__device__ __forceinline__ uint2 four_ops(uint32_t w0, uint32_t w1, float f) {
+  if (FORMAT == QP_E4M3) return make_uint2(pack_half2(bf16lo(w0) * f, bf16hi(w0) * f), pack_half2(bf16lo(w1) * f, bf16hi(w1) * f));
+  return make_uint2(pack_half2(bf16lo(w0) * f, bf16lo(w1) * f), pack_half2(bf16hi(w0) * f, bf16hi(w1) * f));
+}
+__device__ __forceinline__ uint32_t abs_max(uint32_t m, const uint4& v) {
+  m = __vmaxu2(m, v.x & 0x7fff7fffu);
+  m = __vmaxu2(m, v.y & 0x7fff7fffu);
+  m = __vmaxu2(m, v.z & 0x7fff7fffu);
+  return __vmaxu2(m, v.w & 0x7fff7fffu);
+}
+// the power of two that brings the magnitude with these bf16 bits into [1, 2), and its inverse
+__device__ __forceinline__ float2 to_one(uint32_t m) {
+  m = max(m & 0xffffu, m >> 16);
+  const int e = min(max((int)(m >> 7), 1), 253);
+  return make_float2(__uint_as_float((uint32_t)(254 - e) << 23), __uint_as_float((uint32_t)e << 23));
+}
+// 64 columns of this warp's 32 TMEM lanes
+__device__ __forceinline__ void tmem_st64(uint32_t taddr, const uint32_t (&r)[64]) {
+  auto st = [&](uint32_t at, const uint32_t* v) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};\n" ::"r"(v[0]),
+        "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]),
+        "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]),
+        "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]), "r"(at)
+        : "memory");
+  };
+  st(taddr, r);
+  st(taddr + 32, r + 32);
+}
+// registers of a thread from here on; for all warps of a warpgroup
+template <int N>
+__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(N)); }
+__device__ __forceinline__ void bar_sync(int id, int n) { asm volatile("bar.sync %0, %1;\n" ::"r"(id), "r"(n) : "memory"); }
+
+enum : int {
+  CB_FULL = 0, CB_EMPTY = PC_SLOTS, CB_S = 2 * PC_SLOTS, CB_P = CB_S + 2, CB_Q = CB_P + 2, CB_RAW = CB_Q + 1, CB_RAW_EMPTY = CB_RAW + 2 * PC_RAW,
+  CB_COUNT = CB_RAW_EMPTY + 2 * PC_RAW
+};
+
+struct Slot {                                                   // a team's place in the ring of slots, with the parity of the round
+  int i;
+  uint32_t round = 0;
+  __device__ __forceinline__ void next() {
+    i += 2;
+    if (i >= PC_SLOTS) { i -= PC_SLOTS; round ^= 1u; }
+  }
+};
+
+template <int FORMAT, int D>
+__global__ void __launch_bounds__(PC_THREADS, 1)
+chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
+  constexpr uint32_t SLOT = 128 * D * 2, RAW = 32 * D;
+  constexpr uint32_t ID_S = (1u << 4) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
+  constexpr uint32_t ID_O = (1u << 4) | (1u << 16) | (((uint32_t)D >> 3) << 17) | ((128u >> 4) << 24);        // B: rows contract
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ uint64_t bars[CB_COUNT];
+  __shared__ float s_fk[PC_SCALES][4];                          // per 32 tokens: what S is multiplied by
+  __shared__ float4 s_fv[PC_SCALES][2];                         // log2 of the values' scale, its inverse, for two times 32 tokens
+  __shared__ float2 s_ml[128];
+  __shared__ uint32_t tmem_base_slot;
+  __shared__ int give_up;
+  const PagedAttnArgs& a = p.a;
+  const StepView& s = a.s;
+  const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+  const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t sQ = sbase, ring = sbase + 2 * SLOT, raw_base = ring + PC_SLOTS * SLOT;
+  const uint32_t bar0 = smem_u32(&bars[0]);
+  auto bar = [&](int which, int i) { return bar0 + (uint32_t)(which + i) * 8u; };
+  const volatile int* gu = &give_up;
+  if (tid == 0) {
+    for (int i = 0; i < PC_SLOTS; ++i) {
+      mbar_init(bar(CB_FULL, i), PC_TEAM);
+      mbar_init(bar(CB_EMPTY, i), 1);                           // a tcgen05.commit
+    }
+    for (int u = 0; u < 2; ++u) {
+      mbar_init(bar(CB_S, u), 1);                               // a tcgen05.commit
+      mbar_init(bar(CB_P, u), 4);                               // the group's warps
+    }
+    mbar_init(bar(CB_Q, 0), PC_SOFT);
+    for (int i = 0; i < 2 * PC_RAW; ++i) {
+      mbar_init(bar(CB_RAW, i), 1);
+      mbar_init(bar(CB_RAW_EMPTY, i), PC_TEAM);
+    }
+    give_up = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+  }
+  if (warp == PC_MMA) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(&tmem_base_slot)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+  const uint32_t tmem = tmem_base_slot;
+  chain_enter();
+  const int entries = p.head[0], T = p.head[1], cta = blockIdx.x;
+  const int x0 = c_start(cta, T), x1 = c_start(cta + 1, T);
+  auto tS = [&](int u) { return tmem + (uint32_t)u * 128u; };
+  auto tO = [&](int u) { return tmem + 256u + (uint32_t)u * D; };
+
+  // the pieces of the run: (item, its tiles j .. j + n - 1)
+  struct Piece {
+    Place at;
+    Seq q;
+    int n, rows, two;
+  };
+  auto piece_at = [&](int x) {
+    Piece c;
+    c.at = place_of(p, entries, x);
+    c.q = seq_of(s, c.at.b);
+    c.n = min(c.at.tiles - c.at.j, x1 - x);
+    c.rows = min(256, c.q.n * p.G - c.at.rg * 256);
+    c.two = c.rows > 128;
+    return c;
+  };
+
+  // tokens of a piece's sequence that are in whole pages
+  auto whole_tokens = [&](const Piece& c) { return (c.q.len + c.q.n) / s.page * s.page; };
+  // Of a 32-token box: what the product with its keys is multiplied by; of its values the log2 of that, and its inverse.  Written with
+  // the keys: the softmax of a tile begins when they are there, whatever has become of the values.
+  auto set_scales = [&](int tile, int box, float fk, float fv) {
+    s_fk[tile & (PC_SCALES - 1)][box] = fk;
+    fv = fv == 0.f ? 0x1p-60f : fv;                             // zeros: any scale that leaves the others theirs
+    float* d = reinterpret_cast<float*>(&s_fv[tile & (PC_SCALES - 1)][box >> 1]) + 2 * (box & 1);
+    d[0] = log2f(fv);
+    d[1] = __fdiv_rn(1.f, fv);
+  };
+
+  // 512 threads have 128 registers each: the softmax takes 56 from the others, whose 8 warps give back what its 8 warps take
+  if (warp < PC_SOFT) {
+    // ---- softmax groups
+    more_registers<PC_SOFT_REGS>();
+    const int u = warp >> 2, rl = (warp & 3) * 32 + lane;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const float scale_log2 = 1.4426950408889634f * rsqrtf((float)D);
+    uint32_t phase = 0;                                         // of CB_S[u]
+    bool ok = true;
+    int tiles_done = 0;                                         // of the run, for the scales' ring
+    for (int x = x0; x < x1;) {                                 // (one that gave up goes on, without waits: the groups have barriers)
+      const Piece c = piece_at(x);
+      const int r = (c.two ? u * 128 : 0) + rl;                 // row of the item
+      const bool has = r < c.rows;
+      const bool work = (c.two ? u * 128 : 0) + (warp & 3) * 32 < c.rows;            // warp-uniform
+      const int gr = c.at.rg * 256 + r, tok = gr / p.G, head = c.at.h * p.G + gr - tok * p.G;
+      // the row, in fp16 times the power of two that brings its largest magnitude near 1
+      float cq = 0.f;
+      {
+        const uint4* src = reinterpret_cast<const uint4*>(a.q + (c.q.row0 + tok) * a.qs + (size_t)head * D);
+        uint32_t m = 0u;
+        uint4 v[D / 8];
+#pragma unroll
+        for (int k = 0; k < D / 8; ++k) v[k] = has ? __ldg(src + k) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int k = 0; k < D / 8; ++k) m = abs_max(m, v[k]);
+        const float2 f = to_one(m);
+        cq = f.y * scale_log2;
+        if (c.two || u == 0) {
+          const uint32_t dst = sQ + (c.two ? u : 0) * SLOT;
+#pragma unroll
+          for (int k = 0; k < D / 8; ++k) {
+            const uint2 lo = four_ops<FORMAT>(v[k].x, v[k].y, f.x), hi = four_ops<FORMAT>(v[k].z, v[k].w, f.x);
+            sts128(dst + op_off(rl, k), make_uint4(lo.x, lo.y, hi.x, hi.y));
+          }
+        }
+        asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(CB_Q, 0));
+      }
+      // columns of a box to logits; never 0, which would make a hidden column's -inf a NaN
+      auto factor = [&](float fk) {
+        const float f = fk * cq;
+        return f < 0x1p-126f ? 0x1p-126f : f;                   // (NaN stays)
+      };
+      const int lim = has ? c.q.len + tok + 1 : 0;              // positions this row sees
+      const int least = c.q.len + (c.at.rg * 256) / p.G + 1;    // and the item's first row
+      float m_run = -INFINITY, l_run = 0.f;
+      float s0 = 1.f, log_s0 = 0.f;
+      bool any = false;
+      for (int k = c.two ? 0 : u; k < c.n && ok; k += c.two ? 1 : 2) {
+        const int j = c.at.j + k;
+        ok = mbar_wait_warp(bar(CB_S, u), phase, gu);
+        phase ^= 1u;
+        if (!ok) break;
+        if (work) {
+          asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+          const uint32_t ts = tS(u) + lanes;
+          const int sr = (tiles_done + k) & (PC_SCALES - 1);
+          if (!any) {                                           // (both groups: of the first tile)
+            log_s0 = s_fv[tiles_done & (PC_SCALES - 1)][0].x;
+            s0 = ex2a(log_s0);
+          }
+          if (128 * (j + 1) > least) {                          // what the row does not see leaves S
+#pragma unroll 1
+            for (int c0 = 0; c0 < 128; c0 += 16) {
+              uint32_t v[16];
+              tmem_ld16_issue(ts + c0, v);
+              tmem_wait16(v);
+#pragma unroll
+              for (int i = 0; i < 16; ++i) v[i] = 128 * j + c0 + i < lim ? v[i] : 0xff800000u;
+              __syncwarp();
+              tmem_st(ts + c0, v);
+            }
+            tmem_wait_st();
+          }
+          // One pass: the weights against the reference as it is, and the maximum beside them.  Where the reference turns out to
+          // be exceeded by more than 2^4 (a block's first tiles), it is renewed, O with it, and the pass taken again; S is still
+          // there, for the weights stay in registers until then.
+          uint32_t pk[64];
+          float sum;
+          for (;;) {
+            const float ref = PC_HEAD - (m_run == -INFINITY ? 0.f : m_run);
+            uint32_t x[2][32];
+            float mx = -INFINITY;
+            sum = 0.f;
+            tmem_ld32_issue(ts, x[0]);
+#pragma unroll
+            for (int box = 0; box < 4; ++box) {
+              uint32_t (&v)[32] = x[box & 1];
+              tmem_wait(v);
+              if (box < 3) tmem_ld32_issue(ts + 32 * (box + 1), x[(box + 1) & 1]);
+              const float4 fv4 = s_fv[sr][box >> 1];
+              const float lv = box & 1 ? fv4.z : fv4.x, f = factor(s_fk[sr][box]);
+              const uint64_t sc = pack2(f, f), nm = pack2(ref + lv, ref + lv);
+              uint64_t sum2 = pack2(0.f, 0.f), sum3 = sum2;
+              float mx0 = -INFINITY, mx1 = -INFINITY;
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                const float a0 = __uint_as_float(v[2 * i]), a1 = __uint_as_float(v[2 * i + 1]);
+                if (i & 1) mx1 = max3(mx1, a0, a1); else mx0 = max3(mx0, a0, a1);
+                float e0, e1;
+                uint64_t y = fma2(pack2(a0, a1), sc, nm);
+                if (i % PC_POLY == PC_POLY - 1) {               // a share of the exponentials on the FMA pipe
+                  y = ex2_poly2<true>(y);
+                  unpack2(y, e0, e1);
+                } else {
+                  unpack2(y, e0, e1);
+                  e0 = ex2a(e0);
+                  e1 = ex2a(e1);
+                }
+                pk[16 * box + i] = pack_half2(e0, e1);
+                if (i & 1) sum3 = add2(sum3, pack2(e0, e1)); else sum2 = add2(sum2, pack2(e0, e1));
+              }
+              sum2 = add2(sum2, sum3);
+              float a0, a1;
+              unpack2(sum2, a0, a1);
+              sum = fmaf(a0 + a1, fminf((box & 1 ? fv4.w : fv4.y) * s0, 0x1p96f), sum);
+              mx = fmaxf(mx, fmaf(fmaxf(mx0, mx1), f, lv));
+            }
+            const bool renew = mx > m_run + PC_SLACK;
+            if (!__any_sync(0xffffffffu, renew)) break;
+            const float mn = renew ? mx : m_run, corr = renew ? ex2a(m_run - mn) : 1.f;
+            m_run = mn;
+            l_run *= corr;
+            if (any) {
+#pragma unroll 1
+              for (int c0 = 0; c0 < D; c0 += 16) {
+                uint32_t o[16];
+                tmem_ld16_issue(tO(u) + lanes + c0, o);
+                tmem_wait16(o);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * corr);
+                __syncwarp();
+                tmem_st(tO(u) + lanes + c0, o);
+              }
+              tmem_wait_st();
+            }
+          }
+          any = true;
+          l_run += sum;
+          __syncwarp();
+          tmem_st64(ts, pk);
+          tmem_wait_st();
+          asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(CB_P, u));
+      }
+      // O is complete with one more commit
+      ok = ok && mbar_wait_warp(bar(CB_S, u), phase, gu);
+      phase ^= 1u;
+      asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+      if (!ok) {                                                // what is lost must not look like a row that sees nothing
+        give_up = 1;
+        m_run = 0.f;
+        l_run = NAN;
+      }
+      const bool whole = c.at.j == 0 && c.n == c.at.tiles;
+      const int rec = 2 * cta + (x == x0 ? 0 : 1);
+      float f_own = 1.f, f_other = 0.f;
+      if (l_run != l_run) m_run = 0.f;                          // (a sum that is no number has to be looked at)
+      float M = m_run, L = l_run;
+      constexpr int HALF = D / 2;                               // channels that are exchanged at a time
+      const uint32_t xch = sQ + SLOT;                           // the second row tile's place, free where there is one
+      auto xch_off = [&](int ch) { return xch + (uint32_t)(rl * (HALF * 4) + ((ch ^ (rl & (HALF / 4 - 1))) << 4)); };
+      if (!c.two) {                                             // the two groups' parts of a row come together in group 0
+        if (u == 1) s_ml[rl] = make_float2(any || l_run != l_run ? m_run : -INFINITY, l_run);
+        bar_sync(3, PC_SOFT * 32);
+        if (u == 0) {
+          const float2 o = s_ml[rl];
+          M = fmaxf(m_run, o.x);
+          f_own = m_run == -INFINITY ? 0.f : ex2a(m_run - M);
+          f_other = o.x == -INFINITY ? 0.f : ex2a(o.x - M);
+          L = (m_run == -INFINITY ? 0.f : l_run * f_own) + (o.x == -INFINITY ? 0.f : o.y * f_other);
+        }
+      }
+      const bool writes = has && (c.two || u == 0);
+      const float inv = __fdiv_rn(1.f, L);
+      if (writes && !whole) p.rec_ml[(size_t)rec * 256 + r] = make_float2(M == -INFINITY ? M : M - log_s0, L);
+      uint16_t* out = a.out + ((size_t)(c.q.row0 + tok) * a.Hq + head) * D;
+      float* part = p.rec + ((size_t)rec * 256 + r) * D;
+#pragma unroll 1
+      for (int half = 0; half < 2; ++half) {
+        if (!c.two) {
+          if (u == 1 && any) {
+#pragma unroll 1
+            for (int c0 = 0; c0 < HALF; c0 += 16) {
+              uint32_t o[16];
+              tmem_ld16_issue(tO(u) + lanes + half * HALF + c0, o);
+              tmem_wait16(o);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) sts128(xch_off(c0 / 4 + i), make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]));
+            }
+          }
+          bar_sync(3, PC_SOFT * 32);
+        }
+        if (work && (c.two || u == 0)) {
+#pragma unroll 1
+          for (int c0 = 0; c0 < HALF; c0 += 16) {
+            uint32_t o[16];
+            if (any) {
+              tmem_ld16_issue(tO(u) + lanes + half * HALF + c0, o);
+              tmem_wait16(o);
+            }
+            float v[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = any && f_own != 0.f ? __uint_as_float(o[i]) * f_own : 0.f;
+            if (!c.two && f_other != 0.f) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const uint4 w = lds128(xch_off(c0 / 4 + i));
+                v[4 * i] = fmaf(__uint_as_float(w.x), f_other, v[4 * i]);
+                v[4 * i + 1] = fmaf(__uint_as_float(w.y), f_other, v[4 * i + 1]);
+                v[4 * i + 2] = fmaf(__uint_as_float(w.z), f_other, v[4 * i + 2]);
+                v[4 * i + 3] = fmaf(__uint_as_float(w.w), f_other, v[4 * i + 3]);
+              }
+            }
+            if (FORMAT == QP_INT8) {                            // columns 0, 1, 2, 3 are channels 0, 2, 1, 3
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const float t = v[4 * i + 1];
+                v[4 * i + 1] = v[4 * i + 2];
+                v[4 * i + 2] = t;
+              }
+            }
+            if (writes) {
+              const int ch = half * HALF + c0;
+              if (whole) {
+                uint32_t w[8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  w[2 * i] = pack_bf16x2(v[4 * i] * inv * s0, v[4 * i + 1] * inv * s0);
+                  w[2 * i + 1] = pack_bf16x2(v[4 * i + 2] * inv * s0, v[4 * i + 3] * inv * s0);
+                }
+                *reinterpret_cast<uint4*>(out + ch) = make_uint4(w[0], w[1], w[2], w[3]);
+                *reinterpret_cast<uint4*>(out + ch + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+              } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                  *reinterpret_cast<float4*>(part + ch + 4 * i) = make_float4(v[4 * i] * s0, v[4 * i + 1] * s0, v[4 * i + 2] * s0, v[4 * i + 3] * s0);
+              }
+            }
+          }
+        }
+        if (!c.two) bar_sync(3, PC_SOFT * 32);
+      }
+      asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+      tiles_done += c.n;
+      x += c.n;
+    }
+    fewer_registers<128>();
+  } else {
+    fewer_registers<256 - PC_SOFT_REGS>();
+    if (warp == PC_MMA) {
+    // ---- products.  Operands in the ring: keys of tile 0, values of tile 0, keys of tile 1, ..., across pieces
+    bool ok = true;
+    Slot kr{0}, vr{1};
+    uint32_t pq = 0, pp[2] = {0, 0};                            // phases of CB_Q, CB_P
+    auto wait_full = [&](const Slot& r) { ok = ok && mbar_wait_warp(bar(CB_FULL, r.i), r.round, gu); };
+    auto wait_p = [&](int u) {
+      ok = ok && mbar_wait_warp(bar(CB_P, u), pp[u], gu);
+      pp[u] ^= 1u;
+    };
+    auto issue_s = [&](int u, int qt, bool last_reader) {
+      asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+      const uint32_t q = uniform(desc_lo(sQ + qt * SLOT, 1)), kk = uniform(desc_lo(ring + kr.i * SLOT, 1));
+      const uint32_t d = uniform(tS(u)), done = uniform(bar(CB_S, u)), empty = uniform(bar(CB_EMPTY, kr.i));
+      if (elect_one()) {
+        umma_ss<false>(d, q, kk, ID_S);
+#pragma unroll
+        for (int k = 1; k < D / 16; ++k) umma_ss<true>(d, q + (k / 4) * 1024 + (k % 4) * 2, kk + (k / 4) * 1024 + (k % 4) * 2, ID_S);
+        umma_commit(done);
+        if (last_reader) umma_commit(empty);
+      }
+      __syncwarp();
+      if (last_reader) kr.next();
+    };
+    auto issue_o = [&](int u, bool first, bool last_reader) {
+      asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+      const uint32_t vv = uniform(desc_lo(ring + vr.i * SLOT, 1024)), d = uniform(tO(u)), pt = uniform(tS(u));
+      const uint32_t empty = uniform(bar(CB_EMPTY, vr.i));
+      if (elect_one()) {
+        umma_ts(d, pt, vv, ID_O, first ? 0u : 1u);
+#pragma unroll
+        for (int k = 1; k < 8; ++k) umma_ts(d, pt + 8 * k, vv + k * 128, ID_O, 1u);
+        if (last_reader) umma_commit(empty);
+      }
+      __syncwarp();
+      if (last_reader) vr.next();
+    };
+    auto finish = [&](int u) {                                  // one more commit: O[u] is complete
+      const uint32_t done = uniform(bar(CB_S, u));
+      if (elect_one()) umma_commit(done);
+      __syncwarp();
+    };
+    for (int x = x0; x < x1 && ok;) {
+      const Piece c = piece_at(x);
+      ok = mbar_wait_warp(bar(CB_Q, 0), pq, gu);
+      pq ^= 1u;
+      if (c.two) {
+        wait_full(kr);
+        if (ok) issue_s(0, 0, false);
+        if (ok) issue_s(1, 1, true);
+        for (int j = 0; j < c.n && ok; ++j)
+          for (int u = 0; u < 2 && ok; ++u) {
+            if (u == 0) wait_full(vr);
+            wait_p(u);
+            if (!ok) break;
+            issue_o(u, j == 0, u == 1);
+            if (j + 1 < c.n) {
+              if (u == 0) wait_full(kr);
+              if (ok) issue_s(u, u, u == 1);
+            } else {
+              finish(u);
+            }
+          }
+      } else {
+        for (int j = 0; j < min(2, c.n) && ok; ++j) {
+          wait_full(kr);
+          if (ok) issue_s(j, 0, true);
+        }
+        if (c.n == 1 && ok) finish(1);                          // (the second group has no tile)
+        for (int j = 0; j < c.n && ok; ++j) {
+          const int u = j & 1;
+          wait_full(vr);
+          wait_p(u);
+          if (!ok) break;
+          issue_o(u, j < 2, true);
+          if (j + 2 < c.n) {
+            wait_full(kr);
+            if (ok) issue_s(u, 0, true);
+          } else {
+            finish(u);
+          }
+        }
+      }
+      x += c.n;
+    }
+    if (!ok) give_up = 1;
+    } else if (warp == PC_COPY) {
+      // ---- copies: the boxes of 32 tokens of keys and of values, and their scales.  Lane i copies box i % 4 of a tile's keys (i < 4) or
+      // values, as soon as its stage is free.
+      bool ok = true;
+      const int lg = 31 - __clz(s.page / 32), box = lane & 3, team = lane >> 2;       // lg: log2 of boxes per page
+      int n_box = 0, tile = 0;                                  // boxes copied, tiles of the run before this one
+      for (int x = x0; x < x1 && ok;) {
+        const Piece c = piece_at(x);
+        const int whole = whole_tokens(c);
+        int window = -64, w_id = -1;                            // 32 pages: ids and scales in the lanes
+        float w_ks = NAN, w_vs = NAN;
+        for (int k = 0; k < c.n && ok; ++k, ++tile) {
+          const int t0 = 128 * (c.at.j + k), boxes = min(4, max(0, (whole - t0) / 32));
+          if (boxes == 0) continue;
+          const int pg0 = t0 / 32 >> lg, pg1 = (t0 / 32 + boxes - 1) >> lg;
+          if (pg0 < window || pg1 >= window + 32) {
+            window = pg0;
+            const int i = pg0 + lane;
+            w_id = i < whole / s.page ? page_of(s, c.at.b, i) : -1;
+            w_ks = w_vs = NAN;                                  // a page outside the pool makes its rows NaN
+            if (w_id >= 0) {
+              w_ks = bf16_bits_to_f32(__ldg(a.k_scale + (size_t)w_id * a.Hkv + c.at.h));
+              w_vs = bf16_bits_to_f32(__ldg(a.v_scale + (size_t)w_id * a.Hkv + c.at.h));
+            }
+          }
+          const int bx = t0 / 32 + min(box, boxes - 1), src = (bx >> lg) - window;
+          const int id = max(0, __shfl_sync(0xffffffffu, w_id, src));
+          const float ks = __shfl_sync(0xffffffffu, w_ks, src), vs = __shfl_sync(0xffffffffu, w_vs, src);
+          const int n = n_box + box, st = team * PC_RAW + n % PC_RAW, row = (id * a.Hkv + c.at.h) * s.page + (bx & ((1 << lg) - 1)) * 32;
+          bool todo = lane < 8 && box < boxes;
+          if (todo && team == 0) set_scales(tile, box, ks, vs);
+          for (uint32_t y = 0; __any_sync(0xffffffffu, todo); ++y) {
+            if (todo && (n < PC_RAW || mbar_try_wait(bar(CB_RAW_EMPTY, st), (uint32_t)(n / PC_RAW + 1) & 1u))) {
+              mbar_expect_tx(bar(CB_RAW, st), RAW);
+              tma_load_2d(raw_base + st * RAW, team ? &map_v : &map_k, 0, row, bar(CB_RAW, st));
+              todo = false;
+            }
+            if (y >= TC_SPIN_LIMIT || ((y & 255u) == 255u && *gu)) break;
+          }
+          ok = !__any_sync(0xffffffffu, todo);
+          n_box += boxes;
+        }
+        x += c.n;
+      }
+      if (!ok) give_up = 1;
+      // nothing may still be on its way into this block's shared memory when it is given up: the last copies are waited for (bounded)
+      for (int i = max(0, n_box - PC_RAW); ok && i < n_box; ++i)
+        for (int h = 0; h < 2; ++h)
+          for (uint32_t y = 0; y < TC_SPIN_LIMIT; ++y)
+            if (mbar_try_wait(bar(CB_RAW, h * PC_RAW + i % PC_RAW), (uint32_t)(i / PC_RAW) & 1u)) break;
+    } else {
+      // ---- codes to operands
+      const int team = (warp - PC_SOFT) / PC_TEAM, tw = (warp - PC_SOFT) % PC_TEAM;
+      const uint16_t* tails = team ? a.v_tail : a.k_tail;
+      const uint32_t raw0 = raw_base + team * PC_RAW * RAW;
+      // a warp takes 8 rows x 4 chunks at a time: the lanes of a quarter have rows i and i ^ 5, whose chunks meet no bank twice
+      const int row8 = (lane >> 3) ^ (lane & 4 ? 5 : 0), c4 = lane & 3;
+      const uint32_t from = raw_off<D>(row8, c4), to0 = op_off(row8, 2 * c4), to1 = op_off(row8, 2 * c4 + 1);
+      constexpr int PARTS = D / 64, ITEMS = 4 * PARTS, MOST = (ITEMS + PC_TEAM - 1) / PC_TEAM;   // of a box: 8 rows x 64 channels
+      bool ok = true;
+      Slot wr{team};
+      int n_box = 0, tile = 0;
+      for (int x = x0; x < x1 && ok;) {
+        const Piece c = piece_at(x);
+        const int whole = whole_tokens(c), end = c.q.len + c.q.n;
+        for (int k = 0; k < c.n && ok; ++k, ++tile) {
+          const int t0 = 128 * (c.at.j + k), boxes = min(4, max(0, (whole - t0) / 32));
+          const uint32_t slot = ring + wr.i * SLOT;
+          if (tile >= 2) ok = mbar_wait_warp(bar(CB_EMPTY, wr.i), wr.round ^ 1u, gu);
+          for (int box = 0; box < boxes && ok; ++box, ++n_box) {
+            const int stage = n_box % PC_RAW, first = (tw + n_box) % PC_TEAM;      // (the shares differ: in turn)
+            ok = mbar_wait_warp(bar(CB_RAW, team * PC_RAW + stage), (uint32_t)(n_box / PC_RAW) & 1u, gu);
+            if (!ok) break;
+            uint4 w[MOST];
+#pragma unroll
+            for (int q = 0; q < MOST; ++q) {
+              const int i = first + q * PC_TEAM, g8 = i / PARTS, part = i % PARTS;
+              if (i < ITEMS) w[q] = lds128(raw0 + stage * RAW + g8 * 8 * D + (from ^ (part * 64)));
+            }
+#pragma unroll
+            for (int q = 0; q < MOST; ++q) {
+              const int i = first + q * PC_TEAM, g8 = i / PARTS, part = i % PARTS;
+              if (i < ITEMS) {
+                const uint32_t at = slot + (4 * box + g8) * 1024 + part * 16384;
+                const uint2 o0 = four_codes<FORMAT>(w[q].x), o1 = four_codes<FORMAT>(w[q].y), o2 = four_codes<FORMAT>(w[q].z), o3 = four_codes<FORMAT>(w[q].w);
+                sts128(at + to0, make_uint4(o0.x, o0.y, o1.x, o1.y));
+                sts128(at + to1, make_uint4(o2.x, o2.y, o3.x, o3.y));
+              }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(CB_RAW_EMPTY, team * PC_RAW + stage));
+          }
+          if (!ok) break;
+          // waiting rows, a box a warp, a row a lane: bf16 to fp16 times a power of two; zeros behind the last
+          for (int box = boxes + tw; box < 4; box += PC_TEAM) {
+            const int t = t0 + 32 * box + lane;
+            const size_t row = (((size_t)c.at.b * a.Hkv + c.at.h) * s.page + t - whole) * (D / 8);
+            auto scale_of = [&](const uint16_t* tail) {
+              uint32_t m = 0u;
+              if (t < end)
+#pragma unroll 4
+                for (int q = 0; q < D / 8; ++q) m = abs_max(m, reinterpret_cast<const uint4*>(tail)[row + q]);
+              m = __reduce_max_sync(0xffffffffu, max(m & 0xffffu, m >> 16));
+              return m ? to_one(m) : make_float2(1.f, 0.f);
+            };
+            const float2 f = scale_of(tails);
+#pragma unroll 4
+            for (int q = 0; q < D / 8; ++q) {
+              const uint4 v = t < end ? reinterpret_cast<const uint4*>(tails)[row + q] : make_uint4(0u, 0u, 0u, 0u);
+              const uint2 lo = four_ops<FORMAT>(v.x, v.y, f.x), hi = four_ops<FORMAT>(v.z, v.w, f.x);
+              sts128(slot + op_off(32 * box + lane, q), make_uint4(lo.x, lo.y, hi.x, hi.y));
+            }
+            if (team == 0) {
+              const float2 fv = scale_of(a.v_tail);
+              if (lane == 0) set_scales(tile, box, f.y, fv.y);
+            }
+          }
+          asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(CB_FULL, wr.i));
+          wr.next();
+        }
+        x += c.n;
+      }
+      if (!ok) give_up = 1;
+    }
+    more_registers<128>();
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+  if (warp == PC_MMA)
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(512u) : "memory");
+}
+
+// the items that cuts go through: out from their records, in order.  A block row (y) for every cut, which takes the item if it is its
+// first; a thread for 4 channels of a row
+template <int D>
+__global__ void __launch_bounds__(256)
+chunk_merge_kernel(const __grid_constant__ ChunkLaunch p) {
+  chain_enter();
+  const int entries = p.head[0], T = p.head[1], cut = blockIdx.y + 1;
+  if (T == 0) return;
+  const int x = c_start(cut, T);
+  if (x >= T || x == c_start(cut - 1, T)) return;               // (runs without tiles)
+  const Place at = place_of(p, entries, x);
+  const int first = x - at.j, last = first + at.tiles - 1;      // the item's tiles
+  if (at.j == 0 || c_owner(first, T) != cut - 1) return;        // the cut falls between items, or is not the item's first
+  const PagedAttnArgs& a = p.a;
+  const Seq q = seq_of(a.s, at.b);
+  const int i = blockIdx.x * 256 + threadIdx.x, r = i / (D / 4), ch = i % (D / 4), gr = at.rg * 256 + r;
+  if (r >= 256 || gr >= q.n * p.G) return;
+  const int c1 = c_owner(last, T);
+  float M = -INFINITY, L = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int c = cut - 1; c <= c1; ++c) {
+    const int s0 = c_start(c, T);
+    if (s0 == c_start(c + 1, T)) continue;
+    const size_t row = (size_t)(2 * c + (s0 >= first ? 0 : 1)) * 256 + r;
+    const float2 ml = p.rec_ml[row];
+    const float4 v = *reinterpret_cast<const float4*>(p.rec + row * D + 4 * ch);
+    if (ml.x == -INFINITY) continue;                            // a piece of which the row sees nothing
+    const float n = fmaxf(M, ml.x), f = M == -INFINITY ? 0.f : ex2a(M - n), e = ex2a(ml.x - n);
+    M = n;
+    L = L * f + ml.y * e;
+    o.x = o.x * f + v.x * e; o.y = o.y * f + v.y * e;
+    o.z = o.z * f + v.z * e; o.w = o.w * f + v.w * e;
+  }
+  const float inv = __fdiv_rn(1.f, L);
+  const int tok = gr / p.G;
+  *reinterpret_cast<uint2*>(a.out + ((size_t)(q.row0 + tok) * a.Hq + at.h * p.G + gr - tok * p.G) * D + 4 * ch) =
+      make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+}
+
+struct ChunkCarve {
+  size_t entry, ml, rec, total;
+  int entries;
+};
+ChunkCarve chunk_carve(int n_seqs, int n_tokens, int Hq, int Hkv, int D) {
+  ChunkCarve c;
+  c.entries = (int)((long long)n_tokens * (Hq / Hkv) / 256) + n_seqs;
+  auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
+  c.entry = 256;
+  c.ml = up(c.entry + (size_t)c.entries * sizeof(ChunkEntry));
+  c.rec = c.ml + up((size_t)2 * PC_BLOCKS * 256 * sizeof(float2));
+  c.total = c.rec + (size_t)2 * PC_BLOCKS * 256 * D * sizeof(float);
+  return c;
+}
+
+template <int FORMAT, int D>
+cudaError_t launch_chunk_t(const ChunkLaunch& p, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t st) {
+  static unsigned char done[64];
+  constexpr size_t smem = (2 + PC_SLOTS) * 128 * D * 2 + 2 * PC_RAW * 32 * D + 1024;
+  auto kernel = chunk_kernel<FORMAT, D>;
+  cudaError_t e = allow_smem(kernel, smem, done);
+  if (e == cudaSuccess) e = launch_chained(chunk_plan_kernel, dim3(1), dim3(1024), 0, st, p);
+  if (e == cudaSuccess) e = launch_chained(kernel, dim3(PC_BLOCKS), dim3(PC_THREADS), smem, st, p, mk, mv);
+  if (e == cudaSuccess) e = launch_chained(chunk_merge_kernel<D>, dim3(D / 4, PC_BLOCKS - 1), dim3(256), 0, st, p);
+  return e;
+}
+
+}  // namespace
+
+size_t paged_chunk_workspace(int n_seqs, int n_tokens, int Hq, int Hkv, int D) { return chunk_carve(n_seqs, n_tokens, Hq, Hkv, D).total; }
+
+bool paged_chunk_fits(int n_seqs, int n_tokens, int Hq, int Hkv, long long most_len) {
+  const long long entries = (long long)n_tokens * (Hq / Hkv) / 256 + n_seqs;
+  return entries < 0x7fffffffLL / Hkv / ((most_len + 127) / 128);
+}
+
+cudaError_t launch_paged_chunk(const PagedAttnArgs& a, void* ws, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t st) {
+  ChunkLaunch p{};
+  p.a = a;
+  p.G = a.Hq / a.Hkv;
+  const ChunkCarve c = chunk_carve(a.s.n_seqs, a.s.n_tokens, a.Hq, a.Hkv, a.D);
+  char* w = static_cast<char*>(ws);
+  p.max_entries = c.entries;
+  p.head = reinterpret_cast<int*>(w);
+  p.entry = reinterpret_cast<ChunkEntry*>(w + c.entry);
+  p.rec_ml = reinterpret_cast<float2*>(w + c.ml);
+  p.rec = reinterpret_cast<float*>(w + c.rec);
+  if (a.format == QP_E4M3) return a.D == 128 ? launch_chunk_t<QP_E4M3, 128>(p, mk, mv, st) : launch_chunk_t<QP_E4M3, 64>(p, mk, mv, st);
+  return a.D == 128 ? launch_chunk_t<QP_INT8, 128>(p, mk, mv, st) : launch_chunk_t<QP_INT8, 64>(p, mk, mv, st);
+}
+
+}  // namespace qp
