@@ -3,10 +3,10 @@
 // With one new token a sequence the cache's bytes are the floor: 2 D bytes a token and KV head against 4 G D flop.  The products run on
 // mma.sync (m16n8k16, fp16): tokens, then channels, are the 16 rows, the G n query rows of a KV head the 8 columns, so a code is turned
 // into an fp16 operand once whatever G is.
-//   e4m3   sign, exponent and mantissa moved to their places in fp16 are the number times 2^-8 (subnormals included)
+//   e4m3   the hardware's conversion, two codes at a time
 //   int8   the code xor 128 in a lane of 16 bits is the subnormal fp16 number (c + 128) 2^-24; the 128 come off again through the
 //          sum of the query (keys) and of the weights (values)
-// so a pair of operands costs two to four integer instructions and no multiplication; the page's scales meet 32-bit accumulators.
+// so a pair of operands costs one to two instructions and no multiplication; the page's scales meet 32-bit accumulators.
 //
 // Work: every (sequence, KV head, 8 NB query rows) is an item of ceil(tokens of whole pages / 32) tiles followed by one for every 16
 // waiting rows.  The tiles of all items are one sequence, cut into one equal run for each warp of the grid, found by each block from
@@ -25,11 +25,15 @@ namespace qp {
 
 namespace {
 
-constexpr int PA_WARPS = 8, PA_THREADS = PA_WARPS * 32;
-constexpr int PA_STAGES = 3;
+// Warps of a block and copy stages of a warp.  WIDE: for calls with 64 items and more, of one block of query rows each.  Twelve warps
+// hide more of a tile's chain of dependent steps (64 sequences of up to 16000 tokens: 201 -> 188 us, D = 64 125 -> 107; 64 of 1000:
+// 36.7 -> 35.3), but fill the SM's registers, so that neither the merge nor the next call's blocks come in beside them (one sequence
+// of 2000 tokens: 8.2 us against 10.7).
+__host__ __device__ constexpr int pa_warps(int wide) { return wide ? 12 : 8; }
+__host__ __device__ constexpr int pa_stages(int wide) { return wide ? 2 : 3; }
 constexpr int PA_MAX_SEQS = 2048;
 constexpr int PA_SMS = 148;                                     // of a B200; the layout of the workspace goes by it
-constexpr int PA_WORKERS = PA_SMS * PA_WARPS;
+constexpr int PA_WORKERS = PA_SMS * pa_warps(1);               // most of a launch
 constexpr float PA_HEAD = 11.f;                                 // weights are held against the reference times 2^-11, to use fp16's upper range
 constexpr float PA_SLACK = 4.f;                                 // a maximum is renewed when it is exceeded by 2^4
 
@@ -63,7 +67,10 @@ __device__ __forceinline__ Shape shape_of(const Seq& q, int page, int G, int RB)
 }
 // the run of worker w: [w T / W, (w + 1) T / W); the worker that has tile x
 __device__ __forceinline__ int run_start(int w, int T, int W) { return (int)((long long)w * T / W); }
-__device__ __forceinline__ int owner_of(int x, int T, int W) { return (int)((((long long)x + 1) * W - 1) / T); }
+__device__ __forceinline__ int owner_of(int x, int T, int W) {
+  if (T < 1 << 20) return (int)(((uint32_t)(x + 1) * (uint32_t)W - 1u) / (uint32_t)T);       // W <= 2^11: a short division will do
+  return (int)((((long long)x + 1) * W - 1) / T);
+}
 __device__ __forceinline__ int workers_of(const PagedLaunch& p, int T) {
   return max(1, min(p.n_workers, (T + p.min_tiles - 1) / p.min_tiles));
 }
@@ -73,19 +80,20 @@ __device__ __forceinline__ uint32_t movmatrix(uint32_t v) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(d) : "r"(v));
   return d;
 }
-// fp16 operands of the even and odd bytes of w, see above
-template <int FORMAT>
-__device__ __forceinline__ uint32_t even_codes(uint32_t w) {
-  if (FORMAT == QP_E4M3) return ((w << 7) & 0x3f803f80u) | ((w << 8) & 0x80008000u);
-  return (w & 0x00ff00ffu) ^ 0x00800080u;
+// fp16 operands of the four codes of w, see above: of two pairs of keys' channels (x: the b0 of a product, y: its b1), and of two
+// tokens' values of a channel (x) and of the next (y)
+__device__ __forceinline__ uint2 int8_codes(uint32_t w) { return make_uint2((w & 0x00ff00ffu) ^ 0x00800080u, ((w >> 8) & 0x00ff00ffu) ^ 0x00800080u); }
+__device__ __forceinline__ uint2 e4m3_codes(uint32_t w) {
+  uint2 d;
+  asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\tcvt.rn.f16x2.e4m3x2 %1, hi;\n\t}\n" : "=r"(d.x), "=r"(d.y) : "r"(w));
+  return d;
 }
 template <int FORMAT>
-__device__ __forceinline__ uint32_t odd_codes(uint32_t w) {
-  if (FORMAT == QP_E4M3) return ((w >> 1) & 0x3f803f80u) | (w & 0x80008000u);
-  return ((w >> 8) & 0x00ff00ffu) ^ 0x00800080u;
-}
+__device__ __forceinline__ uint2 key_codes(uint32_t w) { return FORMAT == QP_E4M3 ? e4m3_codes(w) : int8_codes(w); }
 template <int FORMAT>
-constexpr float kCodeUnit = FORMAT == QP_E4M3 ? 0x1p8f : 0x1p24f;
+__device__ __forceinline__ uint2 value_codes(uint32_t w) { return FORMAT == QP_E4M3 ? e4m3_codes(__byte_perm(w, 0u, 0x3120)) : int8_codes(w); }
+template <int FORMAT>
+constexpr float kCodeUnit = FORMAT == QP_E4M3 ? 1.f : 0x1p24f;
 
 // The swizzles of the copies: 16-byte chunk c of row r of a tile whose rows are 64 or 128 bytes
 template <int ROW>
@@ -97,11 +105,11 @@ __device__ __forceinline__ uint32_t swz(int r, int c) {
 template <int D>
 __device__ __forceinline__ int token_of(int i) { return D == 128 ? (i & 1) * 4 + (i >> 1) : i; }
 
-template <int FORMAT, int D, int NB>
-__global__ void __launch_bounds__(PA_THREADS, 1)
+template <int FORMAT, int D, int NB, int WIDE>
+__global__ void __launch_bounds__(pa_warps(WIDE) * 32, 1)
 paged_decode_kernel(const __grid_constant__ PagedLaunch p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                     const __grid_constant__ CUtensorMap map_kt, const __grid_constant__ CUtensorMap map_vt) {
-  constexpr int RB = 8 * NB, KS = D / 16;
+  constexpr int RB = 8 * NB, KS = D / 16, PA_WARPS = pa_warps(WIDE), PA_STAGES = pa_stages(WIDE), PA_THREADS = PA_WARPS * 32;
   constexpr uint32_t SLOT = 64 * D, HALF_SLOT = SLOT / 2;       // keys, then values: 32 tokens of codes, or 16 of bf16
   extern __shared__ unsigned char smem_raw[];
   __shared__ uint64_t bars[PA_WARPS * PA_STAGES];
@@ -175,6 +183,7 @@ paged_decode_kernel(const __grid_constant__ PagedLaunch p, const __grid_constant
     int end;                                                    // tile at which the sequence ends
     int first_page, page_lane;                                  // the 32 pages whose ids the lanes hold
     float ks_lane, vs_lane;
+    bool fresh = false;
   } c;
   auto enter = [&](int x) {                                     // the cursor to tile x
     c.b = seq_at(x);
@@ -199,6 +208,18 @@ paged_decode_kernel(const __grid_constant__ PagedLaunch p, const __grid_constant
         c.first_page = pg;
         const int i = pg + lane;
         c.page_lane = i < c.page_tiles >> lg_tp ? page_of(s, c.b, i) : -1;
+        c.fresh = true;
+      }
+      const int src = pg - c.first_page;
+      const int id = max(0, __shfl_sync(0xffffffffu, c.page_lane, src));
+      if (lane == 0) {
+        const int row = (id * a.Hkv + c.h) * s.page + (c.j & ((1 << lg_tp) - 1)) * 32;
+        mbar_expect_tx(bar, SLOT);
+        tma_load_2d(dst, &map_k, 0, row, bar);
+        tma_load_2d(dst + HALF_SLOT, &map_v, 0, row, bar);
+      }
+      if (c.fresh) {                                            // (the copies need not wait for the scales)
+        c.fresh = false;
         c.ks_lane = c.vs_lane = NAN;                            // a page outside the pool makes its rows NaN
         if (c.page_lane >= 0) {
           const size_t ph = (size_t)c.page_lane * a.Hkv + c.h;
@@ -206,16 +227,8 @@ paged_decode_kernel(const __grid_constant__ PagedLaunch p, const __grid_constant
           c.vs_lane = bf16_bits_to_f32(__ldg(a.v_scale + ph));
         }
       }
-      const int src = pg - c.first_page;
-      const int id = max(0, __shfl_sync(0xffffffffu, c.page_lane, src));
       const float ks = __shfl_sync(0xffffffffu, c.ks_lane, src), vs = __shfl_sync(0xffffffffu, c.vs_lane, src);
-      if (lane == 0) {
-        s_scale[warp * PA_STAGES + slot] = make_float2(ks, vs);
-        const int row = (id * a.Hkv + c.h) * s.page + (c.j & ((1 << lg_tp) - 1)) * 32;
-        mbar_expect_tx(bar, SLOT);
-        tma_load_2d(dst, &map_k, 0, row, bar);
-        tma_load_2d(dst + HALF_SLOT, &map_v, 0, row, bar);
-      }
+      if (lane == 0) s_scale[warp * PA_STAGES + slot] = make_float2(ks, vs);
     } else if (lane == 0) {
       const int row = (c.b * a.Hkv + c.h) * s.page + (c.j - c.page_tiles) * 16;
       mbar_expect_tx(bar, SLOT);
@@ -306,9 +319,9 @@ paged_decode_kernel(const __grid_constant__ PagedLaunch p, const __grid_constant
         for (int cb = 0; cb < D / 64; ++cb) {
           const uint32_t w[8] = {v[cb][0].x, v[cb][0].y, v[cb][0].z, v[cb][0].w, v[cb][1].x, v[cb][1].y, v[cb][1].z, v[cb][1].w};
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {                         // a word of codes: channels 4i .. 4i + 3 as (0, 2) and (1, 3)
-            const uint32_t lo = pack_half2(bf16lo(w[2 * i]) * down, bf16lo(w[2 * i + 1]) * down);
-            const uint32_t hi = pack_half2(bf16hi(w[2 * i]) * down, bf16hi(w[2 * i + 1]) * down);
+          for (int i = 0; i < 4; ++i) {                         // a word of codes: channels 4i .. 4i + 3, int8 as (0, 2) and (1, 3)
+            const float c0 = bf16lo(w[2 * i]) * down, c1 = bf16hi(w[2 * i]) * down, c2 = bf16lo(w[2 * i + 1]) * down, c3 = bf16hi(w[2 * i + 1]) * down;
+            const uint32_t lo = FORMAT == QP_INT8 ? pack_half2(c0, c2) : pack_half2(c0, c1), hi = FORMAT == QP_INT8 ? pack_half2(c1, c3) : pack_half2(c2, c3);
             qf[nb][4 * cb + i][0] = lo;
             qf[nb][4 * cb + i][1] = hi;
             if (FORMAT == QP_INT8) {
@@ -395,9 +408,9 @@ paged_decode_kernel(const __grid_constant__ PagedLaunch p, const __grid_constant
             const uint32_t u0[4] = {w0.x, w0.y, w0.z, w0.w}, u1[4] = {w1.x, w1.y, w1.z, w1.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const uint32_t a0 = even_codes<FORMAT>(u0[i]), a1 = even_codes<FORMAT>(u1[i]), a2 = odd_codes<FORMAT>(u0[i]), a3 = odd_codes<FORMAT>(u1[i]);
+              const uint2 x0 = key_codes<FORMAT>(u0[i]), x1 = key_codes<FORMAT>(u1[i]);
 #pragma unroll
-              for (int nb = 0; nb < NB; ++nb) mma_f16_m16n8k16(sv[nb][mb], a0, a1, a2, a3, qf[nb][4 * cb + i][0], qf[nb][4 * cb + i][1]);
+              for (int nb = 0; nb < NB; ++nb) mma_f16_m16n8k16(sv[nb][mb], x0.x, x1.x, x0.y, x1.y, qf[nb][4 * cb + i][0], qf[nb][4 * cb + i][1]);
             }
           }
         uint32_t pb[NB][2][2];                                  // weights as B operands: tokens x columns
@@ -441,13 +454,12 @@ paged_decode_kernel(const __grid_constant__ PagedLaunch p, const __grid_constant
         for (int ch = 0; ch < KS; ++ch) {
           uint32_t w0, w1, w2, w3;
           ldmatrix_x4_trans(w0, w1, w2, w3, vt + swz<D>(vr, ch));
-          const uint32_t e0 = even_codes<FORMAT>(w0), e1 = even_codes<FORMAT>(w1), e2 = even_codes<FORMAT>(w2), e3 = even_codes<FORMAT>(w3);
-          const uint32_t o0 = odd_codes<FORMAT>(w0), o1 = odd_codes<FORMAT>(w1), o2 = odd_codes<FORMAT>(w2), o3 = odd_codes<FORMAT>(w3);
+          const uint2 v0 = value_codes<FORMAT>(w0), v1 = value_codes<FORMAT>(w1), v2 = value_codes<FORMAT>(w2), v3 = value_codes<FORMAT>(w3);
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb) {
             float o[4] = {0.f, 0.f, 0.f, 0.f};
-            mma_f16_m16n8k16(o, e0, o0, e1, o1, pb[nb][0][0], pb[nb][0][1]);
-            mma_f16_m16n8k16(o, e2, o2, e3, o3, pb[nb][1][0], pb[nb][1][1]);
+            mma_f16_m16n8k16(o, v0.x, v0.y, v1.x, v1.y, pb[nb][0][0], pb[nb][0][1]);
+            mma_f16_m16n8k16(o, v2.x, v2.y, v3.x, v3.y, pb[nb][1][0], pb[nb][1][1]);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
               acc[nb][ch][i] = fmaf(FORMAT == QP_INT8 ? o[i] - psum[nb][i & 1] : o[i], fv, acc[nb][ch][i]);
@@ -554,50 +566,84 @@ paged_decode_kernel(const __grid_constant__ PagedLaunch p, const __grid_constant
   }
 }
 
-// out from the records, in their order: a block of four warps for every (query row of a sequence)
-template <int D>
-__global__ void __launch_bounds__(128)
+// out from the records, in their order: WPR warps for a query row of a sequence, each with four records on their way at a time.  A
+// block is 8 warps: one row where there are few (and so many records for each), else 8 rows.
+constexpr int PM_WARPS = 8, PM_BATCH = 4;
+template <int D, int WPR>
+__global__ void __launch_bounds__(PM_WARPS * 32)
 paged_merge_kernel(const __grid_constant__ PagedLaunch p) {
-  __shared__ float s_m[4], s_l[4];
-  __shared__ float s_o[4][D];
+  __shared__ float s_m[PM_WARPS], s_l[PM_WARPS];
+  __shared__ float s_o[WPR > 1 ? PM_WARPS : 1][D];
   chain_enter();
   const PagedAttnArgs& a = p.a;
   const StepView& s = a.s;
-  const int b = blockIdx.y, tok = blockIdx.x / a.Hq, head = blockIdx.x % a.Hq, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const Seq q = seq_of(s, b);
-  if (tok >= q.n) return;
-  const Shape sh = shape_of(q, s.page, p.G, p.RB);
+  const int warp = WPR > 1 ? threadIdx.x >> 5 : 0, lane = threadIdx.x & 31;
+  const int row0 = WPR > 1 ? blockIdx.x : blockIdx.x * PM_WARPS + (threadIdx.x >> 5);
+  const int b = blockIdx.y, tok = row0 / a.Hq, head = row0 - tok * a.Hq;
+  const SeqBase at = p.base[b];
   const int T = p.base[s.n_seqs].tile;
-  if (T == 0) return;
+  const Seq q = seq_of(s, b);
+  if (tok >= q.n || T == 0) return;
+  const Shape sh = shape_of(q, s.page, p.G, p.RB);
   const int W = workers_of(p, T), per = sh.page_tiles + sh.tail_tiles;
-  const int h = head / p.G, gr = tok * p.G + head % p.G, rb = gr / p.RB, r = gr % p.RB, item = h * sh.row_blocks + rb;
-  const int x = p.base[b].tile + item * per, slot0 = 2 * (p.base[b].item + item);
-  // workers of the pages' tiles and of the waiting rows'
-  const int w0 = sh.page_tiles ? owner_of(x, T, W) : 0, n0 = sh.page_tiles ? owner_of(x + sh.page_tiles - 1, T, W) - w0 + 1 : 0;
-  const int w1 = sh.tail_tiles ? owner_of(x + sh.page_tiles, T, W) : 0, n1 = sh.tail_tiles ? owner_of(x + per - 1, T, W) - w1 + 1 : 0;
+  const int h = head / p.G, gr = tok * p.G + head - h * p.G, rb = gr / p.RB, r = gr - rb * p.RB, item = h * sh.row_blocks + rb;
+  const int x = at.tile + item * per, slot0 = 2 * (at.item + item);
+  // workers of the pages' tiles and of the waiting rows': of the first and the last of each
+  const int mine = owner_of(max(0, x + (lane == 0 ? 0 : lane == 1 ? sh.page_tiles - 1 : lane == 2 ? sh.page_tiles : per - 1)), T, W);
+  const int w0 = __shfl_sync(0xffffffffu, mine, 0), w1 = __shfl_sync(0xffffffffu, mine, 2);
+  const int n0 = sh.page_tiles ? __shfl_sync(0xffffffffu, mine, 1) - w0 + 1 : 0, n1 = sh.tail_tiles ? __shfl_sync(0xffffffffu, mine, 3) - w1 + 1 : 0;
   constexpr int V = D / 32;                                     // channels of a lane
   float M = -INFINITY, L = 0.f, o[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) o[i] = 0.f;
-  for (int k = warp; k < n0 + n1; k += 4) {
-    const size_t row = (size_t)(k < n0 ? slot0 + w0 + k : slot0 + 1 + w1 + k - n0) * p.RB + r;
-    const float2 ml = p.rec_ml[row];
-    const float* src = p.rec + row * D + V * lane;
-    float v[V];
-    if constexpr (V == 4) {
-      const float4 f = *reinterpret_cast<const float4*>(src);
-      v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
-    } else {
-      const float2 f = *reinterpret_cast<const float2*>(src);
-      v[0] = f.x; v[1] = f.y;
-    }
-    if (ml.x == -INFINITY) continue;                            // nothing seen
-    const float n = M > ml.x ? M : ml.x;
-    const float f = M == -INFINITY ? 0.f : ex2a(M - n), e = ex2a(ml.x - n);
-    M = n;
-    L = L * f + ml.y * e;
+  for (int k0 = warp; k0 < n0 + n1; k0 += WPR * PM_BATCH) {
+    float2 ml[PM_BATCH];
+    float v[PM_BATCH][V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) o[i] = o[i] * f + v[i] * e;
+    for (int j = 0; j < PM_BATCH; ++j) {
+      const int k = k0 + j * WPR;
+      ml[j] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[j][i] = 0.f;
+      if (k < n0 + n1) {
+        const size_t row = (size_t)(k < n0 ? slot0 + w0 + k : slot0 + 1 + w1 + k - n0) * p.RB + r;
+        ml[j] = p.rec_ml[row];
+        const float* src = p.rec + row * D + V * lane;
+        if constexpr (V == 4) {
+          const float4 f = *reinterpret_cast<const float4*>(src);
+          v[j][0] = f.x; v[j][1] = f.y; v[j][2] = f.z; v[j][3] = f.w;
+        } else {
+          const float2 f = *reinterpret_cast<const float2*>(src);
+          v[j][0] = f.x; v[j][1] = f.y;
+        }
+      }
+    }
+    float n = M;
+#pragma unroll
+    for (int j = 0; j < PM_BATCH; ++j) n = fmaxf(n, ml[j].x);
+    if (n == -INFINITY) continue;                               // nothing seen
+    const float f = M == -INFINITY ? 0.f : ex2a(M - n);
+    M = n;
+    L *= f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) o[i] *= f;
+#pragma unroll
+    for (int j = 0; j < PM_BATCH; ++j) {
+      const float e = ml[j].x == -INFINITY ? 0.f : ex2a(ml[j].x - n);
+      if (ml[j].x == -INFINITY) continue;
+      L = fmaf(ml[j].y, e, L);
+#pragma unroll
+      for (int i = 0; i < V; ++i) o[i] = fmaf(v[j][i], e, o[i]);
+    }
+  }
+  uint16_t* out = a.out + ((size_t)(q.row0 + tok) * a.Hq + head) * D;
+  if constexpr (WPR == 1) {
+    const float inv = __fdiv_rn(1.f, L);
+    if constexpr (V == 4)
+      *reinterpret_cast<uint2*>(out + 4 * lane) = make_uint2(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
+    else
+      *reinterpret_cast<uint32_t*>(out + 2 * lane) = pack_bf16x2(o[0] * inv, o[1] * inv);
+    return;
   }
   if (lane == 0) { s_m[warp] = M; s_l[warp] = L; }
 #pragma unroll
@@ -607,21 +653,22 @@ paged_merge_kernel(const __grid_constant__ PagedLaunch p) {
   if (d >= D) return;
   float m = s_m[0];
 #pragma unroll
-  for (int w = 1; w < 4; ++w) m = m > s_m[w] ? m : s_m[w];
+  for (int w = 1; w < PM_WARPS; ++w) m = fmaxf(m, s_m[w]);
   float l = 0.f, acc = 0.f;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
+  for (int w = 0; w < PM_WARPS; ++w) {
     const float e = s_m[w] == -INFINITY ? 0.f : ex2a(s_m[w] - m);
     l += s_l[w] * e;
     acc += s_o[w][d] * e;
   }
   const __nv_bfloat16 v = __float2bfloat16_rn(__fdiv_rn(acc, l));
-  a.out[((size_t)(q.row0 + tok) * a.Hq + head) * D + d] = *reinterpret_cast<const uint16_t*>(&v);
+  out[d] = *reinterpret_cast<const uint16_t*>(&v);
 }
 
 // more query rows per KV head than the products here are made for
-bool many_rows(int max_new, int G) { return (long long)max_new * G > 16; }
-int rows_of(int max_new, int G) { return max_new * G <= 8 ? 8 : 16; }
+bool many_rows(int max_new, int G) { return (long long)max_new * G > 32; }
+// (17 to 24 rows at once rather than in two: 5 tokens x 4 heads of 16 sequences of 3000 to 4100, 51.9 us against 53.2)
+int rows_of(int max_new, int G) { return max_new * G <= 8 ? 8 : max_new * G > 16 && max_new * G <= 24 ? 24 : 16; }
 
 struct Carve {
   size_t base, ml, rec, total;
@@ -653,16 +700,18 @@ cudaError_t byte_map(CUtensorMap* map, const void* base, size_t rows, int row_by
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-template <int FORMAT, int D, int NB>
+template <int FORMAT, int D, int NB, int WIDE>
 cudaError_t launch_decode_t(const PagedLaunch& p, const CUtensorMap (&m)[4], cudaStream_t st) {
   static unsigned char done[64];
-  constexpr size_t smem = PA_WARPS * PA_STAGES * 64 * D + 1024;
-  auto kernel = paged_decode_kernel<FORMAT, D, NB>;
+  constexpr size_t smem = pa_warps(WIDE) * pa_stages(WIDE) * 64 * D + 1024;
+  auto kernel = paged_decode_kernel<FORMAT, D, NB, WIDE>;
   cudaError_t e = allow_smem(kernel, smem, done);
   if (e != cudaSuccess) return e;
-  e = launch_chained(kernel, dim3(PA_SMS), dim3(PA_THREADS), smem, st, p, m[0], m[1], m[2], m[3]);
+  e = launch_chained(kernel, dim3(PA_SMS), dim3(pa_warps(WIDE) * 32), smem, st, p, m[0], m[1], m[2], m[3]);
   if (e != cudaSuccess) return e;
-  return launch_chained(paged_merge_kernel<D>, dim3((unsigned)p.a.s.max_new * p.a.Hq, p.a.s.n_seqs), dim3(128), 0, st, p);
+  const unsigned rows = (unsigned)p.a.s.max_new * p.a.Hq;
+  if (rows * p.a.s.n_seqs <= 8 * PA_SMS) return launch_chained(paged_merge_kernel<D, PM_WARPS>, dim3(rows, p.a.s.n_seqs), dim3(PM_WARPS * 32), 0, st, p);
+  return launch_chained(paged_merge_kernel<D, 1>, dim3((rows + PM_WARPS - 1) / PM_WARPS, p.a.s.n_seqs), dim3(PM_WARPS * 32), 0, st, p);
 }
 
 }  // namespace
@@ -688,7 +737,8 @@ cudaError_t launch_paged_attn(const PagedAttnArgs& a, void* ws, cudaStream_t st)
   p.a = a;
   p.G = a.Hq / a.Hkv;
   p.RB = rows_of(a.s.max_new, p.G);
-  p.n_workers = PA_WORKERS;
+  const bool wide = p.RB == 8 && a.s.n_seqs * a.Hkv >= 64;
+  p.n_workers = PA_SMS * pa_warps(wide);
   p.min_tiles = 2;
   const Carve c = carve(a.s.n_seqs, a.s.n_tokens, a.s.max_new, a.Hq, a.Hkv, a.D);
   p.max_items = c.items;
@@ -699,8 +749,11 @@ cudaError_t launch_paged_attn(const PagedAttnArgs& a, void* ws, cudaStream_t st)
   e = byte_map(&m[2], a.k_tail, tail_rows, 2 * a.D, 16, 128);
   if (e == cudaSuccess) e = byte_map(&m[3], a.v_tail, tail_rows, 2 * a.D, 16, 128);
   if (e != cudaSuccess) return e;
-#define QP_PAGED(F, DD)                                                                                         \
-  return p.RB == 8 ? launch_decode_t<F, DD, 1>(p, m, st) : launch_decode_t<F, DD, 2>(p, m, st)
+#define QP_PAGED(F, DD)                                             \
+  return wide           ? launch_decode_t<F, DD, 1, 1>(p, m, st)    \
+         : p.RB == 8    ? launch_decode_t<F, DD, 1, 0>(p, m, st)    \
+         : p.RB == 16   ? launch_decode_t<F, DD, 2, 0>(p, m, st)    \
+                        : launch_decode_t<F, DD, 3, 0>(p, m, st)
   if (a.format == QP_E4M3) {
     if (a.D == 128) QP_PAGED(QP_E4M3, 128);
     QP_PAGED(QP_E4M3, 64);

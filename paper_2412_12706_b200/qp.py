@@ -878,11 +878,14 @@ def rope(rot_dim: int, base: float = 10000.0, interleaved: bool = False, scaling
     return r
 
 
-def _strides(t: torch.Tensor):
+_Strides = ctypes.c_int64 * 3
+
+
+def _strides(t: torch.Tensor, b: int, h: int, n: int):
     """Strides of batch, head and token as qp_rotary takes them (0 where there is one only)."""
-    (b, h, n, d), (sb, sh, sn, sd) = t.shape, t.stride()
-    assert t.dtype is torch.bfloat16 and t.get_device() == _current_device() and (sd == 1 or d == 1), (t.device, t.dtype, t.stride())
-    return (ctypes.c_int64 * 3)(sb if b > 1 else 0, sh if h > 1 else 0, sn if n > 1 else 0)
+    sb, sh, sn, sd = t.stride()
+    assert t.dtype is torch.bfloat16 and t.get_device() == _current_device() and sd == 1, (t.device, t.dtype, t.stride())
+    return _Strides(sb if b > 1 else 0, sh if h > 1 else 0, sn if n > 1 else 0)
 
 
 def rotary(x: torch.Tensor, pos: torch.Tensor, rope_: qp_rope, out: torch.Tensor | None = None, transpose: bool = False) -> torch.Tensor:
@@ -890,18 +893,19 @@ def rotary(x: torch.Tensor, pos: torch.Tensor, rope_: qp_rope, out: torch.Tensor
     rotated by pos int32 [L] or [Bt,L]; ``out`` may be x.  transpose: by the negative angles (the gradient; the way back where the
     rotation has no factor)."""
     Bt, H, L, D = x.shape
-    if out is None:
-        out = x.new_empty((Bt, H, L, D))
-    assert out.shape == x.shape
+    fresh = out is None
+    if fresh:
+        out = x.new_empty(x.shape)
+    assert fresh or out.shape == x.shape
     if pos.dim() == 1:
         _dev(pos, torch.int32, (L,))
         ps = 0
     else:
         _dev(pos, torch.int32, (Bt, L))
         ps = L
-    to = _strides(out)
-    assert (to[0] or Bt == 1) and (to[1] or H == 1) and (to[2] or L == 1), "rows of out overlap"
-    status = lib().qp_rotary(x.data_ptr(), _strides(x), out.data_ptr(), to, Bt, H, L, D, pos.data_ptr(), ps, ctypes.byref(rope_),
+    to = _Strides(H * L * D, L * D, D) if fresh else _strides(out, Bt, H, L)
+    assert fresh or ((to[0] or Bt == 1) and (to[1] or H == 1) and (to[2] or L == 1)), "rows of out overlap"
+    status = lib().qp_rotary(x.data_ptr(), _strides(x, Bt, H, L), out.data_ptr(), to, Bt, H, L, D, pos.data_ptr(), ps, ctypes.byref(rope_),
                              int(transpose), _stream())
     if status:
         _check(status, "qp_rotary")
