@@ -37,13 +37,8 @@ constexpr int PC_SOFT = 8, PC_TEAM = 3;                         // softmax warps
 constexpr int PC_MMA = PC_SOFT + 2 * PC_TEAM, PC_COPY = PC_MMA + 1;   // the warp that issues the products, the one that copies
 constexpr int PC_THREADS = (PC_COPY + 1) * 32;
 constexpr int PC_SLOTS = 4, PC_RAW = 4;                         // operand slots, keys and values in turn; raw stages of a team (32 tokens each)
-constexpr int PC_SOFT_REGS = 184;
 constexpr int PC_BLOCKS = 148;                                  // of a B200, one a SM; the layout of the workspace goes by it
 constexpr int PC_SCALES = 8;                                    // tiles whose scales are kept: more than copies can be ahead of the softmax
-#ifndef QP_PC_POLY
-#define QP_PC_POLY 99
-#endif
-constexpr int PC_POLY = QP_PC_POLY;                             // every so many pairs of exponentials is a polynomial
 constexpr float PC_HEAD = 11.f, PC_SLACK = 4.f;                 // see PA_HEAD, PA_SLACK
 
 struct ChunkEntry {                                             // 256 rows of a sequence
@@ -186,26 +181,6 @@ __device__ __forceinline__ float2 to_one(uint32_t m) {
   const int e = min(max((int)(m >> 7), 1), 253);
   return make_float2(__uint_as_float((uint32_t)(254 - e) << 23), __uint_as_float((uint32_t)e << 23));
 }
-// 64 columns of this warp's 32 TMEM lanes
-__device__ __forceinline__ void tmem_st64(uint32_t taddr, const uint32_t (&r)[64]) {
-  auto st = [&](uint32_t at, const uint32_t* v) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};\n" ::"r"(v[0]),
-        "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]),
-        "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]),
-        "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]), "r"(at)
-        : "memory");
-  };
-  st(taddr, r);
-  st(taddr + 32, r + 32);
-}
-// registers of a thread from here on; for all warps of a warpgroup
-template <int N>
-__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(N)); }
-template <int N>
-__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(N)); }
 __device__ __forceinline__ void bar_sync(int id, int n) { asm volatile("bar.sync %0, %1;\n" ::"r"(id), "r"(n) : "memory"); }
 
 enum : int {
@@ -232,7 +207,6 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
   __shared__ uint64_t bars[CB_COUNT];
   __shared__ float s_fk[PC_SCALES][4];                          // per 32 tokens: what S is multiplied by
   __shared__ float4 s_fv[PC_SCALES][2];                         // log2 of the values' scale, its inverse, for two times 32 tokens
-  __shared__ float2 s_ml[128];
   __shared__ uint32_t tmem_base_slot;
   __shared__ int give_up;
   const PagedAttnArgs& a = p.a;
@@ -280,9 +254,19 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
     Seq q;
     int n, rows, two;
   };
-  auto piece_at = [&](int x) {
+  // the first is searched for, the others follow one another: the next head, or the next entry
+  auto piece_at = [&](int x, const Piece* before = nullptr) {
     Piece c;
-    c.at = place_of(p, entries, x);
+    if (!before) {
+      c.at = place_of(p, entries, x);
+    } else {
+      c.at = before->at;
+      c.at.j = 0;
+      if (++c.at.h == a.Hkv) {
+        const ChunkEntry en = p.entry[++c.at.e];
+        c.at = Place{c.at.e, en.b, 0, en.rg, en.tiles, 0};
+      }
+    }
     c.q = seq_of(s, c.at.b);
     c.n = min(c.at.tiles - c.at.j, x1 - x);
     c.rows = min(256, c.q.n * p.G - c.at.rg * 256);
@@ -302,18 +286,17 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
     d[1] = __fdiv_rn(1.f, fv);
   };
 
-  // 512 threads have 128 registers each: the softmax takes 56 from the others, whose 8 warps give back what its 8 warps take
   if (warp < PC_SOFT) {
     // ---- softmax groups
-    more_registers<PC_SOFT_REGS>();
     const int u = warp >> 2, rl = (warp & 3) * 32 + lane;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const float scale_log2 = 1.4426950408889634f * rsqrtf((float)D);
     uint32_t phase = 0;                                         // of CB_S[u]
     bool ok = true;
     int tiles_done = 0;                                         // of the run, for the scales' ring
+    Piece c;
     for (int x = x0; x < x1;) {                                 // (one that gave up goes on, without waits: the groups have barriers)
-      const Piece c = piece_at(x);
+      c = x == x0 ? piece_at(x) : piece_at(x, &c);
       const int r = (c.two ? u * 128 : 0) + rl;                 // row of the item
       const bool has = r < c.rows;
       const bool work = (c.two ? u * 128 : 0) + (warp & 3) * 32 < c.rows;            // warp-uniform
@@ -378,52 +361,29 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
             }
             tmem_wait_st();
           }
-          // One pass: the weights against the reference as it is, and the maximum beside them.  Where the reference turns out to
-          // be exceeded by more than 2^4 (a block's first tiles), it is renewed, O with it, and the pass taken again; S is still
-          // there, for the weights stay in registers until then.
-          uint32_t pk[64];
-          float sum;
-          for (;;) {
-            const float ref = PC_HEAD - (m_run == -INFINITY ? 0.f : m_run);
-            uint32_t x[2][32];
-            float mx = -INFINITY;
-            sum = 0.f;
-            tmem_ld32_issue(ts, x[0]);
+          // Loops of small bodies: the groups, the expanding warps and the others share each quarter of the SM's instruction cache, and
+          // straight code of a whole row's columns is waited for (the weights kept in registers over one unrolled pass: 1390 us for
+          // 1999 tokens of 64 heads at 14301, against 1119).
+          float mx = -INFINITY;
+#pragma unroll 1
+          for (int h2 = 0; h2 < 2; ++h2) {
+            uint32_t xa[32], xb[32];
+            tmem_ld32_issue(ts + 64 * h2, xa);
+            tmem_ld32_issue(ts + 64 * h2 + 32, xb);
+            tmem_wait(xa);
+            tmem_wait(xb);
+            float mx0 = -INFINITY, mx1 = -INFINITY;
 #pragma unroll
-            for (int box = 0; box < 4; ++box) {
-              uint32_t (&v)[32] = x[box & 1];
-              tmem_wait(v);
-              if (box < 3) tmem_ld32_issue(ts + 32 * (box + 1), x[(box + 1) & 1]);
-              const float4 fv4 = s_fv[sr][box >> 1];
-              const float lv = box & 1 ? fv4.z : fv4.x, f = factor(s_fk[sr][box]);
-              const uint64_t sc = pack2(f, f), nm = pack2(ref + lv, ref + lv);
-              uint64_t sum2 = pack2(0.f, 0.f), sum3 = sum2;
-              float mx0 = -INFINITY, mx1 = -INFINITY;
-#pragma unroll
-              for (int i = 0; i < 16; ++i) {
-                const float a0 = __uint_as_float(v[2 * i]), a1 = __uint_as_float(v[2 * i + 1]);
-                if (i & 1) mx1 = max3(mx1, a0, a1); else mx0 = max3(mx0, a0, a1);
-                float e0, e1;
-                uint64_t y = fma2(pack2(a0, a1), sc, nm);
-                if (i % PC_POLY == PC_POLY - 1) {               // a share of the exponentials on the FMA pipe
-                  y = ex2_poly2<true>(y);
-                  unpack2(y, e0, e1);
-                } else {
-                  unpack2(y, e0, e1);
-                  e0 = ex2a(e0);
-                  e1 = ex2a(e1);
-                }
-                pk[16 * box + i] = pack_half2(e0, e1);
-                if (i & 1) sum3 = add2(sum3, pack2(e0, e1)); else sum2 = add2(sum2, pack2(e0, e1));
-              }
-              sum2 = add2(sum2, sum3);
-              float a0, a1;
-              unpack2(sum2, a0, a1);
-              sum = fmaf(a0 + a1, fminf((box & 1 ? fv4.w : fv4.y) * s0, 0x1p96f), sum);
-              mx = fmaxf(mx, fmaf(fmaxf(mx0, mx1), f, lv));
+            for (int i = 0; i < 32; i += 2) {
+              mx0 = max3(mx0, __uint_as_float(xa[i]), __uint_as_float(xa[i + 1]));
+              mx1 = max3(mx1, __uint_as_float(xb[i]), __uint_as_float(xb[i + 1]));
             }
-            const bool renew = mx > m_run + PC_SLACK;
-            if (!__any_sync(0xffffffffu, renew)) break;
+            const float4 fv = s_fv[sr][h2];
+            mx = max3(mx, fmaf(mx0, factor(s_fk[sr][2 * h2]), fv.x), fmaf(mx1, factor(s_fk[sr][2 * h2 + 1]), fv.z));
+          }
+          // a new reference only where the old one is exceeded by more than 2^4 (or there is none yet)
+          const bool renew = mx > m_run + PC_SLACK;
+          if (__any_sync(0xffffffffu, renew)) {
             const float mn = renew ? mx : m_run, corr = renew ? ex2a(m_run - mn) : 1.f;
             m_run = mn;
             l_run *= corr;
@@ -441,10 +401,38 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
               tmem_wait_st();
             }
           }
+          const float ref = PC_HEAD - (m_run == -INFINITY ? 0.f : m_run);
+          // P over columns of S that have been read
+          uint32_t v[32], pk[16];
+          tmem_ld32_issue(ts, v);
+#pragma unroll 1
+          for (int box = 0; box < 4; ++box) {
+            tmem_wait(v);
+            const float2 fv = reinterpret_cast<const float2*>(s_fv[sr])[box];
+            const float f = factor(s_fk[sr][box]), n = ref + fv.x;
+            const uint64_t sc = pack2(f, f), nm = pack2(n, n);
+            uint64_t y[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) y[i] = fma2(pack2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), sc, nm);
+            if (box < 3) tmem_ld32_issue(ts + 32 * (box + 1), v);
+            uint64_t sum2 = pack2(0.f, 0.f), sum3 = sum2;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              float e0, e1;
+              unpack2(y[i], e0, e1);
+              e0 = ex2a(e0);
+              e1 = ex2a(e1);
+              pk[i] = pack_half2(e0, e1);
+              if (i & 1) sum3 = add2(sum3, pack2(e0, e1)); else sum2 = add2(sum2, pack2(e0, e1));
+            }
+            sum2 = add2(sum2, sum3);
+            float a0, a1;
+            unpack2(sum2, a0, a1);
+            l_run = fmaf(a0 + a1, fminf(fv.y * s0, 0x1p96f), l_run);
+            __syncwarp();
+            tmem_st(ts + 16 * box, pk);
+          }
           any = true;
-          l_run += sum;
-          __syncwarp();
-          tmem_st64(ts, pk);
           tmem_wait_st();
           asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
         }
@@ -462,101 +450,102 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
       }
       const bool whole = c.at.j == 0 && c.n == c.at.tiles;
       const int rec = 2 * cta + (x == x0 ? 0 : 1);
-      float f_own = 1.f, f_other = 0.f;
       if (l_run != l_run) m_run = 0.f;                          // (a sum that is no number has to be looked at)
-      float M = m_run, L = l_run;
-      constexpr int HALF = D / 2;                               // channels that are exchanged at a time
-      const uint32_t xch = sQ + SLOT;                           // the second row tile's place, free where there is one
-      auto xch_off = [&](int ch) { return xch + (uint32_t)(rl * (HALF * 4) + ((ch ^ (rl & (HALF / 4 - 1))) << 4)); };
-      if (!c.two) {                                             // the two groups' parts of a row come together in group 0
-        if (u == 1) s_ml[rl] = make_float2(any || l_run != l_run ? m_run : -INFINITY, l_run);
-        bar_sync(3, PC_SOFT * 32);
-        if (u == 0) {
-          const float2 o = s_ml[rl];
-          M = fmaxf(m_run, o.x);
-          f_own = m_run == -INFINITY ? 0.f : ex2a(m_run - M);
-          f_other = o.x == -INFINITY ? 0.f : ex2a(o.x - M);
-          L = (m_run == -INFINITY ? 0.f : l_run * f_own) + (o.x == -INFINITY ? 0.f : o.y * f_other);
+      // the sum and O in units without s0, and the reference that goes with them
+      const float m_own = m_run == -INFINITY ? m_run : m_run - log_s0;
+      // four channels of an output row: unnormalised, with the reference and the sum, where others have a part in it
+      auto put = [&](int row, int ch, float4 v, float M, float L, float inv) {
+        if (FORMAT == QP_INT8) {                                // columns 0, 1, 2, 3 are channels 0, 2, 1, 3
+          const float t = v.y;
+          v.y = v.z;
+          v.z = t;
         }
-      }
-      const bool writes = has && (c.two || u == 0);
-      const float inv = __fdiv_rn(1.f, L);
-      if (writes && !whole) p.rec_ml[(size_t)rec * 256 + r] = make_float2(M == -INFINITY ? M : M - log_s0, L);
-      uint16_t* out = a.out + ((size_t)(c.q.row0 + tok) * a.Hq + head) * D;
-      float* part = p.rec + ((size_t)rec * 256 + r) * D;
+        if (whole) {
+          const int g = c.at.rg * 256 + row, t = g / p.G;
+          *reinterpret_cast<uint2*>(a.out + ((size_t)(c.q.row0 + t) * a.Hq + c.at.h * p.G + g - t * p.G) * D + ch) =
+              make_uint2(pack_bf16x2(v.x * inv, v.y * inv), pack_bf16x2(v.z * inv, v.w * inv));
+        } else {
+          *reinterpret_cast<float4*>(p.rec + ((size_t)rec * 256 + row) * D + ch) = v;
+          if (ch == 0) p.rec_ml[(size_t)rec * 256 + row] = make_float2(M, L);
+        }
+      };
+      if (c.two) {
+        const float inv = __fdiv_rn(1.f, l_run);
+        if (work) {
 #pragma unroll 1
-      for (int half = 0; half < 2; ++half) {
-        if (!c.two) {
-          if (u == 1 && any) {
-#pragma unroll 1
-            for (int c0 = 0; c0 < HALF; c0 += 16) {
-              uint32_t o[16];
-              tmem_ld16_issue(tO(u) + lanes + half * HALF + c0, o);
-              tmem_wait16(o);
+          for (int c0 = 0; c0 < D; c0 += 16) {
+            uint32_t o[16];
+            tmem_ld16_issue(tO(u) + lanes + c0, o);
+            tmem_wait16(o);
+            const float f = any && m_run != -INFINITY ? s0 : 0.f;
 #pragma unroll
-              for (int i = 0; i < 4; ++i) sts128(xch_off(c0 / 4 + i), make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]));
+            for (int i = 0; i < 4; ++i)
+              if (has)
+                put(r, c0 + 4 * i, f == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f)
+                                            : make_float4(__uint_as_float(o[4 * i]) * f, __uint_as_float(o[4 * i + 1]) * f,
+                                                          __uint_as_float(o[4 * i + 2]) * f, __uint_as_float(o[4 * i + 3]) * f), m_own, l_run, inv);
+          }
+        }
+      } else {
+        // the two groups' parts of a row come together through shared memory: statistics in the queries' place, a
+        // quarter of the channels at a time in the second row tile's
+        constexpr int QD = D / 4, CH = QD / 4;                  // channels of a quarter, 16-byte chunks
+        const uint32_t xch = sQ + SLOT;
+        float2* s_ml = reinterpret_cast<float2*>(smem_raw + (sQ - smem_u32(smem_raw)));
+        auto total = [&](int row, float& M, float& L) {
+          M = -INFINITY;
+          L = 0.f;
+          for (int i = 0; i < 2; ++i) M = fmaxf(M, s_ml[i * 128 + row].x);
+          for (int i = 0; i < 2; ++i) {
+            const float2 ml = s_ml[i * 128 + row];
+            if (ml.x != -INFINITY) L = fmaf(ml.y, ex2a(ml.x - M), L);
+          }
+        };
+        bar_sync(3, PC_SOFT * 32);                              // both groups have seen their last product: nobody reads the queries
+        s_ml[u * 128 + rl] = make_float2(any || l_run != l_run ? m_own : -INFINITY, l_run);
+        bar_sync(3, PC_SOFT * 32);
+        float M = -INFINITY, L;
+        if (has) total(r, M, L);
+        const float f = any && has && m_own != -INFINITY ? ex2a(m_own - M) * s0 : 0.f;
+#pragma unroll 1
+        for (int quarter = 0; quarter < 4; ++quarter) {
+          if (work) {
+#pragma unroll 1
+            for (int c0 = 0; c0 < QD; c0 += 16) {
+              uint32_t o[16];
+              if (any) {
+                tmem_ld16_issue(tO(u) + lanes + quarter * QD + c0, o);
+                tmem_wait16(o);
+              }
+#pragma unroll
+              for (int i = 0; i < 16; ++i) o[i] = f != 0.f ? __float_as_uint(__uint_as_float(o[i]) * f) : 0u;
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                sts128(xch + (u * 128 + rl) * (QD * 4) + (((c0 / 4 + i) ^ (rl & (CH - 1))) << 4), make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]));
             }
           }
           bar_sync(3, PC_SOFT * 32);
-        }
-        if (work && (c.two || u == 0)) {
-#pragma unroll 1
-          for (int c0 = 0; c0 < HALF; c0 += 16) {
-            uint32_t o[16];
-            if (any) {
-              tmem_ld16_issue(tO(u) + lanes + half * HALF + c0, o);
-              tmem_wait16(o);
+          for (int i = tid; i < c.rows * CH; i += PC_SOFT * 32) {
+            const int row = i / CH, ch = i % CH;
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int k = 0; k < 2; ++k) {
+              const int at = k * 128 + row;
+              const uint4 w = lds128(xch + at * (QD * 4) + ((ch ^ (at & (CH - 1))) << 4));
+              v.x += __uint_as_float(w.x); v.y += __uint_as_float(w.y);
+              v.z += __uint_as_float(w.z); v.w += __uint_as_float(w.w);
             }
-            float v[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = any && f_own != 0.f ? __uint_as_float(o[i]) * f_own : 0.f;
-            if (!c.two && f_other != 0.f) {
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const uint4 w = lds128(xch_off(c0 / 4 + i));
-                v[4 * i] = fmaf(__uint_as_float(w.x), f_other, v[4 * i]);
-                v[4 * i + 1] = fmaf(__uint_as_float(w.y), f_other, v[4 * i + 1]);
-                v[4 * i + 2] = fmaf(__uint_as_float(w.z), f_other, v[4 * i + 2]);
-                v[4 * i + 3] = fmaf(__uint_as_float(w.w), f_other, v[4 * i + 3]);
-              }
-            }
-            if (FORMAT == QP_INT8) {                            // columns 0, 1, 2, 3 are channels 0, 2, 1, 3
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const float t = v[4 * i + 1];
-                v[4 * i + 1] = v[4 * i + 2];
-                v[4 * i + 2] = t;
-              }
-            }
-            if (writes) {
-              const int ch = half * HALF + c0;
-              if (whole) {
-                uint32_t w[8];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  w[2 * i] = pack_bf16x2(v[4 * i] * inv * s0, v[4 * i + 1] * inv * s0);
-                  w[2 * i + 1] = pack_bf16x2(v[4 * i + 2] * inv * s0, v[4 * i + 3] * inv * s0);
-                }
-                *reinterpret_cast<uint4*>(out + ch) = make_uint4(w[0], w[1], w[2], w[3]);
-                *reinterpret_cast<uint4*>(out + ch + 8) = make_uint4(w[4], w[5], w[6], w[7]);
-              } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                  *reinterpret_cast<float4*>(part + ch + 4 * i) = make_float4(v[4 * i] * s0, v[4 * i + 1] * s0, v[4 * i + 2] * s0, v[4 * i + 3] * s0);
-              }
-            }
+            float rM, rL;
+            total(row, rM, rL);
+            put(row, quarter * QD + 4 * ch, v, rM, rL, __fdiv_rn(1.f, rL));
           }
+          bar_sync(3, PC_SOFT * 32);
         }
-        if (!c.two) bar_sync(3, PC_SOFT * 32);
       }
       asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
       tiles_done += c.n;
       x += c.n;
     }
-    fewer_registers<128>();
-  } else {
-    fewer_registers<256 - PC_SOFT_REGS>();
-    if (warp == PC_MMA) {
+  } else if (warp == PC_MMA) {
     // ---- products.  Operands in the ring: keys of tile 0, values of tile 0, keys of tile 1, ..., across pieces
     bool ok = true;
     Slot kr{0}, vr{1};
@@ -598,8 +587,9 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
       if (elect_one()) umma_commit(done);
       __syncwarp();
     };
+    Piece c;
     for (int x = x0; x < x1 && ok;) {
-      const Piece c = piece_at(x);
+      c = x == x0 ? piece_at(x) : piece_at(x, &c);
       ok = mbar_wait_warp(bar(CB_Q, 0), pq, gu);
       pq ^= 1u;
       if (c.two) {
@@ -648,8 +638,9 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
       bool ok = true;
       const int lg = 31 - __clz(s.page / 32), box = lane & 3, team = lane >> 2;       // lg: log2 of boxes per page
       int n_box = 0, tile = 0;                                  // boxes copied, tiles of the run before this one
+      Piece c;
       for (int x = x0; x < x1 && ok;) {
-        const Piece c = piece_at(x);
+        c = x == x0 ? piece_at(x) : piece_at(x, &c);
         const int whole = whole_tokens(c);
         int window = -64, w_id = -1;                            // 32 pages: ids and scales in the lanes
         float w_ks = NAN, w_vs = NAN;
@@ -704,8 +695,9 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
       bool ok = true;
       Slot wr{team};
       int n_box = 0, tile = 0;
+      Piece c;
       for (int x = x0; x < x1 && ok;) {
-        const Piece c = piece_at(x);
+        c = x == x0 ? piece_at(x) : piece_at(x, &c);
         const int whole = whole_tokens(c), end = c.q.len + c.q.n;
         for (int k = 0; k < c.n && ok; ++k, ++tile) {
           const int t0 = 128 * (c.at.j + k), boxes = min(4, max(0, (whole - t0) / 32));
@@ -768,8 +760,6 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
       }
       if (!ok) give_up = 1;
     }
-    more_registers<128>();
-  }
   asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
