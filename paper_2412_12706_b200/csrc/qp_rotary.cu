@@ -229,6 +229,9 @@ append_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ qp_r
   __shared__ __align__(16) float2 table[ROT_TOKENS * 64];
   __shared__ int s_pos[ROT_TOKENS];
   __shared__ uint32_t s_max[THREADS / 32];
+  __shared__ uint64_t turn[64];                                 // (each lane reads another: constant memory answers one at a time)
+  if (threadIdx.x < rope.rot_dim >> 1) turn[threadIdx.x] = rope.turn[threadIdx.x];
+  __syncthreads();
   chain_enter();
   const int bid = blockIdx.x, tid = threadIdx.x;
   const StepView& s = a.s;
@@ -251,7 +254,7 @@ append_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ qp_r
     auto fill = [&]() {
       for (int i = tid; i < n * pitch; i += THREADS) {
         const int t = i / pitch, p = i - t * pitch;
-        if (p < half) table[i] = cos_sin(rope.turn[p], s_pos[t], rope.factor);
+        if (p < half) table[i] = cos_sin(turn[p], s_pos[t], rope.factor);
       }
       __syncthreads();
     };
@@ -291,7 +294,7 @@ append_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ qp_r
     if (fresh && keys && rot) {
       const int at = a.pos ? __ldg(a.pos + r) : p;
       rotate_unit<MODE>(x, y, u, rot, row, [&](int j) {
-        const float2 c = cos_sin(rope.turn[j], at, rope.factor), d = cos_sin(rope.turn[min(j + 1, 63)], at, rope.factor);
+        const float2 c = cos_sin(turn[j], at, rope.factor), d = cos_sin(turn[min(j + 1, (rot >> 1) - 1)], at, rope.factor);
         return make_float4(c.x, c.y, d.x, d.y);
       });
     }

@@ -8,6 +8,7 @@ when the library has not been built.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from dataclasses import dataclass
 
@@ -878,14 +879,20 @@ def rope(rot_dim: int, base: float = 10000.0, interleaved: bool = False, scaling
     return r
 
 
-_Strides = ctypes.c_int64 * 3
+_contiguous, _empty_like, _bf16, _int32 = torch.contiguous_format, torch.empty_like, torch.bfloat16, torch.int32
 
 
-def _strides(t: torch.Tensor, b: int, h: int, n: int):
+@functools.lru_cache(maxsize=256)
+def _int64x3(a: int, b: int, c: int):
+    """A host array of these numbers for the library to read."""
+    return (ctypes.c_int64 * 3)(a, b, c)
+
+
+def _strides(t: torch.Tensor, b: int, h: int, n: int, device: int):
     """Strides of batch, head and token as qp_rotary takes them (0 where there is one only)."""
     sb, sh, sn, sd = t.stride()
-    assert t.dtype is torch.bfloat16 and t.get_device() == _current_device() and sd == 1, (t.device, t.dtype, t.stride())
-    return _Strides(sb if b > 1 else 0, sh if h > 1 else 0, sn if n > 1 else 0)
+    assert t.dtype is _bf16 and t.get_device() == device and sd == 1, (t.device, t.dtype, t.stride())
+    return _int64x3(sb if b > 1 else 0, sh if h > 1 else 0, sn if n > 1 else 0)
 
 
 def rotary(x: torch.Tensor, pos: torch.Tensor, rope_: qp_rope, out: torch.Tensor | None = None, transpose: bool = False) -> torch.Tensor:
@@ -893,20 +900,22 @@ def rotary(x: torch.Tensor, pos: torch.Tensor, rope_: qp_rope, out: torch.Tensor
     rotated by pos int32 [L] or [Bt,L]; ``out`` may be x.  transpose: by the negative angles (the gradient; the way back where the
     rotation has no factor)."""
     Bt, H, L, D = x.shape
-    fresh = out is None
-    if fresh:
-        out = x.new_empty(x.shape)
-    assert fresh or out.shape == x.shape
+    device = _current_device()
+    xs = _strides(x, Bt, H, L, device)
+    if out is None:
+        out = _empty_like(x, memory_format=_contiguous)
+        to = _int64x3(H * L * D, L * D, D)
+    else:
+        assert out.shape == x.shape
+        to = _strides(out, Bt, H, L, device)
+        assert (to[0] or Bt == 1) and (to[1] or H == 1) and (to[2] or L == 1), "rows of out overlap"
     if pos.dim() == 1:
-        _dev(pos, torch.int32, (L,))
+        _dev(pos, _int32, (L,))
         ps = 0
     else:
-        _dev(pos, torch.int32, (Bt, L))
+        _dev(pos, _int32, (Bt, L))
         ps = L
-    to = _Strides(H * L * D, L * D, D) if fresh else _strides(out, Bt, H, L)
-    assert fresh or ((to[0] or Bt == 1) and (to[1] or H == 1) and (to[2] or L == 1)), "rows of out overlap"
-    status = lib().qp_rotary(x.data_ptr(), _strides(x, Bt, H, L), out.data_ptr(), to, Bt, H, L, D, pos.data_ptr(), ps, ctypes.byref(rope_),
-                             int(transpose), _stream())
+    status = lib().qp_rotary(x.data_ptr(), xs, out.data_ptr(), to, Bt, H, L, D, pos.data_ptr(), ps, ctypes.byref(rope_), int(transpose), _stream())
     if status:
         _check(status, "qp_rotary")
     return out
@@ -931,6 +940,11 @@ class PagedCache:
     v_scale: torch.Tensor
     k_tail: torch.Tensor     # bf16 [n_seqs,Hkv,page,D]
     v_tail: torch.Tensor
+
+    def __post_init__(self):
+        d = self.desc
+        self.ref = ctypes.byref(d)                              # (nothing of the descriptor changes from call to call)
+        self.heads, self.table, self.device = (d.n_q_heads, d.n_kv_heads, d.head_dim), (d.n_seqs, d.max_pages), self.k_codes.get_device()
 
 
 def paged_layout(n_seqs: int, n_q_heads: int, n_kv_heads: int, head_dim: int, format: int, page: int, n_pages: int,
@@ -977,19 +991,23 @@ class PagedStep:
         self.start, self.len, self.pages, self.n_tokens, self.max_new = start, len, pages, n_tokens, max_new
         self.shape, self.device = (n_seqs, max_pages), start.get_device()
         self.desc = qp_step(n_tokens, max_new, start.data_ptr(), len.data_ptr(), pages.data_ptr())
+        self.ref = ctypes.byref(self.desc)
 
 
-def _token_rows(t: torch.Tensor, n: int, heads: int, D: int) -> int:
-    """bf16 rows [n, heads, D] whose heads lie one behind the other, on the current device: elements from a row to the next."""
-    assert (t.dtype is torch.bfloat16 and t.shape == (n, heads, D) and t.get_device() == _current_device() and t.stride(2) == 1
-            and (heads == 1 or t.stride(1) == D)), (t.device, t.dtype, t.shape, t.stride())
-    return t.stride(0) if n > 1 else heads * D
+def _token_rows(t: torch.Tensor, n: int, heads: int, D: int, device: int) -> int:
+    """bf16 rows [n, heads, D] whose heads lie one behind the other, on the device in use: elements from a row to the next."""
+    row, head, one = t.stride()
+    assert (t.dtype is _bf16 and t.shape == (n, heads, D) and t.get_device() == device and one == 1 and (head == D or heads == 1)), \
+        (t.device, t.dtype, t.shape, t.stride())
+    return row if n > 1 else heads * D
 
 
-def _fits(cache: PagedCache, step: PagedStep) -> None:
-    d = cache.desc
-    assert step.shape == (d.n_seqs, d.max_pages) and step.device == _current_device() == cache.k_codes.get_device(), \
+def _fits(cache: PagedCache, step: PagedStep) -> int:
+    """The device in use, which both have to be on."""
+    device = _current_device()
+    assert step.shape == cache.table and step.device == device == cache.device, \
         "step and cache do not belong together, or are not on the current device"
+    return device
 
 
 def paged_append(k_new: torch.Tensor, v_new: torch.Tensor, cache: PagedCache, step: PagedStep, rope_: "qp_rope | None" = None,
@@ -997,21 +1015,20 @@ def paged_append(k_new: torch.Tensor, v_new: torch.Tensor, cache: PagedCache, st
     """qp_paged_append: the step's keys and values [n_tokens,Hkv,D] go into the cache, keys rotated unless rope_ is None, at the
     tokens' positions in their sequences or at ``pos`` int32 [n_tokens]; returns the step's queries q [n_tokens,Hq,D] rotated, if
     they are given.  Rows may be parts of a fused projection's."""
-    d, n = cache.desc, step.n_tokens
-    _fits(cache, step)
-    ks, vs = _token_rows(k_new, n, d.n_kv_heads, d.head_dim), _token_rows(v_new, n, d.n_kv_heads, d.head_dim)
-    qs = 0
+    n, (Hq, Hkv, D), device = step.n_tokens, cache.heads, _fits(cache, step)
+    ks, vs = _token_rows(k_new, n, Hkv, D, device), _token_rows(v_new, n, Hkv, D, device)
+    qs, q_from, q_to = 0, None, None
     if q is not None:
-        qs = _token_rows(q, n, d.n_q_heads, d.head_dim)
+        qs, q_from = _token_rows(q, n, Hq, D, device), q.data_ptr()
         if q_out is None:
-            q_out = q.new_empty((n, d.n_q_heads, d.head_dim))
+            q_out = _empty_like(q, memory_format=_contiguous)
         else:
-            _dev(q_out, torch.bfloat16, (n, d.n_q_heads, d.head_dim))
+            _dev(q_out, _bf16, (n, Hq, D))
+        q_to = q_out.data_ptr()
     if pos is not None:
-        _dev(pos, torch.int32, (n,))
-    status = lib().qp_paged_append(k_new.data_ptr(), ks, v_new.data_ptr(), vs, ctypes.byref(d), ctypes.byref(step.desc),
-                                   None if rope_ is None else ctypes.byref(rope_), _ptr(pos), _ptr(q), qs, None if q is None else _ptr(q_out),
-                                   _stream())
+        _dev(pos, _int32, (n,))
+    status = lib().qp_paged_append(k_new.data_ptr(), ks, v_new.data_ptr(), vs, cache.ref, step.ref, None if rope_ is None else ctypes.byref(rope_),
+                                   None if pos is None else pos.data_ptr(), q_from, qs, q_to, _stream())
     if status:
         _check(status, "qp_paged_append")
     return None if q is None else q_out
@@ -1025,16 +1042,16 @@ def paged_attn(q: torch.Tensor, cache: PagedCache, step: PagedStep, out: torch.T
                workspace: torch.Tensor | None = None) -> torch.Tensor:
     """qp_paged_attn: attention of the step's tokens, which paged_append has taken in, over their sequences: q [n_tokens,Hq,D] ->
     out [n_tokens,Hq,D] (rows that are no sequence's are left as they are)."""
-    d, n = cache.desc, step.n_tokens
-    _fits(cache, step)
-    qs = _token_rows(q, n, d.n_q_heads, d.head_dim)
+    n, (Hq, _, D), device = step.n_tokens, cache.heads, _fits(cache, step)
+    qs = _token_rows(q, n, Hq, D, device)
     if out is None:
-        out = q.new_empty((n, d.n_q_heads, d.head_dim))
+        out = _empty_like(q, memory_format=_contiguous)
     else:
-        _dev(out, torch.bfloat16, (n, d.n_q_heads, d.head_dim))
+        _dev(out, _bf16, (n, Hq, D))
     if workspace is None:
         workspace = new_decode_workspace(paged_attn_workspace_bytes(cache, n, step.max_new), q.device)
-    status = lib().qp_paged_attn(q.data_ptr(), qs, ctypes.byref(d), ctypes.byref(step.desc), out.data_ptr(), *_scratch(workspace), _stream())
+    address, size = _scratch(workspace)
+    status = lib().qp_paged_attn(q.data_ptr(), qs, cache.ref, step.ref, out.data_ptr(), address, size, _stream())
     if status:
         _check(status, "qp_paged_attn")
     return out
@@ -1045,13 +1062,12 @@ def paged_layer_step(q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, 
                      workspace: torch.Tensor | None = None) -> torch.Tensor:
     """One layer of a step: qp_paged_append (with the queries, if there is a rotation), then qp_paged_attn.  A step that is refused
     has changed nothing: what the second call asks for is looked at before the first takes the tokens in."""
-    d, n = cache.desc, step.n_tokens
-    _fits(cache, step)
-    stride = _token_rows(q, n, d.n_q_heads, d.head_dim)
+    n, (Hq, _, D), device = step.n_tokens, cache.heads, _fits(cache, step)
+    stride = _token_rows(q, n, Hq, D, device)
     if out is None:
-        out = q.new_empty((n, d.n_q_heads, d.head_dim))
+        out = _empty_like(q, memory_format=_contiguous)
     else:
-        _dev(out, torch.bfloat16, (n, d.n_q_heads, d.head_dim))
+        _dev(out, _bf16, (n, Hq, D))
     need = paged_attn_workspace_bytes(cache, n, step.max_new)
     if workspace is None:
         workspace = new_decode_workspace(need, q.device)

@@ -216,6 +216,7 @@ def library(lib, monkeypatch):
     monkeypatch.setattr(qp, "lib", lambda: fake)
     monkeypatch.setattr(qp, "_current_device", lambda: 0)
     monkeypatch.setattr(qp, "_stream", lambda: 0)
+    monkeypatch.setattr(qp, "_empty_like", lambda t, memory_format=None: t.new_empty(t.shape))
     return fake
 
 
