@@ -487,8 +487,9 @@ qp_status qp_rotary(const void* x, const int64_t* x_stride /* host, 3 */, void* 
  * the stored scale, rounded to nearest even.  Pages are only ever whole, so what a page holds does not depend on how its tokens came
  * in; a whole page is not written again and can be in several sequences' tables (a shared beginning of two prompts).
  * A sequence keeps its row b of the tails and of the page table as long as it lives; a row whose sequence has ended serves the next.
- * n_seqs <= QP_MAX_SEQS, head_dim 64 or 128, page 32, 64 or 128, n_pages * Hkv * page and n_seqs * Hkv * page < 2^31 - 1024,
- * max_pages * page < 2^31 - 1024.
+ * A number that is not finite makes the scale, and with it every token of its page and head, so.
+ * n_seqs <= QP_MAX_SEQS, at most 2^16 query heads, 8 for each KV head, head_dim 64 or 128, page 32, 64 or 128, n_pages * Hkv * page,
+ * n_seqs * Hkv * page and max_pages * page < 2^31 - 1024.
  */
 #define QP_E4M3 0
 #define QP_INT8 1
@@ -511,7 +512,9 @@ qp_status qp_paged_layout(int n_seqs, int n_q_heads, int n_kv_heads, int head_di
  * n_tokens and max_new (rows of the arrays that are no sequence's are not looked at, and left as they are in outputs).
  * A sequence whose numbers do not belong together (rows outside 0 .. n_tokens-1, more than max_new new tokens, a negative len, more
  * positions than its row of the page table) is left out, nothing of it is written; a page number outside the pool is not written to,
- * and makes attention rows of its sequence NaN: those that read it, and possibly others of the step.  len[b] may be set back only to where b's last whole page ends or behind.
+ * and makes attention rows of its sequence NaN: those that read it, and possibly others of the step.  Rows that two sequences claim
+ * come out as one of them has them, or are left out with the whole step.  len[b] may be set back only to where b's last whole page
+ * ends or behind.
  */
 typedef struct qp_step {
   int32_t n_tokens;      /* rows of the step's arrays */
@@ -535,8 +538,12 @@ qp_status qp_paged_append(const void* k_new, int64_t k_stride, const void* v_new
 /*
  * Attention of the step's tokens, after qp_paged_append has taken them in: the token at position p of its sequence sees the tokens at
  * positions <= p,   out[r,h,:] = softmax_t(q[r,h].K[t] / sqrt(D)) V.   q bf16 rows [n_tokens, Hq, D] (device), q_stride elements apart;
- * out bf16 [n_tokens, Hq, D], contiguous.  Magnitudes are free (queries and waiting rows meet the tensor cores scaled by powers of
- * two), but that with more than 16 query rows per KV head the value scales of a head's pages have to be within 2^90 of one another.
+ * out bf16 [n_tokens, Hq, D], contiguous.  Queries and waiting rows meet the tensor cores scaled by powers of two, so magnitudes are
+ * free as long as queries, values and their logits stay below 2^100; with more than 32 query rows per KV head (max_new * Hq / Hkv) the
+ * value scales of a head's pages have to be within 2^90 of one another, too, and what is below 2^-24 of the largest number in 32
+ * waiting rows of a head counts for nothing (as little as it will when their page is whole).  Rows that see a key or value that is not finite, or a
+ * query of their own, are NaN or what the formula makes of it; a value that is not finite may also make NaN of rows of the same step
+ * and sequence that stand before it.
  * workspace: its contents are irrelevant; calls that may run at the same time must not share it.
  * Bounded waits as for qp_window_scores; one that runs out makes the rows that hang on it NaN.
  */

@@ -897,7 +897,8 @@ static qp_status check_paged(const qp_paged* c, bool need_ptrs) {
   qp_status s = check_shape(1, c->n_q_heads, c->n_kv_heads, c->head_dim);
   if (s != QP_OK) return s;
   if (c->n_seqs < 1 || c->n_pages < 1 || c->max_pages < 1) return QP_ERR_INVALID_ARG;
-  if ((c->format != QP_E4M3 && c->format != QP_INT8) || !ok_group(c->page) || c->n_seqs > QP_MAX_SEQS) return QP_ERR_UNSUPPORTED;
+  if ((c->format != QP_E4M3 && c->format != QP_INT8) || !ok_group(c->page) || c->n_seqs > QP_MAX_SEQS || c->n_q_heads > 1 << 16)
+    return QP_ERR_UNSUPPORTED;
   const long long most = 0x7fffffffLL - 1024, rows = (long long)c->n_kv_heads * c->page;
   if (rows > most || c->n_pages > most / rows || c->n_seqs > most / rows || c->max_pages > most / c->page) return QP_ERR_UNSUPPORTED;
   if (need_ptrs) {

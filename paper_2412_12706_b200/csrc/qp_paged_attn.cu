@@ -719,7 +719,7 @@ cudaError_t launch_decode_t(const PagedLaunch& p, const CUtensorMap (&m)[4], cud
 bool paged_attn_fits(int n_seqs, int n_tokens, int max_new, int Hq, int Hkv, long long most_len) {
   if (many_rows(max_new, Hq / Hkv)) return paged_chunk_fits(n_seqs, n_tokens, Hq, Hkv, most_len);
   const long long G = Hq / Hkv, items = Hkv * (n_tokens * G / rows_of(max_new, (int)G) + n_seqs);
-  return items * (most_len / 32 + 8) < 0x7fffffffLL;
+  return items < 0x7fffffffLL / (most_len / 32 + 8);
 }
 size_t paged_attn_workspace(int n_seqs, int n_tokens, int max_new, int Hq, int Hkv, int D) {
   if (many_rows(max_new, Hq / Hkv)) return paged_chunk_workspace(n_seqs, n_tokens, Hq, Hkv, D);

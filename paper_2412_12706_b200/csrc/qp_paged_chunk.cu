@@ -44,10 +44,14 @@ constexpr float PC_HEAD = 11.f, PC_SLACK = 4.f;                 // see PA_HEAD, 
 struct ChunkEntry {                                             // 256 rows of a sequence
   int tile, tiles, b, rg;                                       // first of its Hkv * tiles tiles
 };
+struct Place {                                                  // a tile of the flat sequence: entry, its numbers, head, place in the item
+  int e, b, h, rg, tiles, j;
+};
 struct ChunkLaunch {
   PagedAttnArgs a;
   int G, max_entries;
   int* head;                                                    // {entries, tiles}
+  Place* cut;                                                   // [PC_BLOCKS]: where each block's run begins
   ChunkEntry* entry;
   float* rec;                                                   // [2 * PC_BLOCKS][256][D]
   float2* rec_ml;                                               // [2 * PC_BLOCKS][256]
@@ -56,7 +60,7 @@ struct ChunkLaunch {
 __device__ __forceinline__ int c_start(int c, int T) { return (int)((long long)T * c / PC_BLOCKS); }
 __device__ __forceinline__ int c_owner(int x, int T) { return (int)((((long long)x + 1) * PC_BLOCKS - 1) / T); }
 
-// numbers the items' tiles: one thread for a sequence, then one for 256 rows of one
+// numbers the items' tiles, one thread for a sequence, then one for 256 rows of one, and finds where the blocks' runs begin
 __global__ void __launch_bounds__(1024)
 chunk_plan_kernel(const __grid_constant__ ChunkLaunch p) {
   __shared__ int s_sum[32], s_first[QP_MAX_SEQS + 1];           // first entry of every sequence
@@ -113,21 +117,18 @@ chunk_plan_kernel(const __grid_constant__ ChunkLaunch p) {
     p.head[0] = entries;
     p.head[1] = tiles;
   }
-}
-
-// a tile of the flat sequence
-struct Place {
-  int e, b, h, rg, tiles, j;
-};
-__device__ __forceinline__ Place place_of(const ChunkLaunch& p, int entries, int x) {
-  int lo = 0, hi = entries;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (p.entry[mid].tile <= x) lo = mid; else hi = mid;
+  __syncthreads();                                              // (the entries are this block's own writes)
+  const int x = c_start(tid, tiles);
+  if (tid < PC_BLOCKS && x < tiles) {
+    int lo = 0, hi = entries;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (p.entry[mid].tile <= x) lo = mid; else hi = mid;
+    }
+    const ChunkEntry en = p.entry[lo];
+    const int in = x - en.tile, h = in / en.tiles;
+    p.cut[tid] = Place{lo, en.b, h, en.rg, en.tiles, in - h * en.tiles};
   }
-  const ChunkEntry en = p.entry[lo];
-  const int in = x - en.tile, h = in / en.tiles;
-  return Place{lo, en.b, h, en.rg, en.tiles, in - h * en.tiles};
 }
 
 // byte offset of 16-byte chunk c of row r in an operand tile of 128 rows
@@ -175,6 +176,11 @@ __device__ __forceinline__ uint32_t abs_max(uint32_t m, const uint4& v) {
   m = __vmaxu2(m, v.z & 0x7fff7fffu);
   return __vmaxu2(m, v.w & 0x7fff7fffu);
 }
+// infinities and what is no number out of it
+__device__ __forceinline__ uint4 finite(const uint4& v) {
+  auto f = [](uint32_t w) { return w & __vcmpltu2(w & 0x7fff7fffu, 0x7f807f80u); };
+  return make_uint4(f(v.x), f(v.y), f(v.z), f(v.w));
+}
 // the power of two that brings the magnitude with these bf16 bits into [1, 2), and its inverse
 __device__ __forceinline__ float2 to_one(uint32_t m) {
   m = max(m & 0xffffu, m >> 16);
@@ -206,7 +212,7 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
   extern __shared__ unsigned char smem_raw[];
   __shared__ uint64_t bars[CB_COUNT];
   __shared__ float s_fk[PC_SCALES][4];                          // per 32 tokens: what S is multiplied by
-  __shared__ float4 s_fv[PC_SCALES][2];                         // log2 of the values' scale, its inverse, for two times 32 tokens
+  __shared__ float4 s_fv[PC_SCALES][2];                         // log2 of the values' scale, 2^-6 / scale, for two times 32 tokens
   __shared__ uint32_t tmem_base_slot;
   __shared__ int give_up;
   const PagedAttnArgs& a = p.a;
@@ -243,7 +249,7 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
   asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
   const uint32_t tmem = tmem_base_slot;
   chain_enter();
-  const int entries = p.head[0], T = p.head[1], cta = blockIdx.x;
+  const int T = p.head[1], cta = blockIdx.x;
   const int x0 = c_start(cta, T), x1 = c_start(cta + 1, T);
   auto tS = [&](int u) { return tmem + (uint32_t)u * 128u; };
   auto tO = [&](int u) { return tmem + 256u + (uint32_t)u * D; };
@@ -254,11 +260,11 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
     Seq q;
     int n, rows, two;
   };
-  // the first is searched for, the others follow one another: the next head, or the next entry
+  // the first has been found, the others follow one another: the next head, or the next entry
   auto piece_at = [&](int x, const Piece* before = nullptr) {
     Piece c;
     if (!before) {
-      c.at = place_of(p, entries, x);
+      c.at = p.cut[cta];
     } else {
       c.at = before->at;
       c.at.j = 0;
@@ -276,14 +282,15 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
 
   // tokens of a piece's sequence that are in whole pages
   auto whole_tokens = [&](const Piece& c) { return (c.q.len + c.q.n) / s.page * s.page; };
-  // Of a 32-token box: what the product with its keys is multiplied by; of its values the log2 of that, and its inverse.  Written with
-  // the keys: the softmax of a tile begins when they are there, whatever has become of the values.
+  // Of a 32-token box: what the product with its keys is multiplied by; of its values the log2 of that, and its inverse, times 2^-6 so
+  // that the smallest bf16 number has one.  Written with the keys: the softmax of a tile begins when they are there, whatever has
+  // become of the values.
   auto set_scales = [&](int tile, int box, float fk, float fv) {
     s_fk[tile & (PC_SCALES - 1)][box] = fk;
     fv = fv == 0.f ? 0x1p-60f : fv;                             // zeros: any scale that leaves the others theirs
     float* d = reinterpret_cast<float*>(&s_fv[tile & (PC_SCALES - 1)][box >> 1]) + 2 * (box & 1);
     d[0] = log2f(fv);
-    d[1] = __fdiv_rn(1.f, fv);
+    d[1] = __fdiv_rn(0x1p-6f, fv);
   };
 
   if (warp < PC_SOFT) {
@@ -332,7 +339,7 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
       };
       const int lim = has ? c.q.len + tok + 1 : 0;              // positions this row sees
       const int least = c.q.len + (c.at.rg * 256) / p.G + 1;    // and the item's first row
-      float m_run = -INFINITY, l_run = 0.f;
+      float m_run = -INFINITY, l_run = 0.f;                     // (the sum is times 2^-6 until the piece ends)
       float s0 = 1.f, log_s0 = 0.f;
       bool any = false;
       for (int k = c.two ? 0 : u; k < c.n && ok; k += c.two ? 1 : 2) {
@@ -345,8 +352,9 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
           const uint32_t ts = tS(u) + lanes;
           const int sr = (tiles_done + k) & (PC_SCALES - 1);
           if (!any) {                                           // (both groups: of the first tile)
-            log_s0 = s_fv[tiles_done & (PC_SCALES - 1)][0].x;
-            s0 = ex2a(log_s0);
+            const float4 fv = s_fv[tiles_done & (PC_SCALES - 1)][0];
+            log_s0 = fv.x;
+            s0 = __fdiv_rn(0x1p-6f, fv.y);
           }
           if (128 * (j + 1) > least) {                          // what the row does not see leaves S
 #pragma unroll 1
@@ -428,7 +436,7 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
             sum2 = add2(sum2, sum3);
             float a0, a1;
             unpack2(sum2, a0, a1);
-            l_run = fmaf(a0 + a1, fminf(fv.y * s0, 0x1p96f), l_run);
+            l_run = fmaf(a0 + a1, fminf(fv.y * s0, 0x1p90f), l_run);
             __syncwarp();
             tmem_st(ts + 16 * box, pk);
           }
@@ -439,6 +447,7 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(CB_P, u));
       }
+      l_run *= 64.f;
       // O is complete with one more commit
       ok = ok && mbar_wait_warp(bar(CB_S, u), phase, gu);
       phase ^= 1u;
@@ -638,6 +647,8 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
       bool ok = true;
       const int lg = 31 - __clz(s.page / 32), box = lane & 3, team = lane >> 2;       // lg: log2 of boxes per page
       int n_box = 0, tile = 0;                                  // boxes copied, tiles of the run before this one
+      uint32_t left = 0;                                        // of the last tile with boxes: lanes that could not copy theirs
+      int n_last = 0;                                           // and its boxes
       Piece c;
       for (int x = x0; x < x1 && ok;) {
         c = x == x0 ? piece_at(x) : piece_at(x, &c);
@@ -672,17 +683,22 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
             }
             if (y >= TC_SPIN_LIMIT || ((y & 255u) == 255u && *gu)) break;
           }
-          ok = !__any_sync(0xffffffffu, todo);
+          left = __ballot_sync(0xffffffffu, todo);
+          ok = left == 0;
+          n_last = boxes;
           n_box += boxes;
         }
         x += c.n;
       }
       if (!ok) give_up = 1;
       // nothing may still be on its way into this block's shared memory when it is given up: the last copies are waited for (bounded)
-      for (int i = max(0, n_box - PC_RAW); ok && i < n_box; ++i)
-        for (int h = 0; h < 2; ++h)
-          for (uint32_t y = 0; y < TC_SPIN_LIMIT; ++y)
-            if (mbar_try_wait(bar(CB_RAW, h * PC_RAW + i % PC_RAW), (uint32_t)(i / PC_RAW) & 1u)) break;
+      for (int i = max(0, n_box - PC_RAW); i < n_box; ++i)
+        for (int h = 0; h < 2; ++h) {
+          const int in_last = i - (n_box - n_last);             // (a box that could not be copied: its stage's one before)
+          const int n = in_last >= 0 && (left >> (4 * h + in_last) & 1u) ? i - PC_RAW : i;
+          for (uint32_t y = 0; n >= 0 && y < TC_SPIN_LIMIT; ++y)
+            if (mbar_try_wait(bar(CB_RAW, h * PC_RAW + n % PC_RAW), (uint32_t)(n / PC_RAW) & 1u)) break;
+        }
     } else {
       // ---- codes to operands
       const int team = (warp - PC_SOFT) / PC_TEAM, tw = (warp - PC_SOFT) % PC_TEAM;
@@ -735,7 +751,7 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
               uint32_t m = 0u;
               if (t < end)
 #pragma unroll 4
-                for (int q = 0; q < D / 8; ++q) m = abs_max(m, reinterpret_cast<const uint4*>(tail)[row + q]);
+                for (int q = 0; q < D / 8; ++q) m = abs_max(m, finite(reinterpret_cast<const uint4*>(tail)[row + q]));
               m = __reduce_max_sync(0xffffffffu, max(m & 0xffffu, m >> 16));
               return m ? to_one(m) : make_float2(1.f, 0.f);
             };
@@ -773,11 +789,11 @@ template <int D>
 __global__ void __launch_bounds__(256)
 chunk_merge_kernel(const __grid_constant__ ChunkLaunch p) {
   chain_enter();
-  const int entries = p.head[0], T = p.head[1], cut = blockIdx.y + 1;
+  const int T = p.head[1], cut = blockIdx.y + 1;
   if (T == 0) return;
   const int x = c_start(cut, T);
   if (x >= T || x == c_start(cut - 1, T)) return;               // (runs without tiles)
-  const Place at = place_of(p, entries, x);
+  const Place at = p.cut[cut];
   const int first = x - at.j, last = first + at.tiles - 1;      // the item's tiles
   if (at.j == 0 || c_owner(first, T) != cut - 1) return;        // the cut falls between items, or is not the item's first
   const PagedAttnArgs& a = p.a;
@@ -814,7 +830,7 @@ ChunkCarve chunk_carve(int n_seqs, int n_tokens, int Hq, int Hkv, int D) {
   ChunkCarve c;
   c.entries = (int)((long long)n_tokens * (Hq / Hkv) / 256) + n_seqs;
   auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
-  c.entry = 256;
+  c.entry = up(256 + PC_BLOCKS * sizeof(Place));
   c.ml = up(c.entry + (size_t)c.entries * sizeof(ChunkEntry));
   c.rec = c.ml + up((size_t)2 * PC_BLOCKS * 256 * sizeof(float2));
   c.total = c.rec + (size_t)2 * PC_BLOCKS * 256 * D * sizeof(float);
@@ -829,7 +845,9 @@ cudaError_t launch_chunk_t(const ChunkLaunch& p, const CUtensorMap& mk, const CU
   cudaError_t e = allow_smem(kernel, smem, done);
   if (e == cudaSuccess) e = launch_chained(chunk_plan_kernel, dim3(1), dim3(1024), 0, st, p);
   if (e == cudaSuccess) e = launch_chained(kernel, dim3(PC_BLOCKS), dim3(PC_THREADS), smem, st, p, mk, mv);
-  if (e == cudaSuccess) e = launch_chained(chunk_merge_kernel<D>, dim3(D / 4, PC_BLOCKS - 1), dim3(256), 0, st, p);
+  const unsigned rows = (unsigned)std::min(256LL, (long long)p.a.s.max_new * p.G);   // of an item, at most
+  if (e == cudaSuccess)
+    e = launch_chained(chunk_merge_kernel<D>, dim3((rows * (D / 4) + 255) / 256, PC_BLOCKS - 1), dim3(256), 0, st, p);
   return e;
 }
 
@@ -850,6 +868,7 @@ cudaError_t launch_paged_chunk(const PagedAttnArgs& a, void* ws, const CUtensorM
   char* w = static_cast<char*>(ws);
   p.max_entries = c.entries;
   p.head = reinterpret_cast<int*>(w);
+  p.cut = reinterpret_cast<Place*>(w + 256);
   p.entry = reinterpret_cast<ChunkEntry*>(w + c.entry);
   p.rec_ml = reinterpret_cast<float2*>(w + c.ml);
   p.rec = reinterpret_cast<float*>(w + c.rec);

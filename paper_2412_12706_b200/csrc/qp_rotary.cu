@@ -23,8 +23,8 @@ inline int pairing(const qp_rope& r) { return r.interleaved ? PAIR_NEXT : r.rot_
 // Cosine and sine, times m, of pair `turn` at position pos.  The upper half of the product is the fraction of a turn in units of 2^-32:
 // two bits of quadrant, and the rest as y in [-1/2, 1/2] quarter turns, cut to 24 bits.  sin(y pi/2) / y and cos(y pi/2) are
 // polynomials in y^2, degree 3 and 4, fitted here by linear programming on [0, 1/4] for the least largest error (5e-9 and 3e-10); in 32
-// bits both results are within 9e-8, the cut included within 2^-22.  (sincospif with the conversion to float
-// in its place is twice the instructions: 8192 tokens x 32 heads x 128 rotated in 26.4 us, against 25.4.)
+// bits both results are within 9e-8, the cut included within 2^-22.  (sincospif and a conversion to float in
+// its place, with the rows asked for after the table: 8192 tokens x 32 heads x 128 in 28.4 us, against 25.4.)
 __device__ __forceinline__ float2 cos_sin(uint64_t turn, int pos, float m) {
   const uint32_t frac = (uint32_t)((turn * (uint64_t)(int64_t)pos) >> 32) + 0x20000000u;
   const uint32_t quarter = frac >> 30;
@@ -353,7 +353,7 @@ append_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ qp_r
 
 cudaError_t launch_rotary(const RotaryArgs& a, const qp_rope& rope, cudaStream_t st) {
   const int units = units_a_thread((long long)a.Bt * a.L * a.H, a.D), tokens = tokens_a_block(a.H, a.D, units);
-  const dim3 grid((a.L + tokens - 1) / tokens, std::min(a.Bt, 65535));
+  const dim3 grid((unsigned)(((long long)a.L + tokens - 1) / tokens), std::min(a.Bt, 65535));
   auto launch = [&](auto kernel) { return launch_chained(kernel, grid, dim3(THREADS), 0, st, a, rope, tokens, inverse_of(a.H)); };
   switch (pairing(rope)) {
     case PAIR_NEXT: return units == 4 ? launch(rotary_kernel<PAIR_NEXT, 4>) : launch(rotary_kernel<PAIR_NEXT, 1>);
@@ -367,7 +367,7 @@ cudaError_t launch_paged_append(const AppendArgs& a, const qp_rope* rope_or_null
   if (rope_or_null) rope = *rope_or_null;
   const int rot_units = units_a_thread((long long)a.s.n_tokens * a.Hq, a.D), tokens = tokens_a_block(a.Hq, a.D, rot_units);
   const long long edge = 2LL * a.s.n_seqs * a.Hkv, whole = 2LL * (a.s.n_tokens / a.s.page) * a.Hkv;
-  const long long queries = a.q ? (a.s.n_tokens + tokens - 1) / tokens : 0;
+  const long long queries = a.q ? ((long long)a.s.n_tokens + tokens - 1) / tokens : 0;
   if (edge + whole + queries > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
   const dim3 grid((unsigned)(edge + whole + queries));
   auto launch = [&](auto kernel) {

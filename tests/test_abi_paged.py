@@ -111,7 +111,7 @@ def test_layout(lib):
     assert ctypes.sizeof(qp.qp_paged) == 8 * 4 + 3 * 8 + 6 * 8 and ctypes.sizeof(qp.qp_step) == 2 * 4 + 3 * 8
     assert ctypes.sizeof(qp.qp_rope) == 16 + 64 * 8
     for bad, code in ((dict(n_seqs=0), 1), (dict(Hq=7), 1), (dict(n_pages=0), 1), (dict(max_pages=0), 1), (dict(D=96), 2), (dict(Hq=32), 2),
-                      (dict(fmt=2), 2), (dict(fmt=-1), 2), (dict(page=16), 2), (dict(page=48), 2), (dict(n_seqs=qp.QP_MAX_SEQS + 1), 2),
+                      (dict(fmt=2), 2), (dict(fmt=-1), 2), (dict(page=16), 2), (dict(page=48), 2), (dict(n_seqs=qp.QP_MAX_SEQS + 1), 2), (dict(Hq=65544, Hkv=8193), 2),
                       (dict(n_pages=1 << 25), 2), (dict(max_pages=1 << 25), 2), (dict(Hq=1 << 26, Hkv=1 << 26), 2)):
         with pytest.raises(qp.QpError) as e:
             paged(**bad)

@@ -5,7 +5,8 @@ channel.  A logit is a sum of D products in 32 bits, off by (D + 8) 2^-23 sum|q 
 the small channels; int8 codes enter as c + 128, so there |k| is |k| + 128 scale.  A weight is off by e^(2 e) - 1 of the largest such e,
 by 2^-11 for its rounding to fp16 (and by as much in the sum it is divided by), by 2^-20 for the exponential, and by 2^-35 of the
 heaviest weight where it is too small for fp16.  The sums over n tokens are in 32 bits, (n / 16 + 64) 2^-23.  All of that counts against
-the weighted sum of |v| (int8: |v| + 128 scale); the output is rounded to bf16, 2^-8 of itself."""
+the weighted sum of |v| (int8: |v| + 128 scale); the output is rounded to bf16, 2^-8 of itself, or where it is subnormal half of the
+smallest bf16 number, 2^-134 (and the sums then to multiples of 2^-149, together less than as much again)."""
 import math
 
 import pytest
@@ -218,7 +219,7 @@ def ref_attn(q, c, table, lens, new):
             bounds.append(w)
         r0 += m
     out, w = torch.cat(outs), torch.cat(bounds)
-    return out, w + 2.0 ** -8 * out.abs()
+    return out, w + 2.0 ** -8 * out.abs() + 2.0 ** -133
 
 
 def check_attn(c, table, lens, new, seed=0, q_scale=1.0, q=None, pad=0):
@@ -263,6 +264,68 @@ def test_many_sequences():
     check_attn(c, table, lens, new)
 
 
+@pytest.mark.parametrize("Hq,Hkv,D,page,dtype,most", [
+    (8, 2, 64, 32, INT8, 1), (8, 1, 128, 64, INT8, 1), (6, 2, 64, 64, E4M3, 3), (32, 8, 128, 32, E4M3, 5), (8, 2, 128, 128, E4M3, 60), (6, 2, 64, 32, INT8, 90)])
+def test_many_sequences_of_every_form(Hq, Hkv, D, page, dtype, most):
+    lens = [(53 * b * b) % 900 for b in range(90)]
+    new = [(b * 7) % (most + 1) for b in range(90)]
+    c, table = make(90, Hq, Hkv, D, page, dtype, 900 + most)
+    fill(c, table, [a + b for a, b in zip(lens, new)], 3)
+    check_attn(c, table, lens, new, pad=5)
+
+
+@pytest.mark.parametrize("most", [1, 40])
+def test_all_the_rows_of_a_table(most):
+    seqs = qp.QP_MAX_SEQS
+    lens = [(29 * b) % 70 for b in range(seqs)]
+    new = [b % (most + 1) if b % 9 == 0 or b == seqs - 1 else 0 for b in range(seqs)]
+    c, table = make(seqs, 4, 2, 64, 32, E4M3, 70 + most)
+    fill(c, table, [a + b for a, b in zip(lens, new)], 3)
+    check_attn(c, table, lens, new)
+
+
+@pytest.mark.parametrize("new", [[1, 1], [30, 70]])
+def test_a_pool_beyond_32_bits(new):
+    """Codes of 5 GB: pages whose bytes stand beyond 2^32, appended and attended to."""
+    Hq, Hkv, D, page = 16, 8, 128, 128
+    lens = [700, 127]
+    c, table = make(2, Hq, Hkv, D, page, INT8, 896, spare=40000, seed=2)
+    c.k_codes.view(torch.uint8).fill_(1)
+    assert int(table.max()) * Hkv * page * D > 2 ** 32
+    total = [a + b for a, b in zip(lens, new)]
+    k, v = ([randn((n, Hkv, D), 10 * s + b) for b, n in enumerate(total)] for s in (1, 2))
+    for at, m in (([0, 0], lens), (lens, new)):
+        cut = lambda x: torch.cat([x[b][at[b]:at[b] + m[b]] for b in range(2)])
+        qp.paged_append(cut(k), cut(v), c, qp.PagedStep(start_of(m), ints(at), table, sum(m), max(m)))
+    check_cache(c, table, k, v, total, INT8)
+    check_attn(c, table, lens, new)
+
+
+def test_two_captured_calls_replayed_together():
+    """Without workspaces of the caller's: each graph keeps its own."""
+    jobs = []
+    for dtype, new, seed in ((E4M3, [1, 1], 1), (INT8, [20, 3], 2), (E4M3, [150, 1], 3)):
+        lens = [700, 64]
+        c, table = make(2, 8, 2, 128, 64, dtype, 900)
+        fill(c, table, [a + b for a, b in zip(lens, new)], seed)
+        q = randn((sum(new), 8, 128), seed)
+        step = qp.PagedStep(start_of(new), ints(lens), table, sum(new), max(new))
+        want = qp.paged_attn(q, c, step)
+        out = torch.zeros_like(want)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            qp.paged_attn(q, c, step, out=out)
+        jobs.append((graph, torch.cuda.Stream(), out, want, (q, c, step)))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for graph, stream, *_ in jobs:
+            with torch.cuda.stream(stream):
+                graph.replay()
+    torch.cuda.synchronize()
+    for _, _, out, want, _ in jobs:
+        assert torch.equal(out, want)
+
+
 @pytest.mark.parametrize("dtype", [E4M3, INT8])
 @pytest.mark.parametrize("ks,vs,qs", [(1e-6, 1e-6, 1e6), (1e6, 1e6, 1e-6), (1.0, 1e-20, 1.0), (30.0, 1e20, 30.0), (1.0, 1.0, 0.0)])
 @pytest.mark.parametrize("new", [[1, 1], [40, 9]])
@@ -271,6 +334,38 @@ def test_attention_at_any_magnitude(dtype, ks, vs, qs, new):
     c, table = make(2, 8, 2, 128, 64, dtype, 540)
     fill(c, table, [a + b for a, b in zip(lens, new)], 11, ks, vs)
     check_attn(c, table, lens, new, q_scale=qs)
+
+
+@pytest.mark.parametrize("dtype", [E4M3, INT8])
+@pytest.mark.parametrize("ks,vs,qs", [(1.0, 1e-37, 1.0), (1.0, 1e28, 1.0), (1e-28, 1.0, 1e28), (1e-38, 1e-38, 1.0)])
+@pytest.mark.parametrize("new", [[1, 1], [40, 9]])
+def test_attention_at_the_ends_of_the_range(dtype, ks, vs, qs, new):
+    lens = [500, 70]
+    c, table = make(2, 8, 2, 128, 64, dtype, 540)
+    fill(c, table, [a + b for a, b in zip(lens, new)], 11, ks, vs)
+    check_attn(c, table, lens, new, q_scale=qs)
+
+
+@pytest.mark.parametrize("dtype", [E4M3, INT8])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf"), 3e38])
+@pytest.mark.parametrize("new", [[3, 2], [20, 9], [70, 1]])
+def test_keys_that_earlier_rows_do_not_see(dtype, bad, new):
+    lens = [500, 70]
+    c, table = make(2, 8, 2, 128, 64, dtype, 600)
+    fill(c, table, [a + b for a, b in zip(lens, new)], 11)
+    q = randn((sum(new), 8, 128), 3)
+    step = qp.PagedStep(start_of(new), ints(lens), table, sum(new), max(new))
+    ref, bound = ref_attn(q, c, table, lens, new)
+    last = (lens[0] + new[0] - 1) % 64                             # of the first sequence; its key is seen by its own row only
+    c.k_tail[0, :, last, 7] = bad
+    got = qp.paged_attn(q, c, step)
+    if math.isfinite(bad):                                         # the bound counts the largest waiting key
+        ref, bound = ref_attn(q, c, table, lens, new)
+    rows = [r for r in range(sum(new)) if r != new[0] - 1]
+    err = (got.double() - ref).abs() - bound
+    assert float(err[rows].max()) <= 0 and not torch.isnan(got[rows]).any()
+    if math.isnan(bad):
+        assert torch.isnan(got[new[0] - 1]).all()
 
 
 def test_peaked_rows_and_pages_of_zeros():
