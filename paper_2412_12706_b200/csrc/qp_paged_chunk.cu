@@ -23,6 +23,12 @@
 //   softmax (8)   two groups u, a row a thread, which also fetch the queries and write the output
 // u is a tile of 128 rows when there are two, else the parity of the token tile, so that one group's exponentials always run beside
 // the other's products.  Every wait is bounded; a block that gives up leaves NaN.
+//
+// Measured: the last 1999 of 16300 tokens, 64 query and 8 KV heads (1.0 TFLOP) 1.10 ms, 0.91 PFLOP/s.  The bound is the chain of a
+// tile's softmax (read S, maximum, 256 x 128 exponentials, weights back to tensor memory) with the two hand-overs around it: without
+// the products it takes nearly as long (0.97 ms), the exponentials alone would be half of it, expansion and copies wait for free slots,
+// and the GPU is at its power limit.  Few rows leave most of a row tile empty: 16 sequences of 3000 to 4100 tokens with 20 rows per KV
+// head are 67 us here, 49 in the form for few rows, with 64 rows 71 us here.
 #include <algorithm>
 
 #include "qp_mma.cuh"

@@ -101,7 +101,8 @@ __device__ __forceinline__ void rotate_unit(uint4& a, uint4& b, int u, int rot, 
 }
 
 // ---- rotation alone, and of a step's queries.  HBM-bound: 4 bytes a number.  A block takes up to 32 tokens of all heads, so that
-// the cosines and sines are computed once a token and read from shared memory by every head.
+// the cosines and sines are computed once a token and read from shared memory by every head.  8192 tokens x 32 heads x 128: 25.3 us,
+// 5.3 TB/s.
 // The rows are asked for before the table is made (fill, which ends with the block's barrier), so that the two wait together.
 // n < 2^16 / H tokens; inv_h = ceil(2^32 / H), or 0 for one head.  pitch: pairs of a token in the table.
 template <int MODE, int ROT_UNITS, typename OK, typename FILL>
@@ -220,6 +221,7 @@ __device__ __forceinline__ uint32_t abs_max2(uint32_t m, const uint4& v) {
 // between the search for the largest magnitude and the rounding to codes: page * D / 16 / 128 = UNITS units of 16 channels a thread.
 // At most 64 registers up to 4 units, so that eight blocks are on an SM (64 one-token sequences 5.2 -> 3.9 us, 8192 tokens with 32
 // query heads 41.3 -> 39.7 us).
+// 8192 tokens with 32 query and 8 KV heads are 39.6 us (185 MB, 4.7 TB/s), one token 2.3 us, mostly launch.
 // The host does not know the sequences' lengths, so it launches a whole-page block for every `page` rows of the step: unit u belongs
 // to the last sequence b with start[b] / page <= u, which has at least as many of them as pages begin and end in its new tokens.
 template <int UNITS, int MODE, int ROT_UNITS>
