@@ -749,29 +749,31 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
             if (lane == 0) mbar_arrive(bar(CB_RAW_EMPTY, team * PC_RAW + stage));
           }
           if (!ok) break;
-          // waiting rows, a box a warp, a row a lane: bf16 to fp16 times a power of two; zeros behind the last
+          // waiting rows, a box a warp, read once: bf16 to fp16 times a power of two; zeros behind the last
           for (int box = boxes + tw; box < 4; box += PC_TEAM) {
-            const int t = t0 + 32 * box + lane;
-            const size_t row = (((size_t)c.at.b * a.Hkv + c.at.h) * s.page + t - whole) * (D / 8);
-            auto scale_of = [&](const uint16_t* tail) {
+            constexpr int CH = D / 8, STEP = 32 / CH;           // 16-byte chunks of a row; rows at a time
+            const int r0 = lane / CH, ch = lane % CH, left = end - (t0 + 32 * box);
+            const size_t from_row = (((size_t)c.at.b * a.Hkv + c.at.h) * s.page + t0 + 32 * box - whole) * CH + lane;
+            uint4 v[CH];
+            auto fetch = [&](const uint16_t* tail) {
+#pragma unroll
+              for (int q = 0; q < CH; ++q)
+                v[q] = r0 + q * STEP < left ? reinterpret_cast<const uint4*>(tail)[from_row + 32 * q] : make_uint4(0u, 0u, 0u, 0u);
               uint32_t m = 0u;
-              if (t < end)
-#pragma unroll 4
-                for (int q = 0; q < D / 8; ++q) m = abs_max(m, finite(reinterpret_cast<const uint4*>(tail)[row + q]));
+#pragma unroll
+              for (int q = 0; q < CH; ++q) m = abs_max(m, finite(v[q]));
               m = __reduce_max_sync(0xffffffffu, max(m & 0xffffu, m >> 16));
               return m ? to_one(m) : make_float2(1.f, 0.f);
             };
-            const float2 f = scale_of(tails);
-#pragma unroll 4
-            for (int q = 0; q < D / 8; ++q) {
-              const uint4 v = t < end ? reinterpret_cast<const uint4*>(tails)[row + q] : make_uint4(0u, 0u, 0u, 0u);
-              const uint2 lo = four_ops<FORMAT>(v.x, v.y, f.x), hi = four_ops<FORMAT>(v.z, v.w, f.x);
-              sts128(slot + op_off(32 * box + lane, q), make_uint4(lo.x, lo.y, hi.x, hi.y));
+            float2 fv = make_float2(0.f, 0.f);
+            if (team == 0) fv = fetch(a.v_tail);
+            const float2 f = fetch(tails);
+#pragma unroll
+            for (int q = 0; q < CH; ++q) {
+              const uint2 lo = four_ops<FORMAT>(v[q].x, v[q].y, f.x), hi = four_ops<FORMAT>(v[q].z, v[q].w, f.x);
+              sts128(slot + op_off(32 * box + r0 + q * STEP, ch), make_uint4(lo.x, lo.y, hi.x, hi.y));
             }
-            if (team == 0) {
-              const float2 fv = scale_of(a.v_tail);
-              if (lane == 0) set_scales(tile, box, f.y, fv.y);
-            }
+            if (team == 0 && lane == 0) set_scales(tile, box, f.y, fv.y);
           }
           asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
           __syncwarp();
