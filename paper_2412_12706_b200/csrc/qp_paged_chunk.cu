@@ -314,24 +314,36 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
       const bool has = r < c.rows;
       const bool work = (c.two ? u * 128 : 0) + (warp & 3) * 32 < c.rows;            // warp-uniform
       const int gr = c.at.rg * 256 + r, tok = gr / p.G, head = c.at.h * p.G + gr - tok * p.G;
-      // the row, in fp16 times the power of two that brings its largest magnitude near 1
+      // The row, in fp16 times the power of two that brings its largest magnitude near 1.  A warp's 32 rows come (and leave, below)
+      // whole through their place in the queries' tile: a row a lane would touch 32 lines with every access, 7000 clocks to fetch the
+      // 256 rows of an item and 10000 to write them.
+      constexpr int CH = D / 8, STEP = 32 / CH;                 // 16-byte chunks of a row of 16-bit numbers; rows at a time
+      const int wr = (warp & 3) * 32 + lane / CH, ch = lane % CH;
+      const uint32_t place = sQ + u * SLOT;
       float cq = 0.f;
       {
-        const uint4* src = reinterpret_cast<const uint4*>(a.q + (c.q.row0 + tok) * a.qs + (size_t)head * D);
+        const long long from = has ? (c.q.row0 + tok) * a.qs + (long long)head * D : -1;
         uint32_t m = 0u;
-        uint4 v[D / 8];
+        uint4 v[CH];
 #pragma unroll
-        for (int k = 0; k < D / 8; ++k) v[k] = has ? __ldg(src + k) : make_uint4(0u, 0u, 0u, 0u);
+        for (int k = 0; k < CH; ++k) {
+          const long long o = __shfl_sync(0xffffffffu, from, k * STEP + lane / CH);
+          v[k] = o >= 0 ? __ldg(reinterpret_cast<const uint4*>(a.q + o) + ch) : make_uint4(0u, 0u, 0u, 0u);
+        }
 #pragma unroll
-        for (int k = 0; k < D / 8; ++k) m = abs_max(m, v[k]);
+        for (int k = 0; k < CH; ++k) sts128(place + op_off(wr + k * STEP, ch), v[k]);
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < CH; ++k) v[k] = lds128(place + op_off(rl, k));
+#pragma unroll
+        for (int k = 0; k < CH; ++k) m = abs_max(m, v[k]);
         const float2 f = to_one(m);
         cq = f.y * scale_log2;
         if (c.two || u == 0) {
-          const uint32_t dst = sQ + (c.two ? u : 0) * SLOT;
 #pragma unroll
-          for (int k = 0; k < D / 8; ++k) {
+          for (int k = 0; k < CH; ++k) {
             const uint2 lo = four_ops<FORMAT>(v[k].x, v[k].y, f.x), hi = four_ops<FORMAT>(v[k].z, v[k].w, f.x);
-            sts128(dst + op_off(rl, k), make_uint4(lo.x, lo.y, hi.x, hi.y));
+            sts128(place + op_off(rl, k), make_uint4(lo.x, lo.y, hi.x, hi.y));
           }
         }
         asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
@@ -364,14 +376,18 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
           }
           if (128 * (j + 1) > least) {                          // what the row does not see leaves S
 #pragma unroll 1
-            for (int c0 = 0; c0 < 128; c0 += 16) {
-              uint32_t v[16];
-              tmem_ld16_issue(ts + c0, v);
-              tmem_wait16(v);
+            for (int c0 = 0; c0 < 128; c0 += 32) {
+              uint32_t v[32], lo[16], hi[16];
+              tmem_ld32_issue(ts + c0, v);
+              tmem_wait(v);
 #pragma unroll
-              for (int i = 0; i < 16; ++i) v[i] = 128 * j + c0 + i < lim ? v[i] : 0xff800000u;
+              for (int i = 0; i < 16; ++i) {
+                lo[i] = 128 * j + c0 + i < lim ? v[i] : 0xff800000u;
+                hi[i] = 128 * j + c0 + 16 + i < lim ? v[16 + i] : 0xff800000u;
+              }
               __syncwarp();
-              tmem_st(ts + c0, v);
+              tmem_st(ts + c0, lo);
+              tmem_st(ts + c0 + 16, hi);
             }
             tmem_wait_st();
           }
@@ -485,21 +501,51 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
         }
       };
       if (c.two) {
-        const float inv = __fdiv_rn(1.f, l_run);
         if (work) {
-#pragma unroll 1
-          for (int c0 = 0; c0 < D; c0 += 16) {
-            uint32_t o[16];
-            tmem_ld16_issue(tO(u) + lanes + c0, o);
-            tmem_wait16(o);
-            const float f = any && m_run != -INFINITY ? s0 : 0.f;
+          const float f = any && m_run != -INFINITY ? s0 : 0.f, inv = __fdiv_rn(1.f, l_run);
+          const int t = gr / p.G;
+          const long long to = whole ? ((long long)(c.q.row0 + t) * a.Hq + c.at.h * p.G + gr - t * p.G) * D : 0;
+          auto channels = [&](int c0, float (&o)[16]) {
+            uint32_t v[16];
+            tmem_ld16_issue(tO(u) + lanes + c0, v);
+            tmem_wait16(v);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (has)
-                put(r, c0 + 4 * i, f == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f)
-                                            : make_float4(__uint_as_float(o[4 * i]) * f, __uint_as_float(o[4 * i + 1]) * f,
-                                                          __uint_as_float(o[4 * i + 2]) * f, __uint_as_float(o[4 * i + 3]) * f), m_own, l_run, inv);
+            for (int i = 0; i < 16; ++i)                        // (int8: columns 0, 1, 2, 3 are channels 0, 2, 1, 3)
+              o[i] = f == 0.f ? 0.f : __uint_as_float(v[FORMAT == QP_INT8 && ((i + 1) & 2) ? i ^ 3 : i]) * f;
+          };
+          // half: fp32 records take a row's place twice
+          for (int half = 0; half < (whole ? 1 : 2); ++half) {
+#pragma unroll 1
+            for (int c0 = 0; c0 < (whole ? D : D / 2); c0 += 16) {
+              float o[16];
+              channels(half * (D / 2) + c0, o);
+              if (whole) {
+#pragma unroll
+                for (int i = 0; i < 16; i += 8)
+                  sts128(place + op_off(rl, (c0 + i) / 8), make_uint4(pack_bf16x2(o[i] * inv, o[i + 1] * inv), pack_bf16x2(o[i + 2] * inv, o[i + 3] * inv),
+                                                                     pack_bf16x2(o[i + 4] * inv, o[i + 5] * inv), pack_bf16x2(o[i + 6] * inv, o[i + 7] * inv)));
+              } else {
+#pragma unroll
+                for (int i = 0; i < 16; i += 4)
+                  sts128(place + op_off(rl, (c0 + i) / 4),
+                         make_uint4(__float_as_uint(o[i]), __float_as_uint(o[i + 1]), __float_as_uint(o[i + 2]), __float_as_uint(o[i + 3])));
+              }
+            }
+            __syncwarp();
+#pragma unroll 4
+            for (int k = 0; k < CH; ++k) {
+              const uint4 v = lds128(place + op_off(wr + k * STEP, ch));
+              const long long o = __shfl_sync(0xffffffffu, to, k * STEP + lane / CH);
+              const int row = u * 128 + wr + k * STEP;
+              if (row >= c.rows) continue;
+              if (whole)
+                *(reinterpret_cast<uint4*>(a.out + o) + ch) = v;
+              else
+                *reinterpret_cast<uint4*>(p.rec + ((size_t)rec * 256 + row) * D + half * (D / 2) + 4 * ch) = v;
+            }
+            __syncwarp();
           }
+          if (!whole && has) p.rec_ml[(size_t)rec * 256 + r] = make_float2(m_own, l_run);
         }
       } else {
         // the two groups' parts of a row come together through shared memory: statistics in the queries' place, a
