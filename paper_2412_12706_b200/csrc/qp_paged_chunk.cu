@@ -42,9 +42,10 @@ namespace {
 constexpr int PC_SOFT = 8, PC_TEAM = 3;                         // softmax warps; warps that expand the keys, and the values
 constexpr int PC_MMA = PC_SOFT + 2 * PC_TEAM, PC_COPY = PC_MMA + 1;   // the warp that issues the products, the one that copies
 constexpr int PC_THREADS = (PC_COPY + 1) * 32;
-constexpr int PC_SLOTS = 4, PC_RAW = 4;                         // operand slots, keys and values in turn; raw stages of a team (32 tokens each)
+constexpr int PC_SLOTS = 4;                                     // operand slots, keys and values in turn
+__host__ __device__ constexpr int raw_stages(int D) { return D == 64 ? 12 : 4; }    // of a team, 32 tokens each: what shared memory has room for
 constexpr int PC_BLOCKS = 148;                                  // of a B200, one a SM; the layout of the workspace goes by it
-constexpr int PC_SCALES = 8;                                    // tiles whose scales are kept: more than copies can be ahead of the softmax
+constexpr int PC_SCALES = 8;                                    // tiles whose scales are kept: more than the expansion can be ahead of the softmax
 constexpr float PC_HEAD = 11.f, PC_SLACK = 4.f;                 // see PA_HEAD, PA_SLACK
 
 struct ChunkEntry {                                             // 256 rows of a sequence
@@ -195,10 +196,7 @@ __device__ __forceinline__ float2 to_one(uint32_t m) {
 }
 __device__ __forceinline__ void bar_sync(int id, int n) { asm volatile("bar.sync %0, %1;\n" ::"r"(id), "r"(n) : "memory"); }
 
-enum : int {
-  CB_FULL = 0, CB_EMPTY = PC_SLOTS, CB_S = 2 * PC_SLOTS, CB_P = CB_S + 2, CB_Q = CB_P + 2, CB_RAW = CB_Q + 1, CB_RAW_EMPTY = CB_RAW + 2 * PC_RAW,
-  CB_COUNT = CB_RAW_EMPTY + 2 * PC_RAW
-};
+enum : int { CB_FULL = 0, CB_EMPTY = PC_SLOTS, CB_S = 2 * PC_SLOTS, CB_P = CB_S + 2, CB_Q = CB_P + 2, CB_RAW = CB_Q + 1 };
 
 struct Slot {                                                   // a team's place in the ring of slots, with the parity of the round
   int i;
@@ -213,12 +211,14 @@ template <int FORMAT, int D>
 __global__ void __launch_bounds__(PC_THREADS, 1)
 chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
   constexpr uint32_t SLOT = 128 * D * 2, RAW = 32 * D;
+  constexpr int PC_RAW = raw_stages(D), CB_RAW_EMPTY = CB_RAW + 2 * PC_RAW, CB_COUNT = CB_RAW_EMPTY + 2 * PC_RAW;
   constexpr uint32_t ID_S = (1u << 4) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
   constexpr uint32_t ID_O = (1u << 4) | (1u << 16) | (((uint32_t)D >> 3) << 17) | ((128u >> 4) << 24);        // B: rows contract
   extern __shared__ unsigned char smem_raw[];
   __shared__ uint64_t bars[CB_COUNT];
   __shared__ float s_fk[PC_SCALES][4];                          // per 32 tokens: what S is multiplied by
   __shared__ float4 s_fv[PC_SCALES][2];                         // log2 of the values' scale, 2^-6 / scale, for two times 32 tokens
+  __shared__ float3 s_raw[PC_RAW];                              // the same of the raw stages
   __shared__ uint32_t tmem_base_slot;
   __shared__ int give_up;
   const PagedAttnArgs& a = p.a;
@@ -289,14 +289,18 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
   // tokens of a piece's sequence that are in whole pages
   auto whole_tokens = [&](const Piece& c) { return (c.q.len + c.q.n) / s.page * s.page; };
   // Of a 32-token box: what the product with its keys is multiplied by; of its values the log2 of that, and its inverse, times 2^-6 so
-  // that the smallest bf16 number has one.  Written with the keys: the softmax of a tile begins when they are there, whatever has
-  // become of the values.
-  auto set_scales = [&](int tile, int box, float fk, float fv) {
-    s_fk[tile & (PC_SCALES - 1)][box] = fk;
+  // that the smallest bf16 number has one.
+  auto scales_of = [&](float fk, float fv) {
     fv = fv == 0.f ? 0x1p-60f : fv;                             // zeros: any scale that leaves the others theirs
+    return make_float3(fk, log2f(fv), __fdiv_rn(0x1p-6f, fv));
+  };
+  // Written with the keys' operands: the softmax of a tile begins when they are there, whatever has become of the values, and the copies
+  // may be any number of tiles further.
+  auto set_scales = [&](int tile, int box, float3 f) {
+    s_fk[tile & (PC_SCALES - 1)][box] = f.x;
     float* d = reinterpret_cast<float*>(&s_fv[tile & (PC_SCALES - 1)][box >> 1]) + 2 * (box & 1);
-    d[0] = log2f(fv);
-    d[1] = __fdiv_rn(0x1p-6f, fv);
+    d[0] = f.y;
+    d[1] = f.z;
   };
 
   if (warp < PC_SOFT) {
@@ -307,9 +311,10 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
     uint32_t phase = 0;                                         // of CB_S[u]
     bool ok = true;
     int tiles_done = 0;                                         // of the run, for the scales' ring
-    Piece c;
+    Piece c, after;
+    if (x0 < x1) after = piece_at(x0);
     for (int x = x0; x < x1;) {                                 // (one that gave up goes on, without waits: the groups have barriers)
-      c = x == x0 ? piece_at(x) : piece_at(x, &c);
+      c = after;
       const int r = (c.two ? u * 128 : 0) + rl;                 // row of the item
       const bool has = r < c.rows;
       const bool work = (c.two ? u * 128 : 0) + (warp & 3) * 32 < c.rows;            // warp-uniform
@@ -470,6 +475,7 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
         if (lane == 0) mbar_arrive(bar(CB_P, u));
       }
       l_run *= 64.f;
+      if (x + c.n < x1) after = piece_at(x + c.n, &c);          // (its numbers are on their way meanwhile)
       // O is complete with one more commit
       ok = ok && mbar_wait_warp(bar(CB_S, u), phase, gu);
       phase ^= 1u;
@@ -726,9 +732,10 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
           const float ks = __shfl_sync(0xffffffffu, w_ks, src), vs = __shfl_sync(0xffffffffu, w_vs, src);
           const int n = n_box + box, st = team * PC_RAW + n % PC_RAW, row = (id * a.Hkv + c.at.h) * s.page + (bx & ((1 << lg) - 1)) * 32;
           bool todo = lane < 8 && box < boxes;
-          if (todo && team == 0) set_scales(tile, box, ks, vs);
+          const float3 scales = scales_of(ks, vs);
           for (uint32_t y = 0; __any_sync(0xffffffffu, todo); ++y) {
             if (todo && (n < PC_RAW || mbar_try_wait(bar(CB_RAW_EMPTY, st), (uint32_t)(n / PC_RAW + 1) & 1u))) {
+              if (team == 0) s_raw[st] = scales;
               mbar_expect_tx(bar(CB_RAW, st), RAW);
               tma_load_2d(raw_base + st * RAW, team ? &map_v : &map_k, 0, row, bar(CB_RAW, st));
               todo = false;
@@ -775,6 +782,7 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
             const int stage = n_box % PC_RAW, first = (tw + n_box) % PC_TEAM;      // (the shares differ: in turn)
             ok = mbar_wait_warp(bar(CB_RAW, team * PC_RAW + stage), (uint32_t)(n_box / PC_RAW) & 1u, gu);
             if (!ok) break;
+            if (team == 0 && first == 0 && lane == 0) set_scales(tile, box, s_raw[stage]);
             uint4 w[MOST];
 #pragma unroll
             for (int q = 0; q < MOST; ++q) {
@@ -800,26 +808,43 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
             constexpr int CH = D / 8, STEP = 32 / CH;           // 16-byte chunks of a row; rows at a time
             const int r0 = lane / CH, ch = lane % CH, left = end - (t0 + 32 * box);
             const size_t from_row = (((size_t)c.at.b * a.Hkv + c.at.h) * s.page + t0 + 32 * box - whole) * CH + lane;
-            uint4 v[CH];
+            auto at = [&](int q) { return slot + op_off(32 * box + r0 + q * STEP, ch); };
+            // the box to its place as it is, and the power of two for it
             auto fetch = [&](const uint16_t* tail) {
+              uint4 v[CH];
 #pragma unroll
               for (int q = 0; q < CH; ++q)
                 v[q] = r0 + q * STEP < left ? reinterpret_cast<const uint4*>(tail)[from_row + 32 * q] : make_uint4(0u, 0u, 0u, 0u);
-              uint32_t m = 0u;
 #pragma unroll
-              for (int q = 0; q < CH; ++q) m = abs_max(m, finite(v[q]));
+              for (int q = 0; q < CH; ++q) sts128(at(q), v[q]);
+              uint32_t m = 0u;
+#pragma unroll 4
+              for (int q = 0; q < CH; ++q) m = abs_max(m, lds128(at(q)));
               m = __reduce_max_sync(0xffffffffu, max(m & 0xffffu, m >> 16));
+              if (m >= 0x7f80u) {                               // of what is finite
+                m = 0u;
+#pragma unroll 1
+                for (int q = 0; q < CH; ++q) m = abs_max(m, finite(lds128(at(q))));
+                m = __reduce_max_sync(0xffffffffu, max(m & 0xffffu, m >> 16));
+              }
               return m ? to_one(m) : make_float2(1.f, 0.f);
             };
+            if (left <= 0) {                                    // (hidden keys, and values of weight 0)
+#pragma unroll
+              for (int q = 0; q < CH; ++q) sts128(at(q), make_uint4(0u, 0u, 0u, 0u));
+              if (team == 0 && lane == 0) set_scales(tile, box, scales_of(0.f, 0.f));
+              continue;
+            }
             float2 fv = make_float2(0.f, 0.f);
             if (team == 0) fv = fetch(a.v_tail);
             const float2 f = fetch(tails);
-#pragma unroll
+#pragma unroll 2
             for (int q = 0; q < CH; ++q) {
-              const uint2 lo = four_ops<FORMAT>(v[q].x, v[q].y, f.x), hi = four_ops<FORMAT>(v[q].z, v[q].w, f.x);
-              sts128(slot + op_off(32 * box + r0 + q * STEP, ch), make_uint4(lo.x, lo.y, hi.x, hi.y));
+              const uint4 v = lds128(at(q));
+              const uint2 lo = four_ops<FORMAT>(v.x, v.y, f.x), hi = four_ops<FORMAT>(v.z, v.w, f.x);
+              sts128(at(q), make_uint4(lo.x, lo.y, hi.x, hi.y));
             }
-            if (team == 0 && lane == 0) set_scales(tile, box, f.y, fv.y);
+            if (team == 0 && lane == 0) set_scales(tile, box, scales_of(f.y, fv.y));
           }
           asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
           __syncwarp();
@@ -894,7 +919,7 @@ ChunkCarve chunk_carve(int n_seqs, int n_tokens, int Hq, int Hkv, int D) {
 template <int FORMAT, int D>
 cudaError_t launch_chunk_t(const ChunkLaunch& p, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t st) {
   static unsigned char done[64];
-  constexpr size_t smem = (2 + PC_SLOTS) * 128 * D * 2 + 2 * PC_RAW * 32 * D + 1024;
+  constexpr size_t smem = (2 + PC_SLOTS) * 128 * D * 2 + 2 * raw_stages(D) * 32 * D + 1024;
   auto kernel = chunk_kernel<FORMAT, D>;
   cudaError_t e = allow_smem(kernel, smem, done);
   if (e == cudaSuccess) e = launch_chained(chunk_plan_kernel, dim3(1), dim3(1024), 0, st, p);

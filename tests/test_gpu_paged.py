@@ -6,7 +6,11 @@ the small channels; int8 codes enter as c + 128, so there |k| is |k| + 128 scale
 by 2^-11 for its rounding to fp16 (and by as much in the sum it is divided by), by 2^-20 for the exponential, and by 2^-35 of the
 heaviest weight where it is too small for fp16.  The sums over n tokens are in 32 bits, (n / 16 + 64) 2^-23.  All of that counts against
 the weighted sum of |v| (int8: |v| + 128 scale); the output is rounded to bf16, 2^-8 of itself, or where it is subnormal half of the
-smallest bf16 number, 2^-134 (and the sums then to multiples of 2^-149, together less than as much again)."""
+smallest bf16 number, 2^-134 (and the sums then to multiples of 2^-149, together less than as much again).
+
+Waiting values, like queries, are fp16 times the power of two that brings the largest of their block of 32 into [1, 2): a bf16 number has
+8 bits, so it is exact from 2^-17 on, and below that rounded to a multiple of 2^-24, so off by at most 2^-25 of the largest; weights sum
+to 1, so the output is off by as much."""
 import math
 
 import pytest
@@ -219,7 +223,8 @@ def ref_attn(q, c, table, lens, new):
             bounds.append(w)
         r0 += m
     out, w = torch.cat(outs), torch.cat(bounds)
-    return out, w + 2.0 ** -8 * out.abs() + 2.0 ** -133
+    waiting = max(float(c.v_tail[b, :, :(n0 + m) % page].abs().nan_to_num(posinf=0).max()) if (n0 + m) % page else 0 for b, (n0, m) in enumerate(zip(lens, new)))
+    return out, w + 2.0 ** -8 * out.abs() + 2.0 ** -133 + 2.0 ** -25 * waiting
 
 
 def check_attn(c, table, lens, new, seed=0, q_scale=1.0, q=None, pad=0):
@@ -272,6 +277,16 @@ def test_many_sequences_of_every_form(Hq, Hkv, D, page, dtype, most):
     c, table = make(90, Hq, Hkv, D, page, dtype, 900 + most)
     fill(c, table, [a + b for a, b in zip(lens, new)], 3)
     check_attn(c, table, lens, new, pad=5)
+
+
+@pytest.mark.parametrize("dtype,D", [(E4M3, 64), (INT8, 128)])
+def test_short_prompts_between_longer_ones(dtype, D):
+    """Runs of sequences that have no whole page yet, which the copies of pages have nothing to wait for in."""
+    lens = [90 if b % 11 == 10 else 0 for b in range(1500)]
+    new = [10 + b % 13 for b in range(1500)]
+    c, table = make(1500, 8, 2, D, 32, dtype, 128)
+    fill(c, table, [a + b for a, b in zip(lens, new)], 3)
+    check_attn(c, table, lens, new)
 
 
 @pytest.mark.parametrize("most", [1, 40])
