@@ -24,11 +24,12 @@
 // u is a tile of 128 rows when there are two, else the parity of the token tile, so that one group's exponentials always run beside
 // the other's products.  Every wait is bounded; a block that gives up leaves NaN.
 //
-// Measured: the last 1999 of 16300 tokens, 64 query and 8 KV heads (1.0 TFLOP) 1.10 ms, 0.91 PFLOP/s.  The bound is the chain of a
+// Measured: the last 1999 of 16300 tokens, 64 query and 8 KV heads (1.0 TFLOP) 1.07 ms, 0.94 PFLOP/s.  The bound is the chain of a
 // tile's softmax (read S, maximum, 256 x 128 exponentials, weights back to tensor memory) with the two hand-overs around it: without
-// the products it takes nearly as long (0.97 ms), the exponentials alone would be half of it, expansion and copies wait for free slots,
-// and the GPU is at its power limit.  Few rows leave most of a row tile empty: 16 sequences of 3000 to 4100 tokens with 20 rows per KV
-// head are 67 us here, 49 in the form for few rows, with 64 rows 71 us here.
+// the products it took nearly as long (0.97 of 1.12 ms), the exponentials alone would be half of it, expansion and copies wait for
+// free slots, and the GPU is at its power limit.  Few rows leave most of a row tile empty: 16 sequences of 3000 to 4100 tokens with 20
+// rows per KV head are 67 us here, 49 in the form for few rows, with 64 rows 69 us here.  Short items are bound by the chain queries,
+// product, softmax, output of each: 64 chunks of 97 tokens 92 us, 11 us of it an item's fixed cost.
 #include <algorithm>
 
 #include "qp_mma.cuh"
@@ -398,7 +399,7 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
           }
           // Loops of small bodies: the groups, the expanding warps and the others share each quarter of the SM's instruction cache, and
           // straight code of a whole row's columns is waited for (the weights kept in registers over one unrolled pass: 1390 us for
-          // 1999 tokens of 64 heads at 14301, against 1119).
+          // 1999 tokens of 64 heads at 14301, against 1119 then).
           float mx = -INFINITY;
 #pragma unroll 1
           for (int h2 = 0; h2 < 2; ++h2) {
