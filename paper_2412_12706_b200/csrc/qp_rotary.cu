@@ -100,6 +100,10 @@ __device__ __forceinline__ void rotate_unit(uint4& a, uint4& b, int u, int rot, 
   b = make_uint4(w[4], w[5], w[6], w[7]);
 }
 
+// Where pair p stands in its token's part of the table: the first two pairs of every unit, then the next two of every unit, ..., so that
+// the lanes of a row read 16 bytes each, one behind the other (in order, four of them would meet in the same banks)
+__device__ __forceinline__ int table_place(int p, int pitch) { return ((p & 6) >> 1) * (pitch >> 2) + (p >> 3) * 2 + (p & 1); }
+
 // ---- rotation alone, and of a step's queries.  HBM-bound: 4 bytes a number.  A block takes up to 32 tokens of all heads, so that
 // the cosines and sines are computed once a token and read from shared memory by every head.  8192 tokens x 32 heads x 128: 25.3 us,
 // 5.3 TB/s.
@@ -132,7 +136,7 @@ __device__ __forceinline__ void rotate_tokens(const uint16_t* x, long long xh, l
 #pragma unroll
     for (int k = 0; k < ROT_UNITS; ++k)
       if (base + k * THREADS + (int)threadIdx.x < units)
-        rotate_unit<MODE>(a[k], b[k], u, rot, src[k], [&](int p) { return *reinterpret_cast<const float4*>(table + tok[k] * pitch + p); });
+        rotate_unit<MODE>(a[k], b[k], u, rot, src[k], [&](int p) { return *reinterpret_cast<const float4*>(table + tok[k] * pitch + table_place(p, pitch)); });
     if (MODE == PAIR_ODD) __syncwarp();                         // in place: a row's units are one warp's, all read before one writes
 #pragma unroll
     for (int k = 0; k < ROT_UNITS; ++k)
@@ -163,7 +167,7 @@ rotary_kernel(const __grid_constant__ RotaryArgs a, const __grid_constant__ qp_r
         if (p >= half) continue;
         float2 cs = cos_sin(rope.turn[p], __ldg(a.pos + b * a.ps + t0 + t), rope.factor);
         if (a.transpose) cs.y = -cs.y;
-        table[i] = cs;
+        table[t * pitch + table_place(p, pitch)] = cs;
       }
       __syncthreads();
     };
@@ -256,7 +260,7 @@ append_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ qp_r
     auto fill = [&]() {
       for (int i = tid; i < n * pitch; i += THREADS) {
         const int t = i / pitch, p = i - t * pitch;
-        if (p < half) table[i] = cos_sin(turn[p], s_pos[t], rope.factor);
+        if (p < half) table[t * pitch + table_place(p, pitch)] = cos_sin(turn[p], s_pos[t], rope.factor);
       }
       __syncthreads();
     };
