@@ -24,7 +24,7 @@ inline int pairing(const qp_rope& r) { return r.interleaved ? PAIR_NEXT : r.rot_
 // two bits of quadrant, and the rest as y in [-1/2, 1/2] quarter turns, cut to 24 bits.  sin(y pi/2) / y and cos(y pi/2) are
 // polynomials in y^2, degree 3 and 4, fitted here by linear programming on [0, 1/4] for the least largest error (5e-9 and 3e-10); in 32
 // bits both results are within 9e-8, the cut included within 2^-22.  (sincospif and a conversion to float in
-// its place, with the rows asked for after the table: 8192 tokens x 32 heads x 128 in 28.4 us, against 25.4.)
+// its place, with the rows asked for after the table: 8192 tokens x 32 heads x 128 in 28.4 us, against 25.4 then.)
 __device__ __forceinline__ float2 cos_sin(uint64_t turn, int pos, float m) {
   const uint32_t frac = (uint32_t)((turn * (uint64_t)(int64_t)pos) >> 32) + 0x20000000u;
   const uint32_t quarter = frac >> 30;
@@ -101,12 +101,13 @@ __device__ __forceinline__ void rotate_unit(uint4& a, uint4& b, int u, int rot, 
 }
 
 // Where pair p stands in its token's part of the table: the first two pairs of every unit, then the next two of every unit, ..., so that
-// the lanes of a row read 16 bytes each, one behind the other (in order, four of them would meet in the same banks)
+// the lanes of a row read 16 bytes each, one behind the other (in order, four of them meet in the same banks: 8192 tokens x 32 heads x 128
+// 25.3 us, against 19.4)
 __device__ __forceinline__ int table_place(int p, int pitch) { return ((p & 6) >> 1) * (pitch >> 2) + (p >> 3) * 2 + (p & 1); }
 
 // ---- rotation alone, and of a step's queries.  HBM-bound: 4 bytes a number.  A block takes up to 32 tokens of all heads, so that
-// the cosines and sines are computed once a token and read from shared memory by every head.  8192 tokens x 32 heads x 128: 25.3 us,
-// 5.3 TB/s.
+// the cosines and sines are computed once a token and read from shared memory by every head.  8192 tokens x 32 heads x 128: 19.4 us,
+// 6.9 TB/s (what is written last stays in L2).
 // The rows are asked for before the table is made (fill, which ends with the block's barrier), so that the two wait together.
 // n < 2^16 / H tokens; inv_h = ceil(2^32 / H), or 0 for one head.  pitch: pairs of a token in the table.
 template <int MODE, int ROT_UNITS, typename OK, typename FILL>
@@ -148,8 +149,8 @@ __device__ __forceinline__ void rotate_tokens(const uint16_t* x, long long xh, l
 }
 __host__ __device__ inline int table_pitch(int rot) { return ((rot >> 1) + 7) & ~7; }
 uint32_t inverse_of(int H) { return H == 1 ? 0u : (uint32_t)(((1ull << 32) + H - 1) / H); }
-// Units a thread has in flight: four where that still leaves every SM its eight blocks (8192 tokens x 32 heads x 128: 25.4 us, against
-// 26.8 with one), else one, so that short calls spread over the SMs (3 x 5001 tokens x 8 heads x 64: 6.1 us against 7.8).
+// Units a thread has in flight: four where that still leaves every SM its eight blocks (8192 tokens x 32 heads x 128: 19.4 us, against
+// 24.7 with one), else one, so that short calls spread over the SMs (3 x 5001 tokens x 8 heads x 64: 6.2 us against 9.5).
 int units_a_thread(long long rows, int D) { return rows * (D / 16) >= 148LL * 8 * THREADS * 4 ? 4 : 1; }
 // tokens of a block of THREADS * `units` units, but no more than the table holds
 int tokens_a_block(int H, int D, int units) { return std::max(1, std::min(ROT_TOKENS, THREADS * units / (H * (D / 16)))); }
@@ -223,9 +224,9 @@ __device__ __forceinline__ uint32_t abs_max2(uint32_t m, const uint4& v) {
 //   query   some tokens' queries
 // The edge block reads the waiting rows it uses up before it writes new ones in their place.  A page's numbers stay in registers
 // between the search for the largest magnitude and the rounding to codes: page * D / 16 / 128 = UNITS units of 16 channels a thread.
-// At most 64 registers up to 4 units, so that eight blocks are on an SM (64 one-token sequences 5.2 -> 3.9 us, 8192 tokens with 32
-// query heads 41.3 -> 39.7 us).
-// 8192 tokens with 32 query and 8 KV heads are 39.6 us (185 MB, 4.7 TB/s), one token 2.3 us, mostly launch.
+// At most 64 registers up to 4 units, so that eight blocks are on an SM (64 one-token sequences 5.2 -> 3.9 us when taken, 8192 tokens
+// with 32 query heads 37.8 -> 33.0 us).
+// 8192 tokens with 32 query and 8 KV heads are 33.0 us (185 MB, 5.6 TB/s), one token 2.1 us, mostly launch.
 // The host does not know the sequences' lengths, so it launches a whole-page block for every `page` rows of the step: unit u belongs
 // to the last sequence b with start[b] / page <= u, which has at least as many of them as pages begin and end in its new tokens.
 template <int UNITS, int MODE, int ROT_UNITS>
