@@ -33,15 +33,19 @@ namespace qp {
 
 namespace {
 
-// Warps of a block and copy stages of a warp.  WIDE: for calls with 64 items and more, of one block of query rows each.  Twelve warps
-// hide more of a tile's chain of dependent steps (64 sequences of up to 16000 tokens: 201 -> 188 us, D = 64 125 -> 107; 64 of 1000:
-// 36.7 -> 35.3), but fill the SM's registers, so that neither the merge nor the next call's blocks come in beside them (one sequence
-// of 2000 tokens: 8.2 us against 10.7).
-__host__ __device__ constexpr int pa_warps(int wide) { return wide ? 12 : 8; }
-__host__ __device__ constexpr int pa_stages(int wide) { return wide ? 2 : 3; }
+// BUSY: calls with 64 (sequence, KV head) pairs and more.  Warps of a block and copy stages of a warp, and registers of a thread:
+//   8 rows    busy: twelve warps, which hide more of a tile's chain of dependent steps (64 sequences of up to 16000 tokens: 201 -> 188
+//             us, D = 64 125 -> 107; 64 of 1000: 36.7 -> 35.3), but fill the SM's registers, so that neither the merge nor the next
+//             call's blocks come in beside them (one sequence of 2000 tokens: 8.2 us against 10.7)
+//   16 rows   else 208 registers, which leave room for a block of the merge (one sequence of 3000 to 4100 tokens with 4 drafts 13.4 us,
+//             against 15.4), busy 255 (16 of them with 8 drafts 52.5 us, against 55.7)
+//   24 rows   255: with 208 a part is spilled (16 sequences with 5 drafts 50 -> 58 us)
+__host__ __device__ constexpr int pa_warps(int nb, int busy) { return nb == 1 && busy ? 12 : 8; }
+__host__ __device__ constexpr int pa_stages(int nb, int busy) { return nb == 1 && busy ? 2 : 3; }
+__host__ __device__ constexpr int pa_registers(int nb, int busy) { return nb == 1 && busy ? 168 : nb < 3 && !busy ? 208 : 255; }
 constexpr int PA_MAX_SEQS = 2048;
 constexpr int PA_SMS = 148;                                     // of a B200; the layout of the workspace goes by it
-constexpr int PA_WORKERS = PA_SMS * pa_warps(1);               // most of a launch
+constexpr int PA_WORKERS = PA_SMS * pa_warps(1, 1);            // most of a launch
 constexpr float PA_HEAD = 11.f;                                 // weights are held against the reference times 2^-11, to use fp16's upper range
 constexpr float PA_SLACK = 4.f;                                 // a maximum is renewed when it is exceeded by 2^4
 
@@ -113,11 +117,11 @@ __device__ __forceinline__ uint32_t swz(int r, int c) {
 template <int D>
 __device__ __forceinline__ int token_of(int i) { return D == 128 ? (i & 1) * 4 + (i >> 1) : i; }
 
-template <int FORMAT, int D, int NB, int WIDE>
-__global__ void __launch_bounds__(pa_warps(WIDE) * 32, 1)
+template <int FORMAT, int D, int NB, int BUSY>
+__global__ void __maxnreg__(pa_registers(NB, BUSY))
 paged_decode_kernel(const __grid_constant__ PagedLaunch p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                     const __grid_constant__ CUtensorMap map_kt, const __grid_constant__ CUtensorMap map_vt) {
-  constexpr int RB = 8 * NB, KS = D / 16, PA_WARPS = pa_warps(WIDE), PA_STAGES = pa_stages(WIDE), PA_THREADS = PA_WARPS * 32;
+  constexpr int RB = 8 * NB, KS = D / 16, PA_WARPS = pa_warps(NB, BUSY), PA_STAGES = pa_stages(NB, BUSY), PA_THREADS = PA_WARPS * 32;
   constexpr uint32_t SLOT = 64 * D, HALF_SLOT = SLOT / 2;       // keys, then values: 32 tokens of codes, or 16 of bf16
   extern __shared__ unsigned char smem_raw[];
   __shared__ uint64_t bars[PA_WARPS * PA_STAGES];
@@ -707,14 +711,14 @@ cudaError_t byte_map(CUtensorMap* map, const void* base, size_t rows, int row_by
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-template <int FORMAT, int D, int NB, int WIDE>
+template <int FORMAT, int D, int NB, int BUSY>
 cudaError_t launch_decode_t(const PagedLaunch& p, const CUtensorMap (&m)[4], cudaStream_t st) {
   static unsigned char done[64];
-  constexpr size_t smem = pa_warps(WIDE) * pa_stages(WIDE) * 64 * D + 1024;
-  auto kernel = paged_decode_kernel<FORMAT, D, NB, WIDE>;
+  constexpr size_t smem = pa_warps(NB, BUSY) * pa_stages(NB, BUSY) * 64 * D + 1024;
+  auto kernel = paged_decode_kernel<FORMAT, D, NB, BUSY>;
   cudaError_t e = allow_smem(kernel, smem, done);
   if (e != cudaSuccess) return e;
-  e = launch_chained(kernel, dim3(PA_SMS), dim3(pa_warps(WIDE) * 32), smem, st, p, m[0], m[1], m[2], m[3]);
+  e = launch_chained(kernel, dim3(PA_SMS), dim3(pa_warps(NB, BUSY) * 32), smem, st, p, m[0], m[1], m[2], m[3]);
   if (e != cudaSuccess) return e;
   const unsigned rows = (unsigned)p.a.s.max_new * p.a.Hq;
   if (rows * p.a.s.n_seqs <= 8 * PA_SMS) return launch_chained(paged_merge_kernel<D, PM_WARPS>, dim3(rows, p.a.s.n_seqs), dim3(PM_WARPS * 32), 0, st, p);
@@ -744,8 +748,8 @@ cudaError_t launch_paged_attn(const PagedAttnArgs& a, void* ws, cudaStream_t st)
   p.a = a;
   p.G = a.Hq / a.Hkv;
   p.RB = rows_of(a.s.max_new, p.G);
-  const bool wide = p.RB == 8 && a.s.n_seqs * a.Hkv >= 64;
-  p.n_workers = PA_SMS * pa_warps(wide);
+  const bool busy = (long long)a.s.n_seqs * a.Hkv >= 64;
+  p.n_workers = PA_SMS * pa_warps(p.RB / 8, busy);
   p.min_tiles = 2;
   const Carve c = carve(a.s.n_seqs, a.s.n_tokens, a.s.max_new, a.Hq, a.Hkv, a.D);
   p.max_items = c.items;
@@ -757,10 +761,9 @@ cudaError_t launch_paged_attn(const PagedAttnArgs& a, void* ws, cudaStream_t st)
   if (e == cudaSuccess) e = byte_map(&m[3], a.v_tail, tail_rows, 2 * a.D, 16, 128);
   if (e != cudaSuccess) return e;
 #define QP_PAGED(F, DD)                                             \
-  return wide           ? launch_decode_t<F, DD, 1, 1>(p, m, st)    \
-         : p.RB == 8    ? launch_decode_t<F, DD, 1, 0>(p, m, st)    \
-         : p.RB == 16   ? launch_decode_t<F, DD, 2, 0>(p, m, st)    \
-                        : launch_decode_t<F, DD, 3, 0>(p, m, st)
+  return p.RB == 8    ? busy ? launch_decode_t<F, DD, 1, 1>(p, m, st) : launch_decode_t<F, DD, 1, 0>(p, m, st) \
+         : p.RB == 16 ? busy ? launch_decode_t<F, DD, 2, 1>(p, m, st) : launch_decode_t<F, DD, 2, 0>(p, m, st) \
+                      : launch_decode_t<F, DD, 3, 0>(p, m, st)
   if (a.format == QP_E4M3) {
     if (a.D == 128) QP_PAGED(QP_E4M3, 128);
     QP_PAGED(QP_E4M3, 64);
