@@ -538,12 +538,13 @@ qp_status qp_paged_append(const void* k_new, int64_t k_stride, const void* v_new
 /*
  * Attention of the step's tokens, after qp_paged_append has taken them in: the token at position p of its sequence sees the tokens at
  * positions <= p,   out[r,h,:] = softmax_t(q[r,h].K[t] / sqrt(D)) V.   q bf16 rows [n_tokens, Hq, D] (device), q_stride elements apart;
- * out bf16 [n_tokens, Hq, D], contiguous.  Queries and waiting rows meet the tensor cores scaled by powers of two, so magnitudes are
- * free as long as queries, values and their logits stay below 2^100; with more than 32 query rows per KV head (max_new * Hq / Hkv) the
- * value scales of a head's pages have to be within 2^90 of one another, too, and what is below 2^-24 of the largest number in 32
- * waiting rows of a head counts for nothing (as little as it will when their page is whole).  Rows that see a key or value that is not finite, or a
- * query of their own, are NaN or what the formula makes of it; a value that is not finite may also make NaN of rows of the same step
- * and sequence that stand before it.
+ * out bf16 [n_tokens, Hq, D], contiguous, elsewhere than q.
+ * Queries and waiting rows meet the tensor cores scaled by powers of two, so magnitudes are free as long as queries, values and their
+ * logits stay below 2^100.  With more than 32 query rows per KV head (max_new * Hq / Hkv) the value scales of a head's pages have to be
+ * within 2^90 of one another, too, and what is below 2^-24 of the largest number in 32 waiting rows of a head counts for nothing (as
+ * little as it will when their page is whole).
+ * Rows that see a key or value that is not finite, or have such a query, are NaN or what the formula makes of it; a value that is not
+ * finite may also make NaN of rows of the same step and sequence that stand before it.
  * workspace: its contents are irrelevant; calls that may run at the same time must not share it.
  * Bounded waits as for qp_window_scores; one that runs out makes the rows that hang on it NaN.
  */
