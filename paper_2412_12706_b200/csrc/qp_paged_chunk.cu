@@ -356,13 +356,13 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(CB_Q, 0));
       }
-      // columns of a box to logits; never 0, which would make a hidden column's -inf a NaN
-      auto factor = [&](float fk) {
+      // columns of a box to logits; never 0, which would make a hidden column's -inf a NaN, nor, where all of the box is hidden, what is
+      // no number, as the scale of a page with such a key is
+      auto factor = [&](float fk, bool hidden) {
         const float f = fk * cq;
-        return f < 0x1p-126f ? 0x1p-126f : f;                   // (NaN stays)
+        return f < 0x1p-126f || hidden ? 0x1p-126f : f;         // (NaN stays)
       };
-      const int lim = has ? c.q.len + tok + 1 : 0;              // positions this row sees
-      const int least = c.q.len + (c.at.rg * 256) / p.G + 1;    // and the item's first row
+      const int lim = c.q.len + (has ? tok : c.q.n - 1) + 1;    // positions this row sees
       float m_run = -INFINITY, l_run = 0.f;                     // (the sum is times 2^-6 until the piece ends)
       float s0 = 1.f, log_s0 = 0.f;
       bool any = false;
@@ -380,7 +380,10 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
             log_s0 = fv.x;
             s0 = __fdiv_rn(0x1p-6f, fv.y);
           }
-          if (128 * (j + 1) > least) {                          // what the row does not see leaves S
+          const int vis = lim - 128 * j;                        // columns of the tile that the row sees
+          int boxes = 4;                                        // of which a row of the warp sees something
+          if (__any_sync(0xffffffffu, vis < 128)) {             // what a row does not see leaves S
+            boxes = min(4, max(1, (__reduce_max_sync(0xffffffffu, vis) + 31) >> 5));
 #pragma unroll 1
             for (int c0 = 0; c0 < 128; c0 += 32) {
               uint32_t v[32], lo[16], hi[16];
@@ -388,8 +391,8 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
               tmem_wait(v);
 #pragma unroll
               for (int i = 0; i < 16; ++i) {
-                lo[i] = 128 * j + c0 + i < lim ? v[i] : 0xff800000u;
-                hi[i] = 128 * j + c0 + 16 + i < lim ? v[16 + i] : 0xff800000u;
+                lo[i] = c0 + i < vis ? v[i] : 0xff800000u;
+                hi[i] = c0 + 16 + i < vis ? v[16 + i] : 0xff800000u;
               }
               __syncwarp();
               tmem_st(ts + c0, lo);
@@ -415,7 +418,7 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
               mx1 = max3(mx1, __uint_as_float(xb[i]), __uint_as_float(xb[i + 1]));
             }
             const float4 fv = s_fv[sr][h2];
-            mx = max3(mx, fmaf(mx0, factor(s_fk[sr][2 * h2]), fv.x), fmaf(mx1, factor(s_fk[sr][2 * h2 + 1]), fv.z));
+            mx = max3(mx, fmaf(mx0, factor(s_fk[sr][2 * h2], false), fv.x), fmaf(mx1, factor(s_fk[sr][2 * h2 + 1], false), fv.z));   // (NaN does not count)
           }
           // a new reference only where the old one is exceeded by more than 2^4 (or there is none yet)
           const bool renew = mx > m_run + PC_SLACK;
@@ -442,15 +445,15 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
           uint32_t v[32], pk[16];
           tmem_ld32_issue(ts, v);
 #pragma unroll 1
-          for (int box = 0; box < 4; ++box) {
+          for (int box = 0; box < boxes; ++box) {
             tmem_wait(v);
             const float2 fv = reinterpret_cast<const float2*>(s_fv[sr])[box];
-            const float f = factor(s_fk[sr][box]), n = ref + fv.x;
+            const float f = factor(s_fk[sr][box], 32 * box >= vis), n = ref + fv.x;
             const uint64_t sc = pack2(f, f), nm = pack2(n, n);
             uint64_t y[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) y[i] = fma2(pack2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), sc, nm);
-            if (box < 3) tmem_ld32_issue(ts + 32 * (box + 1), v);
+            if (box + 1 < boxes) tmem_ld32_issue(ts + 32 * (box + 1), v);
             uint64_t sum2 = pack2(0.f, 0.f), sum3 = sum2;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
@@ -468,6 +471,10 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
             __syncwarp();
             tmem_st(ts + 16 * box, pk);
           }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) pk[i] = 0u;
+#pragma unroll 1
+          for (int box = boxes; box < 4; ++box) tmem_st(ts + 16 * box, pk);
           any = true;
           tmem_wait_st();
           asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");

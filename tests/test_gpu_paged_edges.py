@@ -1,0 +1,62 @@
+"""The paged cache at its edges: pages that hold what is no number, or are none, among those a row sees and those it does not.
+
+Outputs of rows that see nothing of it are held to the bound of tests/test_gpu_paged.py; rows that do are not finite, whatever form of the
+attention takes them, and however its work is cut."""
+import math
+
+import pytest
+import torch
+
+from paper_2412_12706_b200 import qp
+from tests.test_gpu_paged import DEV, E4M3, INT8, fill, ints, make, randn, ref_attn, start_of
+
+pytestmark = pytest.mark.gpu
+NAN, INF = float("nan"), float("inf")
+
+FORMS = [  # Hq, Hkv, D, page, dtype, tokens before, new tokens
+    (4, 2, 128, 32, E4M3, [500, 70], [100, 33]),                   # rows of both halves of an item
+    (2, 2, 64, 32, INT8, [100, 300], [100, 77]),                   # up to 128 rows
+    (8, 1, 128, 64, E4M3, [3000, 5], [300, 1]),                    # several items, each cut
+    (8, 2, 128, 128, INT8, [0, 130], [700, 260]),
+    (1, 1, 128, 128, E4M3, [2800], [160]),                         # a tile a block
+    (8, 8, 64, 32, E4M3, [20 * (b % 5) for b in range(40)], [40 + b for b in range(40)]),     # items that are whole in a block
+]
+
+
+def whole_pages(lens, new, page):
+    """(sequence, page) of the pages that the step completes."""
+    return [(b, i) for b, (n, m) in enumerate(zip(lens, new)) for i in range(n // page, (n + m) // page)]
+
+
+@pytest.mark.parametrize("bad", [NAN, INF])
+@pytest.mark.parametrize("Hq,Hkv,D,page,dtype,lens,new", FORMS)
+def test_a_key_in_a_new_page_leaves_the_rows_before_it_alone(Hq, Hkv, D, page, dtype, lens, new, bad):
+    """A key that is not finite makes the scale of its page so; rows that stand before the page see none of it."""
+    total = [a + b for a, b in zip(lens, new)]
+    c, table = make(len(lens), Hq, Hkv, D, page, dtype, max(total))
+    fill(c, table, total, 11)
+    q = randn((sum(new), Hq, D), 3)
+    step = qp.PagedStep(start_of(new), ints(lens), table, sum(new), max(new))
+    ref, bound = ref_attn(q, c, table, lens, new)
+    pages = whole_pages(lens, new, page)
+    pages = pages[:3] + pages[3::max(1, len(pages) // 12)]
+    assert pages
+    at = start_of(new).tolist()
+    behind = 0
+    for b, i in pages:
+        row = int(table[b, i])
+        first = max(0, i * page - lens[b])                         # rows of the sequence before the page
+        behind += first
+        kept = c.k_scale[row].clone(), c.k_codes[row].clone()
+        head = i % Hkv                                             # one head's
+        c.k_scale[row, head] = bad
+        c.k_codes.view(torch.uint8)[row, head, page - 1, 5] = 0x7f  # as the cache stores it: e4m3 has a code for what is no number
+        got = qp.paged_attn(q, c, step)
+        sees = torch.zeros((sum(new), Hq), dtype=torch.bool, device=DEV)
+        sees[at[b] + first:at[b + 1], head * (Hq // Hkv):(head + 1) * (Hq // Hkv)] = True
+        err = (got.double() - ref).abs() - bound
+        assert (err[~sees] <= 0).all(), (b, i, int(torch.isnan(got[~sees]).any(-1).sum()))
+        if math.isnan(bad):                                        # (an infinite logit of the other sign weighs nothing)
+            assert torch.isnan(got[sees]).all(), (b, i)
+        c.k_scale[row], c.k_codes[row] = kept
+    assert behind > 0
