@@ -495,9 +495,9 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
       }
       const bool whole = c.at.j == 0 && c.n == c.at.tiles;
       const int rec = 2 * cta + (x == x0 ? 0 : 1);
-      if (l_run != l_run) m_run = 0.f;                          // (a sum that is no number has to be looked at)
-      // the sum and O in units without s0, and the reference that goes with them
-      const float m_own = m_run == -INFINITY ? m_run : m_run - log_s0;
+      // The sum and O in units without s0, and the reference that goes with them.  A sum that is no number has to be looked at by those who
+      // join the parts, so its reference is one that counts, whatever has become of m_run and of the scale.
+      const float m_own = l_run != l_run ? 0.f : m_run == -INFINITY ? m_run : m_run - log_s0;
       // four channels of an output row: unnormalised, with the reference and the sum, where others have a part in it
       auto put = [&](int row, int ch, float4 v, float M, float L, float inv) {
         if (FORMAT == QP_INT8) {                                // columns 0, 1, 2, 3 are channels 0, 2, 1, 3
@@ -577,7 +577,7 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
           }
         };
         bar_sync(3, PC_SOFT * 32);                              // both groups have seen their last product: nobody reads the queries
-        s_ml[u * 128 + rl] = make_float2(any || l_run != l_run ? m_own : -INFINITY, l_run);
+        s_ml[u * 128 + rl] = make_float2(m_own, l_run);         // (a group without a tile: -inf, as it began)
         bar_sync(3, PC_SOFT * 32);
         float M = -INFINITY, L;
         if (has) total(r, M, L);

@@ -60,3 +60,39 @@ def test_a_key_in_a_new_page_leaves_the_rows_before_it_alone(Hq, Hkv, D, page, d
             assert torch.isnan(got[sees]).all(), (b, i)
         c.k_scale[row], c.k_codes[row] = kept
     assert behind > 0
+
+
+@pytest.mark.parametrize("what", ["outside the pool", "key scale", "value scale", "infinite value scale"])
+@pytest.mark.parametrize("Hq,Hkv,D,page,dtype,lens,new", FORMS + [
+    (8, 2, 128, 128, E4M3, [1500, 300], [1, 1]), (8, 1, 64, 32, INT8, [900], [3])])              # a few rows
+def test_a_page_that_is_no_number_shows_in_every_row_that_sees_it(Hq, Hkv, D, page, dtype, lens, new, what):
+    """A page number outside the pool, or a page whose scale is no number: none of its rows comes out as if the page were not there,
+    wherever the cuts between blocks fall (a page of 128 tokens is the first of some block's piece, whichever it is)."""
+    total = [a + b for a, b in zip(lens, new)]
+    c, table = make(len(lens), Hq, Hkv, D, page, dtype, max(total))
+    fill(c, table, total, 11)
+    q = randn((sum(new), Hq, D), 3)
+    at = start_of(new).tolist()
+    run = lambda t: qp.paged_attn(q, c, qp.PagedStep(start_of(new), ints(lens), t, sum(new), max(new)))
+    good = run(table)
+    pages = [(b, i) for b, n in enumerate(total) for i in range(n // page)]
+    pages = pages[:30] + pages[30::max(1, len(pages) // 20)]
+    for b, i in pages:
+        row, head = int(table[b, i]), i % Hkv
+        t, kept = table, (c.k_scale[row].clone(), c.v_scale[row].clone())
+        heads = slice(head * (Hq // Hkv), (head + 1) * (Hq // Hkv))
+        if what == "outside the pool":
+            t, heads = table.clone(), slice(0, Hq)
+            t[b, i] = (-1, c.desc.n_pages)[i % 2]
+        else:
+            (c.k_scale if what == "key scale" else c.v_scale)[row, head] = INF if what.startswith("inf") else NAN
+        got = run(t)
+        rows = slice(at[b] + max(0, i * page - lens[b]), at[b + 1])
+        if what.startswith("inf"):                                 # its zeros are no numbers, all else is infinite
+            assert not torch.isfinite(got[rows, heads]).any(), (b, i)
+        else:
+            assert torch.isnan(got[rows, heads]).all(), (b, i, int(torch.isfinite(got[rows, heads]).sum()))
+        rest = torch.ones(got.shape[:2], dtype=torch.bool, device=DEV)
+        rest[at[b]:at[b + 1], heads] = False                       # (rows before the page, too, may be lost to a value)
+        assert torch.equal(got[rest], good[rest]), (b, i)
+        c.k_scale[row], c.v_scale[row] = kept
