@@ -284,7 +284,7 @@ append_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ qp_r
     b = last_at_most(s.start, s.n_seqs, which, [&](int x) { return x >> lgp; });
     q = seq_of(s, b);
     pg = ((q.len + page - 1) >> lgp) + which - (q.row0 >> lgp);
-    if (which < q.row0 >> lgp || (pg + 1) << lgp > q.len + q.n) return;
+    if (which < q.row0 >> lgp || pg >= (q.len + q.n) >> lgp) return;   // (compared in pages: in tokens it could pass 31 bits)
   }
   if (q.n == 0) return;
   const uint16_t* rows = (keys ? a.k : a.v) + (size_t)h * D;

@@ -8,7 +8,7 @@ import pytest
 import torch
 
 from paper_2412_12706_b200 import qp
-from tests.test_gpu_paged import DEV, E4M3, INT8, fill, ints, make, randn, ref_attn, start_of
+from tests.test_gpu_paged import DEV, E4M3, INT8, fill, ints, make, randn, ref_attn, start_of, stored
 
 pytestmark = pytest.mark.gpu
 NAN, INF = float("nan"), float("inf")
@@ -96,3 +96,35 @@ def test_a_page_that_is_no_number_shows_in_every_row_that_sees_it(Hq, Hkv, D, pa
         rest[at[b]:at[b + 1], heads] = False                       # (rows before the page, too, may be lost to a value)
         assert torch.equal(got[rest], good[rest]), (b, i)
         c.k_scale[row], c.v_scale[row] = kept
+
+
+def test_rows_of_nobody_behind_a_sequence_near_the_last_position():
+    """Units of the padding's rows, counted on from the sequence's last page, would stand at tokens beyond 2^31."""
+    Hkv, D, page, n_tokens, m = 2, 64, 32, 5000, 40
+    max_pages = (2 ** 31 - 1025) // page
+    n = max_pages * page - m
+    assert n % page == 24 and (n + n_tokens) // page * page >= 2 ** 31
+    c = qp.alloc_paged(1, 4, Hkv, D, 3, max_pages, page, E4M3)
+    for t in (c.k_codes, c.v_codes):
+        t.view(torch.uint8).fill_(0x7f)
+    for t in (c.k_scale, c.v_scale):
+        t.fill_(NAN)
+    old = [randn((Hkv, 24, D), s) for s in (1, 2)]
+    for t, x in zip((c.k_tail, c.v_tail), old):
+        t[0, :, :24] = x
+    tails = c.k_tail.clone(), c.v_tail.clone()
+    table = torch.zeros((1, max_pages), dtype=torch.int32, device=DEV)
+    table[0, -2:] = ints([1, 2])
+    k, v, q = randn((n_tokens, Hkv, D), 3), randn((n_tokens, Hkv, D), 4), randn((n_tokens, 4, D), 5)
+    rope = qp.rope(D)
+    pos = torch.arange(n, n + m, dtype=torch.int32, device=DEV)
+    turn = lambda x: qp.rotary(x[:m].transpose(0, 1)[None], pos, rope)[0].transpose(0, 1)
+    turned = torch.full_like(q, 55.0)
+    qp.paged_append(k, v, c, qp.PagedStep(ints([0, m]), ints([n]), table, n_tokens, m), rope, q=q, q_out=turned)
+    for codes, scale, before, x in ((c.k_codes, c.k_scale, old[0], turn(k)), (c.v_codes, c.v_scale, old[1], v[:m])):
+        x = torch.cat([before, x.transpose(0, 1)], 1).view(Hkv, 2, page, D).transpose(0, 1)
+        want, s = stored(x, E4M3)
+        assert torch.equal(scale[1:], s) and torch.equal(codes.view(torch.uint8)[1:].view(E4M3).float(), want)
+        assert torch.isnan(scale[0]).all() and (codes.view(torch.uint8)[0] == 0x7f).all()
+    assert torch.equal(turned[:m], turn(q)) and (turned[m:] == 55.0).all()
+    assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(tails, (c.k_tail, c.v_tail)))
