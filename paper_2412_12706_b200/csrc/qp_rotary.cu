@@ -218,6 +218,140 @@ __device__ __forceinline__ uint32_t abs_max2(uint32_t m, const uint4& v) {
   return __vmaxu2(m, v.w & 0x7fff7fffu);
 }
 
+// what an edge or whole block has to do with
+struct PageJob {
+  const uint16_t* rows;                                         // new rows of its head, keys or values
+  long long stride;
+  uint16_t* tail;                                               // the sequence's waiting rows
+  int b, h;
+  bool keys;
+  Seq q;
+};
+__device__ __forceinline__ PageJob page_job(const AppendArgs& a, int b, int h, bool keys, const Seq& q) {
+  const uint16_t* rows = (keys ? a.k : a.v) + (size_t)h * a.D;
+  uint16_t* tail = (keys ? a.k_tail : a.v_tail) + ((size_t)b * a.Hkv + h) * a.s.page * a.D;
+  return PageJob{rows, keys ? a.ks : a.vs, tail, b, h, keys, q};
+}
+// unit u of the row at position p of the sequence; new rows of keys are rotated
+template <int MODE>
+__device__ __forceinline__ void load_unit(const AppendArgs& a, const qp_rope& rope, const uint64_t* turn, const PageJob& w, int p, int u, uint4& x,
+                                          uint4& y, int& c0, int& c1) {
+  const int rot = rope.rot_dim;
+  const bool fresh = p >= w.q.len;
+  const int r = w.q.row0 + p - w.q.len;
+  const uint16_t* row = fresh ? w.rows + r * w.stride : w.tail + (p & (a.s.page - 1)) * a.D;
+  unit_vectors(MODE, rot, u, c0, c1);
+  x = *reinterpret_cast<const uint4*>(row + 8 * c0);
+  y = *reinterpret_cast<const uint4*>(row + 8 * c1);
+  if (fresh && w.keys && rot) {
+    const int at = a.pos ? __ldg(a.pos + r) : p;
+    rotate_unit<MODE>(x, y, u, rot, row, [&](int j) {
+      const float2 c = cos_sin(turn[j], at, rope.factor), d = cos_sin(turn[min(j + 1, (rot >> 1) - 1)], at, rope.factor);
+      return make_float4(c.x, c.y, d.x, d.y);
+    });
+  }
+}
+// stores page pg of the sequence; all of the block, which meets at a barrier after every row has been read
+template <int UNITS, int MODE>
+__device__ __forceinline__ void store_page(const AppendArgs& a, const qp_rope& rope, const uint64_t* turn, uint32_t* s_max, const PageJob& w, int pg) {
+  const int D = a.D, lgu = D == 128 ? 3 : 2, lgp = 31 - __clz(a.s.page), tid = threadIdx.x;
+  const int id = page_of(a.s, w.b, pg);
+  uint4 x[UNITS], y[UNITS];
+  uint32_t m = 0u;
+#pragma unroll
+  for (int k = 0; k < UNITS; ++k) {
+    const int j = tid + k * THREADS;
+    int c0, c1;
+    load_unit<MODE>(a, rope, turn, w, (pg << lgp) + (j >> lgu), j & ((1 << lgu) - 1), x[k], y[k], c0, c1);
+    m = abs_max2(abs_max2(m, x[k]), y[k]);
+  }
+  m = max(m & 0xffffu, m >> 16);
+  m = __reduce_max_sync(0xffffffffu, m);
+  if ((tid & 31) == 0) s_max[tid >> 5] = m;
+  __syncthreads();
+  m = max(max(s_max[0], s_max[1]), max(s_max[2], s_max[3]));
+  // the scale is rounded up to bf16, so that no code is cut off; a number that is none makes the whole page so
+  const bool e4m3 = a.format == QP_E4M3;
+  const float top = __uint_as_float(m << 16);
+  const uint32_t sb = m > 0x7f80u ? 0x7fc0u : (__float_as_uint(__fdiv_rn(top, e4m3 ? 448.f : 127.f)) + 0xffffu) >> 16;
+  const float sc = __uint_as_float(sb << 16), inv = sc == 0.f ? 0.f : fminf(__fdiv_rn(1.f, sc), FLT_MAX);
+  if (id < 0) return;
+  const size_t ph = (size_t)id * a.Hkv + w.h;
+  uint8_t* codes = (w.keys ? a.kc : a.vc) + (ph << lgp) * D;
+  if (tid == 0) (w.keys ? a.k_scale : a.v_scale)[ph] = (uint16_t)sb;
+#pragma unroll
+  for (int k = 0; k < UNITS; ++k) {
+    const int j = tid + k * THREADS;
+    int c0, c1;
+    unit_vectors(MODE, rope.rot_dim, j & ((1 << lgu) - 1), c0, c1);
+    uint8_t* row = codes + (j >> lgu) * D;
+    *reinterpret_cast<uint2*>(row + 8 * c0) = codes8(x[k], inv, e4m3);
+    *reinterpret_cast<uint2*>(row + 8 * c1) = codes8(y[k], inv, e4m3);
+  }
+}
+
+// The sequence that a unit of whole pages, or a row, is taken to belong to.
+__device__ __forceinline__ int unit_owner(const StepView& s, int unit) {
+  const int lgp = 31 - __clz(s.page);
+  return last_at_most(s.start, s.n_seqs, unit, [&](int x) { return x >> lgp; });
+}
+__device__ __forceinline__ int row_owner(const StepView& s, int r) {
+  return last_at_most(s.start, s.n_seqs, r, [](int x) { return x; });
+}
+__device__ __forceinline__ bool has_row(const Seq& q, int r) { return q.n > 0 && r >= q.row0 && r < q.row0 + q.n; }
+
+// Where start falls, those searches can miss the sequence that a unit or a row belongs to, and no block of theirs does the work.  The
+// sequence before the first fall is one that is left out, and its edge blocks do it instead: each for its KV head (and keys or values),
+// sequence by sequence.  Slow, and never met by a step whose numbers belong together.
+template <int UNITS, int MODE>
+__device__ __noinline__ void append_missed(const AppendArgs& a, const qp_rope& rope, const uint64_t* turn, uint32_t* s_max, int fall, int h, bool keys) {
+  const StepView& s = a.s;
+  const int page = s.page, lgp = 31 - __clz(page), lgu = a.D == 128 ? 3 : 2, G = a.Hq / a.Hkv, rot = rope.rot_dim, tid = threadIdx.x;
+  for (int b = 0; b < fall; ++b)
+    if (__ldg(s.start + b) > __ldg(s.start + b + 1)) return;    // not the first
+  for (int b = 0; b < s.n_seqs; ++b) {
+    const Seq q = seq_of(s, b);
+    if (q.n == 0) continue;
+    const int first = (q.len + page - 1) >> lgp, n = ((q.len + q.n) >> lgp) - first;
+    for (int i = 0; i < n; ++i) {
+      if (unit_owner(s, (q.row0 >> lgp) + i) == b) continue;
+      store_page<UNITS, MODE>(a, rope, turn, s_max, page_job(a, b, h, keys, q), first + i);
+      __syncthreads();                                          // (s_max has been read)
+    }
+  }
+  if (!a.q || !keys) return;
+  for (long long i0 = 0; i0 < ((long long)s.n_tokens * G) << lgu; i0 += THREADS) {
+    const long long i = i0 + tid;
+    const int row = (int)(i >> lgu), u = (int)i & ((1 << lgu) - 1), r = row / G, head = h * G + row - r * G;
+    bool mine = false;
+    Seq q{0, 0, 0};
+    if (r < s.n_tokens && !has_row(seq_of(s, row_owner(s, r)), r))
+      for (int b = 0; b < s.n_seqs && !mine; ++b) {
+        q = seq_of(s, b);
+        mine = has_row(q, r);
+      }
+    uint4 x, y;
+    int c0, c1;
+    unit_vectors(MODE, rot, u, c0, c1);
+    if (mine) {
+      const uint16_t* src = a.q + r * a.qs + (long long)head * a.D;
+      const int at = a.pos ? __ldg(a.pos + r) : q.len + r - q.row0;
+      x = *reinterpret_cast<const uint4*>(src + 8 * c0);
+      y = *reinterpret_cast<const uint4*>(src + 8 * c1);
+      rotate_unit<MODE>(x, y, u, rot, src, [&](int j) {
+        const float2 c = cos_sin(turn[j], at, rope.factor), d = cos_sin(turn[min(j + 1, (rot >> 1) - 1)], at, rope.factor);
+        return make_float4(c.x, c.y, d.x, d.y);
+      });
+    }
+    __syncwarp();                                               // (in place: a row's units are one warp's)
+    if (mine) {
+      uint16_t* dst = a.q_out + ((size_t)r * a.Hq + head) * a.D;
+      *reinterpret_cast<uint4*>(dst + 8 * c0) = x;
+      *reinterpret_cast<uint4*>(dst + 8 * c1) = y;
+    }
+  }
+}
+
 // A block is one of three kinds:
 //   edge    (sequence, head, keys or values): the page that waiting rows and new ones complete together, then the new rows that wait
 //   whole   (whole page of new tokens, head, keys or values)
@@ -229,6 +363,7 @@ __device__ __forceinline__ uint32_t abs_max2(uint32_t m, const uint4& v) {
 // 8192 tokens with 32 query and 8 KV heads are 33.0 us (185 MB, 5.6 TB/s), one token 2.1 us, mostly launch.
 // The host does not know the sequences' lengths, so it launches a whole-page block for every `page` rows of the step: unit u belongs
 // to the last sequence b with start[b] / page <= u, which has at least as many of them as pages begin and end in its new tokens.
+// Numbers that do not belong together leave out their own sequence only, see append_missed.
 template <int UNITS, int MODE, int ROT_UNITS>
 __global__ void __launch_bounds__(THREADS, UNITS <= 4 ? 8 : 1)
 append_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ qp_rope rope, int edge_blocks, int page_blocks, int tokens,
@@ -248,9 +383,9 @@ append_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ qp_r
     const int t0 = (bid - page_blocks) * tokens, n = min(tokens, s.n_tokens - t0), half = rot >> 1, pitch = table_pitch(rot);
     bool in = false;
     if (tid < n) {
-      const int r = t0 + tid, b = last_at_most(s.start, s.n_seqs, r, [](int x) { return x; });
-      const Seq q = seq_of(s, b);
-      in = r >= q.row0 && r < q.row0 + q.n;
+      const int r = t0 + tid;
+      const Seq q = seq_of(s, row_owner(s, r));
+      in = has_row(q, r);
       s_pos[tid] = a.pos ? __ldg(a.pos + r) : q.len + r - q.row0;
     }
     __shared__ uint32_t s_in;                                   // tokens that are a sequence's
@@ -280,76 +415,24 @@ append_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ qp_r
     q = seq_of(s, b);
     pg = q.len >> lgp;
     if (q.len == pg << lgp || q.len + q.n < (pg + 1) << lgp) pg = -1;
+    if (q.n == 0 && __ldg(s.start + b) > __ldg(s.start + b + 1)) append_missed<UNITS, MODE>(a, rope, turn, s_max, b, h, keys);
   } else {
-    b = last_at_most(s.start, s.n_seqs, which, [&](int x) { return x >> lgp; });
+    b = unit_owner(s, which);
     q = seq_of(s, b);
     pg = ((q.len + page - 1) >> lgp) + which - (q.row0 >> lgp);
     if (which < q.row0 >> lgp || pg >= (q.len + q.n) >> lgp) return;   // (compared in pages: in tokens it could pass 31 bits)
   }
   if (q.n == 0) return;
-  const uint16_t* rows = (keys ? a.k : a.v) + (size_t)h * D;
-  const long long stride = keys ? a.ks : a.vs;
-  uint16_t* tail = (keys ? a.k_tail : a.v_tail) + (((size_t)b * a.Hkv + h) << lgp) * D;
-  // unit u of the row at position p of the sequence; new rows of keys are rotated
-  auto load = [&](int p, int u, uint4& x, uint4& y, int& c0, int& c1) {
-    const bool fresh = p >= q.len;
-    const int r = q.row0 + p - q.len;
-    const uint16_t* row = fresh ? rows + r * stride : tail + (p & (page - 1)) * D;
-    unit_vectors(MODE, rot, u, c0, c1);
-    x = *reinterpret_cast<const uint4*>(row + 8 * c0);
-    y = *reinterpret_cast<const uint4*>(row + 8 * c1);
-    if (fresh && keys && rot) {
-      const int at = a.pos ? __ldg(a.pos + r) : p;
-      rotate_unit<MODE>(x, y, u, rot, row, [&](int j) {
-        const float2 c = cos_sin(turn[j], at, rope.factor), d = cos_sin(turn[min(j + 1, (rot >> 1) - 1)], at, rope.factor);
-        return make_float4(c.x, c.y, d.x, d.y);
-      });
-    }
-  };
-  if (pg >= 0) {
-    const int id = page_of(s, b, pg);
-    uint4 x[UNITS], y[UNITS];
-    uint32_t m = 0u;
-#pragma unroll
-    for (int k = 0; k < UNITS; ++k) {
-      const int j = tid + k * THREADS;
-      int c0, c1;
-      load((pg << lgp) + (j >> lgu), j & ((1 << lgu) - 1), x[k], y[k], c0, c1);
-      m = abs_max2(abs_max2(m, x[k]), y[k]);
-    }
-    m = max(m & 0xffffu, m >> 16);
-    m = __reduce_max_sync(0xffffffffu, m);
-    if ((tid & 31) == 0) s_max[tid >> 5] = m;
-    __syncthreads();
-    m = max(max(s_max[0], s_max[1]), max(s_max[2], s_max[3]));
-    // the scale is rounded up to bf16, so that no code is cut off; a number that is none makes the whole page so
-    const bool e4m3 = a.format == QP_E4M3;
-    const float top = __uint_as_float(m << 16);
-    const uint32_t sb = m > 0x7f80u ? 0x7fc0u : (__float_as_uint(__fdiv_rn(top, e4m3 ? 448.f : 127.f)) + 0xffffu) >> 16;
-    const float sc = __uint_as_float(sb << 16), inv = sc == 0.f ? 0.f : fminf(__fdiv_rn(1.f, sc), FLT_MAX);
-    if (id >= 0) {
-      const size_t ph = (size_t)id * a.Hkv + h;
-      uint8_t* codes = (keys ? a.kc : a.vc) + (ph << lgp) * D;
-      if (tid == 0) (keys ? a.k_scale : a.v_scale)[ph] = (uint16_t)sb;
-#pragma unroll
-      for (int k = 0; k < UNITS; ++k) {
-        const int j = tid + k * THREADS;
-        int c0, c1;
-        unit_vectors(MODE, rot, j & ((1 << lgu) - 1), c0, c1);
-        uint8_t* row = codes + (j >> lgu) * D;
-        *reinterpret_cast<uint2*>(row + 8 * c0) = codes8(x[k], inv, e4m3);
-        *reinterpret_cast<uint2*>(row + 8 * c1) = codes8(y[k], inv, e4m3);
-      }
-    }
-  }
+  const PageJob w = page_job(a, b, h, keys, q);
+  if (pg >= 0) store_page<UNITS, MODE>(a, rope, turn, s_max, w, pg);
   if (edge) {                                                   // (the barrier above: every waiting row of the page has been read)
     const int end = q.len + q.n, lo = max(q.len, end >> lgp << lgp);
     for (int j = tid; j < (end - lo) << lgu; j += THREADS) {
       const int p = lo + (j >> lgu);
       uint4 x, y;
       int c0, c1;
-      load(p, j & ((1 << lgu) - 1), x, y, c0, c1);
-      uint16_t* row = tail + (p & (page - 1)) * D;
+      load_unit<MODE>(a, rope, turn, w, p, j & ((1 << lgu) - 1), x, y, c0, c1);
+      uint16_t* row = w.tail + (p & (page - 1)) * D;
       *reinterpret_cast<uint4*>(row + 8 * c0) = x;
       *reinterpret_cast<uint4*>(row + 8 * c1) = y;
     }

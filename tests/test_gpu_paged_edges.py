@@ -128,3 +128,63 @@ def test_rows_of_nobody_behind_a_sequence_near_the_last_position():
         assert torch.isnan(scale[0]).all() and (codes.view(torch.uint8)[0] == 0x7f).all()
     assert torch.equal(turned[:m], turn(q)) and (turned[m:] == 55.0).all()
     assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(tails, (c.k_tail, c.v_tail)))
+
+
+def arrays(c):
+    return [t.view(torch.uint8) if t.dtype != torch.bfloat16 else t.view(torch.int16) for t in (c.k_codes, c.v_codes, c.k_scale, c.v_scale, c.k_tail, c.v_tail)]
+
+
+def check_left_out(c, table, start, lens, n, most, seed):
+    """An append of n rows with these starts: sequences whose numbers belong together are taken in as if each were alone, the others,
+    and rows that are nobody's, are left as they are."""
+    Hq, Hkv, D, page = c.desc.n_q_heads, c.desc.n_kv_heads, c.desc.head_dim, c.desc.page
+    seqs, limit = len(lens), c.desc.max_pages * page
+    q, k, v = randn((n, Hq, D), seed), randn((n, Hkv, D), seed + 1), randn((n, Hkv, D), seed + 2)
+    rope = qp.rope(D)
+    before = [t.clone() for t in arrays(c)]
+    good = [b for b in range(seqs) if 0 <= start[b] <= start[b + 1] <= n and start[b + 1] - start[b] <= most and lens[b] >= 0
+            and lens[b] + start[b + 1] - start[b] <= limit]
+    owners = [[b for b in good if start[b] <= r < start[b + 1]] for r in range(n)]
+    alone = []                                                     # the queries, by sequence
+    for b in good:                                                 # (each writes its own pages and tails only)
+        s = [start[b]] * (b + 1) + [start[b + 1]] * (seqs - b)
+        alone.append(qp.paged_append(k, v, c, qp.PagedStep(ints(s), ints(lens), table, n, most), rope, q=q, q_out=torch.full_like(q, 55.0)))
+    want = [t.clone() for t in arrays(c)]
+    for t, x in zip(arrays(c), before):
+        t.copy_(x)
+    got = qp.paged_append(k, v, c, qp.PagedStep(ints(start), ints(lens), table, n, most), rope, q=q, q_out=torch.full_like(q, 55.0))
+    for name, t, x in zip(("k codes", "v codes", "k scales", "v scales", "k tail", "v tail"), arrays(c), want):
+        assert torch.equal(t, x), (name, start[:8])
+    by = dict(zip(good, alone))
+    for r, mine in enumerate(owners):
+        # (each is within 2^-8 of itself and 2^-20 (|u| + |v|) of the formula, see the rotation's tests)
+        close = lambda x: ((got[r].double() - x.double()).abs() <= 2.0 ** -7 * x.double().abs() + 2.0 ** -18 * float(q[r].abs().max())).all()
+        assert any(close(by[b][r]) for b in mine) if mine else (got[r] == 55.0).all(), (r, mine, start[:8])
+    for t, x in zip(arrays(c), before):
+        t.copy_(x)
+    return len(good), sum(len(m) > 1 for m in owners)
+
+
+@pytest.mark.parametrize("D,page,dtype", [(128, 32, E4M3), (64, 64, INT8), (128, 128, E4M3)])
+def test_starts_that_do_not_ascend_leave_out_their_own_sequences_only(D, page, dtype):
+    lens = [100, 40, 70, 0]
+    c, table = make(4, 4, 2, D, page, dtype, 512, seed=1)
+    fill(c, table, lens, 5)
+    seen = [check_left_out(c, table, start, lens, 400, 400, 7 + i) for i, start in enumerate((
+        [0, 999, 2, 300, 400], [0, 250, 1, 200, 90], [-5, 100, 100, 260, 400], [400, 0, 130, 50, 200], [0, 130, 401, 130, 390],
+        [10, 300, 20, 310, 30], [2 ** 31 - 1, -2 ** 31, 7, 150, 150], [300, 200, 100, 50, 0], [0, 100, 200, 300, 400]))]
+    assert [s[0] for s in seen] == [2, 2, 3, 2, 2, 2, 2, 0, 4] and any(s[1] for s in seen), seen
+
+
+def test_starts_of_many_sequences_that_do_not_ascend():
+    seqs, n = 300, 700
+    lens = [(37 * b) % 90 for b in range(seqs)]
+    c, table = make(seqs, 2, 1, 64, 32, E4M3, 400, seed=1)
+    fill(c, table, lens, 5)
+    start = [0] * (seqs + 1)
+    for b in range(seqs):
+        start[b + 1] = start[b] + (b * b) % 5
+    assert start[-1] <= n
+    start[7], start[150], start[299] = 5000, 3, -1
+    good, twice = check_left_out(c, table, start, lens, n, 700, 3)
+    assert 290 < good < 300 and twice > 0
