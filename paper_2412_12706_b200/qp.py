@@ -1076,6 +1076,8 @@ def paged_layer_step(q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, 
         raise QpError(2, "paged_layer_step")
     if size < need:
         raise QpError(4, "paged_layer_step")
+    if stride < Hq * D:
+        raise QpError(1, "paged_layer_step")
     if (address | q.data_ptr() | out.data_ptr()) & 15 or stride & 7:
         raise QpError(5, "paged_layer_step")
     turned = paged_append(k_new, v_new, cache, step, rope_, pos, None if rope_ is None else q)

@@ -322,3 +322,14 @@ def test_rotary_refuses_other_tensors(library):
         with pytest.raises(AssertionError):
             qp.rotary(a["x"], a["pos"], r, a["out"])
     assert len(library.calls) == 1
+
+
+@pytest.mark.parametrize("turned", [False, True])
+@pytest.mark.parametrize("stride", [0, D, HQ * D - 8])
+def test_queries_that_lie_over_one_another_are_refused_before_the_append(lib, library, stride, turned):
+    """Rows of queries nearer to one another than they are long: the attention's refusal, made before the tokens are taken in."""
+    assert lib.qp_paged_attn(A, stride, ctypes.byref(paged()), ctypes.byref(step()), 2 * A, A, BIG, None) == 1
+    with pytest.raises(qp.QpError) as e:
+        qp.paged_layer_step(rows(HQ, strides=(stride, D, 1)), rows(HKV), rows(HKV), held(), new_step(), qp.rope(D) if turned else None, None,
+                            rows(HQ), Tensor((1 << 26,), torch.uint8))
+    assert e.value.status == 1 and not library.calls
