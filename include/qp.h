@@ -566,9 +566,9 @@ qp_status qp_paged_attn(const void* q, int64_t q_stride, const qp_paged* cache /
 qp_status qp_debug_check(uint32_t* words4 /* host, out */);
 
 /*
- * Debug build only: from now on thread block `block` of every qp_decode_attn_tree launch on the current device reports, after its
- * work is done and all its waits have returned, that a bounded wait ran out; -1: none does.  For tests of what is made of such a
- * block.  Synchronises like a cudaMemcpy.  The normal build returns QP_ERR_UNSUPPORTED.
+ * Debug build only: from now on thread block `block` of every qp_decode_attn_tree launch, and of the attention kernel of every
+ * qp_paged_attn, on the current device reports, after its waits have returned, that a bounded wait ran out; -1: none does.  For tests of
+ * what is made of such a block.  Synchronises like a cudaMemcpy.  The normal build returns QP_ERR_UNSUPPORTED.
  */
 qp_status qp_debug_give_up(int block);
 

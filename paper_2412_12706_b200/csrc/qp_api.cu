@@ -558,6 +558,8 @@ cudaError_t quant_check_read(unsigned int (&out)[4]);
 cudaError_t decode_check_read(unsigned int (&out)[4]);
 cudaError_t topk_check_read(unsigned int (&out)[4]);
 cudaError_t tree_give_up(int block);
+cudaError_t paged_attn_give_up(int block);
+cudaError_t paged_chunk_give_up(int block);
 }
 extern "C" {
 #endif
@@ -581,7 +583,9 @@ qp_status qp_debug_check(uint32_t* words4) {
 qp_status qp_debug_give_up(int block) {
   if (block < -1) return QP_ERR_INVALID_ARG;
 #ifdef QP_CHECKED
-  return qp::tree_give_up(block) == cudaSuccess ? QP_OK : QP_ERR_CUDA;
+  return qp::tree_give_up(block) == cudaSuccess && qp::paged_attn_give_up(block) == cudaSuccess &&
+                 qp::paged_chunk_give_up(block) == cudaSuccess
+             ? QP_OK : QP_ERR_CUDA;
 #else
   return QP_ERR_UNSUPPORTED;
 #endif

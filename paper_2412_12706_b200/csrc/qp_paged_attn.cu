@@ -117,6 +117,10 @@ __device__ __forceinline__ uint32_t swz(int r, int c) {
 template <int D>
 __device__ __forceinline__ int token_of(int i) { return D == 128 ? (i & 1) * 4 + (i >> 1) : i; }
 
+#ifdef QP_CHECKED
+__device__ int g_give_up = -1;                                  // see qp_debug_give_up
+#endif
+
 template <int FORMAT, int D, int NB, int BUSY>
 __global__ void __maxnreg__(pa_registers(NB, BUSY))
 paged_decode_kernel(const __grid_constant__ PagedLaunch p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
@@ -538,7 +542,12 @@ paged_decode_kernel(const __grid_constant__ PagedLaunch p, const __grid_constant
       __syncwarp();
       if (issued < total) issue(issued++);
     }
-    if (!ok) {                                                  // what is lost, here and in the rest of the run, shows as NaN
+#ifdef QP_CHECKED
+    const bool lost = (int)blockIdx.x == g_give_up;
+#else
+    constexpr bool lost = false;
+#endif
+    if (!ok || lost) {                                          // what is lost, here and in the rest of the run, shows as NaN
       x = seg + (j1 - j0);
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) { m_run[nb][0] = m_run[nb][1] = 0.f; l[nb][0] = l[nb][1] = NAN; }
@@ -726,6 +735,10 @@ cudaError_t launch_decode_t(const PagedLaunch& p, const CUtensorMap (&m)[4], cud
 }
 
 }  // namespace
+
+#ifdef QP_CHECKED
+cudaError_t paged_attn_give_up(int block) { return cudaMemcpyToSymbol(g_give_up, &block, sizeof(block)); }
+#endif
 
 bool paged_attn_fits(int n_seqs, int n_tokens, int max_new, int Hq, int Hkv, long long most_len) {
   if (many_rows(max_new, Hq / Hkv)) return paged_chunk_fits(n_seqs, n_tokens, Hq, Hkv, most_len);

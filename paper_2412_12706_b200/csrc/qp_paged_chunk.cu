@@ -208,6 +208,10 @@ struct Slot {                                                   // a team's plac
   }
 };
 
+#ifdef QP_CHECKED
+__device__ int g_give_up = -1;                                  // see qp_debug_give_up
+#endif
+
 template <int FORMAT, int D>
 __global__ void __launch_bounds__(PC_THREADS, 1)
 chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
@@ -488,8 +492,13 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
       ok = ok && mbar_wait_warp(bar(CB_S, u), phase, gu);
       phase ^= 1u;
       asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
-      if (!ok) {                                                // what is lost must not look like a row that sees nothing
-        give_up = 1;
+      if (!ok) give_up = 1;
+#ifdef QP_CHECKED
+      const bool lost = cta == g_give_up;
+#else
+      constexpr bool lost = false;
+#endif
+      if (!ok || lost) {                                        // what is lost must not look like a row that sees nothing
         m_run = 0.f;
         l_run = NAN;
       }
@@ -939,6 +948,10 @@ cudaError_t launch_chunk_t(const ChunkLaunch& p, const CUtensorMap& mk, const CU
 }
 
 }  // namespace
+
+#ifdef QP_CHECKED
+cudaError_t paged_chunk_give_up(int block) { return cudaMemcpyToSymbol(g_give_up, &block, sizeof(block)); }
+#endif
 
 size_t paged_chunk_workspace(int n_seqs, int n_tokens, int Hq, int Hkv, int D) { return chunk_carve(n_seqs, n_tokens, Hq, Hkv, D).total; }
 

@@ -3,6 +3,9 @@
 Outputs of rows that see nothing of it are held to the bound of tests/test_gpu_paged.py; rows that do are not finite, whatever form of the
 attention takes them, and however its work is cut."""
 import math
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -12,6 +15,7 @@ from tests.test_gpu_paged import DEV, E4M3, INT8, fill, ints, make, randn, ref_a
 
 pytestmark = pytest.mark.gpu
 NAN, INF = float("nan"), float("inf")
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 FORMS = [  # Hq, Hkv, D, page, dtype, tokens before, new tokens
     (4, 2, 128, 32, E4M3, [500, 70], [100, 33]),                   # rows of both halves of an item
@@ -188,3 +192,44 @@ def test_starts_of_many_sequences_that_do_not_ascend():
     start[7], start[150], start[299] = 5000, 3, -1
     good, twice = check_left_out(c, table, start, lens, n, 700, 3)
     assert 290 < good < 300 and twice > 0
+
+
+# Every block in turn reports that a wait ran out, after all its waits have returned (the range-checked build has a call for it).  The
+# rows that hang on it are NaN, all others as they were: a part that was left out instead would show in other bits.
+GIVE_UP = """
+import torch
+from paper_2412_12706_b200 import qp
+from tests.test_gpu_paged import E4M3, INT8, fill, ints, make, randn, start_of
+for Hq, Hkv, D, page, dtype, lens, new in (
+        (8, 2, 128, 64, E4M3, [3000, 5], [1, 1]), (8, 8, 64, 32, INT8, [700] * 9, [1] * 9), (8, 1, 128, 32, E4M3, [900], [3]),
+        (8, 2, 64, 128, E4M3, [1000, 20], [4, 2]),
+        (4, 2, 128, 32, E4M3, [500, 70], [100, 33]), (2, 2, 64, 32, INT8, [100, 300], [100, 77]), (8, 1, 128, 64, INT8, [3000, 5], [300, 1]),
+        (8, 8, 64, 32, E4M3, [20 * (b % 5) for b in range(40)], [40 + b for b in range(40)])):
+    total = [a + b for a, b in zip(lens, new)]
+    c, table = make(len(lens), Hq, Hkv, D, page, dtype, max(total))
+    fill(c, table, total, 5)
+    q = randn((sum(new), Hq, D), 1)
+    step = qp.PagedStep(start_of(new), ints(lens), table, sum(new), max(new))
+    good = qp.paged_attn(q, c, step)
+    assert torch.isfinite(good).all()
+    seen, blocks = torch.zeros(good.shape[:2], dtype=torch.bool, device="cuda"), 0
+    for block in range(148):
+        assert qp.debug_give_up(block) == 0
+        out = qp.paged_attn(q, c, step)
+        lost = torch.isnan(out).all(-1)
+        assert torch.equal(out[~lost], good[~lost]), (Hq, Hkv, D, lens, block)
+        seen |= lost
+        blocks += bool(lost.any())
+    G, work = Hq // Hkv, 0                                         # at least: a block for 32 tiles of 32 tokens, or for one of 128
+    for n, m in zip(total, new):
+        work += Hkv * (-(-m * G // 256) * -(-(n - m) // 128) if max(new) * G > 32 else n // page * page // 32 // 32)
+    assert seen.all() and blocks >= max(1, min(148, work)), (blocks, work)
+    assert qp.debug_give_up(-1) == 0 and torch.equal(good, qp.paged_attn(q, c, step))
+print("poisoned")
+"""
+
+
+def test_what_a_block_lost_whose_wait_ran_out_is_nan():
+    env = dict(os.environ, QP_LIBRARY=os.environ.get("QP_CHECKED_LIBRARY") or os.path.join(ROOT, "paper_2412_12706_b200", "libqp_checked.so"))
+    r = subprocess.run([sys.executable, "-c", GIVE_UP], env=env, cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.strip() == "poisoned", r.stdout[-1000:] + r.stderr[-3000:]
