@@ -555,10 +555,10 @@ qp_status qp_paged_attn(const void* q, int64_t q_stride, const qp_paged* cache /
 /*
  * Debug build only (libqp_checked.so, compiled with -DQP_CHECKED; no counterpart in the paper).  In that build
  * every index a kernel reads from DEVICE memory and then uses as an address (the kept positions given to the
- * gather / quantize kernels, the side lists' tile pointers and entries), and every output position the top-k kernels
- * compute from their counts, is compared with its limit first; a
+ * gather / quantize kernels, the side lists' tile pointers and entries, the starts, lengths and page numbers of a qp_step), and every
+ * output position the top-k kernels compute from their counts, is compared with its limit first; a
  * violation never traps: the first one is recorded, all are counted, and the access goes to element 0 or is
- * skipped.  This call synchronises the device, copies the record to words4 (host: 1 + site of the first
+ * skipped.  (Those of a qp_step are skipped in every build, and counted once for each time that they are looked at.)  This call synchronises the device, copies the record to words4 (host: 1 + site of the first
  * violation or 0, the offending index, its limit, the number of violations) and clears it.  Indices that
  * come from host fields (n_keep, n_cap, n_tail, shapes) are validated by every entry point before any launch in
  * both builds.  The normal build returns QP_ERR_UNSUPPORTED and zeros.

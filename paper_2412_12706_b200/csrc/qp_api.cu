@@ -557,6 +557,9 @@ namespace qp {
 cudaError_t quant_check_read(unsigned int (&out)[4]);
 cudaError_t decode_check_read(unsigned int (&out)[4]);
 cudaError_t topk_check_read(unsigned int (&out)[4]);
+cudaError_t rotary_check_read(unsigned int (&out)[4]);
+cudaError_t paged_attn_check_read(unsigned int (&out)[4]);
+cudaError_t paged_chunk_check_read(unsigned int (&out)[4]);
 cudaError_t tree_give_up(int block);
 cudaError_t paged_attn_give_up(int block);
 cudaError_t paged_chunk_give_up(int block);
@@ -566,13 +569,16 @@ extern "C" {
 qp_status qp_debug_check(uint32_t* words4) {
   if (!words4) return QP_ERR_INVALID_ARG;
 #ifdef QP_CHECKED
-  unsigned int a[4], b[4], c[4];
-  if (qp::quant_check_read(a) != cudaSuccess || qp::decode_check_read(b) != cudaSuccess ||
-      qp::topk_check_read(c) != cudaSuccess)
-    return QP_ERR_CUDA;
-  const unsigned int* first = a[0] ? a : b[0] ? b : c;
-  words4[0] = first[0]; words4[1] = first[1]; words4[2] = first[2];
-  words4[3] = a[3] + b[3] + c[3];
+  cudaError_t (*const units[])(unsigned int (&)[4]) = {qp::quant_check_read,  qp::decode_check_read,     qp::topk_check_read,
+                                                       qp::rotary_check_read, qp::paged_attn_check_read, qp::paged_chunk_check_read};
+  unsigned int all[4] = {0u, 0u, 0u, 0u};
+  for (auto read : units) {
+    unsigned int one[4];
+    if (read(one) != cudaSuccess) return QP_ERR_CUDA;
+    if (!all[0]) { all[0] = one[0]; all[1] = one[1]; all[2] = one[2]; }
+    all[3] += one[3];
+  }
+  for (int i = 0; i < 4; ++i) words4[i] = all[i];
   return QP_OK;
 #else
   words4[0] = words4[1] = words4[2] = words4[3] = 0u;

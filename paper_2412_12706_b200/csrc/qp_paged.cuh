@@ -3,6 +3,7 @@
 
 #include <cuda.h>
 
+#include "qp_checked.cuh"
 #include "qp_common.cuh"
 
 namespace qp {
@@ -14,20 +15,31 @@ struct StepView {
 };
 // Sequence b of a step: rows row0 .. row0 + n - 1 of the step's arrays stand at positions len .. len + n - 1.  Numbers that do not
 // belong together (rows outside the arrays, more tokens than the host said, more than the page table's row holds) give n = 0: the
-// sequence is left out, and nothing is addressed by them.
+// sequence is left out, and nothing is addressed by them.  (The range-checked build records them, too.)
 struct Seq {
   int row0, n, len;
 };
 __device__ __forceinline__ Seq seq_of(const StepView& s, int b) {
   const int r0 = __ldg(s.start + b), r1 = __ldg(s.start + b + 1), len = __ldg(s.len + b);
-  const bool ok = r0 >= 0 && r1 >= r0 && r1 <= s.n_tokens && r1 - r0 <= s.max_new && len >= 0 &&
-                  (long long)len + (r1 - r0) <= (long long)s.max_pages * s.page;
+  const bool rows = r0 >= 0 && r1 >= r0 && r1 <= s.n_tokens && r1 - r0 <= s.max_new;
+  const bool ok = rows && len >= 0 && (long long)len + (r1 - r0) <= (long long)s.max_pages * s.page;
+#ifdef QP_CHECKED
+  if (!rows) {
+    if (QP_IN_RANGE(r0, s.n_tokens + 1LL, QP_SITE_STEP_START)) QP_IN_RANGE((long long)r1 - r0, min(s.max_new, s.n_tokens - r0) + 1LL, QP_SITE_STEP_START);
+  } else if (r1 > r0) {
+    QP_IN_RANGE(len, (long long)s.max_pages * s.page - (r1 - r0) + 1, QP_SITE_STEP_LEN);
+  }
+#endif
   return Seq{r0, ok ? r1 - r0 : 0, len};
 }
 // page i of sequence b; one that is outside the pool becomes -1
 __device__ __forceinline__ int page_of(const StepView& s, int b, int i) {
   const int p = __ldg(s.pages + (size_t)b * s.max_pages + i);
-  return (unsigned)p < (unsigned)s.n_pages ? p : -1;
+  const bool ok = (unsigned)p < (unsigned)s.n_pages;
+#ifdef QP_CHECKED
+  if (!ok) QP_IN_RANGE(p, s.n_pages, QP_SITE_STEP_PAGE);
+#endif
+  return ok ? p : -1;
 }
 
 struct RotaryArgs {

@@ -737,6 +737,7 @@ cudaError_t launch_decode_t(const PagedLaunch& p, const CUtensorMap (&m)[4], cud
 }  // namespace
 
 #ifdef QP_CHECKED
+cudaError_t paged_attn_check_read(unsigned int (&out)[4]) { return checked::read_and_clear(out); }
 cudaError_t paged_attn_give_up(int block) { return cudaMemcpyToSymbol(g_give_up, &block, sizeof(block)); }
 #endif
 

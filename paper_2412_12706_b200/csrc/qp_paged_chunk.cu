@@ -950,6 +950,7 @@ cudaError_t launch_chunk_t(const ChunkLaunch& p, const CUtensorMap& mk, const CU
 }  // namespace
 
 #ifdef QP_CHECKED
+cudaError_t paged_chunk_check_read(unsigned int (&out)[4]) { return checked::read_and_clear(out); }
 cudaError_t paged_chunk_give_up(int block) { return cudaMemcpyToSymbol(g_give_up, &block, sizeof(block)); }
 #endif
 

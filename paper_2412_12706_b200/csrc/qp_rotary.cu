@@ -481,4 +481,8 @@ cudaError_t launch_paged_append(const AppendArgs& a, const qp_rope* rope_or_null
 #undef QP_APPEND
 }
 
+#ifdef QP_CHECKED
+cudaError_t rotary_check_read(unsigned int (&out)[4]) { return checked::read_and_clear(out); }
+#endif
+
 }  // namespace qp

@@ -233,3 +233,47 @@ def test_what_a_block_lost_whose_wait_ran_out_is_nan():
     env = dict(os.environ, QP_LIBRARY=os.environ.get("QP_CHECKED_LIBRARY") or os.path.join(ROOT, "paper_2412_12706_b200", "libqp_checked.so"))
     r = subprocess.run([sys.executable, "-c", GIVE_UP], env=env, cwd=ROOT, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and r.stdout.strip() == "poisoned", r.stdout[-1000:] + r.stderr[-3000:]
+
+
+# The range-checked build says which number of a step it left out; what comes out is the normal build's.
+CHECKED = """
+import torch
+from paper_2412_12706_b200 import qp
+from tests.test_gpu_paged import E4M3, fill, ints, make, randn, start_of
+for new in ([1, 1], [60, 3]):
+    lens, n = [100, 40], sum(new)
+    c, table = make(2, 8, 2, 128, 32, E4M3, 256)
+    fill(c, table, lens, 5)
+    q, k = randn((n, 8, 128), 1), randn((n, 2, 128), 2)
+    def run(start=start_of(new).tolist(), ln=lens, t=table, attend=True):
+        step = qp.PagedStep(ints(start), ints(ln), t, n, max(new))
+        turned = qp.paged_append(k, k, c, step, qp.rope(128), q=q)
+        out = qp.paged_attn(q, c, step, out=torch.full_like(q, 77.0)) if attend else None
+        status, words = qp.debug_check()
+        assert status == STATUS, status
+        return out, words
+    good, words = run()
+    assert words == [0, 0, 0, 0] and torch.isfinite(good).all(), words
+    bad = table.clone()
+    bad[0, 1] = c.desc.n_pages + 5
+    for got, site, index, limit in ((run(t=bad), 9, c.desc.n_pages + 5, c.desc.n_pages), (run([0, new[0], n + 1]), 7, new[1] + 1, min(max(new), new[1]) + 1),
+                                    (run([-1, new[0], n]), 7, 2 ** 32 - 1, n + 1), (run(ln=[256, 40]), 8, 256, 256 - new[0] + 1)):
+        out, words = got
+        if STATUS == 0:
+            assert words[:3] == [1 + site, index, limit] and words[3] > 0, (words, site, index, limit)
+        if site == 9:
+            assert torch.isnan(out[:new[0]]).all() and torch.equal(out[new[0]:], good[new[0]:])
+        else:
+            lost = slice(new[0], n) if site == 7 and index == new[1] + 1 else slice(0, new[0])
+            kept = slice(0, new[0]) if lost.start else slice(new[0], n)
+            assert (out[lost] == 77.0).all() and torch.equal(out[kept], good[kept])
+    assert run()[1] == [0, 0, 0, 0]
+print("checked")
+"""
+
+
+@pytest.mark.parametrize("library,status", [("libqp_checked.so", 0), ("libqp.so", 2)])
+def test_the_range_checked_build_names_what_was_left_out(library, status):
+    env = dict(os.environ, QP_LIBRARY=os.path.join(ROOT, "paper_2412_12706_b200", library))
+    r = subprocess.run([sys.executable, "-c", CHECKED.replace("STATUS", str(status))], env=env, cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.strip() == "checked", r.stdout[-1000:] + r.stderr[-3000:]
