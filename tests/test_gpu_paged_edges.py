@@ -277,3 +277,46 @@ def test_the_range_checked_build_names_what_was_left_out(library, status):
     env = dict(os.environ, QP_LIBRARY=os.path.join(ROOT, "paper_2412_12706_b200", library))
     r = subprocess.run([sys.executable, "-c", CHECKED.replace("STATUS", str(status))], env=env, cwd=ROOT, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and r.stdout.strip() == "checked", r.stdout[-1000:] + r.stderr[-3000:]
+
+
+def overlapping_run(apart):
+    """Decode calls that may overlap one another, each handing its output to rotations, appends and paged attention that write what the
+    next reads; apart: with a synchronisation after every call."""
+    Bt, H, D, steps, page = 1, 8, 128, 40, 32
+    K, V = randn((Bt, H, 600, D), 1), randn((Bt, H, 600, D), 2)
+    X, _ = qp.compress_layer(K, V, randn((Bt, H, 32, D), 3), 256 * 8, 8, 32, 7)
+    c, table = make(1, H, H, D, page, E4M3, 200)
+    rope, ws = qp.rope(D), qp.new_decode_workspace(qp.decode_workspace_bytes(X), DEV)
+    paged_ws = qp.new_decode_workspace(qp.paged_attn_workspace_bytes(c, 1, 1), DEV)
+    outs = [torch.zeros((Bt, H, D), dtype=torch.bfloat16, device=DEV) for _ in range(5 * steps)]
+    done = torch.cuda.synchronize if apart else lambda: None
+    start, lens = ints([0, 1]), [ints([s]) for s in range(steps)]
+    plan = [qp.PagedStep(start, n, table, 1, 1) for n in lens]
+    q = randn((Bt, H, D), 4)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        qp.decode_overlap(True)
+        for s in range(steps):
+            a, b, t, o, e = outs[5 * s:5 * s + 5]
+            qp.decode_attn(q, X, a, ws); done()
+            qp.decode_attn(a, X, b, ws); done()
+            qp.rotary(b.view(Bt, H, 1, D), lens[s], rope, out=t.view(Bt, H, 1, D)); done()
+            qp.decode_attn(t, X, e, ws); done()
+            qp.paged_append(t, b, c, plan[s], rope, q=e, q_out=o); done()
+            qp.decode_attn(o, X, a, ws); done()
+            qp.paged_attn(a, c, plan[s], out=e, workspace=paged_ws); done()
+            q = e
+        qp.decode_overlap(False)
+    torch.cuda.synchronize()
+    n = steps // page * page
+    ids = table[0, :n // page].long()
+    return outs + [c.k_tail[0, :, :steps - n], c.v_tail[0, :, :steps - n]] + [t.view(torch.uint8)[ids] for t in (c.k_codes, c.v_codes)]
+
+
+def test_paged_calls_among_decode_calls_that_may_overlap():
+    want = overlapping_run(True)
+    assert all(torch.isfinite(t.float()).all() for t in want)
+    for _ in range(5):
+        for i, (a, b) in enumerate(zip(want, overlapping_run(False))):
+            assert torch.equal(a, b), i
