@@ -542,7 +542,8 @@ qp_status qp_paged_append(const void* k_new, int64_t k_stride, const void* v_new
  * Queries and waiting rows meet the tensor cores scaled by powers of two, so magnitudes are free as long as queries, values and their
  * logits stay below 2^100.  With more than 32 query rows per KV head (max_new * Hq / Hkv) the value scales of a head's pages have to be
  * within 2^90 of one another, too, and what is below 2^-24 of the largest number in 32 waiting rows of a head counts for nothing (as
- * little as it will when their page is whole).
+ * little as it will when their page is whole).  There the scale of 32 waiting rows is their largest value, and that of a page, or of 32
+ * waiting rows, of nothing but zeros is 2^-60: beside such, scales below 2^-70 cost accuracy.
  * Rows that see a key or value that is not finite, or have such a query, are NaN or what the formula makes of it; a value that is not
  * finite may also make NaN of rows of the same step and sequence that stand before it.
  * workspace: its contents are irrelevant; calls that may run at the same time must not share it.

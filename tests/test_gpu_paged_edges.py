@@ -11,7 +11,7 @@ import pytest
 import torch
 
 from paper_2412_12706_b200 import qp
-from tests.test_gpu_paged import DEV, E4M3, INT8, fill, ints, make, randn, ref_attn, start_of, stored
+from tests.test_gpu_paged import DEV, E4M3, INT8, check_attn, fill, ints, make, randn, ref_attn, start_of, stored
 
 pytestmark = pytest.mark.gpu
 NAN, INF = float("nan"), float("inf")
@@ -320,3 +320,20 @@ def test_paged_calls_among_decode_calls_that_may_overlap():
     for _ in range(5):
         for i, (a, b) in enumerate(zip(want, overlapping_run(False))):
             assert torch.equal(a, b), i
+
+
+@pytest.mark.parametrize("dtype", [E4M3, INT8])
+@pytest.mark.parametrize("v_scale", [2.0 ** -60, 1.0, 2.0 ** 34])
+@pytest.mark.parametrize("new", [[2, 1], [40, 9], [300, 70]])
+def test_values_that_are_zero_beside_small_and_large_ones(dtype, v_scale, new):
+    """Whole pages, and 32 waiting rows, of zeros take their share of the weight and leave the others theirs."""
+    lens = [500, 70]
+    total = [a + b for a, b in zip(lens, new)]
+    c, table = make(2, 8, 2, 128, 128, dtype, max(total))
+    fill(c, table, total, 11, 1.0, v_scale)
+    for b, i in ((0, 0), (0, 2)):                                  # the first of all, and one between others
+        row = int(table[b, i])
+        c.v_codes.view(torch.uint8)[row] = 0
+        c.v_scale[row] = 0
+    c.v_tail[1, 0, :32] = 0
+    check_attn(c, table, lens, new)
