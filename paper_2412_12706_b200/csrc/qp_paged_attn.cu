@@ -38,8 +38,8 @@ namespace {
 //             us, D = 64 125 -> 107; 64 of 1000: 36.7 -> 35.3), but fill the SM's registers, so that neither the merge nor the next
 //             call's blocks come in beside them (one sequence of 2000 tokens: 8.2 us against 10.7)
 //   16 rows   else 208 registers, which leave room for a block of the merge (one sequence of 3000 to 4100 tokens with 4 drafts 13.4 us,
-//             against 15.4), busy 255 (16 of them with 8 drafts 52.5 us, against 55.7)
-//   24 rows   255: with 208 a part is spilled (16 sequences with 5 drafts 50 -> 58 us)
+//             against 15.4), busy 255 (16 of them with 8 drafts 52.5 us, against 55.7); D = 64 needs 202, so there is one form of it
+//   24 rows   255, where D = 128 spills three to nine of them: with 208 it spills far more (16 sequences with 5 drafts 50 -> 58 us)
 __host__ __device__ constexpr int pa_warps(int nb, int busy) { return nb == 1 && busy ? 12 : 8; }
 __host__ __device__ constexpr int pa_stages(int nb, int busy) { return nb == 1 && busy ? 2 : 3; }
 __host__ __device__ constexpr int pa_registers(int nb, int busy) { return nb == 1 && busy ? 168 : nb < 3 && !busy ? 208 : 255; }
@@ -776,7 +776,7 @@ cudaError_t launch_paged_attn(const PagedAttnArgs& a, void* ws, cudaStream_t st)
   if (e != cudaSuccess) return e;
 #define QP_PAGED(F, DD)                                             \
   return p.RB == 8    ? busy ? launch_decode_t<F, DD, 1, 1>(p, m, st) : launch_decode_t<F, DD, 1, 0>(p, m, st) \
-         : p.RB == 16 ? busy ? launch_decode_t<F, DD, 2, 1>(p, m, st) : launch_decode_t<F, DD, 2, 0>(p, m, st) \
+         : p.RB == 16 ? busy ? launch_decode_t<F, DD, 2, DD == 128>(p, m, st) : launch_decode_t<F, DD, 2, 0>(p, m, st) \
                       : launch_decode_t<F, DD, 3, 0>(p, m, st)
   if (a.format == QP_E4M3) {
     if (a.D == 128) QP_PAGED(QP_E4M3, 128);
