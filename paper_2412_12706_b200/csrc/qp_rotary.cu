@@ -48,6 +48,8 @@ __device__ __forceinline__ void unit_vectors(int mode, int rot, int u, int& c0, 
   c0 = across ? u : 2 * u;
   c1 = across ? u + half : 2 * u + 1;
 }
+// x c + y s, rounded as written here wherever it is: what a page holds must not depend on the kernel that a token came in with
+__device__ __forceinline__ float turned(float x, float c, float y, float s) { return fmaf(x, c, __fmul_rn(y, s)); }
 // Rotates a unit whose vectors are a and b.  cs2(i): cosines and sines of pairs i and i + 1, i even.  row: the row itself, which PAIR_ODD reads again.
 template <int MODE, typename CS>
 __device__ __forceinline__ void rotate_unit(uint4& a, uint4& b, int u, int rot, const uint16_t* row, CS cs2) {
@@ -59,8 +61,8 @@ __device__ __forceinline__ void rotate_unit(uint4& a, uint4& b, int u, int rot, 
       if (2 * p < rot) {
         const float4 t = cs2(p);
         const float x = bf16lo(w[i]), y = bf16hi(w[i]), z = bf16lo(w[i + 1]), v = bf16hi(w[i + 1]);
-        w[i] = pack_bf16x2(x * t.x - y * t.y, y * t.x + x * t.y);
-        if (2 * p + 2 < rot) w[i + 1] = pack_bf16x2(z * t.z - v * t.w, v * t.z + z * t.w);
+        w[i] = pack_bf16x2(turned(x, t.x, -y, t.y), turned(y, t.x, x, t.y));
+        if (2 * p + 2 < rot) w[i + 1] = pack_bf16x2(turned(z, t.z, -v, t.w), turned(v, t.z, z, t.w));
       }
     }
   } else if (MODE == PAIR_HALF) {
@@ -69,8 +71,8 @@ __device__ __forceinline__ void rotate_unit(uint4& a, uint4& b, int u, int rot, 
       for (int i = 0; i < 4; ++i) {
         const float4 t = cs2(8 * u + 2 * i);
         const float x0 = bf16lo(w[i]), x1 = bf16hi(w[i]), y0 = bf16lo(w[4 + i]), y1 = bf16hi(w[4 + i]);
-        w[i] = pack_bf16x2(x0 * t.x - y0 * t.y, x1 * t.z - y1 * t.w);
-        w[4 + i] = pack_bf16x2(y0 * t.x + x0 * t.y, y1 * t.z + x1 * t.w);
+        w[i] = pack_bf16x2(turned(x0, t.x, -y0, t.y), turned(x1, t.z, -y1, t.w));
+        w[4 + i] = pack_bf16x2(turned(y0, t.x, x0, t.y), turned(y1, t.z, x1, t.w));
       }
     }
   } else {
@@ -88,7 +90,7 @@ __device__ __forceinline__ void rotate_unit(uint4& a, uint4& b, int u, int rot, 
           const float4 both = cs2(p & ~1);
           const float2 t = p & 1 ? make_float2(both.z, both.w) : make_float2(both.x, both.y);
           const float y = bf16_bits_to_f32(row[d < half ? d + half : d - half]);
-          o[j] = x * t.x + (d < half ? -y : y) * t.y;
+          o[j] = turned(x, t.x, d < half ? -y : y, t.y);
         }
       }
 #pragma unroll

@@ -11,7 +11,7 @@ import pytest
 import torch
 
 from paper_2412_12706_b200 import qp
-from tests.test_gpu_paged import DEV, E4M3, INT8, check_attn, fill, ints, make, randn, ref_attn, start_of, stored
+from tests.test_gpu_paged import DEV, E4M3, INT8, check_attn, check_cache, fill, ints, make, randn, ref_attn, start_of, stored
 
 pytestmark = pytest.mark.gpu
 NAN, INF = float("nan"), float("inf")
@@ -161,9 +161,7 @@ def check_left_out(c, table, start, lens, n, most, seed):
         assert torch.equal(t, x), (name, start[:8])
     by = dict(zip(good, alone))
     for r, mine in enumerate(owners):
-        # (each is within 2^-8 of itself and 2^-20 (|u| + |v|) of the formula, see the rotation's tests)
-        close = lambda x: ((got[r].double() - x.double()).abs() <= 2.0 ** -7 * x.double().abs() + 2.0 ** -18 * float(q[r].abs().max())).all()
-        assert any(close(by[b][r]) for b in mine) if mine else (got[r] == 55.0).all(), (r, mine, start[:8])
+        assert any(torch.equal(got[r], by[b][r]) for b in mine) if mine else (got[r] == 55.0).all(), (r, mine, start[:8])
     for t, x in zip(arrays(c), before):
         t.copy_(x)
     return len(good), sum(len(m) > 1 for m in owners)
@@ -337,3 +335,29 @@ def test_values_that_are_zero_beside_small_and_large_ones(dtype, v_scale, new):
         c.v_scale[row] = 0
     c.v_tail[1, 0, :32] = 0
     check_attn(c, table, lens, new)
+
+
+@pytest.mark.parametrize("rot,inter", [(128, False), (80, False), (64, True), (22, False)])
+@pytest.mark.parametrize("dtype,page", [(E4M3, 32), (INT8, 128)])
+def test_every_call_rounds_a_rotation_alike(rot, inter, dtype, page):
+    """Many numbers, so that sums that nearly cancel are among them, where fused and separate products round differently: queries and keys
+    of an append are qp_rotary's, and a page holds the same, whatever the calls' sizes, which choose between kernels."""
+    n, Hq, Hkv, D = 6000, 32, 8, 128
+    k, q = randn((n, Hkv, D), 1), randn((n, Hq, D), 2)
+    rope = qp.rope(rot, 500000.0, inter)
+    pos = torch.arange(n, dtype=torch.int32, device=DEV)
+    turn = lambda x: qp.rotary(x.transpose(0, 1)[None], pos, rope)[0].transpose(0, 1)
+    kr, qr = turn(k), turn(q)
+    assert torch.equal(qr[:, :1], torch.cat([qp.rotary(q[i:i + 500, :1].transpose(0, 1)[None], pos[i:i + 500], rope)[0].transpose(0, 1)
+                                             for i in range(0, n, 500)]))
+    held = []
+    for size in (n, 500, 37):
+        c, table = make(1, Hq, Hkv, D, page, dtype, n)
+        for i in range(0, n, size):
+            m = min(size, n - i)
+            out = qp.paged_append(k[i:i + m], k[i:i + m], c, qp.PagedStep(ints([0, m]), ints([i]), table, m, m), rope, q=q[i:i + m])
+            assert torch.equal(out, qr[i:i + m]), (size, i, int((out != qr[i:i + m]).sum()))
+        held.append([t[table[0, :n // page].long()] for t in arrays(c)[:4]] + [c.k_tail[0, :, :n % page]])
+        check_cache(c, table, [kr], [k], [n], dtype)
+    for other in held[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(held[0], other))
