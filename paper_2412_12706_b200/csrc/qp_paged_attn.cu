@@ -18,11 +18,15 @@
 //
 // Waiting rows are bf16 and are multiplied as such, the weights as the sum of two bf16 numbers.
 //
-// Measured, of a replayed graph: 64 sequences of up to 16000 tokens (1.1 GB) 187 us, 5.9 TB/s, bound by HBM; 8 sequences of 32000 in
-// int8 (511 MB) 92 us, 5.6 TB/s; one of 2000 tokens 8.2 us, two launches and three dependent reads (lengths, page, tile).  More rows
-// per KV head are bound by the chain of dependent instructions of a tile (conversion, product, softmax, product) in the two warps that
-// a scheduler has, 255 registers each: 16 sequences of 3000 to 4100 tokens, 8 / 16 / 20 rows 37 / 41 / 49 us against 18 for the bytes,
-// issue slots 36 %, tensor pipe 28 %.
+// Rounded to fewer than 32 bits, because the products' operands are: queries, to fp16 times one power of two for a row (exact from 2^-17
+// of the row's largest on, and what is below 2^-24 of it lost), and the weights of pages, to fp16, 2^-11 of themselves against the 2^-8 of
+// the output.  The sum takes the weights as rounded, so a heavy one's rounding cancels.
+//
+// Measured over changing inputs: 64 sequences of up to 16000 tokens (1.1 GB) 194 us, 5.6 TB/s, bound by HBM; 8 sequences of 32000 in
+// int8 (511 MB) 97 us, 5.3 TB/s; one of 2000 tokens 10.2 us (8.2 of one cache in L2), two launches and three dependent reads (lengths,
+// page, tile).  More rows per KV head are bound by the chain of dependent instructions of a tile (conversion, product, softmax, product)
+// in the two warps that a scheduler has, 255 registers each: 16 sequences of 3000 to 4100 tokens, 8 / 16 / 20 / 24 / 32 rows 38 / 44 /
+// 53 / 53 / 57 us against 18 for the bytes, issue slots 36 %, tensor pipe 28 % (at 20).
 #include <algorithm>
 
 #include "qp_mma.cuh"

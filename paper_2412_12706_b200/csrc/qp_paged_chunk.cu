@@ -24,12 +24,19 @@
 // u is a tile of 128 rows when there are two, else the parity of the token tile, so that one group's exponentials always run beside
 // the other's products.  Every wait is bounded; a block that gives up leaves NaN.
 //
-// Measured: the last 1999 of 16300 tokens, 64 query and 8 KV heads (1.0 TFLOP) 1.07 ms, 0.94 PFLOP/s.  The bound is the chain of a
+// Rounded to fewer than 32 bits, because the products' operands are: queries, and waiting rows, to fp16 times one power of two for a row,
+// or for 32 of them (exact from 2^-17 of the largest on, and what is below 2^-24 of it lost), and weights to fp16, 2^-11 of themselves
+// against the 2^-8 of the output.  The sum takes the weights before that rounding (32 bits; summing them as rounded would take two
+// conversions more for each pair of a loop that bounds the kernel), so a heavy one's rounding stays in the output, an eighth of its own.
+//
+// Measured: the last 1999 of 16300 tokens, 64 query and 8 KV heads (1.0 TFLOP) 1.09 ms, 0.92 PFLOP/s.  The bound is the chain of a
 // tile's softmax (read S, maximum, 256 x 128 exponentials, weights back to tensor memory) with the two hand-overs around it: without
 // the products it took nearly as long (0.97 of 1.12 ms), the exponentials alone would be half of it, expansion and copies wait for
-// free slots, and the GPU is at its power limit.  Few rows leave most of a row tile empty: 16 sequences of 3000 to 4100 tokens with 20
-// rows per KV head are 67 us here, 49 in the form for few rows, with 64 rows 69 us here.  Short items are bound by the chain queries,
-// product, softmax, output of each: 64 chunks of 97 tokens 92 us, 11 us of it an item's fixed cost.
+// free slots, and the GPU is at its power limit.  Prompts from nothing, 32 query and 8 KV heads: 4096 tokens 391 us, 8192 tokens 1.10 ms.
+// Few rows leave most of a row tile empty: 16 sequences of 3000 to 4100 tokens with 20 rows per KV head are 67 us here, 53 in the form for
+// few rows, with 64 rows 69 us here; and a chunk of 512 tokens beside 63 single ones on up to 15000, all of which come here with it, 869
+// us, where the two forms take 212 for the two parts.  Short items are bound by the chain queries, product, softmax, output of each: 64
+// chunks of 97 tokens 85 us, 11 us of it an item's fixed cost.
 #include <algorithm>
 
 #include "qp_mma.cuh"
@@ -471,7 +478,7 @@ chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUte
             sum2 = add2(sum2, sum3);
             float a0, a1;
             unpack2(sum2, a0, a1);
-            l_run = fmaf(a0 + a1, fminf(fv.y * s0, 0x1p90f), l_run);
+            l_run = fmaf(a0 + a1, fminf(fv.y * s0, 0x1p90f), l_run);        // (a scale that is no number: nor are the weights that see it)
             __syncwarp();
             tmem_st(ts + 16 * box, pk);
           }

@@ -2,8 +2,9 @@
 //
 // A pair (u, v) of channels turns by the angle a = pos * w:  u' = m (u cos a - v sin a),  v' = m (v cos a + u sin a).  What counts of
 // pos * w is its fraction of a full turn, so w is held as w / 2 pi in units of 2^-64 and the product taken in 64-bit integers, whose
-// overflow drops the whole turns: exact to 2^-33 of a turn at any 31-bit position, where a 32-bit float angle is off by 0.06 at a
-// million.
+// overflow drops the whole turns: at any 31-bit position it is off by 2^-34 of a turn, from the rounding of w.  The cosine and sine are
+// taken of its upper 32 bits, rounded to multiples of 2^-25 of a turn: off by 2^-26 of a turn, 1e-7 radians, where a 32-bit float angle
+// is off by 0.06 at a million.
 #include <algorithm>
 #include <cfloat>
 
@@ -21,10 +22,11 @@ enum : int { PAIR_NEXT = 0, PAIR_HALF = 1, PAIR_ODD = 2 };
 inline int pairing(const qp_rope& r) { return r.interleaved ? PAIR_NEXT : r.rot_dim % 16 == 0 ? PAIR_HALF : PAIR_ODD; }
 
 // Cosine and sine, times m, of pair `turn` at position pos.  The upper half of the product is the fraction of a turn in units of 2^-32:
-// two bits of quadrant, and the rest as y in [-1/2, 1/2] quarter turns, cut to 24 bits.  sin(y pi/2) / y and cos(y pi/2) are
-// polynomials in y^2, degree 3 and 4, fitted here by linear programming on [0, 1/4] for the least largest error (5e-9 and 3e-10); in 32
-// bits both results are within 9e-8, the cut included within 2^-22.  (sincospif and a conversion to float in
-// its place, with the rows asked for after the table: 8192 tokens x 32 heads x 128 in 28.4 us, against 25.4 then.)
+// two bits of quadrant, and the rest as y in [-1/2, 1/2] quarter turns, rounded to multiples of 2^-23.  sin(y pi/2) / y and cos(y pi/2)
+// are polynomials in y^2, degree 3 and 4, fitted here by linear programming on [0, 1/4] for the least largest error; with coefficients
+// of 32 bits they are off by 5.3e-8 and 3.5e-9.  In 32-bit arithmetic both results are within 9e-8, the rounding of y included within
+// 2^-22.  (sincospif and a conversion to float in its place, with the rows asked for after the table: 8192 tokens x 32 heads x 128 in
+// 28.4 us, against 25.4 then.)
 __device__ __forceinline__ float2 cos_sin(uint64_t turn, int pos, float m) {
   const uint32_t frac = (uint32_t)((turn * (uint64_t)(int64_t)pos) >> 32) + 0x20000000u;
   const uint32_t quarter = frac >> 30;
@@ -108,8 +110,9 @@ __device__ __forceinline__ void rotate_unit(uint4& a, uint4& b, int u, int rot, 
 __device__ __forceinline__ int table_place(int p, int pitch) { return ((p & 6) >> 1) * (pitch >> 2) + (p >> 3) * 2 + (p & 1); }
 
 // ---- rotation alone, and of a step's queries.  HBM-bound: 4 bytes a number.  A block takes up to 32 tokens of all heads, so that
-// the cosines and sines are computed once a token and read from shared memory by every head.  8192 tokens x 32 heads x 128: 19.4 us,
-// 6.9 TB/s (what is written last stays in L2).
+// the cosines and sines are computed once a token and read from shared memory by every head.  8192 tokens x 32 heads x 128: 22.7 us over
+// changing inputs, 5.9 TB/s (19.4 where a graph writes one output over and over, which stays in L2: the figures compared below).
+// Half layout with rot_dim no multiple of 16 (PAIR_ODD) reads its rows again by scalars: 88.8 us with 44 channels.
 // The rows are asked for before the table is made (fill, which ends with the block's barrier), so that the two wait together.
 // n < 2^16 / H tokens; inv_h = ceil(2^32 / H), or 0 for one head.  pitch: pairs of a token in the table.
 template <int MODE, int ROT_UNITS, typename OK, typename FILL>
@@ -362,7 +365,9 @@ __device__ __noinline__ void append_missed(const AppendArgs& a, const qp_rope& r
 // between the search for the largest magnitude and the rounding to codes: page * D / 16 / 128 = UNITS units of 16 channels a thread.
 // At most 64 registers up to 4 units, so that eight blocks are on an SM (64 one-token sequences 5.2 -> 3.9 us when taken, 8192 tokens
 // with 32 query heads 37.8 -> 33.0 us).
-// 8192 tokens with 32 query and 8 KV heads are 33.0 us (185 MB, 5.6 TB/s), one token 2.1 us, mostly launch.
+// 8192 tokens with 32 query and 8 KV heads are 35.3 us over changing inputs (185 MB, 5.2 TB/s; 33.8 where a graph writes one cache over
+// and over), one token 2.1 us, mostly launch.  Pages of 128 tokens with D = 128 take 8 units a thread, 120 to 148 registers and three
+// or four blocks an SM: 51.2 us; PAIR_ODD 138 us with 44 channels.
 // The host does not know the sequences' lengths, so it launches a whole-page block for every `page` rows of the step: unit u belongs
 // to the last sequence b with start[b] / page <= u, which has at least as many of them as pages begin and end in its new tokens.
 // Numbers that do not belong together leave out their own sequence only, see append_missed.
