@@ -1073,7 +1073,7 @@ def paged_layer_step(q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, 
         workspace = new_decode_workspace(need, q.device)
     address, size = _scratch(workspace)
     if need == 0:
-        raise QpError(2, "paged_layer_step")
+        raise QpError(2 if 1 <= step.max_new <= n else 1, "paged_layer_step")
     if size < need:
         raise QpError(4, "paged_layer_step")
     if stride < Hq * D:

@@ -333,3 +333,19 @@ def test_queries_that_lie_over_one_another_are_refused_before_the_append(lib, li
         qp.paged_layer_step(rows(HQ, strides=(stride, D, 1)), rows(HKV), rows(HKV), held(), new_step(), qp.rope(D) if turned else None, None,
                             rows(HQ), Tensor((1 << 26,), torch.uint8))
     assert e.value.status == 1 and not library.calls
+
+
+@pytest.mark.parametrize("n,m,status", [(N, N + 1, 1), (N, 0, 1), (4096, 2, 2)])
+def test_a_refused_layer_step_says_what_the_calls_say(lib, library, n, m, status):
+    """A step whose numbers do not belong together, and one of more work than is numbered in 31 bits."""
+    far = 1 << 24
+    c = held() if status == 1 else qp.paged_cache(64, *(Tensor((PAGES, 8, PAGE, D), torch.float8_e4m3fn) for _ in range(2)),
+                                                 *(Tensor((PAGES, 8)) for _ in range(2)), *(Tensor((2048, 8, PAGE, D)) for _ in range(2)), far)
+    seqs, most = c.table
+    t = qp.PagedStep(Tensor((seqs + 1,), I32), Tensor((seqs,), I32), Tensor((seqs, most), I32), n, m)
+    Hq, Hkv, _ = c.heads
+    ref = ctypes.byref(c.desc), ctypes.byref(t.desc)
+    assert lib.qp_paged_attn(A, Hq * D, *ref, 2 * A, A, BIG, None) == status
+    with pytest.raises(qp.QpError) as e:
+        qp.paged_layer_step(rows(Hq, n), rows(Hkv, n), rows(Hkv, n), c, t, None, None, rows(Hq, n), Tensor((1 << 26,), torch.uint8))
+    assert e.value.status == status and not library.calls
